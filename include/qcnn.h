@@ -633,6 +633,109 @@ qcnn_status qcnn_net_forward_host(const qcnn_layer *layers, int n_layers,
                                   int W, float *y_host, void *workspace,
                                   size_t workspace_bytes, void *stream);
 
+/*
+ * Training of dense layers.  The paper's procedure for a whole network (Sec. 4.2.3)
+ * quantizes the conv layers, fine-tunes the FC layers behind them, which are still
+ * dense, and quantizes those last.  The calls below are the middle step: a dense layer
+ * with its backward pass, softmax cross entropy over the outputs of a last layer with
+ * its gradient, and the orthogonalised update of a weight matrix.
+ *
+ * Matrices are row-major; ld* is the distance between rows in elements (at least the
+ * row's length), so that a part of a larger matrix can be given.  `dtype` is the type
+ * of every matrix of the call (QCNN_F32, QCNN_BF16); bias, its gradient, losses and
+ * their weights are fp32 always.  Arrays are aligned to their element size.  Sizes
+ * are positive, except N, which may be 0 (gradients of weights are then zero); element
+ * counts may pass 2^31.  Outputs must not overlap inputs, with the exceptions named.
+ *
+ * Arithmetic: bf16 operands are multiplied exactly and summed in fp32, each output
+ * rounded to bf16 once.  fp32 operands are taken in three bf16 pieces, which hold all
+ * their 24 bits, and summed in fp32, or (N <= 8) multiplied as they are: results are
+ * as close to the exact ones as those of fp32 multiply-adds.  A non-finite operand (or
+ * one above 3.38e38) makes the outputs that it enters non-finite, NaN where plain
+ * arithmetic would give an infinity.  Sums are in a fixed order: results repeat bit
+ * for bit.
+ *
+ * Workspace: from the query, 256-byte aligned.  `aligned` says that every bf16 matrix
+ * that is an input has a 16-byte aligned base and row distances that are multiples of
+ * 8 (with 0 there is room for copies that have; fp32 calls need none).
+ */
+typedef enum { QCNN_F32 = 0, QCNN_BF16 = 1 } qcnn_dtype;
+typedef enum {
+    QCNN_ACT_NONE = 0,
+    QCNN_ACT_RELU = 1,
+    QCNN_ACT_GELU = 2, /* z Phi(z), by erf                                   */
+    QCNN_ACT_SILU = 3  /* z / (1 + exp(-z))                                  */
+} qcnn_activation;
+
+/*
+ * qcnn_dense_forward -- y = act(z) + residual with z = x W^T + bias.
+ *   x [N][Cs], W [Ct][Cs] (qcnn_pq_quantize's layout), bias [Ct] or NULL,
+ *   residual [N][Ct] or NULL (may be y itself), y [N][Ct], pre [N][Ct] or NULL: z,
+ *   for the backward pass.
+ * qcnn_dense_backward -- of the gradient dy [N][Ct] of y, with dz = dy * act'(z):
+ *   dx [N][Cs] = dz W, dW [Ct][Cs] = dz^T x, dbias [Ct] = sum over rows of dz; each may
+ *   be NULL.  pre: z, or NULL with QCNN_ACT_NONE (of a ReLU without residual y will do).
+ *   The residual's gradient is dy.  x may be NULL without dW, W without dx.
+ *   dz is rounded to bf16 once in bf16 calls, before the two products; dbias sums it
+ *   as it is.
+ */
+qcnn_status qcnn_dense_forward_workspace_size(int N, int Cs, int Ct, int dtype, int aligned,
+                                              size_t *bytes);
+qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, const void *W,
+                               long long ldw, int Ct, const float *bias, int act,
+                               const void *residual, long long ldr, void *y, long long ldy,
+                               void *pre, long long ldp, int dtype, void *workspace,
+                               size_t workspace_bytes, void *stream);
+qcnn_status qcnn_dense_backward_workspace_size(int N, int Cs, int Ct, int dtype, int aligned,
+                                               size_t *bytes);
+qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, long long ldx,
+                                const void *W, long long ldw, const void *pre, long long ldp,
+                                int N, int Cs, int Ct, int act, void *dx, long long lddx, void *dW,
+                                long long lddw, float *dbias, int dtype, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
+ * Softmax cross entropy of a linear layer's outputs l = x W^T + bias over Ct classes,
+ * in pieces of the classes, so that the logits [N][Ct] never exist as a whole where they
+ * would be large:
+ *   lse[n] = log sum_c exp l[n][c],   loss[n] = lse[n] - l[n][target n].
+ *   targets [N] int64.  A row whose target is no class (negative, e.g. -100) has loss 0
+ *   and gradient 0, whatever its x holds (so has one of Ct or above, a caller's error that
+ *   the debug build records); lse is computed for it all the same.
+ *   A bias of -inf takes a class out.  A row without any class left has NaN.
+ * qcnn_xent_grad also gives the gradients of sum_n dloss[n] loss[n]; dloss NULL: of the
+ * mean of the losses over the rows with a class (0 if there are none):
+ *   dx [N][Cs], dW [Ct][Cs], dbias [Ct] (or NULL).
+ * In bf16 calls the gradient of the logits is rounded to bf16 once, before the products
+ * (dbias sums it as it is).
+ */
+qcnn_status qcnn_xent_workspace_size(int N, int Cs, int Ct, int dtype, int aligned, int grad,
+                                     size_t *bytes);
+qcnn_status qcnn_xent_forward(const void *x, long long ldx, int N, int Cs, const void *W,
+                              long long ldw, int Ct, const float *bias, const int64_t *targets,
+                              float *loss, float *lse, int dtype, void *workspace,
+                              size_t workspace_bytes, void *stream);
+qcnn_status qcnn_xent_grad(const void *x, long long ldx, int N, int Cs, const void *W, long long ldw,
+                           int Ct, const float *bias, const int64_t *targets, const float *dloss,
+                           float *loss, float *lse, void *dx, long long lddx, void *dW,
+                           long long lddw, float *dbias, int dtype, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * qcnn_orthogonalize -- the update of a weight matrix with its singular values brought near
+ * 1 by Newton-Schulz products (Jordan et al. 2024, the Muon optimiser):
+ *   X = G / (||G||_F + eps); steps times: A = X X^T, X = a X + (b A + c A A) X
+ *   (X^T X from the right where G has more rows than columns, the same polynomial).
+ *   G [m][n], out [m][n] (may be G itself); coeffs: host array {a, b, c} or NULL for
+ *   {3.4445, -4.7750, 2.0315}; 0 <= steps <= 100; eps >= 0.
+ * Between the products X, A and b A + c A A are kept in two bf16 pieces (16 bits) in bf16
+ * calls, in three (24 bits) in fp32 calls.
+ */
+qcnn_status qcnn_orthogonalize_workspace_size(int m, int n, int dtype, size_t *bytes);
+qcnn_status qcnn_orthogonalize(const void *G, long long ldg, int m, int n, int steps,
+                               const float *coeffs, float eps, void *out, long long ldo, int dtype,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,8 @@ __all__ = ["lut_build", "fc_forward", "conv_forward", "conv_pack_codes", "maxpoo
            "code_bits", "pack_bits", "unpack_bits", "fc_pack_codes", "serialize_model",
            "model_info", "load_model",
            "ConvLayer", "FCLayer", "PoolLayer", "Net", "launch_count", "QcnnError", "load",
-           "set_debug", "debug_checks", "device_check", "smem_load_rate"]
+           "set_debug", "debug_checks", "device_check", "smem_load_rate",
+           "dense_forward", "dense_backward", "xent_forward", "xent_grad", "orthogonalize"]
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -756,3 +757,7 @@ def load_model(blob_or_path, device="cuda", stream=None) -> LoadedNet:
         with open(blob_or_path, "rb") as f:
             blob = f.read()
     return LoadedNet(bytes(blob), device, stream)
+
+
+from .finetune import (dense_backward, dense_forward, orthogonalize, xent_forward,  # noqa: E402
+                       xent_grad)

@@ -10,6 +10,7 @@ import threading
 from . import build as _build
 
 c_int, c_size_t, c_void_p, c_uint64 = ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_uint64
+c_int64 = ctypes.c_int64
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_DATA = 0, 1, 2, 3, 4, 5
 ERR_DEVICE_CHECK = 6
@@ -19,6 +20,8 @@ ALGO_FUSED_VARIANT = 256  # + v: fused tile variant v
 ALGO_NO_CLUSTER = 1 << 16  # flag: no thread-block clusters for split sub-spaces
 CODES_CANONICAL, CODES_PACKED = 0, 1
 LUT = {"fp32": 0, "bf16": 1}
+F32, BF16 = 0, 1  # qcnn_dtype
+ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 LAYER_CONV, LAYER_FC, LAYER_MAXPOOL = 0, 1, 2
 
 
@@ -109,6 +112,24 @@ _SIGS = {
     "qcnn_ec_quantize_fc": (c_int, [c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int,
                                     c_void_p, c_void_p, c_int, c_int, c_void_p, c_size_t,
                                     c_void_p]),
+    "qcnn_dense_forward_workspace_size": (c_int, [c_int] * 5 + [ctypes.POINTER(c_size_t)]),
+    "qcnn_dense_forward": (c_int, [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int,
+                                   c_void_p, c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                   c_int64, c_int, c_void_p, c_size_t, c_void_p]),
+    "qcnn_dense_backward_workspace_size": (c_int, [c_int] * 5 + [ctypes.POINTER(c_size_t)]),
+    "qcnn_dense_backward": (c_int, [c_void_p, c_int64] * 4 + [c_int] * 4 +
+                            [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p,
+                             c_size_t, c_void_p]),
+    "qcnn_xent_workspace_size": (c_int, [c_int] * 6 + [ctypes.POINTER(c_size_t)]),
+    "qcnn_xent_forward": (c_int, [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int,
+                                  c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_size_t,
+                                  c_void_p]),
+    "qcnn_xent_grad": (c_int, [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int, c_void_p,
+                               c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p,
+                               c_int64, c_void_p, c_int, c_void_p, c_size_t, c_void_p]),
+    "qcnn_orthogonalize_workspace_size": (c_int, [c_int] * 3 + [ctypes.POINTER(c_size_t)]),
+    "qcnn_orthogonalize": (c_int, [c_void_p, c_int64, c_int, c_int, c_int, c_void_p, ctypes.c_float,
+                                   c_void_p, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
     "qcnn_pq_quantize": (c_int, [c_int, c_void_p, c_int, c_int, c_int, c_int, c_int, c_int,
                                  c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_size_t,
                                  c_void_p]),

@@ -1,0 +1,507 @@
+// dense.cu -- qcnn_dense_forward and qcnn_dense_backward: a dense layer with its epilogue,
+// and its gradients.
+//
+//   z = x W^T + b, y = act(z) + r;   dz = dy * act'(z), dx = dz W, dW = dz^T x, db = sum dz
+//
+// Each product is gemm.cuh's, with the layer's outputs (dx, dW: its inputs) as the
+// contiguous index m.  Three ways, by the estimated time of each:
+//   few rows (forward, N <= 8): no tensor cores; the weights are streamed once through
+//     fp32 multiply-adds, which then take less than the memory does;
+//   fp32 operands split on their way to shared memory: no pass over the operands, so it
+//     has the products that their bytes bound;
+//   planes in the workspace (fp32), or the bf16 operands themselves: the rest.
+#include "train.cuh"
+
+#include <algorithm>
+
+namespace qcnn {
+namespace {
+
+// ------------------------------------------------------------- few rows
+// A warp sums kFewOut outputs x NB rows over its part of the inputs: lanes take
+// neighbouring 16 bytes (VEC) or elements.  kw warps share an output's inputs and add up
+// through shared memory; 8 / kw groups of kFewOut outputs per CTA.  The rows x are
+// read from L1/L2 once per kFewOut weights rows.
+constexpr int kFewOut = 4;
+
+template <typename T>
+__device__ __forceinline__ float as_float(T v) {
+    if constexpr (sizeof(T) == 4) return v;
+    else return bf16_to_float(v);
+}
+// V neighbouring elements (16 bytes)
+template <typename T, int V>
+__device__ __forceinline__ void load_vec(const T *p, float (&v)[V]) {
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = *reinterpret_cast<const float4 *>(p);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    } else {
+        const uint4 a = *reinterpret_cast<const uint4 *>(p);
+        const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = __uint_as_float(w[j] << 16);
+            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+    }
+}
+
+template <typename T, int NB, bool VEC>
+__global__ void __launch_bounds__(256) few_rows_kernel(FewRows f, int kw) {
+    constexpr int V = VEC ? 16 / (int)sizeof(T) : 4;
+    __shared__ float red[8][kFewOut * NB];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = warp / kw, part = warp - group * kw;
+    const int c0 = (blockIdx.x * (8 / kw) + group) * kFewOut;
+    grid_dep_sync();
+    const T *x = static_cast<const T *>(f.x), *w = static_cast<const T *>(f.W);
+    float acc[kFewOut][NB] = {};
+    const T *wr[kFewOut];
+#pragma unroll
+    for (int i = 0; i < kFewOut; ++i) wr[i] = w + (long long)min(c0 + i, f.Ct - 1) * f.ldw;
+    const T *xr[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) xr[n] = x + (long long)min(n, f.N - 1) * f.ldx;
+    const int step = kw * 32 * V;
+    // (VEC: Cs is a multiple of V)
+    if constexpr (VEC) {
+#pragma unroll 2
+        for (int k = (part * 32 + lane) * V; k < f.Cs; k += step) {
+            float wv[kFewOut][V];
+#pragma unroll
+            for (int i = 0; i < kFewOut; ++i) load_vec<T, V>(wr[i] + k, wv[i]);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                float xv[V];
+                load_vec<T, V>(xr[n] + k, xv);
+#pragma unroll
+                for (int i = 0; i < kFewOut; ++i)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[i][n] = fmaf(wv[i][j], xv[j], acc[i][n]);
+            }
+        }
+    } else {
+        for (int k0 = part * 32 * V + lane; k0 < f.Cs; k0 += step) {
+            float wv[kFewOut][V];
+#pragma unroll
+            for (int i = 0; i < kFewOut; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) wv[i][j] = k0 + j * 32 < f.Cs ? as_float<T>(wr[i][k0 + j * 32]) : 0.f;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float xv = k0 + j * 32 < f.Cs ? as_float<T>(xr[n][k0 + j * 32]) : 0.f;
+#pragma unroll
+                    for (int i = 0; i < kFewOut; ++i) acc[i][n] = fmaf(wv[i][j], xv, acc[i][n]);
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kFewOut; ++i)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            float v = acc[i][n];
+#pragma unroll
+            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (lane == 0) red[warp][i * NB + n] = v;
+        }
+    __syncthreads();
+    // one thread per output of the CTA
+    const int per = kFewOut * NB, t = threadIdx.x;
+    if (t >= (8 / kw) * per) return;
+    const int g = t / per, o = t - g * per;
+    // (neighbouring threads: neighbouring outputs of a row)
+    const int i = o % kFewOut, n = o / kFewOut;
+    const int m = (blockIdx.x * (8 / kw) + g) * kFewOut + i;
+    if (m >= f.Ct || n >= f.N) return;
+    float v = 0.f;
+    for (int p = 0; p < kw; ++p) v += red[g * kw + p][i * NB + n];
+    const GemmEpi &e = f.e;
+    if (e.bias) v += e.bias[m];
+    auto put = [&](void *p, long long ld, float r) {
+        if (e.out_type == GEMM_T_F32) static_cast<float *>(p)[(long long)n * ld + m] = r;
+        else static_cast<unsigned short *>(p)[(long long)n * ld + m] = float_to_bf16(r);
+    };
+    if (e.pre) put(e.pre, e.ldp, v);
+    v = act_apply(v, e.act);
+    if (e.add) v += load_as(e.add, e.add_type, (long long)n * e.lda + m, 0);
+    put(e.out, e.ldo, v);
+}
+
+template <typename T, bool VEC>
+qcnn_status few_rows_of(const FewRows &f, cudaStream_t st) {
+    constexpr int V = VEC ? 16 / (int)sizeof(T) : 4;
+    // as many warps to an output as have inputs, and fewer where outputs alone fill the SMs
+    int kw = 8;
+    while (kw > 1 && (f.Cs <= kw / 2 * 32 * V || cdiv(f.Ct, kFewOut * 8 / (kw / 2)) >= num_sms() * 4)) kw /= 2;
+    const dim3 grid(cdiv(f.Ct, kFewOut * 8 / kw));
+    if (f.N == 1) return launch_pdl(few_rows_kernel<T, 1, VEC>, grid, dim3(256), 0, st, f, kw);
+    if (f.N == 2) return launch_pdl(few_rows_kernel<T, 2, VEC>, grid, dim3(256), 0, st, f, kw);
+    if (f.N <= 4) return launch_pdl(few_rows_kernel<T, 4, VEC>, grid, dim3(256), 0, st, f, kw);
+    return launch_pdl(few_rows_kernel<T, 8, VEC>, grid, dim3(256), 0, st, f, kw);
+}
+
+// ------------------------------------------------- gradient of z, bias
+// dz = dy * act'(z) in `out_type` (none: only sums) and sums over a slab of rows:
+// part[slab][cols].  A CTA takes 128 columns x a slab: a warp a row, a lane four
+// columns.
+template <typename T>
+__global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, const T *pre, long long ldp,
+                                                 int N, int Ct, int act, void *out, int out_type,
+                                                 long long ldo, long long plane, float *part, int slab,
+                                                 int vec) {
+    __shared__ float red[8][128];
+    grid_dep_sync();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = blockIdx.x * 128 + lane * 4;
+    const int r1 = min(N, ((int)blockIdx.y + 1) * slab);
+    float sum[4] = {};
+    auto load4 = [&](const T *p, float (&v)[4]) {
+        if (vec && c + 4 <= Ct) {
+            if constexpr (sizeof(T) == 4) {
+                const float4 a = *reinterpret_cast<const float4 *>(p);
+                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+            } else {
+                const uint2 a = *reinterpret_cast<const uint2 *>(p);
+                v[0] = __uint_as_float(a.x << 16), v[1] = __uint_as_float(a.x & 0xffff0000u);
+                v[2] = __uint_as_float(a.y << 16), v[3] = __uint_as_float(a.y & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = c + j < Ct ? as_float<T>(p[j]) : 0.f;
+        }
+    };
+    if (c < Ct) {
+#pragma unroll 2
+        for (int r = (int)blockIdx.y * slab + warp; r < r1; r += 8) {
+            float v[4];
+            load4(dy + (long long)r * lddy + c, v);
+            if (act != QCNN_ACT_NONE) {
+                float z[4];
+                load4(pre + (long long)r * ldp + c, z);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] *= act_slope(z[j], act);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += v[j];
+            if (out) {  // (its rows are ours: multiples of 8 elements, 16-byte aligned)
+                const long long o = (long long)r * ldo + c;
+                if (out_type == GEMM_T_F32) {
+                    *reinterpret_cast<float4 *>(static_cast<float *>(out) + o) =
+                        make_float4(v[0], v[1], v[2], v[3]);
+                } else {
+                    unsigned w[3][2];
+                    unsigned short *d = static_cast<unsigned short *>(out) + o;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+                    *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
+                    if (out_type == GEMM_T_PLANES3) {
+                        *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
+                        *reinterpret_cast<uint2 *>(d + 2 * plane) = make_uint2(w[2][0], w[2][1]);
+                    }
+                }
+            }
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) red[warp][lane * 4 + j] = sum[j];
+    __syncthreads();
+    const int t = threadIdx.x, col = blockIdx.x * 128 + t;
+    if (t < 128 && col < Ct) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += red[w][t];
+        part[(long long)blockIdx.y * Ct + col] = v;
+    }
+}
+
+__global__ void __launch_bounds__(256) column_join_kernel(const float *part, int rows, long long ld, int cols,
+                                                          const float *scale, float *dst) {
+    grid_dep_sync();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c < cols) dst[c] = add_groups<true>(part + c, rows, ld) * (scale ? *scale : 1.f);
+}
+
+// Rows per CTA of dz_kernel: enough CTAs to fill the SMs twice, 32 rows at least.
+int dz_slab(int N, int Ct) {
+    const int want = std::max(1, 4 * num_sms() / cdiv(Ct, 128));
+    return std::max(32, cdiv(cdiv(N, want), 8) * 8);
+}
+
+// ---------------------------------------------------------------- plans
+// Forward (fp32): the operands as they are, or planes.
+struct ForwardPlan {
+    bool few = false, planes = false;  // planes: copies of x and W in the workspace
+    Product g;
+};
+ForwardPlan plan_forward(int N, int Cs, int Ct, int dtype, bool aligned) {
+    ForwardPlan p;
+    if (N <= kFewRows) {
+        p.few = true;
+    } else if (dtype == QCNN_BF16) {
+        p.planes = !aligned;
+        p.g.plan = plan_gemm(1, GEMM_OUT, Ct, N, Cs, 64);
+    } else {
+        p.g.plan = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, 64);
+        const GemmPlan q = plan_gemm(3, GEMM_OUT, Ct, N, Cs, 64);
+        const double more = pass_clocks(((double)N + Ct) * Cs * 16.0);
+        if (q.score + more < p.g.plan.score) {
+            p.planes = true;
+            p.g.plan = q;
+        }
+    }
+    return p;
+}
+struct ForwardSpace {
+    unsigned short *x = nullptr, *w = nullptr;
+    void *partial = nullptr;
+    size_t bytes = 0;
+};
+// copies of x / W where the plan has them; bf16: of each that is not aligned
+ForwardSpace carve_forward(const ForwardPlan &p, int N, int Cs, int Ct, int dtype, bool x_copy, bool w_copy,
+                           void *ws) {
+    Carver c{static_cast<uint8_t *>(ws)};
+    ForwardSpace s;
+    const int P = dtype == QCNN_F32 ? 3 : 1;
+    if (p.planes && x_copy) s.x = c.array<unsigned short>((size_t)P * N * pad8(Cs));
+    if (p.planes && w_copy) s.w = c.array<unsigned short>((size_t)P * Ct * pad8(Cs));
+    s.partial = c.take(p.g.scratch());
+    s.bytes = c.used;
+    return s;
+}
+
+struct BackwardPlan {
+    bool planes = false;  // fp32: dz, x and W in planes; bf16: copies of what is not aligned
+    bool dz_copy = false;
+    int dz_type = GEMM_T_F32, slab = 0, slabs = 1;
+    Product gx, gw;
+};
+BackwardPlan plan_backward(int N, int Cs, int Ct, int dtype) {
+    BackwardPlan p;
+    p.slab = dz_slab(N, Ct);
+    p.slabs = cdiv(N, p.slab);
+    if (dtype == QCNN_BF16) {
+        p.dz_type = GEMM_T_BF16;
+        p.gx.plan = plan_gemm(1, GEMM_OUT, Cs, N, Ct, 64);
+        p.gw.plan = plan_gemm(1, GEMM_OUT, Cs, Ct, N, 64);
+        return p;
+    }
+    p.gx.plan = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
+    p.gw.plan = plan_gemm(GEMM_F32, GEMM_OUT, Cs, Ct, N, 64);
+    const GemmPlan qx = plan_gemm(3, GEMM_OUT, Cs, N, Ct, 64), qw = plan_gemm(3, GEMM_OUT, Cs, Ct, N, 64);
+    const double more = pass_clocks(((double)N + Ct) * Cs * 16.0 + (double)N * Ct * 4.0);
+    if (qx.score + qw.score + more < p.gx.plan.score + p.gw.plan.score) {
+        p.planes = true;
+        p.dz_type = GEMM_T_PLANES3;
+        p.gx.plan = qx;
+        p.gw.plan = qw;
+    }
+    return p;
+}
+struct BackwardSpace {
+    void *dz = nullptr;
+    unsigned short *x = nullptr, *w = nullptr;
+    float *db = nullptr;
+    void *partial = nullptr;
+    size_t bytes = 0;
+};
+BackwardSpace carve_backward(const BackwardPlan &p, int N, int Cs, int Ct, int dtype, bool dz, bool x_copy,
+                             bool w_copy, void *ws) {
+    Carver c{static_cast<uint8_t *>(ws)};
+    BackwardSpace s;
+    const size_t P = p.planes ? 3 : 1;
+    if (dz) s.dz = c.take(P * N * pad8(Ct) * (p.dz_type == GEMM_T_F32 ? 4 : 2));
+    if (x_copy) s.x = c.array<unsigned short>(P * N * pad8(Cs));
+    if (w_copy) s.w = c.array<unsigned short>(P * Ct * pad8(Cs));
+    if (p.slabs > 1) s.db = c.array<float>((size_t)p.slabs * Ct);
+    s.partial = c.take(std::max(p.gx.scratch(), p.gw.scratch()));
+    s.bytes = c.used;
+    return s;
+}
+
+}  // namespace
+
+qcnn_status launch_few_rows(const FewRows &f, cudaStream_t st) {
+    const int v = f.bf16 ? 8 : 4;
+    const bool vec = reinterpret_cast<uintptr_t>(f.x) % 16 == 0 && reinterpret_cast<uintptr_t>(f.W) % 16 == 0 &&
+                     f.ldx % v == 0 && f.ldw % v == 0 && f.Cs % v == 0;
+    if (f.bf16) return vec ? few_rows_of<unsigned short, true>(f, st) : few_rows_of<unsigned short, false>(f, st);
+    return vec ? few_rows_of<float, true>(f, st) : few_rows_of<float, false>(f, st);
+}
+
+qcnn_status launch_column_join(const float *part, int rows, long long ld, int cols, const float *scale,
+                               float *dst, cudaStream_t st) {
+    return launch_pdl(column_join_kernel, dim3(cdiv(cols, 256)), dim3(256), 0, st, part, rows, ld, cols, scale, dst);
+}
+
+}  // namespace qcnn
+
+using namespace qcnn;
+
+extern "C" {
+
+qcnn_status qcnn_dense_forward_workspace_size(int N, int Cs, int Ct, int dtype, int aligned,
+                                              size_t *bytes) {
+    if (!bytes || N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
+    *bytes = N ? carve_forward(plan_forward(N, Cs, Ct, dtype, aligned != 0), N, Cs, Ct, dtype, true, true,
+                               nullptr).bytes
+               : 0;
+    return QCNN_OK;
+}
+
+qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, const void *W, long long ldw,
+                               int Ct, const float *bias, int act, const void *residual, long long ldr,
+                               void *y, long long ldy, void *pre, long long ldp, int dtype,
+                               void *workspace, size_t workspace_bytes, void *stream) {
+    if (N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype) || act < QCNN_ACT_NONE || act > QCNN_ACT_SILU)
+        return QCNN_ERR_INVALID_ARG;
+    if (!matrix_ok(x, ldx, N, Cs, dtype) || !matrix_ok(W, ldw, Ct, Cs, dtype) ||
+        !matrix_ok(y, ldy, N, Ct, dtype) || (residual && !matrix_ok(residual, ldr, N, Ct, dtype)) ||
+        (pre && !matrix_ok(pre, ldp, N, Ct, dtype)) || reinterpret_cast<uintptr_t>(bias) % 4)
+        return QCNN_ERR_INVALID_ARG;
+    if (N == 0) return QCNN_OK;
+    const bool bf16 = dtype == QCNN_BF16;
+    const bool xa = tma_ok(x, ldx), wa = tma_ok(W, ldw);
+    const ForwardPlan p = plan_forward(N, Cs, Ct, dtype, xa && wa);
+    const ForwardSpace s = carve_forward(p, N, Cs, Ct, dtype, !bf16 || !xa, !bf16 || !wa, workspace);
+    qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
+    if (rc != QCNN_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    PdlScope pdl;
+    GemmProblem g;
+    const int type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
+    g.e.bias = bias;
+    g.e.act = act;
+    g.e.beta = 1.f;
+    g.e.add = residual;
+    g.e.lda = ldr;
+    g.e.add_type = type;
+    g.e.out = y;
+    g.e.ldo = ldy;
+    g.e.out_type = type;
+    g.e.pre = pre;
+    g.e.ldp = ldp;
+    if (p.few) return launch_few_rows(FewRows{x, W, ldx, ldw, N, Cs, Ct, bf16, g.e}, st);
+    g.m = Ct;
+    g.n = N;
+    g.k = Cs;
+    g.a = GemmOperand{W, ldw, 0, 0};
+    g.b = GemmOperand{x, ldx, 0, 0};
+    const int P = bf16 ? 1 : 3;
+    const long long pitch = pad8(Cs);
+    if (s.x) {
+        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, N * pitch, nullptr, 0, st);
+        if (rc != QCNN_OK) return rc;
+        g.b = GemmOperand{s.x, pitch, N * pitch, 0};
+    }
+    if (s.w) {
+        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, Ct * pitch, nullptr, 0, st);
+        if (rc != QCNN_OK) return rc;
+        g.a = GemmOperand{s.w, pitch, Ct * pitch, 0};
+    }
+    return p.g.run(g, s.partial, st);
+}
+
+qcnn_status qcnn_dense_backward_workspace_size(int N, int Cs, int Ct, int dtype, int aligned,
+                                               size_t *bytes) {
+    if (!bytes || N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
+    const BackwardPlan p = plan_backward(N, Cs, Ct, dtype);
+    const bool copy = dtype == QCNN_F32 ? p.planes : !aligned;
+    *bytes = N ? carve_backward(p, N, Cs, Ct, dtype, true, copy, copy, nullptr).bytes : 0;
+    return QCNN_OK;
+}
+
+qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, long long ldx, const void *W,
+                                long long ldw, const void *pre, long long ldp, int N, int Cs, int Ct,
+                                int act, void *dx, long long lddx, void *dW, long long lddw,
+                                float *dbias, int dtype, void *workspace, size_t workspace_bytes,
+                                void *stream) {
+    if (N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype) || act < QCNN_ACT_NONE || act > QCNN_ACT_SILU)
+        return QCNN_ERR_INVALID_ARG;
+    if (!matrix_ok(dy, lddy, N, Ct, dtype) || (dW && !matrix_ok(x, ldx, N, Cs, dtype)) ||
+        (dx && !matrix_ok(W, ldw, Ct, Cs, dtype)) ||
+        (act != QCNN_ACT_NONE && !matrix_ok(pre, ldp, N, Ct, dtype)) ||
+        (dx && !matrix_ok(dx, lddx, N, Cs, dtype)) || (dW && !matrix_ok(dW, lddw, Ct, Cs, dtype)) ||
+        reinterpret_cast<uintptr_t>(dbias) % 4)
+        return QCNN_ERR_INVALID_ARG;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool bf16 = dtype == QCNN_BF16;
+    if (N == 0) {  // sums of nothing
+        cudaError_t e = cudaSuccess;
+        if (dW) e = cudaMemset2DAsync(dW, lddw * type_bytes(dtype), 0, Cs * type_bytes(dtype), Ct, st);
+        if (dbias && e == cudaSuccess) e = cudaMemsetAsync(dbias, 0, (size_t)Ct * 4, st);
+        return cuda_status(e);
+    }
+    const BackwardPlan p = plan_backward(N, Cs, Ct, dtype);
+    // dy itself where it is dz in a form that the products read
+    const bool products = dx || dW;
+    const bool dz = products && (act != QCNN_ACT_NONE || p.planes || (bf16 && !tma_ok(dy, lddy)));
+    const bool x_copy = dW && (bf16 ? !tma_ok(x, ldx) : p.planes);
+    const bool w_copy = dx && (bf16 ? !tma_ok(W, ldw) : p.planes);
+    const BackwardSpace s = carve_backward(p, N, Cs, Ct, dtype, dz, x_copy, w_copy, workspace);
+    qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
+    if (rc != QCNN_OK) return rc;
+    PdlScope pdl;
+    const long long pz = pad8(Ct), pc = pad8(Cs);
+    const int P = bf16 ? 1 : 3;
+    GemmOperand z{dy, lddy, 0, 0}, xo{x, ldx, 0, 1}, wo{W, ldw, 0, 1};
+    if (dz || dbias) {
+        const dim3 grid(cdiv(Ct, 128), p.slabs);
+        float *const part = !dbias ? nullptr : p.slabs > 1 ? s.db : dbias;
+        const int e = bf16 ? 2 : 4;
+        const auto vec_ok = [&](const void *q, long long ld) {
+            return reinterpret_cast<uintptr_t>(q) % (4 * e) == 0 && ld % 4 == 0;
+        };
+        const int vec = vec_ok(dy, lddy) && (act == QCNN_ACT_NONE || vec_ok(pre, ldp));
+        if (bf16)
+            rc = launch_pdl(dz_kernel<unsigned short>, grid, dim3(256), 0, st,
+                            static_cast<const unsigned short *>(dy), lddy,
+                            static_cast<const unsigned short *>(pre), ldp, N, Ct, act, s.dz, p.dz_type, pz,
+                            (long long)N * pz, part, p.slab, vec);
+        else
+            rc = launch_pdl(dz_kernel<float>, grid, dim3(256), 0, st, static_cast<const float *>(dy), lddy,
+                            static_cast<const float *>(pre), ldp, N, Ct, act, s.dz, p.dz_type, pz,
+                            (long long)N * pz, part, p.slab, vec);
+        if (rc != QCNN_OK) return rc;
+        if (dbias && p.slabs > 1 && (rc = launch_column_join(s.db, p.slabs, Ct, Ct, nullptr, dbias, st)) != QCNN_OK)
+            return rc;
+        if (dz) z = GemmOperand{s.dz, pz, (long long)N * pz, 0};
+    }
+    if (x_copy) {
+        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, N * pc, nullptr, 0, st);
+        if (rc != QCNN_OK) return rc;
+        xo = GemmOperand{s.x, pc, N * pc, 1};
+    }
+    if (w_copy) {
+        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, Ct * pc, nullptr, 0, st);
+        if (rc != QCNN_OK) return rc;
+        wo = GemmOperand{s.w, pc, Ct * pc, 1};
+    }
+    GemmProblem g;
+    g.e.out_type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
+    g.m = Cs;
+    if (dx) {
+        g.a = wo;
+        g.b = z;
+        g.n = N;
+        g.k = Ct;
+        g.e.out = dx;
+        g.e.ldo = lddx;
+        if ((rc = p.gx.run(g, s.partial, st)) != QCNN_OK) return rc;
+    }
+    if (dW) {
+        g.a = xo;
+        g.b = z;
+        g.b.mn = 1;
+        g.n = Ct;
+        g.k = N;
+        g.e.out = dW;
+        g.e.ldo = lddw;
+        if ((rc = p.gw.run(g, s.partial, st)) != QCNN_OK) return rc;
+    }
+    return QCNN_OK;
+}
+
+}  // extern "C"

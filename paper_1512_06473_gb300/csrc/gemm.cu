@@ -1,0 +1,315 @@
+// gemm.cu -- plans and launches of the tensor-core products (gemm.cuh), the join of
+// split ones, and the pass that lays fp32 or unaligned data out as planes.
+#include "gemm_kernel.cuh"
+
+#include <algorithm>
+#include <array>
+#include <map>
+#include <mutex>
+
+namespace qcnn {
+
+// (gemm_p1.cu, gemm_p2.cu, gemm_p3.cu, gemm_f32.cu)
+using GemmLaunch = qcnn_status (*)(const void *, int, size_t, cudaStream_t);
+GemmLaunch gemm_launch_p1(int kind, int cg);
+GemmLaunch gemm_launch_p2(int kind, int cg);
+GemmLaunch gemm_launch_p3(int kind, int cg);
+GemmLaunch gemm_launch_p3_sym(int cg);
+GemmLaunch gemm_launch_f32();
+
+namespace {
+
+constexpr size_t kSmemMax = 225 * 1024;  // dynamic, with 1 KB to align the stages
+// one CTA per SM, whatever it needs: all tensor memory is taken
+constexpr size_t kSmemLeast = 120 * 1024;
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                                 const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static EncodeTiled f = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                             &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            f = reinterpret_cast<EncodeTiled>(p);
+        cudaGetLastError();
+    });
+    return f;
+}
+
+int block_k(int planes) { return planes == 1 ? 64 : 32; }
+int real_planes(int planes) { return planes == GEMM_F32 ? 3 : planes; }
+
+unsigned operand_bytes(int P, int mn, int rows) {
+    const unsigned bk = block_k(P);
+    return mn ? (unsigned)cdiv(rows, 64) * P * bk * 128 : (unsigned)P * rows * bk * 2;
+}
+
+// An operand of `rows` rows (this CTA's part of a tile); rows_all x k is its matrix.
+qcnn_status set_operand(const GemmOperand &o, int planes, int rows, int rows_all, int k, OpArgs *a,
+                        CUtensorMap *map) {
+    const int P = real_planes(planes), bk = block_k(P);
+    a->mn = o.mn;
+    a->bytes = operand_bytes(P, o.mn, rows);
+    a->group_bytes = P * bk * 128;
+    a->plane = o.mn ? bk * 128 / 16 : rows * bk * 2 / 16;
+    a->kstep = o.mn ? 2048 / 16 : 32 / 16;
+    const bool sw64 = !o.mn && bk == 32;
+    const uint64_t sbo = sw64 ? 512 : 1024, lbo = o.mn ? a->group_bytes : 16;
+    a->desc = (lbo >> 4) << 16 | (sbo >> 4) << 32 | 1ull << 46 | (uint64_t)(sw64 ? 4 : 2) << 61;
+    a->src = static_cast<const float *>(o.p);
+    a->ld = o.ld;
+    a->rows = rows_all;
+    a->vec = reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.ld % 4 == 0;
+    if (planes == GEMM_F32) return QCNN_OK;
+    const EncodeTiled enc = encode_tiled();
+    if (!enc) return QCNN_ERR_CUDA;
+    const cuuint64_t inner = o.mn ? rows_all : k, outer = o.mn ? k : rows_all;
+    const cuuint64_t dims[3] = {inner, outer, (cuuint64_t)P};
+    const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(P > 1 ? o.plane : o.ld * outer) * 2};
+    const cuuint32_t box[3] = {o.mn ? 64u : (cuuint32_t)bk, o.mn ? (cuuint32_t)bk : (cuuint32_t)rows,
+                               (cuuint32_t)P};
+    const cuuint32_t steps[3] = {1, 1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(o.p), dims, strides,
+                           box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           sw64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return cuda_status(cudaErrorInvalidValue);
+    return QCNN_OK;
+}
+
+GemmLaunch launcher(const GemmPlan &p) {
+    switch (p.planes) {
+        case 1: return gemm_launch_p1(p.kind, p.cg);
+        case 2: return gemm_launch_p2(p.kind, p.cg);
+        case 3: return p.kind == GEMM_SYM ? gemm_launch_p3_sym(p.cg) : gemm_launch_p3(p.kind, p.cg);
+        default: return gemm_launch_f32();
+    }
+}
+
+// ----------------------------------------------------------------- join
+// A thread per output; neighbours along m.
+__global__ void __launch_bounds__(256) gemm_join_kernel(GemmEpi e, int m_all, int n_all, int splits) {
+    grid_dep_sync();
+    const int m = blockIdx.x * 256 + threadIdx.x;
+    if (m >= m_all) return;
+    const float bias = e.bias ? e.bias[m] : 0.f, alpha = e.alpha_ptr ? *e.alpha_ptr : e.alpha;
+    const size_t stride = (size_t)m_all * n_all;
+    for (int n = blockIdx.y; n < n_all; n += gridDim.y) {
+        float v = add_groups<true>(e.partial + (size_t)n * m_all + m, splits, stride);
+        v = fmaf(alpha, v, bias);
+        const long long o = (long long)n * e.ldo + m;
+        if (e.pre) {
+            const long long q = (long long)n * e.ldp + m;
+            if (e.out_type == GEMM_T_F32) static_cast<float *>(e.pre)[q] = v;
+            else static_cast<unsigned short *>(e.pre)[q] = float_to_bf16(v);
+        }
+        v = act_apply(v, e.act);
+        if (e.add) v = fmaf(e.beta, load_as(e.add, e.add_type, (long long)n * e.lda + m, e.add_plane), v);
+        if (e.out_type == GEMM_T_F32) {
+            static_cast<float *>(e.out)[o] = v;
+        } else {
+            unsigned w[3] = {};
+            if (e.out_type == GEMM_T_BF16) w[0] = pack_bf16x2(v, 0.f);
+            else if (e.out_type == GEMM_T_PLANES2) planes2(v, 0.f, w[0], w[1]);
+            else planes3(v, 0.f, w[0], w[1], w[2]);
+            unsigned short *p = static_cast<unsigned short *>(e.out) + o;
+            p[0] = (unsigned short)w[0];
+            if (e.out_type >= GEMM_T_PLANES2) p[e.out_plane] = (unsigned short)w[1];
+            if (e.out_type == GEMM_T_PLANES3) p[2 * e.out_plane] = (unsigned short)w[2];
+        }
+    }
+}
+
+// --------------------------------------------------------------- planes
+// A thread per eight columns: two 16-byte loads (or eight of an element), a 16-byte
+// store per plane.
+template <typename T>
+__global__ void __launch_bounds__(256) planes_kernel(const T *src, long long rows, int cols, long long ld,
+                                                     int planes, unsigned short *dst, long long plane,
+                                                     const long long *keep, int classes, int vec) {
+    grid_dep_sync();
+    const int c8 = (cols + 7) / 8;
+    const long long pitch = (long long)c8 * 8, all = rows * c8;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        const long long r = i / c8;
+        const int c = (int)(i - r * c8) * 8;
+        float v[8] = {};
+        const bool in = !keep || (unsigned long long)keep[r] < (unsigned long long)classes;
+        const T *s = src + r * ld + c;
+        if (in && vec && c + 8 <= cols) {
+            if constexpr (sizeof(T) == 4) {
+                const float4 a = *reinterpret_cast<const float4 *>(s), b = *reinterpret_cast<const float4 *>(s + 4);
+                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+            } else {
+                const uint4 a = *reinterpret_cast<const uint4 *>(s);
+                const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[2 * j] = __uint_as_float(w[j] << 16);
+                    v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                }
+            }
+        } else if (in) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j < cols) {
+                    if constexpr (sizeof(T) == 4) v[j] = s[j];
+                    else v[j] = bf16_to_float(s[j]);
+                }
+        }
+        unsigned w[3][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (planes == 3) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+            else if (planes == 2) planes2(v[2 * j], v[2 * j + 1], w[0][j], w[1][j]);
+            else w[0][j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+            if (p < planes)
+                *reinterpret_cast<uint4 *>(dst + p * plane + r * pitch + c) =
+                    make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+    }
+}
+
+}  // namespace
+
+static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int max_splits, int sms) {
+    GemmPlan best;
+    const int P = real_planes(planes), bk = block_k(P), kblocks = std::max(1, cdiv(k, bk));
+    static const int tiles[6] = {16, 32, 64, 128, 192, 256};
+    const int mmas = P == 1 ? 4 : P == 2 ? 6 : 12;
+    for (int cg = 1; cg <= (planes == GEMM_F32 ? 1 : 2); ++cg) {
+        for (int bn : tiles) {
+            if (planes == GEMM_F32 && bn > 128) continue;
+            if (cg == 2 && bn != 256) continue;
+            if (kind == GEMM_SYM && bn % (kMT * cg)) continue;
+            if (bn > 16 && kind != GEMM_SYM && bn >= 2 * n) continue;
+            const int mt = cdiv(m, kMT * cg), nt = cdiv(n, bn), slots = sms / cg;
+            long long units = (long long)mt * nt;
+            if (kind == GEMM_SYM) {
+                units = 0;
+                for (int i = 0; i < nt; ++i) units += std::max(0, mt - i * (bn / (kMT * cg)));
+            }
+            const double mma = mmas * (bn / 2 + 10.0);
+            const double bytes = (double)P * (kMT + bn / cg) * bk * 2;
+            double per = std::max(mma, bytes / 48.0);
+            if (planes == GEMM_F32) per = std::max({mma, (kMT + bn) * 4.0, (kMT + bn) * 128.0 / 23.0});
+            if (P == 3) per = std::max(per, 2.5 * bn + 100.0);
+            const double tail = 2500.0 + bn * (kind == GEMM_OUT ? 8.0 : 14.0);
+            for (int sp = 1; sp <= std::min({max_splits, kblocks, 64}); ++sp) {
+                const int kps = cdiv(kblocks, sp);
+                if (cdiv(kblocks, kps) != sp) continue;
+                if (sp > 1 && units * sp > 4 * slots) break;
+                const double waves = (double)((units * sp + slots - 1) / slots);
+                const double join = sp > 1 ? 4000.0 + 2.0 * sp * m * (double)n * 4.0 / 3500.0 : 0.0;
+                const double score = waves * (kps * per + tail) + join;
+                if (best.bn && score >= best.score) continue;
+                best.planes = planes;
+                best.kind = kind;
+                best.cg = cg;
+                best.bn = bn;
+                best.splits = sp;
+                best.kb_per_split = kps;
+                best.score = score;
+                best.n_tiles = nt;
+                best.partial_bytes = sp > 1 ? align_up((size_t)sp * m * n * sizeof(float), kWsAlign) : 0;
+            }
+        }
+    }
+    return best;
+}
+
+GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_splits) {
+    // (a plan takes some 5 us of host time, a small call has a few)
+    static std::mutex mu;
+    static std::map<std::array<int, 7>, GemmPlan> cache;
+    const int sms = num_sms();
+    const std::array<int, 7> key = {planes, kind, m, n, k, max_splits, sms};
+    {
+        std::lock_guard<std::mutex> g(mu);
+        const auto it = cache.find(key);
+        if (it != cache.end()) return it->second;
+    }
+    const GemmPlan p = plan_gemm_anew(planes, kind, m, n, k, max_splits, sms);
+    std::lock_guard<std::mutex> g(mu);
+    if (cache.size() >= 256) cache.clear();
+    cache.emplace(key, p);
+    return p;
+}
+
+qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, cudaStream_t st) {
+    const bool gen = plan.planes == GEMM_F32;
+    const int P = real_planes(plan.planes), bk = block_k(P), cg = plan.cg, bnc = plan.bn / cg;
+    GemmArgs g = {};
+    unsigned a_bytes = 0, b_bytes = 0;
+    for (int i = 0; i < count; ++i) {
+        const GemmProblem &s = ps[i];
+        ProblemArgs &p = g.p[i];
+        qcnn_status rc = set_operand(s.a, plan.planes, kMT, s.m, s.k, &p.a, &p.map_a);
+        if (rc == QCNN_OK) rc = set_operand(s.b, plan.planes, bnc, s.n, s.k, &p.b, &p.map_b);
+        if (rc != QCNN_OK) return rc;
+        a_bytes = std::max(a_bytes, p.a.bytes);
+        b_bytes = std::max(b_bytes, p.b.bytes);
+        p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (s.a.mn ? 1u << 15 : 0) | (s.b.mn ? 1u << 16 : 0) |
+                  (uint32_t)(plan.bn >> 3) << 17 | (uint32_t)(kMT * cg >> 4) << 24;
+        p.m = s.m;
+        p.n = s.n;
+        p.k = s.k;
+        p.kblocks = std::max(1, cdiv(s.k, bk));
+        p.m_tiles = cdiv(s.m, kMT * cg);
+        p.n_tiles = cdiv(s.n, plan.bn);
+        p.splits = count > 1 ? 1 : plan.splits;
+        p.kb_per_split = p.splits > 1 ? plan.kb_per_split : p.kblocks;
+        p.group = std::max(1, 16 / cg);
+        p.e = s.e;
+        if (p.splits == 1) p.e.partial = nullptr;
+        long long units = (long long)p.m_tiles * p.n_tiles * p.splits;
+        if (plan.kind == GEMM_SYM) {
+            units = 0;
+            for (int j = 0; j < p.n_tiles; ++j) units += std::max(0, p.m_tiles - j * (plan.bn / (kMT * cg)));
+        }
+        if (units > (1 << 30)) return QCNN_ERR_UNSUPPORTED;
+        p.units = (int)units;
+        g.units += p.units;
+    }
+    g.count = count;
+    g.bn = plan.bn;
+    g.b_off = a_bytes;  // (multiples of 1024: 128 rows; 64 rows of 128 bytes)
+    g.stage = (unsigned)align_up(a_bytes + b_bytes, 1024);
+    const size_t raw = gen ? (size_t)kRawSlots * cdiv((kMT + plan.bn) * 4, kGenThreads) * 32 * kGenThreads : 0;
+    g.S = (int)std::min<size_t>(gen ? 3 : kStagesMax, (kSmemMax - 1024 - raw) / g.stage);
+    if (g.S < 2) return QCNN_ERR_UNSUPPORTED;
+    const size_t smem = std::max(kSmemLeast, g.S * (size_t)g.stage + raw + 1024);
+    const int ctas = std::min(g.units, num_sms() / cg) * cg;
+    return launcher(plan)(&g, ctas, smem, st);
+}
+
+qcnn_status launch_gemm_join(const GemmPlan &plan, const GemmProblem &p, cudaStream_t st) {
+    const dim3 grid(cdiv(p.m, 256), std::min(p.n, 65535));
+    return launch_pdl(gemm_join_kernel, grid, dim3(256), 0, st, p.e, p.m, p.n, plan.splits);
+}
+
+qcnn_status launch_planes(const void *src, int bf16, long long rows, int cols, long long ld, int planes,
+                          void *dst, long long plane, const long long *keep, int classes,
+                          cudaStream_t st) {
+    const long long all = rows * ((cols + 7) / 8);
+    if (all == 0) return QCNN_OK;
+    const int grid = (int)std::min<long long>((all + 255) / 256, (long long)num_sms() * 16);
+    const int vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
+    unsigned short *d = static_cast<unsigned short *>(dst);
+    if (bf16)
+        return launch_pdl(planes_kernel<unsigned short>, dim3(grid), dim3(256), 0, st,
+                          static_cast<const unsigned short *>(src), rows, cols, ld, planes, d, plane, keep,
+                          classes, vec);
+    return launch_pdl(planes_kernel<float>, dim3(grid), dim3(256), 0, st, static_cast<const float *>(src),
+                      rows, cols, ld, planes, d, plane, keep, classes, vec);
+}
+
+}  // namespace qcnn

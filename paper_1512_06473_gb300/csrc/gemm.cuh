@@ -1,0 +1,173 @@
+// gemm.cuh -- matrix products on the tensor cores for the operators that train
+// dense layers (dense.cu, xent.cu, orthogonalize.cu): what a product is made of,
+// its plan and its launch.  The kernel is in gemm_kernel.cuh.
+//
+// A product is C[n][m] = sum_k A[m][k] B[n][k], with m the index that is contiguous
+// in the result.  Operands are bf16 "planes": one for bf16 data; two or three whose
+// sum is the value where more bits are needed (split2, split3).  Either operand may
+// lie with k or with its row index contiguous, so no operand is ever transposed in
+// memory: x W^T, dz W and dz^T x are the same kernel.
+#pragma once
+
+#include "qcnn_internal.cuh"
+
+#include <cuda.h>
+
+namespace qcnn {
+
+// An operand: planes of bf16, `plane` elements apart, rows of `ld` elements (16-byte
+// multiples); mn: [k][row], else [row][k].  Of the fp32 kernel (GEMM_F32): p is
+// fp32, any ld and alignment, one plane.
+struct GemmOperand {
+    const void *p = nullptr;
+    long long ld = 0, plane = 0;
+    int mn = 0;
+};
+
+enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1, GEMM_T_PLANES2 = 2, GEMM_T_PLANES3 = 3 };
+
+// What becomes of a sum.  OUT: v = alpha * sum + bias[m] (alpha: *alpha_ptr where set); pre = v; v = act(v);
+// v += beta * add[n][m]; out[n][m] = v.  With partial set: the sums of this split
+// alone, fp32 [split][n][m], for launch_gemm_join.  SYM: the product is symmetric
+// (A and B the same matrix): only m >= n is computed and stored at both places.
+// STATS: m are rows, n classes: the maximum and the sum of exp over a tile's classes
+// of v = sum + bias[n], and the value at the row's target.  DLOGITS: m are classes,
+// n rows: out = g_n (exp(v - lse_n) - [target_n == m]).
+struct GemmEpi {
+    float alpha = 1.f, beta = 0.f;
+    const float *alpha_ptr = nullptr;  // in device memory
+    const float *bias = nullptr;
+    void *out = nullptr;
+    long long ldo = 0, out_plane = 0;
+    int out_type = GEMM_T_F32;
+    void *pre = nullptr;  // same type as out
+    long long ldp = 0;
+    const void *add = nullptr;
+    long long lda = 0, add_plane = 0;
+    int add_type = GEMM_T_F32;
+    int act = 0;
+    float *partial = nullptr;
+    int sym = 0;
+    // STATS, DLOGITS
+    float2 *stats = nullptr;           // [tile along n][half][m]
+    const long long *targets = nullptr;
+    float *target_logit = nullptr;     // [m]
+    const float4 *rows = nullptr;      // [n]: lse, g, target (bits), -
+    int class0 = 0;                    // first class of this piece
+    float *col_part = nullptr;         // DLOGITS: sums over a tile's rows, [tile along n][half][ld_col]
+    long long ld_col = 0;
+};
+
+enum GemmKind { GEMM_OUT = 0, GEMM_SYM = 1, GEMM_STATS = 2, GEMM_DLOGITS = 3 };
+
+struct GemmProblem {
+    GemmOperand a, b;
+    int m = 0, n = 0, k = 0;
+    GemmEpi e;
+};
+
+// planes: 1, 2, 3, or GEMM_F32 (fp32 operands, split into three planes on their way
+// to shared memory).
+constexpr int GEMM_F32 = 0;
+
+struct GemmPlan {
+    int planes = 1, kind = 0, cg = 1;
+    int bn = 0;       // tile columns
+    int splits = 1, kb_per_split = 0;
+    double score = 0;  // estimated SM clocks
+    size_t partial_bytes = 0;  // 0 where splits == 1
+    int n_tiles = 0;
+};
+// max_splits 1: the sums must end in one tile (epilogues that launch_gemm_join does
+// not have)
+GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_splits);
+
+// One launch of one or two products of the same kind and planes (the second fills
+// the SMs that the first one's last tiles leave idle); both with `plan`'s tile, each
+// unsplit if there are two.  With plan.splits > 1, p[0].e.partial must be set, and
+// launch_gemm_join finishes.
+qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *p, int count, cudaStream_t st);
+// The epilogue of a split product: the sums of its splits, in order.
+qcnn_status launch_gemm_join(const GemmPlan &plan, const GemmProblem &p, cudaStream_t st);
+
+// Smallest multiple of 8 elements: rows of 16-byte multiples.
+inline long long pad8(long long v) { return (v + 7) / 8 * 8; }
+
+// src [rows][cols] (fp32 or bf16, row stride ld) -> bf16 planes [planes][rows][pad8(cols)],
+// plane elements apart; columns past cols are zero.  keep: per row, a class index: rows
+// where it is outside [0, classes) become zero (null: all rows as they are).
+qcnn_status launch_planes(const void *src, int bf16, long long rows, int cols, long long ld, int planes,
+                          void *dst, long long plane, const long long *keep, int classes,
+                          cudaStream_t st);
+
+}  // namespace qcnn
+
+#ifdef __CUDACC__
+namespace qcnn {
+
+// v = b0 + b1 (+ b2), bf16 pieces of two values each (low half: the first).  b0 is
+// rounded to nearest, the differences are exact; of three pieces b1 is cut off and b2
+// the rest, which has at most 8 bits: the sum is v, exactly, down to 2^-133 (bf16's
+// last bit).  Of two, b1 is rounded: 16 to 17 bits of v.
+__device__ __forceinline__ float2 bf16_rest(float v0, float v1, unsigned p) {
+    return __ffma2_rn(make_float2(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)),
+                      make_float2(-1.f, -1.f), make_float2(v0, v1));
+}
+__device__ __forceinline__ void planes3(float v0, float v1, unsigned &p0, unsigned &p1, unsigned &p2) {
+    p0 = pack_bf16x2(v0, v1);
+    const float2 r = bf16_rest(v0, v1, p0);
+    const unsigned rx = __float_as_uint(r.x), ry = __float_as_uint(r.y);
+    p1 = __byte_perm(rx, ry, 0x7632);
+    const float2 s = bf16_rest(r.x, r.y, p1);
+    p2 = __byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x7632);
+}
+__device__ __forceinline__ void planes2(float v0, float v1, unsigned &p0, unsigned &p1) {
+    p0 = pack_bf16x2(v0, v1);
+    const float2 r = bf16_rest(v0, v1, p0);
+    p1 = pack_bf16x2(r.x, r.y);
+}
+
+// Activations and their derivatives (include/qcnn.h, qcnn_activation).
+__device__ __forceinline__ float act_apply(float z, int act) {
+    switch (act) {
+        case QCNN_ACT_RELU: return z < 0.f ? 0.f : z;  // (NaN stays)
+        case QCNN_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+        case QCNN_ACT_SILU: return z / (1.f + expf(-z));
+        default: return z;
+    }
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+    switch (act) {
+        case QCNN_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
+        case QCNN_ACT_GELU:
+            return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
+                   z * 0.39894228040143268f * expf(-0.5f * z * z);
+        case QCNN_ACT_SILU: {
+            const float s = 1.f / (1.f + expf(-z));
+            return s * (1.f + z * (1.f - s));
+        }
+        default: return 1.f;
+    }
+}
+
+__device__ __forceinline__ float bf16_to_float(unsigned short v) {
+    return __uint_as_float((unsigned)v << 16);
+}
+__device__ __forceinline__ unsigned short float_to_bf16(float v) {
+    return (unsigned short)(pack_bf16x2(v, 0.f) & 0xffffu);
+}
+// One value of a matrix of `type`, element offset o.
+__device__ __forceinline__ float load_as(const void *p, int type, long long o, long long plane) {
+    if (type == GEMM_T_F32) return static_cast<const float *>(p)[o];
+    const unsigned short *s = static_cast<const unsigned short *>(p) + o;
+    float v = bf16_to_float(s[0]);
+    if (type >= GEMM_T_PLANES2) {
+        float w = bf16_to_float(s[plane]);
+        if (type == GEMM_T_PLANES3) w += bf16_to_float(s[2 * plane]);
+        v += w;
+    }
+    return v;
+}
+
+}  // namespace qcnn
+#endif

@@ -1,0 +1,19 @@
+// gemm_p3.cu -- the tensor-core product (gemm_kernel.cuh) of operands in 3 planes.
+#define QCNN_UNIT_RECORDS
+#include "gemm_kernel.cuh"
+
+namespace qcnn {
+
+using GemmLaunch = qcnn_status (*)(const void *, int, size_t, cudaStream_t);
+GemmLaunch gemm_launch_p3(int kind, int cg) {
+    switch (kind) {
+        case GEMM_STATS:
+            return cg == 1 ? GemmKernel<3, GEMM_STATS, 1, false>::launch : GemmKernel<3, GEMM_STATS, 2, false>::launch;
+        case GEMM_DLOGITS:
+            return cg == 1 ? GemmKernel<3, GEMM_DLOGITS, 1, false>::launch : GemmKernel<3, GEMM_DLOGITS, 2, false>::launch;
+        default:
+            return cg == 1 ? GemmKernel<3, GEMM_OUT, 1, false>::launch : GemmKernel<3, GEMM_OUT, 2, false>::launch;
+    }
+}
+
+}  // namespace qcnn

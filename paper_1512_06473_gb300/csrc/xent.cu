@@ -1,0 +1,516 @@
+// xent.cu -- qcnn_xent_forward and qcnn_xent_grad: softmax cross entropy over the classes of
+// a linear layer, with its gradient.
+//
+//   l = x W^T + b;  lse_n = log sum_c exp l_nc;  loss_n = lse_n - l_n,t(n)
+//   dl = g_n (exp(l - lse_n) - [c == t(n)]);  dx = dl W;  dW = dl^T x;  db = sum_n dl
+//
+// Two ways:
+//   small (the fp32 logits fit kPiece bytes): the logits are one piece, kept for the call:
+//     a product, a pass per row (lse, loss), and for the gradient a pass over the piece
+//     (dl, db) and two products.
+//   large: the logits are never stored.  One product over all classes leaves, per tile
+//     and row, the maximum and the sum of exp; joined they are lse.  The gradient then goes
+//     in pieces of the classes: the piece's logits again, whose epilogue turns them into dl
+//     (bf16, or planes), dx += dl W_piece (summed in fp32), dW_piece = dl^T x.  A fourth
+//     product instead of 4 N Ct bytes: at Cs = 2048 that is 1.1 ns per row and 1000 classes,
+//     writing and reading the logits 1.2 ns.
+#include "train.cuh"
+
+#include <algorithm>
+
+namespace qcnn {
+namespace {
+
+constexpr size_t kPiece = 64u << 20;    // bytes of a kept piece of logits
+constexpr size_t kPieceDl = 128u << 20;  // bytes of a piece of their gradient
+
+__device__ __forceinline__ int class_of(const int64_t *targets, int n, int Ct) {
+    const long long t = targets[n];
+    QCNN_CHECK(t < Ct, QCNN_CHECK_CODE);
+    return t >= 0 && t < Ct ? (int)t : -1;
+}
+
+// 1 / (rows with a class), by one CTA of 256 threads.
+__device__ void count_rows(const int64_t *targets, int N, int Ct, float *inv) {
+    __shared__ int part[8];
+    int c = 0;
+    for (int n = threadIdx.x; n < N; n += 256) c += (unsigned long long)targets[n] < (unsigned long long)Ct;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = c;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) c += part[i];
+        *inv = c ? 1.f / (float)c : 0.f;
+    }
+}
+
+// Maximum and sum of exp, of two parts (as in the products' epilogue).
+__device__ __forceinline__ void join(float &top, float &sum, float t2, float s2) {
+    const float t = fmaxf(top, t2);
+    if (t == -INFINITY) {
+        sum += s2;
+        return;
+    }
+    sum = sum * expf(top - t) + s2 * expf(t2 - t);
+    top = t;
+}
+struct RowOut {
+    const int64_t *targets;
+    const float *dloss;
+    float *loss, *lse;
+    float4 *rows;  // null: no gradient
+    float *inv;
+    int N, Ct;
+};
+__device__ __forceinline__ void finish_row(const RowOut &o, int n, float top, float sum, float target_logit) {
+    const int t = class_of(o.targets, n, o.Ct);
+    const float lse = top + logf(sum);
+    o.lse[n] = lse;
+    o.loss[n] = t >= 0 ? lse - target_logit : 0.f;
+    if (o.rows) o.rows[n] = make_float4(lse, o.dloss ? o.dloss[n] : 1.f, __int_as_float(t), 0.f);
+}
+
+// Small: a CTA per row of logits; one more counts the rows.
+__global__ void __launch_bounds__(256) rows_kernel(const float *logits, RowOut o) {
+    grid_dep_sync();
+    if ((int)blockIdx.x == o.N) {
+        count_rows(o.targets, o.N, o.Ct, o.inv);
+        return;
+    }
+    __shared__ float tops[8], sums[8];
+    const float *l = logits + (size_t)blockIdx.x * o.Ct;
+    float top = -INFINITY, sum = 0.f;
+    for (int c0 = threadIdx.x; c0 < o.Ct; c0 += 256 * 8) {
+        float v[8], t = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = c0 + i * 256 < o.Ct ? l[c0 + i * 256] : -INFINITY;
+            t = fmaxf(t, v[i]);
+        }
+        if (t == -INFINITY) {  // nothing to add (or NaN)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (v[i] != v[i]) sum = v[i];
+            continue;
+        }
+        sum = top == -INFINITY ? sum : sum * expf(top - t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += expf(v[i] - t);
+        top = t;
+    }
+#pragma unroll
+    for (int s = 16; s; s >>= 1)
+        join(top, sum, __shfl_xor_sync(0xffffffffu, top, s), __shfl_xor_sync(0xffffffffu, sum, s));
+    if ((threadIdx.x & 31) == 0) {
+        tops[threadIdx.x >> 5] = top;
+        sums[threadIdx.x >> 5] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) join(top, sum, tops[i], sums[i]);
+        const int t = class_of(o.targets, blockIdx.x, o.Ct);
+        finish_row(o, blockIdx.x, top, sum, t >= 0 ? l[t] : 0.f);
+    }
+}
+
+// Large: the tiles' maxima and sums of 32 rows per CTA; eight warps take the tiles in turn.
+__global__ void __launch_bounds__(256) stats_join_kernel(const float2 *stats, int parts,
+                                                         const float *target_logit, RowOut o) {
+    grid_dep_sync();
+    if ((int)blockIdx.x * 32 >= o.N) {
+        count_rows(o.targets, o.N, o.Ct, o.inv);
+        return;
+    }
+    __shared__ float2 red[8][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockIdx.x * 32 + lane;
+    float top = -INFINITY, sum = 0.f;
+    if (n < o.N)
+        for (int p = warp; p < parts; p += 32) {
+            float2 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = p + 8 * i < parts ? stats[(size_t)(p + 8 * i) * o.N + n] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) join(top, sum, v[i].x, v[i].y);
+        }
+    red[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (warp == 0 && n < o.N) {
+        for (int i = 1; i < 8; ++i) join(top, sum, red[i][lane].x, red[i][lane].y);
+        finish_row(o, n, top, sum, target_logit[n]);
+    }
+}
+
+// Small: the gradient of the logits and its sums over a slab of rows.  A CTA takes 128
+// classes x a slab: a warp a row, a lane four classes.
+__global__ void __launch_bounds__(256) dl_kernel(const float *logits, const float4 *rows, int N, int Ct, void *out, int out_type, long long ldo,
+                                                 long long plane, float *part, int slab) {
+    __shared__ float red[8][128];
+    grid_dep_sync();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = blockIdx.x * 128 + lane * 4;
+    const int r1 = min(N, ((int)blockIdx.y + 1) * slab);
+    float sum[4] = {};
+    if (c < Ct) {
+#pragma unroll 2
+        for (int r = (int)blockIdx.y * slab + warp; r < r1; r += 8) {
+            const float4 row = rows[r];
+            const int target = __float_as_int(row.z);
+            const float *l = logits + (size_t)r * Ct + c;
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = c + j < Ct ? l[j] : -INFINITY;
+            const float g = row.y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = expf(v[j] - row.x);
+                // (a row without a class is zero, whatever its logits are)
+                v[j] = target >= 0 && c + j < Ct ? g * (target == c + j ? p - 1.f : p) : 0.f;
+                sum[j] += v[j];
+            }
+            const long long o = (long long)r * ldo + c;  // (rows of multiples of 8)
+            if (out_type == GEMM_T_F32) {
+                *reinterpret_cast<float4 *>(static_cast<float *>(out) + o) = make_float4(v[0], v[1], v[2], v[3]);
+            } else {
+                unsigned w[3][2];
+                unsigned short *d = static_cast<unsigned short *>(out) + o;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+                *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
+                if (out_type == GEMM_T_PLANES3) {
+                    *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
+                    *reinterpret_cast<uint2 *>(d + 2 * plane) = make_uint2(w[2][0], w[2][1]);
+                }
+            }
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) red[warp][lane * 4 + j] = sum[j];
+    __syncthreads();
+    const int t = threadIdx.x, col = blockIdx.x * 128 + t;
+    if (t < 128 && col < Ct) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += red[w][t];
+        part[(long long)blockIdx.y * Ct + col] = v;
+    }
+}
+
+// fp32 rows with a class, zeros for the others (16-byte rows).
+__global__ void __launch_bounds__(256) keep_rows_kernel(const float *x, long long ldx, int Cs,
+                                                        const int64_t *targets, int Ct, float *out,
+                                                        long long ldo) {
+    grid_dep_sync();
+    const bool in = (unsigned long long)targets[blockIdx.x] < (unsigned long long)Ct;
+    for (int c = blockIdx.y * 256 + threadIdx.x; c < Cs; c += gridDim.y * 256)
+        out[(long long)blockIdx.x * ldo + c] = in ? x[(long long)blockIdx.x * ldx + c] : 0.f;
+}
+
+struct XentPlan {
+    bool small = false, few = false;
+    bool lplanes = false;  // fp32: the product of the logits is of planes
+    bool gplanes = false;  // and those of the gradient
+    Product logits, stats, dl, dx, dw;
+    int piece = 0;         // classes of a piece
+    int slab = 0, slabs = 1;
+    int dl_type = GEMM_T_BF16;
+};
+XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool grad) {
+    XentPlan p;
+    const bool bf16 = dtype == QCNN_BF16;
+    p.small = (size_t)N * Ct * 4 <= kPiece;
+    p.piece = Ct;
+    const double size = ((double)N + Ct) * Cs;
+    if (p.small) {
+        p.few = N <= kFewRows;
+        p.slab = std::max(32, cdiv(cdiv(N, std::max(1, 4 * num_sms() / cdiv(Ct, 128))), 8) * 8);
+        p.slabs = cdiv(N, p.slab);
+        GemmPlan l, x, w;
+        double planes = 0, direct = 0;
+        if (bf16) {
+            l = plan_gemm(1, GEMM_OUT, Ct, N, Cs, 64);
+            x = plan_gemm(1, GEMM_OUT, Cs, N, Ct, 64);
+            w = plan_gemm(1, GEMM_OUT, Cs, Ct, N, 64);
+        } else {
+            // planes of x and W, once for the products that take them, or none of them
+            l = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, 64);
+            x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
+            w = plan_gemm(GEMM_F32, GEMM_OUT, Cs, Ct, N, 64);
+            const GemmPlan ql = plan_gemm(3, GEMM_OUT, Ct, N, Cs, 64), qx = plan_gemm(3, GEMM_OUT, Cs, N, Ct, 64),
+                           qw = plan_gemm(3, GEMM_OUT, Cs, Ct, N, 64);
+            direct = (p.few ? 0 : l.score) + (grad ? x.score + w.score : 0);
+            planes = (p.few ? 0 : ql.score) + (grad ? qx.score + qw.score : 0) + pass_clocks(size * 16.0);
+            if (planes < direct) {
+                p.lplanes = p.gplanes = true;
+                l = ql, x = qx, w = qw;
+            }
+        }
+        p.logits.plan = l;
+        p.dx.plan = x;
+        p.dw.plan = w;
+        p.dl_type = bf16 ? GEMM_T_BF16 : p.gplanes ? GEMM_T_PLANES3 : GEMM_T_F32;
+        return p;
+    }
+    const int P = bf16 ? 1 : 3;
+    p.lplanes = p.gplanes = !bf16;
+    p.dl_type = bf16 ? GEMM_T_BF16 : GEMM_T_PLANES3;
+    p.stats.plan = plan_gemm(P, GEMM_STATS, N, Ct, Cs, 1);
+    const long long most = (long long)(kPieceDl / ((size_t)N * 2 * P)) / 256 * 256;
+    p.piece = (int)std::min<long long>(Ct, std::max<long long>(256, most));
+    // (pieces of equal size)
+    p.piece = std::min(Ct, cdiv(cdiv(Ct, cdiv(Ct, p.piece)), 256) * 256);
+    p.dl.plan = plan_gemm(P, GEMM_DLOGITS, p.piece, N, Cs, 1);
+    p.dx.plan = plan_gemm(P, GEMM_OUT, Cs, N, p.piece, 1);
+    p.dw.plan = plan_gemm(P, GEMM_OUT, Cs, p.piece, N, 1);
+    return p;
+}
+struct XentSpace {
+    float *inv = nullptr, *logits = nullptr, *target_logit = nullptr, *db = nullptr, *dx = nullptr, *xkeep32 = nullptr;
+    float4 *rows = nullptr;
+    float2 *stats = nullptr;
+    unsigned short *x = nullptr, *w = nullptr, *xkeep = nullptr;
+    void *dl = nullptr, *partial = nullptr;
+    size_t bytes = 0;
+};
+XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool grad, bool x_copy, bool w_copy,
+                     void *ws) {
+    Carver c{static_cast<uint8_t *>(ws)};
+    XentSpace s;
+    const bool bf16 = dtype == QCNN_BF16;
+    const size_t P = bf16 ? 1 : 3;
+    const long long pc = pad8(Cs);
+    s.inv = c.array<float>(1);
+    if (grad) s.rows = c.array<float4>(N);
+    if (x_copy) s.x = c.array<unsigned short>(P * N * pc);
+    if (w_copy) s.w = c.array<unsigned short>(P * Ct * pc);
+    size_t partial = 0;
+    if (p.small) {
+        s.logits = c.array<float>((size_t)N * Ct);
+        if (!p.few) partial = p.logits.scratch();
+    } else {
+        s.stats = c.array<float2>((size_t)p.stats.plan.n_tiles * 2 * N);
+        s.target_logit = c.array<float>(N);
+    }
+    if (grad) {
+        // rows without a class must not reach dW, not even as 0 * NaN
+        if (bf16 || p.gplanes) s.xkeep = c.array<unsigned short>(P * N * pc);
+        else s.xkeep32 = c.array<float>((size_t)N * pc);
+        s.dl = c.take((size_t)N * pad8(p.piece) * (p.dl_type == GEMM_T_F32 ? 4 : 2 * P));
+        partial = std::max({partial, p.dx.scratch(), p.dw.scratch()});
+        if (p.small) {
+            s.db = c.array<float>((size_t)p.slabs * Ct);
+        } else {
+            s.db = c.array<float>((size_t)p.dl.plan.n_tiles * 2 * p.piece);
+            if (p.piece < Ct) s.dx = c.array<float>((size_t)N * Cs);
+        }
+    }
+    s.partial = c.take(partial);
+    s.bytes = c.used;
+    return s;
+}
+
+struct XentCall {
+    const void *x, *W;
+    long long ldx, ldw;
+    int N, Cs, Ct, dtype;
+    const float *bias;
+    const int64_t *targets;
+    const float *dloss;
+    float *loss, *lse;
+    void *dx, *dW;
+    long long lddx, lddw;
+    float *dbias;
+    bool grad;
+};
+
+qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes, cudaStream_t st) {
+    const int N = a.N, Cs = a.Cs, Ct = a.Ct;
+    const bool bf16 = a.dtype == QCNN_BF16;
+    const XentPlan p = plan_xent(N, Cs, Ct, a.dtype, a.grad);
+    // (few rows without a gradient read the operands as they are)
+    const bool products = !p.few || a.grad;
+    const bool x_copy = !p.few && (bf16 ? !tma_ok(a.x, a.ldx) : p.lplanes);
+    const bool w_copy = products && (bf16 ? !tma_ok(a.W, a.ldw) : p.lplanes);
+    const XentSpace s = carve_xent(p, N, Cs, Ct, a.dtype, a.grad, x_copy, w_copy, workspace);
+    qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
+    if (rc != QCNN_OK) return rc;
+    PdlScope pdl;
+    const int P = bf16 ? 1 : 3;
+    const long long pc = pad8(Cs);
+    GemmOperand xo{a.x, a.ldx, 0, 0}, wo{a.W, a.ldw, 0, 0}, xk;
+    if (s.x) {
+        if ((rc = launch_planes(a.x, bf16, N, Cs, a.ldx, P, s.x, N * pc, nullptr, 0, st)) != QCNN_OK) return rc;
+        xo = GemmOperand{s.x, pc, N * pc, 0};
+    }
+    if (s.w) {
+        if ((rc = launch_planes(a.W, bf16, Ct, Cs, a.ldw, P, s.w, Ct * pc, nullptr, 0, st)) != QCNN_OK) return rc;
+        wo = GemmOperand{s.w, pc, Ct * pc, 0};
+    }
+    if (s.xkeep) {
+        rc = launch_planes(a.x, bf16, N, Cs, a.ldx, P, s.xkeep, N * pc,
+                           reinterpret_cast<const long long *>(a.targets), Ct, st);
+        xk = GemmOperand{s.xkeep, pc, N * pc, 1};
+    } else if (s.xkeep32) {
+        rc = launch_pdl(keep_rows_kernel, dim3(N, std::min(cdiv(Cs, 256), 64)), dim3(256), 0, st,
+                        static_cast<const float *>(a.x), a.ldx, Cs, a.targets, Ct, s.xkeep32, pc);
+        xk = GemmOperand{s.xkeep32, pc, 0, 1};
+    }
+    if (rc != QCNN_OK) return rc;
+    RowOut ro{a.targets, a.dloss, a.loss, a.lse, s.rows, s.inv, N, Ct};
+    const int type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
+    GemmProblem g;
+    if (p.small) {
+        g.e.bias = a.bias;
+        g.e.out = s.logits;
+        g.e.ldo = Ct;
+        if (p.few) {
+            rc = launch_few_rows(FewRows{a.x, a.W, a.ldx, a.ldw, N, Cs, Ct, bf16, g.e}, st);
+        } else {
+            g.a = wo;
+            g.b = xo;
+            g.m = Ct;
+            g.n = N;
+            g.k = Cs;
+            rc = p.logits.run(g, s.partial, st);
+        }
+        if (rc != QCNN_OK) return rc;
+        rc = launch_pdl(rows_kernel, dim3(N + (a.grad ? 1 : 0)), dim3(256), 0, st, s.logits, ro);
+    } else {
+        g.a = xo;
+        g.b = wo;
+        g.m = N;
+        g.n = Ct;
+        g.k = Cs;
+        g.e.bias = a.bias;
+        g.e.stats = s.stats;
+        g.e.targets = reinterpret_cast<const long long *>(a.targets);
+        g.e.target_logit = s.target_logit;
+        if ((rc = launch_gemm(p.stats.plan, &g, 1, st)) != QCNN_OK) return rc;
+        rc = launch_pdl(stats_join_kernel, dim3(cdiv(N, 32) + (a.grad ? 1 : 0)), dim3(256), 0, st, s.stats,
+                        p.stats.plan.n_tiles * 2, s.target_logit, ro);
+    }
+    if (rc != QCNN_OK || !a.grad) return rc;
+
+    // The factor 1 / rows of a mean is left out of dl and joins the sums that it is in:
+    // rounded to bf16 with dl it would put the same error into every gradient (0.2%).
+    const float *inv = a.dloss ? nullptr : s.inv;
+    for (int c0 = 0; c0 < Ct; c0 += p.piece) {
+        const int cn = std::min(p.piece, Ct - c0);
+        const long long pz = pad8(cn), zplane = (long long)N * pz;
+        const GemmOperand wp{static_cast<const uint8_t *>(wo.p) + c0 * wo.ld * (bf16 || p.gplanes ? 2 : 4), wo.ld,
+                             wo.plane, 1};
+        if (p.small) {
+            float *const part = a.dbias ? s.db : nullptr;
+            rc = launch_pdl(dl_kernel, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0, st, s.logits, s.rows, N, Ct,
+                            s.dl, p.dl_type, pz, zplane, part, p.slab);
+            if (rc == QCNN_OK && a.dbias)
+                rc = launch_column_join(s.db, p.slabs, Ct, Ct, inv, a.dbias, st);
+        } else {
+            GemmProblem d;
+            d.a = wp;
+            d.a.mn = 0;
+            d.b = xo;
+            d.m = cn;
+            d.n = N;
+            d.k = Cs;
+            d.e.bias = a.bias ? a.bias + c0 : nullptr;
+            d.e.rows = s.rows;
+            d.e.class0 = c0;
+            d.e.out = s.dl;
+            d.e.out_type = p.dl_type;
+            d.e.ldo = pz;
+            d.e.out_plane = zplane;
+            d.e.col_part = s.db;
+            d.e.ld_col = p.piece;
+            rc = launch_gemm(p.dl.plan, &d, 1, st);
+            if (rc == QCNN_OK && a.dbias)
+                rc = launch_column_join(s.db, p.dl.plan.n_tiles * 2, p.piece, cn, inv, a.dbias + c0, st);
+        }
+        if (rc != QCNN_OK) return rc;
+        GemmProblem q;
+        q.a = wp;
+        q.b = GemmOperand{s.dl, pz, zplane, 0};
+        q.m = Cs;
+        q.n = N;
+        q.k = cn;
+        const bool first = c0 == 0, last = c0 + cn == Ct;
+        if (!first) {
+            q.e.add = s.dx;
+            q.e.lda = Cs;
+            q.e.beta = 1.f;
+        }
+        q.e.alpha_ptr = inv;
+        q.e.out = last ? a.dx : s.dx;
+        q.e.ldo = last ? a.lddx : Cs;
+        q.e.out_type = last ? type : GEMM_T_F32;
+        if ((rc = p.dx.run(q, s.partial, st)) != QCNN_OK) return rc;
+        GemmProblem v;
+        v.a = xk;
+        v.b = GemmOperand{s.dl, pz, zplane, 1};
+        v.m = Cs;
+        v.n = cn;
+        v.k = N;
+        v.e.alpha_ptr = inv;
+        v.e.out = static_cast<uint8_t *>(a.dW) + c0 * a.lddw * type_bytes(a.dtype);
+        v.e.ldo = a.lddw;
+        v.e.out_type = type;
+        if ((rc = p.dw.run(v, s.partial, st)) != QCNN_OK) return rc;
+    }
+    return QCNN_OK;
+}
+
+bool xent_args_ok(const XentCall &a) {
+    return a.N >= 0 && a.Cs > 0 && a.Ct > 0 && dtype_ok(a.dtype) && matrix_ok(a.x, a.ldx, a.N, a.Cs, a.dtype) &&
+           matrix_ok(a.W, a.ldw, a.Ct, a.Cs, a.dtype) && reinterpret_cast<uintptr_t>(a.bias) % 4 == 0 &&
+           (a.N == 0 || (a.targets && a.loss && a.lse)) && reinterpret_cast<uintptr_t>(a.targets) % 8 == 0 &&
+           reinterpret_cast<uintptr_t>(a.loss) % 4 == 0 && reinterpret_cast<uintptr_t>(a.lse) % 4 == 0 &&
+           reinterpret_cast<uintptr_t>(a.dloss) % 4 == 0 && reinterpret_cast<uintptr_t>(a.dbias) % 4 == 0;
+}
+
+}  // namespace
+}  // namespace qcnn
+
+using namespace qcnn;
+
+extern "C" {
+
+qcnn_status qcnn_xent_workspace_size(int N, int Cs, int Ct, int dtype, int aligned, int grad, size_t *bytes) {
+    if (!bytes || N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
+    *bytes = 0;
+    if (N == 0) return QCNN_OK;
+    const XentPlan p = plan_xent(N, Cs, Ct, dtype, grad != 0);
+    const bool copy = dtype == QCNN_BF16 ? !aligned : p.lplanes;
+    *bytes = carve_xent(p, N, Cs, Ct, dtype, grad != 0, copy && !p.few, copy && (!p.few || grad), nullptr).bytes;
+    return QCNN_OK;
+}
+
+qcnn_status qcnn_xent_forward(const void *x, long long ldx, int N, int Cs, const void *W, long long ldw, int Ct,
+                              const float *bias, const int64_t *targets, float *loss, float *lse, int dtype,
+                              void *workspace, size_t workspace_bytes, void *stream) {
+    const XentCall a{x, W, ldx, ldw, N, Cs, Ct, dtype, bias, targets, nullptr, loss, lse, nullptr, nullptr, 0, 0,
+                     nullptr, false};
+    if (!xent_args_ok(a)) return QCNN_ERR_INVALID_ARG;
+    if (N == 0) return QCNN_OK;
+    return run_xent(a, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+qcnn_status qcnn_xent_grad(const void *x, long long ldx, int N, int Cs, const void *W, long long ldw, int Ct,
+                           const float *bias, const int64_t *targets, const float *dloss, float *loss,
+                           float *lse, void *dx, long long lddx, void *dW, long long lddw, float *dbias,
+                           int dtype, void *workspace, size_t workspace_bytes, void *stream) {
+    const XentCall a{x, W, ldx, ldw, N, Cs, Ct, dtype, bias, targets, dloss, loss, lse, dx, dW, lddx, lddw,
+                     dbias, true};
+    if (!xent_args_ok(a) || !matrix_ok(dx, lddx, N, Cs, dtype) || !matrix_ok(dW, lddw, Ct, Cs, dtype))
+        return QCNN_ERR_INVALID_ARG;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (N == 0) {
+        cudaError_t e = cudaMemset2DAsync(dW, lddw * type_bytes(dtype), 0, Cs * type_bytes(dtype), Ct, st);
+        if (dbias && e == cudaSuccess) e = cudaMemsetAsync(dbias, 0, (size_t)Ct * 4, st);
+        return cuda_status(e);
+    }
+    return run_xent(a, workspace, workspace_bytes, st);
+}
+
+}  // extern "C"
