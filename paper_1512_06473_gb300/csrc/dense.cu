@@ -7,9 +7,9 @@
 // contiguous index m.  Three ways, by the estimated time of each:
 //   few rows (forward, N <= 8): no tensor cores; the weights are streamed once through
 //     fp32 multiply-adds, which then take less than the memory does;
-//   fp32 operands split on their way to shared memory: no pass over the operands, so it
-//     has the products that their bytes bound;
-//   planes in the workspace (fp32), or the bf16 operands themselves: the rest.
+//   fp32 weights split on their way to the tensor cores: no pass over them, so it has the
+//     products that their bytes bound (the other operand's planes are small then);
+//   all operands as planes in the workspace (fp32), or the bf16 operands themselves.
 #include "train.cuh"
 
 #include <algorithm>
@@ -143,12 +143,12 @@ qcnn_status few_rows_of(const FewRows &f, cudaStream_t st) {
 }
 
 // ------------------------------------------------- gradient of z, bias
-// dz = dy * act'(z) in `out_type` (none: only sums) and sums over a slab of rows:
+// dz = dy * act'(z) in planes (out null: only sums) and sums over a slab of rows:
 // part[slab][cols].  A CTA takes 128 columns x a slab: a warp a row, a lane four
 // columns.
 template <typename T>
 __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, const T *pre, long long ldp,
-                                                 int N, int Ct, int act, void *out, int out_type,
+                                                 int N, int Ct, int act, void *out, int planes,
                                                  long long ldo, long long plane, float *part, int slab,
                                                  int vec) {
     __shared__ float red[8][128];
@@ -187,19 +187,14 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, co
             for (int j = 0; j < 4; ++j) sum[j] += v[j];
             if (out) {  // (its rows are ours: multiples of 8 elements, 16-byte aligned)
                 const long long o = (long long)r * ldo + c;
-                if (out_type == GEMM_T_F32) {
-                    *reinterpret_cast<float4 *>(static_cast<float *>(out) + o) =
-                        make_float4(v[0], v[1], v[2], v[3]);
-                } else {
-                    unsigned w[3][2];
-                    unsigned short *d = static_cast<unsigned short *>(out) + o;
+                unsigned w[3][2];
+                unsigned short *d = static_cast<unsigned short *>(out) + o;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
-                    *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
-                    if (out_type == GEMM_T_PLANES3) {
-                        *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
-                        *reinterpret_cast<uint2 *>(d + 2 * plane) = make_uint2(w[2][0], w[2][1]);
-                    }
+                for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+                *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
+                if (planes == 3) {
+                    *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
+                    *reinterpret_cast<uint2 *>(d + 2 * plane) = make_uint2(w[2][0], w[2][1]);
                 }
             }
         }
@@ -231,24 +226,23 @@ int dz_slab(int N, int Ct) {
 }
 
 // ---------------------------------------------------------------- plans
-// Forward (fp32): the operands as they are, or planes.
+// fp32: rows (x, dz) always as planes; wplanes: the weights too.  bf16: copies of what
+// TMA cannot read.
 struct ForwardPlan {
-    bool few = false, planes = false;  // planes: copies of x and W in the workspace
+    bool few = false, wplanes = false;
     Product g;
 };
-ForwardPlan plan_forward(int N, int Cs, int Ct, int dtype, bool aligned) {
+ForwardPlan plan_forward(int N, int Cs, int Ct, int dtype) {
     ForwardPlan p;
     if (N <= kFewRows) {
         p.few = true;
     } else if (dtype == QCNN_BF16) {
-        p.planes = !aligned;
         p.g.plan = plan_gemm(1, GEMM_OUT, Ct, N, Cs, 64);
     } else {
         p.g.plan = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, 64);
         const GemmPlan q = plan_gemm(3, GEMM_OUT, Ct, N, Cs, 64);
-        const double more = pass_clocks(((double)N + Ct) * Cs * 16.0);
-        if (q.score + more < p.g.plan.score) {
-            p.planes = true;
+        if (q.score + pass_clocks((double)Ct * Cs * 10.0) < p.g.plan.score) {
+            p.wplanes = true;
             p.g.plan = q;
         }
     }
@@ -259,44 +253,38 @@ struct ForwardSpace {
     void *partial = nullptr;
     size_t bytes = 0;
 };
-// copies of x / W where the plan has them; bf16: of each that is not aligned
-ForwardSpace carve_forward(const ForwardPlan &p, int N, int Cs, int Ct, int dtype, bool x_copy, bool w_copy,
-                           void *ws) {
+ForwardSpace carve_forward(const ForwardPlan &p, int N, int Cs, int Ct, int dtype, bool xa, bool wa, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     ForwardSpace s;
-    const int P = dtype == QCNN_F32 ? 3 : 1;
-    if (p.planes && x_copy) s.x = c.array<unsigned short>((size_t)P * N * pad8(Cs));
-    if (p.planes && w_copy) s.w = c.array<unsigned short>((size_t)P * Ct * pad8(Cs));
+    if (p.few) return s;
+    const bool bf16 = dtype == QCNN_BF16;
+    const int P = bf16 ? 1 : 3;
+    if (!bf16 || !xa) s.x = c.array<unsigned short>((size_t)P * N * pad8(Cs));
+    if (bf16 ? !wa : p.wplanes) s.w = c.array<unsigned short>((size_t)P * Ct * pad8(Cs));
     s.partial = c.take(p.g.scratch());
     s.bytes = c.used;
     return s;
 }
 
 struct BackwardPlan {
-    bool planes = false;  // fp32: dz, x and W in planes; bf16: copies of what is not aligned
-    bool dz_copy = false;
-    int dz_type = GEMM_T_F32, slab = 0, slabs = 1;
+    bool wplanes = false;
+    int slab = 0, slabs = 1;
     Product gx, gw;
 };
 BackwardPlan plan_backward(int N, int Cs, int Ct, int dtype) {
     BackwardPlan p;
     p.slab = dz_slab(N, Ct);
     p.slabs = cdiv(N, p.slab);
-    if (dtype == QCNN_BF16) {
-        p.dz_type = GEMM_T_BF16;
-        p.gx.plan = plan_gemm(1, GEMM_OUT, Cs, N, Ct, 64);
-        p.gw.plan = plan_gemm(1, GEMM_OUT, Cs, Ct, N, 64);
-        return p;
-    }
-    p.gx.plan = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
-    p.gw.plan = plan_gemm(GEMM_F32, GEMM_OUT, Cs, Ct, N, 64);
-    const GemmPlan qx = plan_gemm(3, GEMM_OUT, Cs, N, Ct, 64), qw = plan_gemm(3, GEMM_OUT, Cs, Ct, N, 64);
-    const double more = pass_clocks(((double)N + Ct) * Cs * 16.0 + (double)N * Ct * 4.0);
-    if (qx.score + qw.score + more < p.gx.plan.score + p.gw.plan.score) {
-        p.planes = true;
-        p.dz_type = GEMM_T_PLANES3;
-        p.gx.plan = qx;
-        p.gw.plan = qw;
+    const int P = dtype == QCNN_BF16 ? 1 : 3;
+    p.gw.plan = plan_gemm(P, GEMM_OUT, Cs, Ct, N, 64);
+    p.gx.plan = plan_gemm(P, GEMM_OUT, Cs, N, Ct, 64);
+    p.wplanes = true;
+    if (P == 3) {
+        const GemmPlan q = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
+        if (q.score <= p.gx.plan.score + pass_clocks((double)Ct * Cs * 10.0)) {
+            p.wplanes = false;
+            p.gx.plan = q;
+        }
     }
     return p;
 }
@@ -311,8 +299,8 @@ BackwardSpace carve_backward(const BackwardPlan &p, int N, int Cs, int Ct, int d
                              bool w_copy, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     BackwardSpace s;
-    const size_t P = p.planes ? 3 : 1;
-    if (dz) s.dz = c.take(P * N * pad8(Ct) * (p.dz_type == GEMM_T_F32 ? 4 : 2));
+    const size_t P = dtype == QCNN_BF16 ? 1 : 3;
+    if (dz) s.dz = c.take(P * N * pad8(Ct) * 2);
     if (x_copy) s.x = c.array<unsigned short>(P * N * pad8(Cs));
     if (w_copy) s.w = c.array<unsigned short>(P * Ct * pad8(Cs));
     if (p.slabs > 1) s.db = c.array<float>((size_t)p.slabs * Ct);
@@ -345,8 +333,7 @@ extern "C" {
 qcnn_status qcnn_dense_forward_workspace_size(int N, int Cs, int Ct, int dtype, int aligned,
                                               size_t *bytes) {
     if (!bytes || N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
-    *bytes = N ? carve_forward(plan_forward(N, Cs, Ct, dtype, aligned != 0), N, Cs, Ct, dtype, true, true,
-                               nullptr).bytes
+    *bytes = N ? carve_forward(plan_forward(N, Cs, Ct, dtype), N, Cs, Ct, dtype, aligned, aligned, nullptr).bytes
                : 0;
     return QCNN_OK;
 }
@@ -364,8 +351,8 @@ qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, cons
     if (N == 0) return QCNN_OK;
     const bool bf16 = dtype == QCNN_BF16;
     const bool xa = tma_ok(x, ldx), wa = tma_ok(W, ldw);
-    const ForwardPlan p = plan_forward(N, Cs, Ct, dtype, xa && wa);
-    const ForwardSpace s = carve_forward(p, N, Cs, Ct, dtype, !bf16 || !xa, !bf16 || !wa, workspace);
+    const ForwardPlan p = plan_forward(N, Cs, Ct, dtype);
+    const ForwardSpace s = carve_forward(p, N, Cs, Ct, dtype, xa, wa, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -392,12 +379,12 @@ qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, cons
     const int P = bf16 ? 1 : 3;
     const long long pitch = pad8(Cs);
     if (s.x) {
-        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, N * pitch, nullptr, 0, st);
+        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, nullptr, nullptr, 0, st);
         if (rc != QCNN_OK) return rc;
         g.b = GemmOperand{s.x, pitch, N * pitch, 0};
     }
     if (s.w) {
-        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, Ct * pitch, nullptr, 0, st);
+        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, nullptr, nullptr, 0, st);
         if (rc != QCNN_OK) return rc;
         g.a = GemmOperand{s.w, pitch, Ct * pitch, 0};
     }
@@ -408,8 +395,9 @@ qcnn_status qcnn_dense_backward_workspace_size(int N, int Cs, int Ct, int dtype,
                                                size_t *bytes) {
     if (!bytes || N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
     const BackwardPlan p = plan_backward(N, Cs, Ct, dtype);
-    const bool copy = dtype == QCNN_F32 ? p.planes : !aligned;
-    *bytes = N ? carve_backward(p, N, Cs, Ct, dtype, true, copy, copy, nullptr).bytes : 0;
+    const bool f32 = dtype == QCNN_F32;
+    *bytes = N ? carve_backward(p, N, Cs, Ct, dtype, true, f32 || !aligned, f32 ? p.wplanes : !aligned, nullptr).bytes
+               : 0;
     return QCNN_OK;
 }
 
@@ -437,9 +425,9 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
     const BackwardPlan p = plan_backward(N, Cs, Ct, dtype);
     // dy itself where it is dz in a form that the products read
     const bool products = dx || dW;
-    const bool dz = products && (act != QCNN_ACT_NONE || p.planes || (bf16 && !tma_ok(dy, lddy)));
-    const bool x_copy = dW && (bf16 ? !tma_ok(x, ldx) : p.planes);
-    const bool w_copy = dx && (bf16 ? !tma_ok(W, ldw) : p.planes);
+    const bool dz = products && (act != QCNN_ACT_NONE || !bf16 || !tma_ok(dy, lddy));
+    const bool x_copy = dW && (!bf16 || !tma_ok(x, ldx));
+    const bool w_copy = dx && (bf16 ? !tma_ok(W, ldw) : p.wplanes);
     const BackwardSpace s = carve_backward(p, N, Cs, Ct, dtype, dz, x_copy, w_copy, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;
@@ -458,11 +446,11 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
         if (bf16)
             rc = launch_pdl(dz_kernel<unsigned short>, grid, dim3(256), 0, st,
                             static_cast<const unsigned short *>(dy), lddy,
-                            static_cast<const unsigned short *>(pre), ldp, N, Ct, act, s.dz, p.dz_type, pz,
+                            static_cast<const unsigned short *>(pre), ldp, N, Ct, act, s.dz, bf16 ? 1 : 3, pz,
                             (long long)N * pz, part, p.slab, vec);
         else
             rc = launch_pdl(dz_kernel<float>, grid, dim3(256), 0, st, static_cast<const float *>(dy), lddy,
-                            static_cast<const float *>(pre), ldp, N, Ct, act, s.dz, p.dz_type, pz,
+                            static_cast<const float *>(pre), ldp, N, Ct, act, s.dz, bf16 ? 1 : 3, pz,
                             (long long)N * pz, part, p.slab, vec);
         if (rc != QCNN_OK) return rc;
         if (dbias && p.slabs > 1 && (rc = launch_column_join(s.db, p.slabs, Ct, Ct, nullptr, dbias, st)) != QCNN_OK)
@@ -470,12 +458,12 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
         if (dz) z = GemmOperand{s.dz, pz, (long long)N * pz, 0};
     }
     if (x_copy) {
-        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, N * pc, nullptr, 0, st);
+        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, nullptr, nullptr, 0, st);
         if (rc != QCNN_OK) return rc;
         xo = GemmOperand{s.x, pc, N * pc, 1};
     }
     if (w_copy) {
-        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, Ct * pc, nullptr, 0, st);
+        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, nullptr, nullptr, 0, st);
         if (rc != QCNN_OK) return rc;
         wo = GemmOperand{s.w, pc, Ct * pc, 1};
     }

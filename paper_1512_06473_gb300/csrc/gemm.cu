@@ -19,7 +19,7 @@ GemmLaunch gemm_launch_f32();
 
 namespace {
 
-constexpr size_t kSmemMax = 225 * 1024;  // dynamic, with 1 KB to align the stages
+constexpr size_t kSmemMax = 222 * 1024;  // dynamic, with 1 KB to align the stages
 // one CTA per SM, whatever it needs: all tensor memory is taken
 constexpr size_t kSmemLeast = 120 * 1024;
 
@@ -50,7 +50,8 @@ unsigned operand_bytes(int P, int mn, int rows) {
     return mn ? (unsigned)cdiv(rows, 64) * P * bk * 128 : (unsigned)P * rows * bk * 2;
 }
 
-// An operand of `rows` rows (this CTA's part of a tile); rows_all x k is its matrix.
+// An operand of `rows` rows (this CTA's part of a tile); rows_all x k is its matrix.  map:
+// null for an fp32 one.
 qcnn_status set_operand(const GemmOperand &o, int planes, int rows, int rows_all, int k, OpArgs *a,
                         CUtensorMap *map) {
     const int P = real_planes(planes), bk = block_k(P);
@@ -66,7 +67,7 @@ qcnn_status set_operand(const GemmOperand &o, int planes, int rows, int rows_all
     a->ld = o.ld;
     a->rows = rows_all;
     a->vec = reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.ld % 4 == 0;
-    if (planes == GEMM_F32) return QCNN_OK;
+    if (!map) return QCNN_OK;
     const EncodeTiled enc = encode_tiled();
     if (!enc) return QCNN_ERR_CUDA;
     const cuuint64_t inner = o.mn ? rows_all : k, outer = o.mn ? k : rows_all;
@@ -127,54 +128,61 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(GemmEpi e, int m_all, in
 }
 
 // --------------------------------------------------------------- planes
-// A thread per eight columns: two 16-byte loads (or eight of an element), a 16-byte
-// store per plane.
+// A warp takes pieces of rows, a lane eight columns at a time: two 16-byte loads (or eight
+// of an element), a 16-byte store per plane.
+constexpr int kPieceCols = 1024;
 template <typename T>
-__global__ void __launch_bounds__(256) planes_kernel(const T *src, long long rows, int cols, long long ld,
-                                                     int planes, unsigned short *dst, long long plane,
-                                                     const long long *keep, int classes, int vec) {
+__global__ void __launch_bounds__(256) planes_kernel(const T *src, long long all, int per_row, int cols,
+                                                     long long ld, int planes, unsigned short *dst,
+                                                     unsigned short *kept, long long plane,
+                                                     const long long *classes, int Ct, int vec) {
     grid_dep_sync();
-    const int c8 = (cols + 7) / 8;
-    const long long pitch = (long long)c8 * 8, all = rows * c8;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long r = i / c8;
-        const int c = (int)(i - r * c8) * 8;
-        float v[8] = {};
-        const bool in = !keep || (unsigned long long)keep[r] < (unsigned long long)classes;
-        const T *s = src + r * ld + c;
-        if (in && vec && c + 8 <= cols) {
-            if constexpr (sizeof(T) == 4) {
-                const float4 a = *reinterpret_cast<const float4 *>(s), b = *reinterpret_cast<const float4 *>(s + 4);
-                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-            } else {
-                const uint4 a = *reinterpret_cast<const uint4 *>(s);
-                const unsigned w[4] = {a.x, a.y, a.z, a.w};
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long pitch = (cols + 7) / 8 * 8;
+    for (long long i = (long long)blockIdx.x * 8 + warp; i < all; i += (long long)gridDim.x * 8) {
+        const long long r = i / per_row;
+        const int first = (int)(i - r * per_row) * kPieceCols, end = min(cols, first + kPieceCols);
+        const bool in = !kept || (unsigned long long)classes[r] < (unsigned long long)Ct;
+        const T *s = src + r * ld;
+#pragma unroll 2
+        for (int c = first + lane * 8; c < end; c += 256) {
+            float v[8];
+            if (vec && c + 8 <= cols) {
+                if constexpr (sizeof(T) == 4) {
+                    const float4 a = *reinterpret_cast<const float4 *>(s + c);
+                    const float4 b = *reinterpret_cast<const float4 *>(s + c + 4);
+                    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+                } else {
+                    const uint4 a = *reinterpret_cast<const uint4 *>(s + c);
+                    const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[2 * j] = __uint_as_float(w[j] << 16);
-                    v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                    for (int j = 0; j < 4; ++j) {
+                        v[2 * j] = __uint_as_float(w[j] << 16);
+                        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = 0.f;
+                    if (c + j < cols) {
+                        if constexpr (sizeof(T) == 4) v[j] = s[c + j];
+                        else v[j] = bf16_to_float(s[c + j]);
+                    }
                 }
             }
-        } else if (in) {
+            unsigned w[3][4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c + j < cols) {
-                    if constexpr (sizeof(T) == 4) v[j] = s[j];
-                    else v[j] = bf16_to_float(s[j]);
-                }
+            for (int j = 0; j < 4; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                if (p >= planes) break;
+                const uint4 q = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+                const long long o = p * plane + r * pitch + c;
+                if (dst) *reinterpret_cast<uint4 *>(dst + o) = q;
+                if (kept) *reinterpret_cast<uint4 *>(kept + o) = in ? q : make_uint4(0, 0, 0, 0);
+            }
         }
-        unsigned w[3][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (planes == 3) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
-            else if (planes == 2) planes2(v[2 * j], v[2 * j + 1], w[0][j], w[1][j]);
-            else w[0][j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p)
-            if (p < planes)
-                *reinterpret_cast<uint4 *>(dst + p * plane + r * pitch + c) =
-                    make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
     }
 }
 
@@ -200,7 +208,8 @@ static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int ma
             const double mma = mmas * (bn / 2 + 10.0);
             const double bytes = (double)P * (kMT + bn / cg) * bk * 2;
             double per = std::max(mma, bytes / 48.0);
-            if (planes == GEMM_F32) per = std::max({mma, (kMT + bn) * 4.0, (kMT + bn) * 128.0 / 23.0});
+            // (A's bytes at the memory's rate, B's planes at the L2's; the converters)
+            if (planes == GEMM_F32) per = std::max({mma, kMT * 128.0 / 21.0, bn * 192.0 / 40.0, 600.0});
             if (P == 3) per = std::max(per, 2.5 * bn + 100.0);
             const double tail = 2500.0 + bn * (kind == GEMM_OUT ? 8.0 : 14.0);
             for (int sp = 1; sp <= std::min({max_splits, kblocks, 64}); ++sp) {
@@ -252,12 +261,13 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     for (int i = 0; i < count; ++i) {
         const GemmProblem &s = ps[i];
         ProblemArgs &p = g.p[i];
-        qcnn_status rc = set_operand(s.a, plan.planes, kMT, s.m, s.k, &p.a, &p.map_a);
+        qcnn_status rc = set_operand(s.a, plan.planes, kMT, s.m, s.k, &p.a, gen ? nullptr : &p.map_a);
         if (rc == QCNN_OK) rc = set_operand(s.b, plan.planes, bnc, s.n, s.k, &p.b, &p.map_b);
         if (rc != QCNN_OK) return rc;
-        a_bytes = std::max(a_bytes, p.a.bytes);
+        if (!gen) a_bytes = std::max(a_bytes, p.a.bytes);
         b_bytes = std::max(b_bytes, p.b.bytes);
-        p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (s.a.mn ? 1u << 15 : 0) | (s.b.mn ? 1u << 16 : 0) |
+        // (A in TMEM has its terms along the columns, however it lay in memory)
+        p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (s.a.mn && !gen ? 1u << 15 : 0) | (s.b.mn ? 1u << 16 : 0) |
                   (uint32_t)(plan.bn >> 3) << 17 | (uint32_t)(kMT * cg >> 4) << 24;
         p.m = s.m;
         p.n = s.n;
@@ -283,8 +293,8 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     g.bn = plan.bn;
     g.b_off = a_bytes;  // (multiples of 1024: 128 rows; 64 rows of 128 bytes)
     g.stage = (unsigned)align_up(a_bytes + b_bytes, 1024);
-    const size_t raw = gen ? (size_t)kRawSlots * cdiv((kMT + plan.bn) * 4, kGenThreads) * 32 * kGenThreads : 0;
-    g.S = (int)std::min<size_t>(gen ? 3 : kStagesMax, (kSmemMax - 1024 - raw) / g.stage);
+    const size_t raw = gen ? (size_t)kRawSlots * kGenWarps * 2048 : 0;
+    g.S = (int)std::min<size_t>(gen ? kGenStagesMax : kStagesMax, (kSmemMax - 1024 - raw) / g.stage);
     if (g.S < 2) return QCNN_ERR_UNSUPPORTED;
     const size_t smem = std::max(kSmemLeast, g.S * (size_t)g.stage + raw + 1024);
     const int ctas = std::min(g.units, num_sms() / cg) * cg;
@@ -297,19 +307,18 @@ qcnn_status launch_gemm_join(const GemmPlan &plan, const GemmProblem &p, cudaStr
 }
 
 qcnn_status launch_planes(const void *src, int bf16, long long rows, int cols, long long ld, int planes,
-                          void *dst, long long plane, const long long *keep, int classes,
-                          cudaStream_t st) {
-    const long long all = rows * ((cols + 7) / 8);
-    if (all == 0) return QCNN_OK;
-    const int grid = (int)std::min<long long>((all + 255) / 256, (long long)num_sms() * 16);
+                          void *dst, void *kept, const long long *classes, int Ct, cudaStream_t st) {
+    const int per_row = cdiv(cols, kPieceCols);
+    const long long all = rows * per_row, plane = rows * pad8(cols);
+    const int grid = (int)std::min<long long>((all + 7) / 8, (long long)num_sms() * 8);
     const int vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
-    unsigned short *d = static_cast<unsigned short *>(dst);
+    unsigned short *d = static_cast<unsigned short *>(dst), *k = static_cast<unsigned short *>(kept);
     if (bf16)
         return launch_pdl(planes_kernel<unsigned short>, dim3(grid), dim3(256), 0, st,
-                          static_cast<const unsigned short *>(src), rows, cols, ld, planes, d, plane, keep,
-                          classes, vec);
-    return launch_pdl(planes_kernel<float>, dim3(grid), dim3(256), 0, st, static_cast<const float *>(src),
-                      rows, cols, ld, planes, d, plane, keep, classes, vec);
+                          static_cast<const unsigned short *>(src), all, per_row, cols, ld, planes, d, k, plane,
+                          classes, Ct, vec);
+    return launch_pdl(planes_kernel<float>, dim3(grid), dim3(256), 0, st, static_cast<const float *>(src), all,
+                      per_row, cols, ld, planes, d, k, plane, classes, Ct, vec);
 }
 
 }  // namespace qcnn

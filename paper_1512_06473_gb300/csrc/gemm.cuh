@@ -16,8 +16,8 @@
 namespace qcnn {
 
 // An operand: planes of bf16, `plane` elements apart, rows of `ld` elements (16-byte
-// multiples); mn: [k][row], else [row][k].  Of the fp32 kernel (GEMM_F32): p is
-// fp32, any ld and alignment, one plane.
+// multiples); mn: [k][row], else [row][k].  A of the fp32 kernel (GEMM_F32): fp32, any
+// ld and alignment.
 struct GemmOperand {
     const void *p = nullptr;
     long long ld = 0, plane = 0;
@@ -66,8 +66,8 @@ struct GemmProblem {
     GemmEpi e;
 };
 
-// planes: 1, 2, 3, or GEMM_F32 (fp32 operands, split into three planes on their way
-// to shared memory).
+// planes: 1, 2, 3, or GEMM_F32 (A in fp32, split on its way to the tensor cores; B in
+// three planes).
 constexpr int GEMM_F32 = 0;
 
 struct GemmPlan {
@@ -94,11 +94,10 @@ qcnn_status launch_gemm_join(const GemmPlan &plan, const GemmProblem &p, cudaStr
 inline long long pad8(long long v) { return (v + 7) / 8 * 8; }
 
 // src [rows][cols] (fp32 or bf16, row stride ld) -> bf16 planes [planes][rows][pad8(cols)],
-// plane elements apart; columns past cols are zero.  keep: per row, a class index: rows
-// where it is outside [0, classes) become zero (null: all rows as they are).
+// rows * pad8(cols) elements apart, to dst (null: not) and to kept (null: not), there with
+// zeros in the rows whose class index in `classes` is outside [0, Ct).
 qcnn_status launch_planes(const void *src, int bf16, long long rows, int cols, long long ld, int planes,
-                          void *dst, long long plane, const long long *keep, int classes,
-                          cudaStream_t st);
+                          void *dst, void *kept, const long long *classes, int Ct, cudaStream_t st);
 
 }  // namespace qcnn
 

@@ -17,23 +17,33 @@
 // multiply-adds (K = 4096: 1.4e-7 of the result).
 //
 // Roles (12 warps): 0 TMA, 1 MMA, 2 TMEM, 4-11 drain and epilogue: two warps per TMEM
-// lane quarter, 16 columns in turn.  GEN adds warps 12-19, which take the place of TMA: they
-// copy fp32 operands of any stride and alignment (cp.async), split them and store the
-// planes.  That costs no pass over the operands, so a product bound by their bytes (few
-// rows) reads them once.
+// lane quarter, 16 columns in turn.
+//
+// GEN: A is fp32 of any stride and alignment (a layer's weights), split on its way, so that
+// a product bound by A's bytes (few rows n) reads them once and writes no planes.  Warps
+// 12-19 copy it (cp.async, kRawSlots - 1 stages ahead: some 64 KB in flight per SM), split
+// it and store the planes to TMEM as the MMAs' A operand: shared memory then carries per
+// stage of 32 terms and 128 columns 32 KB for the copies, 24 KB of B's planes and 48 KB that
+// the twelve MMAs read, 832 clocks of its bandwidth to the 888 of the MMAs.  (With A's
+// planes in shared memory and B split by the same warps it was 1664, and the kernel took
+// 3,500: 115 us for 128 rows of 9216 -> 4096.)
 #pragma once
 
 #include "gemm.cuh"
+
+#include <type_traits>
 
 namespace qcnn {
 namespace {
 
 constexpr int kMT = 128;          // rows of a CTA's tile
-constexpr int kAccCols = 256;     // TMEM columns of an accumulator, of two
+constexpr int kAccCols = 256;     // TMEM columns of an accumulator, of two (GEN: 128)
 constexpr int kStagesMax = 8;
 constexpr int kEpiWarps = 8;
-constexpr int kGenThreads = 256;  // converters
-constexpr int kRawSlots = 3;      // GEN: raw copies in flight, stages
+constexpr int kGenWarps = 8;      // converters
+constexpr int kRawSlots = 5;      // GEN: stages of raw copies, 2 KB per warp each
+constexpr int kGenCols = 48;      // TMEM columns of a stage's A: 3 planes x 32 terms
+constexpr int kGenStagesMax = 5;  // (512 - 2 * 128) / 48
 constexpr unsigned kPolls = 1u << 22;
 
 // An operand of a problem as the kernel sees it.
@@ -235,119 +245,186 @@ __device__ __forceinline__ void tmem_ld16(unsigned taddr, float (&v)[16]) {
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void tmem_st16(unsigned taddr, const float (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n" ::"r"(taddr),
+        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]),
+        "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+        : "memory");
+}
+
 // ------------------------------------------------------------------ epilogue
+// The loops below are over 16 columns of a lane, unrolled, with what does not change
+// decided outside them: inside, a decision per element kept each load behind the one
+// before (a tile with a residual took 123 us instead of its product's 52).
+
 // 16 columns of a lane to out[n0 + i][m] (m in range), row by row: the warp's lanes are
-// neighbours.
+// neighbours.  left: columns that exist.
 __device__ __forceinline__ void store16(void *out, int type, long long ld, long long plane, int m, int n0,
-                                        int n_end, const float (&v)[16]) {
-    long long o = (long long)n0 * ld + m;
+                                        int left, const float (&v)[16]) {
+    const long long o = (long long)n0 * ld + m;
     if (type == GEMM_T_F32) {
         float *p = static_cast<float *>(out) + o;
 #pragma unroll
         for (int i = 0; i < 16; ++i, p += ld)
-            if (n0 + i < n_end) *p = v[i];
+            if (i < left) *p = v[i];
         return;
     }
     unsigned short *p = static_cast<unsigned short *>(out) + o;
+    auto put = [&](unsigned short *d, const unsigned (&w)[8]) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 2, p += 2 * ld) {
-        unsigned w[3];
-        if (type == GEMM_T_BF16) w[0] = pack_bf16x2(v[i], v[i + 1]);
-        else if (type == GEMM_T_PLANES2) planes2(v[i], v[i + 1], w[0], w[1]);
-        else planes3(v[i], v[i + 1], w[0], w[1], w[2]);
-        const int np = type == GEMM_T_BF16 ? 1 : type;
-#pragma unroll
-        for (int j = 0; j < 3; ++j) {
-            if (j >= np) break;
-            if (n0 + i < n_end) p[j * plane] = (unsigned short)w[j];
-            if (n0 + i + 1 < n_end) p[j * plane + ld] = (unsigned short)(w[j] >> 16);
+        for (int i = 0; i < 8; ++i, d += 2 * ld) {
+            if (2 * i < left) d[0] = (unsigned short)w[i];
+            if (2 * i + 1 < left) d[ld] = (unsigned short)(w[i] >> 16);
         }
+    };
+    unsigned w0[8], w1[8], w2[8];
+    if (type == GEMM_T_BF16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w0[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        put(p, w0);
+    } else if (type == GEMM_T_PLANES2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) planes2(v[2 * i], v[2 * i + 1], w0[i], w1[i]);
+        put(p, w0);
+        put(p + plane, w1);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
+        put(p, w0);
+        put(p + plane, w1);
+        put(p + 2 * plane, w2);
+    }
+}
+// 16 columns of a lane of a matrix; the last that exists again past the end.
+__device__ __forceinline__ void load16(const void *src, int type, long long ld, long long plane, int m, int n0,
+                                       int left, float (&v)[16]) {
+    const long long o = (long long)n0 * ld + m;
+    if (type == GEMM_T_F32) {
+        const float *p = static_cast<const float *>(src) + o;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            v[i] = *p;
+            if (i + 1 < left) p += ld;
+        }
+        return;
+    }
+    const unsigned short *p = static_cast<const unsigned short *>(src) + o;
+    auto get = [&](const unsigned short *d, float (&r)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            r[i] = bf16_to_float(*d);
+            if (i + 1 < left) d += ld;
+        }
+    };
+    if (type == GEMM_T_BF16) {
+        get(p, v);
+        return;
+    }
+    float w[16];
+    if (type == GEMM_T_PLANES2) {
+        get(p, v);
+        get(p + plane, w);
+    } else {
+        float x[16];
+        get(p, v);
+        get(p + plane, w);
+        get(p + 2 * plane, x);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] += x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] += w[i];
+}
+__device__ __forceinline__ void act16(float (&v)[16], int act) {
+    if (act == QCNN_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = act_apply(v[i], QCNN_ACT_RELU);
+    } else if (act == QCNN_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = act_apply(v[i], QCNN_ACT_GELU);
+    } else if (act == QCNN_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = act_apply(v[i], QCNN_ACT_SILU);
     }
 }
 
-// OUT and SYM: sums v of lane m, columns n0 .. n0 + 15.
+// OUT and SYM: sums v of lane m (in range), columns n0 .. n0 + left - 1; r: what add has
+// there.
 template <int KIND>
-__device__ __forceinline__ void finish_out(const GemmEpi &e, int m, int m_end, int n0, int n_end,
-                                           float alpha, float bias, float (&v)[16]) {
-    if (m >= m_end) return;
+__device__ __forceinline__ void finish_out(const GemmEpi &e, int m, int n0, int left, float alpha, float bias,
+                                           float (&v)[16], const float (&r)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = fmaf(alpha, v[i], bias);
-    if (e.pre) store16(e.pre, e.out_type, e.ldp, 0, m, n0, n_end, v);
-    if (e.act != QCNN_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = act_apply(v[i], e.act);
-    }
+    if (KIND == GEMM_OUT && e.pre) store16(e.pre, e.out_type, e.ldp, 0, m, n0, left, v);
+    if constexpr (KIND == GEMM_OUT) act16(v, e.act);
     if (e.add) {
-        const long long o = (long long)n0 * e.lda + m;
-        float r[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            r[i] = n0 + i < n_end ? load_as(e.add, e.add_type, o + i * e.lda, e.add_plane) : 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = fmaf(e.beta, r[i], v[i]);
     }
     if constexpr (KIND == GEMM_OUT) {
-        store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, n_end, v);
+        store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, left, v);
     } else {
         // one value for both places: this tile's where m >= n
-        const int end = min(n_end, m + 1);
-        if (n0 >= end) return;
-        store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, end, v);
+        left = min(left, m + 1 - n0);
+        if (left <= 0) return;
+        store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, left, v);
         unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)m * e.ldo + n0;
+        auto put = [&](unsigned short *d, const unsigned (&w)[8]) {
+            if (left >= 16) {  // (rows of planes: 16-byte multiples)
+                *reinterpret_cast<uint4 *>(d) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(d + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+            } else {
 #pragma unroll
-        for (int h = 0; h < 16; h += 8) {  // (rows of planes: 16-byte multiples)
-            unsigned w[3][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (e.out_type == GEMM_T_PLANES2) planes2(v[h + 2 * i], v[h + 2 * i + 1], w[0][i], w[1][i]);
-                else planes3(v[h + 2 * i], v[h + 2 * i + 1], w[0][i], w[1][i], w[2][i]);
+                for (int i = 0; i < 16; ++i)
+                    if (i < left) d[i] = (unsigned short)(w[i / 2] >> (i & 1) * 16);
             }
+        };
+        unsigned w0[8], w1[8], w2[8];
+        if (e.out_type == GEMM_T_PLANES2) {
 #pragma unroll
-            for (int j = 0; j < 3; ++j) {
-                if (j >= e.out_type) break;
-                unsigned short *d = p + j * e.out_plane + h;
-                if (n0 + h + 8 <= end) {
-                    *reinterpret_cast<uint4 *>(d) = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
-                } else {
+            for (int i = 0; i < 8; ++i) planes2(v[2 * i], v[2 * i + 1], w0[i], w1[i]);
+        } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (n0 + h + i < end) d[i] = (unsigned short)(w[j][i / 2] >> (i & 1) * 16);
-                }
-            }
+            for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
+            put(p + 2 * e.out_plane, w2);
         }
+        put(p, w0);
+        put(p + e.out_plane, w1);
     }
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
+// 2^x to 2 ulp; results below 2^-126 are zero.
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
 // Running maximum and sum of exp of a lane.  A maximum of -inf has no sum (and adds
 // nothing: exp of -inf minus -inf is left out).
 struct RunningSum {
     float top = -INFINITY, sum = 0.f;
 };
-__device__ __forceinline__ void running_join(RunningSum &a, float top, float sum) {
-    const float t = fmaxf(a.top, top);
-    if (t == -INFINITY) {
-        a.sum += sum;  // (NaN stays NaN)
-        return;
-    }
-    a.sum = a.sum * exp2f((a.top - t) * kLog2e) + sum * exp2f((top - t) * kLog2e);
-    a.top = t;
-}
-__device__ __forceinline__ void stats16(const GemmEpi &e, RunningSum &s, int n0, int n_end, int target,
-                                        float *target_logit, float (&v)[16]) {
-    float top = -INFINITY;
+// bias: of the 16 classes, -inf past the last.
+__device__ __forceinline__ void stats16(RunningSum &s, int n0, int target, float *target_logit,
+                                        const float *bias, float (&v)[16]) {
+    float t0 = s.top, t1 = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        v[i] = n0 + i < n_end ? (e.bias ? v[i] + e.bias[n0 + i] : v[i]) : -INFINITY;
-        top = fmaxf(top, v[i]);
+    for (int i = 0; i < 16; i += 4) {
+        const float4 b = *reinterpret_cast<const float4 *>(bias + i);
+        v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
+        t0 = fmaxf(t0, fmaxf(v[i], v[i + 1]));
+        t1 = fmaxf(t1, fmaxf(v[i + 2], v[i + 3]));
     }
     if ((unsigned)(target - n0) < 16u) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (target == n0 + i) *target_logit = v[i];
     }
-    top = fmaxf(top, s.top);
+    const float top = fmaxf(t0, t1);
     if (top == -INFINITY) {
         // all -inf (nothing to add) or NaN (which fmaxf passes over)
 #pragma unroll
@@ -359,55 +436,31 @@ __device__ __forceinline__ void stats16(const GemmEpi &e, RunningSum &s, int n0,
     float a0 = 0.f, a1 = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-        a0 += exp2f(fmaf(v[i], kLog2e, -shift));
-        a1 += exp2f(fmaf(v[i + 1], kLog2e, -shift));
+        a0 += ex2(fmaf(v[i], kLog2e, -shift));
+        a1 += ex2(fmaf(v[i + 1], kLog2e, -shift));
     }
-    s.sum = (s.top == -INFINITY ? s.sum : s.sum * exp2f(fmaf(s.top, kLog2e, -shift))) + (a0 + a1);
+    s.sum = (s.top == -INFINITY ? s.sum : s.sum * ex2(fmaf(s.top, kLog2e, -shift))) + (a0 + a1);
     s.top = top;
 }
 
-// Gradient of a class (lane m) for 16 rows.
-__device__ __forceinline__ void dlogits16(const GemmEpi &e, int m, int m_end, int n0, int n_end, float bias,
-                                          float &col, float (&v)[16]) {
+// Gradient of a class (lane m) for 16 rows; rows: theirs, without a class past the last.
+__device__ __forceinline__ void dlogits16(const GemmEpi &e, int m, int m_end, int n0, int left, float bias,
+                                          const float4 *rows, float &col, float (&v)[16]) {
+    const int c = e.class0 + m;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        float d = 0.f;
-        if (n0 + i < n_end) {
-            const float4 r = e.rows[n0 + i];
-            const int target = __float_as_int(r.z);
-            const float p = exp2f((v[i] + bias - r.x) * kLog2e);
-            // (a row without a class is zero, whatever its logits are)
-            if (target >= 0) d = r.y * (target == e.class0 + m ? p - 1.f : p);
-        }
-        v[i] = d;
-        col += d;
+        const float4 r = rows[i];
+        const int target = __float_as_int(r.z);
+        float p = ex2((v[i] + bias - r.x) * kLog2e);
+        if (target == c) p -= 1.f;
+        // (a row without a class is zero, whatever its logits are)
+        v[i] = target >= 0 ? r.y * p : 0.f;
+        col += v[i];
     }
-    if (m < m_end) store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, n_end, v);
+    if (m < m_end) store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, left, v);
 }
 
 // ---------------------------------------------------------------------- GEN
-// A thread's copies of a stage: 8 neighbouring elements of one row (32 bytes), items
-// kGenThreads apart.  Rows of k: item = row * 4 + k / 8; rows of m: item = k * (rows / 8)
-// + row / 8.
-struct GenItem {
-    unsigned dst;     // bytes into the operand's stage part, plane 0
-    int row, k;       // first element
-};
-__device__ __forceinline__ GenItem gen_item(const OpArgs &o, int rows8, int it) {
-    GenItem r;
-    if (!o.mn) {
-        const int row = it >> 2, c = it & 3;
-        r.row = row;
-        r.k = c * 8;
-        r.dst = row * 64 + ((c ^ (row >> 1 & 3)) << 4);  // 64-byte swizzle
-    } else {
-        const int k = it / rows8, c = it - k * rows8;
-        r.row = c * 8;
-        r.k = k;
-        r.dst = (c >> 3) * o.group_bytes + k * 128 + (((c & 7) ^ (k & 7)) << 4);  // 128-byte swizzle
-    }
-    return r;
-}
 __device__ __forceinline__ void cp_async16_part(unsigned dst, const void *src, unsigned bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes)
                  : "memory");
@@ -416,32 +469,55 @@ __device__ __forceinline__ void cp_async4_part(unsigned dst, const void *src, un
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(bytes)
                  : "memory");
 }
-// Elements i .. of the item to raw (its two halves 16 * kGenThreads bytes apart); what is
-// outside the matrix is zero.
-__device__ __forceinline__ void gen_copy(const OpArgs &o, int row, int k, int k_end, unsigned raw) {
-    // along the contiguous index: first element, and how many of the eight exist
-    const int first = o.mn ? row : k, line = o.mn ? k : row;
-    const int have = (o.mn ? o.rows : k_end) - first;
-    const bool in = line < (o.mn ? k_end : o.rows) && have > 0;
-    const float *s = in ? o.src + (long long)line * o.ld + first : o.src;
-    const int n = in ? min(have, 8) : 0;
-    if (o.vec) {
-        cp_async16_part(raw, n > 0 ? s : o.src, 4 * min(n, 4));
-        cp_async16_part(raw + 16 * kGenThreads, n > 4 ? s + 4 : o.src, n > 4 ? 4 * (n - 4) : 0);
+// n (may be negative, or more) of four elements from src to dst; the others become zero.
+// none: any address that may be read.
+__device__ __forceinline__ void copy4(unsigned dst, const float *src, int n, bool vec, const float *none) {
+    n = max(0, min(n, 4));
+    if (vec) {
+        cp_async16_part(dst, n ? src : none, 4 * n);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            cp_async4_part(raw + (i >> 2) * 16 * kGenThreads + (i & 3) * 4, i < n ? s + i : o.src, i < n ? 4 : 0);
+        for (int i = 0; i < 4; ++i) cp_async4_part(dst + 4 * i, i < n ? src + i : none, i < n ? 4 : 0);
     }
 }
+__device__ __forceinline__ void mma_ts(unsigned d, unsigned a, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"((unsigned)acc)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned (&v)[8]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+        : "memory");
+}
+template <int REGS>
+__device__ __forceinline__ void regs_dec() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(REGS));
+}
+template <int REGS>
+__device__ __forceinline__ void regs_inc() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(REGS));
+}
+// GEN: registers per thread of the five warpgroups (roles, two of drains, two of
+// converters), of 5 x 96 at launch
+constexpr int kRegsRoles = 80, kRegsDrain = 120, kRegsConvert = 80;
+static_assert(kRegsRoles + 2 * kRegsDrain + 2 * kRegsConvert <= 5 * 96, "register pool");
 
 // ------------------------------------------------------------------- kernel
 template <int P, int KIND, int CG, bool GEN>
 __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
     constexpr int BK = P == 1 ? 64 : 32, KS = BK / 16;
     constexpr bool DRAIN = P == 3;  // a stage's sum at a time
+    constexpr int ACC = GEN ? 128 : kAccCols;
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ Shared sh;
+    // what belongs to the 16 columns that a warp is at: bias (STATS), rows (DLOGITS)
+    using Column = std::conditional_t<KIND == GEMM_DLOGITS, float4, float>;
+    constexpr bool COLUMNS = KIND == GEMM_STATS || KIND == GEMM_DLOGITS;
+    __shared__ __align__(16) Column columns[COLUMNS ? kEpiWarps : 1][2][16];
     unsigned char *const smem = smem_raw + (-smem_addr(smem_raw) & 1023u);  // (swizzle atoms)
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -451,7 +527,7 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
 
     if (tid == 0) {
         for (int i = 0; i < g.S; ++i) {
-            mbar_init(&sh.full[i], GEN ? kGenThreads : 1);
+            mbar_init(&sh.full[i], GEN ? 1 + kGenWarps : 1);
             mbar_init(&sh.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -471,8 +547,13 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
     const unsigned tmem = sh.tmem;
     grid_dep_sync();
 
+    if constexpr (GEN) {
+        if (warp < 4) regs_dec<kRegsRoles>();
+        else if (warp < 12) regs_inc<kRegsDrain>();
+        else regs_dec<kRegsConvert>();
+    }
     if (warp == 0) {
-        if constexpr (!GEN) {
+        {
             // ----------------------------------------------------------- TMA
             if (elect_one()) {
                 int slot = 0, issued = 0;
@@ -483,14 +564,15 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
                     const ProblemArgs &p = g.p[t.q];
                     const int m0 = (t.mt * CG + (int)rank) * kMT;
                     const int bn = g.bn / CG, n0 = t.nt * g.bn + (int)rank * bn;
-                    const unsigned bytes = (p.a.bytes + p.b.bytes) * CG;
+                    const unsigned bytes = ((GEN ? 0 : p.a.bytes) + p.b.bytes) * CG;
                     for (int kb = t.kb0; kb < t.kb1; ++kb) {
                         if (!(ok = wait_one(sh, &sh.empty[slot], par ^ 1))) break;
                         uint64_t *const full = &sh.full[slot];
                         if (rank == 0) arrive_expect(full, bytes);
                         const unsigned a = smem_addr(smem) + slot * g.stage, b = a + g.b_off;
                         const int k = kb * BK;
-                        if (p.a.mn) {
+                        if (GEN) {
+                        } else if (p.a.mn) {
                             tma_load<CG>(a, &p.map_a, m0, k, full);
                             tma_load<CG>(a + p.a.group_bytes, &p.map_a, m0 + 64, k, full);
                         } else {
@@ -537,13 +619,15 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
                     }
                     if (!(ok = wait_one(sh, &sh.full[slot], par))) break;
                     tc_fence_after_sync();
-                    const unsigned d = tmem + (use & 1) * kAccCols;
+                    const unsigned d = tmem + (use & 1) * ACC;
+                    [[maybe_unused]] const unsigned at = tmem + 2 * ACC + slot * kGenCols;
                     const uint64_t a = da + slot * (g.stage >> 4), b = db + slot * (g.stage >> 4);
                     bool acc = !fresh;
                     auto product = [&](int i, int j) {
 #pragma unroll
                         for (int s = 0; s < KS; ++s) {
-                            mma_ss<CG>(d, a + i * pa + s * ka, b + j * pb + s * kb_, idesc, acc);
+                            if constexpr (GEN) mma_ts(d, at + i * 16 + s * 8, b + j * pb + s * kb_, idesc, acc);
+                            else mma_ss<CG>(d, a + i * pa + s * ka, b + j * pb + s * kb_, idesc, acc);
                             acc = true;
                         }
                     };
@@ -593,34 +677,22 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
             const ProblemArgs &p = g.p[t.q];
             const GemmEpi &e = p.e;
             const int m = (t.mt * CG + (int)rank) * kMT + quarter * 32 + lane, n0 = t.nt * g.bn;
-            float bias = 0.f;
-            RunningSum run;
-            int target = -1;
-            float col = 0.f;
+            const bool in = m < p.m;
+            [[maybe_unused]] float bias = 0.f, col = 0.f;
             [[maybe_unused]] const float alpha = KIND == GEMM_OUT && e.alpha_ptr ? *e.alpha_ptr : e.alpha;
+            [[maybe_unused]] RunningSum run;
+            [[maybe_unused]] int target = -1;
+            [[maybe_unused]] const bool adds = in && e.add && !e.partial;
             if constexpr (KIND == GEMM_STATS) {
-                if (m < p.m) {
+                if (in) {
                     const long long c = e.targets[m];
                     target = c >= 0 && c < p.n ? (int)c : -1;
                 }
             } else {
-                if (e.bias && m < p.m && !e.partial) bias = e.bias[m];
+                if (e.bias && in && !e.partial) bias = e.bias[m];
             }
-            auto chunk = [&](int n, float (&v)[16]) {
-                if constexpr (KIND == GEMM_STATS) {
-                    stats16(e, run, n, p.n, target, e.target_logit + m, v);
-                } else if constexpr (KIND == GEMM_DLOGITS) {
-                    dlogits16(e, m, p.m, n, p.n, bias, col, v);
-                } else {
-                    if (KIND == GEMM_OUT && e.partial) {
-                        if (m < p.m)
-                            store16(e.partial + (long long)t.split * p.n * p.m, GEMM_T_F32, p.m, 0, m, n,
-                                    p.n, v);
-                    } else {
-                        finish_out<KIND>(e, m, p.m, n, p.n, alpha, bias, v);
-                    }
-                }
-            };
+            // the sums of the tile, in TMEM at tl + buf * ACC
+            unsigned buf = use & 1;
             if constexpr (DRAIN) {
                 constexpr int CH = GEN ? 4 : 8;  // chunks of a warp at most
                 float acc[CH][16];
@@ -629,121 +701,179 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
                 for (int kb = t.kb0; kb < t.kb1; ++kb, ++use) {
-                    const unsigned buf = use & 1;
+                    buf = use & 1;
                     if (!(ok = wait_warp(sh, &sh.tfull[buf], use >> 1 & 1))) break;
                     tc_fence_after_sync();
 #pragma unroll
                     for (int c = 0; c < CH; ++c) {
                         if (2 * c + half < chunks) {
                             float v[16];
-                            tmem_ld16(tl + buf * kAccCols + (2 * c + half) * 16, v);
+                            tmem_ld16(tl + buf * ACC + (2 * c + half) * 16, v);
 #pragma unroll
                             for (int i = 0; i < 16; i += 2)
                                 add2(acc[c][i], acc[c][i + 1], v[i], v[i + 1]);
                         }
                     }
-                    release(buf);
+                    // (the last: its columns take the sums, for a loop over chunks that is
+                    // not unrolled: instructions fetched once per tile cost more)
+                    if (kb + 1 < t.kb1) release(buf);
                 }
                 if (!ok) break;
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
-                    if (2 * c + half < chunks) chunk(n0 + (2 * c + half) * 16, acc[c]);
+                    if (2 * c + half < chunks) tmem_st16(tl + buf * ACC + (2 * c + half) * 16, acc[c]);
+                asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
             } else {
-                const unsigned buf = use & 1;
-                if (!(ok = wait_warp(sh, &sh.tfull[buf], use >> 1 & 1))) break;
-                tc_fence_after_sync();
-                for (int c = half; c < chunks; c += 2) {
-                    float v[16];
-                    tmem_ld16(tl + buf * kAccCols + c * 16, v);
-                    chunk(n0 + c * 16, v);
-                }
-                release(buf);
                 ++use;
             }
+            // (what a chunk of columns needs from memory is fetched one chunk ahead)
+            float add[16];
+            [[maybe_unused]] Column column = {};
+            auto fetch = [&](int c) {
+                if constexpr (COLUMNS) {
+                    const int n = n0 + c * 16 + (lane & 15);
+                    const bool is = c < chunks && n < p.n;
+                    if constexpr (KIND == GEMM_STATS)
+                        column = !is ? -INFINITY : e.bias ? e.bias[n] : 0.f;
+                    else
+                        column = is ? e.rows[n] : make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
+                }
+                if constexpr (KIND == GEMM_OUT || KIND == GEMM_SYM) {
+                    const int left = p.n - (n0 + c * 16);
+                    if (adds && c < chunks && left > 0)
+                        load16(e.add, e.add_type, e.lda, e.add_plane, m, n0 + c * 16, left, add);
+                }
+            };
+            fetch(half);
+            if constexpr (!DRAIN) {
+                if (!(ok = wait_warp(sh, &sh.tfull[buf], (use - 1) >> 1 & 1))) break;
+                tc_fence_after_sync();
+            }
+#pragma unroll 1
+            for (int c = half; c < chunks; c += 2) {
+                const int n = n0 + c * 16, left = p.n - n;
+                float v[16], r[16];
+                if constexpr (KIND == GEMM_OUT || KIND == GEMM_SYM) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) r[i] = add[i];
+                    fetch(c + 2);
+                }
+                [[maybe_unused]] Column *const cols = columns[COLUMNS ? warp - 4 : 0][c >> 1 & 1];
+                if constexpr (COLUMNS) {
+                    if (lane < 16) cols[lane] = column;
+                    __syncwarp();
+                    fetch(c + 2);
+                }
+                tmem_ld16(tl + buf * ACC + c * 16, v);
+                if constexpr (KIND == GEMM_STATS) {
+                    stats16(run, n, target, e.target_logit + m, cols, v);
+                } else if constexpr (KIND == GEMM_DLOGITS) {
+                    dlogits16(e, m, p.m, n, left, bias, cols, col, v);
+                } else if (in && left > 0) {
+                    if (KIND == GEMM_OUT && e.partial)
+                        store16(e.partial + (long long)t.split * p.n * p.m, GEMM_T_F32, p.m, 0, m, n, left, v);
+                    else
+                        finish_out<KIND>(e, m, n, left, alpha, bias, v, r);
+                }
+            }
+            release(buf);
             if constexpr (KIND == GEMM_STATS) {
-                if (m < p.m) e.stats[(long long)(t.nt * 2 + half) * p.m + m] = make_float2(run.top, run.sum);
+                if (in) e.stats[(long long)(t.nt * 2 + half) * p.m + m] = make_float2(run.top, run.sum);
             }
             if constexpr (KIND == GEMM_DLOGITS) {
-                if (m < p.m) e.col_part[(long long)(t.nt * 2 + half) * e.ld_col + m] = col;
+                if (in) e.col_part[(long long)(t.nt * 2 + half) * e.ld_col + m] = col;
             }
         }
     } else if (GEN && warp >= 12) {
         // ------------------------------------------ copy, split, store planes
-        const int gt = tid - 384;
-        unsigned char *const raw0 = smem + (size_t)g.S * g.stage + gt * 16;
+        // A warp has 32 rows (its TMEM lanes) x 16 terms of every stage, and copies them
+        // itself: no barrier between copying and splitting.  Rows of k: [32][16] floats, the
+        // 16-byte pieces of a row permuted so that eight lanes of neighbouring rows read
+        // from all banks; rows of m: [16][32].
+        const int quarter = warp & 3, half = (warp - 12) >> 2;
         const ProblemArgs &p = g.p[0];
-        const int a_items = kMT * 4, items = a_items + g.bn * 4;  // 32 terms of 128 + bn rows
-        constexpr int IT = 4;                                      // a thread's at most (bn <= 128)
-        const unsigned raw_slot = (unsigned)((items + kGenThreads - 1) / kGenThreads) * 32 * kGenThreads;
-        // the stages of this CTA, in order: raw copies run kRawSlots - 1 ahead
-        int cu = first_unit, ckb = 0;  // next to copy: unit and block
-        Tile ct = {};
-        bool cok = cu < g.units;
-        if (cok) {
-            ct = tile_of<KIND, CG>(g, cu);
-            ckb = ct.kb0;
-        }
-        int cslot = 0;
+        const bool mn = p.a.mn, vec = p.a.vec;
+        const float *const base = p.a.src;
+        const long long ld = p.a.ld;
+        const unsigned raw = smem_addr(smem) + g.S * g.stage + (warp - 12) * (kRawSlots * 2048);
+        // this lane's four copies per stage: the first's row and term, the others 8 rows (rows of
+        // m: 4 terms) on
+        const int row0 = mn ? (lane & 7) * 4 : lane >> 2, k0 = half * 16 + (mn ? lane >> 3 : (lane & 3) * 4);
+        const long long gap = mn ? 4 * ld : 8 * ld, step_k = mn ? 32 * ld : 32;
+        // (rows of k: piece (lane & 3) of row r lies at ((lane & 3) ^ (r >> 1 & 3)))
+        const unsigned dst0 = mn ? (lane >> 3) * 128 + (lane & 7) * 16
+                                 : (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3 & 3)) << 4);
+        const float *src = base;
+        int cu = first_unit, ck = 0, ckb = 0, ckb1 = 0, cslot = 0, rows = 0;
+        auto open_tile = [&]() {
+            const Tile t = tile_of<KIND, CG>(g, cu);
+            ckb = t.kb0;
+            ckb1 = t.kb1;
+            ck = t.kb0 * BK + k0;
+            const int row = t.mt * kMT + quarter * 32 + row0;
+            rows = p.m - row;  // that exist from this lane's first on
+            src = base + (mn ? (long long)ck * ld + row : (long long)row * ld + ck);
+        };
+        if (cu < g.units) open_tile();
         auto copy_next = [&]() {
-            if (cok) {
-                const int m0 = ct.mt * kMT, n0 = ct.nt * g.bn, k0 = ckb * BK;
-                const unsigned raw = smem_addr(raw0) + cslot * raw_slot;
+            if (cu < g.units) {
+                const unsigned d = raw + cslot * 2048 + dst0;
+                const int k_in = p.k - ck;
+                const float *s = src;
 #pragma unroll
-                for (int j = 0; j < IT; ++j) {
-                    const int it = gt + j * kGenThreads;
-                    if (it < items) {
-                        const bool is_a = it < a_items;
-                        const OpArgs &o = is_a ? p.a : p.b;
-                        const GenItem x = gen_item(o, (is_a ? kMT : g.bn) / 8, is_a ? it : it - a_items);
-                        gen_copy(o, (is_a ? m0 : n0) + x.row, k0 + x.k, p.k, raw + j * 32 * kGenThreads);
-                    }
+                for (int j = 0; j < 4; ++j, s += gap) {
+                    // (8 rows on, the permutation is the same: 4 pairs of rows)
+                    if (mn) copy4(d + j * 512, s, k_in > 4 * j ? rows : 0, vec, base);
+                    else copy4(d + j * 512, s, rows > 8 * j ? k_in : 0, vec, base);
                 }
-                if (++ckb == ct.kb1) {
+                src += step_k;
+                ck += BK;
+                if (++ckb == ckb1) {
                     cu += step;
-                    if ((cok = cu < g.units)) {
-                        ct = tile_of<KIND, CG>(g, cu);
-                        ckb = ct.kb0;
-                    }
+                    if (cu < g.units) open_tile();
                 }
                 if (++cslot == kRawSlots) cslot = 0;
             }
             cp_async_commit();
         };
         for (int i = 0; i < kRawSlots - 1; ++i) copy_next();
+        const unsigned a_dst = tmem + 2 * ACC + ((unsigned)(quarter * 32) << 16) + half * 8;
         int slot = 0, rslot = 0;
         unsigned par = 0;
         bool ok = true;
         for (int u = first_unit; u < g.units && ok; u += step) {
             const Tile t = tile_of<KIND, CG>(g, u);
             for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                copy_next();
-                cp_async_wait<kRawSlots - 1>();
-                if (!(ok = wait_warp(sh, &sh.empty[slot], par ^ 1))) break;
-                const unsigned char *raw = raw0 + rslot * raw_slot;
-                unsigned char *const st = smem + (size_t)slot * g.stage;
+                cp_async_wait<kRawSlots - 2>();
+                __syncwarp();
+                const unsigned r = raw + rslot * 2048;
+                float v[16];
+                if (mn) {
 #pragma unroll
-                for (int j = 0; j < IT; ++j) {
-                    const int it = gt + j * kGenThreads;
-                    if (it < items) {
-                        const bool is_a = it < a_items;
-                        const OpArgs &o = is_a ? p.a : p.b;
-                        const GenItem x = gen_item(o, (is_a ? kMT : g.bn) / 8, is_a ? it : it - a_items);
-                        const float4 f = *reinterpret_cast<const float4 *>(raw + j * 32 * kGenThreads);
-                        const float4 h = *reinterpret_cast<const float4 *>(raw + j * 32 * kGenThreads +
-                                                                          16 * kGenThreads);
-                        uint4 w0, w1, w2;
-                        planes3(f.x, f.y, w0.x, w1.x, w2.x);
-                        planes3(f.z, f.w, w0.y, w1.y, w2.y);
-                        planes3(h.x, h.y, w0.z, w1.z, w2.z);
-                        planes3(h.z, h.w, w0.w, w1.w, w2.w);
-                        unsigned char *d = st + (is_a ? 0u : g.b_off) + x.dst;
-                        *reinterpret_cast<uint4 *>(d) = w0;
-                        *reinterpret_cast<uint4 *>(d + o.plane * 16) = w1;
-                        *reinterpret_cast<uint4 *>(d + o.plane * 32) = w2;
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(r + i * 128 + lane * 4));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+                                     : "=f"(v[4 * i]), "=f"(v[4 * i + 1]), "=f"(v[4 * i + 2]), "=f"(v[4 * i + 3])
+                                     : "r"(r + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)));
                 }
-                fence_async_smem();
-                arrive(&sh.full[slot]);
+                unsigned w0[8], w1[8], w2[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
+                __syncwarp();  // (all have read: the slot may be copied to)
+                copy_next();
+                if (!(ok = wait_warp(sh, &sh.empty[slot], par ^ 1))) break;
+                tc_fence_after_sync();
+                const unsigned d = a_dst + slot * kGenCols;
+                tmem_st8(d, w0);
+                tmem_st8(d + 16, w1);
+                tmem_st8(d + 32, w2);
+                asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) arrive(&sh.full[slot]);
                 if (++slot == g.S) {
                     slot = 0;
                     par ^= 1;

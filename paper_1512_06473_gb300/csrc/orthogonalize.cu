@@ -15,67 +15,82 @@
 namespace qcnn {
 namespace {
 
-constexpr int kNormBlocks = 304;
+constexpr int kNormBlocks = 608;
 
+// The eight (or fewer) columns from c of a row in fp32, zeros past the last; vec: 16-byte
+// loads are possible.
 template <typename T>
-__device__ __forceinline__ float value(const T *p) {
-    if constexpr (sizeof(T) == 4) return *p;
-    else return bf16_to_float(*p);
-}
-
-// Sums of squares by CTA: of values above 2^48 scaled by 2^-64, and of the others (whose
-// squares neither overflow nor, where they count beside eps, vanish).
-constexpr float kLarge = 281474976710656.f, kLargeScale = 5.421010862427522e-20f;
-template <typename T>
-__global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, long long rows, int cols, int vec,
-                                                   double2 *part) {
-    __shared__ double2 red[8];
-    grid_dep_sync();
-    float small = 0.f, large = 0.f;
-    double dsmall = 0., dlarge = 0.;
-    const int c4 = (cols + 3) / 4;
-    const long long all = rows * c4;
-    int n = 0;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long r = i / c4;
-        const int c = (int)(i - r * c4) * 4;
-        const T *s = g + r * ldg + c;
-        float v[4];
-        if (vec && c + 4 <= cols) {
-            if constexpr (sizeof(T) == 4) {
-                const float4 a = *reinterpret_cast<const float4 *>(s);
-                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-            } else {
-                const uint2 a = *reinterpret_cast<const uint2 *>(s);
-                v[0] = __uint_as_float(a.x << 16), v[1] = __uint_as_float(a.x & 0xffff0000u);
-                v[2] = __uint_as_float(a.y << 16), v[3] = __uint_as_float(a.y & 0xffff0000u);
-            }
+__device__ __forceinline__ void row8(const T *row, int c, int cols, bool vec, float (&v)[8]) {
+    if (vec && c + 8 <= cols) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = *reinterpret_cast<const float4 *>(row + c), b = *reinterpret_cast<const float4 *>(row + c + 4);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
         } else {
+            const uint4 a = *reinterpret_cast<const uint4 *>(row + c);
+            const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = c + j < cols ? value(s + j) : 0.f;
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] = __uint_as_float(w[j] << 16);
+                v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            }
         }
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool big = fabsf(v[j]) > kLarge;
-            const float w = big ? v[j] * kLargeScale : v[j];
-            if (big) large = fmaf(w, w, large);
-            else small = fmaf(w, w, small);  // (NaN too)
-        }
-        if (++n == 16) {  // (runs of 64 squares in fp32)
-            dsmall += small;
-            dlarge += large;
-            small = large = 0.f;
-            n = 0;
+        for (int j = 0; j < 8; ++j) {
+            float x = 0.f;
+            if (c + j < cols) {
+                if constexpr (sizeof(T) == 4) x = row[c + j];
+                else x = bf16_to_float(row[c + j]);
+            }
+            v[j] = x;
         }
     }
-    dsmall += small;
-    dlarge += large;
+}
+
+// Both passes over G: a warp takes pieces of rows (of at most kPieceCols columns), a lane
+// eight columns at a time.
+constexpr int kPieceCols = 2048;
+struct Pieces {
+    long long rows, all;  // rows, and rows x pieces of a row
+    int cols, per_row;
+};
+
+// Sums of squares by CTA: of values above 2^48 scaled by 2^-64, and of the others (whose
+// squares neither overflow nor, where they count beside eps, vanish).  A lane's run of up
+// to 64 squares is in fp32, the rest in fp64.
+constexpr float kLarge = 281474976710656.f, kLargeScale = 5.421010862427522e-20f;
+template <typename T>
+__global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, Pieces q, int vec, double2 *part) {
+    __shared__ double2 red[8];
+    grid_dep_sync();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    double dsmall = 0., dlarge = 0.;
+    for (long long i = (long long)blockIdx.x * 8 + warp; i < q.all; i += (long long)gridDim.x * 8) {
+        const long long r = i / q.per_row;
+        const int first = (int)(i - r * q.per_row) * kPieceCols, end = min(q.cols, first + kPieceCols);
+        const T *row = g + r * ldg;
+        float small = 0.f, large = 0.f;
+#pragma unroll 4
+        for (int c = first + lane * 8; c < end; c += 256) {
+            float v[8];
+            row8(row, c, end, vec, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool big = fabsf(v[j]) > kLarge;
+                const float w = big ? v[j] * kLargeScale : v[j];
+                large = fmaf(big ? w : 0.f, w, large);
+                small = fmaf(big ? 0.f : w, w, small);  // (NaN too)
+            }
+        }
+        dsmall += small;
+        dlarge += large;
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         dsmall += __shfl_xor_sync(0xffffffffu, dsmall, o);
         dlarge += __shfl_xor_sync(0xffffffffu, dlarge, o);
     }
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_double2(dsmall, dlarge);
+    if (lane == 0) red[warp] = make_double2(dsmall, dlarge);
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 8; ++i) {
@@ -86,65 +101,69 @@ __global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, lo
     }
 }
 
-// X = G / (norm + eps) in planes (or, planes 0, as the result); every CTA adds the sums up
-// in the same order.
+// X = G / (norm + eps) in planes of rows of pitch elements (or, planes 0, as the result);
+// every CTA adds the sums up in the same order.
 template <typename T>
-__global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, long long rows, int cols,
+__global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, Pieces q, int vec,
                                                     const double2 *part, int parts, float eps, int planes,
-                                                    unsigned short *dst, long long plane, T *out, long long ldo) {
-    __shared__ double2 red[256];
+                                                    unsigned short *dst, long long pitch, T *out, long long ldo) {
+    __shared__ double2 red[8];
     grid_dep_sync();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     double2 s = make_double2(0., 0.);
     for (int i = threadIdx.x; i < parts; i += 256) {
         s.x += part[i].x;
         s.y += part[i].y;
     }
-    red[threadIdx.x] = s;
-    __syncthreads();
-    for (int o = 128; o; o >>= 1) {
-        if ((int)threadIdx.x < o) {
-            red[threadIdx.x].x += red[threadIdx.x + o].x;
-            red[threadIdx.x].y += red[threadIdx.x + o].y;
-        }
-        __syncthreads();
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
+        s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
     }
-    const double norm = sqrt(red[0].x + red[0].y * 340282366920938463463374607431768211456.0) + (double)eps;
-    // (a norm of zero with eps zero: the matrix is zero; a factor above fp32's range is
-    // taken in two)
+    if (lane == 0) red[warp] = s;
+    __syncthreads();
+    s = red[0];
+    for (int i = 1; i < 8; ++i) {
+        s.x += red[i].x;
+        s.y += red[i].y;
+    }
+    const double norm = sqrt(s.x + s.y * 340282366920938463463374607431768211456.0) + (double)eps;
+    // (a norm of zero with eps zero: the matrix is zero; a factor above fp32's range, of tiny
+    // matrices with a tiny eps, is taken in two: f2 is 1 otherwise)
     const double f = norm > 0. || norm != norm ? 1.0 / norm : 0.;
-    const int c8 = (cols + 7) / 8;
-    const long long pitch = (long long)c8 * 8, all = rows * c8;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long r = i / c8;
-        const int c = (int)(i - r * c8) * 8;
-        float v[8];
-        const float ff = (float)f;
-        const bool plain = ff < 3e38f;
+    const float f2 = f > 1e30 ? 1e30f : 1.f, f1 = (float)(f > 1e30 ? f / 1e30f : f);
+    const long long plane = q.rows * pitch;
+    for (long long i = (long long)blockIdx.x * 8 + warp; i < q.all; i += (long long)gridDim.x * 8) {
+        const long long r = i / q.per_row;
+        const int first = (int)(i - r * q.per_row) * kPieceCols, end = min(q.cols, first + kPieceCols);
+        const T *row = g + r * ldg;
+#pragma unroll 2
+        for (int c = first + lane * 8; c < end; c += 256) {
+            float v[8];
+            row8(row, c, end, vec, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = c + j < cols ? value(g + r * ldg + c + j) : 0.f;
-            v[j] = plain ? x * ff : (float)(x * f);
+            for (int j = 0; j < 8; ++j) v[j] = v[j] * f1 * f2;
+            if (planes == 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < end) {
+                        if constexpr (sizeof(T) == 4) out[r * ldo + c + j] = v[j];
+                        else out[r * ldo + c + j] = float_to_bf16(v[j]);
+                    }
+                continue;
+            }
+            unsigned w[3][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (planes == 3) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+                else planes2(v[2 * j], v[2 * j + 1], w[0][j], w[1][j]);
+            }
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+                if (p < planes)
+                    *reinterpret_cast<uint4 *>(dst + p * plane + r * pitch + c) =
+                        make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
         }
-        if (planes == 0) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c + j < cols) {
-                    if constexpr (sizeof(T) == 4) out[r * ldo + c + j] = v[j];
-                    else out[r * ldo + c + j] = float_to_bf16(v[j]);
-                }
-            continue;
-        }
-        unsigned w[3][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (planes == 3) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
-            else planes2(v[2 * j], v[2 * j + 1], w[0][j], w[1][j]);
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p)
-            if (p < planes)
-                *reinterpret_cast<uint4 *>(dst + p * plane + r * pitch + c) =
-                    make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
     }
 }
 
@@ -187,15 +206,15 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
                       long long ldo, const OrthoPlan &o, const OrthoSpace &s, cudaStream_t st) {
     PdlScope pdl;
     const bool wide = m <= n;
-    const long long all = (long long)m * cdiv(n, 4);
-    const int blocks = (int)std::min<long long>(kNormBlocks, (all + 255) / 256);
-    const int vec = reinterpret_cast<uintptr_t>(G) % (4 * sizeof(T)) == 0 && ldg % 4 == 0;
-    qcnn_status rc = launch_pdl(norm_kernel<T>, dim3(blocks), dim3(256), 0, st, G, ldg, (long long)m, n, vec, s.norm);
+    const Pieces q{m, (long long)m * cdiv(n, kPieceCols), n, cdiv(n, kPieceCols)};
+    const int blocks = (int)std::min<long long>(kNormBlocks, (q.all + 7) / 8);
+    const int vec = tma_ok(G, ldg);  // (16-byte rows; of fp32 more than it needs)
+    qcnn_status rc = launch_pdl(norm_kernel<T>, dim3(blocks), dim3(256), 0, st, G, ldg, q, vec, s.norm);
     if (rc != QCNN_OK) return rc;
     const long long px = pad8(n), xplane = m * px, pa = pad8(o.p), aplane = o.p * pa;
-    const int grid = (int)std::min<long long>(((long long)m * cdiv(n, 8) + 255) / 256, (long long)num_sms() * 8);
-    rc = launch_pdl(scale_kernel<T>, dim3(grid), dim3(256), 0, st, G, ldg, (long long)m, n, s.norm, blocks, eps,
-                    steps ? o.P : 0, s.x[0], xplane, out, ldo);
+    const int grid = (int)std::min<long long>(2 * kNormBlocks, (q.all + 7) / 8);
+    rc = launch_pdl(scale_kernel<T>, dim3(grid), dim3(256), 0, st, G, ldg, q, vec, s.norm, blocks, eps,
+                    steps ? o.P : 0, s.x[0], px, out, ldo);
     for (int i = 0; i < steps && rc == QCNN_OK; ++i) {
         const GemmOperand x{s.x[i & 1], px, xplane, 0}, a{s.a, pa, aplane, 0}, b{s.b, pa, aplane, 0};
         const int type = o.P;  // GEMM_T_PLANES2, GEMM_T_PLANES3

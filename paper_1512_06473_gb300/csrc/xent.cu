@@ -144,8 +144,8 @@ __global__ void __launch_bounds__(256) stats_join_kernel(const float2 *stats, in
 
 // Small: the gradient of the logits and its sums over a slab of rows.  A CTA takes 128
 // classes x a slab: a warp a row, a lane four classes.
-__global__ void __launch_bounds__(256) dl_kernel(const float *logits, const float4 *rows, int N, int Ct, void *out, int out_type, long long ldo,
-                                                 long long plane, float *part, int slab) {
+__global__ void __launch_bounds__(256) dl_kernel(const float *logits, const float4 *rows, int N, int Ct, unsigned short *out, int planes,
+                                                 long long ldo, long long plane, float *part, int slab) {
     __shared__ float red[8][128];
     grid_dep_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -170,18 +170,14 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
                 sum[j] += v[j];
             }
             const long long o = (long long)r * ldo + c;  // (rows of multiples of 8)
-            if (out_type == GEMM_T_F32) {
-                *reinterpret_cast<float4 *>(static_cast<float *>(out) + o) = make_float4(v[0], v[1], v[2], v[3]);
-            } else {
-                unsigned w[3][2];
-                unsigned short *d = static_cast<unsigned short *>(out) + o;
+            unsigned w[3][2];
+            unsigned short *d = out + o;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
-                *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
-                if (out_type == GEMM_T_PLANES3) {
-                    *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
-                    *reinterpret_cast<uint2 *>(d + 2 * plane) = make_uint2(w[2][0], w[2][1]);
-                }
+            for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+            *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
+            if (planes == 3) {
+                *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
+                *reinterpret_cast<uint2 *>(d + 2 * plane) = make_uint2(w[2][0], w[2][1]);
             }
         }
     }
@@ -198,64 +194,41 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
     }
 }
 
-// fp32 rows with a class, zeros for the others (16-byte rows).
-__global__ void __launch_bounds__(256) keep_rows_kernel(const float *x, long long ldx, int Cs,
-                                                        const int64_t *targets, int Ct, float *out,
-                                                        long long ldo) {
-    grid_dep_sync();
-    const bool in = (unsigned long long)targets[blockIdx.x] < (unsigned long long)Ct;
-    for (int c = blockIdx.y * 256 + threadIdx.x; c < Cs; c += gridDim.y * 256)
-        out[(long long)blockIdx.x * ldo + c] = in ? x[(long long)blockIdx.x * ldx + c] : 0.f;
-}
-
+// fp32: x and dl always as planes; wplanes: the weights too.  bf16: copies of what TMA
+// cannot read.
 struct XentPlan {
-    bool small = false, few = false;
-    bool lplanes = false;  // fp32: the product of the logits is of planes
-    bool gplanes = false;  // and those of the gradient
+    bool small = false, few = false, wplanes = false;
     Product logits, stats, dl, dx, dw;
-    int piece = 0;         // classes of a piece
+    int piece = 0;  // classes of a piece
     int slab = 0, slabs = 1;
-    int dl_type = GEMM_T_BF16;
 };
 XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool grad) {
     XentPlan p;
     const bool bf16 = dtype == QCNN_BF16;
+    const int P = bf16 ? 1 : 3;
     p.small = (size_t)N * Ct * 4 <= kPiece;
     p.piece = Ct;
-    const double size = ((double)N + Ct) * Cs;
+    p.wplanes = true;
     if (p.small) {
         p.few = N <= kFewRows;
         p.slab = std::max(32, cdiv(cdiv(N, std::max(1, 4 * num_sms() / cdiv(Ct, 128))), 8) * 8);
         p.slabs = cdiv(N, p.slab);
-        GemmPlan l, x, w;
-        double planes = 0, direct = 0;
-        if (bf16) {
-            l = plan_gemm(1, GEMM_OUT, Ct, N, Cs, 64);
-            x = plan_gemm(1, GEMM_OUT, Cs, N, Ct, 64);
-            w = plan_gemm(1, GEMM_OUT, Cs, Ct, N, 64);
-        } else {
-            // planes of x and W, once for the products that take them, or none of them
-            l = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, 64);
-            x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
-            w = plan_gemm(GEMM_F32, GEMM_OUT, Cs, Ct, N, 64);
-            const GemmPlan ql = plan_gemm(3, GEMM_OUT, Ct, N, Cs, 64), qx = plan_gemm(3, GEMM_OUT, Cs, N, Ct, 64),
-                           qw = plan_gemm(3, GEMM_OUT, Cs, Ct, N, 64);
-            direct = (p.few ? 0 : l.score) + (grad ? x.score + w.score : 0);
-            planes = (p.few ? 0 : ql.score) + (grad ? qx.score + qw.score : 0) + pass_clocks(size * 16.0);
-            if (planes < direct) {
-                p.lplanes = p.gplanes = true;
-                l = ql, x = qx, w = qw;
+        p.logits.plan = plan_gemm(P, GEMM_OUT, Ct, N, Cs, 64);
+        p.dx.plan = plan_gemm(P, GEMM_OUT, Cs, N, Ct, 64);
+        p.dw.plan = plan_gemm(P, GEMM_OUT, Cs, Ct, N, 64);
+        if (!bf16) {
+            const GemmPlan l = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, 64);
+            const GemmPlan x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
+            const double planes = (p.few ? 0 : p.logits.plan.score) + (grad ? p.dx.plan.score : 0);
+            const double direct = (p.few ? 0 : l.score) + (grad ? x.score : 0);
+            if (direct <= planes + pass_clocks((double)Ct * Cs * 10.0)) {
+                p.wplanes = false;
+                p.logits.plan = l;
+                p.dx.plan = x;
             }
         }
-        p.logits.plan = l;
-        p.dx.plan = x;
-        p.dw.plan = w;
-        p.dl_type = bf16 ? GEMM_T_BF16 : p.gplanes ? GEMM_T_PLANES3 : GEMM_T_F32;
         return p;
     }
-    const int P = bf16 ? 1 : 3;
-    p.lplanes = p.gplanes = !bf16;
-    p.dl_type = bf16 ? GEMM_T_BF16 : GEMM_T_PLANES3;
     p.stats.plan = plan_gemm(P, GEMM_STATS, N, Ct, Cs, 1);
     const long long most = (long long)(kPieceDl / ((size_t)N * 2 * P)) / 256 * 256;
     p.piece = (int)std::min<long long>(Ct, std::max<long long>(256, most));
@@ -267,15 +240,14 @@ XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool grad) {
     return p;
 }
 struct XentSpace {
-    float *inv = nullptr, *logits = nullptr, *target_logit = nullptr, *db = nullptr, *dx = nullptr, *xkeep32 = nullptr;
+    float *inv = nullptr, *logits = nullptr, *target_logit = nullptr, *db = nullptr, *dx = nullptr;
     float4 *rows = nullptr;
     float2 *stats = nullptr;
-    unsigned short *x = nullptr, *w = nullptr, *xkeep = nullptr;
-    void *dl = nullptr, *partial = nullptr;
+    unsigned short *x = nullptr, *w = nullptr, *kept = nullptr, *dl = nullptr;
+    void *partial = nullptr;
     size_t bytes = 0;
 };
-XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool grad, bool x_copy, bool w_copy,
-                     void *ws) {
+XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool grad, bool xa, bool wa, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     XentSpace s;
     const bool bf16 = dtype == QCNN_BF16;
@@ -283,8 +255,9 @@ XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool g
     const long long pc = pad8(Cs);
     s.inv = c.array<float>(1);
     if (grad) s.rows = c.array<float4>(N);
-    if (x_copy) s.x = c.array<unsigned short>(P * N * pc);
-    if (w_copy) s.w = c.array<unsigned short>(P * Ct * pc);
+    // (few rows read the operands as they are; their gradient does not)
+    if (!p.few && (!bf16 || !xa)) s.x = c.array<unsigned short>(P * N * pc);
+    if ((!p.few || grad) && (bf16 ? !wa : p.wplanes)) s.w = c.array<unsigned short>(P * Ct * pc);
     size_t partial = 0;
     if (p.small) {
         s.logits = c.array<float>((size_t)N * Ct);
@@ -295,9 +268,8 @@ XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool g
     }
     if (grad) {
         // rows without a class must not reach dW, not even as 0 * NaN
-        if (bf16 || p.gplanes) s.xkeep = c.array<unsigned short>(P * N * pc);
-        else s.xkeep32 = c.array<float>((size_t)N * pc);
-        s.dl = c.take((size_t)N * pad8(p.piece) * (p.dl_type == GEMM_T_F32 ? 4 : 2 * P));
+        s.kept = c.array<unsigned short>(P * N * pc);
+        s.dl = c.array<unsigned short>(P * N * pad8(p.piece));
         partial = std::max({partial, p.dx.scratch(), p.dw.scratch()});
         if (p.small) {
             s.db = c.array<float>((size_t)p.slabs * Ct);
@@ -329,35 +301,24 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
     const int N = a.N, Cs = a.Cs, Ct = a.Ct;
     const bool bf16 = a.dtype == QCNN_BF16;
     const XentPlan p = plan_xent(N, Cs, Ct, a.dtype, a.grad);
-    // (few rows without a gradient read the operands as they are)
-    const bool products = !p.few || a.grad;
-    const bool x_copy = !p.few && (bf16 ? !tma_ok(a.x, a.ldx) : p.lplanes);
-    const bool w_copy = products && (bf16 ? !tma_ok(a.W, a.ldw) : p.lplanes);
-    const XentSpace s = carve_xent(p, N, Cs, Ct, a.dtype, a.grad, x_copy, w_copy, workspace);
+    const XentSpace s = carve_xent(p, N, Cs, Ct, a.dtype, a.grad, tma_ok(a.x, a.ldx), tma_ok(a.W, a.ldw), workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;
     PdlScope pdl;
     const int P = bf16 ? 1 : 3;
     const long long pc = pad8(Cs);
-    GemmOperand xo{a.x, a.ldx, 0, 0}, wo{a.W, a.ldw, 0, 0}, xk;
-    if (s.x) {
-        if ((rc = launch_planes(a.x, bf16, N, Cs, a.ldx, P, s.x, N * pc, nullptr, 0, st)) != QCNN_OK) return rc;
-        xo = GemmOperand{s.x, pc, N * pc, 0};
+    GemmOperand xo{a.x, a.ldx, 0, 0}, wo{a.W, a.ldw, 0, 0};
+    if (s.x || s.kept) {
+        rc = launch_planes(a.x, bf16, N, Cs, a.ldx, P, s.x, s.kept, reinterpret_cast<const long long *>(a.targets),
+                           Ct, st);
+        if (rc != QCNN_OK) return rc;
+        if (s.x) xo = GemmOperand{s.x, pc, N * pc, 0};
     }
     if (s.w) {
-        if ((rc = launch_planes(a.W, bf16, Ct, Cs, a.ldw, P, s.w, Ct * pc, nullptr, 0, st)) != QCNN_OK) return rc;
+        if ((rc = launch_planes(a.W, bf16, Ct, Cs, a.ldw, P, s.w, nullptr, nullptr, 0, st)) != QCNN_OK) return rc;
         wo = GemmOperand{s.w, pc, Ct * pc, 0};
     }
-    if (s.xkeep) {
-        rc = launch_planes(a.x, bf16, N, Cs, a.ldx, P, s.xkeep, N * pc,
-                           reinterpret_cast<const long long *>(a.targets), Ct, st);
-        xk = GemmOperand{s.xkeep, pc, N * pc, 1};
-    } else if (s.xkeep32) {
-        rc = launch_pdl(keep_rows_kernel, dim3(N, std::min(cdiv(Cs, 256), 64)), dim3(256), 0, st,
-                        static_cast<const float *>(a.x), a.ldx, Cs, a.targets, Ct, s.xkeep32, pc);
-        xk = GemmOperand{s.xkeep32, pc, 0, 1};
-    }
-    if (rc != QCNN_OK) return rc;
+    const GemmOperand xk{s.kept, pc, N * pc, 1};
     RowOut ro{a.targets, a.dloss, a.loss, a.lse, s.rows, s.inv, N, Ct};
     const int type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
     GemmProblem g;
@@ -399,12 +360,12 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
     for (int c0 = 0; c0 < Ct; c0 += p.piece) {
         const int cn = std::min(p.piece, Ct - c0);
         const long long pz = pad8(cn), zplane = (long long)N * pz;
-        const GemmOperand wp{static_cast<const uint8_t *>(wo.p) + c0 * wo.ld * (bf16 || p.gplanes ? 2 : 4), wo.ld,
+        const GemmOperand wp{static_cast<const uint8_t *>(wo.p) + c0 * wo.ld * (bf16 || s.w ? 2 : 4), wo.ld,
                              wo.plane, 1};
         if (p.small) {
             float *const part = a.dbias ? s.db : nullptr;
             rc = launch_pdl(dl_kernel, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0, st, s.logits, s.rows, N, Ct,
-                            s.dl, p.dl_type, pz, zplane, part, p.slab);
+                            s.dl, P, pz, zplane, part, p.slab);
             if (rc == QCNN_OK && a.dbias)
                 rc = launch_column_join(s.db, p.slabs, Ct, Ct, inv, a.dbias, st);
         } else {
@@ -419,7 +380,7 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
             d.e.rows = s.rows;
             d.e.class0 = c0;
             d.e.out = s.dl;
-            d.e.out_type = p.dl_type;
+            d.e.out_type = bf16 ? GEMM_T_BF16 : GEMM_T_PLANES3;
             d.e.ldo = pz;
             d.e.out_plane = zplane;
             d.e.col_part = s.db;
@@ -481,8 +442,7 @@ qcnn_status qcnn_xent_workspace_size(int N, int Cs, int Ct, int dtype, int align
     *bytes = 0;
     if (N == 0) return QCNN_OK;
     const XentPlan p = plan_xent(N, Cs, Ct, dtype, grad != 0);
-    const bool copy = dtype == QCNN_BF16 ? !aligned : p.lplanes;
-    *bytes = carve_xent(p, N, Cs, Ct, dtype, grad != 0, copy && !p.few, copy && (!p.few || grad), nullptr).bytes;
+    *bytes = carve_xent(p, N, Cs, Ct, dtype, grad != 0, aligned, aligned, nullptr).bytes;
     return QCNN_OK;
 }
 
