@@ -293,7 +293,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     g.bn = plan.bn;
     g.b_off = a_bytes;  // (multiples of 1024: 128 rows; 64 rows of 128 bytes)
     g.stage = (unsigned)align_up(a_bytes + b_bytes, 1024);
-    const size_t raw = gen ? (size_t)kRawSlots * kGenWarps * 2048 : 0;
+    const size_t raw = gen ? (size_t)kRawSlots * kGenWarps * 4096 : 0;
     g.S = (int)std::min<size_t>(gen ? kGenStagesMax : kStagesMax, (kSmemMax - 1024 - raw) / g.stage);
     if (g.S < 2) return QCNN_ERR_UNSUPPORTED;
     const size_t smem = std::max(kSmemLeast, g.S * (size_t)g.stage + raw + 1024);

@@ -21,7 +21,7 @@
 //
 // GEN: A is fp32 of any stride and alignment (a layer's weights), split on its way, so that
 // a product bound by A's bytes (few rows n) reads them once and writes no planes.  Warps
-// 12-19 copy it (cp.async, kRawSlots - 1 stages ahead: some 64 KB in flight per SM), split
+// 12-15 copy it (cp.async, kRawSlots - 1 stages ahead: some 64 KB in flight per SM), split
 // it and store the planes to TMEM as the MMAs' A operand: shared memory then carries per
 // stage of 32 terms and 128 columns 32 KB for the copies, 24 KB of B's planes and 48 KB that
 // the twelve MMAs read, 832 clocks of its bandwidth to the 888 of the MMAs.  (With A's
@@ -40,8 +40,8 @@ constexpr int kMT = 128;          // rows of a CTA's tile
 constexpr int kAccCols = 256;     // TMEM columns of an accumulator, of two (GEN: 128)
 constexpr int kStagesMax = 8;
 constexpr int kEpiWarps = 8;
-constexpr int kGenWarps = 8;      // converters
-constexpr int kRawSlots = 5;      // GEN: stages of raw copies, 2 KB per warp each
+constexpr int kGenWarps = 4;      // converters
+constexpr int kRawSlots = 5;      // GEN: stages of raw copies, 4 KB per warp each
 constexpr int kGenCols = 48;      // TMEM columns of a stage's A: 3 planes x 32 terms
 constexpr int kGenStagesMax = 5;  // (512 - 2 * 128) / 48
 constexpr unsigned kPolls = 1u << 22;
@@ -493,22 +493,9 @@ __device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned (&v)[8])
         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
         : "memory");
 }
-template <int REGS>
-__device__ __forceinline__ void regs_dec() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(REGS));
-}
-template <int REGS>
-__device__ __forceinline__ void regs_inc() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(REGS));
-}
-// GEN: registers per thread of the five warpgroups (roles, two of drains, two of
-// converters), of 5 x 96 at launch
-constexpr int kRegsRoles = 80, kRegsDrain = 120, kRegsConvert = 80;
-static_assert(kRegsRoles + 2 * kRegsDrain + 2 * kRegsConvert <= 5 * 96, "register pool");
-
 // ------------------------------------------------------------------- kernel
 template <int P, int KIND, int CG, bool GEN>
-__global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
+__global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
     constexpr int BK = P == 1 ? 64 : 32, KS = BK / 16;
     constexpr bool DRAIN = P == 3;  // a stage's sum at a time
     constexpr int ACC = GEN ? 128 : kAccCols;
@@ -547,11 +534,6 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
     const unsigned tmem = sh.tmem;
     grid_dep_sync();
 
-    if constexpr (GEN) {
-        if (warp < 4) regs_dec<kRegsRoles>();
-        else if (warp < 12) regs_inc<kRegsDrain>();
-        else regs_dec<kRegsConvert>();
-    }
     if (warp == 0) {
         {
             // ----------------------------------------------------------- TMA
@@ -786,48 +768,52 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
         }
     } else if (GEN && warp >= 12) {
         // ------------------------------------------ copy, split, store planes
-        // A warp has 32 rows (its TMEM lanes) x 16 terms of every stage, and copies them
-        // itself: no barrier between copying and splitting.  Rows of k: [32][16] floats, the
-        // 16-byte pieces of a row permuted so that eight lanes of neighbouring rows read
-        // from all banks; rows of m: [16][32].
-        const int quarter = warp & 3, half = (warp - 12) >> 2;
+        // A warp has 32 rows (its TMEM lanes) x 32 terms of every stage, and copies them
+        // itself: no barrier between copying and splitting.  Rows of k: [32][32] floats, the
+        // 16-byte pieces of a row permuted so that eight neighbouring rows read from all
+        // banks; rows of m: [32 terms][32].  Both are eight copies of 16 bytes per lane, four
+        // lines on.
+        const int quarter = warp & 3;
         const ProblemArgs &p = g.p[0];
         const bool mn = p.a.mn, vec = p.a.vec;
         const float *const base = p.a.src;
-        const long long ld = p.a.ld;
-        const unsigned raw = smem_addr(smem) + g.S * g.stage + (warp - 12) * (kRawSlots * 2048);
-        // this lane's four copies per stage: the first's row and term, the others 8 rows (rows of
-        // m: 4 terms) on
-        const int row0 = mn ? (lane & 7) * 4 : lane >> 2, k0 = half * 16 + (mn ? lane >> 3 : (lane & 3) * 4);
-        const long long gap = mn ? 4 * ld : 8 * ld, step_k = mn ? 32 * ld : 32;
-        // (rows of k: piece (lane & 3) of row r lies at ((lane & 3) ^ (r >> 1 & 3)))
-        const unsigned dst0 = mn ? (lane >> 3) * 128 + (lane & 7) * 16
-                                 : (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3 & 3)) << 4);
+        const long long ld = p.a.ld, gap = 4 * ld, step_k = mn ? 32 * ld : 32;
+        const unsigned raw = smem_addr(smem) + g.S * g.stage + (warp - 12) * (kRawSlots * 4096);
+        // this lane's first line (row, or term) and place along it
+        const int line0 = lane >> 3, along = (lane & 7) * 4;
         const float *src = base;
-        int cu = first_unit, ck = 0, ckb = 0, ckb1 = 0, cslot = 0, rows = 0;
+        int cu = first_unit, ckb = 0, ckb1 = 0, cslot = 0;
+        int line_in = 0, along_in = 0;  // lines and elements along them that exist from here on
         auto open_tile = [&]() {
             const Tile t = tile_of<KIND, CG>(g, cu);
             ckb = t.kb0;
             ckb1 = t.kb1;
-            ck = t.kb0 * BK + k0;
-            const int row = t.mt * kMT + quarter * 32 + row0;
-            rows = p.m - row;  // that exist from this lane's first on
-            src = base + (mn ? (long long)ck * ld + row : (long long)row * ld + ck);
+            const int row = t.mt * kMT + quarter * 32 + (mn ? along : line0);
+            const int k = t.kb0 * BK + (mn ? line0 : along);
+            line_in = mn ? p.k - k : p.m - row;
+            along_in = mn ? p.m - row : p.k - k;
+            src = base + (mn ? (long long)k * ld + row : (long long)row * ld + k);
         };
         if (cu < g.units) open_tile();
         auto copy_next = [&]() {
             if (cu < g.units) {
-                const unsigned d = raw + cslot * 2048 + dst0;
-                const int k_in = p.k - ck;
                 const float *s = src;
+                const unsigned d = raw + cslot * 4096 + line0 * 128;
+                // (row r's piece c lies at c ^ (r & 7); r is line0, line0 + 4, ...)
+                const unsigned c0 = mn ? (lane & 7) * 16 : ((lane & 7) ^ line0) * 16;
+                const unsigned c1 = mn ? c0 : c0 ^ 64;
+                if (vec && line_in > 28 && along_in >= 4) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j, s += gap) {
-                    // (8 rows on, the permutation is the same: 4 pairs of rows)
-                    if (mn) copy4(d + j * 512, s, k_in > 4 * j ? rows : 0, vec, base);
-                    else copy4(d + j * 512, s, rows > 8 * j ? k_in : 0, vec, base);
+                    for (int j = 0; j < 8; ++j, s += gap)
+                        cp_async16_part(d + j * 512 + (j & 1 ? c1 : c0), s, 16);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j, s += gap)
+                        copy4(d + j * 512 + (j & 1 ? c1 : c0), s, line_in > 4 * j ? along_in : 0, vec, base);
                 }
                 src += step_k;
-                ck += BK;
+                if (mn) line_in -= 32;
+                else along_in -= 32;
                 if (++ckb == ckb1) {
                     cu += step;
                     if (cu < g.units) open_tile();
@@ -837,7 +823,7 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
             cp_async_commit();
         };
         for (int i = 0; i < kRawSlots - 1; ++i) copy_next();
-        const unsigned a_dst = tmem + 2 * ACC + ((unsigned)(quarter * 32) << 16) + half * 8;
+        const unsigned a_dst = tmem + 2 * ACC + ((unsigned)(quarter * 32) << 16);
         int slot = 0, rslot = 0;
         unsigned par = 0;
         bool ok = true;
@@ -846,30 +832,34 @@ __global__ void __launch_bounds__(GEN ? 640 : 384, 1) gemm_kernel(const __grid_c
             for (int kb = t.kb0; kb < t.kb1; ++kb) {
                 cp_async_wait<kRawSlots - 2>();
                 __syncwarp();
-                const unsigned r = raw + rslot * 2048;
-                float v[16];
+                const unsigned r = raw + rslot * 4096;
+                float v[32];
                 if (mn) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
+                    for (int i = 0; i < 32; ++i)
                         asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(r + i * 128 + lane * 4));
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 8; ++i)
                         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n"
                                      : "=f"(v[4 * i]), "=f"(v[4 * i + 1]), "=f"(v[4 * i + 2]), "=f"(v[4 * i + 3])
-                                     : "r"(r + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)));
+                                     : "r"(r + lane * 128 + ((i ^ (lane & 7)) << 4)));
                 }
-                unsigned w0[8], w1[8], w2[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
-                __syncwarp();  // (all have read: the slot may be copied to)
-                copy_next();
                 if (!(ok = wait_warp(sh, &sh.empty[slot], par ^ 1))) break;
                 tc_fence_after_sync();
                 const unsigned d = a_dst + slot * kGenCols;
-                tmem_st8(d, w0);
-                tmem_st8(d + 16, w1);
-                tmem_st8(d + 32, w2);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    unsigned w0[8], w1[8], w2[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        planes3(v[16 * h + 2 * i], v[16 * h + 2 * i + 1], w0[i], w1[i], w2[i]);
+                    tmem_st8(d + 8 * h, w0);
+                    tmem_st8(d + 8 * h + 16, w1);
+                    tmem_st8(d + 8 * h + 32, w2);
+                }
+                __syncwarp();  // (all have read: the slot may be copied to)
+                copy_next();
                 asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
                 tc_fence_before_sync();
                 __syncwarp();
@@ -900,7 +890,7 @@ struct GemmKernel {
         const auto k = gemm_kernel<P, KIND, CG, GEN>;
         qcnn_status rc = allow_smem(reinterpret_cast<const void *>(k));
         if (rc != QCNN_OK) return rc;
-        return launch_k(k, dim3(ctas), dim3(GEN ? 640 : 384), smem, st, CG == 2 ? dim3(2, 1, 1) : dim3(0, 0, 0), g);
+        return launch_k(k, dim3(ctas), dim3(GEN ? 512 : 384), smem, st, CG == 2 ? dim3(2, 1, 1) : dim3(0, 0, 0), g);
     }
 };
 
