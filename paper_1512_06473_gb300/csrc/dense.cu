@@ -259,7 +259,8 @@ ForwardSpace carve_forward(const ForwardPlan &p, int N, int Cs, int Ct, int dtyp
     if (p.few) return s;
     const bool bf16 = dtype == QCNN_BF16;
     const int P = bf16 ? 1 : 3;
-    if (!bf16 || !xa) s.x = c.array<unsigned short>((size_t)P * N * pad8(Cs));
+    const bool x_copy = !bf16 || !xa;
+    if (x_copy) s.x = c.array<unsigned short>((size_t)P * N * pad8(Cs));
     if (bf16 ? !wa : p.wplanes) s.w = c.array<unsigned short>((size_t)P * Ct * pad8(Cs));
     s.partial = c.take(p.g.scratch());
     s.bytes = c.used;

@@ -42,39 +42,28 @@ EncodeTiled encode_tiled() {
     return f;
 }
 
-int block_k(int planes) { return planes == 1 ? 64 : 32; }
-int real_planes(int planes) { return planes == GEMM_F32 ? 3 : planes; }
+// Terms of a stage: 64 of one plane; GEN (A in fp32): 32 of B's three planes.
+int block_k(bool gen) { return gen ? 32 : 64; }
 
-unsigned operand_bytes(int P, int mn, int rows) {
-    const unsigned bk = block_k(P);
-    return mn ? (unsigned)cdiv(rows, 64) * P * bk * 128 : (unsigned)P * rows * bk * 2;
-}
-
-// An operand of `rows` rows (this CTA's part of a tile); rows_all x k is its matrix.  map:
-// null for an fp32 one.
-qcnn_status set_operand(const GemmOperand &o, int planes, int rows, int rows_all, int k, OpArgs *a,
+// An operand of `rows` rows (this CTA's part of a tile); rows_all x k is its matrix.
+qcnn_status set_operand(const GemmOperand &o, int P, bool gen, int rows, int rows_all, int k, OpArgs *a,
                         CUtensorMap *map) {
-    const int P = real_planes(planes), bk = block_k(P);
+    const int bk = block_k(gen), box_planes = gen ? P : 1;
     a->mn = o.mn;
-    a->bytes = operand_bytes(P, o.mn, rows);
-    a->group_bytes = P * bk * 128;
+    a->group_bytes = box_planes * bk * 128;
+    a->bytes = o.mn ? cdiv(rows, 64) * a->group_bytes : (unsigned)box_planes * rows * bk * 2;
     a->plane = o.mn ? bk * 128 / 16 : rows * bk * 2 / 16;
     a->kstep = o.mn ? 2048 / 16 : 32 / 16;
     const bool sw64 = !o.mn && bk == 32;
     const uint64_t sbo = sw64 ? 512 : 1024, lbo = o.mn ? a->group_bytes : 16;
     a->desc = (lbo >> 4) << 16 | (sbo >> 4) << 32 | 1ull << 46 | (uint64_t)(sw64 ? 4 : 2) << 61;
-    a->src = static_cast<const float *>(o.p);
-    a->ld = o.ld;
-    a->rows = rows_all;
-    a->vec = reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.ld % 4 == 0;
-    if (!map) return QCNN_OK;
     const EncodeTiled enc = encode_tiled();
     if (!enc) return QCNN_ERR_CUDA;
     const cuuint64_t inner = o.mn ? rows_all : k, outer = o.mn ? k : rows_all;
     const cuuint64_t dims[3] = {inner, outer, (cuuint64_t)P};
     const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(P > 1 ? o.plane : o.ld * outer) * 2};
     const cuuint32_t box[3] = {o.mn ? 64u : (cuuint32_t)bk, o.mn ? (cuuint32_t)bk : (cuuint32_t)rows,
-                               (cuuint32_t)P};
+                               (cuuint32_t)box_planes};
     const cuuint32_t steps[3] = {1, 1, 1};
     const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(o.p), dims, strides,
                            box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -82,6 +71,19 @@ qcnn_status set_operand(const GemmOperand &o, int planes, int rows, int rows_all
                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return cuda_status(cudaErrorInvalidValue);
     return QCNN_OK;
+}
+
+long long tiles_of(int kind, int m_tiles, int n_tiles, int per) {
+    if (kind != GEMM_SYM) return (long long)m_tiles * n_tiles;
+    long long t = 0;
+    for (int i = 0; i < n_tiles; ++i) t += std::max(0, m_tiles - i * per);
+    return t;
+}
+
+// Whether a matrix of two-byte elements can go in pairs of neighbours along m.
+bool pairs(const void *p, int type, long long ld, long long plane, int m) {
+    return type != GEMM_T_F32 && p && reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 2 == 0 && plane % 2 == 0 &&
+           (m % 2 == 0 || type >= GEMM_T_PLANES2);  // (rows of planes have room for one more)
 }
 
 GemmLaunch launcher(const GemmPlan &p) {
@@ -124,6 +126,43 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(GemmEpi e, int m_all, in
             if (e.out_type >= GEMM_T_PLANES2) p[e.out_plane] = (unsigned short)w[1];
             if (e.out_type == GEMM_T_PLANES3) p[2 * e.out_plane] = (unsigned short)w[2];
         }
+    }
+}
+
+// The same of a symmetric product: only m >= n was summed.  A CTA has a 32 x 32 patch below
+// (or on) the diagonal, which goes to its mirror image through shared memory.
+__global__ void __launch_bounds__(256) gemm_join_sym_kernel(GemmEpi e, int m_all, int splits) {
+    grid_dep_sync();
+    __shared__ float patch[32][33];
+    const int bm = blockIdx.x, bn = blockIdx.y;
+    if (bn > bm) return;
+    const int x = threadIdx.x & 31, y0 = threadIdx.x >> 5, m = bm * 32 + x;
+    const size_t stride = (size_t)m_all * m_all;
+    auto put = [&](float v, int row, int col) {
+        unsigned w[3] = {};
+        if (e.out_type == GEMM_T_PLANES2) planes2(v, 0.f, w[0], w[1]);
+        else planes3(v, 0.f, w[0], w[1], w[2]);
+        unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)row * e.ldo + col;
+        p[0] = (unsigned short)w[0];
+        p[e.out_plane] = (unsigned short)w[1];
+        if (e.out_type == GEMM_T_PLANES3) p[2 * e.out_plane] = (unsigned short)w[2];
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int y = y0 + 8 * i, n = bn * 32 + y;
+        float v = 0.f;
+        if (m < m_all && n <= m) {
+            v = e.alpha * add_groups<true>(e.partial + (size_t)n * m_all + m, splits, stride);
+            if (e.add) v = fmaf(e.beta, load_as(e.add, e.add_type, (long long)n * e.lda + m, e.add_plane), v);
+            put(v, n, m);
+        }
+        patch[y][x] = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = bm * 32 + y0 + 8 * i, col = bn * 32 + x;
+        if (row < m_all && col < row) put(patch[x][y0 + 8 * i], row, col);
     }
 }
 
@@ -190,35 +229,34 @@ __global__ void __launch_bounds__(256) planes_kernel(const T *src, long long all
 
 static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int max_splits, int sms) {
     GemmPlan best;
-    const int P = real_planes(planes), bk = block_k(P), kblocks = std::max(1, cdiv(k, bk));
+    const bool gen = planes == GEMM_F32;
+    const int P = gen ? 3 : planes, bk = block_k(gen), kblocks = std::max(1, cdiv(k, bk));
     static const int tiles[6] = {16, 32, 64, 128, 192, 256};
-    const int mmas = P == 1 ? 4 : P == 2 ? 6 : 12;
-    for (int cg = 1; cg <= (planes == GEMM_F32 ? 1 : 2); ++cg) {
+    const int mmas = (P == 1 ? 1 : P == 2 ? 3 : 6) * bk / 16;
+    for (int cg = 1; cg <= (gen ? 1 : 2); ++cg) {
         for (int bn : tiles) {
-            if (planes == GEMM_F32 && bn > 128) continue;
+            if (gen && bn > 128) continue;
             if (cg == 2 && bn != 256) continue;
+            if (planes == 3 && cg == 1 && bn > 128) continue;  // (stages: launch_gemm)
             if (kind == GEMM_SYM && bn % (kMT * cg)) continue;
             if (bn > 16 && kind != GEMM_SYM && bn >= 2 * n) continue;
             const int mt = cdiv(m, kMT * cg), nt = cdiv(n, bn), slots = sms / cg;
-            long long units = (long long)mt * nt;
-            if (kind == GEMM_SYM) {
-                units = 0;
-                for (int i = 0; i < nt; ++i) units += std::max(0, mt - i * (bn / (kMT * cg)));
-            }
-            const double mma = mmas * (bn / 2 + 10.0);
-            const double bytes = (double)P * (kMT + bn / cg) * bk * 2;
-            double per = std::max(mma, bytes / 48.0);
-            // (A's bytes at the memory's rate, B's planes at the L2's; the converters)
-            if (planes == GEMM_F32) per = std::max({mma, kMT * 128.0 / 21.0, bn * 192.0 / 40.0, 600.0});
-            if (P == 3) per = std::max(per, 2.5 * bn + 100.0);
-            const double tail = 2500.0 + bn * (kind == GEMM_OUT ? 8.0 : 14.0);
+            const long long units = tiles_of(kind, mt, nt, bn / (kMT * cg));
+            // Clocks of a block of terms: its MMAs, its bytes (TMA 60 bytes per clock and SM;
+            // GEN: fp32 at the memory's rate when all SMs read, and 1200 as measured), or what
+            // goes through shared memory (128 bytes per clock: written once, read per MMA).
+            const double mma = mmas * (bn / 2 + 10.0), bytes = P * (kMT + bn / cg) * bk * 2.0;
+            double per = std::max({mma, bytes / 60.0, (bytes + mmas * (kMT + bn / cg) * 32.0) / 128.0});
+            if (gen) per = std::max({mma * 1.15, kMT * bk * 4 / 21.0, bn * 192.0 / 40.0, 800.0});
+            // (and of a tile: first loads, last sums, epilogue)
+            const double tail = 5000.0 + bn * (kind == GEMM_OUT ? 12.0 : 20.0);
             for (int sp = 1; sp <= std::min({max_splits, kblocks, 64}); ++sp) {
                 const int kps = cdiv(kblocks, sp);
                 if (cdiv(kblocks, kps) != sp) continue;
                 if (sp > 1 && units * sp > 4 * slots) break;
                 const double waves = (double)((units * sp + slots - 1) / slots);
-                const double join = sp > 1 ? 4000.0 + 2.0 * sp * m * (double)n * 4.0 / 3500.0 : 0.0;
-                const double score = waves * (kps * per + tail) + join;
+                const double join = sp > 1 ? 5000.0 + 2.0 * sp * m * (double)n * 4.0 / 3500.0 : 0.0;
+                const double score = waves * kps * per + tail + (waves - 1) * 1000.0 + join;
                 if (best.bn && score >= best.score) continue;
                 best.planes = planes;
                 best.kind = kind;
@@ -255,24 +293,31 @@ GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_splits) {
 
 qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, cudaStream_t st) {
     const bool gen = plan.planes == GEMM_F32;
-    const int P = real_planes(plan.planes), bk = block_k(P), cg = plan.cg, bnc = plan.bn / cg;
+    const int P = gen ? 3 : plan.planes, cg = plan.cg, bnc = plan.bn / cg;
     GemmArgs g = {};
     unsigned a_bytes = 0, b_bytes = 0;
     for (int i = 0; i < count; ++i) {
         const GemmProblem &s = ps[i];
         ProblemArgs &p = g.p[i];
-        qcnn_status rc = set_operand(s.a, plan.planes, kMT, s.m, s.k, &p.a, gen ? nullptr : &p.map_a);
-        if (rc == QCNN_OK) rc = set_operand(s.b, plan.planes, bnc, s.n, s.k, &p.b, &p.map_b);
+        qcnn_status rc = set_operand(s.b, P, gen, bnc, s.n, s.k, &p.b, &p.map_b);
         if (rc != QCNN_OK) return rc;
-        if (!gen) a_bytes = std::max(a_bytes, p.a.bytes);
+        if (gen) {
+            p.a.mn = s.a.mn;
+            p.a.src = static_cast<const float *>(s.a.p);
+            p.a.ld = s.a.ld;
+            p.a.vec = reinterpret_cast<uintptr_t>(s.a.p) % 16 == 0 && s.a.ld % 4 == 0;
+        } else if ((rc = set_operand(s.a, P, gen, kMT, s.m, s.k, &p.a, &p.map_a)) != QCNN_OK) {
+            return rc;
+        }
+        a_bytes = std::max(a_bytes, p.a.bytes);
         b_bytes = std::max(b_bytes, p.b.bytes);
         // (A in TMEM has its terms along the columns, however it lay in memory)
-        p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (s.a.mn && !gen ? 1u << 15 : 0) | (s.b.mn ? 1u << 16 : 0) |
-                  (uint32_t)(plan.bn >> 3) << 17 | (uint32_t)(kMT * cg >> 4) << 24;
+        p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (s.a.mn && !gen ? 1u << 15 : 0) |
+                  (s.b.mn ? 1u << 16 : 0) | (uint32_t)(plan.bn >> 3) << 17 | (uint32_t)(kMT * cg >> 4) << 24;
         p.m = s.m;
         p.n = s.n;
         p.k = s.k;
-        p.kblocks = std::max(1, cdiv(s.k, bk));
+        p.kblocks = std::max(1, cdiv(s.k, block_k(gen)));
         p.m_tiles = cdiv(s.m, kMT * cg);
         p.n_tiles = cdiv(s.n, plan.bn);
         p.splits = count > 1 ? 1 : plan.splits;
@@ -280,13 +325,13 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
         p.group = std::max(1, 16 / cg);
         p.e = s.e;
         if (p.splits == 1) p.e.partial = nullptr;
-        long long units = (long long)p.m_tiles * p.n_tiles * p.splits;
-        if (plan.kind == GEMM_SYM) {
-            units = 0;
-            for (int j = 0; j < p.n_tiles; ++j) units += std::max(0, p.m_tiles - j * (plan.bn / (kMT * cg)));
-        }
-        if (units > (1 << 30)) return QCNN_ERR_UNSUPPORTED;
-        p.units = (int)units;
+        p.e.pair = (pairs(s.e.out, s.e.out_type, s.e.ldo, s.e.out_plane, s.m) ? 1 : 0) |
+                   (pairs(s.e.pre, s.e.out_type, s.e.ldp, 0, s.m) ? 2 : 0) |
+                   (pairs(s.e.add, s.e.add_type, s.e.lda, s.e.add_plane, s.m) ? 4 : 0);
+        const long long tiles = tiles_of(plan.kind, p.m_tiles, p.n_tiles, plan.bn / (kMT * cg));
+        if (tiles * p.splits > (1 << 30)) return QCNN_ERR_UNSUPPORTED;
+        p.tiles = (int)tiles;
+        p.units = p.tiles * p.splits;
         g.units += p.units;
     }
     g.count = count;
@@ -294,14 +339,20 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     g.b_off = a_bytes;  // (multiples of 1024: 128 rows; 64 rows of 128 bytes)
     g.stage = (unsigned)align_up(a_bytes + b_bytes, 1024);
     const size_t raw = gen ? (size_t)kRawSlots * kGenWarps * 4096 : 0;
-    g.S = (int)std::min<size_t>(gen ? kGenStagesMax : kStagesMax, (kSmemMax - 1024 - raw) / g.stage);
-    if (g.S < 2) return QCNN_ERR_UNSUPPORTED;
+    g.S = (int)std::min<size_t>(gen ? kGenStages : kStagesMax, (kSmemMax - 1024 - raw) / g.stage);
+    // (three planes: two rings, each with room for a block's planes)
+    if (P == 3) g.S &= ~1;
+    if (g.S < (gen ? 2 : P == 3 ? 6 : P)) return QCNN_ERR_UNSUPPORTED;
     const size_t smem = std::max(kSmemLeast, g.S * (size_t)g.stage + raw + 1024);
     const int ctas = std::min(g.units, num_sms() / cg) * cg;
     return launcher(plan)(&g, ctas, smem, st);
 }
 
 qcnn_status launch_gemm_join(const GemmPlan &plan, const GemmProblem &p, cudaStream_t st) {
+    if (plan.kind == GEMM_SYM) {
+        const dim3 patches(cdiv(p.m, 32), cdiv(p.m, 32));
+        return launch_pdl(gemm_join_sym_kernel, patches, dim3(256), 0, st, p.e, p.m, plan.splits);
+    }
     const dim3 grid(cdiv(p.m, 256), std::min(p.n, 65535));
     return launch_pdl(gemm_join_kernel, grid, dim3(256), 0, st, p.e, p.m, p.n, plan.splits);
 }

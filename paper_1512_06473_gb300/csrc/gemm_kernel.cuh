@@ -6,17 +6,18 @@
 // store 32 neighbours whatever the row stride and alignment, bias and column sums are a
 // register per lane, and few rows n (a small batch) make a narrow tile, not an empty one.
 //
-// Operands come by TMA, 16 to 48 KB a stage, in the 128-byte swizzle (64-byte where the
-// stage is 32 terms deep and k is contiguous), with k or the row index contiguous.
+// Operands come by TMA, with k or the row index contiguous, in the 128-byte swizzle: a
+// stage is 64 terms of one plane of A and B, 32 to 48 KB.  (Rows of 64 bytes, 32 terms of
+// all planes, came at 40 bytes per clock and SM; rows of 128 come at 68.)
 //
-// Planes.  One: bf16 data, 64 terms a stage, one product, the whole sum in TMEM.  Two
-// (16 to 17 bits): 32 terms a stage, three products, the small ones first.  Three (all 24
-// bits of fp32): the six products of order <= 2; tcgen05.mma adds without rounding to
-// nearest, so a stage's sum (32 terms, small products first) is drained to fp32
-// registers and added there.  Against 64 bits that is closer than a chain of fp32
+// Planes.  One: bf16 data, one product, the whole sum in TMEM.  Two (16 to 17 bits): three
+// products, the small ones first.  Three (all 24 bits of fp32): the six products of order
+// <= 2; tcgen05.mma adds without rounding to nearest, so the sum of 64 terms (GEN: 32;
+// small products first) is drained to fp32 registers and added there.  A plane's stage is
+// free again after its last product.  Against 64 bits that is closer than a chain of fp32
 // multiply-adds (K = 4096: 1.4e-7 of the result).
 //
-// Roles (12 warps): 0 TMA, 1 MMA, 2 TMEM, 4-11 drain and epilogue: two warps per TMEM
+// Roles (12 warps): 0 TMA, 1 (three planes: and 3) MMA, 2 TMEM, 4-11 drain and epilogue: two warps per TMEM
 // lane quarter, 16 columns in turn.
 //
 // GEN: A is fp32 of any stride and alignment (a layer's weights), split on its way, so that
@@ -43,24 +44,24 @@ constexpr int kEpiWarps = 8;
 constexpr int kGenWarps = 4;      // converters
 constexpr int kRawSlots = 5;      // GEN: stages of raw copies, 4 KB per warp each
 constexpr int kGenCols = 48;      // TMEM columns of a stage's A: 3 planes x 32 terms
-constexpr int kGenStagesMax = 5;  // (512 - 2 * 128) / 48
+constexpr int kGenStages = 4;     // (at most (512 - 2 * 128) / 48)
 constexpr unsigned kPolls = 1u << 22;
 
 // An operand of a problem as the kernel sees it.
 struct OpArgs {
     int mn;                        // row index contiguous
     unsigned bytes, group_bytes;   // of a stage; of 64 rows (mn)
-    unsigned plane, kstep;         // descriptor units (16 bytes)
+    unsigned plane, kstep;         // descriptor units (16 bytes): GEN's planes; 16 terms
     unsigned long long desc;       // descriptor without the address
     const float *src;              // GEN
     long long ld;
-    int rows, vec;                 // GEN: extent, 16-byte copies possible
+    int vec;                       // GEN: 16-byte copies possible
 };
 struct ProblemArgs {
     CUtensorMap map_a, map_b;
     OpArgs a, b;
     unsigned idesc;
-    int m, n, k, kblocks, m_tiles, n_tiles, splits, kb_per_split, group, units;
+    int m, n, k, kblocks, m_tiles, n_tiles, tiles, splits, kb_per_split, group, units;
     GemmEpi e;
 };
 struct GemmArgs {
@@ -70,7 +71,7 @@ struct GemmArgs {
 };
 
 struct Shared {
-    uint64_t full[kStagesMax], empty[kStagesMax], tfull[2], tempty[2], done;
+    uint64_t full[kStagesMax], empty[kStagesMax], tfull[2], tempty[2], done[2];
     unsigned tmem;
     int give_up;
 };
@@ -90,6 +91,8 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u) {
     if constexpr (KIND == GEMM_SYM) {
         const int per = g.bn / (kMT * CG);  // row tiles per column tile (bn a multiple)
         int nt = 0, first = 0;
+        t.split = u / p.tiles;
+        u -= t.split * p.tiles;
         while (u >= p.m_tiles - first) {
             u -= p.m_tiles - first;
             ++nt;
@@ -97,11 +100,9 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u) {
         }
         t.nt = nt;
         t.mt = first + u;
-        t.split = 0;
     } else {
-        const int tiles = p.m_tiles * p.n_tiles;
-        t.split = u / tiles;
-        u -= t.split * tiles;
+        t.split = u / p.tiles;
+        u -= t.split * p.tiles;
         const int per = p.group * p.n_tiles, gr = u / per, m0 = gr * p.group;
         const int w = min(p.group, p.m_tiles - m0);
         u -= gr * per;
@@ -147,19 +148,19 @@ __device__ __forceinline__ void arrive_expect(uint64_t *bar, unsigned bytes) {
 // A box of a tensor map to shared memory, counted on the barrier (CG 2: on the one at
 // the same place in the pair's first CTA).
 template <int CG>
-__device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap *map, int x, int y,
+__device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap *map, int x, int y, int z,
                                          uint64_t *bar) {
     if constexpr (CG == 1)
         asm volatile(
             "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes "
             "[%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(0), "r"(smem_addr(bar))
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
             : "memory");
     else
         asm volatile(
             "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
             "[%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(0), "r"(smem_addr(bar) & 0xFEFFFFFFu)
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar) & 0xFEFFFFFFu)
             : "memory");
 }
 template <int CG>
@@ -218,6 +219,12 @@ __device__ __forceinline__ void tmem_dealloc_cg(unsigned t) {
     else
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;\n" ::"r"(t) : "memory");
 }
+template <typename T>
+__device__ __forceinline__ void swap(T &a, T &b) {
+    const T t = a;
+    a = b;
+    b = t;
+}
 __device__ __forceinline__ bool elect_one() {
     unsigned p;
     asm volatile(
@@ -259,83 +266,141 @@ __device__ __forceinline__ void tmem_st16(unsigned taddr, const float (&v)[16]) 
 // decided outside them: inside, a decision per element kept each load behind the one
 // before (a tile with a residual took 123 us instead of its product's 52).
 
-// 16 columns of a lane to out[n0 + i][m] (m in range), row by row: the warp's lanes are
-// neighbours.  left: columns that exist.
-__device__ __forceinline__ void store16(void *out, int type, long long ld, long long plane, int m, int n0,
-                                        int left, const float (&v)[16]) {
-    const long long o = (long long)n0 * ld + m;
+// Types of two bytes go in pairs where pairs are aligned (`pair`): of columns 2 i and 2 i + 1
+// an even lane takes the first for itself and its neighbour, the odd one the second, after
+// (before) an exchange between the two.  Half the accesses: with one of two bytes per
+// element the epilogue took 8 x 3,700 clocks for a tile of 256 columns in three planes.
+
+// The word of this lane after the exchange: w = (column 2 i, column 2 i + 1) of its row m ->
+// (even) column 2 i of rows m, m + 1, (odd) column 2 i + 1 of m - 1, m.  And back.
+__device__ __forceinline__ unsigned exchange(unsigned w, bool odd) {
+    const unsigned o = __shfl_xor_sync(0xffffffffu, w, 1);
+    return odd ? __byte_perm(o, w, 0x7632) : __byte_perm(w, o, 0x5410);
+}
+
+// 16 columns of a lane to out[n0 + i][m], row by row: the warp's lanes are neighbours.
+// m_end, left: rows m and columns that exist (of planes, a row more may be written).  The
+// whole warp calls it.
+__device__ __forceinline__ void store_plane(unsigned short *out, long long ld, bool pair, int m_end, int m, int n0,
+                                            int left, const unsigned (&w)[8]) {
+    const bool odd = m & 1;
+    const bool in = (pair ? m - odd : m) < m_end;
+    if (pair) {
+        unsigned short *p = out + (long long)(n0 + odd) * ld + (m - odd);
+        if (odd) --left;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, p += 2 * ld) {
+            const unsigned x = exchange(w[i], odd);
+            if (in && 2 * i < left) *reinterpret_cast<unsigned *>(p) = x;
+        }
+    } else {
+        unsigned short *p = out + (long long)n0 * ld + m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, p += 2 * ld) {
+            if (in && 2 * i < left) p[0] = (unsigned short)w[i];
+            if (in && 2 * i + 1 < left) p[ld] = (unsigned short)(w[i] >> 16);
+        }
+    }
+}
+__device__ __forceinline__ void store16(void *out, int type, long long ld, long long plane, bool pair, int m_end,
+                                        int m, int n0, int left, const float (&v)[16]) {
     if (type == GEMM_T_F32) {
-        float *p = static_cast<float *>(out) + o;
+        const bool in = m < m_end;
+        float *p = static_cast<float *>(out) + (long long)n0 * ld + m;
 #pragma unroll
         for (int i = 0; i < 16; ++i, p += ld)
-            if (i < left) *p = v[i];
+            if (in && i < left) *p = v[i];
         return;
     }
-    unsigned short *p = static_cast<unsigned short *>(out) + o;
-    auto put = [&](unsigned short *d, const unsigned (&w)[8]) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i, d += 2 * ld) {
-            if (2 * i < left) d[0] = (unsigned short)w[i];
-            if (2 * i + 1 < left) d[ld] = (unsigned short)(w[i] >> 16);
-        }
-    };
+    unsigned short *p = static_cast<unsigned short *>(out);
     unsigned w0[8], w1[8], w2[8];
     if (type == GEMM_T_BF16) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w0[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-        put(p, w0);
     } else if (type == GEMM_T_PLANES2) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) planes2(v[2 * i], v[2 * i + 1], w0[i], w1[i]);
-        put(p, w0);
-        put(p + plane, w1);
+        store_plane(p + plane, ld, pair, m_end, m, n0, left, w1);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
-        put(p, w0);
-        put(p + plane, w1);
-        put(p + 2 * plane, w2);
+        store_plane(p + plane, ld, pair, m_end, m, n0, left, w1);
+        store_plane(p + 2 * plane, ld, pair, m_end, m, n0, left, w2);
+    }
+    store_plane(p, ld, pair, m_end, m, n0, left, w0);
+}
+
+// 16 columns of a lane of a matrix, on their way: loaded by fetch, values by take (a chunk
+// of columns later: nothing waits in between).  fp32 and single elements: 16 words; pairs:
+// eight words a plane (planes always go in pairs).
+struct Chunk16 {
+    unsigned w[24];
+};
+template <int J>
+__device__ __forceinline__ void fetch_pairs(Chunk16 &c, const unsigned short *src, long long ld, int m_end, int m,
+                                            int n0, int left) {
+    const bool odd = m & 1, in = m - odd < m_end;
+    const unsigned short *p = src + (long long)(n0 + odd) * ld + (m - odd);
+    if (odd) --left;
+#pragma unroll
+    for (int i = 0; i < 8; ++i, p += 2 * ld) {
+        c.w[8 * J + i] = 0;
+        if (in && 2 * i < left) c.w[8 * J + i] = *reinterpret_cast<const unsigned *>(p);
     }
 }
-// 16 columns of a lane of a matrix; the last that exists again past the end.
-__device__ __forceinline__ void load16(const void *src, int type, long long ld, long long plane, int m, int n0,
-                                       int left, float (&v)[16]) {
-    const long long o = (long long)n0 * ld + m;
+__device__ __forceinline__ void fetch16(Chunk16 &c, const void *src, int type, long long ld, long long plane,
+                                        bool pair, int m_end, int m, int n0, int left) {
+    const bool in = m < m_end;
+    const unsigned short *p = static_cast<const unsigned short *>(src);
     if (type == GEMM_T_F32) {
-        const float *p = static_cast<const float *>(src) + o;
+        const float *f = static_cast<const float *>(src) + (long long)n0 * ld + m;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            v[i] = *p;
-            if (i + 1 < left) p += ld;
+        for (int i = 0; i < 16; ++i, f += ld) {
+            c.w[i] = 0;
+            if (in && i < left) c.w[i] = __float_as_uint(*f);
         }
-        return;
-    }
-    const unsigned short *p = static_cast<const unsigned short *>(src) + o;
-    auto get = [&](const unsigned short *d, float (&r)[16]) {
+    } else if (!pair) {
+        p += (long long)n0 * ld + m;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            r[i] = bf16_to_float(*d);
-            if (i + 1 < left) d += ld;
+        for (int i = 0; i < 16; ++i, p += ld) {
+            c.w[i] = 0;
+            if (in && i < left) c.w[i] = *p;
         }
-    };
-    if (type == GEMM_T_BF16) {
-        get(p, v);
-        return;
-    }
-    float w[16];
-    if (type == GEMM_T_PLANES2) {
-        get(p, v);
-        get(p + plane, w);
     } else {
-        float x[16];
-        get(p, v);
-        get(p + plane, w);
-        get(p + 2 * plane, x);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] += x[i];
+        fetch_pairs<0>(c, p, ld, m_end, m, n0, left);
+        if (type >= GEMM_T_PLANES2) fetch_pairs<1>(c, p + plane, ld, m_end, m, n0, left);
+        if (type == GEMM_T_PLANES3) fetch_pairs<2>(c, p + 2 * plane, ld, m_end, m, n0, left);
     }
+}
+// v += scale * what was fetched.
+__device__ __forceinline__ void take16(const Chunk16 &c, int type, bool pair, bool odd, float scale,
+                                       float (&v)[16]) {
+    if (type == GEMM_T_F32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] += w[i];
+        for (int i = 0; i < 16; ++i) v[i] = fmaf(scale, __uint_as_float(c.w[i]), v[i]);
+    } else if (!pair) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = fmaf(scale, __uint_as_float(c.w[i] << 16), v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned x = exchange(c.w[i], odd);
+            float lo = __uint_as_float(x << 16), hi = __uint_as_float(x & 0xffff0000u);
+            if (type >= GEMM_T_PLANES2) {
+                const unsigned y = exchange(c.w[8 + i], odd);
+                float lo1 = __uint_as_float(y << 16), hi1 = __uint_as_float(y & 0xffff0000u);
+                if (type == GEMM_T_PLANES3) {
+                    const unsigned z = exchange(c.w[16 + i], odd);
+                    lo1 += __uint_as_float(z << 16);
+                    hi1 += __uint_as_float(z & 0xffff0000u);
+                }
+                lo += lo1;
+                hi += hi1;
+            }
+            v[2 * i] = fmaf(scale, lo, v[2 * i]);
+            v[2 * i + 1] = fmaf(scale, hi, v[2 * i + 1]);
+        }
+    }
 }
 __device__ __forceinline__ void act16(float (&v)[16], int act) {
     if (act == QCNN_ACT_RELU) {
@@ -350,38 +415,46 @@ __device__ __forceinline__ void act16(float (&v)[16], int act) {
     }
 }
 
-// OUT and SYM: sums v of lane m (in range), columns n0 .. n0 + left - 1; r: what add has
-// there.
-template <int KIND>
-__device__ __forceinline__ void finish_out(const GemmEpi &e, int m, int n0, int left, float alpha, float bias,
-                                           float (&v)[16], const float (&r)[16]) {
+// OUT and SYM: sums v of lane m, columns n0 .. n0 + left - 1; c: what add has there, which
+// next() then fetches for the columns that follow.  The whole warp calls it; rows m up to
+// m_end exist.
+template <int KIND, typename F>
+__device__ __forceinline__ void finish_out(const GemmEpi &e, int m_end, int m, int n0, int left, float alpha,
+                                           float bias, float (&v)[16], const Chunk16 &c, F &&next) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = fmaf(alpha, v[i], bias);
-    if (KIND == GEMM_OUT && e.pre) store16(e.pre, e.out_type, e.ldp, 0, m, n0, left, v);
+    if (KIND == GEMM_OUT && e.pre) store16(e.pre, e.out_type, e.ldp, 0, e.pair & 2, m_end, m, n0, left, v);
     if constexpr (KIND == GEMM_OUT) act16(v, e.act);
     if (e.add) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = fmaf(e.beta, r[i], v[i]);
+        take16(c, e.add_type, e.pair & 4, m & 1, e.beta, v);
+        next();
     }
     if constexpr (KIND == GEMM_OUT) {
-        store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, left, v);
+        store16(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
     } else {
-        // one value for both places: this tile's where m >= n
+        // one value for both places: this tile's where m >= n.  (Above the diagonal inside a
+        // tile: the other place's are stored, by the lanes whose row is the column here.)
+        const bool in = m < m_end;
         left = min(left, m + 1 - n0);
-        if (left <= 0) return;
-        store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, left, v);
-        unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)m * e.ldo + n0;
-        auto put = [&](unsigned short *d, const unsigned (&w)[8]) {
-            if (left >= 16) {  // (rows of planes: 16-byte multiples)
+        unsigned short *p = static_cast<unsigned short *>(e.out);
+        unsigned w0[8], w1[8], w2[8];
+        auto put = [&](unsigned short *plane, const unsigned (&w)[8]) {
+            unsigned short *q = plane + (long long)n0 * e.ldo + m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i, q += 2 * e.ldo) {
+                if (in && 2 * i < left) q[0] = (unsigned short)w[i];
+                if (in && 2 * i + 1 < left) q[e.ldo] = (unsigned short)(w[i] >> 16);
+            }
+            unsigned short *d = plane + (long long)m * e.ldo + n0;
+            if (in && left >= 16) {  // (rows of planes: 16-byte multiples)
                 *reinterpret_cast<uint4 *>(d) = make_uint4(w[0], w[1], w[2], w[3]);
                 *reinterpret_cast<uint4 *>(d + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-            } else {
+            } else if (in && left > 0) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (i < left) d[i] = (unsigned short)(w[i / 2] >> (i & 1) * 16);
             }
         };
-        unsigned w0[8], w1[8], w2[8];
         if (e.out_type == GEMM_T_PLANES2) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) planes2(v[2 * i], v[2 * i + 1], w0[i], w1[i]);
@@ -444,7 +517,7 @@ __device__ __forceinline__ void stats16(RunningSum &s, int n0, int target, float
 }
 
 // Gradient of a class (lane m) for 16 rows; rows: theirs, without a class past the last.
-__device__ __forceinline__ void dlogits16(const GemmEpi &e, int m, int m_end, int n0, int left, float bias,
+__device__ __forceinline__ void dlogits16(const GemmEpi &e, int m_end, int m, int n0, int left, float bias,
                                           const float4 *rows, float &col, float (&v)[16]) {
     const int c = e.class0 + m;
 #pragma unroll
@@ -457,7 +530,7 @@ __device__ __forceinline__ void dlogits16(const GemmEpi &e, int m, int m_end, in
         v[i] = target >= 0 ? r.y * p : 0.f;
         col += v[i];
     }
-    if (m < m_end) store16(e.out, e.out_type, e.ldo, e.out_plane, m, n0, left, v);
+    store16(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
 }
 
 // ---------------------------------------------------------------------- GEN
@@ -496,8 +569,14 @@ __device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned (&v)[8])
 // ------------------------------------------------------------------- kernel
 template <int P, int KIND, int CG, bool GEN>
 __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
-    constexpr int BK = P == 1 ? 64 : 32, KS = BK / 16;
-    constexpr bool DRAIN = P == 3;  // a stage's sum at a time
+    constexpr int BK = GEN ? 32 : 64, KS = BK / 16;
+    constexpr int PL = GEN ? 1 : P;  // stages (planes) of a block of terms
+    constexpr bool DRAIN = P == 3;   // a block's sum at a time
+    // Rings of stages, blocks in turn, and as many warps that issue MMAs, each with a ring
+    // and an accumulator of its own.  (A warp's waits come back behind the MMAs that it has
+    // issued: one alone left the tensor core idle between accumulators, 1,204 clocks per block
+    // of 888.  And a ring has one consumer: a wait for a phase two ahead passes at once.)
+    constexpr int RINGS = DRAIN ? 2 : 1;
     constexpr int ACC = GEN ? 128 : kAccCols;
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ Shared sh;
@@ -520,8 +599,8 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.tfull[i], 1);
             mbar_init(&sh.tempty[i], kEpiWarps * CG);
+            mbar_init(&sh.done[i], 1);
         }
-        mbar_init(&sh.done, 1);
         sh.give_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async_smem();
@@ -532,111 +611,152 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
     if constexpr (CG == 2) cluster_sync_all();
     tc_fence_after_sync();
     const unsigned tmem = sh.tmem;
-    grid_dep_sync();
+    // (each role waits for the kernel before it where it first needs memory: what it works
+    // out before that, a first tile and its operands' maps, took 2,000 clocks)
 
     if (warp == 0) {
-        {
-            // ----------------------------------------------------------- TMA
-            if (elect_one()) {
-                int slot = 0, issued = 0;
-                unsigned par = 0;
-                bool ok = true;
-                for (int u = first_unit; u < g.units && ok; u += step) {
-                    const Tile t = tile_of<KIND, CG>(g, u);
-                    const ProblemArgs &p = g.p[t.q];
-                    const int m0 = (t.mt * CG + (int)rank) * kMT;
-                    const int bn = g.bn / CG, n0 = t.nt * g.bn + (int)rank * bn;
-                    const unsigned bytes = ((GEN ? 0 : p.a.bytes) + p.b.bytes) * CG;
-                    for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                        if (!(ok = wait_one(sh, &sh.empty[slot], par ^ 1))) break;
-                        uint64_t *const full = &sh.full[slot];
+        // --------------------------------------------------------------- TMA
+        if (elect_one()) {
+            const int S = g.S / RINGS;
+            int slot = 0, slot2 = 0;           // next stage of the block's ring, of the other
+            unsigned par = 0, par2 = 0, ring = 0;
+            unsigned issued = 0, issued2 = 0;
+            bool ok = true, synced = false;
+            for (int u = first_unit; u < g.units && ok; u += step) {
+                const Tile t = tile_of<KIND, CG>(g, u);
+                const ProblemArgs &p = g.p[t.q];
+                const int m0 = (t.mt * CG + (int)rank) * kMT;
+                const int bn = g.bn / CG, n0 = t.nt * g.bn + (int)rank * bn;
+                const unsigned bytes = ((GEN ? 0 : p.a.bytes) + p.b.bytes) * CG;
+                const bool a_mn = p.a.mn, b_mn = p.b.mn;
+                const CUtensorMap *const map_a = &p.map_a, *const map_b = &p.map_b;
+                const unsigned a_group = p.a.group_bytes, b_group = p.b.group_bytes;
+                // (no prefetch.tensormap: with it every copy of the kernel came slower, 4096 rows of
+                // 4096 -> 8192 in 179 us instead of 173)
+                if (!synced) {
+                    grid_dep_sync();
+                    synced = true;
+                }
+                for (int kb = t.kb0; kb < t.kb1 && ok; ++kb) {
+                    const int k = kb * BK;
+#pragma unroll
+                    for (int z = PL - 1; z >= 0; --z) {  // (in the order that they become free)
+                        const int at = (int)ring * S + slot;
+                        if (!(ok = wait_one(sh, &sh.empty[at], par ^ 1))) break;
+                        uint64_t *const full = &sh.full[at];
                         if (rank == 0) arrive_expect(full, bytes);
-                        const unsigned a = smem_addr(smem) + slot * g.stage, b = a + g.b_off;
-                        const int k = kb * BK;
+                        const unsigned a = smem_addr(smem) + at * g.stage, b = a + g.b_off;
                         if (GEN) {
-                        } else if (p.a.mn) {
-                            tma_load<CG>(a, &p.map_a, m0, k, full);
-                            tma_load<CG>(a + p.a.group_bytes, &p.map_a, m0 + 64, k, full);
+                        } else if (a_mn) {
+                            tma_load<CG>(a, map_a, m0, k, z, full);
+                            tma_load<CG>(a + a_group, map_a, m0 + 64, k, z, full);
                         } else {
-                            tma_load<CG>(a, &p.map_a, k, m0, full);
+                            tma_load<CG>(a, map_a, k, m0, z, full);
                         }
-                        if (p.b.mn) {
+                        if (b_mn) {
                             for (int i = 0; i < bn; i += 64)
-                                tma_load<CG>(b + (i >> 6) * p.b.group_bytes, &p.map_b, n0 + i, k, full);
+                                tma_load<CG>(b + (i >> 6) * b_group, map_b, n0 + i, k, z, full);
                         } else {
-                            tma_load<CG>(b, &p.map_b, k, n0, full);
+                            tma_load<CG>(b, map_b, k, n0, z, full);
                         }
                         ++issued;
-                        if (++slot == g.S) {
+                        if (++slot == S) {
                             slot = 0;
                             par ^= 1;
                         }
                     }
+                    if constexpr (RINGS == 2) {
+                        ring ^= 1;
+                        swap(slot, slot2);
+                        swap(par, par2);
+                        swap(issued, issued2);
+                    }
                 }
-                // no copy of its own under way when the CTA leaves
-                if (rank == 0 || !ok)
-                    for (int i = max(0, issued - g.S); i < issued; ++i)
-                        mbar_wait_bounded(rank == 0 ? &sh.full[i % g.S] : &sh.empty[i % g.S],
-                                          (unsigned)(i / g.S) & 1, kPolls);
             }
+            if (!synced) grid_dep_sync();
+            // no copy of its own under way when the CTA leaves
+            if (rank == 0 || !ok)
+                for (int r = 0; r < RINGS; ++r, ring ^= 1, issued = issued2)
+                    for (unsigned i = issued > (unsigned)S ? issued - S : 0; i < issued; ++i) {
+                        const int at = (int)ring * S + (int)(i % S);
+                        mbar_wait_bounded(rank == 0 ? &sh.full[at] : &sh.empty[at], i / S & 1, kPolls);
+                    }
         }
         __syncwarp();
-    } else if (warp == 1) {
+    } else if (warp == 1 || (RINGS == 2 && warp == 3)) {
         // --------------------------------------------------------------- MMA
         if (rank == 0 && elect_one()) {
+            const unsigned ring = warp >> 1;  // this warp's, and its accumulator
+            const int S = g.S / RINGS;
             int slot = 0;
-            unsigned par = 0, use = 0;  // use: accumulators so far
+            unsigned par = 0;
+            unsigned use = 0, block = 0;  // accumulators, blocks so far
             bool ok = true;
-            const uint64_t base = (uint64_t)((smem_addr(smem) >> 4) & 0x3FFFu);
+            const unsigned stage = g.stage >> 4;
+            const uint64_t base = (uint64_t)((smem_addr(smem) >> 4) & 0x3FFFu) + ring * S * stage;
             for (int u = first_unit; u < g.units && ok; u += step) {
                 const Tile t = tile_of<KIND, CG>(g, u);
                 const ProblemArgs &p = g.p[t.q];
                 const uint64_t da = p.a.desc + base, db = p.b.desc + base + (g.b_off >> 4);
-                const unsigned pa = p.a.plane, pb = p.b.plane, ka = p.a.kstep, kb_ = p.b.kstep;
+                const unsigned ka = p.a.kstep, kb_ = p.b.kstep;
+                [[maybe_unused]] const unsigned pb = p.b.plane;
                 const uint32_t idesc = p.idesc;
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (RINGS == 2 && (block++ & 1) != ring) continue;  // the other warp's
                     const bool fresh = DRAIN || kb == t.kb0;
+                    const unsigned buf = RINGS == 2 ? ring : use & 1;
                     if (fresh) {
-                        if (!(ok = wait_one(sh, &sh.tempty[use & 1], (use >> 1 & 1) ^ 1))) break;
+                        const unsigned n = RINGS == 2 ? use : use >> 1;  // of this accumulator
+                        if (!(ok = wait_one(sh, &sh.tempty[buf], (n & 1) ^ 1))) break;
                     }
-                    if (!(ok = wait_one(sh, &sh.full[slot], par))) break;
+                    // the stages of this block's planes, the last plane first
+                    int at[PL];
+#pragma unroll
+                    for (int z = PL - 1; z >= 0; --z) {
+                        at[z] = slot;
+                        ok = ok && wait_one(sh, &sh.full[ring * S + slot], par);
+                        if (++slot == S) {
+                            slot = 0;
+                            par ^= 1;
+                        }
+                    }
+                    if (!ok) break;
                     tc_fence_after_sync();
-                    const unsigned d = tmem + (use & 1) * ACC;
-                    [[maybe_unused]] const unsigned at = tmem + 2 * ACC + slot * kGenCols;
-                    const uint64_t a = da + slot * (g.stage >> 4), b = db + slot * (g.stage >> 4);
+                    const unsigned d = tmem + buf * ACC;
                     bool acc = !fresh;
                     auto product = [&](int i, int j) {
 #pragma unroll
                         for (int s = 0; s < KS; ++s) {
-                            if constexpr (GEN) mma_ts(d, at + i * 16 + s * 8, b + j * pb + s * kb_, idesc, acc);
-                            else mma_ss<CG>(d, a + i * pa + s * ka, b + j * pb + s * kb_, idesc, acc);
+                            if constexpr (GEN)
+                                mma_ts(d, tmem + 2 * ACC + (ring * S + at[0]) * kGenCols + i * 16 + s * 8,
+                                       db + at[0] * stage + j * pb + s * kb_, idesc, acc);
+                            else
+                                mma_ss<CG>(d, da + at[i] * stage + s * ka, db + at[j] * stage + s * kb_, idesc, acc);
                             acc = true;
                         }
                     };
                     if constexpr (P == 3) {
-                        product(2, 0);
                         product(1, 1);
+                        product(2, 0);
                         product(0, 2);
+                        if constexpr (!GEN) commit<CG>(&sh.empty[ring * S + at[PL - 1]]);
                     }
                     if constexpr (P >= 2) {
                         product(1, 0);
                         product(0, 1);
+                        if constexpr (!GEN) commit<CG>(&sh.empty[ring * S + at[PL > 1]]);
                     }
                     product(0, 0);
-                    commit<CG>(&sh.empty[slot]);
+                    commit<CG>(&sh.empty[ring * S + at[0]]);
                     if (DRAIN || kb + 1 == t.kb1) {
-                        commit<CG>(&sh.tfull[use & 1]);
+                        commit<CG>(&sh.tfull[buf]);
                         ++use;
-                    }
-                    if (++slot == g.S) {
-                        slot = 0;
-                        par ^= 1;
                     }
                 }
             }
             // nothing in flight when the tensor memory is freed
-            commit_here<CG>(&sh.done);
-            mbar_wait_bounded(&sh.done, 0, kPolls);
+            commit_here<CG>(&sh.done[ring]);
+            mbar_wait_bounded(&sh.done[ring], 0, kPolls);
         }
         __syncwarp();
     } else if (warp >= 4 && warp < 4 + kEpiWarps) {
@@ -644,6 +764,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const unsigned tl = tmem + ((unsigned)(quarter * 32) << 16);
         const int chunks = g.bn / 16;  // this warp's: half, half + 2, ...
+        grid_dep_sync();
         unsigned use = 0;
         bool ok = true;
         auto release = [&](unsigned buf) {
@@ -664,7 +785,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             [[maybe_unused]] const float alpha = KIND == GEMM_OUT && e.alpha_ptr ? *e.alpha_ptr : e.alpha;
             [[maybe_unused]] RunningSum run;
             [[maybe_unused]] int target = -1;
-            [[maybe_unused]] const bool adds = in && e.add && !e.partial;
+            [[maybe_unused]] const bool adds = e.add && !e.partial;
             if constexpr (KIND == GEMM_STATS) {
                 if (in) {
                     const long long c = e.targets[m];
@@ -675,7 +796,8 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             }
             // the sums of the tile, in TMEM at tl + buf * ACC
             unsigned buf = use & 1;
-            if constexpr (DRAIN) {
+            const bool drain = DRAIN && t.kb1 - t.kb0 > 1;
+            if (drain) {
                 constexpr int CH = GEN ? 4 : 8;  // chunks of a warp at most
                 float acc[CH][16];
 #pragma unroll
@@ -709,7 +831,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 ++use;
             }
             // (what a chunk of columns needs from memory is fetched one chunk ahead)
-            float add[16];
+            [[maybe_unused]] Chunk16 add;
             [[maybe_unused]] Column column = {};
             auto fetch = [&](int c) {
                 if constexpr (COLUMNS) {
@@ -723,23 +845,18 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 if constexpr (KIND == GEMM_OUT || KIND == GEMM_SYM) {
                     const int left = p.n - (n0 + c * 16);
                     if (adds && c < chunks && left > 0)
-                        load16(e.add, e.add_type, e.lda, e.add_plane, m, n0 + c * 16, left, add);
+                        fetch16(add, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0 + c * 16, left);
                 }
             };
             fetch(half);
-            if constexpr (!DRAIN) {
+            if (!drain) {
                 if (!(ok = wait_warp(sh, &sh.tfull[buf], (use - 1) >> 1 & 1))) break;
                 tc_fence_after_sync();
             }
 #pragma unroll 1
             for (int c = half; c < chunks; c += 2) {
                 const int n = n0 + c * 16, left = p.n - n;
-                float v[16], r[16];
-                if constexpr (KIND == GEMM_OUT || KIND == GEMM_SYM) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) r[i] = add[i];
-                    fetch(c + 2);
-                }
+                float v[16];
                 [[maybe_unused]] Column *const cols = columns[COLUMNS ? warp - 4 : 0][c >> 1 & 1];
                 if constexpr (COLUMNS) {
                     if (lane < 16) cols[lane] = column;
@@ -750,12 +867,13 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 if constexpr (KIND == GEMM_STATS) {
                     stats16(run, n, target, e.target_logit + m, cols, v);
                 } else if constexpr (KIND == GEMM_DLOGITS) {
-                    dlogits16(e, m, p.m, n, left, bias, cols, col, v);
-                } else if (in && left > 0) {
-                    if (KIND == GEMM_OUT && e.partial)
-                        store16(e.partial + (long long)t.split * p.n * p.m, GEMM_T_F32, p.m, 0, m, n, left, v);
+                    dlogits16(e, p.m, m, n, left, bias, cols, col, v);
+                } else if (left > 0) {
+                    if (e.partial)
+                        store16(e.partial + (long long)t.split * p.n * p.m, GEMM_T_F32, p.m, 0, false, p.m, m, n,
+                                left, v);
                     else
-                        finish_out<KIND>(e, m, n, left, alpha, bias, v, r);
+                        finish_out<KIND>(e, p.m, m, n, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                 }
             }
             release(buf);
@@ -795,6 +913,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             src = base + (mn ? (long long)k * ld + row : (long long)row * ld + k);
         };
         if (cu < g.units) open_tile();
+        // (the weights are the caller's, complete before the first kernel of this call: no wait)
         auto copy_next = [&]() {
             if (cu < g.units) {
                 const float *s = src;
@@ -824,8 +943,9 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         };
         for (int i = 0; i < kRawSlots - 1; ++i) copy_next();
         const unsigned a_dst = tmem + 2 * ACC + ((unsigned)(quarter * 32) << 16);
-        int slot = 0, rslot = 0;
-        unsigned par = 0;
+        const int S = g.S / RINGS;
+        int slot = 0, slot2 = 0, rslot = 0;  // (stages: as the TMA's)
+        unsigned par = 0, par2 = 0, ring = 0;
         bool ok = true;
         for (int u = first_unit; u < g.units && ok; u += step) {
             const Tile t = tile_of<KIND, CG>(g, u);
@@ -845,9 +965,10 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                                      : "=f"(v[4 * i]), "=f"(v[4 * i + 1]), "=f"(v[4 * i + 2]), "=f"(v[4 * i + 3])
                                      : "r"(r + lane * 128 + ((i ^ (lane & 7)) << 4)));
                 }
-                if (!(ok = wait_warp(sh, &sh.empty[slot], par ^ 1))) break;
+                const int at = (int)ring * S + slot;
+                if (!(ok = wait_warp(sh, &sh.empty[at], par ^ 1))) break;
                 tc_fence_after_sync();
-                const unsigned d = a_dst + slot * kGenCols;
+                const unsigned d = a_dst + at * kGenCols;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     unsigned w0[8], w1[8], w2[8];
@@ -863,11 +984,14 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) arrive(&sh.full[slot]);
-                if (++slot == g.S) {
+                if (lane == 0) arrive(&sh.full[at]);
+                if (++slot == S) {
                     slot = 0;
                     par ^= 1;
                 }
+                ring ^= 1;
+                swap(slot, slot2);
+                swap(par, par2);
                 if (++rslot == kRawSlots) rslot = 0;
             }
         }

@@ -176,8 +176,13 @@ OrthoPlan plan_ortho(int m, int n, int dtype) {
     o.P = dtype == QCNN_F32 ? 3 : 2;
     o.p = std::min(m, n);
     o.q = std::max(m, n);
-    o.gram.plan = plan_gemm(o.P, GEMM_SYM, o.p, o.p, o.q, 1);
-    o.poly.plan = plan_gemm(o.P, GEMM_SYM, o.p, o.p, o.p, 1);
+    // (one side of the diagonal, or both in smaller tiles where that is sooner done)
+    const auto sym = [&](int k) {
+        const GemmPlan s = plan_gemm(o.P, GEMM_SYM, o.p, o.p, k, 64), f = plan_gemm(o.P, GEMM_OUT, o.p, o.p, k, 64);
+        return f.score < s.score ? f : s;
+    };
+    o.gram.plan = sym(o.q);
+    o.poly.plan = sym(o.p);
     o.apply.plan = m <= n ? plan_gemm(o.P, GEMM_OUT, o.q, o.p, o.p, 64) : plan_gemm(o.P, GEMM_OUT, o.p, o.q, o.p, 64);
     return o;
 }
@@ -196,7 +201,7 @@ OrthoSpace carve_ortho(const OrthoPlan &o, int m, int n, void *ws) {
     s.x[1] = c.array<unsigned short>(xs);
     s.a = c.array<unsigned short>(as);
     s.b = c.array<unsigned short>(as);
-    s.partial = c.take(o.apply.scratch());
+    s.partial = c.take(std::max({o.gram.scratch(), o.poly.scratch(), o.apply.scratch()}));
     s.bytes = c.used;
     return s;
 }
@@ -227,7 +232,7 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
         g.e.ldo = pa;
         g.e.out_plane = aplane;
         g.e.out_type = type;
-        if ((rc = launch_gemm(o.gram.plan, &g, 1, st)) != QCNN_OK) break;
+        if ((rc = o.gram.run(g, s.partial, st)) != QCNN_OK) break;
         g.a = g.b = a;
         g.k = o.p;
         g.e.alpha = k[2];
@@ -237,7 +242,7 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
         g.e.add_plane = aplane;
         g.e.add_type = type;
         g.e.out = s.b;
-        if ((rc = launch_gemm(o.poly.plan, &g, 1, st)) != QCNN_OK) break;
+        if ((rc = o.poly.run(g, s.partial, st)) != QCNN_OK) break;
         GemmProblem u;
         u.k = o.p;
         if (wide) {  // X' [p][q] = B X

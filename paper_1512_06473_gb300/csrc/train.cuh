@@ -38,7 +38,7 @@ inline qcnn_status workspace_ok(const void *ws, size_t have, size_t need) {
     return QCNN_OK;
 }
 
-// One product on the tensor cores, split or not; its operands in bf16 planes or fp32.
+// One product on the tensor cores, split or not.
 struct Product {
     GemmPlan plan;
     size_t scratch() const { return plan.partial_bytes; }

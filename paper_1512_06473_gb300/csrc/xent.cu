@@ -256,7 +256,8 @@ XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool g
     s.inv = c.array<float>(1);
     if (grad) s.rows = c.array<float4>(N);
     // (few rows read the operands as they are; their gradient does not)
-    if (!p.few && (!bf16 || !xa)) s.x = c.array<unsigned short>(P * N * pc);
+    const bool x_copy = !p.few && (!bf16 || !xa);
+    if (x_copy) s.x = c.array<unsigned short>(P * N * pc);
     if ((!p.few || grad) && (bf16 ? !wa : p.wplanes)) s.w = c.array<unsigned short>(P * Ct * pc);
     size_t partial = 0;
     if (p.small) {
