@@ -13,6 +13,7 @@
 #include "train.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace qcnn {
 namespace {
@@ -145,20 +146,22 @@ qcnn_status few_rows_of(const FewRows &f, cudaStream_t st) {
 // ------------------------------------------------- gradient of z, bias
 // dz = dy * act'(z) in planes (out null: only sums) and sums over a slab of rows:
 // part[slab][cols].  A CTA takes 128 columns x a slab: a warp a row, a lane four
-// columns.
-template <typename T>
+// columns: neighbours (VEC), or 32 apart, so that rows off the 8- or 16-byte alignment are
+// read and written by neighbouring lanes too (3001 x 5003 in bf16 41 us with the lane's four
+// next to each other).
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, const T *pre, long long ldp,
-                                                 int N, int Ct, int act, void *out, int planes,
-                                                 long long ldo, long long plane, float *part, int slab,
-                                                 int vec) {
+                                                 int N, int Ct, int act, unsigned short *out, int planes,
+                                                 long long ldo, long long plane, float *part, int slab) {
     __shared__ float red[8][128];
     grid_dep_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c = blockIdx.x * 128 + lane * 4;
+    constexpr int GAP = VEC ? 1 : 32;
+    const int own = VEC ? lane * 4 : lane, c = blockIdx.x * 128 + own;
     const int r1 = min(N, ((int)blockIdx.y + 1) * slab);
     float sum[4] = {};
     auto load4 = [&](const T *p, float (&v)[4]) {
-        if (vec && c + 4 <= Ct) {
+        if (VEC && c + 4 <= Ct) {
             if constexpr (sizeof(T) == 4) {
                 const float4 a = *reinterpret_cast<const float4 *>(p);
                 v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
@@ -169,11 +172,11 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, co
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = c + j < Ct ? as_float<T>(p[j]) : 0.f;
+            for (int j = 0; j < 4; ++j) v[j] = c + j * GAP < Ct ? as_float<T>(p[j * GAP]) : 0.f;
         }
     };
     if (c < Ct) {
-#pragma unroll 2
+#pragma unroll 4
         for (int r = (int)blockIdx.y * slab + warp; r < r1; r += 8) {
             float v[4];
             load4(dy + (long long)r * lddy + c, v);
@@ -186,22 +189,27 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, co
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[j] += v[j];
             if (out) {  // (its rows are ours: multiples of 8 elements, 16-byte aligned)
-                const long long o = (long long)r * ldo + c;
                 unsigned w[3][2];
-                unsigned short *d = static_cast<unsigned short *>(out) + o;
+                unsigned short *d = out + (long long)r * ldo + c;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
-                *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
-                if (planes == 3) {
-                    *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
-                    *reinterpret_cast<uint2 *>(d + 2 * plane) = make_uint2(w[2][0], w[2][1]);
+#pragma unroll
+                for (int i = 0; i < 3; ++i, d += plane) {
+                    if (i >= planes) break;
+                    if constexpr (VEC) {
+                        *reinterpret_cast<uint2 *>(d) = make_uint2(w[i][0], w[i][1]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (c + j * GAP < Ct) d[j * GAP] = (unsigned short)(w[i][j / 2] >> (j & 1) * 16);
+                    }
                 }
             }
         }
     }
     if (!part) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) red[warp][lane * 4 + j] = sum[j];
+    for (int j = 0; j < 4; ++j) red[warp][own + j * GAP] = sum[j];
     __syncthreads();
     const int t = threadIdx.x, col = blockIdx.x * 128 + t;
     if (t < 128 && col < Ct) {
@@ -443,16 +451,19 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
         const auto vec_ok = [&](const void *q, long long ld) {
             return reinterpret_cast<uintptr_t>(q) % (4 * e) == 0 && ld % 4 == 0;
         };
-        const int vec = vec_ok(dy, lddy) && (act == QCNN_ACT_NONE || vec_ok(pre, ldp));
+        const bool vec = vec_ok(dy, lddy) && (act == QCNN_ACT_NONE || vec_ok(pre, ldp));
+        unsigned short *const out = static_cast<unsigned short *>(s.dz);
+        const auto launch = [&](auto k, auto *type) {
+            using T = std::remove_pointer_t<decltype(type)>;
+            return launch_pdl(k, grid, dim3(256), 0, st, static_cast<const T *>(dy), lddy,
+                              static_cast<const T *>(pre), ldp, N, Ct, act, out, P, pz, (long long)N * pz, part,
+                              p.slab);
+        };
         if (bf16)
-            rc = launch_pdl(dz_kernel<unsigned short>, grid, dim3(256), 0, st,
-                            static_cast<const unsigned short *>(dy), lddy,
-                            static_cast<const unsigned short *>(pre), ldp, N, Ct, act, s.dz, bf16 ? 1 : 3, pz,
-                            (long long)N * pz, part, p.slab, vec);
+            rc = launch(vec ? dz_kernel<unsigned short, true> : dz_kernel<unsigned short, false>,
+                        static_cast<unsigned short *>(nullptr));
         else
-            rc = launch_pdl(dz_kernel<float>, grid, dim3(256), 0, st, static_cast<const float *>(dy), lddy,
-                            static_cast<const float *>(pre), ldp, N, Ct, act, s.dz, bf16 ? 1 : 3, pz,
-                            (long long)N * pz, part, p.slab, vec);
+            rc = launch(vec ? dz_kernel<float, true> : dz_kernel<float, false>, static_cast<float *>(nullptr));
         if (rc != QCNN_OK) return rc;
         if (dbias && p.slabs > 1 && (rc = launch_column_join(s.db, p.slabs, Ct, Ct, nullptr, dbias, st)) != QCNN_OK)
             return rc;

@@ -295,6 +295,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     const bool gen = plan.planes == GEMM_F32;
     const int P = gen ? 3 : plan.planes, cg = plan.cg, bnc = plan.bn / cg;
     GemmArgs g = {};
+    g.stay = 1;
     unsigned a_bytes = 0, b_bytes = 0;
     for (int i = 0; i < count; ++i) {
         const GemmProblem &s = ps[i];
@@ -333,6 +334,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
         p.tiles = (int)tiles;
         p.units = p.tiles * p.splits;
         g.units += p.units;
+        if (p.kb_per_split * block_k(gen) > 128) g.stay = 0;
     }
     g.count = count;
     g.bn = plan.bn;

@@ -67,6 +67,7 @@ struct ProblemArgs {
 struct GemmArgs {
     ProblemArgs p[2];
     int count, units, bn, S;
+    int stay;               // three planes: a tile's sum stays in TMEM
     unsigned stage, b_off;  // bytes of a stage, of A's part of it
 };
 
@@ -279,8 +280,10 @@ __device__ __forceinline__ unsigned exchange(unsigned w, bool odd) {
 }
 
 // 16 columns of a lane to out[n0 + i][m], row by row: the warp's lanes are neighbours.
-// m_end, left: rows m and columns that exist (of planes, a row more may be written).  The
-// whole warp calls it.
+// m_end, left: rows m and columns that exist (of planes, a row more may be written).  FULL:
+// all 16 and all 32 do, and nothing is asked per element (in three planes with an addend,
+// the questions were most of 6,300 clocks per 16 columns).  The whole warp calls it.
+template <bool FULL>
 __device__ __forceinline__ void store_plane(unsigned short *out, long long ld, bool pair, int m_end, int m, int n0,
                                             int left, const unsigned (&w)[8]) {
     const bool odd = m & 1;
@@ -291,17 +294,18 @@ __device__ __forceinline__ void store_plane(unsigned short *out, long long ld, b
 #pragma unroll
         for (int i = 0; i < 8; ++i, p += 2 * ld) {
             const unsigned x = exchange(w[i], odd);
-            if (in && 2 * i < left) *reinterpret_cast<unsigned *>(p) = x;
+            if (FULL || (in && 2 * i < left)) *reinterpret_cast<unsigned *>(p) = x;
         }
     } else {
         unsigned short *p = out + (long long)n0 * ld + m;
 #pragma unroll
         for (int i = 0; i < 8; ++i, p += 2 * ld) {
-            if (in && 2 * i < left) p[0] = (unsigned short)w[i];
-            if (in && 2 * i + 1 < left) p[ld] = (unsigned short)(w[i] >> 16);
+            if (FULL || (in && 2 * i < left)) p[0] = (unsigned short)w[i];
+            if (FULL || (in && 2 * i + 1 < left)) p[ld] = (unsigned short)(w[i] >> 16);
         }
     }
 }
+template <bool FULL>
 __device__ __forceinline__ void store16(void *out, int type, long long ld, long long plane, bool pair, int m_end,
                                         int m, int n0, int left, const float (&v)[16]) {
     if (type == GEMM_T_F32) {
@@ -309,7 +313,7 @@ __device__ __forceinline__ void store16(void *out, int type, long long ld, long 
         float *p = static_cast<float *>(out) + (long long)n0 * ld + m;
 #pragma unroll
         for (int i = 0; i < 16; ++i, p += ld)
-            if (in && i < left) *p = v[i];
+            if (FULL || (in && i < left)) *p = v[i];
         return;
     }
     unsigned short *p = static_cast<unsigned short *>(out);
@@ -320,14 +324,14 @@ __device__ __forceinline__ void store16(void *out, int type, long long ld, long 
     } else if (type == GEMM_T_PLANES2) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) planes2(v[2 * i], v[2 * i + 1], w0[i], w1[i]);
-        store_plane(p + plane, ld, pair, m_end, m, n0, left, w1);
+        store_plane<FULL>(p + plane, ld, pair, m_end, m, n0, left, w1);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
-        store_plane(p + plane, ld, pair, m_end, m, n0, left, w1);
-        store_plane(p + 2 * plane, ld, pair, m_end, m, n0, left, w2);
+        store_plane<FULL>(p + plane, ld, pair, m_end, m, n0, left, w1);
+        store_plane<FULL>(p + 2 * plane, ld, pair, m_end, m, n0, left, w2);
     }
-    store_plane(p, ld, pair, m_end, m, n0, left, w0);
+    store_plane<FULL>(p, ld, pair, m_end, m, n0, left, w0);
 }
 
 // 16 columns of a lane of a matrix, on their way: loaded by fetch, values by take (a chunk
@@ -336,7 +340,7 @@ __device__ __forceinline__ void store16(void *out, int type, long long ld, long 
 struct Chunk16 {
     unsigned w[24];
 };
-template <int J>
+template <int J, bool FULL>
 __device__ __forceinline__ void fetch_pairs(Chunk16 &c, const unsigned short *src, long long ld, int m_end, int m,
                                             int n0, int left) {
     const bool odd = m & 1, in = m - odd < m_end;
@@ -344,10 +348,11 @@ __device__ __forceinline__ void fetch_pairs(Chunk16 &c, const unsigned short *sr
     if (odd) --left;
 #pragma unroll
     for (int i = 0; i < 8; ++i, p += 2 * ld) {
-        c.w[8 * J + i] = 0;
-        if (in && 2 * i < left) c.w[8 * J + i] = *reinterpret_cast<const unsigned *>(p);
+        if (!FULL) c.w[8 * J + i] = 0;
+        if (FULL || (in && 2 * i < left)) c.w[8 * J + i] = *reinterpret_cast<const unsigned *>(p);
     }
 }
+template <bool FULL>
 __device__ __forceinline__ void fetch16(Chunk16 &c, const void *src, int type, long long ld, long long plane,
                                         bool pair, int m_end, int m, int n0, int left) {
     const bool in = m < m_end;
@@ -356,20 +361,20 @@ __device__ __forceinline__ void fetch16(Chunk16 &c, const void *src, int type, l
         const float *f = static_cast<const float *>(src) + (long long)n0 * ld + m;
 #pragma unroll
         for (int i = 0; i < 16; ++i, f += ld) {
-            c.w[i] = 0;
-            if (in && i < left) c.w[i] = __float_as_uint(*f);
+            if (!FULL) c.w[i] = 0;
+            if (FULL || (in && i < left)) c.w[i] = __float_as_uint(*f);
         }
     } else if (!pair) {
         p += (long long)n0 * ld + m;
 #pragma unroll
         for (int i = 0; i < 16; ++i, p += ld) {
-            c.w[i] = 0;
-            if (in && i < left) c.w[i] = *p;
+            if (!FULL) c.w[i] = 0;
+            if (FULL || (in && i < left)) c.w[i] = *p;
         }
     } else {
-        fetch_pairs<0>(c, p, ld, m_end, m, n0, left);
-        if (type >= GEMM_T_PLANES2) fetch_pairs<1>(c, p + plane, ld, m_end, m, n0, left);
-        if (type == GEMM_T_PLANES3) fetch_pairs<2>(c, p + 2 * plane, ld, m_end, m, n0, left);
+        fetch_pairs<0, FULL>(c, p, ld, m_end, m, n0, left);
+        if (type >= GEMM_T_PLANES2) fetch_pairs<1, FULL>(c, p + plane, ld, m_end, m, n0, left);
+        if (type == GEMM_T_PLANES3) fetch_pairs<2, FULL>(c, p + 2 * plane, ld, m_end, m, n0, left);
     }
 }
 // v += scale * what was fetched.
@@ -418,19 +423,19 @@ __device__ __forceinline__ void act16(float (&v)[16], int act) {
 // OUT and SYM: sums v of lane m, columns n0 .. n0 + left - 1; c: what add has there, which
 // next() then fetches for the columns that follow.  The whole warp calls it; rows m up to
 // m_end exist.
-template <int KIND, typename F>
+template <int KIND, bool FULL, typename F>
 __device__ __forceinline__ void finish_out(const GemmEpi &e, int m_end, int m, int n0, int left, float alpha,
                                            float bias, float (&v)[16], const Chunk16 &c, F &&next) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = fmaf(alpha, v[i], bias);
-    if (KIND == GEMM_OUT && e.pre) store16(e.pre, e.out_type, e.ldp, 0, e.pair & 2, m_end, m, n0, left, v);
+    if (KIND == GEMM_OUT && e.pre) store16<FULL>(e.pre, e.out_type, e.ldp, 0, e.pair & 2, m_end, m, n0, left, v);
     if constexpr (KIND == GEMM_OUT) act16(v, e.act);
     if (e.add) {
         take16(c, e.add_type, e.pair & 4, m & 1, e.beta, v);
         next();
     }
     if constexpr (KIND == GEMM_OUT) {
-        store16(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
+        store16<FULL>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
     } else {
         // one value for both places: this tile's where m >= n.  (Above the diagonal inside a
         // tile: the other place's are stored, by the lanes whose row is the column here.)
@@ -517,7 +522,7 @@ __device__ __forceinline__ void stats16(RunningSum &s, int n0, int target, float
 }
 
 // Gradient of a class (lane m) for 16 rows; rows: theirs, without a class past the last.
-__device__ __forceinline__ void dlogits16(const GemmEpi &e, int m_end, int m, int n0, int left, float bias,
+__device__ __forceinline__ void dlogits16(const GemmEpi &e, bool full, int m_end, int m, int n0, int left, float bias,
                                           const float4 *rows, float &col, float (&v)[16]) {
     const int c = e.class0 + m;
 #pragma unroll
@@ -530,7 +535,8 @@ __device__ __forceinline__ void dlogits16(const GemmEpi &e, int m_end, int m, in
         v[i] = target >= 0 ? r.y * p : 0.f;
         col += v[i];
     }
-    store16(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
+    if (full) store16<true>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
+    else store16<false>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
 }
 
 // ---------------------------------------------------------------------- GEN
@@ -572,8 +578,9 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
     constexpr int BK = GEN ? 32 : 64, KS = BK / 16;
     constexpr int PL = GEN ? 1 : P;  // stages (planes) of a block of terms
     constexpr bool DRAIN = P == 3;   // a block's sum at a time
-    // Rings of stages, blocks in turn, and as many warps that issue MMAs, each with a ring
-    // and an accumulator of its own.  (A warp's waits come back behind the MMAs that it has
+    // Rings of stages, and as many warps that issue MMAs, each with a ring and an accumulator of
+    // its own, which take the accumulators in turn: a block's each, or (g.stay: sums of up to
+    // 128 terms, whose additions in TMEM lose less than 2^-21) a tile's.  (A warp's waits come back behind the MMAs that it has
     // issued: one alone left the tensor core idle between accumulators, 1,204 clocks per block
     // of 888.  And a ring has one consumer: a wait for a phase two ahead passes at once.)
     constexpr int RINGS = DRAIN ? 2 : 1;
@@ -665,7 +672,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                             par ^= 1;
                         }
                     }
-                    if constexpr (RINGS == 2) {
+                    if (RINGS == 2 && (!g.stay || kb + 1 == t.kb1)) {
                         ring ^= 1;
                         swap(slot, slot2);
                         swap(par, par2);
@@ -690,7 +697,8 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             const int S = g.S / RINGS;
             int slot = 0;
             unsigned par = 0;
-            unsigned use = 0, block = 0;  // accumulators, blocks so far
+            unsigned use = 0;  // accumulators so far
+            const bool drain = DRAIN && !g.stay;
             bool ok = true;
             const unsigned stage = g.stage >> 4;
             const uint64_t base = (uint64_t)((smem_addr(smem) >> 4) & 0x3FFFu) + ring * S * stage;
@@ -702,12 +710,12 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 [[maybe_unused]] const unsigned pb = p.b.plane;
                 const uint32_t idesc = p.idesc;
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (RINGS == 2 && (block++ & 1) != ring) continue;  // the other warp's
-                    const bool fresh = DRAIN || kb == t.kb0;
-                    const unsigned buf = RINGS == 2 ? ring : use & 1;
+                    const bool fresh = drain || kb == t.kb0, last = drain || kb + 1 == t.kb1;
+                    const unsigned buf = use & 1, round = use >> 1;
+                    if (last) ++use;
+                    if (RINGS == 2 && buf != ring) continue;  // the other warp's
                     if (fresh) {
-                        const unsigned n = RINGS == 2 ? use : use >> 1;  // of this accumulator
-                        if (!(ok = wait_one(sh, &sh.tempty[buf], (n & 1) ^ 1))) break;
+                        if (!(ok = wait_one(sh, &sh.tempty[buf], (round & 1) ^ 1))) break;
                     }
                     // the stages of this block's planes, the last plane first
                     int at[PL];
@@ -748,10 +756,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     }
                     product(0, 0);
                     commit<CG>(&sh.empty[ring * S + at[0]]);
-                    if (DRAIN || kb + 1 == t.kb1) {
-                        commit<CG>(&sh.tfull[buf]);
-                        ++use;
-                    }
+                    if (last) commit<CG>(&sh.tfull[buf]);
                 }
             }
             // nothing in flight when the tensor memory is freed
@@ -781,6 +786,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             const GemmEpi &e = p.e;
             const int m = (t.mt * CG + (int)rank) * kMT + quarter * 32 + lane, n0 = t.nt * g.bn;
             const bool in = m < p.m;
+            [[maybe_unused]] const bool rows_full = m - lane + 32 <= p.m;  // of the whole warp
             [[maybe_unused]] float bias = 0.f, col = 0.f;
             [[maybe_unused]] const float alpha = KIND == GEMM_OUT && e.alpha_ptr ? *e.alpha_ptr : e.alpha;
             [[maybe_unused]] RunningSum run;
@@ -796,7 +802,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             }
             // the sums of the tile, in TMEM at tl + buf * ACC
             unsigned buf = use & 1;
-            const bool drain = DRAIN && t.kb1 - t.kb0 > 1;
+            const bool drain = DRAIN && !g.stay;
             if (drain) {
                 constexpr int CH = GEN ? 4 : 8;  // chunks of a warp at most
                 float acc[CH][16];
@@ -844,8 +850,14 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 }
                 if constexpr (KIND == GEMM_OUT || KIND == GEMM_SYM) {
                     const int left = p.n - (n0 + c * 16);
-                    if (adds && c < chunks && left > 0)
-                        fetch16(add, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0 + c * 16, left);
+                    if (adds && c < chunks && left > 0) {
+                        if (rows_full && left >= 16)
+                            fetch16<true>(add, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0 + c * 16,
+                                          left);
+                        else
+                            fetch16<false>(add, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m,
+                                           n0 + c * 16, left);
+                    }
                 }
             };
             fetch(half);
@@ -867,13 +879,16 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 if constexpr (KIND == GEMM_STATS) {
                     stats16(run, n, target, e.target_logit + m, cols, v);
                 } else if constexpr (KIND == GEMM_DLOGITS) {
-                    dlogits16(e, p.m, m, n, left, bias, cols, col, v);
+                    dlogits16(e, rows_full && left >= 16, p.m, m, n, left, bias, cols, col, v);
                 } else if (left > 0) {
+                    const bool full = rows_full && left >= 16;
                     if (e.partial)
-                        store16(e.partial + (long long)t.split * p.n * p.m, GEMM_T_F32, p.m, 0, false, p.m, m, n,
-                                left, v);
+                        store16<false>(e.partial + (long long)t.split * p.n * p.m, GEMM_T_F32, p.m, 0, false, p.m, m,
+                                       n, left, v);
+                    else if (full)
+                        finish_out<KIND, true>(e, p.m, m, n, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                     else
-                        finish_out<KIND>(e, p.m, m, n, left, alpha, bias, v, add, [&] { fetch(c + 2); });
+                        finish_out<KIND, false>(e, p.m, m, n, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                 }
             }
             release(buf);
@@ -989,9 +1004,11 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     slot = 0;
                     par ^= 1;
                 }
-                ring ^= 1;
-                swap(slot, slot2);
-                swap(par, par2);
+                if (!g.stay || kb + 1 == t.kb1) {
+                    ring ^= 1;
+                    swap(slot, slot2);
+                    swap(par, par2);
+                }
                 if (++rslot == kRawSlots) rslot = 0;
             }
         }
