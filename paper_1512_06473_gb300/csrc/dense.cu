@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 namespace qcnn {
 namespace {
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(256) few_rows_kernel(FewRows f, int kw) {
     const int step = kw * 32 * V;
     // (VEC: Cs is a multiple of V)
     if constexpr (VEC) {
-#pragma unroll 2
+#pragma unroll(NB <= 2 ? 4 : 2)
         for (int k = (part * 32 + lane) * V; k < f.Cs; k += step) {
             float wv[kFewOut][V];
 #pragma unroll
@@ -479,28 +480,36 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
         if (rc != QCNN_OK) return rc;
         wo = GemmOperand{s.w, pc, Ct * pc, 1};
     }
-    GemmProblem g;
-    g.e.out_type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
-    g.m = Cs;
-    if (dx) {
-        g.a = wo;
-        g.b = z;
-        g.n = N;
-        g.k = Ct;
-        g.e.out = dx;
-        g.e.ldo = lddx;
-        if ((rc = p.gx.run(g, s.partial, st)) != QCNN_OK) return rc;
+    GemmProblem g[2];
+    const int type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
+    GemmProblem &x_ = g[0], &w_ = g[1];
+    x_.a = wo;
+    x_.b = z;
+    x_.m = Cs;
+    x_.n = N;
+    x_.k = Ct;
+    x_.e.out = dx;
+    x_.e.ldo = lddx;
+    x_.e.out_type = type;
+    w_.a = xo;
+    w_.b = z;
+    w_.b.mn = 1;
+    w_.m = Cs;
+    w_.n = Ct;
+    w_.k = N;
+    w_.e.out = dW;
+    w_.e.ldo = lddw;
+    w_.e.out_type = type;
+    if (dx && dW) {  // one launch, the longer tiles first, where that fills the SMs better
+        const bool x_first = Ct >= N;
+        const GemmPlan &px = p.gx.plan, &pw = p.gw.plan;
+        if (x_first ? gemm_together(px, Cs, N, Ct, pw, Cs, Ct, N) : gemm_together(pw, Cs, Ct, N, px, Cs, N, Ct)) {
+            if (!x_first) std::swap(x_, w_);
+            return launch_gemm(px, g, 2, st);
+        }
     }
-    if (dW) {
-        g.a = xo;
-        g.b = z;
-        g.b.mn = 1;
-        g.n = Ct;
-        g.k = N;
-        g.e.out = dW;
-        g.e.ldo = lddw;
-        if ((rc = p.gw.run(g, s.partial, st)) != QCNN_OK) return rc;
-    }
+    if (dx && (rc = p.gx.run(x_, s.partial, st)) != QCNN_OK) return rc;
+    if (dW && (rc = p.gw.run(w_, s.partial, st)) != QCNN_OK) return rc;
     return QCNN_OK;
 }
 

@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(GemmEpi e, int m_all, in
         }
         v = act_apply(v, e.act);
         if (e.add) v = fmaf(e.beta, load_as(e.add, e.add_type, (long long)n * e.lda + m, e.add_plane), v);
+        if (n == m) v += e.diagonal;
         if (e.out_type == GEMM_T_F32) {
             static_cast<float *>(e.out)[o] = v;
         } else {
@@ -154,6 +155,7 @@ __global__ void __launch_bounds__(256) gemm_join_sym_kernel(GemmEpi e, int m_all
         if (m < m_all && n <= m) {
             v = e.alpha * add_groups<true>(e.partial + (size_t)n * m_all + m, splits, stride);
             if (e.add) v = fmaf(e.beta, load_as(e.add, e.add_type, (long long)n * e.lda + m, e.add_plane), v);
+            if (n == m) v += e.diagonal;
             put(v, n, m);
         }
         patch[y][x] = v;
@@ -289,6 +291,25 @@ GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_splits) {
     if (cache.size() >= 256) cache.clear();
     cache.emplace(key, p);
     return p;
+}
+
+bool gemm_together(const GemmPlan &a, int m_a, int n_a, int k_a, const GemmPlan &b, int m_b, int n_b, int k_b) {
+    if (a.planes != b.planes || a.kind != b.kind || a.cg != b.cg || a.bn != b.bn || a.splits > 1 || b.splits > 1)
+        return false;
+    const int slots = num_sms() / a.cg;
+    const long long ta = (long long)cdiv(m_a, kMT * a.cg) * cdiv(n_a, a.bn),
+                    tb = (long long)cdiv(m_b, kMT * a.cg) * cdiv(n_b, a.bn);
+    const long long ka = k_a + 128, kb = k_b + 128;  // (with a tile's own costs, in terms)
+    const long long apart = cdiv((int)std::min<long long>(ta, 1 << 30), slots) * ka +
+                            cdiv((int)std::min<long long>(tb, 1 << 30), slots) * kb;
+    // the longest of the slots: slot i has tiles i, i + slots, ... of a's and then b's
+    long long most = 0;
+    for (int i = 0; i < slots; ++i) {
+        const long long of_a = ta > i ? (ta - i + slots - 1) / slots : 0;
+        const long long all = ta + tb > i ? (ta + tb - i + slots - 1) / slots : 0;
+        most = std::max(most, of_a * ka + (all - of_a) * kb);
+    }
+    return most < apart;
 }
 
 qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, cudaStream_t st) {

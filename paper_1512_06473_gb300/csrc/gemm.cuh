@@ -27,7 +27,7 @@ struct GemmOperand {
 enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1, GEMM_T_PLANES2 = 2, GEMM_T_PLANES3 = 3 };
 
 // What becomes of a sum.  OUT: v = alpha * sum + bias[m] (alpha: *alpha_ptr where set); pre = v; v = act(v);
-// v += beta * add[n][m]; out[n][m] = v.  With partial set: the sums of this split
+// v += beta * add[n][m]; v += diagonal where n == m; out[n][m] = v.  With partial set: the sums of this split
 // alone, fp32 [split][n][m], for launch_gemm_join (a CTA that adds up all splits of its tile
 // because it is the last of them reads 1 MB alone: 54 us instead of 33 for 128 rows of 4096 ->
 // 1000).  SYM: the product is symmetric
@@ -36,7 +36,7 @@ enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1, GEMM_T_PLANES2 = 2, GEMM_T_PLAN
 // of v = sum + bias[n], and the value at the row's target.  DLOGITS: m are classes,
 // n rows: out = g_n (exp(v - lse_n) - [target_n == m]).
 struct GemmEpi {
-    float alpha = 1.f, beta = 0.f;
+    float alpha = 1.f, beta = 0.f, diagonal = 0.f;
     const float *alpha_ptr = nullptr;  // in device memory
     const float *bias = nullptr;
     void *out = nullptr;
@@ -83,6 +83,10 @@ struct GemmPlan {
 // max_splits 1: the sums must end in one tile (epilogues that launch_gemm_join does
 // not have)
 GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_splits);
+
+// Whether two products of one tile shape and kind, a's first, are sooner done in one launch than
+// in two (their tiles are dealt out in turn).
+bool gemm_together(const GemmPlan &a, int m_a, int n_a, int k_a, const GemmPlan &b, int m_b, int n_b, int k_b);
 
 // One launch of one or two products of the same kind and planes (the second fills
 // the SMs that the first one's last tiles leave idle); both with `plan`'s tile, each

@@ -434,6 +434,11 @@ __device__ __forceinline__ void finish_out(const GemmEpi &e, int m_end, int m, i
         take16(c, e.add_type, e.pair & 4, m & 1, e.beta, v);
         next();
     }
+    if (e.diagonal != 0.f && (unsigned)(m - n0) < 16u) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (m == n0 + i) v[i] += e.diagonal;
+    }
     if constexpr (KIND == GEMM_OUT) {
         store16<FULL>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
     } else {

@@ -1,11 +1,12 @@
 // orthogonalize.cu -- qcnn_orthogonalize: Newton-Schulz products.
 //
-//   X = G / (||G||_F + eps); steps times: A = X X^T, B = b A + c A A, X = a X + B X
+//   X = G / (||G||_F + eps); steps times: A = X X^T, B = a I + b A + c A A, X = B X
 //
 // of the smaller side p (q the larger; G with more rows than columns from the right, by
 // reading X with its rows contiguous: nothing is transposed).  Three products a step, of
 // 2 p^2 q, 2 p^3 and 2 p^2 q operations; A and B are symmetric, so of the first two the
-// tiles on one side of the diagonal are computed and stored twice.  X, A and B live as bf16
+// tiles on one side of the diagonal are computed and stored twice.  (a X + (B - a I) X
+// instead of B X read X again in the third product's epilogue, 12 us a step of 1000 x 4096.)  X, A and B live as bf16
 // planes that the epilogues write and TMA reads: two in bf16 calls (in one, each step's
 // rounding of X and B would be that of the result), three in fp32 calls.
 #include "train.cuh"
@@ -241,6 +242,7 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
         g.e.lda = pa;
         g.e.add_plane = aplane;
         g.e.add_type = type;
+        g.e.diagonal = k[0];
         g.e.out = s.b;
         if ((rc = o.poly.run(g, s.partial, st)) != QCNN_OK) break;
         GemmProblem u;
@@ -257,11 +259,6 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
             u.a = b;
             u.b = x;
         }
-        u.e.beta = k[0];
-        u.e.add = s.x[i & 1];
-        u.e.lda = px;
-        u.e.add_plane = xplane;
-        u.e.add_type = type;
         if (i + 1 < steps) {
             u.e.out = s.x[i + 1 & 1];
             u.e.ldo = px;

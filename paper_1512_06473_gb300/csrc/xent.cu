@@ -30,17 +30,17 @@ __device__ __forceinline__ int class_of(const int64_t *targets, int n, int Ct) {
     return t >= 0 && t < Ct ? (int)t : -1;
 }
 
-// 1 / (rows with a class), by one CTA of 256 threads.
+// 1 / (rows with a class), by one CTA.
 __device__ void count_rows(const int64_t *targets, int N, int Ct, float *inv) {
-    __shared__ int part[8];
+    __shared__ int part[32];
     int c = 0;
-    for (int n = threadIdx.x; n < N; n += 256) c += (unsigned long long)targets[n] < (unsigned long long)Ct;
+    for (int n = threadIdx.x; n < N; n += blockDim.x) c += (unsigned long long)targets[n] < (unsigned long long)Ct;
 #pragma unroll
     for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = c;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) c += part[i];
+        for (int i = 1; i < (int)blockDim.x / 32; ++i) c += part[i];
         *inv = c ? 1.f / (float)c : 0.f;
     }
 }
@@ -71,33 +71,48 @@ __device__ __forceinline__ void finish_row(const RowOut &o, int n, float top, fl
     if (o.rows) o.rows[n] = make_float4(lse, o.dloss ? o.dloss[n] : 1.f, __int_as_float(t), 0.f);
 }
 
-// Small: a CTA per row of logits; one more counts the rows.
-__global__ void __launch_bounds__(256) rows_kernel(const float *logits, RowOut o) {
+// Small: a CTA per row of logits; one more counts the rows.  splits > 1: the logits come as
+// that many partial sums [split][N][Ct] without bias, are added up here and (where there is
+// a gradient) left in `logits`.
+__global__ void __launch_bounds__(1024) rows_kernel(const float *part, int splits, const float *bias,
+                                                    float *logits, RowOut o) {
     grid_dep_sync();
     if ((int)blockIdx.x == o.N) {
         count_rows(o.targets, o.N, o.Ct, o.inv);
         return;
     }
-    __shared__ float tops[8], sums[8];
-    const float *l = logits + (size_t)blockIdx.x * o.Ct;
+    __shared__ float tops[32], sums[32], picked;
+    const int t = class_of(o.targets, blockIdx.x, o.Ct), T = blockDim.x;
+    const size_t row = (size_t)blockIdx.x * o.Ct, stride = (size_t)o.N * o.Ct;
+    if (threadIdx.x == 0) picked = 0.f;
+    __syncthreads();
     float top = -INFINITY, sum = 0.f;
-    for (int c0 = threadIdx.x; c0 < o.Ct; c0 += 256 * 8) {
-        float v[8], t = top;
+    for (int c0 = threadIdx.x; c0 < o.Ct; c0 += T * 4) {
+        float v[4], m = top;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = c0 + i * 256 < o.Ct ? l[c0 + i * 256] : -INFINITY;
-            t = fmaxf(t, v[i]);
+        for (int i = 0; i < 4; ++i) {
+            const int c = c0 + i * T;
+            v[i] = -INFINITY;
+            if (c >= o.Ct) continue;
+            if (splits > 1) {
+                v[i] = add_groups<true>(part + row + c, splits, stride) + (bias ? bias[c] : 0.f);
+                if (o.rows) logits[row + c] = v[i];
+            } else {
+                v[i] = logits[row + c];
+            }
+            if (c == t) picked = v[i];
+            m = fmaxf(m, v[i]);
         }
-        if (t == -INFINITY) {  // nothing to add (or NaN)
+        if (m == -INFINITY) {  // nothing to add (or NaN)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 4; ++i)
                 if (v[i] != v[i]) sum = v[i];
             continue;
         }
-        sum = top == -INFINITY ? sum : sum * expf(top - t);
+        sum = top == -INFINITY ? sum : sum * expf(top - m);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += expf(v[i] - t);
-        top = t;
+        for (int i = 0; i < 4; ++i) sum += expf(v[i] - m);
+        top = m;
     }
 #pragma unroll
     for (int s = 16; s; s >>= 1)
@@ -108,36 +123,35 @@ __global__ void __launch_bounds__(256) rows_kernel(const float *logits, RowOut o
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) join(top, sum, tops[i], sums[i]);
-        const int t = class_of(o.targets, blockIdx.x, o.Ct);
-        finish_row(o, blockIdx.x, top, sum, t >= 0 ? l[t] : 0.f);
+        for (int i = 1; i < T / 32; ++i) join(top, sum, tops[i], sums[i]);
+        finish_row(o, blockIdx.x, top, sum, picked);
     }
 }
 
-// Large: the tiles' maxima and sums of 32 rows per CTA; eight warps take the tiles in turn.
-__global__ void __launch_bounds__(256) stats_join_kernel(const float2 *stats, int parts,
+// Large: the tiles' maxima and sums of 32 rows per CTA; 32 warps take the tiles in turn.
+__global__ void __launch_bounds__(1024) stats_join_kernel(const float2 *stats, int parts,
                                                          const float *target_logit, RowOut o) {
     grid_dep_sync();
     if ((int)blockIdx.x * 32 >= o.N) {
         count_rows(o.targets, o.N, o.Ct, o.inv);
         return;
     }
-    __shared__ float2 red[8][32];
+    __shared__ float2 red[32][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockIdx.x * 32 + lane;
     float top = -INFINITY, sum = 0.f;
     if (n < o.N)
-        for (int p = warp; p < parts; p += 32) {
+        for (int p = warp; p < parts; p += 128) {
             float2 v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                v[i] = p + 8 * i < parts ? stats[(size_t)(p + 8 * i) * o.N + n] : make_float2(-INFINITY, 0.f);
+                v[i] = p + 32 * i < parts ? stats[(size_t)(p + 32 * i) * o.N + n] : make_float2(-INFINITY, 0.f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) join(top, sum, v[i].x, v[i].y);
         }
     red[warp][lane] = make_float2(top, sum);
     __syncthreads();
     if (warp == 0 && n < o.N) {
-        for (int i = 1; i < 8; ++i) join(top, sum, red[i][lane].x, red[i][lane].y);
+        for (int i = 1; i < 32; ++i) join(top, sum, red[i][lane].x, red[i][lane].y);
         finish_row(o, n, top, sum, target_logit[n]);
     }
 }
@@ -335,10 +349,14 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
             g.m = Ct;
             g.n = N;
             g.k = Cs;
-            rc = p.logits.run(g, s.partial, st);
+            g.e.partial = static_cast<float *>(s.partial);
+            rc = launch_gemm(p.logits.plan, &g, 1, st);
         }
         if (rc != QCNN_OK) return rc;
-        rc = launch_pdl(rows_kernel, dim3(N + (a.grad ? 1 : 0)), dim3(256), 0, st, s.logits, ro);
+        // (a split product's sums are joined by the pass over its rows)
+        rc = launch_pdl(rows_kernel, dim3(N + (a.grad ? 1 : 0)),
+                        dim3(std::min(1024, std::max(128, cdiv(Ct, 128) * 128))), 0, st,
+                        static_cast<const float *>(s.partial), p.few ? 1 : p.logits.plan.splits, a.bias, s.logits, ro);
     } else {
         g.a = xo;
         g.b = wo;
@@ -350,7 +368,7 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         g.e.targets = reinterpret_cast<const long long *>(a.targets);
         g.e.target_logit = s.target_logit;
         if ((rc = launch_gemm(p.stats.plan, &g, 1, st)) != QCNN_OK) return rc;
-        rc = launch_pdl(stats_join_kernel, dim3(cdiv(N, 32) + (a.grad ? 1 : 0)), dim3(256), 0, st, s.stats,
+        rc = launch_pdl(stats_join_kernel, dim3(cdiv(N, 32) + (a.grad ? 1 : 0)), dim3(1024), 0, st, s.stats,
                         p.stats.plan.n_tiles * 2, s.target_logit, ro);
     }
     if (rc != QCNN_OK || !a.grad) return rc;
