@@ -239,27 +239,26 @@ int dz_slab(int N, int Ct) {
 // TMA cannot read.
 struct ForwardPlan {
     bool few = false, wplanes = false;
-    Product g;
+    GemmPlan g;
 };
 ForwardPlan plan_forward(int N, int Cs, int Ct, int dtype) {
     ForwardPlan p;
     if (N <= kFewRows) {
         p.few = true;
     } else if (dtype == QCNN_BF16) {
-        p.g.plan = plan_gemm(1, GEMM_OUT, Ct, N, Cs, 64);
+        p.g = plan_gemm(1, GEMM_OUT, Ct, N, Cs);
     } else {
-        p.g.plan = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, 64);
-        const GemmPlan q = plan_gemm(3, GEMM_OUT, Ct, N, Cs, 64);
-        if (q.score + pass_clocks((double)Ct * Cs * 10.0) < p.g.plan.score) {
+        p.g = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs);
+        const GemmPlan q = plan_gemm(3, GEMM_OUT, Ct, N, Cs);
+        if (q.score + pass_clocks((double)Ct * Cs * 10.0) < p.g.score) {
             p.wplanes = true;
-            p.g.plan = q;
+            p.g = q;
         }
     }
     return p;
 }
 struct ForwardSpace {
     unsigned short *x = nullptr, *w = nullptr;
-    void *partial = nullptr;
     size_t bytes = 0;
 };
 ForwardSpace carve_forward(const ForwardPlan &p, int N, int Cs, int Ct, int dtype, bool xa, bool wa, void *ws) {
@@ -271,7 +270,6 @@ ForwardSpace carve_forward(const ForwardPlan &p, int N, int Cs, int Ct, int dtyp
     const bool x_copy = !bf16 || !xa;
     if (x_copy) s.x = c.array<unsigned short>((size_t)P * N * pad8(Cs));
     if (bf16 ? !wa : p.wplanes) s.w = c.array<unsigned short>((size_t)P * Ct * pad8(Cs));
-    s.partial = c.take(p.g.scratch());
     s.bytes = c.used;
     return s;
 }
@@ -279,21 +277,21 @@ ForwardSpace carve_forward(const ForwardPlan &p, int N, int Cs, int Ct, int dtyp
 struct BackwardPlan {
     bool wplanes = false;
     int slab = 0, slabs = 1;
-    Product gx, gw;
+    GemmPlan gx, gw;
 };
 BackwardPlan plan_backward(int N, int Cs, int Ct, int dtype) {
     BackwardPlan p;
     p.slab = dz_slab(N, Ct);
     p.slabs = cdiv(N, p.slab);
     const int P = dtype == QCNN_BF16 ? 1 : 3;
-    p.gw.plan = plan_gemm(P, GEMM_OUT, Cs, Ct, N, 64);
-    p.gx.plan = plan_gemm(P, GEMM_OUT, Cs, N, Ct, 64);
+    p.gw = plan_gemm(P, GEMM_OUT, Cs, Ct, N);
+    p.gx = plan_gemm(P, GEMM_OUT, Cs, N, Ct);
     p.wplanes = true;
     if (P == 3) {
-        const GemmPlan q = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
-        if (q.score <= p.gx.plan.score + pass_clocks((double)Ct * Cs * 10.0)) {
+        const GemmPlan q = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct);
+        if (q.score <= p.gx.score + pass_clocks((double)Ct * Cs * 10.0)) {
             p.wplanes = false;
-            p.gx.plan = q;
+            p.gx = q;
         }
     }
     return p;
@@ -302,7 +300,6 @@ struct BackwardSpace {
     void *dz = nullptr;
     unsigned short *x = nullptr, *w = nullptr;
     float *db = nullptr;
-    void *partial = nullptr;
     size_t bytes = 0;
 };
 BackwardSpace carve_backward(const BackwardPlan &p, int N, int Cs, int Ct, int dtype, bool dz, bool x_copy,
@@ -314,7 +311,6 @@ BackwardSpace carve_backward(const BackwardPlan &p, int N, int Cs, int Ct, int d
     if (x_copy) s.x = c.array<unsigned short>(P * N * pad8(Cs));
     if (w_copy) s.w = c.array<unsigned short>(P * Ct * pad8(Cs));
     if (p.slabs > 1) s.db = c.array<float>((size_t)p.slabs * Ct);
-    s.partial = c.take(std::max(p.gx.scratch(), p.gw.scratch()));
     s.bytes = c.used;
     return s;
 }
@@ -398,7 +394,7 @@ qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, cons
         if (rc != QCNN_OK) return rc;
         g.a = GemmOperand{s.w, pitch, Ct * pitch, 0};
     }
-    return p.g.run(g, s.partial, st);
+    return launch_gemm(p.g, &g, 1, st);
 }
 
 qcnn_status qcnn_dense_backward_workspace_size(int N, int Cs, int Ct, int dtype, int aligned,
@@ -502,14 +498,14 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
     w_.e.out_type = type;
     if (dx && dW) {  // one launch, the longer tiles first, where that fills the SMs better
         const bool x_first = Ct >= N;
-        const GemmPlan &px = p.gx.plan, &pw = p.gw.plan;
+        const GemmPlan &px = p.gx, &pw = p.gw;
         if (x_first ? gemm_together(px, Cs, N, Ct, pw, Cs, Ct, N) : gemm_together(pw, Cs, Ct, N, px, Cs, N, Ct)) {
             if (!x_first) std::swap(x_, w_);
             return launch_gemm(px, g, 2, st);
         }
     }
-    if (dx && (rc = p.gx.run(x_, s.partial, st)) != QCNN_OK) return rc;
-    if (dW && (rc = p.gw.run(w_, s.partial, st)) != QCNN_OK) return rc;
+    if (dx && (rc = launch_gemm(p.gx, &x_, 1, st)) != QCNN_OK) return rc;
+    if (dW && (rc = launch_gemm(p.gw, &w_, 1, st)) != QCNN_OK) return rc;
     return QCNN_OK;
 }
 

@@ -1,5 +1,5 @@
-// gemm.cu -- plans and launches of the tensor-core products (gemm.cuh), the join of
-// split ones, and the pass that lays fp32 or unaligned data out as planes.
+// gemm.cu -- plans and launches of the tensor-core products (gemm.cuh), and the pass that lays
+// fp32 or unaligned data out as planes.
 #include "gemm_kernel.cuh"
 
 #include <algorithm>
@@ -12,9 +12,9 @@ namespace qcnn {
 // (gemm_p1.cu, gemm_p2.cu, gemm_p3.cu, gemm_f32.cu)
 using GemmLaunch = qcnn_status (*)(const void *, int, size_t, cudaStream_t);
 GemmLaunch gemm_launch_p1(int kind, int cg);
-GemmLaunch gemm_launch_p2(int kind, int cg);
+const void *gemm_kernel_address();
 GemmLaunch gemm_launch_p3(int kind, int cg);
-GemmLaunch gemm_launch_p3_sym(int cg);
+GemmLaunch gemm_launch_planes(int planes, int kind, int cg);
 GemmLaunch gemm_launch_f32();
 
 namespace {
@@ -87,85 +87,10 @@ bool pairs(const void *p, int type, long long ld, long long plane, int m) {
 }
 
 GemmLaunch launcher(const GemmPlan &p) {
-    switch (p.planes) {
-        case 1: return gemm_launch_p1(p.kind, p.cg);
-        case 2: return gemm_launch_p2(p.kind, p.cg);
-        case 3: return p.kind == GEMM_SYM ? gemm_launch_p3_sym(p.cg) : gemm_launch_p3(p.kind, p.cg);
-        default: return gemm_launch_f32();
-    }
-}
-
-// ----------------------------------------------------------------- join
-// A thread per output; neighbours along m.
-__global__ void __launch_bounds__(256) gemm_join_kernel(GemmEpi e, int m_all, int n_all, int splits) {
-    grid_dep_sync();
-    const int m = blockIdx.x * 256 + threadIdx.x;
-    if (m >= m_all) return;
-    const float bias = e.bias ? e.bias[m] : 0.f, alpha = e.alpha_ptr ? *e.alpha_ptr : e.alpha;
-    const size_t stride = (size_t)m_all * n_all;
-    for (int n = blockIdx.y; n < n_all; n += gridDim.y) {
-        float v = add_groups<true>(e.partial + (size_t)n * m_all + m, splits, stride);
-        v = fmaf(alpha, v, bias);
-        const long long o = (long long)n * e.ldo + m;
-        if (e.pre) {
-            const long long q = (long long)n * e.ldp + m;
-            if (e.out_type == GEMM_T_F32) static_cast<float *>(e.pre)[q] = v;
-            else static_cast<unsigned short *>(e.pre)[q] = float_to_bf16(v);
-        }
-        v = act_apply(v, e.act);
-        if (e.add) v = fmaf(e.beta, load_as(e.add, e.add_type, (long long)n * e.lda + m, e.add_plane), v);
-        if (n == m) v += e.diagonal;
-        if (e.out_type == GEMM_T_F32) {
-            static_cast<float *>(e.out)[o] = v;
-        } else {
-            unsigned w[3] = {};
-            if (e.out_type == GEMM_T_BF16) w[0] = pack_bf16x2(v, 0.f);
-            else if (e.out_type == GEMM_T_PLANES2) planes2(v, 0.f, w[0], w[1]);
-            else planes3(v, 0.f, w[0], w[1], w[2]);
-            unsigned short *p = static_cast<unsigned short *>(e.out) + o;
-            p[0] = (unsigned short)w[0];
-            if (e.out_type >= GEMM_T_PLANES2) p[e.out_plane] = (unsigned short)w[1];
-            if (e.out_type == GEMM_T_PLANES3) p[2 * e.out_plane] = (unsigned short)w[2];
-        }
-    }
-}
-
-// The same of a symmetric product: only m >= n was summed.  A CTA has a 32 x 32 patch below
-// (or on) the diagonal, which goes to its mirror image through shared memory.
-__global__ void __launch_bounds__(256) gemm_join_sym_kernel(GemmEpi e, int m_all, int splits) {
-    grid_dep_sync();
-    __shared__ float patch[32][33];
-    const int bm = blockIdx.x, bn = blockIdx.y;
-    if (bn > bm) return;
-    const int x = threadIdx.x & 31, y0 = threadIdx.x >> 5, m = bm * 32 + x;
-    const size_t stride = (size_t)m_all * m_all;
-    auto put = [&](float v, int row, int col) {
-        unsigned w[3] = {};
-        if (e.out_type == GEMM_T_PLANES2) planes2(v, 0.f, w[0], w[1]);
-        else planes3(v, 0.f, w[0], w[1], w[2]);
-        unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)row * e.ldo + col;
-        p[0] = (unsigned short)w[0];
-        p[e.out_plane] = (unsigned short)w[1];
-        if (e.out_type == GEMM_T_PLANES3) p[2 * e.out_plane] = (unsigned short)w[2];
-    };
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int y = y0 + 8 * i, n = bn * 32 + y;
-        float v = 0.f;
-        if (m < m_all && n <= m) {
-            v = e.alpha * add_groups<true>(e.partial + (size_t)n * m_all + m, splits, stride);
-            if (e.add) v = fmaf(e.beta, load_as(e.add, e.add_type, (long long)n * e.lda + m, e.add_plane), v);
-            if (n == m) v += e.diagonal;
-            put(v, n, m);
-        }
-        patch[y][x] = v;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = bm * 32 + y0 + 8 * i, col = bn * 32 + x;
-        if (row < m_all && col < row) put(patch[x][y0 + 8 * i], row, col);
-    }
+    if (p.planes == GEMM_F32) return gemm_launch_f32();
+    if (p.planes == 2 || p.kind == GEMM_SYM || p.kind == GEMM_PLANES)
+        return gemm_launch_planes(p.planes, p.kind, p.cg);
+    return p.planes == 1 ? gemm_launch_p1(p.kind, p.cg) : gemm_launch_p3(p.kind, p.cg);
 }
 
 // --------------------------------------------------------------- planes
@@ -229,12 +154,13 @@ __global__ void __launch_bounds__(256) planes_kernel(const T *src, long long all
 
 }  // namespace
 
-static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int max_splits, int sms) {
+static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int max_groups, int sms) {
     GemmPlan best;
     const bool gen = planes == GEMM_F32;
     const int P = gen ? 3 : planes, bk = block_k(gen), kblocks = std::max(1, cdiv(k, bk));
-    static const int tiles[6] = {16, 32, 64, 128, 192, 256};
+    static const int tiles[5] = {16, 32, 64, 128, 256};
     const int mmas = (P == 1 ? 1 : P == 2 ? 3 : 6) * bk / 16;
+    const bool whole = kind == GEMM_STATS || kind == GEMM_DLOGITS;  // (no shares)
     for (int cg = 1; cg <= (gen ? 1 : 2); ++cg) {
         for (int bn : tiles) {
             if (gen && bn > 128) continue;
@@ -242,51 +168,74 @@ static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int ma
             if (planes == 3 && cg == 1 && bn > 128) continue;  // (stages: launch_gemm)
             if (kind == GEMM_SYM && bn % (kMT * cg)) continue;
             if (bn > 16 && kind != GEMM_SYM && bn >= 2 * n) continue;
-            const int mt = cdiv(m, kMT * cg), nt = cdiv(n, bn), slots = sms / cg;
+            const int mt = cdiv(m, kMT * cg), nt = cdiv(n, bn);
             const long long units = tiles_of(kind, mt, nt, bn / (kMT * cg));
-            // Clocks of a block of terms: its MMAs, its bytes (TMA 60 bytes per clock and SM;
-            // GEN: fp32 at the memory's rate when all SMs read, and 1200 as measured), or what
-            // goes through shared memory (128 bytes per clock: written once, read per MMA).
+            // Clocks of a block of terms: its MMAs, its bytes (TMA 50 bytes per clock and SM;
+            // GEN: fp32 at the memory's rate when all SMs read, and 975 of 888 as measured),
+            // or what goes through shared memory (128 bytes per clock: written once, read per
+            // MMA).
             const double mma = mmas * (bn / 2 + 10.0), bytes = P * (kMT + bn / cg) * bk * 2.0;
-            double per = std::max({mma, bytes / 60.0, (bytes + mmas * (kMT + bn / cg) * 32.0) / 128.0});
-            if (gen) per = std::max({mma * 1.15, kMT * bk * 4 / 21.0, bn * 192.0 / 40.0, 800.0});
+            double per = std::max({mma, bytes / 50.0, (bytes + mmas * (kMT + bn / cg) * 32.0) / 128.0});
+            if (gen) per = std::max({mma * 1.1, kMT * bk * 4 / 21.0, bn * 192.0 / 40.0, 600.0});
             // (and of a tile: first loads, last sums, epilogue)
-            const double tail = 5000.0 + bn * (kind == GEMM_OUT ? 12.0 : 20.0);
-            for (int sp = 1; sp <= std::min({max_splits, kblocks, 64}); ++sp) {
-                const int kps = cdiv(kblocks, sp);
-                if (cdiv(kblocks, kps) != sp) continue;
-                if (sp > 1 && units * sp > 4 * slots) break;
-                const double waves = (double)((units * sp + slots - 1) / slots);
-                const double join = sp > 1 ? 5000.0 + 2.0 * sp * m * (double)n * 4.0 / 3500.0 : 0.0;
-                const double score = waves * kps * per + tail + (waves - 1) * 1000.0 + join;
+            const double tail = 4500.0 + bn * (kind == GEMM_OUT ? 16.0 : 24.0);
+            for (int cl = 1; cl <= 8; cl *= 2) {
+                if (cl > 1 && (cg > 1 || whole || cl > kblocks)) break;
+                const int kps = cdiv(kblocks, cl);
+                if (cdiv(kblocks, kps) != cl) continue;
+                // (clusters do not span GPCs: fewer of eight CTAs than SMs / 8 are resident)
+                const int slots = cl == 1 ? sms / cg : std::max(1, cluster_capacity(gemm_kernel_address(), 384, cl, kSmemMax));
+                const double waves = (double)((units + slots - 1) / slots);
+                // (shares meet: two barriers of the cluster, bn / cl columns read from each)
+                const double meet = cl > 1 ? 2500.0 + bn * 10.0 : 0.0;
+                // (a cluster has one tile: nothing of the next runs during its epilogue)
+                const double more = cl > 1 ? tail + meet : 1000.0;
+                const double score = waves * kps * per + tail + meet + (waves - 1) * more;
                 if (best.bn && score >= best.score) continue;
                 best.planes = planes;
                 best.kind = kind;
                 best.cg = cg;
                 best.bn = bn;
-                best.splits = sp;
+                best.splits = cl;
+                best.groups = 1;
                 best.kb_per_split = kps;
                 best.score = score;
                 best.n_tiles = nt;
-                best.partial_bytes = sp > 1 ? align_up((size_t)sp * m * n * sizeof(float), kWsAlign) : 0;
+            }
+            for (int gr = 2; gr <= std::min(max_groups, kblocks) && cg == 1; ++gr) {
+                const int kps = cdiv(kblocks, gr);
+                if (cdiv(kblocks, kps) != gr) continue;
+                if (units * gr > sms) break;
+                // (the sums of the others, written and read back through the L2)
+                const double score = kps * per + tail + 1000.0 + (gr - 1) * (double)m * n * 8.0 / 3500.0;
+                if (score >= best.score) continue;
+                best.planes = planes;
+                best.kind = kind;
+                best.cg = cg;
+                best.bn = bn;
+                best.splits = 1;
+                best.groups = gr;
+                best.kb_per_split = kps;
+                best.score = score;
+                best.n_tiles = nt;
             }
         }
     }
     return best;
 }
 
-GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_splits) {
+GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_groups) {
     // (a plan takes some 5 us of host time, a small call has a few)
     static std::mutex mu;
     static std::map<std::array<int, 7>, GemmPlan> cache;
     const int sms = num_sms();
-    const std::array<int, 7> key = {planes, kind, m, n, k, max_splits, sms};
+    const std::array<int, 7> key = {planes, kind, m, n, k, max_groups, sms};
     {
         std::lock_guard<std::mutex> g(mu);
         const auto it = cache.find(key);
         if (it != cache.end()) return it->second;
     }
-    const GemmPlan p = plan_gemm_anew(planes, kind, m, n, k, max_splits, sms);
+    const GemmPlan p = plan_gemm_anew(planes, kind, m, n, k, max_groups, sms);
     std::lock_guard<std::mutex> g(mu);
     if (cache.size() >= 256) cache.clear();
     cache.emplace(key, p);
@@ -313,6 +262,7 @@ bool gemm_together(const GemmPlan &a, int m_a, int n_a, int k_a, const GemmPlan 
 }
 
 qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, cudaStream_t st) {
+    if (count > 1 && plan.splits * plan.groups > 1) return QCNN_ERR_UNSUPPORTED;
     const bool gen = plan.planes == GEMM_F32;
     const int P = gen ? 3 : plan.planes, cg = plan.cg, bnc = plan.bn / cg;
     GemmArgs g = {};
@@ -342,22 +292,21 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
         p.kblocks = std::max(1, cdiv(s.k, block_k(gen)));
         p.m_tiles = cdiv(s.m, kMT * cg);
         p.n_tiles = cdiv(s.n, plan.bn);
-        p.splits = count > 1 ? 1 : plan.splits;
-        p.kb_per_split = p.splits > 1 ? plan.kb_per_split : p.kblocks;
+        p.kb_per_split = plan.splits > 1 || plan.groups > 1 ? plan.kb_per_split : p.kblocks;
         p.group = std::max(1, 16 / cg);
         p.e = s.e;
-        if (p.splits == 1) p.e.partial = nullptr;
         p.e.pair = (pairs(s.e.out, s.e.out_type, s.e.ldo, s.e.out_plane, s.m) ? 1 : 0) |
                    (pairs(s.e.pre, s.e.out_type, s.e.ldp, 0, s.m) ? 2 : 0) |
                    (pairs(s.e.add, s.e.add_type, s.e.lda, s.e.add_plane, s.m) ? 4 : 0);
         const long long tiles = tiles_of(plan.kind, p.m_tiles, p.n_tiles, plan.bn / (kMT * cg));
-        if (tiles * p.splits > (1 << 30)) return QCNN_ERR_UNSUPPORTED;
-        p.tiles = (int)tiles;
-        p.units = p.tiles * p.splits;
+        if (tiles > (1 << 27)) return QCNN_ERR_UNSUPPORTED;
+        p.units = (int)tiles;
         g.units += p.units;
         if (p.kb_per_split * block_k(gen) > 128) g.stay = 0;
     }
     g.count = count;
+    g.cl = plan.splits;
+    g.groups = plan.groups;
     g.bn = plan.bn;
     g.b_off = a_bytes;  // (multiples of 1024: 128 rows; 64 rows of 128 bytes)
     g.stage = (unsigned)align_up(a_bytes + b_bytes, 1024);
@@ -367,17 +316,8 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     if (P == 3) g.S &= ~1;
     if (g.S < (gen ? 2 : P == 3 ? 6 : P)) return QCNN_ERR_UNSUPPORTED;
     const size_t smem = std::max(kSmemLeast, g.S * (size_t)g.stage + raw + 1024);
-    const int ctas = std::min(g.units, num_sms() / cg) * cg;
+    const int ctas = g.cl * g.groups > 1 ? g.units * g.cl * g.groups : std::min(g.units, num_sms() / cg) * cg;
     return launcher(plan)(&g, ctas, smem, st);
-}
-
-qcnn_status launch_gemm_join(const GemmPlan &plan, const GemmProblem &p, cudaStream_t st) {
-    if (plan.kind == GEMM_SYM) {
-        const dim3 patches(cdiv(p.m, 32), cdiv(p.m, 32));
-        return launch_pdl(gemm_join_sym_kernel, patches, dim3(256), 0, st, p.e, p.m, plan.splits);
-    }
-    const dim3 grid(cdiv(p.m, 256), std::min(p.n, 65535));
-    return launch_pdl(gemm_join_kernel, grid, dim3(256), 0, st, p.e, p.m, p.n, plan.splits);
 }
 
 qcnn_status launch_planes(const void *src, int bf16, long long rows, int cols, long long ld, int planes,

@@ -26,14 +26,13 @@ struct GemmOperand {
 
 enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1, GEMM_T_PLANES2 = 2, GEMM_T_PLANES3 = 3 };
 
-// What becomes of a sum.  OUT: v = alpha * sum + bias[m] (alpha: *alpha_ptr where set); pre = v; v = act(v);
-// v += beta * add[n][m]; v += diagonal where n == m; out[n][m] = v.  With partial set: the sums of this split
-// alone, fp32 [split][n][m], for launch_gemm_join (a CTA that adds up all splits of its tile
-// because it is the last of them reads 1 MB alone: 54 us instead of 33 for 128 rows of 4096 ->
-// 1000).  SYM: the product is symmetric
-// (A and B the same matrix): only m >= n is computed and stored at both places.
-// STATS: m are rows, n classes: the maximum and the sum of exp over a tile's classes
-// of v = sum + bias[n], and the value at the row's target.  DLOGITS: m are classes,
+// What becomes of a sum.  OUT: v = alpha * sum + bias[m] (alpha: *alpha_ptr where set); pre =
+// v; v = act(v); v += beta * add[n][m]; out[n][m] = v.  PLANES: v = alpha * sum + beta * add,
+// + diagonal where n == m; out and add are planes of the product's number, whose matrices
+// have room for whole tiles (rows and columns up to the next multiple of 256).  SYM: PLANES
+// of a symmetric product (A and B the same matrix): only m >= n is computed, and stored at
+// both places.  STATS: m are rows, n classes: the maximum and the sum of exp over a tile's
+// classes of v = sum + bias[n], and the value at the row's target.  DLOGITS: m are classes,
 // n rows: out = g_n (exp(v - lse_n) - [target_n == m]).
 struct GemmEpi {
     float alpha = 1.f, beta = 0.f, diagonal = 0.f;
@@ -48,7 +47,6 @@ struct GemmEpi {
     long long lda = 0, add_plane = 0;
     int add_type = GEMM_T_F32;
     int act = 0;
-    float *partial = nullptr;
     int pair = 0;  // (launch_gemm) bits: out, pre, add go in pairs of elements
     // STATS, DLOGITS
     float2 *stats = nullptr;           // [tile along n][half][m]
@@ -60,7 +58,7 @@ struct GemmEpi {
     long long ld_col = 0;
 };
 
-enum GemmKind { GEMM_OUT = 0, GEMM_SYM = 1, GEMM_STATS = 2, GEMM_DLOGITS = 3 };
+enum GemmKind { GEMM_OUT = 0, GEMM_SYM = 1, GEMM_STATS = 2, GEMM_DLOGITS = 3, GEMM_PLANES = 4 };
 
 struct GemmProblem {
     GemmOperand a, b;
@@ -75,29 +73,30 @@ constexpr int GEMM_F32 = 0;
 struct GemmPlan {
     int planes = 1, kind = 0, cg = 1;
     int bn = 0;       // tile columns
+    // Shares of a tile's terms, of a CTA each in a cluster of that many (1, 2, 4, 8).  (Partial
+    // sums through memory and a launch that joined them took 7 us more per product, and 19
+    // of them added up by a tile's last CTA 28 us.)
     int splits = 1, kb_per_split = 0;
+    int groups = 1;   // or shares whose sums stay apart: out is [groups][n][m], fp32, nothing else
     double score = 0;  // estimated SM clocks
-    size_t partial_bytes = 0;  // 0 where splits == 1
     int n_tiles = 0;
 };
-// max_splits 1: the sums must end in one tile (epilogues that launch_gemm_join does
-// not have)
-GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_splits);
+// max_groups > 1: the caller adds up groups.
+GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_groups = 1);
 
 // Whether two products of one tile shape and kind, a's first, are sooner done in one launch than
 // in two (their tiles are dealt out in turn).
 bool gemm_together(const GemmPlan &a, int m_a, int n_a, int k_a, const GemmPlan &b, int m_b, int n_b, int k_b);
 
 // One launch of one or two products of the same kind and planes (the second fills
-// the SMs that the first one's last tiles leave idle); both with `plan`'s tile, each
-// unsplit if there are two.  With plan.splits > 1, p[0].e.partial must be set, and
-// launch_gemm_join finishes.
+// the SMs that the first one's last tiles leave idle); both with `plan`'s tile, unsplit
+// if there are two.
 qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *p, int count, cudaStream_t st);
-// The epilogue of a split product: the sums of its splits, in order.
-qcnn_status launch_gemm_join(const GemmPlan &plan, const GemmProblem &p, cudaStream_t st);
 
 // Smallest multiple of 8 elements: rows of 16-byte multiples.
 inline long long pad8(long long v) { return (v + 7) / 8 * 8; }
+// Of a matrix with room for whole tiles.
+inline long long pad256(long long v) { return (v + 255) / 256 * 256; }
 
 // src [rows][cols] (fp32 or bf16, row stride ld) -> bf16 planes [planes][rows][pad8(cols)],
 // rows * pad8(cols) elements apart, to dst (null: not) and to kept (null: not), there with

@@ -61,12 +61,14 @@ struct ProblemArgs {
     CUtensorMap map_a, map_b;
     OpArgs a, b;
     unsigned idesc;
-    int m, n, k, kblocks, m_tiles, n_tiles, tiles, splits, kb_per_split, group, units;
+    int m, n, k, kblocks, m_tiles, n_tiles, kb_per_split, group, units;
     GemmEpi e;
 };
 struct GemmArgs {
     ProblemArgs p[2];
     int count, units, bn, S;
+    int cl;                 // CTAs of a cluster that share a tile's terms (CG 1)
+    int groups;             // shares whose sums stay apart (OUT, cl 1)
     int stay;               // three planes: a tile's sum stays in TMEM
     unsigned stage, b_off;  // bytes of a stage, of A's part of it
 };
@@ -79,12 +81,13 @@ struct Shared {
 
 struct Tile {
     int q;               // problem
-    int mt, nt, kb0, kb1, split;
+    int mt, nt, kb0, kb1;
 };
-// Unit u of a launch.  Neighbouring units are a patch of `group` row tiles, whose
-// operands the L2 then holds.  SYM: row tiles from the diagonal on.
+// Unit u of a launch, of the terms of CTA `share` of a cluster.  Neighbouring units are a
+// patch of `group` row tiles, whose operands the L2 then holds.  SYM: row tiles from the
+// diagonal on.
 template <int KIND, int CG>
-__device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u) {
+__device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u, int share) {
     Tile t;
     t.q = g.count > 1 && u >= g.p[0].units;
     const ProblemArgs &p = g.p[t.q];
@@ -92,8 +95,6 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u) {
     if constexpr (KIND == GEMM_SYM) {
         const int per = g.bn / (kMT * CG);  // row tiles per column tile (bn a multiple)
         int nt = 0, first = 0;
-        t.split = u / p.tiles;
-        u -= t.split * p.tiles;
         while (u >= p.m_tiles - first) {
             u -= p.m_tiles - first;
             ++nt;
@@ -102,15 +103,13 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u) {
         t.nt = nt;
         t.mt = first + u;
     } else {
-        t.split = u / p.tiles;
-        u -= t.split * p.tiles;
         const int per = p.group * p.n_tiles, gr = u / per, m0 = gr * p.group;
         const int w = min(p.group, p.m_tiles - m0);
         u -= gr * per;
         t.nt = u / w;
         t.mt = m0 + u - t.nt * w;
     }
-    t.kb0 = t.split * p.kb_per_split;
+    t.kb0 = share * p.kb_per_split;
     t.kb1 = min(p.kblocks, t.kb0 + p.kb_per_split);
     return t;
 }
@@ -420,61 +419,52 @@ __device__ __forceinline__ void act16(float (&v)[16], int act) {
     }
 }
 
-// OUT and SYM: sums v of lane m, columns n0 .. n0 + left - 1; c: what add has there, which
-// next() then fetches for the columns that follow.  The whole warp calls it; rows m up to
-// m_end exist.
-template <int KIND, bool FULL, typename F>
+// OUT: sums v of lane m, columns n0 .. n0 + left - 1; c: what add has there, which next() then
+// fetches for the columns that follow.  The whole warp calls it; rows m up to m_end exist.
+template <bool FULL, typename F>
 __device__ __forceinline__ void finish_out(const GemmEpi &e, int m_end, int m, int n0, int left, float alpha,
                                            float bias, float (&v)[16], const Chunk16 &c, F &&next) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = fmaf(alpha, v[i], bias);
-    if (KIND == GEMM_OUT && e.pre) store16<FULL>(e.pre, e.out_type, e.ldp, 0, e.pair & 2, m_end, m, n0, left, v);
-    if constexpr (KIND == GEMM_OUT) act16(v, e.act);
+    if (e.pre) store16<FULL>(e.pre, e.out_type, e.ldp, 0, e.pair & 2, m_end, m, n0, left, v);
+    act16(v, e.act);
     if (e.add) {
         take16(c, e.add_type, e.pair & 4, m & 1, e.beta, v);
         next();
     }
-    if (e.diagonal != 0.f && (unsigned)(m - n0) < 16u) {
+    store16<FULL>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
+}
+
+// PLANES and SYM: v = alpha * sum + beta * add (+ diagonal) to P planes whose matrix has room
+// for whole tiles, so that nothing is asked about an element.  mirror: to the mirror image as
+// well.  (Small products run this once: what counts is how few instructions there are to
+// fetch; element by element at the diagonal it took 12,000 clocks.)
+template <int P>
+__device__ __forceinline__ void finish_planes(const GemmEpi &e, bool mirror, int m, int n0, float (&v)[16],
+                                              const Chunk16 &c) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= e.alpha;
+    if (e.add) take16(c, P, true, m & 1, e.beta, v);
+    if ((unsigned)(m - n0) < 16u) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (m == n0 + i) v[i] += e.diagonal;
     }
-    if constexpr (KIND == GEMM_OUT) {
-        store16<FULL>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
-    } else {
-        // one value for both places: this tile's where m >= n.  (Above the diagonal inside a
-        // tile: the other place's are stored, by the lanes whose row is the column here.)
-        const bool in = m < m_end;
-        left = min(left, m + 1 - n0);
-        unsigned short *p = static_cast<unsigned short *>(e.out);
-        unsigned w0[8], w1[8], w2[8];
-        auto put = [&](unsigned short *plane, const unsigned (&w)[8]) {
-            unsigned short *q = plane + (long long)n0 * e.ldo + m;
+    unsigned w[P][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i, q += 2 * e.ldo) {
-                if (in && 2 * i < left) q[0] = (unsigned short)w[i];
-                if (in && 2 * i + 1 < left) q[e.ldo] = (unsigned short)(w[i] >> 16);
-            }
-            unsigned short *d = plane + (long long)m * e.ldo + n0;
-            if (in && left >= 16) {  // (rows of planes: 16-byte multiples)
-                *reinterpret_cast<uint4 *>(d) = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<uint4 *>(d + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-            } else if (in && left > 0) {
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (P == 3) planes3(v[2 * i], v[2 * i + 1], w[0][i], w[1][i], w[2][i]);
+        else planes2(v[2 * i], v[2 * i + 1], w[0][i], w[1][i]);
+    }
+    unsigned short *p = static_cast<unsigned short *>(e.out);
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i < left) d[i] = (unsigned short)(w[i / 2] >> (i & 1) * 16);
-            }
-        };
-        if (e.out_type == GEMM_T_PLANES2) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) planes2(v[2 * i], v[2 * i + 1], w0[i], w1[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
-            put(p + 2 * e.out_plane, w2);
+    for (int j = 0; j < P; ++j, p += e.out_plane) {
+        store_plane<true>(p, e.ldo, true, 0, m, n0, 16, w[j]);
+        if (mirror) {  // (rows of 16-byte multiples)
+            uint4 *d = reinterpret_cast<uint4 *>(p + (long long)m * e.ldo + n0);
+            d[0] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+            d[1] = make_uint4(w[j][4], w[j][5], w[j][6], w[j][7]);
         }
-        put(p, w0);
-        put(p + e.out_plane, w1);
     }
 }
 
@@ -577,6 +567,26 @@ __device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned (&v)[8])
         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
         : "memory");
 }
+// What add has at 16 columns of a lane.
+template <int KIND, int P>
+__device__ __forceinline__ void fetch_add(Chunk16 &c, const ProblemArgs &p, int m, int n0, bool is, bool rows_full) {
+    if (!is) return;
+    const GemmEpi &e = p.e;
+    if constexpr (KIND == GEMM_PLANES || KIND == GEMM_SYM) {
+        const unsigned short *src = static_cast<const unsigned short *>(e.add);
+        fetch_pairs<0, true>(c, src, e.lda, 0, m, n0, 16);
+        fetch_pairs<1, true>(c, src + e.add_plane, e.lda, 0, m, n0, 16);
+        if constexpr (P == 3) fetch_pairs<2, true>(c, src + 2 * e.add_plane, e.lda, 0, m, n0, 16);
+    } else {
+        const int left = p.n - n0;
+        if (left <= 0) return;
+        if (rows_full && left >= 16)
+            fetch16<true>(c, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0, left);
+        else
+            fetch16<false>(c, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0, left);
+    }
+}
+
 // ------------------------------------------------------------------- kernel
 template <int P, int KIND, int CG, bool GEN>
 __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
@@ -595,13 +605,25 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
     // what belongs to the 16 columns that a warp is at: bias (STATS), rows (DLOGITS)
     using Column = std::conditional_t<KIND == GEMM_DLOGITS, float4, float>;
     constexpr bool COLUMNS = KIND == GEMM_STATS || KIND == GEMM_DLOGITS;
+    constexpr bool PADDED = KIND == GEMM_PLANES || KIND == GEMM_SYM;
     __shared__ __align__(16) Column columns[COLUMNS ? kEpiWarps : 1][2][16];
     unsigned char *const smem = smem_raw + (-smem_addr(smem_raw) & 1023u);  // (swizzle atoms)
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-    unsigned rank = 0;
-    if constexpr (CG == 2) asm("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
-    const int first_unit = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
+    unsigned rank = 0;  // of the pair
+    int share = 0;      // of a tile's terms
+    if constexpr (CG == 2) {
+        asm("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+    } else if (g.cl > 1) {
+        asm("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(share));
+    }
+    // (a cluster has one tile, and so has a CTA of groups)
+    int first_unit = (int)blockIdx.x / (CG * g.cl);
+    const int step = (int)gridDim.x / CG;
+    if (g.groups > 1) {
+        share = first_unit / g.units;
+        first_unit -= share * g.units;
+    }
 
     if (tid == 0) {
         for (int i = 0; i < g.S; ++i) {
@@ -635,7 +657,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             unsigned issued = 0, issued2 = 0;
             bool ok = true, synced = false;
             for (int u = first_unit; u < g.units && ok; u += step) {
-                const Tile t = tile_of<KIND, CG>(g, u);
+                const Tile t = tile_of<KIND, CG>(g, u, share);
                 const ProblemArgs &p = g.p[t.q];
                 const int m0 = (t.mt * CG + (int)rank) * kMT;
                 const int bn = g.bn / CG, n0 = t.nt * g.bn + (int)rank * bn;
@@ -708,7 +730,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             const unsigned stage = g.stage >> 4;
             const uint64_t base = (uint64_t)((smem_addr(smem) >> 4) & 0x3FFFu) + ring * S * stage;
             for (int u = first_unit; u < g.units && ok; u += step) {
-                const Tile t = tile_of<KIND, CG>(g, u);
+                const Tile t = tile_of<KIND, CG>(g, u, share);
                 const ProblemArgs &p = g.p[t.q];
                 const uint64_t da = p.a.desc + base, db = p.b.desc + base + (g.b_off >> 4);
                 const unsigned ka = p.a.kstep, kb_ = p.b.kstep;
@@ -774,6 +796,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const unsigned tl = tmem + ((unsigned)(quarter * 32) << 16);
         const int chunks = g.bn / 16;  // this warp's: half, half + 2, ...
+        [[maybe_unused]] const unsigned stash = smem_addr(smem);  // (where the stages were)
         grid_dep_sync();
         unsigned use = 0;
         bool ok = true;
@@ -786,24 +809,25 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             }
         };
         for (int u = first_unit; u < g.units; u += step) {
-            const Tile t = tile_of<KIND, CG>(g, u);
+            const Tile t = tile_of<KIND, CG>(g, u, share);
             const ProblemArgs &p = g.p[t.q];
             const GemmEpi &e = p.e;
             const int m = (t.mt * CG + (int)rank) * kMT + quarter * 32 + lane, n0 = t.nt * g.bn;
             const bool in = m < p.m;
             [[maybe_unused]] const bool rows_full = m - lane + 32 <= p.m;  // of the whole warp
+            // (SYM: the square on the diagonal is computed whole, what is below it is mirrored)
+            [[maybe_unused]] const bool mirror = KIND == GEMM_SYM && t.mt * CG * kMT >= n0 + g.bn;
             [[maybe_unused]] float bias = 0.f, col = 0.f;
             [[maybe_unused]] const float alpha = KIND == GEMM_OUT && e.alpha_ptr ? *e.alpha_ptr : e.alpha;
             [[maybe_unused]] RunningSum run;
             [[maybe_unused]] int target = -1;
-            [[maybe_unused]] const bool adds = e.add && !e.partial;
             if constexpr (KIND == GEMM_STATS) {
                 if (in) {
                     const long long c = e.targets[m];
                     target = c >= 0 && c < p.n ? (int)c : -1;
                 }
             } else {
-                if (e.bias && in && !e.partial) bias = e.bias[m];
+                if (!PADDED && e.bias && in) bias = e.bias[m];
             }
             // the sums of the tile, in TMEM at tl + buf * ACC
             unsigned buf = use & 1;
@@ -853,19 +877,9 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     else
                         column = is ? e.rows[n] : make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
                 }
-                if constexpr (KIND == GEMM_OUT || KIND == GEMM_SYM) {
-                    const int left = p.n - (n0 + c * 16);
-                    if (adds && c < chunks && left > 0) {
-                        if (rows_full && left >= 16)
-                            fetch16<true>(add, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0 + c * 16,
-                                          left);
-                        else
-                            fetch16<false>(add, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m,
-                                           n0 + c * 16, left);
-                    }
-                }
+                if constexpr (!COLUMNS) fetch_add<KIND, P>(add, p, m, n0 + c * 16, c < chunks && e.add, rows_full);
             };
-            fetch(half);
+            if (g.cl == 1) fetch(half);
             if (!drain) {
                 if (!(ok = wait_warp(sh, &sh.tfull[buf], (use - 1) >> 1 & 1))) break;
                 tc_fence_after_sync();
@@ -885,15 +899,22 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     stats16(run, n, target, e.target_logit + m, cols, v);
                 } else if constexpr (KIND == GEMM_DLOGITS) {
                     dlogits16(e, rows_full && left >= 16, p.m, m, n, left, bias, cols, col, v);
+                } else if (g.cl > 1) {  // to the cluster
+                    const unsigned d = stash + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(d + i * 512), "f"(v[4 * i]),
+                                     "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3])
+                                     : "memory");
+                } else if constexpr (PADDED) {
+                    finish_planes<P>(e, mirror, m, n, v, add);
+                    if (e.add) fetch(c + 2);
                 } else if (left > 0) {
-                    const bool full = rows_full && left >= 16;
-                    if (e.partial)
-                        store16<false>(e.partial + (long long)t.split * p.n * p.m, GEMM_T_F32, p.m, 0, false, p.m, m,
-                                       n, left, v);
-                    else if (full)
-                        finish_out<KIND, true>(e, p.m, m, n, left, alpha, bias, v, add, [&] { fetch(c + 2); });
+                    const int row = n + (g.groups > 1 ? share * p.n : 0);  // (each group's outputs)
+                    if (rows_full && left >= 16)
+                        finish_out<true>(e, p.m, m, row, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                     else
-                        finish_out<KIND, false>(e, p.m, m, n, left, alpha, bias, v, add, [&] { fetch(c + 2); });
+                        finish_out<false>(e, p.m, m, row, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                 }
             }
             release(buf);
@@ -923,7 +944,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         int cu = first_unit, ckb = 0, ckb1 = 0, cslot = 0;
         int line_in = 0, along_in = 0;  // lines and elements along them that exist from here on
         auto open_tile = [&]() {
-            const Tile t = tile_of<KIND, CG>(g, cu);
+            const Tile t = tile_of<KIND, CG>(g, cu, share);
             ckb = t.kb0;
             ckb1 = t.kb1;
             const int row = t.mt * kMT + quarter * 32 + (mn ? along : line0);
@@ -968,7 +989,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         unsigned par = 0, par2 = 0, ring = 0;
         bool ok = true;
         for (int u = first_unit; u < g.units && ok; u += step) {
-            const Tile t = tile_of<KIND, CG>(g, u);
+            const Tile t = tile_of<KIND, CG>(g, u, share);
             for (int kb = t.kb0; kb < t.kb1; ++kb) {
                 cp_async_wait<kRawSlots - 2>();
                 __syncwarp();
@@ -1019,6 +1040,60 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         }
         cp_async_wait<0>();
     }
+    if constexpr (CG == 1 && !COLUMNS) {
+        if (g.cl > 1) {
+            // The sums of a tile's shares meet in shared memory, where each CTA has left its
+            // own: each adds up a part of the columns, in the order of the shares, and does
+            // their epilogue.
+            __syncwarp();
+            cluster_sync_all();
+            if (warp >= 4 && warp < 4 + kEpiWarps) {
+                const int quarter = warp & 3, half = (warp - 4) >> 2;
+                const Tile t = tile_of<KIND, CG>(g, first_unit, share);
+                const ProblemArgs &p = g.p[0];
+                const GemmEpi &e = p.e;
+                const int m = t.mt * kMT + quarter * 32 + lane;
+                const bool rows_full = m - lane + 32 <= p.m;
+                [[maybe_unused]] const bool mirror = KIND == GEMM_SYM && t.mt * kMT >= (t.nt + 1) * g.bn;
+                const float alpha = KIND == GEMM_OUT && e.alpha_ptr ? *e.alpha_ptr : e.alpha;
+                const float bias = !PADDED && e.bias && m < p.m ? e.bias[m] : 0.f;
+#pragma unroll 1
+                for (int c = share + half * g.cl; c < g.bn / 16; c += 2 * g.cl) {
+                    const int n = t.nt * g.bn + c * 16, left = p.n - n;
+                    Chunk16 add;
+                    fetch_add<KIND, P>(add, p, m, n, e.add != nullptr, rows_full);
+                    const unsigned mine = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
+                    float v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+#pragma unroll 4
+                    for (int s = 0; s < g.cl; ++s) {
+                        unsigned at;
+                        asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(mine), "r"(s));
+                        float r[16];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+                                         : "=f"(r[4 * i]), "=f"(r[4 * i + 1]), "=f"(r[4 * i + 2]), "=f"(r[4 * i + 3])
+                                         : "r"(at + i * 512)
+                                         : "memory");
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] += r[i];
+                    }
+                    if constexpr (PADDED) {
+                        finish_planes<P>(e, mirror, m, n, v, add);
+                    } else if (left > 0) {
+                        if (rows_full && left >= 16)
+                            finish_out<true>(e, p.m, m, n, left, alpha, bias, v, add, [] {});
+                        else
+                            finish_out<false>(e, p.m, m, n, left, alpha, bias, v, add, [] {});
+                    }
+                }
+            }
+            __syncwarp();
+            cluster_sync_all();  // (no CTA leaves while another reads from it)
+        }
+    }
     tc_fence_before_sync();
     __syncthreads();
     if constexpr (CG == 2) cluster_sync_all();
@@ -1036,7 +1111,8 @@ struct GemmKernel {
         const auto k = gemm_kernel<P, KIND, CG, GEN>;
         qcnn_status rc = allow_smem(reinterpret_cast<const void *>(k));
         if (rc != QCNN_OK) return rc;
-        return launch_k(k, dim3(ctas), dim3(GEN ? 512 : 384), smem, st, CG == 2 ? dim3(2, 1, 1) : dim3(0, 0, 0), g);
+        const int cluster = CG * g.cl;
+        return launch_k(k, dim3(ctas), dim3(GEN ? 512 : 384), smem, st, dim3(cluster > 1 ? cluster : 0, 1, 1), g);
     }
 };
 

@@ -102,12 +102,13 @@ __global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, Pi
     }
 }
 
-// X = G / (norm + eps) in planes of rows of pitch elements (or, planes 0, as the result);
+// X = G / (norm + eps) in planes, rows of pitch elements (or, planes 0, as the result);
 // every CTA adds the sums up in the same order.
 template <typename T>
 __global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, Pieces q, int vec,
                                                     const double2 *part, int parts, float eps, int planes,
-                                                    unsigned short *dst, long long pitch, T *out, long long ldo) {
+                                                    unsigned short *dst, long long pitch, long long plane, T *out,
+                                                    long long ldo) {
     __shared__ double2 red[8];
     grid_dep_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -133,7 +134,6 @@ __global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, P
     // matrices with a tiny eps, is taken in two: f2 is 1 otherwise)
     const double f = norm > 0. || norm != norm ? 1.0 / norm : 0.;
     const float f2 = f > 1e30 ? 1e30f : 1.f, f1 = (float)(f > 1e30 ? f / 1e30f : f);
-    const long long plane = q.rows * pitch;
     for (long long i = (long long)blockIdx.x * 8 + warp; i < q.all; i += (long long)gridDim.x * 8) {
         const long long r = i / q.per_row;
         const int first = (int)(i - r * q.per_row) * kPieceCols, end = min(q.cols, first + kPieceCols);
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, P
 
 struct OrthoPlan {
     int P, p, q;  // planes; smaller and larger side
-    Product gram, poly, apply;
+    GemmPlan gram, poly, apply;
 };
 OrthoPlan plan_ortho(int m, int n, int dtype) {
     OrthoPlan o;
@@ -179,30 +179,28 @@ OrthoPlan plan_ortho(int m, int n, int dtype) {
     o.q = std::max(m, n);
     // (one side of the diagonal, or both in smaller tiles where that is sooner done)
     const auto sym = [&](int k) {
-        const GemmPlan s = plan_gemm(o.P, GEMM_SYM, o.p, o.p, k, 64), f = plan_gemm(o.P, GEMM_OUT, o.p, o.p, k, 64);
+        const GemmPlan s = plan_gemm(o.P, GEMM_SYM, o.p, o.p, k), f = plan_gemm(o.P, GEMM_PLANES, o.p, o.p, k);
         return f.score < s.score ? f : s;
     };
-    o.gram.plan = sym(o.q);
-    o.poly.plan = sym(o.p);
-    o.apply.plan = m <= n ? plan_gemm(o.P, GEMM_OUT, o.q, o.p, o.p, 64) : plan_gemm(o.P, GEMM_OUT, o.p, o.q, o.p, 64);
+    o.gram = sym(o.q);
+    o.poly = sym(o.p);
+    o.apply = m <= n ? plan_gemm(o.P, GEMM_PLANES, o.q, o.p, o.p) : plan_gemm(o.P, GEMM_PLANES, o.p, o.q, o.p);
     return o;
 }
 struct OrthoSpace {
     double2 *norm;
     unsigned short *x[2], *a, *b;
-    void *partial;
     size_t bytes;
 };
 OrthoSpace carve_ortho(const OrthoPlan &o, int m, int n, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     OrthoSpace s;
-    const size_t xs = (size_t)o.P * m * pad8(n), as = (size_t)o.P * o.p * pad8(o.p);
+    const size_t xs = (size_t)o.P * pad256(m) * pad256(n), as = (size_t)o.P * pad256(o.p) * pad256(o.p);
     s.norm = c.array<double2>(kNormBlocks);
     s.x[0] = c.array<unsigned short>(xs);
     s.x[1] = c.array<unsigned short>(xs);
     s.a = c.array<unsigned short>(as);
     s.b = c.array<unsigned short>(as);
-    s.partial = c.take(std::max({o.gram.scratch(), o.poly.scratch(), o.apply.scratch()}));
     s.bytes = c.used;
     return s;
 }
@@ -217,10 +215,10 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
     const int vec = tma_ok(G, ldg);  // (16-byte rows; of fp32 more than it needs)
     qcnn_status rc = launch_pdl(norm_kernel<T>, dim3(blocks), dim3(256), 0, st, G, ldg, q, vec, s.norm);
     if (rc != QCNN_OK) return rc;
-    const long long px = pad8(n), xplane = m * px, pa = pad8(o.p), aplane = o.p * pa;
+    const long long px = pad256(n), xplane = pad256(m) * px, pa = pad256(o.p), aplane = pa * pa;
     const int grid = (int)std::min<long long>(2 * kNormBlocks, (q.all + 7) / 8);
     rc = launch_pdl(scale_kernel<T>, dim3(grid), dim3(256), 0, st, G, ldg, q, vec, s.norm, blocks, eps,
-                    steps ? o.P : 0, s.x[0], px, out, ldo);
+                    steps ? o.P : 0, s.x[0], px, xplane, out, ldo);
     for (int i = 0; i < steps && rc == QCNN_OK; ++i) {
         const GemmOperand x{s.x[i & 1], px, xplane, 0}, a{s.a, pa, aplane, 0}, b{s.b, pa, aplane, 0};
         const int type = o.P;  // GEMM_T_PLANES2, GEMM_T_PLANES3
@@ -233,7 +231,7 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
         g.e.ldo = pa;
         g.e.out_plane = aplane;
         g.e.out_type = type;
-        if ((rc = o.gram.run(g, s.partial, st)) != QCNN_OK) break;
+        if ((rc = launch_gemm(o.gram, &g, 1, st)) != QCNN_OK) break;
         g.a = g.b = a;
         g.k = o.p;
         g.e.alpha = k[2];
@@ -244,7 +242,7 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
         g.e.add_type = type;
         g.e.diagonal = k[0];
         g.e.out = s.b;
-        if ((rc = o.poly.run(g, s.partial, st)) != QCNN_OK) break;
+        if ((rc = launch_gemm(o.poly, &g, 1, st)) != QCNN_OK) break;
         GemmProblem u;
         u.k = o.p;
         if (wide) {  // X' [p][q] = B X
@@ -259,17 +257,19 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
             u.a = b;
             u.b = x;
         }
+        GemmPlan apply = o.apply;
         if (i + 1 < steps) {
-            u.e.out = s.x[i + 1 & 1];
+            u.e.out = s.x[(i + 1) & 1];
             u.e.ldo = px;
             u.e.out_plane = xplane;
             u.e.out_type = type;
         } else {
+            apply.kind = GEMM_OUT;
             u.e.out = out;
             u.e.ldo = ldo;
             u.e.out_type = sizeof(T) == 4 ? GEMM_T_F32 : GEMM_T_BF16;
         }
-        rc = o.apply.run(u, s.partial, st);
+        rc = launch_gemm(apply, &u, 1, st);
     }
     return rc;
 }

@@ -38,18 +38,6 @@ inline qcnn_status workspace_ok(const void *ws, size_t have, size_t need) {
     return QCNN_OK;
 }
 
-// One product on the tensor cores, split or not.
-struct Product {
-    GemmPlan plan;
-    size_t scratch() const { return plan.partial_bytes; }
-    qcnn_status run(GemmProblem p, void *partial, cudaStream_t st) const {
-        if (plan.splits > 1) p.e.partial = static_cast<float *>(partial);
-        qcnn_status rc = launch_gemm(plan, &p, 1, st);
-        if (rc == QCNN_OK && plan.splits > 1) rc = launch_gemm_join(plan, p, st);
-        return rc;
-    }
-};
-
 // SM clocks that a pass over `bytes` costs a call beside its products (the memory's
 // rate at the SMs' clock, and a launch).
 inline double pass_clocks(double bytes) { return bytes / 3200.0 + 4000.0; }

@@ -23,6 +23,9 @@ namespace {
 
 constexpr size_t kPiece = 64u << 20;    // bytes of a kept piece of logits
 constexpr size_t kPieceDl = 128u << 20;  // bytes of a piece of their gradient
+// Shares of the terms of kept logits, joined by the pass over their rows (128 rows of 4096 ->
+// 1000 in fp32: 9 us with 19, 24 us with clusters of eight CTAs, which fill fewer SMs).
+constexpr int kGroups = 32;
 
 __device__ __forceinline__ int class_of(const int64_t *targets, int n, int Ct) {
     const long long t = targets[n];
@@ -71,10 +74,10 @@ __device__ __forceinline__ void finish_row(const RowOut &o, int n, float top, fl
     if (o.rows) o.rows[n] = make_float4(lse, o.dloss ? o.dloss[n] : 1.f, __int_as_float(t), 0.f);
 }
 
-// Small: a CTA per row of logits; one more counts the rows.  splits > 1: the logits come as
-// that many partial sums [split][N][Ct] without bias, are added up here and (where there is
+// Small: a CTA per row of logits; one more counts the rows.  groups > 1: the logits come as
+// that many partial sums [group][N][Ct] without bias, are added up here and (where there is
 // a gradient) left in `logits`.
-__global__ void __launch_bounds__(1024) rows_kernel(const float *part, int splits, const float *bias,
+__global__ void __launch_bounds__(1024) rows_kernel(const float *part, int groups, const float *bias,
                                                     float *logits, RowOut o) {
     grid_dep_sync();
     if ((int)blockIdx.x == o.N) {
@@ -94,8 +97,8 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float *part, int split
             const int c = c0 + i * T;
             v[i] = -INFINITY;
             if (c >= o.Ct) continue;
-            if (splits > 1) {
-                v[i] = add_groups<true>(part + row + c, splits, stride) + (bias ? bias[c] : 0.f);
+            if (groups > 1) {
+                v[i] = add_groups<true>(part + row + c, groups, stride) + (bias ? bias[c] : 0.f);
                 if (o.rows) logits[row + c] = v[i];
             } else {
                 v[i] = logits[row + c];
@@ -212,7 +215,7 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
 // cannot read.
 struct XentPlan {
     bool small = false, few = false, wplanes = false;
-    Product logits, stats, dl, dx, dw;
+    GemmPlan logits, stats, dl, dx, dw;
     int piece = 0;  // classes of a piece
     int slab = 0, slabs = 1;
 };
@@ -227,38 +230,37 @@ XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool grad) {
         p.few = N <= kFewRows;
         p.slab = std::max(32, cdiv(cdiv(N, std::max(1, 4 * num_sms() / cdiv(Ct, 128))), 8) * 8);
         p.slabs = cdiv(N, p.slab);
-        p.logits.plan = plan_gemm(P, GEMM_OUT, Ct, N, Cs, 64);
-        p.dx.plan = plan_gemm(P, GEMM_OUT, Cs, N, Ct, 64);
-        p.dw.plan = plan_gemm(P, GEMM_OUT, Cs, Ct, N, 64);
+        p.logits = plan_gemm(P, GEMM_OUT, Ct, N, Cs, kGroups);
+        p.dx = plan_gemm(P, GEMM_OUT, Cs, N, Ct);
+        p.dw = plan_gemm(P, GEMM_OUT, Cs, Ct, N);
         if (!bf16) {
-            const GemmPlan l = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, 64);
-            const GemmPlan x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct, 64);
-            const double planes = (p.few ? 0 : p.logits.plan.score) + (grad ? p.dx.plan.score : 0);
+            const GemmPlan l = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, kGroups);
+            const GemmPlan x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct);
+            const double planes = (p.few ? 0 : p.logits.score) + (grad ? p.dx.score : 0);
             const double direct = (p.few ? 0 : l.score) + (grad ? x.score : 0);
             if (direct <= planes + pass_clocks((double)Ct * Cs * 10.0)) {
                 p.wplanes = false;
-                p.logits.plan = l;
-                p.dx.plan = x;
+                p.logits = l;
+                p.dx = x;
             }
         }
         return p;
     }
-    p.stats.plan = plan_gemm(P, GEMM_STATS, N, Ct, Cs, 1);
+    p.stats = plan_gemm(P, GEMM_STATS, N, Ct, Cs);
     const long long most = (long long)(kPieceDl / ((size_t)N * 2 * P)) / 256 * 256;
     p.piece = (int)std::min<long long>(Ct, std::max<long long>(256, most));
     // (pieces of equal size)
     p.piece = std::min(Ct, cdiv(cdiv(Ct, cdiv(Ct, p.piece)), 256) * 256);
-    p.dl.plan = plan_gemm(P, GEMM_DLOGITS, p.piece, N, Cs, 1);
-    p.dx.plan = plan_gemm(P, GEMM_OUT, Cs, N, p.piece, 1);
-    p.dw.plan = plan_gemm(P, GEMM_OUT, Cs, p.piece, N, 1);
+    p.dl = plan_gemm(P, GEMM_DLOGITS, p.piece, N, Cs);
+    p.dx = plan_gemm(P, GEMM_OUT, Cs, N, p.piece);
+    p.dw = plan_gemm(P, GEMM_OUT, Cs, p.piece, N);
     return p;
 }
 struct XentSpace {
-    float *inv = nullptr, *logits = nullptr, *target_logit = nullptr, *db = nullptr, *dx = nullptr;
+    float *inv = nullptr, *logits = nullptr, *part = nullptr, *target_logit = nullptr, *db = nullptr, *dx = nullptr;
     float4 *rows = nullptr;
     float2 *stats = nullptr;
     unsigned short *x = nullptr, *w = nullptr, *kept = nullptr, *dl = nullptr;
-    void *partial = nullptr;
     size_t bytes = 0;
 };
 XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool grad, bool xa, bool wa, void *ws) {
@@ -273,27 +275,24 @@ XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool g
     const bool x_copy = !p.few && (!bf16 || !xa);
     if (x_copy) s.x = c.array<unsigned short>(P * N * pc);
     if ((!p.few || grad) && (bf16 ? !wa : p.wplanes)) s.w = c.array<unsigned short>(P * Ct * pc);
-    size_t partial = 0;
     if (p.small) {
         s.logits = c.array<float>((size_t)N * Ct);
-        if (!p.few) partial = p.logits.scratch();
+        if (!p.few && p.logits.groups > 1) s.part = c.array<float>((size_t)p.logits.groups * N * Ct);
     } else {
-        s.stats = c.array<float2>((size_t)p.stats.plan.n_tiles * 2 * N);
+        s.stats = c.array<float2>((size_t)p.stats.n_tiles * 2 * N);
         s.target_logit = c.array<float>(N);
     }
     if (grad) {
         // rows without a class must not reach dW, not even as 0 * NaN
         s.kept = c.array<unsigned short>(P * N * pc);
         s.dl = c.array<unsigned short>(P * N * pad8(p.piece));
-        partial = std::max({partial, p.dx.scratch(), p.dw.scratch()});
         if (p.small) {
             s.db = c.array<float>((size_t)p.slabs * Ct);
         } else {
-            s.db = c.array<float>((size_t)p.dl.plan.n_tiles * 2 * p.piece);
+            s.db = c.array<float>((size_t)p.dl.n_tiles * 2 * p.piece);
             if (p.piece < Ct) s.dx = c.array<float>((size_t)N * Cs);
         }
     }
-    s.partial = c.take(partial);
     s.bytes = c.used;
     return s;
 }
@@ -349,14 +348,16 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
             g.m = Ct;
             g.n = N;
             g.k = Cs;
-            g.e.partial = static_cast<float *>(s.partial);
-            rc = launch_gemm(p.logits.plan, &g, 1, st);
+            if (p.logits.groups > 1) {
+                g.e.bias = nullptr;
+                g.e.out = s.part;
+            }
+            rc = launch_gemm(p.logits, &g, 1, st);
         }
         if (rc != QCNN_OK) return rc;
-        // (a split product's sums are joined by the pass over its rows)
         rc = launch_pdl(rows_kernel, dim3(N + (a.grad ? 1 : 0)),
                         dim3(std::min(1024, std::max(128, cdiv(Ct, 128) * 128))), 0, st,
-                        static_cast<const float *>(s.partial), p.few ? 1 : p.logits.plan.splits, a.bias, s.logits, ro);
+                        static_cast<const float *>(s.part), p.few ? 1 : p.logits.groups, a.bias, s.logits, ro);
     } else {
         g.a = xo;
         g.b = wo;
@@ -367,9 +368,9 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         g.e.stats = s.stats;
         g.e.targets = reinterpret_cast<const long long *>(a.targets);
         g.e.target_logit = s.target_logit;
-        if ((rc = launch_gemm(p.stats.plan, &g, 1, st)) != QCNN_OK) return rc;
+        if ((rc = launch_gemm(p.stats, &g, 1, st)) != QCNN_OK) return rc;
         rc = launch_pdl(stats_join_kernel, dim3(cdiv(N, 32) + (a.grad ? 1 : 0)), dim3(1024), 0, st, s.stats,
-                        p.stats.plan.n_tiles * 2, s.target_logit, ro);
+                        p.stats.n_tiles * 2, s.target_logit, ro);
     }
     if (rc != QCNN_OK || !a.grad) return rc;
 
@@ -404,9 +405,9 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
             d.e.out_plane = zplane;
             d.e.col_part = s.db;
             d.e.ld_col = p.piece;
-            rc = launch_gemm(p.dl.plan, &d, 1, st);
+            rc = launch_gemm(p.dl, &d, 1, st);
             if (rc == QCNN_OK && a.dbias)
-                rc = launch_column_join(s.db, p.dl.plan.n_tiles * 2, p.piece, cn, inv, a.dbias + c0, st);
+                rc = launch_column_join(s.db, p.dl.n_tiles * 2, p.piece, cn, inv, a.dbias + c0, st);
         }
         if (rc != QCNN_OK) return rc;
         GemmProblem q;
@@ -425,7 +426,7 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         q.e.out = last ? a.dx : s.dx;
         q.e.ldo = last ? a.lddx : Cs;
         q.e.out_type = last ? type : GEMM_T_F32;
-        if ((rc = p.dx.run(q, s.partial, st)) != QCNN_OK) return rc;
+        if ((rc = launch_gemm(p.dx, &q, 1, st)) != QCNN_OK) return rc;
         GemmProblem v;
         v.a = xk;
         v.b = GemmOperand{s.dl, pz, zplane, 1};
@@ -436,7 +437,7 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         v.e.out = static_cast<uint8_t *>(a.dW) + c0 * a.lddw * type_bytes(a.dtype);
         v.e.ldo = a.lddw;
         v.e.out_type = type;
-        if ((rc = p.dw.run(v, s.partial, st)) != QCNN_OK) return rc;
+        if ((rc = launch_gemm(p.dw, &v, 1, st)) != QCNN_OK) return rc;
     }
     return QCNN_OK;
 }
