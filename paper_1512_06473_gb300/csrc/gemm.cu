@@ -177,6 +177,9 @@ static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int ma
             const double mma = mmas * (bn / 2 + 10.0), bytes = P * (kMT + bn / cg) * bk * 2.0;
             double per = std::max({mma, bytes / 50.0, (bytes + mmas * (kMT + bn / cg) * 32.0) / 128.0});
             if (gen) per = std::max({mma * 1.1, kMT * bk * 4 / 21.0, bn * 192.0 / 40.0, 600.0});
+            // (three planes: a tile's sums go through registers, where they have no accumulator
+            // for each block; with one, the next tile's come meanwhile)
+            if (planes == 3 && kblocks == 2 && bn > 128) per += 1500.0;
             // (and of a tile: first loads, last sums, epilogue)
             const double tail = 4500.0 + bn * (kind == GEMM_OUT ? 16.0 : 24.0);
             for (int cl = 1; cl <= 8; cl *= 2) {
@@ -248,15 +251,21 @@ bool gemm_together(const GemmPlan &a, int m_a, int n_a, int k_a, const GemmPlan 
     const int slots = num_sms() / a.cg;
     const long long ta = (long long)cdiv(m_a, kMT * a.cg) * cdiv(n_a, a.bn),
                     tb = (long long)cdiv(m_b, kMT * a.cg) * cdiv(n_b, a.bn);
+    if (ta + tb > 64ll * slots) return false;  // (little is idle in the end)
     const long long ka = k_a + 128, kb = k_b + 128;  // (with a tile's own costs, in terms)
     const long long apart = cdiv((int)std::min<long long>(ta, 1 << 30), slots) * ka +
                             cdiv((int)std::min<long long>(tb, 1 << 30), slots) * kb;
-    // the longest of the slots: slot i has tiles i, i + slots, ... of a's and then b's
+    // the longest of the slots (tiles as unit_at deals them out)
     long long most = 0;
+    const long long all = ta + tb;
     for (int i = 0; i < slots; ++i) {
-        const long long of_a = ta > i ? (ta - i + slots - 1) / slots : 0;
-        const long long all = ta + tb > i ? (ta + tb - i + slots - 1) / slots : 0;
-        most = std::max(most, of_a * ka + (all - of_a) * kb);
+        long long sum = 0;
+        for (long long r = 0;; ++r) {
+            const long long u = r * slots + (r == 1 ? slots - 1 - i : i);
+            if (u >= all) break;
+            sum += u < ta ? ka : kb;
+        }
+        most = std::max(most, sum);
     }
     return most < apart;
 }
@@ -302,7 +311,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
         if (tiles > (1 << 27)) return QCNN_ERR_UNSUPPORTED;
         p.units = (int)tiles;
         g.units += p.units;
-        if (p.kb_per_split * block_k(gen) > 128) g.stay = 0;
+        if (p.kb_per_split > (!gen && plan.bn <= 128 ? 2 : 1)) g.stay = 0;
     }
     g.count = count;
     g.cl = plan.splits;

@@ -114,6 +114,12 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u, int share) {
     return t;
 }
 
+// The unit of a CTA's round r.  Of two products the second round is dealt out backwards: what
+// it still has of the longer tiles goes to those that the last, incomplete round passes by.
+__device__ __forceinline__ int unit_at(const GemmArgs &g, int r, int first, int step) {
+    return r * step + (r == 1 && g.count > 1 ? step - 1 - first : first);
+}
+
 __device__ __forceinline__ bool wait_one(Shared &s, uint64_t *bar, unsigned parity) {
     bool ok = mbar_wait_bounded(bar, parity, 64);
     for (unsigned i = 0; i < kPolls / 64 && !ok; ++i) {
@@ -594,8 +600,8 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
     constexpr int PL = GEN ? 1 : P;  // stages (planes) of a block of terms
     constexpr bool DRAIN = P == 3;   // a block's sum at a time
     // Rings of stages, and as many warps that issue MMAs, each with a ring and an accumulator of
-    // its own, which take the accumulators in turn: a block's each, or (g.stay: sums of up to
-    // 128 terms, whose additions in TMEM lose less than 2^-21) a tile's.  (A warp's waits come back behind the MMAs that it has
+    // its own, which take the accumulators in turn: a block's each, or (g.stay: tiles of one
+    // block, or of two and 128 columns, which have an accumulator each) a tile's.  (A warp's waits come back behind the MMAs that it has
     // issued: one alone left the tensor core idle between accumulators, 1,204 clocks per block
     // of 888.  And a ring has one consumer: a wait for a phase two ahead passes at once.)
     constexpr int RINGS = DRAIN ? 2 : 1;
@@ -656,7 +662,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             unsigned par = 0, par2 = 0, ring = 0;
             unsigned issued = 0, issued2 = 0;
             bool ok = true, synced = false;
-            for (int u = first_unit; u < g.units && ok; u += step) {
+            for (int r = 0, u = first_unit; u < g.units && ok; u = unit_at(g, ++r, first_unit, step)) {
                 const Tile t = tile_of<KIND, CG>(g, u, share);
                 const ProblemArgs &p = g.p[t.q];
                 const int m0 = (t.mt * CG + (int)rank) * kMT;
@@ -710,7 +716,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             if (!synced) grid_dep_sync();
             // no copy of its own under way when the CTA leaves
             if (rank == 0 || !ok)
-                for (int r = 0; r < RINGS; ++r, ring ^= 1, issued = issued2)
+                for (int i2 = 0; i2 < RINGS; ++i2, ring ^= 1, issued = issued2)
                     for (unsigned i = issued > (unsigned)S ? issued - S : 0; i < issued; ++i) {
                         const int at = (int)ring * S + (int)(i % S);
                         mbar_wait_bounded(rank == 0 ? &sh.full[at] : &sh.empty[at], i / S & 1, kPolls);
@@ -729,7 +735,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             bool ok = true;
             const unsigned stage = g.stage >> 4;
             const uint64_t base = (uint64_t)((smem_addr(smem) >> 4) & 0x3FFFu) + ring * S * stage;
-            for (int u = first_unit; u < g.units && ok; u += step) {
+            for (int r = 0, u = first_unit; u < g.units && ok; u = unit_at(g, ++r, first_unit, step)) {
                 const Tile t = tile_of<KIND, CG>(g, u, share);
                 const ProblemArgs &p = g.p[t.q];
                 const uint64_t da = p.a.desc + base, db = p.b.desc + base + (g.b_off >> 4);
@@ -737,11 +743,11 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 [[maybe_unused]] const unsigned pb = p.b.plane;
                 const uint32_t idesc = p.idesc;
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    const bool fresh = drain || kb == t.kb0, last = drain || kb + 1 == t.kb1;
+                    const bool first = drain || kb == t.kb0, last = drain || kb + 1 == t.kb1;
                     const unsigned buf = use & 1, round = use >> 1;
                     if (last) ++use;
                     if (RINGS == 2 && buf != ring) continue;  // the other warp's
-                    if (fresh) {
+                    if (first) {
                         if (!(ok = wait_one(sh, &sh.tempty[buf], (round & 1) ^ 1))) break;
                     }
                     // the stages of this block's planes, the last plane first
@@ -757,8 +763,9 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     }
                     if (!ok) break;
                     tc_fence_after_sync();
-                    const unsigned d = tmem + buf * ACC;
-                    bool acc = !fresh;
+                    // (three planes: each block's sum apart)
+                    const unsigned d = tmem + buf * ACC + (DRAIN && !drain ? (kb - t.kb0) * 128 : 0);
+                    bool acc = DRAIN ? false : !first;
                     auto product = [&](int i, int j) {
 #pragma unroll
                         for (int s = 0; s < KS; ++s) {
@@ -808,7 +815,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 else arrive_leader(&sh.tempty[buf]);
             }
         };
-        for (int u = first_unit; u < g.units; u += step) {
+        for (int r = 0, u = first_unit; u < g.units; u = unit_at(g, ++r, first_unit, step)) {
             const Tile t = tile_of<KIND, CG>(g, u, share);
             const ProblemArgs &p = g.p[t.q];
             const GemmEpi &e = p.e;
@@ -895,6 +902,12 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     fetch(c + 2);
                 }
                 tmem_ld16(tl + buf * ACC + c * 16, v);
+                if (DRAIN && !drain && t.kb1 - t.kb0 > 1) {
+                    float v2[16];
+                    tmem_ld16(tl + buf * ACC + 128 + c * 16, v2);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += v2[i];
+                }
                 if constexpr (KIND == GEMM_STATS) {
                     stats16(run, n, target, e.target_logit + m, cols, v);
                 } else if constexpr (KIND == GEMM_DLOGITS) {
@@ -941,7 +954,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         // this lane's first line (row, or term) and place along it
         const int line0 = lane >> 3, along = (lane & 7) * 4;
         const float *src = base;
-        int cu = first_unit, ckb = 0, ckb1 = 0, cslot = 0;
+        int cu = first_unit, cr = 0, ckb = 0, ckb1 = 0, cslot = 0;
         int line_in = 0, along_in = 0;  // lines and elements along them that exist from here on
         auto open_tile = [&]() {
             const Tile t = tile_of<KIND, CG>(g, cu, share);
@@ -975,7 +988,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 if (mn) line_in -= 32;
                 else along_in -= 32;
                 if (++ckb == ckb1) {
-                    cu += step;
+                    cu = unit_at(g, ++cr, first_unit, step);
                     if (cu < g.units) open_tile();
                 }
                 if (++cslot == kRawSlots) cslot = 0;
@@ -988,7 +1001,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         int slot = 0, slot2 = 0, rslot = 0;  // (stages: as the TMA's)
         unsigned par = 0, par2 = 0, ring = 0;
         bool ok = true;
-        for (int u = first_unit; u < g.units && ok; u += step) {
+        for (int r = 0, u = first_unit; u < g.units && ok; u = unit_at(g, ++r, first_unit, step)) {
             const Tile t = tile_of<KIND, CG>(g, u, share);
             for (int kb = t.kb0; kb < t.kb1; ++kb) {
                 cp_async_wait<kRawSlots - 2>();
