@@ -221,11 +221,21 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, co
     }
 }
 
+// A CTA takes 32 columns; eight warps an eighth of the rows each, added up in their order.
 __global__ void __launch_bounds__(256) column_join_kernel(const float *part, int rows, long long ld, int cols,
                                                           const float *scale, float *dst) {
+    __shared__ float red[8][32];
     grid_dep_sync();
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c < cols) dst[c] = add_groups<true>(part + c, rows, ld) * (scale ? *scale : 1.f);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
+    const int per = (rows + 7) / 8, r0 = min(rows, warp * per), r1 = min(rows, r0 + per);
+    red[warp][lane] = c < cols ? add_groups<true>(part + (long long)r0 * ld + c, r1 - r0, ld) : 0.f;
+    __syncthreads();
+    if (warp == 0 && c < cols) {
+        float v = red[0][lane];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) v += red[w][lane];
+        dst[c] = v * (scale ? *scale : 1.f);
+    }
 }
 
 // Rows per CTA of dz_kernel: enough CTAs to fill the SMs twice, 32 rows at least.
@@ -327,7 +337,7 @@ qcnn_status launch_few_rows(const FewRows &f, cudaStream_t st) {
 
 qcnn_status launch_column_join(const float *part, int rows, long long ld, int cols, const float *scale,
                                float *dst, cudaStream_t st) {
-    return launch_pdl(column_join_kernel, dim3(cdiv(cols, 256)), dim3(256), 0, st, part, rows, ld, cols, scale, dst);
+    return launch_pdl(column_join_kernel, dim3(cdiv(cols, 32)), dim3(256), 0, st, part, rows, ld, cols, scale, dst);
 }
 
 }  // namespace qcnn

@@ -208,9 +208,9 @@ static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int ma
             for (int gr = 2; gr <= std::min(max_groups, kblocks) && cg == 1; ++gr) {
                 const int kps = cdiv(kblocks, gr);
                 if (cdiv(kblocks, kps) != gr) continue;
-                if (units * gr > sms) break;
                 // (the sums of the others, written and read back through the L2)
-                const double score = kps * per + tail + 1000.0 + (gr - 1) * (double)m * n * 8.0 / 3500.0;
+                const double waves = (double)((units * gr + sms - 1) / sms);
+                const double score = waves * (kps * per + 1000.0) + tail + (gr - 1) * (double)m * n * 8.0 / 3500.0;
                 if (score >= best.score) continue;
                 best.planes = planes;
                 best.kind = kind;
@@ -308,9 +308,9 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
                    (pairs(s.e.pre, s.e.out_type, s.e.ldp, 0, s.m) ? 2 : 0) |
                    (pairs(s.e.add, s.e.add_type, s.e.lda, s.e.add_plane, s.m) ? 4 : 0);
         const long long tiles = tiles_of(plan.kind, p.m_tiles, p.n_tiles, plan.bn / (kMT * cg));
-        if (tiles > (1 << 27)) return QCNN_ERR_UNSUPPORTED;
-        p.units = (int)tiles;
-        g.units += p.units;
+        if (tiles * plan.groups > (1 << 27)) return QCNN_ERR_UNSUPPORTED;
+        p.units = (int)tiles;  // (of a group)
+        g.units += p.units * plan.groups;
         if (p.kb_per_split > (!gen && plan.bn <= 128 ? 2 : 1)) g.stay = 0;
     }
     g.count = count;
@@ -325,7 +325,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     if (P == 3) g.S &= ~1;
     if (g.S < (gen ? 2 : P == 3 ? 6 : P)) return QCNN_ERR_UNSUPPORTED;
     const size_t smem = std::max(kSmemLeast, g.S * (size_t)g.stage + raw + 1024);
-    const int ctas = g.cl * g.groups > 1 ? g.units * g.cl * g.groups : std::min(g.units, num_sms() / cg) * cg;
+    const int ctas = g.cl > 1 ? g.units * g.cl : std::min(g.units, num_sms() / cg) * cg;
     return launcher(plan)(&g, ctas, smem, st);
 }
 

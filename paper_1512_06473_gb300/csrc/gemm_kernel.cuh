@@ -81,9 +81,9 @@ struct Shared {
 
 struct Tile {
     int q;               // problem
-    int mt, nt, kb0, kb1;
+    int mt, nt, kb0, kb1, group;
 };
-// Unit u of a launch, of the terms of CTA `share` of a cluster.  Neighbouring units are a
+// Unit u of a launch, of the terms of CTA `share` of a cluster (or of the unit's group).  Neighbouring units are a
 // patch of `group` row tiles, whose operands the L2 then holds.  SYM: row tiles from the
 // diagonal on.
 template <int KIND, int CG>
@@ -92,6 +92,11 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u, int share) {
     t.q = g.count > 1 && u >= g.p[0].units;
     const ProblemArgs &p = g.p[t.q];
     if (t.q) u -= g.p[0].units;
+    t.group = 0;
+    if (KIND == GEMM_OUT && g.groups > 1) {
+        share = t.group = u / p.units;
+        u -= share * p.units;
+    }
     if constexpr (KIND == GEMM_SYM) {
         const int per = g.bn / (kMT * CG);  // row tiles per column tile (bn a multiple)
         int nt = 0, first = 0;
@@ -549,17 +554,6 @@ __device__ __forceinline__ void cp_async4_part(unsigned dst, const void *src, un
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(bytes)
                  : "memory");
 }
-// n (may be negative, or more) of four elements from src to dst; the others become zero.
-// none: any address that may be read.
-__device__ __forceinline__ void copy4(unsigned dst, const float *src, int n, bool vec, const float *none) {
-    n = max(0, min(n, 4));
-    if (vec) {
-        cp_async16_part(dst, n ? src : none, 4 * n);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) cp_async4_part(dst + 4 * i, i < n ? src + i : none, i < n ? 4 : 0);
-    }
-}
 __device__ __forceinline__ void mma_ts(unsigned d, unsigned a, uint64_t b, uint32_t idesc, bool acc) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -623,13 +617,8 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
     } else if (g.cl > 1) {
         asm("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(share));
     }
-    // (a cluster has one tile, and so has a CTA of groups)
-    int first_unit = (int)blockIdx.x / (CG * g.cl);
-    const int step = (int)gridDim.x / CG;
-    if (g.groups > 1) {
-        share = first_unit / g.units;
-        first_unit -= share * g.units;
-    }
+    // (a cluster has one tile)
+    const int first_unit = (int)blockIdx.x / (CG * g.cl), step = (int)gridDim.x / CG;
 
     if (tid == 0) {
         for (int i = 0; i < g.S; ++i) {
@@ -923,7 +912,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     finish_planes<P>(e, mirror, m, n, v, add);
                     if (e.add) fetch(c + 2);
                 } else if (left > 0) {
-                    const int row = n + (g.groups > 1 ? share * p.n : 0);  // (each group's outputs)
+                    const int row = n + t.group * p.n;  // (each group's outputs)
                     if (rows_full && left >= 16)
                         finish_out<true>(e, p.m, m, row, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                     else
@@ -943,16 +932,17 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         // A warp has 32 rows (its TMEM lanes) x 32 terms of every stage, and copies them
         // itself: no barrier between copying and splitting.  Rows of k: [32][32] floats, the
         // 16-byte pieces of a row permuted so that eight neighbouring rows read from all
-        // banks; rows of m: [32 terms][32].  Both are eight copies of 16 bytes per lane, four
-        // lines on.
+        // banks; rows of m: [32 terms][32].  Both are 32 lines of 128 bytes: eight copies of 16
+        // bytes per lane, four lines at a time, or, where rows are off the 16-byte alignment, 32
+        // of 4, a line at a time.
         const int quarter = warp & 3;
         const ProblemArgs &p = g.p[0];
         const bool mn = p.a.mn, vec = p.a.vec;
         const float *const base = p.a.src;
-        const long long ld = p.a.ld, gap = 4 * ld, step_k = mn ? 32 * ld : 32;
+        const long long ld = p.a.ld, step_k = mn ? 32 * ld : 32;
         const unsigned raw = smem_addr(smem) + g.S * g.stage + (warp - 12) * (kRawSlots * 4096);
         // this lane's first line (row, or term) and place along it
-        const int line0 = lane >> 3, along = (lane & 7) * 4;
+        const int line0 = vec ? lane >> 3 : 0, along = vec ? (lane & 7) * 4 : lane;
         const float *src = base;
         int cu = first_unit, cr = 0, ckb = 0, ckb1 = 0, cslot = 0;
         int line_in = 0, along_in = 0;  // lines and elements along them that exist from here on
@@ -971,18 +961,25 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         auto copy_next = [&]() {
             if (cu < g.units) {
                 const float *s = src;
-                const unsigned d = raw + cslot * 4096 + line0 * 128;
-                // (row r's piece c lies at c ^ (r & 7); r is line0, line0 + 4, ...)
-                const unsigned c0 = mn ? (lane & 7) * 16 : ((lane & 7) ^ line0) * 16;
-                const unsigned c1 = mn ? c0 : c0 ^ 64;
-                if (vec && line_in > 28 && along_in >= 4) {
+                const unsigned d = raw + cslot * 4096;
+                // (row r's piece c lies at c ^ (r & 7))
+                if (vec) {
+                    const unsigned c0 = line0 * 128 + (mn ? (lane & 7) * 16 : ((lane & 7) ^ line0) * 16);
+                    const unsigned c1 = mn ? c0 : c0 ^ 64;  // (of rows 4, 12, ...)
+                    const unsigned bytes = 4 * max(0, min(along_in, 4));
 #pragma unroll
-                    for (int j = 0; j < 8; ++j, s += gap)
-                        cp_async16_part(d + j * 512 + (j & 1 ? c1 : c0), s, 16);
+                    for (int j = 0; j < 8; ++j, s += 4 * ld) {
+                        const bool in = line_in > 4 * j && bytes > 0;
+                        cp_async16_part(d + j * 512 + (j & 1 ? c1 : c0), in ? s : base, in ? bytes : 0);
+                    }
                 } else {
+                    const bool in = along_in > 0;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j, s += gap)
-                        copy4(d + j * 512 + (j & 1 ? c1 : c0), s, line_in > 4 * j ? along_in : 0, vec, base);
+                    for (int j = 0; j < 32; ++j, s += ld) {
+                        const unsigned at = mn ? lane * 4 : ((lane >> 2 ^ (j & 7)) << 4) + (lane & 3) * 4;
+                        const bool is = in && line_in > j;
+                        cp_async4_part(d + j * 128 + at, is ? s : base, is ? 4 : 0);
+                    }
                 }
                 src += step_k;
                 if (mn) line_in -= 32;

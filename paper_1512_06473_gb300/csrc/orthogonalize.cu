@@ -9,6 +9,9 @@
 // instead of B X read X again in the third product's epilogue, 12 us a step of 1000 x 4096.)  X, A and B live as bf16
 // planes that the epilogues write and TMA reads: two in bf16 calls (in one, each step's
 // rounding of X and B would be that of the result), three in fp32 calls.
+// Matrices whose smaller side is 64 or less are done in one launch where that is sooner done
+// (orthogonalize_small.cu).
+#include "ortho_small.cuh"
 #include "train.cuh"
 
 #include <algorithm>
@@ -171,6 +174,9 @@ __global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, P
 struct OrthoPlan {
     int P, p, q;  // planes; smaller and larger side
     GemmPlan gram, poly, apply;
+    // of all steps as products, in SM clocks (2,500 more per product than its plan says: the
+    // launch)
+    double score(int steps) const { return 12000.0 + steps * (gram.score + poly.score + apply.score + 3 * 2500.0); }
 };
 OrthoPlan plan_ortho(int m, int n, int dtype) {
     OrthoPlan o;
@@ -293,13 +299,16 @@ qcnn_status qcnn_orthogonalize(const void *G, long long ldg, int m, int n, int s
     if (m <= 0 || n <= 0 || !dtype_ok(dtype) || steps < 0 || steps > 100 || !(eps >= 0.f) ||
         !matrix_ok(G, ldg, m, n, dtype) || !matrix_ok(out, ldo, m, n, dtype))
         return QCNN_ERR_INVALID_ARG;
+    static const float muon[3] = {3.4445f, -4.7750f, 2.0315f};
+    const float *k = coeffs ? coeffs : muon;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const OrthoPlan o = plan_ortho(m, n, dtype);
     const OrthoSpace s = carve_ortho(o, m, n, workspace);
     const qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;
-    static const float muon[3] = {3.4445f, -4.7750f, 2.0315f};
-    const float *k = coeffs ? coeffs : muon;
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const OrthoSmall small = ortho_small_plan(m, n, steps, o.score(steps));
+    if (small.cluster)
+        return launch_ortho_small(small, G, ldg, m, n, steps, k, eps, out, ldo, dtype == QCNN_BF16, st);
     if (dtype == QCNN_F32)
         return run_ortho(static_cast<const float *>(G), ldg, m, n, steps, k, eps, static_cast<float *>(out), ldo, o, s, st);
     return run_ortho(static_cast<const unsigned short *>(G), ldg, m, n, steps, k, eps,

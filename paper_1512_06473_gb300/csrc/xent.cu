@@ -125,9 +125,13 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float *part, int group
         sums[threadIdx.x >> 5] = sum;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < T / 32; ++i) join(top, sum, tops[i], sums[i]);
-        finish_row(o, blockIdx.x, top, sum, picked);
+    if (threadIdx.x < 32) {
+        top = threadIdx.x * 32 < T ? tops[threadIdx.x] : -INFINITY;
+        sum = threadIdx.x * 32 < T ? sums[threadIdx.x] : 0.f;
+#pragma unroll
+        for (int s = 16; s; s >>= 1)
+            join(top, sum, __shfl_xor_sync(0xffffffffu, top, s), __shfl_xor_sync(0xffffffffu, sum, s));
+        if (threadIdx.x == 0) finish_row(o, blockIdx.x, top, sum, picked);
     }
 }
 
@@ -209,6 +213,13 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
         for (int w = 0; w < 8; ++w) v += red[w][t];
         part[(long long)blockIdx.y * Ct + col] = v;
     }
+}
+
+// Threads of rows_kernel: one per class where there are few rows, a quarter of that (four
+// classes in a go) where the rows fill the SMs.
+int rows_threads(int N, int Ct) {
+    const int want = N <= 2 * num_sms() ? Ct : Ct / 4;
+    return std::min(1024, std::max(128, cdiv(want, 128) * 128));
 }
 
 // fp32: x and dl always as planes; wplanes: the weights too.  bf16: copies of what TMA
@@ -356,7 +367,7 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         }
         if (rc != QCNN_OK) return rc;
         rc = launch_pdl(rows_kernel, dim3(N + (a.grad ? 1 : 0)),
-                        dim3(std::min(1024, std::max(128, cdiv(Ct, 128) * 128))), 0, st,
+                        dim3(rows_threads(N, Ct)), 0, st,
                         static_cast<const float *>(s.part), p.few ? 1 : p.logits.groups, a.bias, s.logits, ro);
     } else {
         g.a = xo;
