@@ -73,6 +73,21 @@ qcnn_status set_operand(const GemmOperand &o, int P, bool gen, int rows, int row
     return QCNN_OK;
 }
 
+// The map of an fp32 A: boxes of 32 terms x 128 rows, or of 32 rows x 32 terms where the rows
+// are contiguous.
+qcnn_status raw_map(const GemmOperand &o, int rows, int k, CUtensorMap *map) {
+    const EncodeTiled enc = encode_tiled();
+    if (!enc) return QCNN_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)(o.mn ? rows : k), (cuuint64_t)(o.mn ? k : rows)};
+    const cuuint64_t strides[1] = {(cuuint64_t)o.ld * 4};
+    const cuuint32_t box[2] = {32, o.mn ? 32u : (cuuint32_t)kMT}, steps[2] = {1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(o.p), dims, strides, box,
+                           steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           o.mn ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? QCNN_OK : cuda_status(cudaErrorInvalidValue);
+}
+
 long long tiles_of(int kind, int m_tiles, int n_tiles, int per) {
     if (kind != GEMM_SYM) return (long long)m_tiles * n_tiles;
     long long t = 0;
@@ -287,6 +302,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
             p.a.src = static_cast<const float *>(s.a.p);
             p.a.ld = s.a.ld;
             p.a.vec = reinterpret_cast<uintptr_t>(s.a.p) % 16 == 0 && s.a.ld % 4 == 0;
+            if (p.a.vec && (rc = raw_map(s.a, s.m, s.k, &p.map_a)) != QCNN_OK) return rc;
         } else if ((rc = set_operand(s.a, P, gen, kMT, s.m, s.k, &p.a, &p.map_a)) != QCNN_OK) {
             return rc;
         }
@@ -319,8 +335,13 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     g.bn = plan.bn;
     g.b_off = a_bytes;  // (multiples of 1024: 128 rows; 64 rows of 128 bytes)
     g.stage = (unsigned)align_up(a_bytes + b_bytes, 1024);
-    const size_t raw = gen ? (size_t)kRawSlots * kGenWarps * 4096 : 0;
-    g.S = (int)std::min<size_t>(gen ? kGenStages : kStagesMax, (kSmemMax - 1024 - raw) / g.stage);
+    const size_t raw_stage = kGenWarps * 4096;
+    g.S = (int)std::min<size_t>(gen ? kGenStages : kStagesMax, (kSmemMax - 1024) / g.stage);
+    if (gen) {  // raw copies: by TMA as many stages as there is room for
+        g.raw = (int)std::min<size_t>(kRawMax, (kSmemMax - 1024 - g.S * (size_t)g.stage) / raw_stage);
+        if (!g.p[0].a.vec) g.raw = kRawSlots;
+    }
+    const size_t raw = g.raw * raw_stage;
     // (three planes: two rings, each with room for a block's planes)
     if (P == 3) g.S &= ~1;
     if (g.S < (gen ? 2 : P == 3 ? 6 : P)) return QCNN_ERR_UNSUPPORTED;

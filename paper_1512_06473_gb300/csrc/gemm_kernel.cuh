@@ -21,13 +21,13 @@
 // lane quarter, 16 columns in turn.
 //
 // GEN: A is fp32 of any stride and alignment (a layer's weights), split on its way, so that
-// a product bound by A's bytes (few rows n) reads them once and writes no planes.  Warps
-// 12-15 copy it (cp.async, kRawSlots - 1 stages ahead: some 64 KB in flight per SM), split
-// it and store the planes to TMEM as the MMAs' A operand: shared memory then carries per
-// stage of 32 terms and 128 columns 32 KB for the copies, 24 KB of B's planes and 48 KB that
-// the twelve MMAs read, 832 clocks of its bandwidth to the 888 of the MMAs.  (With A's
-// planes in shared memory and B split by the same warps it was 1664, and the kernel took
-// 3,500: 115 us for 128 rows of 9216 -> 4096.)
+// a product bound by A's bytes (few rows n) reads them once and writes no planes.  It comes
+// to shared memory by TMA (warp 2), or where its rows are off the 16-byte alignment by
+// cp.async of the warps that split it, 12-15; these store the planes to TMEM as the MMAs' A
+// operand.  Shared memory then carries per stage of 32 terms and 128 columns 32 KB for the
+// copies, 24 KB of B's planes and 48 KB that the twelve MMAs read, 832 clocks of its bandwidth
+// to the 888 of the MMAs.  (With A's planes in shared memory and B split by the same warps it
+// was 1664, and the kernel took 3,500: 115 us for 128 rows of 9216 -> 4096.)
 #pragma once
 
 #include "gemm.cuh"
@@ -43,6 +43,7 @@ constexpr int kStagesMax = 8;
 constexpr int kEpiWarps = 8;
 constexpr int kGenWarps = 4;      // converters
 constexpr int kRawSlots = 5;      // GEN: stages of raw copies, 4 KB per warp each
+constexpr int kRawMax = 10;       // the same by TMA, at most
 constexpr int kGenCols = 48;      // TMEM columns of a stage's A: 3 planes x 32 terms
 constexpr int kGenStages = 4;     // (at most (512 - 2 * 128) / 48)
 constexpr unsigned kPolls = 1u << 22;
@@ -67,6 +68,7 @@ struct ProblemArgs {
 struct GemmArgs {
     ProblemArgs p[2];
     int count, units, bn, S;
+    int raw;                // GEN: stages of raw copies
     int cl;                 // CTAs of a cluster that share a tile's terms (CG 1)
     int groups;             // shares whose sums stay apart (OUT, cl 1)
     int stay;               // three planes: a tile's sum stays in TMEM
@@ -75,6 +77,7 @@ struct GemmArgs {
 
 struct Shared {
     uint64_t full[kStagesMax], empty[kStagesMax], tfull[2], tempty[2], done[2];
+    uint64_t raw_full[kRawMax], raw_empty[kRawMax];  // GEN, copies by TMA
     unsigned tmem;
     int give_up;
 };
@@ -173,6 +176,13 @@ __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap *map, i
             "[%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
             "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar) & 0xFEFFFFFFu)
             : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(unsigned dst, const CUtensorMap *map, int x, int y, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar))
+        : "memory");
 }
 template <int CG>
 __device__ __forceinline__ void mma_ss(unsigned d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
@@ -630,6 +640,11 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             mbar_init(&sh.tempty[i], kEpiWarps * CG);
             mbar_init(&sh.done[i], 1);
         }
+        if constexpr (GEN)
+            for (int i = 0; i < g.raw; ++i) {
+                mbar_init(&sh.raw_full[i], 1);
+                mbar_init(&sh.raw_empty[i], kGenWarps);
+            }
         sh.give_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async_smem();
@@ -787,6 +802,42 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             mbar_wait_bounded(&sh.done[ring], 0, kPolls);
         }
         __syncwarp();
+    } else if (GEN && warp == 2) {
+        // ------------------------------------------------- raw copies by TMA
+        // (no wait for the kernel before: the weights are the caller's, complete before the
+        // first kernel of this call)
+        const ProblemArgs &p = g.p[0];
+        if (p.a.vec && elect_one()) {
+            int slot = 0;
+            unsigned par = 0, issued = 0;
+            bool ok = true;
+            const bool mn = p.a.mn;
+            for (int r = 0, u = first_unit; u < g.units && ok; u = unit_at(g, ++r, first_unit, step)) {
+                const Tile t = tile_of<KIND, CG>(g, u, share);
+                const int m0 = t.mt * kMT;
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!(ok = wait_one(sh, &sh.raw_empty[slot], par ^ 1))) break;
+                    uint64_t *const full = &sh.raw_full[slot];
+                    arrive_expect(full, kGenWarps * 4096);
+                    const unsigned d = smem_addr(smem) + g.S * g.stage + slot * (kGenWarps * 4096);
+                    if (mn) {
+#pragma unroll
+                        for (int i = 0; i < kGenWarps; ++i)
+                            tma_load_2d(d + i * 4096, &p.map_a, m0 + i * 32, kb * BK, full);
+                    } else {
+                        tma_load_2d(d, &p.map_a, kb * BK, m0, full);
+                    }
+                    ++issued;
+                    if (++slot == g.raw) {
+                        slot = 0;
+                        par ^= 1;
+                    }
+                }
+            }
+            for (unsigned i = issued > (unsigned)g.raw ? issued - g.raw : 0; i < issued; ++i)
+                mbar_wait_bounded(&sh.raw_full[i % g.raw], i / g.raw & 1, kPolls);
+        }
+        __syncwarp();
     } else if (warp >= 4 && warp < 4 + kEpiWarps) {
         // ---------------------------------------------------- drain, epilogue
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -929,57 +980,44 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         }
     } else if (GEN && warp >= 12) {
         // ------------------------------------------ copy, split, store planes
-        // A warp has 32 rows (its TMEM lanes) x 32 terms of every stage, and copies them
-        // itself: no barrier between copying and splitting.  Rows of k: [32][32] floats, the
-        // 16-byte pieces of a row permuted so that eight neighbouring rows read from all
-        // banks; rows of m: [32 terms][32].  Both are 32 lines of 128 bytes: eight copies of 16
-        // bytes per lane, four lines at a time, or, where rows are off the 16-byte alignment, 32
-        // of 4, a line at a time.
+        // A warp has 32 rows (its TMEM lanes) x 32 terms of every stage.  Rows of k: [32][32]
+        // floats, the 16-byte pieces of a row permuted (TMA's 128-byte swizzle) so that eight
+        // neighbouring rows read from all banks; rows of m: [32 terms][32].  Where TMA cannot
+        // read the rows, the warp copies its own 32 lines of 128 bytes, element by element (a
+        // lane each: neighbours), so that no barrier lies between copying and splitting.
         const int quarter = warp & 3;
         const ProblemArgs &p = g.p[0];
         const bool mn = p.a.mn, vec = p.a.vec;
         const float *const base = p.a.src;
         const long long ld = p.a.ld, step_k = mn ? 32 * ld : 32;
-        const unsigned raw = smem_addr(smem) + g.S * g.stage + (warp - 12) * (kRawSlots * 4096);
-        // this lane's first line (row, or term) and place along it
-        const int line0 = vec ? lane >> 3 : 0, along = vec ? (lane & 7) * 4 : lane;
+        const int slots = vec ? g.raw : kRawSlots;
+        // (TMA: a stage is the four warps' parts one after another)
+        const unsigned raw = smem_addr(smem) + g.S * g.stage + (warp - 12) * (vec ? 4096 : kRawSlots * 4096);
+        const unsigned raw_step = vec ? kGenWarps * 4096 : 4096;
         const float *src = base;
         int cu = first_unit, cr = 0, ckb = 0, ckb1 = 0, cslot = 0;
-        int line_in = 0, along_in = 0;  // lines and elements along them that exist from here on
+        int line_in = 0, along_in = 0;  // lines, and elements of a line from this lane's, that exist
         auto open_tile = [&]() {
             const Tile t = tile_of<KIND, CG>(g, cu, share);
             ckb = t.kb0;
             ckb1 = t.kb1;
-            const int row = t.mt * kMT + quarter * 32 + (mn ? along : line0);
-            const int k = t.kb0 * BK + (mn ? line0 : along);
+            const int row = t.mt * kMT + quarter * 32 + (mn ? lane : 0), k = t.kb0 * BK + (mn ? 0 : lane);
             line_in = mn ? p.k - k : p.m - row;
             along_in = mn ? p.m - row : p.k - k;
             src = base + (mn ? (long long)k * ld + row : (long long)row * ld + k);
         };
-        if (cu < g.units) open_tile();
-        // (the weights are the caller's, complete before the first kernel of this call: no wait)
+        // (the weights are the caller's: no wait, as above)
         auto copy_next = [&]() {
+            if (vec) return;
             if (cu < g.units) {
                 const float *s = src;
-                const unsigned d = raw + cslot * 4096;
-                // (row r's piece c lies at c ^ (r & 7))
-                if (vec) {
-                    const unsigned c0 = line0 * 128 + (mn ? (lane & 7) * 16 : ((lane & 7) ^ line0) * 16);
-                    const unsigned c1 = mn ? c0 : c0 ^ 64;  // (of rows 4, 12, ...)
-                    const unsigned bytes = 4 * max(0, min(along_in, 4));
+                const unsigned d = raw + cslot * raw_step;
+                const bool in = along_in > 0;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j, s += 4 * ld) {
-                        const bool in = line_in > 4 * j && bytes > 0;
-                        cp_async16_part(d + j * 512 + (j & 1 ? c1 : c0), in ? s : base, in ? bytes : 0);
-                    }
-                } else {
-                    const bool in = along_in > 0;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j, s += ld) {
-                        const unsigned at = mn ? lane * 4 : ((lane >> 2 ^ (j & 7)) << 4) + (lane & 3) * 4;
-                        const bool is = in && line_in > j;
-                        cp_async4_part(d + j * 128 + at, is ? s : base, is ? 4 : 0);
-                    }
+                for (int j = 0; j < 32; ++j, s += ld) {
+                    const unsigned at = mn ? lane * 4 : ((lane >> 2 ^ (j & 7)) << 4) + (lane & 3) * 4;
+                    const bool is = in && line_in > j;
+                    cp_async4_part(d + j * 128 + at, is ? s : base, is ? 4 : 0);
                 }
                 src += step_k;
                 if (mn) line_in -= 32;
@@ -992,18 +1030,25 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
             }
             cp_async_commit();
         };
-        for (int i = 0; i < kRawSlots - 1; ++i) copy_next();
+        if (!vec) {
+            if (cu < g.units) open_tile();
+            for (int i = 0; i < kRawSlots - 1; ++i) copy_next();
+        }
         const unsigned a_dst = tmem + 2 * ACC + ((unsigned)(quarter * 32) << 16);
         const int S = g.S / RINGS;
         int slot = 0, slot2 = 0, rslot = 0;  // (stages: as the TMA's)
-        unsigned par = 0, par2 = 0, ring = 0;
+        unsigned par = 0, par2 = 0, ring = 0, rpar = 0;
         bool ok = true;
         for (int r = 0, u = first_unit; u < g.units && ok; u = unit_at(g, ++r, first_unit, step)) {
             const Tile t = tile_of<KIND, CG>(g, u, share);
             for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                cp_async_wait<kRawSlots - 2>();
-                __syncwarp();
-                const unsigned r = raw + rslot * 4096;
+                if (vec) {
+                    if (!(ok = wait_warp(sh, &sh.raw_full[rslot], rpar))) break;
+                } else {
+                    cp_async_wait<kRawSlots - 2>();
+                    __syncwarp();
+                }
+                const unsigned r = raw + rslot * raw_step;
                 float v[32];
                 if (mn) {
 #pragma unroll
@@ -1031,6 +1076,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     tmem_st8(d + 8 * h + 32, w2);
                 }
                 __syncwarp();  // (all have read: the slot may be copied to)
+                if (vec && lane == 0) arrive(&sh.raw_empty[rslot]);
                 copy_next();
                 asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
                 tc_fence_before_sync();
@@ -1045,7 +1091,10 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                     swap(slot, slot2);
                     swap(par, par2);
                 }
-                if (++rslot == kRawSlots) rslot = 0;
+                if (++rslot == slots) {
+                    rslot = 0;
+                    rpar ^= 1;
+                }
             }
         }
         cp_async_wait<0>();
