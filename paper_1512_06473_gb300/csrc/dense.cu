@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(256, NB == 8 ? 2 : 1) few_rows_kernel(FewRows 
     };
     if (e.pre) put(e.pre, e.ldp, v);
     v = act_apply(v, e.act);
-    if (e.add) v += load_as(e.add, e.add_type, (long long)n * e.lda + m, 0);
+    if (e.add) v += load_as(e.add, e.add_type, (long long)n * e.lda + m);
     put(e.out, e.ldo, v);
 }
 

@@ -96,9 +96,8 @@ long long tiles_of(int kind, int m_tiles, int n_tiles, int per) {
 }
 
 // Whether a matrix of two-byte elements can go in pairs of neighbours along m.
-bool pairs(const void *p, int type, long long ld, long long plane, int m) {
-    return type != GEMM_T_F32 && p && reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 2 == 0 && plane % 2 == 0 &&
-           (m % 2 == 0 || type >= GEMM_T_PLANES2);  // (rows of planes have room for one more)
+bool pairs(const void *p, int type, long long ld, int m) {
+    return type != GEMM_T_F32 && p && reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 2 == 0 && m % 2 == 0;
 }
 
 GemmLaunch launcher(const GemmPlan &p) {
@@ -320,9 +319,9 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
         p.kb_per_split = plan.splits > 1 || plan.groups > 1 ? plan.kb_per_split : p.kblocks;
         p.group = std::max(1, 16 / cg);
         p.e = s.e;
-        p.e.pair = (pairs(s.e.out, s.e.out_type, s.e.ldo, s.e.out_plane, s.m) ? 1 : 0) |
-                   (pairs(s.e.pre, s.e.out_type, s.e.ldp, 0, s.m) ? 2 : 0) |
-                   (pairs(s.e.add, s.e.add_type, s.e.lda, s.e.add_plane, s.m) ? 4 : 0);
+        p.e.pair = (pairs(s.e.out, s.e.out_type, s.e.ldo, s.m) ? 1 : 0) |
+                   (pairs(s.e.pre, s.e.out_type, s.e.ldp, s.m) ? 2 : 0) |
+                   (pairs(s.e.add, s.e.add_type, s.e.lda, s.m) ? 4 : 0);
         const long long tiles = tiles_of(plan.kind, p.m_tiles, p.n_tiles, plan.bn / (kMT * cg));
         if (tiles * plan.groups > (1 << 27)) return QCNN_ERR_UNSUPPORTED;
         p.units = (int)tiles;  // (of a group)
@@ -338,8 +337,8 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     const size_t raw_stage = kGenWarps * 4096;
     g.S = (int)std::min<size_t>(gen ? kGenStages : kStagesMax, (kSmemMax - 1024) / g.stage);
     if (gen) {  // raw copies: by TMA as many stages as there is room for
-        g.raw = (int)std::min<size_t>(kRawMax, (kSmemMax - 1024 - g.S * (size_t)g.stage) / raw_stage);
-        if (!g.p[0].a.vec) g.raw = kRawSlots;
+        g.raw = (int)std::min<size_t>(kRawMax, (kSmemMax - 1024 - g.S * (size_t)g.stage) / raw_stage) & ~1;
+        if (!g.p[0].a.vec) g.raw = 2 * kRawSlots;
     }
     const size_t raw = g.raw * raw_stage;
     // (three planes: two rings, each with room for a block's planes)

@@ -24,28 +24,29 @@ struct GemmOperand {
     int mn = 0;
 };
 
-enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1, GEMM_T_PLANES2 = 2, GEMM_T_PLANES3 = 3 };
+enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1 };
 
 // What becomes of a sum.  OUT: v = alpha * sum + bias[m] (alpha: *alpha_ptr where set); pre =
-// v; v = act(v); v += beta * add[n][m]; out[n][m] = v.  PLANES: v = alpha * sum + beta * add,
+// v; v = act(v); v += beta * add[n][m]; out[n][m] = v (products of three planes: all fp32).  PLANES: v = alpha * sum + beta * add,
 // + diagonal where n == m; out and add are planes of the product's number, whose matrices
 // have room for whole tiles (rows and columns up to the next multiple of 256).  SYM: PLANES
 // of a symmetric product (A and B the same matrix): only m >= n is computed, and stored at
 // both places.  STATS: m are rows, n classes: the maximum and the sum of exp over a tile's
 // classes of v = sum + bias[n], and the value at the row's target.  DLOGITS: m are classes,
-// n rows: out = g_n (exp(v - lse_n) - [target_n == m]).
+// n rows: out = g_n (exp(v - lse_n) - [target_n == m]), in planes of the product's number whose
+// rows have room for one more.
 struct GemmEpi {
     float alpha = 1.f, beta = 0.f, diagonal = 0.f;
     const float *alpha_ptr = nullptr;  // in device memory
     const float *bias = nullptr;
     void *out = nullptr;
     long long ldo = 0, out_plane = 0;
-    int out_type = GEMM_T_F32;
+    int out_type = GEMM_T_F32;  // (OUT)
     void *pre = nullptr;  // same type as out
     long long ldp = 0;
     const void *add = nullptr;
     long long lda = 0, add_plane = 0;
-    int add_type = GEMM_T_F32;
+    int add_type = GEMM_T_F32;  // (OUT)
     int act = 0;
     int pair = 0;  // (launch_gemm) bits: out, pre, add go in pairs of elements
     // STATS, DLOGITS
@@ -161,16 +162,9 @@ __device__ __forceinline__ unsigned short float_to_bf16(float v) {
     return (unsigned short)(pack_bf16x2(v, 0.f) & 0xffffu);
 }
 // One value of a matrix of `type`, element offset o.
-__device__ __forceinline__ float load_as(const void *p, int type, long long o, long long plane) {
-    if (type == GEMM_T_F32) return static_cast<const float *>(p)[o];
-    const unsigned short *s = static_cast<const unsigned short *>(p) + o;
-    float v = bf16_to_float(s[0]);
-    if (type >= GEMM_T_PLANES2) {
-        float w = bf16_to_float(s[plane]);
-        if (type == GEMM_T_PLANES3) w += bf16_to_float(s[2 * plane]);
-        v += w;
-    }
-    return v;
+__device__ __forceinline__ float load_as(const void *p, int type, long long o) {
+    return type == GEMM_T_F32 ? static_cast<const float *>(p)[o]
+                              : bf16_to_float(static_cast<const unsigned short *>(p)[o]);
 }
 
 }  // namespace qcnn

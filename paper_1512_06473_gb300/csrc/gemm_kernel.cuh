@@ -41,8 +41,9 @@ constexpr int kMT = 128;          // rows of a CTA's tile
 constexpr int kAccCols = 256;     // TMEM columns of an accumulator, of two (GEN: 128)
 constexpr int kStagesMax = 8;
 constexpr int kEpiWarps = 8;
-constexpr int kGenWarps = 4;      // converters
-constexpr int kRawSlots = 5;      // GEN: stages of raw copies, 4 KB per warp each
+constexpr int kGenWarps = 4;      // that split a block's A
+constexpr int kGenThreads = 640;
+constexpr int kRawSlots = 3;      // GEN: blocks of raw copies, 4 KB per warp each
 constexpr int kRawMax = 10;       // the same by TMA, at most
 constexpr int kGenCols = 48;      // TMEM columns of a stage's A: 3 planes x 32 terms
 constexpr int kGenStages = 4;     // (at most (512 - 2 * 128) / 48)
@@ -325,10 +326,12 @@ __device__ __forceinline__ void store_plane(unsigned short *out, long long ld, b
         }
     }
 }
-template <bool FULL>
-__device__ __forceinline__ void store16(void *out, int type, long long ld, long long plane, bool pair, int m_end,
-                                        int m, int n0, int left, const float (&v)[16]) {
-    if (type == GEMM_T_F32) {
+// fp32 or bf16.  (Sums of three planes go to fp32 alone, F32: what a tile's epilogue has in
+// instructions it fetches once, and waits for.)
+template <bool F32, bool FULL>
+__device__ __forceinline__ void store16(void *out, int type, long long ld, bool pair, int m_end, int m, int n0,
+                                        int left, const float (&v)[16]) {
+    if (F32 || type == GEMM_T_F32) {
         const bool in = m < m_end;
         float *p = static_cast<float *>(out) + (long long)n0 * ld + m;
 #pragma unroll
@@ -336,22 +339,12 @@ __device__ __forceinline__ void store16(void *out, int type, long long ld, long 
             if (FULL || (in && i < left)) *p = v[i];
         return;
     }
-    unsigned short *p = static_cast<unsigned short *>(out);
-    unsigned w0[8], w1[8], w2[8];
-    if (type == GEMM_T_BF16) {
+    if constexpr (!F32) {
+        unsigned w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w0[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    } else if (type == GEMM_T_PLANES2) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) planes2(v[2 * i], v[2 * i + 1], w0[i], w1[i]);
-        store_plane<FULL>(p + plane, ld, pair, m_end, m, n0, left, w1);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) planes3(v[2 * i], v[2 * i + 1], w0[i], w1[i], w2[i]);
-        store_plane<FULL>(p + plane, ld, pair, m_end, m, n0, left, w1);
-        store_plane<FULL>(p + 2 * plane, ld, pair, m_end, m, n0, left, w2);
+        for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        store_plane<FULL>(static_cast<unsigned short *>(out), ld, pair, m_end, m, n0, left, w);
     }
-    store_plane<FULL>(p, ld, pair, m_end, m, n0, left, w0);
 }
 
 // 16 columns of a lane of a matrix, on their way: loaded by fetch, values by take (a chunk
@@ -372,12 +365,12 @@ __device__ __forceinline__ void fetch_pairs(Chunk16 &c, const unsigned short *sr
         if (FULL || (in && 2 * i < left)) c.w[8 * J + i] = *reinterpret_cast<const unsigned *>(p);
     }
 }
-template <bool FULL>
-__device__ __forceinline__ void fetch16(Chunk16 &c, const void *src, int type, long long ld, long long plane,
-                                        bool pair, int m_end, int m, int n0, int left) {
+template <bool F32, bool FULL>
+__device__ __forceinline__ void fetch16(Chunk16 &c, const void *src, int type, long long ld, bool pair, int m_end,
+                                        int m, int n0, int left) {
     const bool in = m < m_end;
     const unsigned short *p = static_cast<const unsigned short *>(src);
-    if (type == GEMM_T_F32) {
+    if (F32 || type == GEMM_T_F32) {
         const float *f = static_cast<const float *>(src) + (long long)n0 * ld + m;
 #pragma unroll
         for (int i = 0; i < 16; ++i, f += ld) {
@@ -393,38 +386,36 @@ __device__ __forceinline__ void fetch16(Chunk16 &c, const void *src, int type, l
         }
     } else {
         fetch_pairs<0, FULL>(c, p, ld, m_end, m, n0, left);
-        if (type >= GEMM_T_PLANES2) fetch_pairs<1, FULL>(c, p + plane, ld, m_end, m, n0, left);
-        if (type == GEMM_T_PLANES3) fetch_pairs<2, FULL>(c, p + 2 * plane, ld, m_end, m, n0, left);
     }
 }
-// v += scale * what was fetched.
+// v += scale * what was fetched: P planes in pairs (one: bf16).
+template <int P>
+__device__ __forceinline__ void take_pairs(const Chunk16 &c, bool odd, float scale, float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float lo = 0.f, hi = 0.f;
+#pragma unroll
+        for (int j = P - 1; j >= 0; --j) {
+            const unsigned x = exchange(c.w[8 * j + i], odd);
+            lo += __uint_as_float(x << 16);
+            hi += __uint_as_float(x & 0xffff0000u);
+        }
+        v[2 * i] = fmaf(scale, lo, v[2 * i]);
+        v[2 * i + 1] = fmaf(scale, hi, v[2 * i + 1]);
+    }
+}
+// fp32 or bf16.
+template <bool F32>
 __device__ __forceinline__ void take16(const Chunk16 &c, int type, bool pair, bool odd, float scale,
                                        float (&v)[16]) {
-    if (type == GEMM_T_F32) {
+    if (F32 || type == GEMM_T_F32) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = fmaf(scale, __uint_as_float(c.w[i]), v[i]);
     } else if (!pair) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = fmaf(scale, __uint_as_float(c.w[i] << 16), v[i]);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const unsigned x = exchange(c.w[i], odd);
-            float lo = __uint_as_float(x << 16), hi = __uint_as_float(x & 0xffff0000u);
-            if (type >= GEMM_T_PLANES2) {
-                const unsigned y = exchange(c.w[8 + i], odd);
-                float lo1 = __uint_as_float(y << 16), hi1 = __uint_as_float(y & 0xffff0000u);
-                if (type == GEMM_T_PLANES3) {
-                    const unsigned z = exchange(c.w[16 + i], odd);
-                    lo1 += __uint_as_float(z << 16);
-                    hi1 += __uint_as_float(z & 0xffff0000u);
-                }
-                lo += lo1;
-                hi += hi1;
-            }
-            v[2 * i] = fmaf(scale, lo, v[2 * i]);
-            v[2 * i + 1] = fmaf(scale, hi, v[2 * i + 1]);
-        }
+        take_pairs<1>(c, odd, scale, v);
     }
 }
 __device__ __forceinline__ void act16(float (&v)[16], int act) {
@@ -442,18 +433,29 @@ __device__ __forceinline__ void act16(float (&v)[16], int act) {
 
 // OUT: sums v of lane m, columns n0 .. n0 + left - 1; c: what add has there, which next() then
 // fetches for the columns that follow.  The whole warp calls it; rows m up to m_end exist.
-template <bool FULL, typename F>
+template <bool F32, bool FULL, typename F>
 __device__ __forceinline__ void finish_out(const GemmEpi &e, int m_end, int m, int n0, int left, float alpha,
                                            float bias, float (&v)[16], const Chunk16 &c, F &&next) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = fmaf(alpha, v[i], bias);
-    if (e.pre) store16<FULL>(e.pre, e.out_type, e.ldp, 0, e.pair & 2, m_end, m, n0, left, v);
+    if (e.pre) store16<F32, FULL>(e.pre, e.out_type, e.ldp, e.pair & 2, m_end, m, n0, left, v);
     act16(v, e.act);
     if (e.add) {
-        take16(c, e.add_type, e.pair & 4, m & 1, e.beta, v);
+        take16<F32>(c, e.add_type, e.pair & 4, m & 1, e.beta, v);
         next();
     }
-    store16<FULL>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
+    store16<F32, FULL>(e.out, e.out_type, e.ldo, e.pair & 1, m_end, m, n0, left, v);
+}
+
+// 16 columns of a lane in P planes.
+template <int P>
+__device__ __forceinline__ void split16(const float (&v)[16], unsigned (&w)[P][8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (P == 3) planes3(v[2 * i], v[2 * i + 1], w[0][i], w[1][i], w[2][i]);
+        else if constexpr (P == 2) planes2(v[2 * i], v[2 * i + 1], w[0][i], w[1][i]);
+        else w[0][i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    }
 }
 
 // PLANES and SYM: v = alpha * sum + beta * add (+ diagonal) to P planes whose matrix has room
@@ -465,18 +467,14 @@ __device__ __forceinline__ void finish_planes(const GemmEpi &e, bool mirror, int
                                               const Chunk16 &c) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] *= e.alpha;
-    if (e.add) take16(c, P, true, m & 1, e.beta, v);
+    if (e.add) take_pairs<P>(c, m & 1, e.beta, v);
     if ((unsigned)(m - n0) < 16u) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (m == n0 + i) v[i] += e.diagonal;
     }
     unsigned w[P][8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (P == 3) planes3(v[2 * i], v[2 * i + 1], w[0][i], w[1][i], w[2][i]);
-        else planes2(v[2 * i], v[2 * i + 1], w[0][i], w[1][i]);
-    }
+    split16<P>(v, w);
     unsigned short *p = static_cast<unsigned short *>(e.out);
 #pragma unroll
     for (int j = 0; j < P; ++j, p += e.out_plane) {
@@ -537,7 +535,9 @@ __device__ __forceinline__ void stats16(RunningSum &s, int n0, int target, float
     s.top = top;
 }
 
-// Gradient of a class (lane m) for 16 rows; rows: theirs, without a class past the last.
+// Gradient of a class (lane m) for 16 rows, in P planes; rows: theirs, without a class past
+// the last.
+template <int P>
 __device__ __forceinline__ void dlogits16(const GemmEpi &e, bool full, int m_end, int m, int n0, int left, float bias,
                                           const float4 *rows, float &col, float (&v)[16]) {
     const int c = e.class0 + m;
@@ -551,8 +551,14 @@ __device__ __forceinline__ void dlogits16(const GemmEpi &e, bool full, int m_end
         v[i] = target >= 0 ? r.y * p : 0.f;
         col += v[i];
     }
-    if (full) store16<true>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
-    else store16<false>(e.out, e.out_type, e.ldo, e.out_plane, e.pair & 1, m_end, m, n0, left, v);
+    unsigned w[P][8];
+    split16<P>(v, w);
+    unsigned short *p = static_cast<unsigned short *>(e.out);
+#pragma unroll
+    for (int j = 0; j < P; ++j, p += e.out_plane) {
+        if (full) store_plane<true>(p, e.ldo, true, m_end, m, n0, left, w[j]);
+        else store_plane<false>(p, e.ldo, true, m_end, m, n0, left, w[j]);
+    }
 }
 
 // ---------------------------------------------------------------------- GEN
@@ -577,6 +583,13 @@ __device__ __forceinline__ void tmem_st8(unsigned taddr, const unsigned (&v)[8])
         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
         : "memory");
 }
+// GEN: a warpgroup's registers per thread.  96 at launch (640 threads); 80 for TMA and MMA, 112
+// for each of the two that drain and 88 for each of the two that split: 480, which is 5 x 96.
+template <int N, bool MORE>
+__device__ __forceinline__ void set_registers() {
+    if constexpr (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(N));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(N));
+}
 // What add has at 16 columns of a lane.
 template <int KIND, int P>
 __device__ __forceinline__ void fetch_add(Chunk16 &c, const ProblemArgs &p, int m, int n0, bool is, bool rows_full) {
@@ -591,15 +604,15 @@ __device__ __forceinline__ void fetch_add(Chunk16 &c, const ProblemArgs &p, int 
         const int left = p.n - n0;
         if (left <= 0) return;
         if (rows_full && left >= 16)
-            fetch16<true>(c, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0, left);
+            fetch16<P == 3, true>(c, e.add, e.add_type, e.lda, e.pair & 4, p.m, m, n0, left);
         else
-            fetch16<false>(c, e.add, e.add_type, e.lda, e.add_plane, e.pair & 4, p.m, m, n0, left);
+            fetch16<P == 3, false>(c, e.add, e.add_type, e.lda, e.pair & 4, p.m, m, n0, left);
     }
 }
 
 // ------------------------------------------------------------------- kernel
 template <int P, int KIND, int CG, bool GEN>
-__global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
+__global__ void __launch_bounds__(GEN ? kGenThreads : 384, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
     constexpr int BK = GEN ? 32 : 64, KS = BK / 16;
     constexpr int PL = GEN ? 1 : P;  // stages (planes) of a block of terms
     constexpr bool DRAIN = P == 3;   // a block's sum at a time
@@ -658,6 +671,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
     // (each role waits for the kernel before it where it first needs memory: what it works
     // out before that, a first tile and its operands' maps, took 2,000 clocks)
 
+    if (GEN && warp < 4) set_registers<80, false>();
     if (warp == 0) {
         // --------------------------------------------------------------- TMA
         if (elect_one()) {
@@ -808,18 +822,21 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
         // first kernel of this call)
         const ProblemArgs &p = g.p[0];
         if (p.a.vec && elect_one()) {
+            // (two rings, as the stages: each has one group of warps that reads it)
+            const int R = g.raw / 2;
             int slot = 0;
-            unsigned par = 0, issued = 0;
+            unsigned par = 0, ring = 0, issued = 0;
             bool ok = true;
             const bool mn = p.a.mn;
             for (int r = 0, u = first_unit; u < g.units && ok; u = unit_at(g, ++r, first_unit, step)) {
                 const Tile t = tile_of<KIND, CG>(g, u, share);
                 const int m0 = t.mt * kMT;
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (!(ok = wait_one(sh, &sh.raw_empty[slot], par ^ 1))) break;
-                    uint64_t *const full = &sh.raw_full[slot];
+                    const int at = (int)ring * R + slot;
+                    if (!(ok = wait_one(sh, &sh.raw_empty[at], par ^ 1))) break;
+                    uint64_t *const full = &sh.raw_full[at];
                     arrive_expect(full, kGenWarps * 4096);
-                    const unsigned d = smem_addr(smem) + g.S * g.stage + slot * (kGenWarps * 4096);
+                    const unsigned d = smem_addr(smem) + g.S * g.stage + at * (kGenWarps * 4096);
                     if (mn) {
 #pragma unroll
                         for (int i = 0; i < kGenWarps; ++i)
@@ -828,18 +845,20 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                         tma_load_2d(d, &p.map_a, kb * BK, m0, full);
                     }
                     ++issued;
-                    if (++slot == g.raw) {
+                    ring ^= 1;
+                    if (ring == 0 && ++slot == R) {
                         slot = 0;
                         par ^= 1;
                     }
                 }
             }
             for (unsigned i = issued > (unsigned)g.raw ? issued - g.raw : 0; i < issued; ++i)
-                mbar_wait_bounded(&sh.raw_full[i % g.raw], i / g.raw & 1, kPolls);
+                mbar_wait_bounded(&sh.raw_full[(i & 1) * R + (i >> 1) % R], (i >> 1) / R & 1, kPolls);
         }
         __syncwarp();
     } else if (warp >= 4 && warp < 4 + kEpiWarps) {
         // ---------------------------------------------------- drain, epilogue
+        if constexpr (GEN) set_registers<112, true>();
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const unsigned tl = tmem + ((unsigned)(quarter * 32) << 16);
         const int chunks = g.bn / 16;  // this warp's: half, half + 2, ...
@@ -951,7 +970,7 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 if constexpr (KIND == GEMM_STATS) {
                     stats16(run, n, target, e.target_logit + m, cols, v);
                 } else if constexpr (KIND == GEMM_DLOGITS) {
-                    dlogits16(e, rows_full && left >= 16, p.m, m, n, left, bias, cols, col, v);
+                    dlogits16<P>(e, rows_full && left >= 16, p.m, m, n, left, bias, cols, col, v);
                 } else if (g.cl > 1) {  // to the cluster
                     const unsigned d = stash + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
 #pragma unroll
@@ -965,9 +984,9 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 } else if (left > 0) {
                     const int row = n + t.group * p.n;  // (each group's outputs)
                     if (rows_full && left >= 16)
-                        finish_out<true>(e, p.m, m, row, left, alpha, bias, v, add, [&] { fetch(c + 2); });
+                        finish_out<P == 3, true>(e, p.m, m, row, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                     else
-                        finish_out<false>(e, p.m, m, row, left, alpha, bias, v, add, [&] { fetch(c + 2); });
+                        finish_out<P == 3, false>(e, p.m, m, row, left, alpha, bias, v, add, [&] { fetch(c + 2); });
                 }
             }
             release(buf);
@@ -978,136 +997,14 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                 if (in) e.col_part[(long long)(t.nt * 2 + half) * e.ld_col + m] = col;
             }
         }
-    } else if (GEN && warp >= 12) {
-        // ------------------------------------------ copy, split, store planes
-        // A warp has 32 rows (its TMEM lanes) x 32 terms of every stage.  Rows of k: [32][32]
-        // floats, the 16-byte pieces of a row permuted (TMA's 128-byte swizzle) so that eight
-        // neighbouring rows read from all banks; rows of m: [32 terms][32].  Where TMA cannot
-        // read the rows, the warp copies its own 32 lines of 128 bytes, element by element (a
-        // lane each: neighbours), so that no barrier lies between copying and splitting.
-        const int quarter = warp & 3;
-        const ProblemArgs &p = g.p[0];
-        const bool mn = p.a.mn, vec = p.a.vec;
-        const float *const base = p.a.src;
-        const long long ld = p.a.ld, step_k = mn ? 32 * ld : 32;
-        const int slots = vec ? g.raw : kRawSlots;
-        // (TMA: a stage is the four warps' parts one after another)
-        const unsigned raw = smem_addr(smem) + g.S * g.stage + (warp - 12) * (vec ? 4096 : kRawSlots * 4096);
-        const unsigned raw_step = vec ? kGenWarps * 4096 : 4096;
-        const float *src = base;
-        int cu = first_unit, cr = 0, ckb = 0, ckb1 = 0, cslot = 0;
-        int line_in = 0, along_in = 0;  // lines, and elements of a line from this lane's, that exist
-        auto open_tile = [&]() {
-            const Tile t = tile_of<KIND, CG>(g, cu, share);
-            ckb = t.kb0;
-            ckb1 = t.kb1;
-            const int row = t.mt * kMT + quarter * 32 + (mn ? lane : 0), k = t.kb0 * BK + (mn ? 0 : lane);
-            line_in = mn ? p.k - k : p.m - row;
-            along_in = mn ? p.m - row : p.k - k;
-            src = base + (mn ? (long long)k * ld + row : (long long)row * ld + k);
-        };
-        // (the weights are the caller's: no wait, as above)
-        auto copy_next = [&]() {
-            if (vec) return;
-            if (cu < g.units) {
-                const float *s = src;
-                const unsigned d = raw + cslot * raw_step;
-                const bool in = along_in > 0;
-#pragma unroll
-                for (int j = 0; j < 32; ++j, s += ld) {
-                    const unsigned at = mn ? lane * 4 : ((lane >> 2 ^ (j & 7)) << 4) + (lane & 3) * 4;
-                    const bool is = in && line_in > j;
-                    cp_async4_part(d + j * 128 + at, is ? s : base, is ? 4 : 0);
-                }
-                src += step_k;
-                if (mn) line_in -= 32;
-                else along_in -= 32;
-                if (++ckb == ckb1) {
-                    cu = unit_at(g, ++cr, first_unit, step);
-                    if (cu < g.units) open_tile();
-                }
-                if (++cslot == kRawSlots) cslot = 0;
-            }
-            cp_async_commit();
-        };
-        if (!vec) {
-            if (cu < g.units) open_tile();
-            for (int i = 0; i < kRawSlots - 1; ++i) copy_next();
-        }
-        const unsigned a_dst = tmem + 2 * ACC + ((unsigned)(quarter * 32) << 16);
-        const int S = g.S / RINGS;
-        int slot = 0, slot2 = 0, rslot = 0;  // (stages: as the TMA's)
-        unsigned par = 0, par2 = 0, ring = 0, rpar = 0;
-        bool ok = true;
-        for (int r = 0, u = first_unit; u < g.units && ok; u = unit_at(g, ++r, first_unit, step)) {
-            const Tile t = tile_of<KIND, CG>(g, u, share);
-            for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                if (vec) {
-                    if (!(ok = wait_warp(sh, &sh.raw_full[rslot], rpar))) break;
-                } else {
-                    cp_async_wait<kRawSlots - 2>();
-                    __syncwarp();
-                }
-                const unsigned r = raw + rslot * raw_step;
-                float v[32];
-                if (mn) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(r + i * 128 + lane * 4));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n"
-                                     : "=f"(v[4 * i]), "=f"(v[4 * i + 1]), "=f"(v[4 * i + 2]), "=f"(v[4 * i + 3])
-                                     : "r"(r + lane * 128 + ((i ^ (lane & 7)) << 4)));
-                }
-                const int at = (int)ring * S + slot;
-                if (!(ok = wait_warp(sh, &sh.empty[at], par ^ 1))) break;
-                tc_fence_after_sync();
-                const unsigned d = a_dst + at * kGenCols;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    unsigned w0[8], w1[8], w2[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        planes3(v[16 * h + 2 * i], v[16 * h + 2 * i + 1], w0[i], w1[i], w2[i]);
-                    tmem_st8(d + 8 * h, w0);
-                    tmem_st8(d + 8 * h + 16, w1);
-                    tmem_st8(d + 8 * h + 32, w2);
-                }
-                __syncwarp();  // (all have read: the slot may be copied to)
-                if (vec && lane == 0) arrive(&sh.raw_empty[rslot]);
-                copy_next();
-                asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
-                tc_fence_before_sync();
+        if constexpr (CG == 1 && !COLUMNS) {
+            if (g.cl > 1) {
+                // The sums of a tile's shares meet in shared memory, where each CTA has left its
+                // own: each adds up a part of the columns, in the order of the shares, and does
+                // their epilogue.  (Here, where these warps have their registers: for all warps
+                // behind the roles the loads of four shares did not fit, 1.5 us more.)
                 __syncwarp();
-                if (lane == 0) arrive(&sh.full[at]);
-                if (++slot == S) {
-                    slot = 0;
-                    par ^= 1;
-                }
-                if (!g.stay || kb + 1 == t.kb1) {
-                    ring ^= 1;
-                    swap(slot, slot2);
-                    swap(par, par2);
-                }
-                if (++rslot == slots) {
-                    rslot = 0;
-                    rpar ^= 1;
-                }
-            }
-        }
-        cp_async_wait<0>();
-    }
-    if constexpr (CG == 1 && !COLUMNS) {
-        if (g.cl > 1) {
-            // The sums of a tile's shares meet in shared memory, where each CTA has left its
-            // own: each adds up a part of the columns, in the order of the shares, and does
-            // their epilogue.
-            __syncwarp();
-            cluster_sync_all();
-            if (warp >= 4 && warp < 4 + kEpiWarps) {
-                const int quarter = warp & 3, half = (warp - 4) >> 2;
+                cluster_sync_all();
                 const Tile t = tile_of<KIND, CG>(g, first_unit, share);
                 const ProblemArgs &p = g.p[0];
                 const GemmEpi &e = p.e;
@@ -1143,14 +1040,137 @@ __global__ void __launch_bounds__(GEN ? 512 : 384, 1) gemm_kernel(const __grid_c
                         finish_planes<P>(e, mirror, m, n, v, add);
                     } else if (left > 0) {
                         if (rows_full && left >= 16)
-                            finish_out<true>(e, p.m, m, n, left, alpha, bias, v, add, [] {});
+                            finish_out<P == 3, true>(e, p.m, m, n, left, alpha, bias, v, add, [] {});
                         else
-                            finish_out<false>(e, p.m, m, n, left, alpha, bias, v, add, [] {});
+                            finish_out<P == 3, false>(e, p.m, m, n, left, alpha, bias, v, add, [] {});
                     }
                 }
+                __syncwarp();
+                cluster_sync_all();  // (no CTA leaves while another reads from it)
             }
+        }
+    } else if (GEN && warp >= 12) {
+        // ------------------------------------------ copy, split, store planes
+        // Two groups of four warps take the blocks in turn, each those of one ring (one group
+        // took 1,100 clocks per block for 300 instructions a warp, most of them waiting for the
+        // one before: 4.4 TB/s of weights).  A warp has 32 rows (its TMEM lanes) x 32 terms of a
+        // block.  Rows of k: [32][32] floats, the 16-byte pieces of a row permuted (TMA's
+        // 128-byte swizzle) so that eight neighbouring rows read from all banks; rows of m: [32
+        // terms][32].  Where TMA cannot read the rows, the warp copies its own 32 lines of 128
+        // bytes, element by element (a lane each: neighbours), so that no barrier lies between
+        // copying and splitting.
+        set_registers<88, false>();
+        const int quarter = warp & 3, ring = (warp - 12) >> 2;
+        const ProblemArgs &p = g.p[0];
+        const bool mn = p.a.mn, vec = p.a.vec;
+        const long long ld = p.a.ld;
+        const int slots = vec ? g.raw / 2 : kRawSlots;
+        // (TMA: a block is the four warps' parts one after another)
+        const unsigned raw = smem_addr(smem) + g.S * g.stage +
+                             (vec ? (ring * slots * kGenWarps + quarter) * 4096 : (warp - 12) * kRawSlots * 4096);
+        const unsigned raw_step = vec ? kGenWarps * 4096 : 4096;
+        // this group's blocks (kb0: the block)
+        struct Walk {
+            int round, u;
+            Tile t;
+        };
+        auto next = [&](Walk &w, int n) {
+#pragma unroll 1
+            for (; n > 0 && w.u < g.units; --n) {
+                if (++w.t.kb0 < w.t.kb1) continue;
+                w.u = unit_at(g, ++w.round, first_unit, step);
+                if (w.u < g.units) w.t = tile_of<KIND, CG>(g, w.u, share);
+            }
+        };
+        Walk at_split = {-1, first_unit, {}};
+        next(at_split, 1 + ring);
+        Walk at_copy = at_split;
+        int cslot = 0;
+        // (the weights are the caller's: no wait, as above)
+        auto copy_next = [&]() {
+            if (vec) return;
+            if (at_copy.u < g.units) {
+                const Tile &t = at_copy.t;
+                const int row = t.mt * kMT + quarter * 32 + (mn ? lane : 0), k = t.kb0 * BK + (mn ? 0 : lane);
+                // lines, and elements of a line from this lane's, that exist
+                const int lines = mn ? p.k - k : p.m - row, along = mn ? p.m - row : p.k - k;
+                const float *s = p.a.src + (mn ? (long long)k * ld + row : (long long)row * ld + k);
+                const unsigned d = raw + cslot * raw_step;
+#pragma unroll 4
+                for (int j = 0; j < 32; ++j, s += ld) {
+                    const unsigned at = mn ? lane * 4 : ((lane >> 2 ^ (j & 7)) << 4) + (lane & 3) * 4;
+                    const bool is = along > 0 && lines > j;
+                    cp_async4_part(d + j * 128 + at, is ? s : p.a.src, is ? 4 : 0);
+                }
+                next(at_copy, 2);
+                if (++cslot == kRawSlots) cslot = 0;
+            }
+            cp_async_commit();
+        };
+        for (int i = 0; i < kRawSlots - 1; ++i) copy_next();
+        const unsigned a_dst = tmem + 2 * ACC + ((unsigned)(quarter * 32) << 16);
+        const int S = g.S / RINGS;
+        int slot = 0, rslot = 0;  // (stages: as the TMA's)
+        unsigned par = 0, rpar = 0;
+        while (at_split.u < g.units) {
+            const int raw_at = ring * slots + rslot;
+            if (vec) {
+                if (!wait_warp(sh, &sh.raw_full[raw_at], rpar)) break;
+            } else {
+                cp_async_wait<kRawSlots - 2>();
+                __syncwarp();
+            }
+            const unsigned r = raw + rslot * raw_step;
+            float v[32];
+            if (mn) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(r + i * 128 + lane * 4));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+                                 : "=f"(v[4 * i]), "=f"(v[4 * i + 1]), "=f"(v[4 * i + 2]), "=f"(v[4 * i + 3])
+                                 : "r"(r + lane * 128 + ((i ^ (lane & 7)) << 4)));
+            }
+            const int at = ring * S + slot;
+            if (!wait_warp(sh, &sh.empty[at], par ^ 1)) break;
+            tc_fence_after_sync();
+            const unsigned d = a_dst + at * kGenCols;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                unsigned w0[8], w1[8], w2[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    planes3(v[16 * h + 2 * i], v[16 * h + 2 * i + 1], w0[i], w1[i], w2[i]);
+                tmem_st8(d + 8 * h, w0);
+                tmem_st8(d + 8 * h + 16, w1);
+                tmem_st8(d + 8 * h + 32, w2);
+            }
+            __syncwarp();  // (all have read: the slot may be copied to)
+            if (vec && lane == 0) arrive(&sh.raw_empty[raw_at]);
+            copy_next();
+            asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+            tc_fence_before_sync();
             __syncwarp();
-            cluster_sync_all();  // (no CTA leaves while another reads from it)
+            if (lane == 0) arrive(&sh.full[at]);
+            if (++slot == S) {
+                slot = 0;
+                par ^= 1;
+            }
+            if (++rslot == slots) {
+                rslot = 0;
+                rpar ^= 1;
+            }
+            next(at_split, 2);
+        }
+        cp_async_wait<0>();
+    }
+    if constexpr (CG == 1 && !COLUMNS) {
+        if (g.cl > 1 && (warp < 4 || warp >= 4 + kEpiWarps)) {  // (as the epilogue's warps)
+            __syncwarp();
+            cluster_sync_all();
+            cluster_sync_all();
         }
     }
     tc_fence_before_sync();
@@ -1171,7 +1191,7 @@ struct GemmKernel {
         qcnn_status rc = allow_smem(reinterpret_cast<const void *>(k));
         if (rc != QCNN_OK) return rc;
         const int cluster = CG * g.cl;
-        return launch_k(k, dim3(ctas), dim3(GEN ? 512 : 384), smem, st, dim3(cluster > 1 ? cluster : 0, 1, 1), g);
+        return launch_k(k, dim3(ctas), dim3(GEN ? kGenThreads : 384), smem, st, dim3(cluster > 1 ? cluster : 0, 1, 1), g);
     }
 };
 

@@ -227,7 +227,6 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
                     steps ? o.P : 0, s.x[0], px, xplane, out, ldo);
     for (int i = 0; i < steps && rc == QCNN_OK; ++i) {
         const GemmOperand x{s.x[i & 1], px, xplane, 0}, a{s.a, pa, aplane, 0}, b{s.b, pa, aplane, 0};
-        const int type = o.P;  // GEMM_T_PLANES2, GEMM_T_PLANES3
         GemmProblem g;
         g.a = g.b = x;
         g.a.mn = g.b.mn = wide ? 0 : 1;
@@ -236,7 +235,6 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
         g.e.out = s.a;
         g.e.ldo = pa;
         g.e.out_plane = aplane;
-        g.e.out_type = type;
         if ((rc = launch_gemm(o.gram, &g, 1, st)) != QCNN_OK) break;
         g.a = g.b = a;
         g.k = o.p;
@@ -245,7 +243,6 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
         g.e.add = s.a;
         g.e.lda = pa;
         g.e.add_plane = aplane;
-        g.e.add_type = type;
         g.e.diagonal = k[0];
         g.e.out = s.b;
         if ((rc = launch_gemm(o.poly, &g, 1, st)) != QCNN_OK) break;
@@ -268,7 +265,6 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
             u.e.out = s.x[(i + 1) & 1];
             u.e.ldo = px;
             u.e.out_plane = xplane;
-            u.e.out_type = type;
         } else {
             apply.kind = GEMM_OUT;
             u.e.out = out;

@@ -411,7 +411,6 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
             d.e.rows = s.rows;
             d.e.class0 = c0;
             d.e.out = s.dl;
-            d.e.out_type = bf16 ? GEMM_T_BF16 : GEMM_T_PLANES3;
             d.e.ldo = pz;
             d.e.out_plane = zplane;
             d.e.col_part = s.db;
