@@ -5,8 +5,8 @@
 //
 // Each product is gemm.cuh's, with the layer's outputs (dx, dW: its inputs) as the
 // contiguous index m.  Three ways, by the estimated time of each:
-//   few rows (forward, N <= 8): no tensor cores; the weights are streamed once through
-//     fp32 multiply-adds, which then take less than the memory does;
+//   few rows (forward, N <= 4, or 8 where few_rows_sooner says so): no tensor cores; the
+//     weights are streamed once through fp32 multiply-adds;
 //   fp32 weights split on their way to the tensor cores: no pass over them, so it has the
 //     products that their bytes bound (the other operand's planes are small then);
 //   all operands as planes in the workspace (fp32), or the bf16 operands themselves.
@@ -49,7 +49,7 @@ __device__ __forceinline__ void load_vec(const T *p, float (&v)[V]) {
 }
 
 // (Eight rows: two CTAs per SM for loads in flight; with one, 8 rows of 4096 -> 19456 in fp32
-// took 111 us, with two 81.  One row takes 51, 6.2 TB/s, four 64.)
+// took 111 us, with two 83.  One row takes 47, 6.8 TB/s, four 51.)
 template <typename T, int NB, bool VEC>
 __global__ void __launch_bounds__(256, NB == 8 ? 2 : 1) few_rows_kernel(FewRows f, int kw) {
     constexpr int V = VEC ? 16 / (int)sizeof(T) : 4;
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(256, NB == 8 ? 2 : 1) few_rows_kernel(FewRows 
     const int step = kw * 32 * V;
     // (VEC: Cs is a multiple of V)
     if constexpr (VEC) {
-#pragma unroll(NB <= 2 ? 4 : 2)
+#pragma unroll(NB * V <= 8 ? 4 : 2)
         for (int k = (part * 32 + lane) * V; k < f.Cs; k += step) {
             float wv[kFewOut][V];
 #pragma unroll
@@ -253,11 +253,9 @@ struct ForwardPlan {
     bool few = false, wplanes = false;
     GemmPlan g;
 };
-ForwardPlan plan_forward(int N, int Cs, int Ct, int dtype) {
+ForwardPlan plan_forward(int N, int Cs, int Ct, int dtype, bool wa) {
     ForwardPlan p;
-    if (N <= kFewRows) {
-        p.few = true;
-    } else if (dtype == QCNN_BF16) {
+    if (dtype == QCNN_BF16) {
         p.g = plan_gemm(1, GEMM_OUT, Ct, N, Cs);
     } else {
         p.g = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs);
@@ -267,6 +265,7 @@ ForwardPlan plan_forward(int N, int Cs, int Ct, int dtype) {
             p.g = q;
         }
     }
+    p.few = few_rows_sooner(N, Cs, Ct, dtype == QCNN_BF16, wa, p.g);
     return p;
 }
 struct ForwardSpace {
@@ -351,8 +350,13 @@ extern "C" {
 qcnn_status qcnn_dense_forward_workspace_size(int N, int Cs, int Ct, int dtype, int aligned,
                                               size_t *bytes) {
     if (!bytes || N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
-    *bytes = N ? carve_forward(plan_forward(N, Cs, Ct, dtype), N, Cs, Ct, dtype, aligned, aligned, nullptr).bytes
-               : 0;
+    *bytes = 0;
+    if (N == 0) return QCNN_OK;
+    for (int wa = 0; wa < 2; ++wa) {  // (of fp32 calls, `aligned` says nothing)
+        if (!wa && aligned && dtype == QCNN_BF16) continue;
+        const ForwardPlan p = plan_forward(N, Cs, Ct, dtype, wa);
+        *bytes = std::max(*bytes, carve_forward(p, N, Cs, Ct, dtype, aligned, aligned, nullptr).bytes);
+    }
     return QCNN_OK;
 }
 
@@ -368,8 +372,8 @@ qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, cons
         return QCNN_ERR_INVALID_ARG;
     if (N == 0) return QCNN_OK;
     const bool bf16 = dtype == QCNN_BF16;
-    const bool xa = tma_ok(x, ldx), wa = tma_ok(W, ldw);
-    const ForwardPlan p = plan_forward(N, Cs, Ct, dtype);
+    const bool xa = tma_ok(x, ldx, dtype), wa = tma_ok(W, ldw, dtype);
+    const ForwardPlan p = plan_forward(N, Cs, Ct, dtype, wa);
     const ForwardSpace s = carve_forward(p, N, Cs, Ct, dtype, xa, wa, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;
@@ -443,9 +447,9 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
     const BackwardPlan p = plan_backward(N, Cs, Ct, dtype);
     // dy itself where it is dz in a form that the products read
     const bool products = dx || dW;
-    const bool dz = products && (act != QCNN_ACT_NONE || !bf16 || !tma_ok(dy, lddy));
-    const bool x_copy = dW && (!bf16 || !tma_ok(x, ldx));
-    const bool w_copy = dx && (bf16 ? !tma_ok(W, ldw) : p.wplanes);
+    const bool dz = products && (act != QCNN_ACT_NONE || !bf16 || !tma_ok(dy, lddy, dtype));
+    const bool x_copy = dW && (!bf16 || !tma_ok(x, ldx, dtype));
+    const bool w_copy = dx && (bf16 ? !tma_ok(W, ldw, dtype) : p.wplanes);
     const BackwardSpace s = carve_backward(p, N, Cs, Ct, dtype, dz, x_copy, w_copy, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;

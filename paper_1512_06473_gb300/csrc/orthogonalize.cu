@@ -218,7 +218,7 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
     const bool wide = m <= n;
     const Pieces q{m, (long long)m * cdiv(n, kPieceCols), n, cdiv(n, kPieceCols)};
     const int blocks = (int)std::min<long long>(kNormBlocks, (q.all + 7) / 8);
-    const int vec = tma_ok(G, ldg);  // (16-byte rows; of fp32 more than it needs)
+    const int vec = tma_ok(G, ldg, sizeof(T) == 4 ? QCNN_F32 : QCNN_BF16);
     qcnn_status rc = launch_pdl(norm_kernel<T>, dim3(blocks), dim3(256), 0, st, G, ldg, q, vec, s.norm);
     if (rc != QCNN_OK) return rc;
     const long long px = pad256(n), xplane = pad256(m) * px, pa = pad256(o.p), aplane = pa * pa;

@@ -230,7 +230,7 @@ struct XentPlan {
     int piece = 0;  // classes of a piece
     int slab = 0, slabs = 1;
 };
-XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool grad) {
+XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool wa, bool grad) {
     XentPlan p;
     const bool bf16 = dtype == QCNN_BF16;
     const int P = bf16 ? 1 : 3;
@@ -238,14 +238,14 @@ XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool grad) {
     p.piece = Ct;
     p.wplanes = true;
     if (p.small) {
-        p.few = N <= kFewRows;
         p.slab = std::max(32, cdiv(cdiv(N, std::max(1, 4 * num_sms() / cdiv(Ct, 128))), 8) * 8);
         p.slabs = cdiv(N, p.slab);
         p.logits = plan_gemm(P, GEMM_OUT, Ct, N, Cs, kGroups);
         p.dx = plan_gemm(P, GEMM_OUT, Cs, N, Ct);
         p.dw = plan_gemm(P, GEMM_OUT, Cs, Ct, N);
+        const GemmPlan l = bf16 ? p.logits : plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, kGroups);
+        p.few = few_rows_sooner(N, Cs, Ct, bf16, wa, l);
         if (!bf16) {
-            const GemmPlan l = plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, kGroups);
             const GemmPlan x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct);
             const double planes = (p.few ? 0 : p.logits.score) + (grad ? p.dx.score : 0);
             const double direct = (p.few ? 0 : l.score) + (grad ? x.score : 0);
@@ -325,8 +325,9 @@ struct XentCall {
 qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes, cudaStream_t st) {
     const int N = a.N, Cs = a.Cs, Ct = a.Ct;
     const bool bf16 = a.dtype == QCNN_BF16;
-    const XentPlan p = plan_xent(N, Cs, Ct, a.dtype, a.grad);
-    const XentSpace s = carve_xent(p, N, Cs, Ct, a.dtype, a.grad, tma_ok(a.x, a.ldx), tma_ok(a.W, a.ldw), workspace);
+    const bool xa = tma_ok(a.x, a.ldx, a.dtype), wa = tma_ok(a.W, a.ldw, a.dtype);
+    const XentPlan p = plan_xent(N, Cs, Ct, a.dtype, wa, a.grad);
+    const XentSpace s = carve_xent(p, N, Cs, Ct, a.dtype, a.grad, xa, wa, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;
     PdlScope pdl;
@@ -471,8 +472,11 @@ qcnn_status qcnn_xent_workspace_size(int N, int Cs, int Ct, int dtype, int align
     if (!bytes || N < 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
     *bytes = 0;
     if (N == 0) return QCNN_OK;
-    const XentPlan p = plan_xent(N, Cs, Ct, dtype, grad != 0);
-    *bytes = carve_xent(p, N, Cs, Ct, dtype, grad != 0, aligned, aligned, nullptr).bytes;
+    for (int wa = 0; wa < 2; ++wa) {  // (of fp32 calls, `aligned` says nothing)
+        if (!wa && aligned && dtype == QCNN_BF16) continue;
+        const XentPlan p = plan_xent(N, Cs, Ct, dtype, wa, grad != 0);
+        *bytes = std::max(*bytes, carve_xent(p, N, Cs, Ct, dtype, grad != 0, aligned, aligned, nullptr).bytes);
+    }
     return QCNN_OK;
 }
 
