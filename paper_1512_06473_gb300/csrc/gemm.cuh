@@ -155,6 +155,14 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     }
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
+// 2^x to 2 ulp; results below 2^-126 are zero.
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 __device__ __forceinline__ float bf16_to_float(unsigned short v) {
     return __uint_as_float((unsigned)v << 16);
 }

@@ -487,14 +487,6 @@ __device__ __forceinline__ void finish_planes(const GemmEpi &e, bool mirror, int
     }
 }
 
-constexpr float kLog2e = 1.4426950408889634f;
-// 2^x to 2 ulp; results below 2^-126 are zero.
-__device__ __forceinline__ float ex2(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
 // Running maximum and sum of exp of a lane.  A maximum of -inf has no sum (and adds
 // nothing: exp of -inf minus -inf is left out).
 struct RunningSum {

@@ -45,16 +45,21 @@ inline double pass_clocks(double bytes) { return bytes / 3200.0 + 4000.0; }
 
 // y = x W^T of few rows (dense.cu).
 constexpr int kFewRows = 8;
+// In SM clocks: up to four rows the weights' bytes, with eight the multiply-adds (0.75 and 1
+// million elements of W per us).
+inline double few_rows_clocks(int N, int Cs, int Ct, bool bf16) {
+    const double elements = (double)Cs * Ct;
+    return 5000.0 + (N <= 4 ? elements * (bf16 ? 2.0 : 4.0) / 3400.0 : elements / (bf16 ? 540.0 : 400.0));
+}
 // Whether that is sooner done than the product g.  Up to four rows it always is (4 x 4096 ->
 // 19456 in fp32 51 us and the product 57), and where W is off TMA's alignment (8 x 4097 -> 19456
-// 72 and 104).  With eight its multiply-adds take longer than the bytes of large weights: 8 x
-// 4096 -> 1000 in fp32 8.3 us and the product 14.4, in bf16 6.9 and 9.4; -> 4096 24.6 and 21.2,
-// 19.4 and 11.5; -> 19456 83 and 58, 50 and 29.  (In clocks: 2.6 us and 0.75 or 1 million
-// elements of W per us; the product with its launches.)
+// 72 and 104).  With eight it depends on the size of the weights: 8 x 4096 -> 1000 in fp32 8.3 us and the
+// product 14.4, in bf16 6.9 and 9.4; -> 4096 24.6 and 21.2, 19.4 and 11.5; -> 19456 83 and 58,
+// 50 and 29.  (7000: the product's launches.)
 inline bool few_rows_sooner(int N, int Cs, int Ct, bool bf16, bool w_aligned, const GemmPlan &g) {
     if (N <= 4 || N > kFewRows || !w_aligned) return N <= kFewRows;
-    const double elements = (double)Cs * Ct;
-    return 5000.0 + elements / (bf16 ? 540.0 : 400.0) < std::max(g.score, elements * (bf16 ? 2.0 : 4.0) / 3400.0) + 7000.0;
+    const double bytes = (double)Cs * Ct * (bf16 ? 2.0 : 4.0);
+    return few_rows_clocks(N, Cs, Ct, bf16) < std::max(g.score, bytes / 3400.0) + 7000.0;
 }
 struct FewRows {
     const void *x, *W;

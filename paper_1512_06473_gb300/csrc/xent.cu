@@ -4,16 +4,17 @@
 //   l = x W^T + b;  lse_n = log sum_c exp l_nc;  loss_n = lse_n - l_n,t(n)
 //   dl = g_n (exp(l - lse_n) - [c == t(n)]);  dx = dl W;  dW = dl^T x;  db = sum_n dl
 //
-// Two ways:
-//   small (the fp32 logits fit kPiece bytes): the logits are one piece, kept for the call:
-//     a product, a pass per row (lse, loss), and for the gradient a pass over the piece
-//     (dl, db) and two products.
-//   large: the logits are never stored.  One product over all classes leaves, per tile
-//     and row, the maximum and the sum of exp; joined they are lse.  The gradient then goes
-//     in pieces of the classes: the piece's logits again, whose epilogue turns them into dl
-//     (bf16, or planes), dx += dl W_piece (summed in fp32), dW_piece = dl^T x.  A fourth
-//     product instead of 4 N Ct bytes: at Cs = 2048 that is 1.1 ns per row and 1000 classes,
-//     writing and reading the logits 1.2 ns.
+// Two ways, by the estimated time of each (plan_xent):
+//   kept (the fp32 logits fit kPiece bytes): a product, a pass per row (lse, loss), and for the
+//     gradient a pass over the logits (dl, db) and two products.  It has products whose terms
+//     are shared among CTAs, and fp32 weights read without a pass over them.
+//   not kept: one product over all classes leaves, per tile and row, the maximum and the sum
+//     of exp; joined they are lse.  The gradient then goes in pieces of the classes: the
+//     piece's logits again, whose epilogue turns them into dl (bf16, or planes), dx += dl
+//     W_piece (summed in fp32), dW_piece = dl^T x.
+// In us, kept and not: 128 x 4096 -> 1000 in fp32 19 and 60, with the gradient 51 and 136; 2048 x
+// 1024 -> 8192 in bf16 46 and 32, 133 and 127; 2048 x 256 -> 8192 36 and 24, 93 and 81; 1024 x
+// 1024 -> 16000 in fp32 164 and 165, 481 and 599 (the fourth product costs six there).
 #include "train.cuh"
 
 #include <algorithm>
@@ -21,8 +22,8 @@
 namespace qcnn {
 namespace {
 
-constexpr size_t kPiece = 64u << 20;    // bytes of a kept piece of logits
-constexpr size_t kPieceDl = 128u << 20;  // bytes of a piece of their gradient
+constexpr size_t kPiece = 128u << 20;    // bytes of kept logits at most
+constexpr size_t kPieceDl = 128u << 20;  // bytes of a piece of the gradient of others
 // Shares of the terms of kept logits, joined by the pass over their rows (128 rows of 4096 ->
 // 1000 in fp32: 9 us with 19, 24 us with clusters of eight CTAs, which fill fewer SMs).
 constexpr int kGroups = 32;
@@ -74,9 +75,12 @@ __device__ __forceinline__ void finish_row(const RowOut &o, int n, float top, fl
     if (o.rows) o.rows[n] = make_float4(lse, o.dloss ? o.dloss[n] : 1.f, __int_as_float(t), 0.f);
 }
 
-// Small: a CTA per row of logits; one more counts the rows.  groups > 1: the logits come as
-// that many partial sums [group][N][Ct] without bias, are added up here and (where there is
-// a gradient) left in `logits`.
+// Kept: a CTA per row of logits; one more counts the rows.  GROUPS: the logits come as
+// partial sums [group][N][Ct] without bias, are added up here and (where there is a gradient)
+// left in `logits`.  U classes of a thread at a time, their loads in flight together; the
+// maximum of all, then the sums.  (Maximum and sum joined pair by pair, and 1024 threads for
+// any row, took 86 us for 2048 rows of 8192.)
+template <bool GROUPS>
 __global__ void __launch_bounds__(1024) rows_kernel(const float *part, int groups, const float *bias,
                                                     float *logits, RowOut o) {
     grid_dep_sync();
@@ -84,58 +88,67 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float *part, int group
         count_rows(o.targets, o.N, o.Ct, o.inv);
         return;
     }
+    constexpr int U = GROUPS ? 4 : 8;
     __shared__ float tops[32], sums[32], picked;
     const int t = class_of(o.targets, blockIdx.x, o.Ct), T = blockDim.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const size_t row = (size_t)blockIdx.x * o.Ct, stride = (size_t)o.N * o.Ct;
     if (threadIdx.x == 0) picked = 0.f;
     __syncthreads();
     float top = -INFINITY, sum = 0.f;
-    for (int c0 = threadIdx.x; c0 < o.Ct; c0 += T * 4) {
-        float v[4], m = top;
+    for (int c0 = threadIdx.x; c0 < o.Ct; c0 += T * U) {
+        float v[U], m = top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < U; ++i) {
             const int c = c0 + i * T;
             v[i] = -INFINITY;
             if (c >= o.Ct) continue;
-            if (groups > 1) {
+            if constexpr (GROUPS) {
                 v[i] = add_groups<true>(part + row + c, groups, stride) + (bias ? bias[c] : 0.f);
                 if (o.rows) logits[row + c] = v[i];
             } else {
                 v[i] = logits[row + c];
             }
-            if (c == t) picked = v[i];
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (c0 + i * T == t) picked = v[i];
             m = fmaxf(m, v[i]);
         }
         if (m == -INFINITY) {  // nothing to add (or NaN)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < U; ++i)
                 if (v[i] != v[i]) sum = v[i];
             continue;
         }
-        sum = top == -INFINITY ? sum : sum * expf(top - m);
+        sum = top == -INFINITY ? sum : sum * ex2((top - m) * kLog2e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += expf(v[i] - m);
+        for (int i = 0; i < U; ++i) sum += ex2((v[i] - m) * kLog2e);
         top = m;
     }
+    float all = top;
 #pragma unroll
-    for (int s = 16; s; s >>= 1)
-        join(top, sum, __shfl_xor_sync(0xffffffffu, top, s), __shfl_xor_sync(0xffffffffu, sum, s));
-    if ((threadIdx.x & 31) == 0) {
-        tops[threadIdx.x >> 5] = top;
-        sums[threadIdx.x >> 5] = sum;
-    }
+    for (int s = 16; s; s >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, s));
+    if (lane == 0) tops[warp] = all;
     __syncthreads();
-    if (threadIdx.x < 32) {
-        top = threadIdx.x * 32 < T ? tops[threadIdx.x] : -INFINITY;
-        sum = threadIdx.x * 32 < T ? sums[threadIdx.x] : 0.f;
+    all = lane * 32 < T ? tops[lane] : -INFINITY;
 #pragma unroll
-        for (int s = 16; s; s >>= 1)
-            join(top, sum, __shfl_xor_sync(0xffffffffu, top, s), __shfl_xor_sync(0xffffffffu, sum, s));
-        if (threadIdx.x == 0) finish_row(o, blockIdx.x, top, sum, picked);
+    for (int s = 16; s; s >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, s));
+    // (-inf minus -inf is left out; a sum of NaN stays)
+    if (top != all) sum *= ex2((top - all) * kLog2e);
+#pragma unroll
+    for (int s = 16; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    if (lane == 0) sums[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+        sum = lane * 32 < T ? sums[lane] : 0.f;
+#pragma unroll
+        for (int s = 16; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+        if (lane == 0) finish_row(o, blockIdx.x, all, sum, picked);
     }
 }
 
-// Large: the tiles' maxima and sums of 32 rows per CTA; 32 warps take the tiles in turn.
+// Not kept: the tiles' maxima and sums of 32 rows per CTA; 32 warps take the tiles in turn.
 __global__ void __launch_bounds__(1024) stats_join_kernel(const float2 *stats, int parts,
                                                          const float *target_logit, RowOut o) {
     grid_dep_sync();
@@ -163,10 +176,12 @@ __global__ void __launch_bounds__(1024) stats_join_kernel(const float2 *stats, i
     }
 }
 
-// Small: the gradient of the logits and its sums over a slab of rows.  A CTA takes 128
-// classes x a slab: a warp a row, a lane four classes.
-__global__ void __launch_bounds__(256) dl_kernel(const float *logits, const float4 *rows, int N, int Ct, unsigned short *out, int planes,
-                                                 long long ldo, long long plane, float *part, int slab) {
+// Kept: the gradient of the logits and its sums over a slab of rows.  A CTA takes 128
+// classes x a slab: a warp a row, a lane four classes (VEC: Ct is a multiple of 4).
+template <bool VEC>
+__global__ void __launch_bounds__(256) dl_kernel(const float *logits, const float4 *rows, int N, int Ct,
+                                                 unsigned short *out, int planes, long long ldo, long long plane,
+                                                 float *part, int slab) {
     __shared__ float red[8][128];
     grid_dep_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -174,18 +189,23 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
     const int r1 = min(N, ((int)blockIdx.y + 1) * slab);
     float sum[4] = {};
     if (c < Ct) {
-#pragma unroll 2
+#pragma unroll 4
         for (int r = (int)blockIdx.y * slab + warp; r < r1; r += 8) {
             const float4 row = rows[r];
             const int target = __float_as_int(row.z);
             const float *l = logits + (size_t)r * Ct + c;
             float v[4];
+            if constexpr (VEC) {
+                const float4 a = *reinterpret_cast<const float4 *>(l);
+                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = c + j < Ct ? l[j] : -INFINITY;
+                for (int j = 0; j < 4; ++j) v[j] = c + j < Ct ? l[j] : -INFINITY;
+            }
             const float g = row.y;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p = expf(v[j] - row.x);
+                const float p = ex2((v[j] - row.x) * kLog2e);
                 // (a row without a class is zero, whatever its logits are)
                 v[j] = target >= 0 && c + j < Ct ? g * (target == c + j ? p - 1.f : p) : 0.f;
                 sum[j] += v[j];
@@ -215,48 +235,59 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
     }
 }
 
-// Threads of rows_kernel: one per class where there are few rows, a quarter of that (four
-// classes in a go) where the rows fill the SMs.
+// Threads of rows_kernel: one per class where there are few rows; where the rows fill the SMs
+// eight CTAs of 256 at most each.
 int rows_threads(int N, int Ct) {
-    const int want = N <= 2 * num_sms() ? Ct : Ct / 4;
-    return std::min(1024, std::max(128, cdiv(want, 128) * 128));
+    if (N <= 2 * num_sms()) return std::min(1024, std::max(128, cdiv(Ct, 128) * 128));
+    return Ct <= 1024 ? 128 : 256;
 }
 
 // fp32: x and dl always as planes; wplanes: the weights too.  bf16: copies of what TMA
 // cannot read.
 struct XentPlan {
-    bool small = false, few = false, wplanes = false;
+    bool keep = false, few = false, wplanes = false;
     GemmPlan logits, stats, dl, dx, dw;
     int piece = 0;  // classes of a piece
     int slab = 0, slabs = 1;
 };
-XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool wa, bool grad) {
+XentPlan plan_kept(int N, int Cs, int Ct, bool bf16, bool wa, bool grad, double *clocks) {
     XentPlan p;
-    const bool bf16 = dtype == QCNN_BF16;
     const int P = bf16 ? 1 : 3;
-    p.small = (size_t)N * Ct * 4 <= kPiece;
+    const double logits = (double)N * Ct;
+    p.keep = true;
     p.piece = Ct;
     p.wplanes = true;
-    if (p.small) {
-        p.slab = std::max(32, cdiv(cdiv(N, std::max(1, 4 * num_sms() / cdiv(Ct, 128))), 8) * 8);
-        p.slabs = cdiv(N, p.slab);
-        p.logits = plan_gemm(P, GEMM_OUT, Ct, N, Cs, kGroups);
-        p.dx = plan_gemm(P, GEMM_OUT, Cs, N, Ct);
-        p.dw = plan_gemm(P, GEMM_OUT, Cs, Ct, N);
-        const GemmPlan l = bf16 ? p.logits : plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, kGroups);
-        p.few = few_rows_sooner(N, Cs, Ct, bf16, wa, l);
-        if (!bf16) {
-            const GemmPlan x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct);
-            const double planes = (p.few ? 0 : p.logits.score) + (grad ? p.dx.score : 0);
-            const double direct = (p.few ? 0 : l.score) + (grad ? x.score : 0);
-            if (direct <= planes + pass_clocks((double)Ct * Cs * 10.0)) {
-                p.wplanes = false;
-                p.logits = l;
-                p.dx = x;
-            }
+    p.slab = std::max(32, cdiv(cdiv(N, std::max(1, 4 * num_sms() / cdiv(Ct, 128))), 8) * 8);
+    p.slabs = cdiv(N, p.slab);
+    p.logits = plan_gemm(P, GEMM_OUT, Ct, N, Cs, kGroups);
+    p.dx = plan_gemm(P, GEMM_OUT, Cs, N, Ct);
+    p.dw = plan_gemm(P, GEMM_OUT, Cs, Ct, N);
+    const GemmPlan l = bf16 ? p.logits : plan_gemm(GEMM_F32, GEMM_OUT, Ct, N, Cs, kGroups);
+    p.few = few_rows_sooner(N, Cs, Ct, bf16, wa, l);
+    const double few = few_rows_clocks(N, Cs, Ct, bf16);
+    *clocks = (p.few ? few : p.logits.score) + (grad ? p.dx.score : 0);
+    if (!bf16) {
+        const GemmPlan x = plan_gemm(GEMM_F32, GEMM_OUT, Cs, N, Ct);
+        const double direct = (p.few ? few : l.score) + (grad ? x.score : 0);
+        *clocks += p.few && !grad ? 0 : pass_clocks((double)Ct * Cs * 10.0);
+        if (direct <= *clocks) {
+            p.wplanes = false;
+            p.logits = l;
+            p.dx = x;
+            *clocks = direct;
         }
-        return p;
     }
+    // (rows_kernel; few rows leave SMs idle)
+    const double sums = 4.0 * (p.few ? 1 : p.logits.groups);
+    *clocks += std::max(pass_clocks(logits * sums), 4000.0 + Ct * sums / 20.0);
+    if (grad) *clocks += pass_clocks(logits * (4.0 + 2.0 * P)) + p.dw.score;
+    return p;
+}
+XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool wa, bool grad) {
+    const bool bf16 = dtype == QCNN_BF16;
+    const int P = bf16 ? 1 : 3;
+    XentPlan p;
+    p.wplanes = true;
     p.stats = plan_gemm(P, GEMM_STATS, N, Ct, Cs);
     const long long most = (long long)(kPieceDl / ((size_t)N * 2 * P)) / 256 * 256;
     p.piece = (int)std::min<long long>(Ct, std::max<long long>(256, most));
@@ -265,7 +296,12 @@ XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool wa, bool grad) {
     p.dl = plan_gemm(P, GEMM_DLOGITS, p.piece, N, Cs);
     p.dx = plan_gemm(P, GEMM_OUT, Cs, N, p.piece);
     p.dw = plan_gemm(P, GEMM_OUT, Cs, p.piece, N);
-    return p;
+    if ((size_t)N * Ct * 4 > kPiece) return p;
+    double kept = 0.0, again = p.stats.score + 5000.0;
+    const XentPlan q = plan_kept(N, Cs, Ct, bf16, wa, grad, &kept);
+    if (!bf16) again += pass_clocks((double)Ct * Cs * 10.0);
+    if (grad) again += cdiv(Ct, p.piece) * (p.dl.score + p.dx.score + p.dw.score);
+    return kept <= again ? q : p;
 }
 struct XentSpace {
     float *inv = nullptr, *logits = nullptr, *part = nullptr, *target_logit = nullptr, *db = nullptr, *dx = nullptr;
@@ -286,7 +322,7 @@ XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool g
     const bool x_copy = !p.few && (!bf16 || !xa);
     if (x_copy) s.x = c.array<unsigned short>(P * N * pc);
     if ((!p.few || grad) && (bf16 ? !wa : p.wplanes)) s.w = c.array<unsigned short>(P * Ct * pc);
-    if (p.small) {
+    if (p.keep) {
         s.logits = c.array<float>((size_t)N * Ct);
         if (!p.few && p.logits.groups > 1) s.part = c.array<float>((size_t)p.logits.groups * N * Ct);
     } else {
@@ -297,7 +333,7 @@ XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool g
         // rows without a class must not reach dW, not even as 0 * NaN
         s.kept = c.array<unsigned short>(P * N * pc);
         s.dl = c.array<unsigned short>(P * N * pad8(p.piece));
-        if (p.small) {
+        if (p.keep) {
             s.db = c.array<float>((size_t)p.slabs * Ct);
         } else {
             s.db = c.array<float>((size_t)p.dl.n_tiles * 2 * p.piece);
@@ -348,7 +384,7 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
     RowOut ro{a.targets, a.dloss, a.loss, a.lse, s.rows, s.inv, N, Ct};
     const int type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
     GemmProblem g;
-    if (p.small) {
+    if (p.keep) {
         g.e.bias = a.bias;
         g.e.out = s.logits;
         g.e.ldo = Ct;
@@ -367,9 +403,10 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
             rc = launch_gemm(p.logits, &g, 1, st);
         }
         if (rc != QCNN_OK) return rc;
-        rc = launch_pdl(rows_kernel, dim3(N + (a.grad ? 1 : 0)),
-                        dim3(rows_threads(N, Ct)), 0, st,
-                        static_cast<const float *>(s.part), p.few ? 1 : p.logits.groups, a.bias, s.logits, ro);
+        const bool groups = !p.few && p.logits.groups > 1;
+        rc = launch_pdl(groups ? rows_kernel<true> : rows_kernel<false>, dim3(N + (a.grad ? 1 : 0)),
+                        dim3(rows_threads(N, Ct)), 0, st, static_cast<const float *>(s.part), p.logits.groups,
+                        a.bias, s.logits, ro);
     } else {
         g.a = xo;
         g.b = wo;
@@ -394,9 +431,9 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         const long long pz = pad8(cn), zplane = (long long)N * pz;
         const GemmOperand wp{static_cast<const uint8_t *>(wo.p) + c0 * wo.ld * (bf16 || s.w ? 2 : 4), wo.ld,
                              wo.plane, 1};
-        if (p.small) {
+        if (p.keep) {
             float *const part = a.dbias ? s.db : nullptr;
-            rc = launch_pdl(dl_kernel, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0, st, s.logits, s.rows, N, Ct,
+            rc = launch_pdl(Ct % 4 ? dl_kernel<false> : dl_kernel<true>, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0, st, s.logits, s.rows, N, Ct,
                             s.dl, P, pz, zplane, part, p.slab);
             if (rc == QCNN_OK && a.dbias)
                 rc = launch_column_join(s.db, p.slabs, Ct, Ct, inv, a.dbias, st);
