@@ -132,3 +132,15 @@ def test_binding_refuses_what_is_not_on_the_gpu():
                  lambda: q.orthogonalize(None)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_workspaces_without_alignment_are_no_smaller(dtype):
+    for N in (1, 4, 5, 8, 9, 100):
+        for Cs, Ct in ((4096, 4096), (4096, 1000), (70, 30), (2047, 3001)):
+            for query, more in (("qcnn_dense_forward_workspace_size", ()), ("qcnn_xent_workspace_size", (0,)),
+                                ("qcnn_xent_workspace_size", (1,))):
+                any_, aligned = (_bytes(query, N, Cs, Ct, dtype, a, *more) for a in (0, 1))
+                assert any_ >= aligned
+                if dtype == F32:
+                    assert any_ == aligned
