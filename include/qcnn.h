@@ -649,8 +649,8 @@ qcnn_status qcnn_net_forward_host(const qcnn_layer *layers, int n_layers,
  *
  * Arithmetic: bf16 operands are multiplied exactly and summed in fp32, each output
  * rounded to bf16 once.  fp32 operands are taken in three bf16 pieces, which hold all
- * their 24 bits, and summed in fp32, or (N <= 8) multiplied as they are: results are
- * as close to the exact ones as those of fp32 multiply-adds.  A non-finite operand (or
+ * their 24 bits, and summed in fp32, or (of few rows) multiplied as they are: results
+ * are as close to the exact ones as those of fp32 multiply-adds.  A non-finite operand (or
  * one above 3.38e38) makes the outputs that it enters non-finite, NaN where plain
  * arithmetic would give an infinity.  Sums are in a fixed order: results repeat bit
  * for bit.
@@ -702,7 +702,8 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
  *   targets [N] int64.  A row whose target is no class (negative, e.g. -100) has loss 0
  *   and gradient 0, whatever its x holds (so has one of Ct or above, a caller's error that
  *   the debug build records); lse is computed for it all the same.
- *   A bias of -inf takes a class out.  A row without any class left has NaN.
+ *   A bias of -inf takes a class out.  A row without any class left has lse -inf and
+ *   loss NaN.
  * qcnn_xent_grad also gives the gradients of sum_n dloss[n] loss[n]; dloss NULL: of the
  * mean of the losses over the rows with a class (0 if there are none):
  *   dx [N][Cs], dW [Ct][Cs], dbias [Ct] (or NULL).
@@ -724,12 +725,12 @@ qcnn_status qcnn_xent_grad(const void *x, long long ldx, int N, int Cs, const vo
 /*
  * qcnn_orthogonalize -- the update of a weight matrix with its singular values brought near
  * 1 by Newton-Schulz products (Jordan et al. 2024, the Muon optimiser):
- *   X = G / (||G||_F + eps); steps times: A = X X^T, X = a X + (b A + c A A) X
+ *   X = G / (||G||_F + eps); steps times: A = X X^T, X = B X with B = a I + b A + c A A
  *   (X^T X from the right where G has more rows than columns, the same polynomial).
  *   G [m][n], out [m][n] (may be G itself); coeffs: host array {a, b, c} or NULL for
  *   {3.4445, -4.7750, 2.0315}; 0 <= steps <= 100; eps >= 0.
- * Between the products X, A and b A + c A A are kept in two bf16 pieces (16 bits) in bf16
- * calls, in three (24 bits) in fp32 calls.
+ * Between the products X, A and B are kept in two bf16 pieces (16 bits) in bf16 calls, in
+ * three (24 bits) in fp32 calls; of small matrices, done in one launch, in fp32.
  */
 qcnn_status qcnn_orthogonalize_workspace_size(int m, int n, int dtype, size_t *bytes);
 qcnn_status qcnn_orthogonalize(const void *G, long long ldg, int m, int n, int steps,

@@ -168,6 +168,12 @@ __global__ void __launch_bounds__(256) planes_kernel(const T *src, long long all
 
 }  // namespace
 
+// The tile, shares and pairing with the least estimated time.  Both sides of each choice, in
+// us: tiles of a pair of CTAs (cg 2), 4096 x 4096 -> 8192 in bf16, 168 and 193 without; shares in
+// clusters, 128 x 9216 -> 4096 in fp32, 56 and 121; shares kept apart, the logits of 128 x 4096 ->
+// 1000, 20 and 25 (with the pass over their rows); a block's sum left in its accumulator
+// (launch_gemm: stay), backward of 128 x 4096 -> 4096, 70 and 72; two products in a launch
+// (gemm_together), backward of 3001 x 2048 -> 5003 in bf16, 114 and 141.
 static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int max_groups, int sms) {
     GemmPlan best;
     const bool gen = planes == GEMM_F32;
@@ -201,7 +207,8 @@ static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int ma
                 const int kps = cdiv(kblocks, cl);
                 if (cdiv(kblocks, kps) != cl) continue;
                 // (clusters do not span GPCs: fewer of eight CTAs than SMs / 8 are resident)
-                const int slots = cl == 1 ? sms / cg : std::max(1, cluster_capacity(gemm_kernel_address(), 384, cl, kSmemMax));
+                const int slots =
+                    cl == 1 ? sms / cg : std::max(1, cluster_capacity(gemm_kernel_address(), 384, cl, kSmemMax));
                 const double waves = (double)((units + slots - 1) / slots);
                 // (shares meet: two barriers of the cluster, bn / cl columns read from each)
                 const double meet = cl > 1 ? 2500.0 + bn * 10.0 : 0.0;

@@ -27,14 +27,14 @@ struct GemmOperand {
 enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1 };
 
 // What becomes of a sum.  OUT: v = alpha * sum + bias[m] (alpha: *alpha_ptr where set); pre =
-// v; v = act(v); v += beta * add[n][m]; out[n][m] = v (products of three planes: all fp32).  PLANES: v = alpha * sum + beta * add,
-// + diagonal where n == m; out and add are planes of the product's number, whose matrices
-// have room for whole tiles (rows and columns up to the next multiple of 256).  SYM: PLANES
-// of a symmetric product (A and B the same matrix): only m >= n is computed, and stored at
-// both places.  STATS: m are rows, n classes: the maximum and the sum of exp over a tile's
-// classes of v = sum + bias[n], and the value at the row's target.  DLOGITS: m are classes,
-// n rows: out = g_n (exp(v - lse_n) - [target_n == m]), in planes of the product's number whose
-// rows have room for one more.
+// v; v = act(v); v += beta * add[n][m]; out[n][m] = v (products of three planes: all fp32).
+// PLANES: v = alpha * sum + beta * add, + diagonal where n == m; out and add are planes of the
+// product's number, whose matrices have room for whole tiles (rows and columns up to the next
+// multiple of 256).  SYM: PLANES of a symmetric product (A and B the same matrix): only m >= n
+// is computed, and stored at both places.  STATS: m are rows, n classes: the maximum and the
+// sum of exp over a tile's classes of v = sum + bias[n], and the value at the row's target.
+// DLOGITS: m are classes, n rows: out = g_n (exp(v - lse_n) - [target_n == m]), in planes of the
+// product's number whose rows have room for one more.
 struct GemmEpi {
     float alpha = 1.f, beta = 0.f, diagonal = 0.f;
     const float *alpha_ptr = nullptr;  // in device memory

@@ -1,5 +1,5 @@
 // gemm_f32.cu -- the tensor-core product (gemm_kernel.cuh) of fp32 operands that are split
-// on their way to shared memory.
+// on their way to tensor memory.
 #define QCNN_UNIT_RECORDS
 #include "gemm_kernel.cuh"
 

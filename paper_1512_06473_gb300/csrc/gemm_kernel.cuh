@@ -17,17 +17,23 @@
 // free again after its last product.  Against 64 bits that is closer than a chain of fp32
 // multiply-adds (K = 4096: 1.4e-7 of the result).
 //
-// Roles (12 warps): 0 TMA, 1 (three planes: and 3) MMA, 2 TMEM, 4-11 drain and epilogue: two warps per TMEM
-// lane quarter, 16 columns in turn.
+// Roles (12 warps): 0 TMA, 1 (three planes: and 3) MMA, 2 TMEM, 4-11 drain and epilogue: two
+// warps per TMEM lane quarter, 16 columns in turn.
 //
-// GEN: A is fp32 of any stride and alignment (a layer's weights), split on its way, so that
-// a product bound by A's bytes (few rows n) reads them once and writes no planes.  It comes
-// to shared memory by TMA (warp 2), or where its rows are off the 16-byte alignment by
-// cp.async of the warps that split it, 12-15; these store the planes to TMEM as the MMAs' A
+// GEN (20 warps): A is fp32 of any stride and alignment (a layer's weights), split on its way,
+// so that a product bound by A's bytes (few rows n) reads them once and writes no planes.  It
+// comes to shared memory by TMA (warp 2), or where its rows are off the 16-byte alignment by
+// cp.async of the warps that split it, 12-19; these store the planes to TMEM as the MMAs' A
 // operand.  Shared memory then carries per stage of 32 terms and 128 columns 32 KB for the
 // copies, 24 KB of B's planes and 48 KB that the twelve MMAs read, 832 clocks of its bandwidth
 // to the 888 of the MMAs.  (With A's planes in shared memory and B split by the same warps it
 // was 1664, and the kernel took 3,500: 115 us for 128 rows of 9216 -> 4096.)
+//
+// Measured, of 6.67 TB/s copied and 1,946 (a long run: 1,742) TFLOP/s of bf16: 4096 x 4096 ->
+// 8192 in bf16 with GELU and residual 168 us, 1,640 TFLOP/s (tensor cores, at the power limit);
+// GEN, 8192 -> 19456: 12 rows 114 us, 5.6 TB/s (the memory and the split), 128 rows 164 us, 1,490
+// TFLOP/s (six products; tensor cores); 128 x 9216 -> 4096 56 us, of which 46 are the product at
+// that rate on the 128 CTAs that 32 tiles make.
 #pragma once
 
 #include "gemm.cuh"
@@ -87,9 +93,9 @@ struct Tile {
     int q;               // problem
     int mt, nt, kb0, kb1, group;
 };
-// Unit u of a launch, of the terms of CTA `share` of a cluster (or of the unit's group).  Neighbouring units are a
-// patch of `group` row tiles, whose operands the L2 then holds.  SYM: row tiles from the
-// diagonal on.
+// Unit u of a launch, of the terms of CTA `share` of a cluster (or of the unit's group).
+// Neighbouring units are a patch of `group` row tiles, whose operands the L2 then holds.  SYM:
+// row tiles from the diagonal on.
 template <int KIND, int CG>
 __device__ __forceinline__ Tile tile_of(const GemmArgs &g, int u, int share) {
     Tile t;
@@ -610,9 +616,10 @@ __global__ void __launch_bounds__(GEN ? kGenThreads : 384, 1) gemm_kernel(const 
     constexpr bool DRAIN = P == 3;   // a block's sum at a time
     // Rings of stages, and as many warps that issue MMAs, each with a ring and an accumulator of
     // its own, which take the accumulators in turn: a block's each, or (g.stay: tiles of one
-    // block, or of two and 128 columns, which have an accumulator each) a tile's.  (A warp's waits come back behind the MMAs that it has
-    // issued: one alone left the tensor core idle between accumulators, 1,204 clocks per block
-    // of 888.  And a ring has one consumer: a wait for a phase two ahead passes at once.)
+    // block, or of two and 128 columns, which have an accumulator each) a tile's.  (A warp's
+    // waits come back behind the MMAs that it has issued: one alone left the tensor core idle
+    // between accumulators, 1,204 clocks per block of 888.  And a ring has one consumer: a wait
+    // for a phase two ahead passes at once.)
     constexpr int RINGS = DRAIN ? 2 : 1;
     constexpr int ACC = GEN ? 128 : kAccCols;
     extern __shared__ __align__(128) unsigned char smem_raw[];
@@ -1183,7 +1190,8 @@ struct GemmKernel {
         qcnn_status rc = allow_smem(reinterpret_cast<const void *>(k));
         if (rc != QCNN_OK) return rc;
         const int cluster = CG * g.cl;
-        return launch_k(k, dim3(ctas), dim3(GEN ? kGenThreads : 384), smem, st, dim3(cluster > 1 ? cluster : 0, 1, 1), g);
+        return launch_k(k, dim3(ctas), dim3(GEN ? kGenThreads : 384), smem, st,
+                        dim3(cluster > 1 ? cluster : 0, 1, 1), g);
     }
 };
 

@@ -10,7 +10,8 @@
 //   B, by every CTA for itself;
 //   X = B X of the slice, eight columns per warp at a time, in place;
 // in fp32 multiply-adds.  It is taken where that is estimated to be sooner done than the
-// products (ortho_small_plan).
+// products (ortho_small_plan): 18 x 36 in 26 us, 65 as products; 31 x 512 in fp32 37 and 73; 48
+// x 1024 69 and 79; 62 x 326 the same.  Bound by the latency of a step's parts, 5 us.
 #include "ortho_small.cuh"
 
 #include <algorithm>

@@ -433,8 +433,8 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
                              wo.plane, 1};
         if (p.keep) {
             float *const part = a.dbias ? s.db : nullptr;
-            rc = launch_pdl(Ct % 4 ? dl_kernel<false> : dl_kernel<true>, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0, st, s.logits, s.rows, N, Ct,
-                            s.dl, P, pz, zplane, part, p.slab);
+            rc = launch_pdl(Ct % 4 ? dl_kernel<false> : dl_kernel<true>, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0,
+                            st, s.logits, s.rows, N, Ct, s.dl, P, pz, zplane, part, p.slab);
             if (rc == QCNN_OK && a.dbias)
                 rc = launch_column_join(s.db, p.slabs, Ct, Ct, inv, a.dbias, st);
         } else {
