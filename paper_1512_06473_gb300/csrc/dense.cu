@@ -152,17 +152,31 @@ qcnn_status few_rows_of(const FewRows &f, cudaStream_t st) {
 // part[slab][cols].  A CTA takes 128 columns x a slab: a warp a row, a lane four
 // columns: neighbours (VEC), or 32 apart, so that rows off the 8- or 16-byte alignment are
 // read and written by neighbouring lanes too (3001 x 5003 in bf16 41 us with the lane's four
-// next to each other).
-template <typename T, bool VEC>
+// next to each other).  JOBS: CTAs past dz's copy the other operands that need it, a launch less
+// (backward of 128 x 4096 -> 4096 in fp32 69 us, 71 apart; with the copies' code in it, dz of 3001
+// x 5003 alone takes 10 us more).
+template <typename T, bool VEC, bool JOBS>
 __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, const T *pre, long long ldp,
                                                  int N, int Ct, int act, unsigned short *out, int planes,
-                                                 long long ldo, long long plane, float *part, int slab) {
+                                                 long long ldo, long long plane, float *part, int slab, int slabs,
+                                                 PlanesJob j0, PlanesJob j1) {
     __shared__ float red[8][128];
     grid_dep_sync();
+    int slab_at = blockIdx.y, tile = blockIdx.x;
+    if constexpr (JOBS) {
+        const int tiles = (Ct + 127) / 128, other = (int)blockIdx.x - tiles * slabs;
+        if (other >= 0) {
+            if (other < j0.blocks) planes_part<T>(j0, other);
+            else planes_part<T>(j1, other - j0.blocks);
+            return;
+        }
+        slab_at = (int)blockIdx.x / tiles;
+        tile = (int)blockIdx.x - slab_at * tiles;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int GAP = VEC ? 1 : 32;
-    const int own = VEC ? lane * 4 : lane, c = blockIdx.x * 128 + own;
-    const int r1 = min(N, ((int)blockIdx.y + 1) * slab);
+    const int own = VEC ? lane * 4 : lane, c = tile * 128 + own;
+    const int r1 = min(N, (slab_at + 1) * slab);
     float sum[4] = {};
     auto load4 = [&](const T *p, float (&v)[4]) {
         if (VEC && c + 4 <= Ct) {
@@ -181,7 +195,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, co
     };
     if (c < Ct) {
 #pragma unroll 4
-        for (int r = (int)blockIdx.y * slab + warp; r < r1; r += 8) {
+        for (int r = slab_at * slab + warp; r < r1; r += 8) {
             float v[4];
             load4(dy + (long long)r * lddy + c, v);
             if (act != QCNN_ACT_NONE) {
@@ -215,12 +229,12 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, co
 #pragma unroll
     for (int j = 0; j < 4; ++j) red[warp][own + j * GAP] = sum[j];
     __syncthreads();
-    const int t = threadIdx.x, col = blockIdx.x * 128 + t;
+    const int t = threadIdx.x, col = tile * 128 + t;
     if (t < 128 && col < Ct) {
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) v += red[w][t];
-        part[(long long)blockIdx.y * Ct + col] = v;
+        part[(long long)slab_at * Ct + col] = v;
     }
 }
 
@@ -401,16 +415,16 @@ qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, cons
     g.b = GemmOperand{x, ldx, 0, 0};
     const int P = bf16 ? 1 : 3;
     const long long pitch = pad8(Cs);
+    PlanesJob jobs[2];
     if (s.x) {
-        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, nullptr, nullptr, 0, st);
-        if (rc != QCNN_OK) return rc;
+        jobs[0] = planes_job(x, bf16, N, Cs, ldx, P, s.x);
         g.b = GemmOperand{s.x, pitch, N * pitch, 0};
     }
     if (s.w) {
-        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, nullptr, nullptr, 0, st);
-        if (rc != QCNN_OK) return rc;
+        jobs[1] = planes_job(W, bf16, Ct, Cs, ldw, P, s.w);
         g.a = GemmOperand{s.w, pitch, Ct * pitch, 0};
     }
+    if ((rc = launch_planes(jobs[0], jobs[1], bf16, st)) != QCNN_OK) return rc;
     return launch_gemm(p.g, &g, 1, st);
 }
 
@@ -458,8 +472,18 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
     const long long pz = pad8(Ct), pc = pad8(Cs);
     const int P = bf16 ? 1 : 3;
     GemmOperand z{dy, lddy, 0, 0}, xo{x, ldx, 0, 1}, wo{W, ldw, 0, 1};
+    PlanesJob jobs[2];
+    if (x_copy) {
+        jobs[0] = planes_job(x, bf16, N, Cs, ldx, P, s.x);
+        xo = GemmOperand{s.x, pc, N * pc, 1};
+    }
+    if (w_copy) {
+        jobs[1] = planes_job(W, bf16, Ct, Cs, ldw, P, s.w);
+        wo = GemmOperand{s.w, pc, Ct * pc, 1};
+    }
     if (dz || dbias) {
-        const dim3 grid(cdiv(Ct, 128), p.slabs);
+        const int copies = jobs[0].blocks + jobs[1].blocks, tiles = cdiv(Ct, 128);
+        const dim3 grid = copies ? dim3(tiles * p.slabs + copies) : dim3(tiles, p.slabs);
         float *const part = !dbias ? nullptr : p.slabs > 1 ? s.db : dbias;
         const int e = bf16 ? 2 : 4;
         const auto vec_ok = [&](const void *q, long long ld) {
@@ -467,31 +491,21 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
         };
         const bool vec = vec_ok(dy, lddy) && (act == QCNN_ACT_NONE || vec_ok(pre, ldp));
         unsigned short *const out = static_cast<unsigned short *>(s.dz);
-        const auto launch = [&](auto k, auto *type) {
+        const auto launch = [&](auto *type) {
             using T = std::remove_pointer_t<decltype(type)>;
+            const auto k = copies ? (vec ? dz_kernel<T, true, true> : dz_kernel<T, false, true>)
+                                  : (vec ? dz_kernel<T, true, false> : dz_kernel<T, false, false>);
             return launch_pdl(k, grid, dim3(256), 0, st, static_cast<const T *>(dy), lddy,
                               static_cast<const T *>(pre), ldp, N, Ct, act, out, P, pz, (long long)N * pz, part,
-                              p.slab);
+                              p.slab, p.slabs, jobs[0], jobs[1]);
         };
-        if (bf16)
-            rc = launch(vec ? dz_kernel<unsigned short, true> : dz_kernel<unsigned short, false>,
-                        static_cast<unsigned short *>(nullptr));
-        else
-            rc = launch(vec ? dz_kernel<float, true> : dz_kernel<float, false>, static_cast<float *>(nullptr));
+        rc = bf16 ? launch(static_cast<unsigned short *>(nullptr)) : launch(static_cast<float *>(nullptr));
         if (rc != QCNN_OK) return rc;
         if (dbias && p.slabs > 1 && (rc = launch_column_join(s.db, p.slabs, Ct, Ct, nullptr, dbias, st)) != QCNN_OK)
             return rc;
         if (dz) z = GemmOperand{s.dz, pz, (long long)N * pz, 0};
-    }
-    if (x_copy) {
-        rc = launch_planes(x, bf16, N, Cs, ldx, P, s.x, nullptr, nullptr, 0, st);
-        if (rc != QCNN_OK) return rc;
-        xo = GemmOperand{s.x, pc, N * pc, 1};
-    }
-    if (w_copy) {
-        rc = launch_planes(W, bf16, Ct, Cs, ldw, P, s.w, nullptr, nullptr, 0, st);
-        if (rc != QCNN_OK) return rc;
-        wo = GemmOperand{s.w, pc, Ct * pc, 1};
+    } else if ((rc = launch_planes(jobs[0], jobs[1], bf16, st)) != QCNN_OK) {
+        return rc;
     }
     GemmProblem g[2];
     const int type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;

@@ -108,62 +108,11 @@ GemmLaunch launcher(const GemmPlan &p) {
 }
 
 // --------------------------------------------------------------- planes
-// A warp takes pieces of rows, a lane eight columns at a time: two 16-byte loads (or eight
-// of an element), a 16-byte store per plane.
-constexpr int kPieceCols = 1024;
 template <typename T>
-__global__ void __launch_bounds__(256) planes_kernel(const T *src, long long all, int per_row, int cols,
-                                                     long long ld, int planes, unsigned short *dst,
-                                                     unsigned short *kept, long long plane,
-                                                     const long long *classes, int Ct, int vec) {
+__global__ void __launch_bounds__(256) planes_kernel(PlanesJob j0, PlanesJob j1) {
     grid_dep_sync();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long pitch = (cols + 7) / 8 * 8;
-    for (long long i = (long long)blockIdx.x * 8 + warp; i < all; i += (long long)gridDim.x * 8) {
-        const long long r = i / per_row;
-        const int first = (int)(i - r * per_row) * kPieceCols, end = min(cols, first + kPieceCols);
-        const bool in = !kept || (unsigned long long)classes[r] < (unsigned long long)Ct;
-        const T *s = src + r * ld;
-#pragma unroll 2
-        for (int c = first + lane * 8; c < end; c += 256) {
-            float v[8];
-            if (vec && c + 8 <= cols) {
-                if constexpr (sizeof(T) == 4) {
-                    const float4 a = *reinterpret_cast<const float4 *>(s + c);
-                    const float4 b = *reinterpret_cast<const float4 *>(s + c + 4);
-                    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-                } else {
-                    const uint4 a = *reinterpret_cast<const uint4 *>(s + c);
-                    const unsigned w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        v[2 * j] = __uint_as_float(w[j] << 16);
-                        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[j] = 0.f;
-                    if (c + j < cols) {
-                        if constexpr (sizeof(T) == 4) v[j] = s[c + j];
-                        else v[j] = bf16_to_float(s[c + j]);
-                    }
-                }
-            }
-            unsigned w[3][4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                if (p >= planes) break;
-                const uint4 q = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
-                const long long o = p * plane + r * pitch + c;
-                if (dst) *reinterpret_cast<uint4 *>(dst + o) = q;
-                if (kept) *reinterpret_cast<uint4 *>(kept + o) = in ? q : make_uint4(0, 0, 0, 0);
-            }
-        }
-    }
+    if ((int)blockIdx.x < j0.blocks) planes_part<T>(j0, blockIdx.x);
+    else planes_part<T>(j1, blockIdx.x - j0.blocks);
 }
 
 }  // namespace
@@ -356,19 +305,28 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     return launcher(plan)(&g, ctas, smem, st);
 }
 
-qcnn_status launch_planes(const void *src, int bf16, long long rows, int cols, long long ld, int planes,
-                          void *dst, void *kept, const long long *classes, int Ct, cudaStream_t st) {
-    const int per_row = cdiv(cols, kPieceCols);
-    const long long all = rows * per_row, plane = rows * pad8(cols);
-    const int grid = (int)std::min<long long>((all + 7) / 8, (long long)num_sms() * 8);
-    const int vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
-    unsigned short *d = static_cast<unsigned short *>(dst), *k = static_cast<unsigned short *>(kept);
-    if (bf16)
-        return launch_pdl(planes_kernel<unsigned short>, dim3(grid), dim3(256), 0, st,
-                          static_cast<const unsigned short *>(src), all, per_row, cols, ld, planes, d, k, plane,
-                          classes, Ct, vec);
-    return launch_pdl(planes_kernel<float>, dim3(grid), dim3(256), 0, st, static_cast<const float *>(src), all,
-                      per_row, cols, ld, planes, d, k, plane, classes, Ct, vec);
+PlanesJob planes_job(const void *src, int bf16, long long rows, int cols, long long ld, int planes, void *dst,
+                     void *kept, const long long *classes, int Ct) {
+    PlanesJob j;
+    j.src = src;
+    j.per_row = cdiv(cols, kPieceCols);
+    j.all = rows * j.per_row;
+    j.cols = cols;
+    j.ld = ld;
+    j.planes = planes;
+    j.dst = static_cast<unsigned short *>(dst);
+    j.kept = static_cast<unsigned short *>(kept);
+    j.plane = rows * pad8(cols);
+    j.classes = classes;
+    j.Ct = Ct;
+    j.vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
+    j.blocks = (int)std::min<long long>((j.all + 7) / 8, (long long)num_sms() * 8);
+    return j;
+}
+qcnn_status launch_planes(const PlanesJob &a, const PlanesJob &b, int bf16, cudaStream_t st) {
+    const dim3 grid(a.blocks + b.blocks);
+    if (!grid.x) return QCNN_OK;
+    return launch_pdl(bf16 ? planes_kernel<unsigned short> : planes_kernel<float>, grid, dim3(256), 0, st, a, b);
 }
 
 }  // namespace qcnn

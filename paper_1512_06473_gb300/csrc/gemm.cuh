@@ -102,8 +102,19 @@ inline long long pad256(long long v) { return (v + 255) / 256 * 256; }
 // src [rows][cols] (fp32 or bf16, row stride ld) -> bf16 planes [planes][rows][pad8(cols)],
 // rows * pad8(cols) elements apart, to dst (null: not) and to kept (null: not), there with
 // zeros in the rows whose class index in `classes` is outside [0, Ct).
-qcnn_status launch_planes(const void *src, int bf16, long long rows, int cols, long long ld, int planes,
-                          void *dst, void *kept, const long long *classes, int Ct, cudaStream_t st);
+struct PlanesJob {
+    const void *src = nullptr;
+    unsigned short *dst = nullptr, *kept = nullptr;
+    const long long *classes = nullptr;
+    long long all = 0, ld = 0, plane = 0;  // all: pieces of rows, per_row of them each
+    int per_row = 0, cols = 0, planes = 0, Ct = 0, vec = 0;
+    int blocks = 0;  // CTAs of 256 threads; 0: nothing to do
+};
+PlanesJob planes_job(const void *src, int bf16, long long rows, int cols, long long ld, int planes, void *dst,
+                     void *kept = nullptr, const long long *classes = nullptr, int Ct = 0);
+constexpr int kPieceCols = 1024;
+// One launch of two of them, of one type.
+qcnn_status launch_planes(const PlanesJob &a, const PlanesJob &b, int bf16, cudaStream_t st);
 
 }  // namespace qcnn
 
@@ -173,6 +184,59 @@ __device__ __forceinline__ unsigned short float_to_bf16(float v) {
 __device__ __forceinline__ float load_as(const void *p, int type, long long o) {
     return type == GEMM_T_F32 ? static_cast<const float *>(p)[o]
                               : bf16_to_float(static_cast<const unsigned short *>(p)[o]);
+}
+
+// CTA `block` of a job.  A warp takes pieces of rows, a lane eight columns at a time: two 16-byte
+// loads (or eight of an element), a 16-byte store per plane.
+template <typename T>
+__device__ __forceinline__ void planes_part(const PlanesJob &j, int block) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cols = j.cols;
+    const long long pitch = (cols + 7) / 8 * 8;
+    for (long long i = (long long)block * 8 + warp; i < j.all; i += (long long)j.blocks * 8) {
+        const long long r = i / j.per_row;
+        const int first = (int)(i - r * j.per_row) * kPieceCols, end = min(cols, first + kPieceCols);
+        const bool in = !j.kept || (unsigned long long)j.classes[r] < (unsigned long long)j.Ct;
+        const T *s = static_cast<const T *>(j.src) + r * j.ld;
+#pragma unroll 2
+        for (int c = first + lane * 8; c < end; c += 256) {
+            float v[8];
+            if (j.vec && c + 8 <= cols) {
+                if constexpr (sizeof(T) == 4) {
+                    const float4 a = *reinterpret_cast<const float4 *>(s + c);
+                    const float4 b = *reinterpret_cast<const float4 *>(s + c + 4);
+                    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+                } else {
+                    const uint4 a = *reinterpret_cast<const uint4 *>(s + c);
+                    const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        v[2 * k] = __uint_as_float(w[k] << 16);
+                        v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = 0.f;
+                    if (c + k < cols) {
+                        if constexpr (sizeof(T) == 4) v[k] = s[c + k];
+                        else v[k] = bf16_to_float(s[c + k]);
+                    }
+                }
+            }
+            unsigned w[3][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) planes3(v[2 * k], v[2 * k + 1], w[0][k], w[1][k], w[2][k]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                if (p >= j.planes) break;
+                const uint4 q = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+                const long long o = p * j.plane + r * pitch + c;
+                if (j.dst) *reinterpret_cast<uint4 *>(j.dst + o) = q;
+                if (j.kept) *reinterpret_cast<uint4 *>(j.kept + o) = in ? q : make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
 }
 
 }  // namespace qcnn

@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(1024) stats_join_kernel(const float2 *stats, i
 template <bool VEC>
 __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const float4 *rows, int N, int Ct,
                                                  unsigned short *out, int planes, long long ldo, long long plane,
-                                                 float *part, int slab) {
+                                                 float *part, const float *scale, int slab) {
     __shared__ float red[8][128];
     grid_dep_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) v += red[w][t];
-        part[(long long)blockIdx.y * Ct + col] = v;
+        part[(long long)blockIdx.y * Ct + col] = scale ? *scale * v : v;
     }
 }
 
@@ -334,7 +334,7 @@ XentSpace carve_xent(const XentPlan &p, int N, int Cs, int Ct, int dtype, bool g
         s.kept = c.array<unsigned short>(P * N * pc);
         s.dl = c.array<unsigned short>(P * N * pad8(p.piece));
         if (p.keep) {
-            s.db = c.array<float>((size_t)p.slabs * Ct);
+            if (p.slabs > 1) s.db = c.array<float>((size_t)p.slabs * Ct);
         } else {
             s.db = c.array<float>((size_t)p.dl.n_tiles * 2 * p.piece);
             if (p.piece < Ct) s.dx = c.array<float>((size_t)N * Cs);
@@ -370,16 +370,17 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
     const int P = bf16 ? 1 : 3;
     const long long pc = pad8(Cs);
     GemmOperand xo{a.x, a.ldx, 0, 0}, wo{a.W, a.ldw, 0, 0};
+    PlanesJob jobs[2];
     if (s.x || s.kept) {
-        rc = launch_planes(a.x, bf16, N, Cs, a.ldx, P, s.x, s.kept, reinterpret_cast<const long long *>(a.targets),
-                           Ct, st);
-        if (rc != QCNN_OK) return rc;
+        jobs[0] = planes_job(a.x, bf16, N, Cs, a.ldx, P, s.x, s.kept, reinterpret_cast<const long long *>(a.targets),
+                             Ct);
         if (s.x) xo = GemmOperand{s.x, pc, N * pc, 0};
     }
     if (s.w) {
-        if ((rc = launch_planes(a.W, bf16, Ct, Cs, a.ldw, P, s.w, nullptr, nullptr, 0, st)) != QCNN_OK) return rc;
+        jobs[1] = planes_job(a.W, bf16, Ct, Cs, a.ldw, P, s.w);
         wo = GemmOperand{s.w, pc, Ct * pc, 0};
     }
+    if ((rc = launch_planes(jobs[0], jobs[1], bf16, st)) != QCNN_OK) return rc;
     const GemmOperand xk{s.kept, pc, N * pc, 1};
     RowOut ro{a.targets, a.dloss, a.loss, a.lse, s.rows, s.inv, N, Ct};
     const int type = bf16 ? GEMM_T_BF16 : GEMM_T_F32;
@@ -432,10 +433,11 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         const GemmOperand wp{static_cast<const uint8_t *>(wo.p) + c0 * wo.ld * (bf16 || s.w ? 2 : 4), wo.ld,
                              wo.plane, 1};
         if (p.keep) {
-            float *const part = a.dbias ? s.db : nullptr;
+            // (of one slab the sums are db: no launch to join them)
+            float *const part = a.dbias && p.slabs > 1 ? s.db : a.dbias;
             rc = launch_pdl(Ct % 4 ? dl_kernel<false> : dl_kernel<true>, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0,
-                            st, s.logits, s.rows, N, Ct, s.dl, P, pz, zplane, part, p.slab);
-            if (rc == QCNN_OK && a.dbias)
+                            st, s.logits, s.rows, N, Ct, s.dl, P, pz, zplane, part, p.slabs > 1 ? nullptr : inv, p.slab);
+            if (rc == QCNN_OK && p.slabs > 1 && a.dbias)
                 rc = launch_column_join(s.db, p.slabs, Ct, Ct, inv, a.dbias, st);
         } else {
             GemmProblem d;
