@@ -387,7 +387,7 @@ qcnn_status qcnn_dense_forward(const void *x, long long ldx, int N, int Cs, cons
         return QCNN_ERR_INVALID_ARG;
     if (N == 0) return QCNN_OK;
     const bool bf16 = dtype == QCNN_BF16;
-    const bool xa = tma_ok(x, ldx, dtype), wa = tma_ok(W, ldw, dtype);
+    const bool xa = tma_ok(x, ldx, dtype), wa = weights_ok(W, ldw, dtype);
     const ForwardPlan p = plan_forward(N, Cs, Ct, dtype, wa);
     const ForwardSpace s = carve_forward(p, N, Cs, Ct, dtype, xa, wa, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);

@@ -75,17 +75,43 @@ qcnn_status set_operand(const GemmOperand &o, int P, bool gen, int rows, int row
 
 // The map of an fp32 A: boxes of 32 terms x 128 rows, or of 32 rows x 32 terms where the rows
 // are contiguous.
-qcnn_status raw_map(const GemmOperand &o, int rows, int k, CUtensorMap *map) {
+qcnn_status raw_map(const void *p, long long inner, long long outer, long long row_bytes, unsigned box_x,
+                    unsigned box_y, bool swizzle, CUtensorMap *map) {
     const EncodeTiled enc = encode_tiled();
     if (!enc) return QCNN_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)(o.mn ? rows : k), (cuuint64_t)(o.mn ? k : rows)};
-    const cuuint64_t strides[1] = {(cuuint64_t)o.ld * 4};
-    const cuuint32_t box[2] = {32, o.mn ? 32u : (cuuint32_t)kMT}, steps[2] = {1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(o.p), dims, strides, box,
-                           steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           o.mn ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+    const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+    const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {box_x, box_y}, steps[2] = {1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(p), dims, strides, box, steps,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? QCNN_OK : cuda_status(cudaErrorInvalidValue);
+}
+// Maps and way of an fp32 A (RawWay).
+qcnn_status set_raw(const GemmOperand &o, int rows, int k, GemmArgs *g) {
+    ProblemArgs &p = g->p[0];
+    const char *const base = static_cast<const char *>(o.p);
+    const long long inner = o.mn ? rows : k, outer = o.mn ? k : rows;
+    g->raw_bytes = kGenWarps * 4096;
+    p.a.way = RAW_WORDS;
+    if (reinterpret_cast<uintptr_t>(base) % 16) return QCNN_OK;
+    if (o.ld % 4 == 0) {
+        p.a.way = RAW_BOXES;
+        return raw_map(base, inner, outer, o.ld * 4, 32, o.mn ? 32 : kMT, !o.mn, &p.map_a);
+    }
+    if (outer < 4) return QCNN_OK;  // (each map has rows)
+    p.a.way = RAW_SHIFTED;
+    g->raw_bytes = (unsigned)align_up(4 * (o.mn ? kShiftedPartMn : kShiftedPart), 128);
+    for (int i = 0; i < 4; ++i) {
+        // row i, i + 4, ...: from the boundary before row i on, which is in the matrix
+        const long long at = i * o.ld * 4;
+        g->shift[i] = (int)(at % 16 / 4);
+        const qcnn_status rc = raw_map(base + at / 16 * 16, g->shift[i] + inner, (outer - i + 3) / 4, o.ld * 16,
+                                       o.mn ? 132 : 36, o.mn ? 8 : 32, false, i ? &g->map_raw[i - 1] : &p.map_a);
+        if (rc != QCNN_OK) return rc;
+    }
+    return QCNN_OK;
 }
 
 long long tiles_of(int kind, int m_tiles, int n_tiles, int per) {
@@ -256,8 +282,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
             p.a.mn = s.a.mn;
             p.a.src = static_cast<const float *>(s.a.p);
             p.a.ld = s.a.ld;
-            p.a.vec = reinterpret_cast<uintptr_t>(s.a.p) % 16 == 0 && s.a.ld % 4 == 0;
-            if (p.a.vec && (rc = raw_map(s.a, s.m, s.k, &p.map_a)) != QCNN_OK) return rc;
+            if ((rc = set_raw(s.a, s.m, s.k, &g)) != QCNN_OK) return rc;
         } else if ((rc = set_operand(s.a, P, gen, kMT, s.m, s.k, &p.a, &p.map_a)) != QCNN_OK) {
             return rc;
         }
@@ -290,13 +315,12 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
     g.bn = plan.bn;
     g.b_off = a_bytes;  // (multiples of 1024: 128 rows; 64 rows of 128 bytes)
     g.stage = (unsigned)align_up(a_bytes + b_bytes, 1024);
-    const size_t raw_stage = kGenWarps * 4096;
     g.S = (int)std::min<size_t>(gen ? kGenStages : kStagesMax, (kSmemMax - 1024) / g.stage);
     if (gen) {  // raw copies: by TMA as many stages as there is room for
-        g.raw = (int)std::min<size_t>(kRawMax, (kSmemMax - 1024 - g.S * (size_t)g.stage) / raw_stage) & ~1;
-        if (!g.p[0].a.vec) g.raw = 2 * kRawSlots;
+        g.raw = (int)std::min<size_t>(kRawMax, (kSmemMax - 1024 - g.S * (size_t)g.stage) / g.raw_bytes) & ~1;
+        if (g.p[0].a.way == RAW_WORDS) g.raw = 2 * kRawSlots;
     }
-    const size_t raw = g.raw * raw_stage;
+    const size_t raw = g.raw * (size_t)g.raw_bytes;
     // (three planes: two rings, each with room for a block's planes)
     if (P == 3) g.S &= ~1;
     if (g.S < (gen ? 2 : P == 3 ? 6 : P)) return QCNN_ERR_UNSUPPORTED;

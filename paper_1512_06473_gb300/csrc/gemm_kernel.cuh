@@ -22,7 +22,7 @@
 //
 // GEN (20 warps): A is fp32 of any stride and alignment (a layer's weights), split on its way,
 // so that a product bound by A's bytes (few rows n) reads them once and writes no planes.  It
-// comes to shared memory by TMA (warp 2), or where its rows are off the 16-byte alignment by
+// comes to shared memory by TMA (warp 2), or where its base is off the 16-byte alignment by
 // cp.async of the warps that split it, 12-19; these store the planes to TMEM as the MMAs' A
 // operand.  Shared memory then carries per stage of 32 terms and 128 columns 32 KB for the
 // copies, 24 KB of B's planes and 48 KB that the twelve MMAs read, 832 clocks of its bandwidth
@@ -51,6 +51,8 @@ constexpr int kGenWarps = 4;      // that split a block's A
 constexpr int kGenThreads = 640;
 constexpr int kRawSlots = 3;      // GEN: blocks of raw copies, 4 KB per warp each
 constexpr int kRawMax = 10;       // the same by TMA, at most
+// A shifted block: [4][32 rows][36 words], or rows contiguous [4][8 terms][132 words].
+constexpr unsigned kShiftedPart = 32 * 36 * 4, kShiftedPartMn = 8 * 132 * 4;
 constexpr int kGenCols = 48;      // TMEM columns of a stage's A: 3 planes x 32 terms
 constexpr int kGenStages = 4;     // (at most (512 - 2 * 128) / 48)
 constexpr unsigned kPolls = 1u << 22;
@@ -63,8 +65,12 @@ struct OpArgs {
     unsigned long long desc;       // descriptor without the address
     const float *src;              // GEN
     long long ld;
-    int vec;                       // GEN: 16-byte copies possible
+    int way;                       // GEN: RawWay
 };
+// How GEN's fp32 comes: element by element; in boxes; or, where only the base is on 16 bytes, in
+// a box for every fourth row (their distance is a multiple of 16 bytes again), four words wider
+// and read from the word where the row begins.
+enum RawWay { RAW_WORDS = 0, RAW_BOXES = 1, RAW_SHIFTED = 2 };
 struct ProblemArgs {
     CUtensorMap map_a, map_b;
     OpArgs a, b;
@@ -75,7 +81,10 @@ struct ProblemArgs {
 struct GemmArgs {
     ProblemArgs p[2];
     int count, units, bn, S;
-    int raw;                // GEN: stages of raw copies
+    int raw;                // GEN: stages of raw copies, of raw_bytes each
+    unsigned raw_bytes;
+    int shift[4];           // GEN: words that rows r mod 4 begin after a 16-byte boundary
+    CUtensorMap map_raw[3];  // GEN, shifted: of rows 1, 2, 3 mod 4 (map_a: 0)
     int cl;                 // CTAs of a cluster that share a tile's terms (CG 1)
     int groups;             // shares whose sums stay apart (OUT, cl 1)
     int stay;               // three planes: a tile's sum stays in TMEM
@@ -820,7 +829,7 @@ __global__ void __launch_bounds__(GEN ? kGenThreads : 384, 1) gemm_kernel(const 
         // (no wait for the kernel before: the weights are the caller's, complete before the
         // first kernel of this call)
         const ProblemArgs &p = g.p[0];
-        if (p.a.vec && elect_one()) {
+        if (p.a.way != RAW_WORDS && elect_one()) {
             // (two rings, as the stages: each has one group of warps that reads it)
             const int R = g.raw / 2;
             int slot = 0;
@@ -834,13 +843,21 @@ __global__ void __launch_bounds__(GEN ? kGenThreads : 384, 1) gemm_kernel(const 
                     const int at = (int)ring * R + slot;
                     if (!(ok = wait_one(sh, &sh.raw_empty[at], par ^ 1))) break;
                     uint64_t *const full = &sh.raw_full[at];
-                    arrive_expect(full, kGenWarps * 4096);
-                    const unsigned d = smem_addr(smem) + g.S * g.stage + at * (kGenWarps * 4096);
-                    if (mn) {
+                    const unsigned d = smem_addr(smem) + g.S * g.stage + at * g.raw_bytes;
+                    if (p.a.way == RAW_SHIFTED) {
+                        const unsigned part = mn ? kShiftedPartMn : kShiftedPart;
+                        const int x = mn ? m0 : kb * BK, y = (mn ? kb * BK : m0) / 4;
+                        arrive_expect(full, 4 * part);
+                        tma_load_2d(d, &p.map_a, x, y, full);
+#pragma unroll
+                        for (int i = 1; i < 4; ++i) tma_load_2d(d + i * part, &g.map_raw[i - 1], x, y, full);
+                    } else if (mn) {
+                        arrive_expect(full, kGenWarps * 4096);
 #pragma unroll
                         for (int i = 0; i < kGenWarps; ++i)
                             tma_load_2d(d + i * 4096, &p.map_a, m0 + i * 32, kb * BK, full);
                     } else {
+                        arrive_expect(full, kGenWarps * 4096);
                         tma_load_2d(d, &p.map_a, kb * BK, m0, full);
                     }
                     ++issued;
@@ -1055,19 +1072,24 @@ __global__ void __launch_bounds__(GEN ? kGenThreads : 384, 1) gemm_kernel(const 
         // one before: 4.4 TB/s of weights).  A warp has 32 rows (its TMEM lanes) x 32 terms of a
         // block.  Rows of k: [32][32] floats, the 16-byte pieces of a row permuted (TMA's
         // 128-byte swizzle) so that eight neighbouring rows read from all banks; rows of m: [32
-        // terms][32].  Where TMA cannot read the rows, the warp copies its own 32 lines of 128
+        // terms][32].  Where TMA cannot read the matrix, the warp copies its own 32 lines of 128
         // bytes, element by element (a lane each: neighbours), so that no barrier lies between
-        // copying and splitting.
+        // copying and splitting (12 rows of 4097 -> 19456: 109 us, with shifted boxes 66).
         set_registers<88, false>();
         const int quarter = warp & 3, ring = (warp - 12) >> 2;
         const ProblemArgs &p = g.p[0];
-        const bool mn = p.a.mn, vec = p.a.vec;
+        const bool mn = p.a.mn, vec = p.a.way != RAW_WORDS, shifted = p.a.way == RAW_SHIFTED;
         const long long ld = p.a.ld;
         const int slots = vec ? g.raw / 2 : kRawSlots;
-        // (TMA: a block is the four warps' parts one after another)
+        // (TMA: a block is the four warps' parts one after another; shifted: this lane's row, or
+        // its first word of the terms 0 mod 4)
+        const unsigned own = !shifted ? quarter * 4096
+                             : mn     ? (quarter * 32 + lane) * 4
+                                      : (lane & 3) * kShiftedPart + (quarter * 8 + (lane >> 2)) * 144 +
+                                        g.shift[lane & 3] * 4;
         const unsigned raw = smem_addr(smem) + g.S * g.stage +
-                             (vec ? (ring * slots * kGenWarps + quarter) * 4096 : (warp - 12) * kRawSlots * 4096);
-        const unsigned raw_step = vec ? kGenWarps * 4096 : 4096;
+                             (vec ? ring * slots * g.raw_bytes + own : (warp - 12) * kRawSlots * 4096);
+        const unsigned raw_step = vec ? g.raw_bytes : 4096;
         // this group's blocks (kb0: the block)
         struct Walk {
             int round, u;
@@ -1121,7 +1143,17 @@ __global__ void __launch_bounds__(GEN ? kGenThreads : 384, 1) gemm_kernel(const 
             }
             const unsigned r = raw + rslot * raw_step;
             float v[32];
-            if (mn) {
+            if (shifted && mn) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    asm volatile("ld.shared.f32 %0, [%1];\n"
+                                 : "=f"(v[i])
+                                 : "r"(r + (i & 3) * kShiftedPartMn + (i >> 2) * 528 + g.shift[i & 3] * 4));
+            } else if (shifted) {  // (no two lanes in a bank: rows four apart lie 36 words apart)
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(r + i * 4));
+            } else if (mn) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
                     asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(r + i * 128 + lane * 4));

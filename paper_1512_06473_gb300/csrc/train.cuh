@@ -20,6 +20,11 @@ inline bool tma_ok(const void *p, long long ld, int dtype) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * type_bytes(dtype) % 16 == 0;
 }
 
+// Weights that a product reads without a pass over them: fp32 of any row distance.
+inline bool weights_ok(const void *p, long long ld, int dtype) {
+    return dtype == QCNN_BF16 ? tma_ok(p, ld, dtype) : reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
+
 // A workspace, carved in order.  With no base it only counts.
 struct Carver {
     uint8_t *base;
@@ -52,12 +57,12 @@ inline double few_rows_clocks(int N, int Cs, int Ct, bool bf16) {
     return 5000.0 + (N <= 4 ? elements * (bf16 ? 2.0 : 4.0) / 3400.0 : elements / (bf16 ? 540.0 : 400.0));
 }
 // Whether that is sooner done than the product g.  Up to four rows it always is (4 x 4096 ->
-// 19456 in fp32 51 us and the product 57), and where W is off TMA's alignment (8 x 4097 -> 19456
-// 72 and 104).  With eight it depends on the size of the weights: 8 x 4096 -> 1000 in fp32 8.3
+// 19456 in fp32 51 us and the product 57), and where a product cannot read W as it is (8 x 4097 ->
+// 19456, fp32 off 16 bytes 72 and 104, bf16 69 and 112).  With eight it depends on the size of the weights: 8 x 4096 -> 1000 in fp32 8.3
 // us and the product 14.4, in bf16 6.9 and 9.4; -> 4096 24.6 and 21.2, 19.4 and 11.5; -> 19456 83
 // and 58, 50 and 29.  (7000: the product's launches.)
-inline bool few_rows_sooner(int N, int Cs, int Ct, bool bf16, bool w_aligned, const GemmPlan &g) {
-    if (N <= 4 || N > kFewRows || !w_aligned) return N <= kFewRows;
+inline bool few_rows_sooner(int N, int Cs, int Ct, bool bf16, bool w_direct, const GemmPlan &g) {
+    if (N <= 4 || N > kFewRows || !w_direct) return N <= kFewRows;
     const double bytes = (double)Cs * Ct * (bf16 ? 2.0 : 4.0);
     return few_rows_clocks(N, Cs, Ct, bf16) < std::max(g.score, bytes / 3400.0) + 7000.0;
 }

@@ -361,7 +361,7 @@ struct XentCall {
 qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes, cudaStream_t st) {
     const int N = a.N, Cs = a.Cs, Ct = a.Ct;
     const bool bf16 = a.dtype == QCNN_BF16;
-    const bool xa = tma_ok(a.x, a.ldx, a.dtype), wa = tma_ok(a.W, a.ldw, a.dtype);
+    const bool xa = tma_ok(a.x, a.ldx, a.dtype), wa = weights_ok(a.W, a.ldw, a.dtype);
     const XentPlan p = plan_xent(N, Cs, Ct, a.dtype, wa, a.grad);
     const XentSpace s = carve_xent(p, N, Cs, Ct, a.dtype, a.grad, xa, wa, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);

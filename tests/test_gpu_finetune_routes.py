@@ -44,6 +44,25 @@ def test_fp32_weights_split_on_their_way(N, Cs, Ct, pad, off):
     _no_timeouts()
 
 
+@pytest.mark.parametrize("ld", [1, 2, 3, 5, 30, 33, 66, 131, 1062])
+@pytest.mark.parametrize("rows", [1, 3, 4, 5, 31, 33, 127, 130, 515])
+def test_fp32_rows_off_16_bytes(rows, ld):
+    """Weights whose base is on 16 bytes and whose rows are not, read along and across them; what
+    lies between the rows (NaN) goes nowhere."""
+    g = _gen(26)
+    for cols in {ld, max(1, ld - 3)}:
+        w = _normal(g, rows, cols, pad=ld - cols)
+        if ld > cols:
+            w.as_strided((rows - 1, ld - cols), (ld, 1), w.storage_offset() + cols).fill_(math.nan)
+        x, dy = _normal(g, 40, cols), _normal(g, 40, rows)
+        want, _, ey, _ = plain.dense_forward(x, w)
+        _near(q.dense_forward(x, w), want, ey)
+        dx = q.dense_backward(dy, x, w, need_dweight=False, need_dbias=False)[0]
+        want, bound = plain.dense_backward(dy, x, w)
+        _near(dx, want[0], bound[0])
+    _no_timeouts()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N,Cs,Ct", [(16, 512, 2000), (64, 128, 20000), (300, 64, 9000), (512, 96, 4100),
                                      (1000, 40, 1000), (2050, 24, 3001), (8, 1024, 9001), (5, 2048, 9000),
