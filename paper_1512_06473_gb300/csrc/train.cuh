@@ -58,9 +58,9 @@ inline double few_rows_clocks(int N, int Cs, int Ct, bool bf16) {
 }
 // Whether that is sooner done than the product g.  Up to four rows it always is (4 x 4096 ->
 // 19456 in fp32 51 us and the product 57), and where a product cannot read W as it is (8 x 4097 ->
-// 19456, fp32 off 16 bytes 72 and 104, bf16 69 and 112).  With eight it depends on the size of the weights: 8 x 4096 -> 1000 in fp32 8.3
-// us and the product 14.4, in bf16 6.9 and 9.4; -> 4096 24.6 and 21.2, 19.4 and 11.5; -> 19456 83
-// and 58, 50 and 29.  (7000: the product's launches.)
+// 19456, fp32 off 16 bytes 72 and 104, bf16 69 and 112).  With eight it depends on the size of
+// the weights: 8 x 4096 -> 1000 in fp32 8.3 us and the product 14.4, in bf16 6.9 and 9.4; -> 4096
+// 24.6 and 21.2, 19.4 and 11.5; -> 19456 83 and 58, 50 and 29.  (7000: the product's launches.)
 inline bool few_rows_sooner(int N, int Cs, int Ct, bool bf16, bool w_direct, const GemmPlan &g) {
     if (N <= 4 || N > kFewRows || !w_direct) return N <= kFewRows;
     const double bytes = (double)Cs * Ct * (bf16 ? 2.0 : 4.0);
