@@ -66,7 +66,8 @@ def test_fp32_rows_off_16_bytes(rows, ld):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N,Cs,Ct", [(16, 512, 2000), (64, 128, 20000), (300, 64, 9000), (512, 96, 4100),
                                      (1000, 40, 1000), (2050, 24, 3001), (8, 1024, 9001), (5, 2048, 9000),
-                                     (320, 72, 999)])
+                                     (320, 72, 999), (1, 300, 40001), (3, 64, 16384), (38, 40, 16390),
+                                     (70, 33, 8200), (2, 8, 4096)])
 def test_xent_kept_and_not(N, Cs, Ct, dtype):
     """Logits kept for the call or computed again, in products with few and many shares."""
     g, x, w, b, t = _xent_case(N, Cs, Ct, dtype, seed=23)
