@@ -300,6 +300,9 @@ XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool wa, bool grad) {
     double kept = 0.0, again = p.stats.score + 5000.0;
     const XentPlan q = plan_kept(N, Cs, Ct, bf16, wa, grad, &kept);
     if (!bf16) again += pass_clocks((double)Ct * Cs * 10.0);
+    // (of few rows the product reads weights at 4.2 TB/s, the stream of few rows at 6.3: 1 x 4096
+    // -> 31273 in bf16 47 us kept, 67 not)
+    if (q.few) again = std::max(again, (double)Ct * Cs * (bf16 ? 2.0 : 4.0) / 2200.0 + 5000.0);
     if (grad) again += cdiv(Ct, p.piece) * (p.dl.score + p.dx.score + p.dw.score);
     return kept <= again ? q : p;
 }
