@@ -439,7 +439,8 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
             // (of one slab the sums are db: no launch to join them)
             float *const part = a.dbias && p.slabs > 1 ? s.db : a.dbias;
             rc = launch_pdl(Ct % 4 ? dl_kernel<false> : dl_kernel<true>, dim3(cdiv(Ct, 128), p.slabs), dim3(256), 0,
-                            st, s.logits, s.rows, N, Ct, s.dl, P, pz, zplane, part, p.slabs > 1 ? nullptr : inv, p.slab);
+                            st, s.logits, s.rows, N, Ct, s.dl, P, pz, zplane, part,
+                            p.slabs > 1 ? nullptr : inv, p.slab);
             if (rc == QCNN_OK && p.slabs > 1 && a.dbias)
                 rc = launch_column_join(s.db, p.slabs, Ct, Ct, inv, a.dbias, st);
         } else {

@@ -110,7 +110,8 @@ def test_workspace_of_any_alignment(dtype):
             grad = torch.empty(nb.value + 1, dtype=torch.uint8, device="cuda")[:nb.value]
             t = torch.randint(0, Ct, (N,), generator=g, device="cuda")
             for pad, off in ((0, 0), (8, 0), (1, 1)):
-                x, w = _normal(g, N, Cs, dtype=dtype, pad=pad, off=off), _normal(g, Ct, Cs, dtype=dtype, pad=pad, off=off)
+                x = _normal(g, N, Cs, dtype=dtype, pad=pad, off=off)
+                w = _normal(g, Ct, Cs, dtype=dtype, pad=pad, off=off)
                 want, _, ey, _ = plain.dense_forward(x, w)
                 _near(q.dense_forward(x, w, workspace=fwd), want, ey)
                 w = w * (1 / math.sqrt(Cs))
