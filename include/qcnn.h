@@ -712,6 +712,13 @@ qcnn_status qcnn_dense_backward(const void *dy, long long lddy, const void *x, l
  */
 qcnn_status qcnn_xent_workspace_size(int N, int Cs, int Ct, int dtype, int aligned, int grad,
                                      size_t *bytes);
+/* qcnn_xent_route_info -- how the calls below (grad: qcnn_xent_grad) go about these sizes with
+ * aligned matrices.  info receives: [0] 1 where the logits are kept, 0 where they are
+ * computed in pieces; [1] classes of a piece of the gradient, [2] of the last one, [3]
+ * pieces; [4] CTAs that share the terms (classes) of a tile of dx in the last piece, [5]
+ * classes of a share (both 0 without grad).  Errors are those of
+ * qcnn_xent_workspace_size, and QCNN_ERR_INVALID_ARG for N = 0. */
+qcnn_status qcnn_xent_route_info(int N, int Cs, int Ct, int dtype, int grad, int info[6]);
 qcnn_status qcnn_xent_forward(const void *x, long long ldx, int N, int Cs, const void *W,
                               long long ldw, int Ct, const float *bias, const int64_t *targets,
                               float *loss, float *lse, int dtype, void *workspace,

@@ -30,7 +30,8 @@ __all__ = ["lut_build", "fc_forward", "conv_forward", "conv_pack_codes", "maxpoo
            "model_info", "load_model",
            "ConvLayer", "FCLayer", "PoolLayer", "Net", "launch_count", "QcnnError", "load",
            "set_debug", "debug_checks", "device_check", "smem_load_rate",
-           "dense_forward", "dense_backward", "xent_forward", "xent_grad", "orthogonalize"]
+           "dense_forward", "dense_backward", "xent_forward", "xent_grad", "xent_route",
+           "orthogonalize"]
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -760,4 +761,4 @@ def load_model(blob_or_path, device="cuda", stream=None) -> LoadedNet:
 
 
 from .finetune import (dense_backward, dense_forward, orthogonalize, xent_forward,  # noqa: E402
-                       xent_grad)
+                       xent_grad, xent_route)

@@ -121,6 +121,7 @@ _SIGS = {
                             [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p,
                              c_size_t, c_void_p]),
     "qcnn_xent_workspace_size": (c_int, [c_int] * 6 + [ctypes.POINTER(c_size_t)]),
+    "qcnn_xent_route_info": (c_int, [c_int] * 5 + [ctypes.POINTER(c_int)]),
     "qcnn_xent_forward": (c_int, [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int,
                                   c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_size_t,
                                   c_void_p]),

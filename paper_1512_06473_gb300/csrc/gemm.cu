@@ -42,13 +42,10 @@ EncodeTiled encode_tiled() {
     return f;
 }
 
-// Terms of a stage: 64 of one plane; GEN (A in fp32): 32 of B's three planes.
-int block_k(bool gen) { return gen ? 32 : 64; }
-
 // An operand of `rows` rows (this CTA's part of a tile); rows_all x k is its matrix.
 qcnn_status set_operand(const GemmOperand &o, int P, bool gen, int rows, int rows_all, int k, OpArgs *a,
                         CUtensorMap *map) {
-    const int bk = block_k(gen), box_planes = gen ? P : 1;
+    const int bk = gemm_block_k(gen ? GEMM_F32 : P), box_planes = gen ? P : 1;
     a->mn = o.mn;
     a->group_bytes = box_planes * bk * 128;
     a->bytes = o.mn ? cdiv(rows, 64) * a->group_bytes : (unsigned)box_planes * rows * bk * 2;
@@ -152,7 +149,7 @@ __global__ void __launch_bounds__(256) planes_kernel(PlanesJob j0, PlanesJob j1)
 static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int max_groups, int sms) {
     GemmPlan best;
     const bool gen = planes == GEMM_F32;
-    const int P = gen ? 3 : planes, bk = block_k(gen), kblocks = std::max(1, cdiv(k, bk));
+    const int P = gen ? 3 : planes, bk = gemm_block_k(planes), kblocks = std::max(1, cdiv(k, bk));
     static const int tiles[5] = {16, 32, 64, 128, 256};
     const int mmas = (P == 1 ? 1 : P == 2 ? 3 : 6) * bk / 16;
     const bool whole = kind == GEMM_STATS || kind == GEMM_DLOGITS;  // (no shares)
@@ -294,7 +291,7 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
         p.m = s.m;
         p.n = s.n;
         p.k = s.k;
-        p.kblocks = std::max(1, cdiv(s.k, block_k(gen)));
+        p.kblocks = std::max(1, cdiv(s.k, gemm_block_k(plan.planes)));
         p.m_tiles = cdiv(s.m, kMT * cg);
         p.n_tiles = cdiv(s.n, plan.bn);
         p.kb_per_split = plan.splits > 1 || plan.groups > 1 ? plan.kb_per_split : p.kblocks;
@@ -303,6 +300,10 @@ qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *ps, int count, 
         p.e.pair = (pairs(s.e.out, s.e.out_type, s.e.ldo, s.m) ? 1 : 0) |
                    (pairs(s.e.pre, s.e.out_type, s.e.ldp, s.m) ? 2 : 0) |
                    (pairs(s.e.add, s.e.add_type, s.e.lda, s.m) ? 4 : 0);
+        // (a plan for another k: a share without terms would never have its sum)
+        const int shares = plan.splits * plan.groups;
+        if ((shares - 1) * (long long)p.kb_per_split >= p.kblocks || shares * (long long)p.kb_per_split < p.kblocks)
+            return QCNN_ERR_UNSUPPORTED;
         const long long tiles = tiles_of(plan.kind, p.m_tiles, p.n_tiles, plan.bn / (kMT * cg));
         if (tiles * plan.groups > (1 << 27)) return QCNN_ERR_UNSUPPORTED;
         p.units = (int)tiles;  // (of a group)

@@ -70,6 +70,8 @@ struct GemmProblem {
 // planes: 1, 2, 3, or GEMM_F32 (A in fp32, split on its way to the tensor cores; B in
 // three planes).
 constexpr int GEMM_F32 = 0;
+// Terms of a block: 64 of one plane; GEMM_F32: 32 of B's three planes.
+constexpr int gemm_block_k(int planes) { return planes == GEMM_F32 ? 32 : 64; }
 
 struct GemmPlan {
     int planes = 1, kind = 0, cg = 1;
@@ -91,7 +93,8 @@ bool gemm_together(const GemmPlan &a, int m_a, int n_a, int k_a, const GemmPlan 
 
 // One launch of one or two products of the same kind and planes (the second fills
 // the SMs that the first one's last tiles leave idle); both with `plan`'s tile, unsplit
-// if there are two.
+// if there are two.  A plan with shares is of the product's own k: one that has shares without
+// terms is refused.
 qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *p, int count, cudaStream_t st);
 
 // Smallest multiple of 8 elements: rows of 16-byte multiples.

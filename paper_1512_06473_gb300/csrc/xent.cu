@@ -306,6 +306,11 @@ XentPlan plan_xent(int N, int Cs, int Ct, int dtype, bool wa, bool grad) {
     if (grad) again += cdiv(Ct, p.piece) * (p.dl.score + p.dx.score + p.dw.score);
     return kept <= again ? q : p;
 }
+// dx += dl W of a piece of cn classes.  (The last piece has fewer terms: shares of a whole one's
+// would leave CTAs of a cluster without any.)
+GemmPlan plan_dx(const XentPlan &p, int N, int Cs, int cn) {
+    return cn == p.piece ? p.dx : plan_gemm(p.dx.planes, GEMM_OUT, Cs, N, cn);
+}
 struct XentSpace {
     float *inv = nullptr, *logits = nullptr, *part = nullptr, *target_logit = nullptr, *db = nullptr, *dx = nullptr;
     float4 *rows = nullptr;
@@ -480,7 +485,7 @@ qcnn_status run_xent(const XentCall &a, void *workspace, size_t workspace_bytes,
         q.e.out = last ? a.dx : s.dx;
         q.e.ldo = last ? a.lddx : Cs;
         q.e.out_type = last ? type : GEMM_T_F32;
-        if ((rc = launch_gemm(p.dx, &q, 1, st)) != QCNN_OK) return rc;
+        if ((rc = launch_gemm(plan_dx(p, N, Cs, cn), &q, 1, st)) != QCNN_OK) return rc;
         GemmProblem v;
         v.a = xk;
         v.b = GemmOperand{s.dl, pz, zplane, 1};
@@ -520,6 +525,21 @@ qcnn_status qcnn_xent_workspace_size(int N, int Cs, int Ct, int dtype, int align
         const XentPlan p = plan_xent(N, Cs, Ct, dtype, wa, grad != 0);
         *bytes = std::max(*bytes, carve_xent(p, N, Cs, Ct, dtype, grad != 0, aligned, aligned, nullptr).bytes);
     }
+    return QCNN_OK;
+}
+
+qcnn_status qcnn_xent_route_info(int N, int Cs, int Ct, int dtype, int grad, int info[6]) {
+    if (!info || N <= 0 || Cs <= 0 || Ct <= 0 || !dtype_ok(dtype)) return QCNN_ERR_INVALID_ARG;
+    const XentPlan p = plan_xent(N, Cs, Ct, dtype, true, grad != 0);
+    info[0] = p.keep;
+    info[1] = grad ? p.piece : Ct;
+    info[2] = Ct - (cdiv(Ct, info[1]) - 1) * info[1];
+    info[3] = grad ? cdiv(Ct, p.piece) : 1;
+    info[4] = info[5] = 0;
+    if (!grad) return QCNN_OK;
+    const GemmPlan last = plan_dx(p, N, Cs, info[2]);
+    info[4] = last.splits;
+    info[5] = last.kb_per_split * gemm_block_k(last.planes);
     return QCNN_OK;
 }
 

@@ -162,6 +162,21 @@ def _xent_args(x, weight, targets, bias):
     return code, ldx, ldw, N, Cs, Ct, t, b
 
 
+def xent_route(N: int, Cs: int, Ct: int, dtype=torch.float32, grad: bool = True):
+    """How xent_grad (or, grad False, xent_forward) goes about these sizes
+    (qcnn_xent_route_info): a dict with "kept" (the logits), classes of a "piece" and of the
+    "last" one, "pieces", and "shares" of a tile's classes in the last piece's dx, of
+    "share_classes" each (both 0 without grad)."""
+    if dtype not in _DTYPES:
+        raise TypeError(f"dtype must be float32 or bfloat16, got {dtype}")
+    info = (ctypes.c_int * 6)()
+    _lib.check(load().qcnn_xent_route_info(N, Cs, Ct, _DTYPES[dtype], int(grad), info),
+               "qcnn_xent_route_info")
+    d = dict(zip(("kept", "piece", "last", "pieces", "shares", "share_classes"), list(info)))
+    d["kept"] = bool(d["kept"])
+    return d
+
+
 def xent_forward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
                  bias: Optional[torch.Tensor] = None, workspace=None, stream=None):
     """Softmax cross entropy of the logits x weight^T + bias: (loss [N], lse [N]), float32,
