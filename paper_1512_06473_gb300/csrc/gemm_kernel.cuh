@@ -531,14 +531,17 @@ __device__ __forceinline__ void stats16(RunningSum &s, int n0, int target, float
             if (v[i] != v[i]) s.sum = v[i];
         return;
     }
-    const float shift = top * kLog2e;
+    // (subtracted before it is scaled: top * log2(e) overflows where a whole block is masked by the
+    // lowest value, and rounded it would leave exp(0) off 1, again with each block)
+    const float2 down = make_float2(-top, -top), scale = make_float2(kLog2e, kLog2e);
     float a0 = 0.f, a1 = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-        a0 += ex2(fmaf(v[i], kLog2e, -shift));
-        a1 += ex2(fmaf(v[i + 1], kLog2e, -shift));
+        const float2 d = __fmul2_rn(__fadd2_rn(make_float2(v[i], v[i + 1]), down), scale);
+        a0 += ex2(d.x);
+        a1 += ex2(d.y);
     }
-    s.sum = (s.top == -INFINITY ? s.sum : s.sum * ex2(fmaf(s.top, kLog2e, -shift))) + (a0 + a1);
+    s.sum = (s.top == -INFINITY ? s.sum : s.sum * ex2((s.top - top) * kLog2e)) + (a0 + a1);
     s.top = top;
 }
 
