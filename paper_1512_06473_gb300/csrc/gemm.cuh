@@ -33,7 +33,7 @@ enum GemmType { GEMM_T_F32 = 0, GEMM_T_BF16 = 1 };
 // multiple of 256).  SYM: PLANES of a symmetric product (A and B the same matrix): only m >= n
 // is computed, and stored at both places.  STATS: m are rows, n classes: the maximum and the
 // sum of exp over a tile's classes of v = sum + bias[n], and the value at the row's target.
-// DLOGITS: m are classes, n rows: out = g_n (exp(v - lse_n) - [target_n == m]), in planes of the
+// DLOGITS: m are classes, n rows: out = g_n (row_share(v) - [target_n == m]), in planes of the
 // product's number whose rows have room for one more.
 struct GemmEpi {
     float alpha = 1.f, beta = 0.f, diagonal = 0.f;
@@ -53,7 +53,7 @@ struct GemmEpi {
     float2 *stats = nullptr;           // [tile along n][half][m]
     const long long *targets = nullptr;
     float *target_logit = nullptr;     // [m]
-    const float4 *rows = nullptr;      // [n]: lse, g, target (bits), -
+    const float4 *rows = nullptr;      // [n]: maximum, g, target (bits), log2 of the sum of exp
     int class0 = 0;                    // first class of this piece
     float *col_part = nullptr;         // DLOGITS: sums over a tile's rows, [tile along n][half][ld_col]
     long long ld_col = 0;
@@ -175,6 +175,10 @@ __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+// The softmax of a logit of a row (GemmEpi's rows).
+__device__ __forceinline__ float row_share(float logit, const float4 &row) {
+    return ex2(fmaf(logit - row.x, kLog2e, -row.w));
 }
 
 __device__ __forceinline__ float bf16_to_float(unsigned short v) {

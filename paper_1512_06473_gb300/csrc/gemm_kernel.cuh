@@ -555,7 +555,7 @@ __device__ __forceinline__ void dlogits16(const GemmEpi &e, bool full, int m_end
     for (int i = 0; i < 16; ++i) {
         const float4 r = rows[i];
         const int target = __float_as_int(r.z);
-        float p = ex2((v[i] + bias - r.x) * kLog2e);
+        float p = row_share(v[i] + bias, r);
         if (target == c) p -= 1.f;
         // (a row without a class is zero, whatever its logits are)
         v[i] = target >= 0 ? r.y * p : 0.f;

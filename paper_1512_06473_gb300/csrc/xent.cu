@@ -4,6 +4,10 @@
 //   l = x W^T + b;  lse_n = log sum_c exp l_nc;  loss_n = lse_n - l_n,t(n)
 //   dl = g_n (exp(l - lse_n) - [c == t(n)]);  dx = dl W;  dW = dl^T x;  db = sum_n dl
 //
+// lse_n = top + log(sum) is rounded where it is an output alone: loss_n is (top - l_n,t) + log(sum) and
+// exp(l - lse) is 2^((l - top) log2 e - log2(sum)).  (With lse in them, rows that the layer is sure of,
+// whose logits are large and whose losses small, had losses off by 2^-24 of the logit.)
+//
 // Two ways, by the estimated time of each (plan_xent):
 //   kept (the fp32 logits fit kPiece bytes): a product, a pass per row (lse, loss), and for the
 //     gradient a pass over the logits (dl, db) and two products.  It has products whose terms
@@ -69,10 +73,10 @@ struct RowOut {
 };
 __device__ __forceinline__ void finish_row(const RowOut &o, int n, float top, float sum, float target_logit) {
     const int t = class_of(o.targets, n, o.Ct);
-    const float lse = top + logf(sum);
-    o.lse[n] = lse;
-    o.loss[n] = t >= 0 ? lse - target_logit : 0.f;
-    if (o.rows) o.rows[n] = make_float4(lse, o.dloss ? o.dloss[n] : 1.f, __int_as_float(t), 0.f);
+    const float log_sum = logf(sum);
+    o.lse[n] = top + log_sum;
+    o.loss[n] = t >= 0 ? (top - target_logit) + log_sum : 0.f;
+    if (o.rows) o.rows[n] = make_float4(top, o.dloss ? o.dloss[n] : 1.f, __int_as_float(t), log2f(sum));
 }
 
 // Kept: a CTA per row of logits; one more counts the rows.  GROUPS: the logits come as
@@ -205,7 +209,7 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
             const float g = row.y;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p = ex2((v[j] - row.x) * kLog2e);
+                const float p = row_share(v[j], row);
                 // (a row without a class is zero, whatever its logits are)
                 v[j] = target >= 0 && c + j < Ct ? g * (target == c + j ? p - 1.f : p) : 0.f;
                 sum[j] += v[j];
