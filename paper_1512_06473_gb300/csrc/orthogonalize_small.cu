@@ -53,6 +53,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_small_kernel(const Args a) 
     extern __shared__ __align__(16) float smem_f[];
     __shared__ double2 norms[kThreads / 32 + 8];
     cg::cluster_group cluster = cg::this_cluster();
+    cluster.barrier_arrive();  // (this CTA runs: its shared memory may be written to)
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int p4 = a.p4, pp = p4 * p4;
@@ -78,6 +79,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_small_kernel(const Args a) 
         large += __shfl_xor_sync(0xffffffffu, large, o);
     }
     if (lane == 0) norms[warp] = make_double2(small, large);
+    cluster.barrier_wait();
     __syncthreads();
     if (tid == 0) {
         double2 s = norms[0];
