@@ -62,49 +62,62 @@ struct Pieces {
     int cols, per_row;
 };
 
-// Sums of squares by CTA: of values above 2^48 scaled by 2^-64, and of the others (whose
-// squares neither overflow nor, where they count beside eps, vanish).  A lane's run of up
-// to 64 squares is in fp32, the rest in fp64.
-constexpr float kLarge = 281474976710656.f, kLargeScale = 5.421010862427522e-20f;
+// Sums of squares by CTA, in fp64; a lane's run of up to 64 squares in fp32.  A run whose largest value
+// is above 2^48 or below 2^-40 is taken again, scaled by 2^-64 or 2^96: no square overflows, and none
+// vanishes or loses bits that the run's sum has (with eps 0 a matrix of subnormal values has its own
+// norm).  (With sums for the three ranges side by side 1000 x 4096 in fp32 is normalized in 35 us, 28.)
+constexpr float kLarge = 0x1p48f, kSmall = 0x1p-40f;
+__device__ __forceinline__ double add_lanes(double v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
 template <typename T>
-__global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, Pieces q, int vec, double2 *part) {
-    __shared__ double2 red[8];
+__global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, Pieces q, int vec, double *part) {
+    __shared__ double red[8];
     grid_dep_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    double dsmall = 0., dlarge = 0.;
+    double s = 0.;
     for (long long i = (long long)blockIdx.x * 8 + warp; i < q.all; i += (long long)gridDim.x * 8) {
         const long long r = i / q.per_row;
         const int first = (int)(i - r * q.per_row) * kPieceCols, end = min(q.cols, first + kPieceCols);
         const T *row = g + r * ldg;
-        float small = 0.f, large = 0.f;
+        float sum = 0.f, top = 0.f;
 #pragma unroll 4
         for (int c = first + lane * 8; c < end; c += 256) {
             float v[8];
             row8(row, c, end, vec, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool big = fabsf(v[j]) > kLarge;
-                const float w = big ? v[j] * kLargeScale : v[j];
-                large = fmaf(big ? w : 0.f, w, large);
-                small = fmaf(big ? 0.f : w, w, small);  // (NaN too)
+                sum = fmaf(v[j], v[j], sum);
+                top = fmaxf(top, fabsf(v[j]));
             }
         }
-        dsmall += small;
-        dlarge += large;
-    }
+        const bool large = top > kLarge;
+        if (large || (top < kSmall && top > 0.f)) {
+            const float scale = large ? 0x1p-64f : 0x1p96f;
+            sum = 0.f;
+#pragma unroll 1
+            for (int c = first + lane * 8; c < end; c += 256) {
+                float v[8];
+                row8(row, c, end, vec, v);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        dsmall += __shfl_xor_sync(0xffffffffu, dsmall, o);
-        dlarge += __shfl_xor_sync(0xffffffffu, dlarge, o);
+                for (int j = 0; j < 8; ++j) {
+                    const float x = v[j] * scale;
+                    sum = fmaf(x, x, sum);
+                }
+            }
+            s = fma((double)sum, large ? 0x1p128 : 0x1p-192, s);
+        } else {
+            s += sum;
+        }
     }
-    if (lane == 0) red[warp] = make_double2(dsmall, dlarge);
+    s = add_lanes(s);
+    if (lane == 0) red[warp] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) {
-            dsmall += red[i].x;
-            dlarge += red[i].y;
-        }
-        part[blockIdx.x] = make_double2(dsmall, dlarge);
+        for (int i = 1; i < 8; ++i) s += red[i];
+        part[blockIdx.x] = s;
     }
 }
 
@@ -112,30 +125,20 @@ __global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, Pi
 // every CTA adds the sums up in the same order.
 template <typename T>
 __global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, Pieces q, int vec,
-                                                    const double2 *part, int parts, float eps, int planes,
+                                                    const double *part, int parts, float eps, int planes,
                                                     unsigned short *dst, long long pitch, long long plane, T *out,
                                                     long long ldo) {
-    __shared__ double2 red[8];
+    __shared__ double red[8];
     grid_dep_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    double2 s = make_double2(0., 0.);
-    for (int i = threadIdx.x; i < parts; i += 256) {
-        s.x += part[i].x;
-        s.y += part[i].y;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
-        s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
-    }
+    double s = 0.;
+    for (int i = threadIdx.x; i < parts; i += 256) s += part[i];
+    s = add_lanes(s);
     if (lane == 0) red[warp] = s;
     __syncthreads();
     s = red[0];
-    for (int i = 1; i < 8; ++i) {
-        s.x += red[i].x;
-        s.y += red[i].y;
-    }
-    const double norm = sqrt(s.x + s.y * 340282366920938463463374607431768211456.0) + (double)eps;
+    for (int i = 1; i < 8; ++i) s += red[i];
+    const double norm = sqrt(s) + (double)eps;
     // (a norm of zero with eps zero: the matrix is zero; a factor above fp32's range, of tiny
     // matrices with a tiny eps, is taken in two: f2 is 1 otherwise)
     const double f = norm > 0. || norm != norm ? 1.0 / norm : 0.;
@@ -197,7 +200,7 @@ OrthoPlan plan_ortho(int m, int n, int dtype) {
     return o;
 }
 struct OrthoSpace {
-    double2 *norm;
+    double *norm;
     unsigned short *x[2], *a, *b;
     size_t bytes;
 };
@@ -205,7 +208,7 @@ OrthoSpace carve_ortho(const OrthoPlan &o, int m, int n, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     OrthoSpace s;
     const size_t xs = (size_t)o.P * pad256(m) * pad256(n), as = (size_t)o.P * pad256(o.p) * pad256(o.p);
-    s.norm = c.array<double2>(kNormBlocks);
+    s.norm = c.array<double>(kNormBlocks);
     s.x[0] = c.array<unsigned short>(xs);
     s.x[1] = c.array<unsigned short>(xs);
     s.a = c.array<unsigned short>(as);
