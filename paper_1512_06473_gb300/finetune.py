@@ -14,36 +14,42 @@ from typing import Optional, Sequence
 
 import torch
 
-from . import _empty, _lib, _scratch, _stream, _workspace
+from . import _device, _empty, _lib, _scratch, _stream, _workspace
 from ._lib import load
 
 _DTYPES = {torch.float32: _lib.F32, torch.bfloat16: _lib.BF16}
 _F32, _I64 = torch.float32, torch.int64
 
 
-def _dtype(t, name):
+def _first(t, name):
+    """The type code and the device of a call's first matrix; the others' devices are held to it."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    return code
+    dev = t.get_device()
+    if dev != _device():
+        raise ValueError(f"{name} must be on the current device, {_device()}, not on device {dev}")
+    return code, dev
 
 
-def _refuse(t, name, dtype, want):
-    """What is wrong with a tensor that should be a CUDA tensor of this type and shape."""
+def _refuse(t, name, dtype, dev, want):
+    """What is wrong with a tensor that should be a CUDA tensor of this type, device and shape."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on device {dev}, as the others, not on device {t.get_device()}")
     raise ValueError(f"{name} must be of shape {want}, columns next to each other and rows apart, "
                      f"got shape {tuple(t.shape)} with strides {t.stride()}")
 
 
 # (a call's host time is its own with small sizes: 0.7 us per matrix, 1.6 per new tensor)
-def _matrix(t, name, dtype, rows=None, cols=None):
+def _matrix(t, name, dtype, dev, rows=None, cols=None):
     """The distance between the rows of a matrix [rows, cols] (None: any)."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda:
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.get_device() == dev:
         shape = t.shape
         if len(shape) == 2:
             r, c = shape
@@ -54,13 +60,13 @@ def _matrix(t, name, dtype, rows=None, cols=None):
                         return ld
                     if r <= 1:
                         return c
-    _refuse(t, name, dtype, tuple("any" if v is None else v for v in (rows, cols)))
+    _refuse(t, name, dtype, dev, tuple("any" if v is None else v for v in (rows, cols)))
 
 
-def _vector(t, name, dtype, n):
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or \
+def _vector(t, name, dtype, dev, n):
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or t.get_device() != dev or \
             t.shape != (n,) or (n > 1 and t.stride(0) != 1):
-        _refuse(t, name, dtype, (n,))
+        _refuse(t, name, dtype, dev, (n,))
     return t.data_ptr()
 
 
@@ -90,24 +96,23 @@ def dense_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
     epilogue.  x [N, Cs], weight [Ct, Cs], bias [Ct] float32, residual [N, Ct]; act is
     "none", "relu", "gelu" (by erf) or "silu".  pre=True returns (y, z): z is what
     dense_backward needs."""
-    code = _dtype(x, "x")
+    code, dev = _first(x, "x")
     dt = x.dtype
-    ldx = _matrix(x, "x", dt)
+    ldx = _matrix(x, "x", dt, dev)
     N, Cs = x.shape
-    ldw = _matrix(weight, "weight", dt, None, Cs)
+    ldw = _matrix(weight, "weight", dt, dev, None, Cs)
     Ct = weight.shape[0]
-    b = None if bias is None else _vector(bias, "bias", _F32, Ct)
+    b = None if bias is None else _vector(bias, "bias", _F32, dev, Ct)
     r, ldr = (None, 0) if residual is None else \
-        (residual.data_ptr(), _matrix(residual, "residual", dt, N, Ct))
+        (residual.data_ptr(), _matrix(residual, "residual", dt, dev, N, Ct))
+    ldy = Ct if out is None else _matrix(out, "out", dt, dev, N, Ct)
     a = _act(act)
     lib = load()
     nb = _scratch(lib, "qcnn_dense_forward_workspace_size", N, Cs, Ct, code,
                   _aligned(code, x, ldx, weight, ldw))
     ws, wsb = _workspace(nb, x.device, workspace, stream) if nb else (None, 0)
     if out is None:
-        out, ldy = _new(x, (N, Ct), dt, stream), Ct
-    else:
-        ldy = _matrix(out, "out", dt, N, Ct)
+        out = _new(x, (N, Ct), dt, stream)
     z = _new(x, (N, Ct), dt, stream) if pre else None
     st = lib.qcnn_dense_forward(x.data_ptr(), ldx, N, Cs, weight.data_ptr(), ldw, Ct, b, a, r, ldr,
                                 out.data_ptr(), ldy, z.data_ptr() if pre else None, Ct, code,
@@ -123,17 +128,17 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     """The gradients (dx, dweight, dbias) of dense_forward for the gradient dy [N, Ct] of
     y, with pre = z (not needed for act "none"; for a ReLU without residual y will do).
     What is not needed is None.  The residual's gradient is dy itself."""
-    code = _dtype(dy, "dy")
+    code, dev = _first(dy, "dy")
     dt = dy.dtype
-    lddy = _matrix(dy, "dy", dt)
+    lddy = _matrix(dy, "dy", dt, dev)
     N, Ct = dy.shape
-    ldx = _matrix(x, "x", dt, N)
+    ldx = _matrix(x, "x", dt, dev, N)
     Cs = x.shape[1]
-    ldw = _matrix(weight, "weight", dt, Ct, Cs)
+    ldw = _matrix(weight, "weight", dt, dev, Ct, Cs)
     a = _act(act)
     if a and pre is None:
         raise ValueError(f"pre is required with act {act!r}")
-    p, ldp = (None, 0) if pre is None else (pre.data_ptr(), _matrix(pre, "pre", dt, N, Ct))
+    p, ldp = (None, 0) if pre is None else (pre.data_ptr(), _matrix(pre, "pre", dt, dev, N, Ct))
     lib = load()
     nb = _scratch(lib, "qcnn_dense_backward_workspace_size", N, Cs, Ct, code,
                   _aligned(code, x, ldx, weight, ldw))
@@ -152,14 +157,14 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
 
 
 def _xent_args(x, weight, targets, bias):
-    code = _dtype(x, "x")
-    ldx = _matrix(x, "x", x.dtype)
+    code, dev = _first(x, "x")
+    ldx = _matrix(x, "x", x.dtype, dev)
     N, Cs = x.shape
-    ldw = _matrix(weight, "weight", x.dtype, None, Cs)
+    ldw = _matrix(weight, "weight", x.dtype, dev, None, Cs)
     Ct = weight.shape[0]
-    t = _vector(targets, "targets", _I64, N)
-    b = None if bias is None else _vector(bias, "bias", _F32, Ct)
-    return code, ldx, ldw, N, Cs, Ct, t, b
+    t = _vector(targets, "targets", _I64, dev, N)
+    b = None if bias is None else _vector(bias, "bias", _F32, dev, Ct)
+    return code, dev, ldx, ldw, N, Cs, Ct, t, b
 
 
 def xent_route(N: int, Cs: int, Ct: int, dtype=torch.float32, grad: bool = True):
@@ -184,7 +189,7 @@ def xent_forward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
     row's target.  x [N, Cs], weight [Ct, Cs], targets [N] int64, bias [Ct] float32
     (-inf takes a class out).  A row with a negative target has loss 0.  The logits are
     not kept where they would be large."""
-    code, ldx, ldw, N, Cs, Ct, t, b = _xent_args(x, weight, targets, bias)
+    code, _, ldx, ldw, N, Cs, Ct, t, b = _xent_args(x, weight, targets, bias)
     lib = load()
     nb = _scratch(lib, "qcnn_xent_workspace_size", N, Cs, Ct, code,
                   _aligned(code, x, ldx, weight, ldw), 0)
@@ -204,8 +209,8 @@ def xent_grad(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
     """xent_forward with the gradients of sum(dloss * loss), or (dloss None) of the mean
     of the losses over the rows with a target: (loss, lse, dx [N, Cs], dweight [Ct, Cs],
     dbias [Ct] float32).  Rows with a negative target have gradient 0."""
-    code, ldx, ldw, N, Cs, Ct, t, b = _xent_args(x, weight, targets, bias)
-    d = None if dloss is None else _vector(dloss, "dloss", _F32, N)
+    code, dev, ldx, ldw, N, Cs, Ct, t, b = _xent_args(x, weight, targets, bias)
+    d = None if dloss is None else _vector(dloss, "dloss", _F32, dev, N)
     lib = load()
     nb = _scratch(lib, "qcnn_xent_workspace_size", N, Cs, Ct, code,
                   _aligned(code, x, ldx, weight, ldw), 1)
@@ -226,13 +231,13 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs: Optional[Sequence[flo
     """The update g [m, n] with its singular values brought near 1, by ``steps``
     Newton-Schulz steps X <- a X + (b A + c A A) X, A = X X^T, from X = g / (||g||_F +
     eps); coeffs (a, b, c), by default those of the Muon optimiser.  ``out`` may be g."""
-    code = _dtype(g, "g")
-    ldg = _matrix(g, "g", g.dtype)
+    code, dev = _first(g, "g")
+    ldg = _matrix(g, "g", g.dtype, dev)
     m, n = g.shape
     if out is None:
         out, ldo = _new(g, (m, n), g.dtype, stream), n
     else:
-        ldo = _matrix(out, "out", g.dtype, m, n)
+        ldo = _matrix(out, "out", g.dtype, dev, m, n)
     k = None
     if coeffs is not None:
         if len(coeffs) != 3:
