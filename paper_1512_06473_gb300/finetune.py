@@ -103,8 +103,7 @@ def dense_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
     ldw = _matrix(weight, "weight", dt, dev, None, Cs)
     Ct = weight.shape[0]
     b = None if bias is None else _vector(bias, "bias", _F32, dev, Ct)
-    r, ldr = (None, 0) if residual is None else \
-        (residual.data_ptr(), _matrix(residual, "residual", dt, dev, N, Ct))
+    ldr = 0 if residual is None else _matrix(residual, "residual", dt, dev, N, Ct)
     ldy = Ct if out is None else _matrix(out, "out", dt, dev, N, Ct)
     a = _act(act)
     lib = load()
@@ -114,7 +113,8 @@ def dense_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
     if out is None:
         out = _new(x, (N, Ct), dt, stream)
     z = _new(x, (N, Ct), dt, stream) if pre else None
-    st = lib.qcnn_dense_forward(x.data_ptr(), ldx, N, Cs, weight.data_ptr(), ldw, Ct, b, a, r, ldr,
+    st = lib.qcnn_dense_forward(x.data_ptr(), ldx, N, Cs, weight.data_ptr(), ldw, Ct, b, a,
+                                None if residual is None else residual.data_ptr(), ldr,
                                 out.data_ptr(), ldy, z.data_ptr() if pre else None, Ct, code,
                                 ws.data_ptr() if nb else None, wsb, _stream(stream))
     if st:
@@ -138,7 +138,7 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     a = _act(act)
     if a and pre is None:
         raise ValueError(f"pre is required with act {act!r}")
-    p, ldp = (None, 0) if pre is None else (pre.data_ptr(), _matrix(pre, "pre", dt, dev, N, Ct))
+    ldp = 0 if pre is None else _matrix(pre, "pre", dt, dev, N, Ct)
     lib = load()
     nb = _scratch(lib, "qcnn_dense_backward_workspace_size", N, Cs, Ct, code,
                   _aligned(code, x, ldx, weight, ldw))
@@ -146,7 +146,8 @@ def dense_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     dx = _new(dy, (N, Cs), dt, stream) if need_dx else None
     dw = _new(dy, (Ct, Cs), dt, stream) if need_dweight else None
     db = _new(dy, (Ct,), _F32, stream) if need_dbias else None
-    st = lib.qcnn_dense_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, weight.data_ptr(), ldw, p, ldp,
+    st = lib.qcnn_dense_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, weight.data_ptr(), ldw,
+                                 None if pre is None else pre.data_ptr(), ldp,
                                  N, Cs, Ct, a, dx.data_ptr() if need_dx else None, Cs,
                                  dw.data_ptr() if need_dweight else None, Cs,
                                  db.data_ptr() if need_dbias else None, code,

@@ -1,6 +1,6 @@
 """Tensors of several devices, or of one that is not the current device, are refused by the
-fine-tuning operators before anything is launched.  (Stand-ins for CUDA tensors: no GPU is
-needed.)"""
+fine-tuning operators before anything is launched; so is what is no tensor.  (Stand-ins for CUDA
+tensors: no GPU is needed.)"""
 import pytest
 import torch
 
@@ -49,3 +49,10 @@ def test_another_device_is_refused(name, args, more):
     # all on one device, but not the current one
     with pytest.raises(ValueError, match="device"):
         getattr(q, name)(**{n: _on(1, *shape, **kw) for n, shape, kw in args}, **more)
+
+@pytest.mark.parametrize("name,args,more", CALLS, ids=[c[0] for c in CALLS])
+def test_what_is_no_tensor_is_refused(name, args, more):
+    for bad in [a[0] for a in args]:
+        given = {n: [0.0] if n == bad else _on(0, *shape, **kw) for n, shape, kw in args}
+        with pytest.raises(TypeError, match=bad):
+            getattr(q, name)(**given, **more)
