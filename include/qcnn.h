@@ -650,10 +650,10 @@ qcnn_status qcnn_net_forward_host(const qcnn_layer *layers, int n_layers,
  * Arithmetic: bf16 operands are multiplied exactly and summed in fp32, each output
  * rounded to bf16 once.  fp32 operands are taken in three bf16 pieces, which hold all
  * their 24 bits, and summed in fp32, or (of few rows) multiplied as they are: results
- * are as close to the exact ones as those of fp32 multiply-adds.  A non-finite operand (or
- * one above 3.38e38) makes the outputs that it enters non-finite, NaN where plain
- * arithmetic would give an infinity.  Sums are in a fixed order: results repeat bit
- * for bit.
+ * are as close to the exact ones as those of fp32 multiply-adds.  A non-finite operand
+ * makes the outputs that it enters non-finite; of an infinite fp32 operand taken in
+ * pieces they are NaN where plain arithmetic (and calls of few rows) would give an
+ * infinity.  Sums are in a fixed order: results repeat bit for bit.
  *
  * Workspace: from the query, 256-byte aligned.  `aligned` says that every bf16 matrix
  * that is an input has a 16-byte aligned base and row distances that are multiples of

@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, long long lddy, co
                 unsigned w[3][2];
                 unsigned short *d = out + (long long)r * ldo + c;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+                for (int j = 0; j < 2; ++j)
+                    planes_of<sizeof(T) == 4>(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
 #pragma unroll
                 for (int i = 0; i < 3; ++i, d += plane) {
                     if (i >= planes) break;

@@ -125,15 +125,21 @@ qcnn_status launch_planes(const PlanesJob &a, const PlanesJob &b, int bf16, cuda
 namespace qcnn {
 
 // v = b0 + b1 (+ b2), bf16 pieces of two values each (low half: the first).  b0 is
-// rounded to nearest, the differences are exact; of three pieces b1 is cut off and b2
+// rounded to nearest (above bf16's largest finite value: to that; an infinity leaves an infinite b1,
+// so that no result of it is finite), the differences are exact; of three pieces b1 is cut off and b2
 // the rest, which has at most 8 bits: the sum is v, exactly, down to 2^-133 (bf16's
 // last bit).  Of two, b1 is rounded: 16 to 17 bits of v.
+__device__ __forceinline__ unsigned pack_bf16x2_finite(float lo, float hi) {
+    unsigned r;
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 __device__ __forceinline__ float2 bf16_rest(float v0, float v1, unsigned p) {
     return __ffma2_rn(make_float2(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)),
                       make_float2(-1.f, -1.f), make_float2(v0, v1));
 }
 __device__ __forceinline__ void planes3(float v0, float v1, unsigned &p0, unsigned &p1, unsigned &p2) {
-    p0 = pack_bf16x2(v0, v1);
+    p0 = pack_bf16x2_finite(v0, v1);
     const float2 r = bf16_rest(v0, v1, p0);
     const unsigned rx = __float_as_uint(r.x), ry = __float_as_uint(r.y);
     p1 = __byte_perm(rx, ry, 0x7632);
@@ -141,9 +147,15 @@ __device__ __forceinline__ void planes3(float v0, float v1, unsigned &p0, unsign
     p2 = __byte_perm(__float_as_uint(s.x), __float_as_uint(s.y), 0x7632);
 }
 __device__ __forceinline__ void planes2(float v0, float v1, unsigned &p0, unsigned &p1) {
-    p0 = pack_bf16x2(v0, v1);
+    p0 = pack_bf16x2_finite(v0, v1);
     const float2 r = bf16_rest(v0, v1, p0);
     p1 = pack_bf16x2(r.x, r.y);
+}
+// Two values in the pieces of a call's type: three in fp32 calls, one (a rounding) in bf16 calls.
+template <bool F32>
+__device__ __forceinline__ void planes_of(float v0, float v1, unsigned &p0, unsigned &p1, unsigned &p2) {
+    if constexpr (F32) planes3(v0, v1, p0, p1, p2);
+    else p0 = pack_bf16x2(v0, v1), p1 = p2 = 0;
 }
 
 // Activations and their derivatives (include/qcnn.h, qcnn_activation).
@@ -233,7 +245,7 @@ __device__ __forceinline__ void planes_part(const PlanesJob &j, int block) {
             }
             unsigned w[3][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) planes3(v[2 * k], v[2 * k + 1], w[0][k], w[1][k], w[2][k]);
+            for (int k = 0; k < 4; ++k) planes_of<sizeof(T) == 4>(v[2 * k], v[2 * k + 1], w[0][k], w[1][k], w[2][k]);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
                 if (p >= j.planes) break;

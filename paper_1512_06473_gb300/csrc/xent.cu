@@ -218,7 +218,10 @@ __global__ void __launch_bounds__(256) dl_kernel(const float *logits, const floa
             unsigned w[3][2];
             unsigned short *d = out + o;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) planes3(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+            for (int j = 0; j < 2; ++j) {
+                if (planes == 3) planes_of<true>(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+                else planes_of<false>(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+            }
             *reinterpret_cast<uint2 *>(d) = make_uint2(w[0][0], w[0][1]);
             if (planes == 3) {
                 *reinterpret_cast<uint2 *>(d + plane) = make_uint2(w[1][0], w[1][1]);
