@@ -166,8 +166,9 @@ def device_check(stream=None) -> int:
     """Synchronize the stream and return the debug build's device-check flags
     since the last check (QCNN_CHECK_CODE 1: a code >= K was read;
     QCNN_CHECK_TABLE 2: a table read outside the built table;
-    QCNN_CHECK_GLOBAL 4: a device-memory access outside its array), clearing
-    them.  Always 0 with the release build."""
+    QCNN_CHECK_GLOBAL 4: a device-memory access outside its array;
+    QCNN_CHECK_TIMEOUT 8: a wait inside a kernel gave up), clearing them.  The
+    release build records the last of these alone."""
     flags = ctypes.c_uint(0)
     st = load().qcnn_device_check(_stream(stream), ctypes.byref(flags))
     if st not in (_lib.OK, _lib.ERR_DEVICE_CHECK):

@@ -572,10 +572,6 @@ __device__ __forceinline__ void dlogits16(const GemmEpi &e, bool full, int m_end
 }
 
 // ---------------------------------------------------------------------- GEN
-__device__ __forceinline__ void cp_async16_part(unsigned dst, const void *src, unsigned bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes)
-                 : "memory");
-}
 __device__ __forceinline__ void cp_async4_part(unsigned dst, const void *src, unsigned bytes) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(bytes)
                  : "memory");

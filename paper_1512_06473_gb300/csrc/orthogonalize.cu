@@ -54,9 +54,9 @@ __device__ __forceinline__ void row8(const T *row, int c, int cols, bool vec, fl
     }
 }
 
-// Both passes over G: a warp takes pieces of rows (of at most kPieceCols columns), a lane
+// Both passes over G: a warp takes pieces of rows (of at most kNormCols columns), a lane
 // eight columns at a time.
-constexpr int kPieceCols = 2048;
+constexpr int kNormCols = 2048;
 struct Pieces {
     long long rows, all;  // rows, and rows x pieces of a row
     int cols, per_row;
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const T *g, long long ldg, Pi
     double s = 0.;
     for (long long i = (long long)blockIdx.x * 8 + warp; i < q.all; i += (long long)gridDim.x * 8) {
         const long long r = i / q.per_row;
-        const int first = (int)(i - r * q.per_row) * kPieceCols, end = min(q.cols, first + kPieceCols);
+        const int first = (int)(i - r * q.per_row) * kNormCols, end = min(q.cols, first + kNormCols);
         const T *row = g + r * ldg;
         float sum = 0.f, top = 0.f;
 #pragma unroll 4
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const T *g, long long ldg, P
     const float f2 = f > 1e30 ? 1e30f : 1.f, f1 = (float)(f > 1e30 ? f / 1e30f : f);
     for (long long i = (long long)blockIdx.x * 8 + warp; i < q.all; i += (long long)gridDim.x * 8) {
         const long long r = i / q.per_row;
-        const int first = (int)(i - r * q.per_row) * kPieceCols, end = min(q.cols, first + kPieceCols);
+        const int first = (int)(i - r * q.per_row) * kNormCols, end = min(q.cols, first + kNormCols);
         const T *row = g + r * ldg;
 #pragma unroll 2
         for (int c = first + lane * 8; c < end; c += 256) {
@@ -222,7 +222,7 @@ qcnn_status run_ortho(const T *G, long long ldg, int m, int n, int steps, const 
                       long long ldo, const OrthoPlan &o, const OrthoSpace &s, cudaStream_t st) {
     PdlScope pdl;
     const bool wide = m <= n;
-    const Pieces q{m, (long long)m * cdiv(n, kPieceCols), n, cdiv(n, kPieceCols)};
+    const Pieces q{m, (long long)m * cdiv(n, kNormCols), n, cdiv(n, kNormCols)};
     const int blocks = (int)std::min<long long>(kNormBlocks, (q.all + 7) / 8);
     const int vec = tma_ok(G, ldg, sizeof(T) == 4 ? QCNN_F32 : QCNN_BF16);
     qcnn_status rc = launch_pdl(norm_kernel<T>, dim3(blocks), dim3(256), 0, st, G, ldg, q, vec, s.norm);
