@@ -50,6 +50,7 @@ def test_another_device_is_refused(name, args, more):
     with pytest.raises(ValueError, match="device"):
         getattr(q, name)(**{n: _on(1, *shape, **kw) for n, shape, kw in args}, **more)
 
+
 @pytest.mark.parametrize("name,args,more", CALLS, ids=[c[0] for c in CALLS])
 def test_what_is_no_tensor_is_refused(name, args, more):
     for bad in [a[0] for a in args]:

@@ -12,6 +12,13 @@ from test_gpu_finetune import BF16, TYPES, _gen, _near, _no_timeouts, _normal, _
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def memory_given_back():
+    """The 64-bit forms take gigabytes, which other tests' measured memory does not have."""
+    yield
+    torch.cuda.empty_cache()
+
+
 # Pieces whose dx is shared by two, four or eight CTAs, the last one too short for as many (on how
 # many depends on the clusters that the device holds at once).
 @pytest.mark.parametrize("N,Cs,Ct", [(17949, 100, 21524), (4096, 128, 145161)])
