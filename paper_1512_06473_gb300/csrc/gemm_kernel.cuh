@@ -30,7 +30,7 @@
 // was 1664, and the kernel took 3,500: 115 us for 128 rows of 9216 -> 4096.)
 //
 // Measured, of 6.67 TB/s copied and 1,946 (a long run: 1,742) TFLOP/s of bf16: 4096 x 4096 ->
-// 8192 in bf16 with GELU and residual 168 us, 1,640 TFLOP/s (tensor cores, at the power limit);
+// 8192 in bf16 with GELU and residual 173 us, 1,590 TFLOP/s (tensor cores; at the power limit 192);
 // GEN, 8192 -> 19456: 12 rows 114 us, 5.6 TB/s (the memory and the split), 128 rows 164 us, 1,490
 // TFLOP/s (six products; tensor cores); 128 x 9216 -> 4096 56 us, of which 46 are the product at
 // that rate on the 128 CTAs that 32 tiles make.

@@ -9,8 +9,8 @@
 // instead of B X read X again in the third product's epilogue, 12 us a step of 1000 x 4096.)
 // X, A and B live as bf16 planes that the epilogues write and TMA reads: two in bf16 calls (in
 // one, each step's rounding of X and B would be that of the result), three in fp32 calls.
-// 4096 x 9216 in bf16, five steps: 4.4 ms, 1,810 TFLOP/s of its three products (tensor cores, at
-// the power limit); 1000 x 4096 in fp32 395 us, half of that rate: 15 products of 36 to 256
+// 4096 x 9216 in bf16, five steps: 4.5 ms, 1,770 TFLOP/s of its three products (tensor cores; at the
+// power limit 4.7); 1000 x 4096 in fp32 391 us, half of that rate: 15 products of 36 to 256
 // tiles one after another.
 // Matrices whose smaller side is 64 or less are done in one launch where that is sooner done
 // (orthogonalize_small.cu).

@@ -5,7 +5,9 @@ the orthogonalised update of a weight matrix.
 
 Matrices are CUDA tensors of one type, float32 or bfloat16, whose rows may be any
 distance apart (the columns of a row are neighbours); bias, losses and their gradients
-are float32.  Weights are [Ct, Cs], as pq_quantize_fc takes them.
+are float32.  Weights are [Ct, Cs], as pq_quantize_fc takes them.  All tensors of a call are on
+the current device; an ``out`` overlaps no input but where that is said.  The gradients are calls
+of their own: no call is recorded for autograd.
 """
 from __future__ import annotations
 
@@ -94,7 +96,7 @@ def dense_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
                   out: Optional[torch.Tensor] = None, workspace=None, stream=None):
     """y = act(z) + residual with z = x weight^T + bias, in one product with its
     epilogue.  x [N, Cs], weight [Ct, Cs], bias [Ct] float32, residual [N, Ct]; act is
-    "none", "relu", "gelu" (by erf) or "silu".  pre=True returns (y, z): z is what
+    "none", "relu", "gelu" (by erf) or "silu"; ``out`` may be residual.  pre=True returns (y, z): z is what
     dense_backward needs."""
     code, dev = _first(x, "x")
     dt = x.dtype
