@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_small_kernel(const Args a) 
         large += __shfl_xor_sync(0xffffffffu, large, o);
     }
     if (lane == 0) norms[warp] = make_double2(small, large);
-    cluster.barrier_wait();
     __syncthreads();
+    cluster.barrier_wait();
     if (tid == 0) {
         double2 s = norms[0];
         for (int w = 1; w < kThreads / 32; ++w) {
