@@ -647,8 +647,10 @@ qcnn_status qcnn_net_forward_host(const qcnn_layer *layers, int n_layers,
  * are positive, except N, which may be 0 (gradients of weights are then zero); element
  * counts may pass 2^31.  Outputs must not overlap inputs, with the exceptions named.
  *
- * Arithmetic: bf16 operands are multiplied exactly and summed in fp32, each output
- * rounded to bf16 once.  fp32 operands are taken in three bf16 pieces, which hold all
+ * Arithmetic: bf16 operands are multiplied exactly and summed in fp32, where each addition
+ * of 16 products may cut off the sum's last bit (K terms: within (K / 16 + 8) 2^-23 of the
+ * sum of their magnitudes; of 10^6 terms of one sign still below bf16's own rounding), each
+ * output rounded to bf16 once.  fp32 operands are taken in three bf16 pieces, which hold all
  * their 24 bits, and summed in fp32, or (of few rows) multiplied as they are: results
  * are as close to the exact ones as those of fp32 multiply-adds.  A non-finite operand
  * makes the outputs that it enters non-finite; of an infinite fp32 operand taken in
