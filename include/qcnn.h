@@ -746,6 +746,61 @@ qcnn_status qcnn_orthogonalize(const void *G, long long ldg, int m, int n, int s
                                const float *coeffs, float eps, void *out, long long ldo, int dtype,
                                void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * qcnn_dropout_forward -- y = keep ? x / (1 - p) : 0, plus residual (or NULL): the dropout of
+ * activations while dense layers are trained.  Nothing is stored for the backward pass: what is kept
+ * follows from seed, offset and an element's place.
+ *   x, residual, y [N][C] of dtype; y may be x or residual.  0 <= p < 1.
+ *   Element i = n C + c has word i mod 4 of Philox-4x32 with ten rounds (Salmon et al. 2011) for the
+ *   counter (i / 4 low, high 32 bits, offset low, high) and the key (seed low, high), whatever the
+ *   distance of the rows; it is dropped if that word is below min(round(p 2^32), 2^32 - 1).
+ *   offset: the call's number; calls with another one draw other words.  offset_add: NULL, or an
+ *   int64 in device memory that is added to it as the kernel runs, so that a captured graph draws
+ *   other words each time its owner has changed it.
+ *   A dropped element is 0 whatever x holds (NaN, infinities).
+ * qcnn_dropout_backward -- dx = keep ? dy / (1 - p) : 0 with the same p, seed, offset and sizes as the
+ *   forward call; dx may be dy.  The residual's gradient is dy.
+ * 1 / (1 - p) is rounded to fp32, the product and the sum with the residual are fp32, then rounded to
+ * dtype once.  No workspace.
+ */
+qcnn_status qcnn_dropout_forward(const void *x, long long ldx, int N, int C, double p, uint64_t seed,
+                                 uint64_t offset, const int64_t *offset_add, const void *residual,
+                                 long long ldr, void *y, long long ldy, int dtype, void *stream);
+qcnn_status qcnn_dropout_backward(const void *dy, long long lddy, int N, int C, double p, uint64_t seed,
+                                  uint64_t offset, const int64_t *offset_add, void *dx, long long lddx,
+                                  int dtype, void *stream);
+
+/*
+ * Dense layers in 8-bit integers: where a fine-tuned layer is to be small without codebooks.
+ *
+ * qcnn_int8_quantize -- rows of x [N][C] (fp32 or bf16) as codes [N][C] and a scale per row:
+ *     scale = max(max_c |x[n][c]| (1 / 127), 2^-126),   code = x (1 / scale) to the nearest integer,
+ *   each step in fp32 rounded to nearest, ties to even: |code| <= 127, and code * scale is within
+ *   (1/2 + 2^-15) scale of x.  A row that holds a NaN or an infinity has scale NaN or infinity and codes 0, so
+ *   that whatever is made of it is not finite.  codes: ldc bytes between rows, any alignment; with
+ *   16-byte aligned rows the products below read them as they are.
+ * qcnn_int8_dense_forward -- y = act(z) + residual with
+ *     z[n][m] = (sum_k q[n][k] W[m][k]) xscale[n] wscale[m] + bias[m].
+ *   W [Ct][Cs] codes with wscale [Ct], as qcnn_int8_quantize gives them for the dense weights.
+ *   xscale NULL: x [N][Cs] of dtype, whose rows the call quantizes as qcnn_int8_quantize does; else x
+ *   [N][Cs] codes with xscale [N].  bias [Ct] fp32 or NULL; residual [N][Ct] of dtype or NULL (may be
+ *   y itself); y [N][Ct] of dtype.  Any code from -128 to 127 will do; Cs <= 131071.
+ *   Sums of up to 1024 terms are exact, those of several such blocks are added in fp32 (exact while
+ *   they stay below 2^24; of up to 8 rows all sums are exact); then two products, bias, activation and
+ *   residual in fp32, and one rounding to dtype.
+ *   Workspace: from the query (x_codes: xscale is given); `aligned`: W, and x if it is codes, have
+ *   16-byte aligned bases and row distances that are multiples of 16.
+ */
+qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_t *codes, long long ldc,
+                               float *scale, int dtype, void *stream);
+qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned,
+                                           size_t *bytes);
+qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *xscale, int N, int Cs,
+                                    const int8_t *W, long long ldw, const float *wscale, int Ct,
+                                    const float *bias, int act, const void *residual, long long ldr,
+                                    void *y, long long ldy, int dtype, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

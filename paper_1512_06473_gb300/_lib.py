@@ -131,6 +131,16 @@ _SIGS = {
     "qcnn_orthogonalize_workspace_size": (c_int, [c_int] * 3 + [ctypes.POINTER(c_size_t)]),
     "qcnn_orthogonalize": (c_int, [c_void_p, c_int64, c_int, c_int, c_int, c_void_p, ctypes.c_float,
                                    c_void_p, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
+    "qcnn_dropout_forward": (c_int, [c_void_p, c_int64, c_int, c_int, ctypes.c_double, c_uint64, c_uint64,
+                                     c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p]),
+    "qcnn_dropout_backward": (c_int, [c_void_p, c_int64, c_int, c_int, ctypes.c_double, c_uint64, c_uint64,
+                                      c_void_p, c_void_p, c_int64, c_int, c_void_p]),
+    "qcnn_int8_quantize": (c_int, [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_void_p, c_int,
+                                   c_void_p]),
+    "qcnn_int8_dense_workspace_size": (c_int, [c_int] * 5 + [ctypes.POINTER(c_size_t)]),
+    "qcnn_int8_dense_forward": (c_int, [c_void_p, c_int64, c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p,
+                                        c_int, c_void_p, c_int, c_void_p, c_int64, c_void_p, c_int64, c_int,
+                                        c_void_p, c_size_t, c_void_p]),
     "qcnn_pq_quantize": (c_int, [c_int, c_void_p, c_int, c_int, c_int, c_int, c_int, c_int,
                                  c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_size_t,
                                  c_void_p]),

@@ -1,7 +1,7 @@
 """The operators that fine-tune the dense layers of a network whose conv layers are
 quantized (the paper's Sec. 4.2.3), before those are quantized as well: a dense layer
-with its epilogue and its backward pass, softmax cross entropy with its gradient, and
-the orthogonalised update of a weight matrix.
+with its epilogue and its backward pass, dropout whose mask is never stored, softmax cross
+entropy with its gradient, and the orthogonalised update of a weight matrix.
 
 Matrices are CUDA tensors of one type, float32 or bfloat16, whose rows may be any
 distance apart (the columns of a row are neighbours); bias, losses and their gradients
@@ -253,3 +253,55 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs: Optional[Sequence[flo
                                       out.data_ptr(), ldo, code, ws.data_ptr(), wsb,
                                       _stream(stream)), "qcnn_orthogonalize")
     return out
+
+
+def _dropout(name, x, x_name, p, seed, offset, residual, out, stream):
+    code, dev = _first(x, x_name)
+    dt = x.dtype
+    ldx = _matrix(x, x_name, dt, dev)
+    N, C = x.shape
+    if not 0.0 <= p < 1.0:
+        raise ValueError(f"p must be at least 0 and below 1, got {p}")
+    if not 0 <= seed < 1 << 64:
+        raise ValueError(f"seed must be a number of 64 bits, got {seed}")
+    add = None
+    if isinstance(offset, torch.Tensor):
+        if offset.dtype is not _I64 or not offset.is_cuda or offset.get_device() != dev or offset.numel() != 1:
+            _refuse(offset, "offset", _I64, dev, (1,))
+        add, offset = offset.data_ptr(), 0
+    elif not 0 <= offset < 1 << 64:
+        raise ValueError(f"offset must be a number of 64 bits, got {offset}")
+    ldr = 0 if residual is None else _matrix(residual, "residual", dt, dev, N, C)
+    if out is None:
+        out, ldo = _new(x, (N, C), dt, stream), C
+    else:
+        ldo = _matrix(out, "out", dt, dev, N, C)
+    lib = load()
+    if name == "qcnn_dropout_forward":
+        st = lib.qcnn_dropout_forward(x.data_ptr(), ldx, N, C, p, seed, offset, add,
+                                      None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldo,
+                                      code, _stream(stream))
+    else:
+        st = lib.qcnn_dropout_backward(x.data_ptr(), ldx, N, C, p, seed, offset, add, out.data_ptr(), ldo, code,
+                                       _stream(stream))
+    if st:
+        _lib.check(st, name)
+    return out
+
+
+def dropout_forward(x: torch.Tensor, p: float, seed: int, offset=0, residual: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, stream=None):
+    """y = x / (1 - p) where an element is kept, else 0; plus residual.  x, residual [N, C]; 0 <= p < 1;
+    ``out`` may be x or residual.  What is kept follows from seed, offset (64 bits each) and an
+    element's place (Philox-4x32, qcnn.h), so that nothing is stored: dropout_backward draws it
+    again.  Give each call of a step an offset of its own, and the backward call the same; or a CUDA
+    int64 tensor of one element, read as the kernel runs, which a captured graph's owner
+    can change between replays."""
+    return _dropout("qcnn_dropout_forward", x, "x", p, seed, offset, residual, out, stream)
+
+
+def dropout_backward(dy: torch.Tensor, p: float, seed: int, offset=0, out: Optional[torch.Tensor] = None,
+                     stream=None):
+    """The gradient of x for the gradient dy [N, C] of dropout_forward's y, with the same p, seed and
+    offset.  ``out`` may be dy.  The residual's gradient is dy itself."""
+    return _dropout("qcnn_dropout_backward", dy, "dy", p, seed, offset, None, out, stream)
