@@ -10,9 +10,12 @@
 #include "train.cuh"
 
 #include <cmath>
+#include <type_traits>
 
 namespace qcnn {
 namespace {
+
+constexpr unsigned long long kManyVectors = 1u << 20;  // from here on four per thread
 
 struct DropoutArgs {
     const void *x, *r;
@@ -55,6 +58,84 @@ __device__ __forceinline__ T from_float(float v) {
     else return float_to_bf16(v);
 }
 
+// 16 bytes of elements in registers; two bf16 in a word.
+template <typename T>
+__device__ __forceinline__ uint4 drop_vec(const uint4 &x, const uint4 &r, bool res, const DropoutArgs &d,
+                                          unsigned long long block, unsigned long long offset) {
+    const unsigned xs[4] = {x.x, x.y, x.z, x.w}, rs[4] = {r.x, r.y, r.z, r.w};
+    unsigned w[4], out[4];
+    philox(block, offset, d.k0, d.k1, w);
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float v = w[j] >= d.threshold ? __uint_as_float(xs[j]) * d.scale : 0.f;
+            if (res) v += __uint_as_float(rs[j]);
+            out[j] = __float_as_uint(v);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j == 2) philox(block + 1, offset, d.k0, d.k1, w);
+            const int k = (j & 1) * 2;
+            float v0 = w[k] >= d.threshold ? __uint_as_float(xs[j] << 16) * d.scale : 0.f;
+            float v1 = w[k + 1] >= d.threshold ? __uint_as_float(xs[j] & 0xffff0000u) * d.scale : 0.f;
+            if (res) v0 += __uint_as_float(rs[j] << 16), v1 += __uint_as_float(rs[j] & 0xffff0000u);
+            out[j] = pack_bf16x2(v0, v1);
+        }
+    }
+    return make_uint4(out[0], out[1], out[2], out[3]);
+}
+
+// U vectors of 16 bytes per thread, all loads first.  FLAT: no gaps between rows, so that the matrix
+// is one row, whatever its width (its last elements, fewer than a vector, go one by one); else rows
+// of whole vectors.
+template <typename T, int U, bool FLAT>
+__global__ void __launch_bounds__(256) dropout_vec_kernel(DropoutArgs d) {
+    constexpr int V = 16 / (int)sizeof(T);
+    using L = unsigned long long;
+    const L vectors = d.n / V, first = (L)blockIdx.x * (256 * U) + threadIdx.x;
+    const L offset = d.offset + (d.offset_add ? *d.offset_add : 0);
+    const bool res = d.r != nullptr;
+    const T *const x = static_cast<const T *>(d.x), *const r = static_cast<const T *>(d.r);
+    T *const y = static_cast<T *>(d.y);
+    // where a vector begins
+    auto at = [&](L v, long long ld) -> long long {
+        if constexpr (FLAT) {
+            return (long long)(v * V);
+        } else {
+            const unsigned per = (unsigned)d.cols / V;
+            const L row = vectors <= 0xffffffffull ? (unsigned)v / per : v / per;
+            return (long long)row * ld + (long long)(v - row * per) * V;
+        }
+    };
+    uint4 a[U], b[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const L v = first + u * 256;
+        if (v >= vectors) continue;
+        a[u] = *reinterpret_cast<const uint4 *>(x + at(v, d.ldx));
+        if (res) b[u] = *reinterpret_cast<const uint4 *>(r + at(v, d.ldr));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const L v = first + u * 256;
+        if (v >= vectors) continue;
+        *reinterpret_cast<uint4 *>(y + at(v, d.ldy)) = drop_vec<T>(a[u], b[u], res, d, v * (V / 4), offset);
+    }
+    if constexpr (FLAT) {
+        const int rest = (int)(d.n - vectors * V);
+        if (blockIdx.x == 0 && (int)threadIdx.x < rest) {
+            const L i = vectors * V + threadIdx.x;
+            unsigned w[4];
+            philox(i / 4, offset, d.k0, d.k1, w);
+            const unsigned word = i & 2 ? (i & 1 ? w[3] : w[2]) : (i & 1 ? w[1] : w[0]);
+            float v = word >= d.threshold ? to_float(x[i]) * d.scale : 0.f;
+            if (res) v += to_float(r[i]);
+            y[i] = from_float<T>(v);
+        }
+    }
+}
+
 // Four elements of a counter per thread, wherever their rows begin.
 template <typename T>
 __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs d) {
@@ -93,9 +174,27 @@ qcnn_status dropout(const void *x, long long ldx, int N, int C, double p, uint64
     d.k0 = (unsigned)seed, d.k1 = (unsigned)(seed >> 32);
     d.threshold = (unsigned)std::min(std::nearbyint(p * 4294967296.0), 4294967295.0);
     d.scale = (float)(1.0 / (1.0 - p));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int V = dtype == QCNN_BF16 ? 8 : 4;
+    const auto vec = [&](const void *q, long long ld, bool flat) {
+        return reinterpret_cast<uintptr_t>(q) % 16 == 0 && (flat || ld % V == 0);
+    };
+    const bool flat = N == 1 || (ldx == C && ldy == C && (!r || ldr == C));
+    if ((flat || C % V == 0) && vec(x, ldx, flat) && vec(y, ldy, flat) && (!r || vec(r, ldr, flat))) {
+        const unsigned long long vectors = d.n / V;
+        const int U = vectors >= kManyVectors ? 4 : 1;
+        const unsigned long long ctas = std::max(1ull, (vectors + 256 * U - 1) / (256 * U));
+        if (ctas > INT_MAX) return QCNN_ERR_UNSUPPORTED;
+        const auto launch = [&](auto *type) {
+            using T = std::remove_pointer_t<decltype(type)>;
+            const auto k = U == 4 ? (flat ? dropout_vec_kernel<T, 4, true> : dropout_vec_kernel<T, 4, false>)
+                                  : (flat ? dropout_vec_kernel<T, 1, true> : dropout_vec_kernel<T, 1, false>);
+            return launch_pdl(k, dim3((unsigned)ctas), dim3(256), 0, st, d);
+        };
+        return V == 8 ? launch(static_cast<unsigned short *>(nullptr)) : launch(static_cast<float *>(nullptr));
+    }
     const unsigned long long ctas = ((d.n + 3) / 4 + 255) / 256;
     if (ctas > INT_MAX) return QCNN_ERR_UNSUPPORTED;
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return launch_pdl(dtype == QCNN_BF16 ? dropout_kernel<unsigned short> : dropout_kernel<float>, dim3((unsigned)ctas),
                       dim3(256), 0, st, d);
 }

@@ -11,38 +11,160 @@ namespace {
 constexpr float kInv127 = 1.f / 127.f;
 constexpr int kMaxTerms = 131071;  // whose sum of products fits 32 bits
 
-template <typename T>
-__device__ __forceinline__ float to_float(T v) {
-    if constexpr (sizeof(T) == 4) return v;
-    else return bf16_to_float(v);
+// --------------------------------------------------------------- quantizer
+// The largest magnitude of a row goes by its bits, whose order is that of the values, infinities and
+// NaN above all.  |x| / scale <= 127 (1 + 2^-21), so no code is clamped.
+struct RowScale {
+    float scale, inverse;
+    bool finite;
+};
+__device__ __forceinline__ RowScale row_scale(unsigned top) {
+    const float t = __fmul_rn(__uint_as_float(top), kInv127), s = t < 1.17549435e-38f ? 1.17549435e-38f : t;
+    const bool finite = top < 0x7f800000u;
+    return {s, finite ? __frcp_rn(s) : 0.f, finite};
+}
+// x / scale to the nearest integer, ties to even: in the low bits of a float around 1.5 2^23.
+constexpr float kRound = 12582912.f;
+__device__ __forceinline__ float rounded(float x, float inverse) { return __fadd_rn(__fmul_rn(x, inverse), kRound); }
+
+__device__ __forceinline__ unsigned pack_codes(float a, float b, float c, float d) {
+    return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
+                       __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
 
-// --------------------------------------------------------------- quantizer
-// A CTA per row: its largest magnitude (as bits, whose order is that of the values, infinities and
-// NaN above all), then its codes.
-template <typename T>
-__global__ void __launch_bounds__(256) quantize_kernel(const T *x, long long ldx, int cols, int8_t *codes,
-                                                       long long ldc, int padded, float *scale) {
-    __shared__ unsigned red[8];
+struct QuantizeArgs {
+    const void *x;
+    long long ldx;
+    int rows, cols, padded;  // (codes from cols to padded are 0)
+    int8_t *codes;
+    long long ldc;
+    float *scale;
+    int wide;  // codes go several at a time
+};
+
+// G threads a row (a warp, several or the CTA), which keep up to H vectors of V elements each between
+// the two steps; what a row has beyond that is read again.  V: 16 bytes, or (rows off 16 bytes) one
+// element.
+template <typename T, int G, int H, bool VEC>
+__global__ void __launch_bounds__(G > 256 ? G : 256) quantize_kernel(QuantizeArgs a) {
+    constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, BLOCK = G > 256 ? G : 256, ROWS = BLOCK / G;
+    constexpr int W = VEC ? 4 : 1;  // words of a vector
+    __shared__ unsigned red[BLOCK / 32];
     grid_dep_sync();
-    const T *row = x + (long long)blockIdx.x * ldx;
-    int8_t *out = codes + (long long)blockIdx.x * ldc;
+    const int t = threadIdx.x % G, group = threadIdx.x / G;
+    const long long row = (long long)blockIdx.x * ROWS + group;
+    const bool is = row < a.rows;
+    const T *const x = static_cast<const T *>(a.x) + (is ? row : 0) * a.ldx;
+    int8_t *const out = a.codes + (is ? row : 0) * a.ldc;
+    const int vectors = is ? a.cols / V : 0;
+    struct Vec {
+        unsigned w[W];
+    };
+    auto load = [&](unsigned v) {
+        Vec r;
+        if constexpr (VEC) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(x + (long long)v * V);
+            r.w[0] = q.x, r.w[1] = q.y, r.w[2] = q.z, r.w[3] = q.w;
+        } else if constexpr (sizeof(T) == 4) {
+            r.w[0] = __float_as_uint(x[v]);
+        } else {
+            r.w[0] = (unsigned)x[v] << 16;
+        }
+        return r;
+    };
     unsigned top = 0;
-    for (int c = threadIdx.x; c < cols; c += 256) top = max(top, __float_as_uint(to_float(row[c])) & 0x7fffffffu);
-    top = __reduce_max_sync(0xffffffffu, top);
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
-    __syncthreads();
+    auto look = [&](const Vec &r) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, red[i]);
-    const bool finite = top < 0x7f800000u;
-    const float t = __fmul_rn(__uint_as_float(top), kInv127), s = t < 1.17549435e-38f ? 1.17549435e-38f : t;
-    const float inverse = __frcp_rn(s);
-    for (int c = threadIdx.x; c < padded; c += 256) {
-        int q = 0;
-        if (finite && c < cols) q = __float2int_rn(__fmul_rn(to_float(row[c]), inverse));
-        out[c] = (int8_t)max(-127, min(127, q));
+        for (int i = 0; i < W; ++i) {
+            if constexpr (VEC && sizeof(T) == 2) top = max(top, r.w[i] << 16 & 0x7fff0000u);
+            top = max(top, r.w[i] & (VEC && sizeof(T) == 2 ? 0x7fff0000u : 0x7fffffffu));
+        }
+    };
+    Vec kept[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+        if (t + h * G < vectors) kept[h] = load(t + h * G);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+        if (t + h * G < vectors) look(kept[h]);
+#pragma unroll 4
+    for (unsigned v = t + H * G; v < (unsigned)vectors; v += G) look(load(v));
+    const int rest = VEC && is ? a.cols % V : 0;
+    unsigned last = 0;  // (an element of the rest)
+    if (t < rest) {
+        const T v = x[(long long)vectors * V + t];
+        if constexpr (sizeof(T) == 4) last = __float_as_uint(v);
+        else last = (unsigned)v << 16;
+        top = max(top, last & 0x7fffffffu);
     }
-    if (threadIdx.x == 0) scale[blockIdx.x] = s;
+    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (G > 32) {
+        if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < G / 32; ++i) top = max(top, red[group * (G / 32) + i]);
+    }
+    if (!is) return;
+    const RowScale s = row_scale(top);
+    if (t == 0) a.scale[row] = s.scale;
+    auto code = [&](unsigned w) { return rounded(s.finite ? __uint_as_float(w) : 0.f, s.inverse); };
+    auto put = [&](unsigned v, const Vec &r) {
+        int8_t *const o = out + (long long)v * V;
+        if constexpr (!VEC) {
+            *o = (int8_t)__float_as_uint(code(r.w[0]));
+        } else {
+            constexpr int N = V / 4;  // words of codes
+            unsigned c[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if constexpr (sizeof(T) == 4)
+                    c[i] = pack_codes(code(r.w[0]), code(r.w[1]), code(r.w[2]), code(r.w[3]));
+                else
+                    c[i] = pack_codes(code(r.w[2 * i] << 16), code(r.w[2 * i] & 0xffff0000u),
+                                      code(r.w[2 * i + 1] << 16), code(r.w[2 * i + 1] & 0xffff0000u));
+            }
+            if (a.wide) {
+                if constexpr (N == 1) *reinterpret_cast<unsigned *>(o) = c[0];
+                else *reinterpret_cast<uint2 *>(o) = make_uint2(c[0], c[1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = (int8_t)(c[i / 4] >> i % 4 * 8);
+            }
+        }
+    };
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+        if (t + h * G < vectors) put(t + h * G, kept[h]);
+#pragma unroll 4
+    for (unsigned v = t + H * G; v < (unsigned)vectors; v += G) put(v, load(v));
+    if (t < rest) out[(long long)vectors * V + t] = (int8_t)__float_as_uint(code(last));
+    for (unsigned c = (unsigned)a.cols + t; c < (unsigned)a.padded; c += G) out[c] = 0;
+}
+
+template <typename T>
+qcnn_status launch_quantize_of(const QuantizeArgs &a, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const auto launch = [&](auto k, int G) {
+        const int rows = G > 256 ? 1 : 256 / G;
+        return launch_pdl(k, dim3((unsigned)((a.rows + (long long)rows - 1) / rows)), dim3(G > 256 ? G : 256), 0, st, a);
+    };
+    if (reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.ldx % V == 0 || a.rows == 1)) {
+        const int vectors = a.cols / V;
+        if (vectors <= 128) return launch(quantize_kernel<T, 32, 4, true>, 32);
+        if (vectors <= 512) return launch(quantize_kernel<T, 128, 4, true>, 128);
+        if (vectors <= 1024) return launch(quantize_kernel<T, 256, 4, true>, 256);
+        return launch(quantize_kernel<T, 512, 8, true>, 512);
+    }
+    if (a.cols <= 256) return launch(quantize_kernel<T, 32, 8, false>, 32);
+    if (a.cols <= 2048) return launch(quantize_kernel<T, 128, 16, false>, 128);
+    return launch(quantize_kernel<T, 512, 16, false>, 512);
+}
+qcnn_status launch_quantize(const void *x, long long ldx, int rows, int cols, int8_t *codes, long long ldc,
+                            int padded, float *scale, int dtype, cudaStream_t st) {
+    const int V = dtype == QCNN_BF16 ? 8 : 4;
+    const int wide = reinterpret_cast<uintptr_t>(codes) % V == 0 && (ldc % V == 0 || rows == 1);
+    const QuantizeArgs a{x, ldx, rows, cols, padded, codes, ldc, scale, wide};
+    return dtype == QCNN_BF16 ? launch_quantize_of<unsigned short>(a, st) : launch_quantize_of<float>(a, st);
 }
 
 // ------------------------------------------------------------------ product
@@ -130,15 +252,6 @@ Space carve(int N, int Cs, bool x_codes, void *ws) {
 }
 bool rows16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 16 == 0; }
 bool codes_ok(const void *p, long long ld, long long rows, long long cols) { return ld >= cols && (rows == 0 || p); }
-
-qcnn_status launch_quantize(const void *x, long long ldx, int rows, int cols, int8_t *codes, long long ldc,
-                            int padded, float *scale, int dtype, cudaStream_t st) {
-    if (dtype == QCNN_BF16)
-        return launch_pdl(quantize_kernel<unsigned short>, dim3(rows), dim3(256), 0, st,
-                          static_cast<const unsigned short *>(x), ldx, cols, codes, ldc, padded, scale);
-    return launch_pdl(quantize_kernel<float>, dim3(rows), dim3(256), 0, st, static_cast<const float *>(x), ldx, cols,
-                      codes, ldc, padded, scale);
-}
 
 }  // namespace
 }  // namespace qcnn
