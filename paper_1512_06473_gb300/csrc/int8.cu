@@ -12,159 +12,203 @@ constexpr float kInv127 = 1.f / 127.f;
 constexpr int kMaxTerms = 131071;  // whose sum of products fits 32 bits
 
 // --------------------------------------------------------------- quantizer
-// The largest magnitude of a row goes by its bits, whose order is that of the values, infinities and
-// NaN above all.  |x| / scale <= 127 (1 + 2^-21), so no code is clamped.
-struct RowScale {
-    float scale, inverse;
-    bool finite;
-};
-__device__ __forceinline__ RowScale row_scale(unsigned top) {
-    const float t = __fmul_rn(__uint_as_float(top), kInv127), s = t < 1.17549435e-38f ? 1.17549435e-38f : t;
-    const bool finite = top < 0x7f800000u;
-    return {s, finite ? __frcp_rn(s) : 0.f, finite};
+// A row's largest magnitude, NaN if it holds one (max.NaN).  |x| / scale <= 127 (1 + 2^-21), so no code
+// is clamped.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
-// x / scale to the nearest integer, ties to even: in the low bits of a float around 1.5 2^23.
+struct RowScale {
+    float scale, inverse;  // (inverse 0 where the scale is not finite)
+};
+__device__ __forceinline__ RowScale row_scale(float top) {
+    const float t = __fmul_rn(top, kInv127), s = t < 1.17549435e-38f ? 1.17549435e-38f : t;
+    return {s, s <= 3.402823466e38f ? __frcp_rn(s) : 0.f};
+}
+// x / scale to the nearest integers, ties to even: in the low bits of floats around 1.5 2^23.
+// (Products one by one: a packed product and a packed sum, in intrinsics or with .rn in PTX, became one
+// operation that rounds once, and ties of bf16 rows went the other way.)
 constexpr float kRound = 12582912.f;
-__device__ __forceinline__ float rounded(float x, float inverse) { return __fadd_rn(__fmul_rn(x, inverse), kRound); }
-
-__device__ __forceinline__ unsigned pack_codes(float a, float b, float c, float d) {
-    return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
-                       __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+__device__ __forceinline__ float2 rounded(float x, float y, float inverse) {
+    return __fadd2_rn(make_float2(__fmul_rn(x, inverse), __fmul_rn(y, inverse)), make_float2(kRound, kRound));
+}
+__device__ __forceinline__ unsigned pack_codes(float2 a, float2 b) {
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
+                       __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+}
+__device__ __forceinline__ unsigned pack_half(float2 a) {  // (exact)
+    const float2 v = __fadd2_rn(a, make_float2(-kRound, -kRound));
+    unsigned r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(v.y), "f"(v.x));
+    return r;
 }
 
 struct QuantizeArgs {
     const void *x;
     long long ldx;
-    int rows, cols, padded;  // (codes from cols to padded are 0)
-    int8_t *codes;
-    long long ldc;
+    int rows, cols;
+    void *codes;    // int8, or (HALF) fp16 with zeros up to the next multiple of 8
+    long long ldc;  // elements
     float *scale;
     int wide;  // codes go several at a time
 };
 
-// G threads a row (a warp, several or the CTA), which keep up to H vectors of V elements each between
-// the two steps; what a row has beyond that is read again.  V: 16 bytes, or (rows off 16 bytes) one
-// element.
-template <typename T, int G, int H, bool VEC>
+// G threads a row (a warp, several or the CTA), which keep up to H vectors of 16 bytes each between
+// the two steps; what a row has beyond that is read again.  SHIFT: rows begin off the 16 bytes, and a
+// vector is taken out of the two aligned ones that it lies in (1000 x 4097 in bf16 8.6 us element by
+// element).
+template <typename T, int G, int H, bool SHIFT, bool HALF>
 __global__ void __launch_bounds__(G > 256 ? G : 256) quantize_kernel(QuantizeArgs a) {
-    constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, BLOCK = G > 256 ? G : 256, ROWS = BLOCK / G;
-    constexpr int W = VEC ? 4 : 1;  // words of a vector
-    __shared__ unsigned red[BLOCK / 32];
+    constexpr int E = (int)sizeof(T), V = 16 / E, BLOCK = G > 256 ? G : 256, ROWS = BLOCK / G;
+    __shared__ float red[BLOCK / 32];
     grid_dep_sync();
     const int t = threadIdx.x % G, group = threadIdx.x / G;
     const long long row = (long long)blockIdx.x * ROWS + group;
     const bool is = row < a.rows;
     const T *const x = static_cast<const T *>(a.x) + (is ? row : 0) * a.ldx;
-    int8_t *const out = a.codes + (is ? row : 0) * a.ldc;
-    const int vectors = is ? a.cols / V : 0;
+    const unsigned vectors = is ? a.cols / V : 0, rest = is ? a.cols % V : 0;
     struct Vec {
-        unsigned w[W];
+        unsigned w[4];
+    };
+    [[maybe_unused]] const uintptr_t base = reinterpret_cast<uintptr_t>(a.x),
+                                     end = base + ((a.rows - 1) * a.ldx + a.cols) * E;
+    auto element = [&](unsigned c) {
+        if constexpr (E == 4) return __float_as_uint(x[c]);
+        else return (unsigned)x[c];
     };
     auto load = [&](unsigned v) {
         Vec r;
-        if constexpr (VEC) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(x + (long long)v * V);
+        if constexpr (!SHIFT) {
+            const uint4 q = reinterpret_cast<const uint4 *>(x)[v];
             r.w[0] = q.x, r.w[1] = q.y, r.w[2] = q.z, r.w[3] = q.w;
-        } else if constexpr (sizeof(T) == 4) {
-            r.w[0] = __float_as_uint(x[v]);
         } else {
-            r.w[0] = (unsigned)x[v] << 16;
+            const uintptr_t at = reinterpret_cast<uintptr_t>(x) + (uintptr_t)v * 16, low = at & ~(uintptr_t)15;
+            const unsigned off = (unsigned)(at - low);
+            if (low >= base && low + 32 <= end) {
+                const uint4 p = *reinterpret_cast<const uint4 *>(low), q = *reinterpret_cast<const uint4 *>(low + 16);
+                unsigned w[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+                if (off & 8) {
+#pragma unroll
+                    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+                }
+                if (off & 4) {
+#pragma unroll
+                    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r.w[i] = E == 4 ? w[i] : __funnelshift_r(w[i], w[i + 1], off * 8 & 16);
+            } else {  // (at the matrix's ends: nothing outside it is read)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (E == 4) r.w[i] = element(v * V + i);
+                    else r.w[i] = element(v * V + 2 * i) | element(v * V + 2 * i + 1) << 16;
+                }
+            }
         }
         return r;
     };
-    unsigned top = 0;
+    auto value = [](const Vec &r, int i) {  // element i
+        if constexpr (E == 4) return __uint_as_float(r.w[i]);
+        else return __uint_as_float(i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
+    };
+    float top = 0.f;
     auto look = [&](const Vec &r) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if constexpr (VEC && sizeof(T) == 2) top = max(top, r.w[i] << 16 & 0x7fff0000u);
-            top = max(top, r.w[i] & (VEC && sizeof(T) == 2 ? 0x7fff0000u : 0x7fffffffu));
-        }
+        for (int i = 0; i < V; ++i) top = max_nan(top, fabsf(value(r, i)));
     };
     Vec kept[H];
 #pragma unroll
     for (int h = 0; h < H; ++h)
         if (t + h * G < vectors) kept[h] = load(t + h * G);
+    Vec last = {};  // (an element of the rest, its first)
+    if (t < rest) last.w[0] = element(vectors * V + t);
 #pragma unroll
     for (int h = 0; h < H; ++h)
         if (t + h * G < vectors) look(kept[h]);
-#pragma unroll 4
-    for (unsigned v = t + H * G; v < (unsigned)vectors; v += G) look(load(v));
-    const int rest = VEC && is ? a.cols % V : 0;
-    unsigned last = 0;  // (an element of the rest)
-    if (t < rest) {
-        const T v = x[(long long)vectors * V + t];
-        if constexpr (sizeof(T) == 4) last = __float_as_uint(v);
-        else last = (unsigned)v << 16;
-        top = max(top, last & 0x7fffffffu);
-    }
-    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (H >= 5)
+#pragma unroll 2
+        for (unsigned v = t + H * G; v < vectors; v += G) look(load(v));
+    top = max_nan(top, fabsf(value(last, 0)));
+    // (as bits: their order is that of the values, NaN above all)
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
     if constexpr (G > 32) {
         if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < G / 32; ++i) top = max(top, red[group * (G / 32) + i]);
+        for (int i = 0; i < G / 32; ++i) top = max_nan(top, red[group * (G / 32) + i]);
     }
     if (!is) return;
     const RowScale s = row_scale(top);
     if (t == 0) a.scale[row] = s.scale;
-    auto code = [&](unsigned w) { return rounded(s.finite ? __uint_as_float(w) : 0.f, s.inverse); };
-    auto put = [&](unsigned v, const Vec &r) {
-        int8_t *const o = out + (long long)v * V;
-        if constexpr (!VEC) {
-            *o = (int8_t)__float_as_uint(code(r.w[0]));
-        } else {
-            constexpr int N = V / 4;  // words of codes
-            unsigned c[N];
+    const bool none = s.inverse == 0.f;
+    int8_t *const bytes = static_cast<int8_t *>(a.codes) + row * a.ldc;
+    unsigned short *const halves = static_cast<unsigned short *>(a.codes) + row * a.ldc;
+    auto put = [&](unsigned v, const Vec &from) {
+        Vec r = from;
+        if (none) r = Vec{};
+        float2 c[V / 2];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if constexpr (sizeof(T) == 4)
-                    c[i] = pack_codes(code(r.w[0]), code(r.w[1]), code(r.w[2]), code(r.w[3]));
-                else
-                    c[i] = pack_codes(code(r.w[2 * i] << 16), code(r.w[2 * i] & 0xffff0000u),
-                                      code(r.w[2 * i + 1] << 16), code(r.w[2 * i + 1] & 0xffff0000u));
-            }
+        for (int i = 0; i < V / 2; ++i) c[i] = rounded(value(r, 2 * i), value(r, 2 * i + 1), s.inverse);
+        if constexpr (HALF) {
+            unsigned short *const o = halves + (size_t)v * V;
+            if constexpr (V == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_half(c[0]), pack_half(c[1]));
+            else *reinterpret_cast<uint4 *>(o) = make_uint4(pack_half(c[0]), pack_half(c[1]), pack_half(c[2]), pack_half(c[3]));
+        } else {
+            int8_t *const o = bytes + (size_t)v * V;
+            unsigned w[V / 4];
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) w[i] = pack_codes(c[2 * i], c[2 * i + 1]);
             if (a.wide) {
-                if constexpr (N == 1) *reinterpret_cast<unsigned *>(o) = c[0];
-                else *reinterpret_cast<uint2 *>(o) = make_uint2(c[0], c[1]);
+                if constexpr (V == 4) *reinterpret_cast<unsigned *>(o) = w[0];
+                else *reinterpret_cast<uint2 *>(o) = make_uint2(w[0], w[1]);
             } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = (int8_t)(c[i / 4] >> i % 4 * 8);
+                for (int i = 0; i < V; ++i) o[i] = (int8_t)(w[i / 4] >> i % 4 * 8);
             }
         }
     };
 #pragma unroll
     for (int h = 0; h < H; ++h)
         if (t + h * G < vectors) put(t + h * G, kept[h]);
-#pragma unroll 4
-    for (unsigned v = t + H * G; v < (unsigned)vectors; v += G) put(v, load(v));
-    if (t < rest) out[(long long)vectors * V + t] = (int8_t)__float_as_uint(code(last));
-    for (unsigned c = (unsigned)a.cols + t; c < (unsigned)a.padded; c += G) out[c] = 0;
+    if constexpr (H >= 5)
+#pragma unroll 2
+        for (unsigned v = t + H * G; v < vectors; v += G) put(v, load(v));
+    const float2 c = rounded(none ? 0.f : value(last, 0), 0.f, s.inverse);
+    if constexpr (HALF) {
+        const unsigned pad = (8 - a.cols % 8) % 8;
+        if (t < rest) halves[(size_t)vectors * V + t] = (unsigned short)pack_half(c);
+        if (t < pad) halves[a.cols + t] = 0;
+    } else {
+        if (t < rest) bytes[(size_t)vectors * V + t] = (int8_t)__float_as_uint(c.x);
+    }
 }
 
-template <typename T>
+template <typename T, bool HALF>
 qcnn_status launch_quantize_of(const QuantizeArgs &a, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
-    const auto launch = [&](auto k, int G) {
+    const bool shift = reinterpret_cast<uintptr_t>(a.x) % 16 || (a.ldx % V && a.rows > 1);
+    const auto launch = [&](auto k, auto ks, int G) {
         const int rows = G > 256 ? 1 : 256 / G;
-        return launch_pdl(k, dim3((unsigned)((a.rows + (long long)rows - 1) / rows)), dim3(G > 256 ? G : 256), 0, st, a);
+        return launch_pdl(shift ? ks : k, dim3((unsigned)((a.rows + (long long)rows - 1) / rows)),
+                          dim3(G > 256 ? G : 256), 0, st, a);
     };
-    if (reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.ldx % V == 0 || a.rows == 1)) {
-        const int vectors = a.cols / V;
-        if (vectors <= 128) return launch(quantize_kernel<T, 32, 4, true>, 32);
-        if (vectors <= 512) return launch(quantize_kernel<T, 128, 4, true>, 128);
-        if (vectors <= 1024) return launch(quantize_kernel<T, 256, 4, true>, 256);
-        return launch(quantize_kernel<T, 512, 8, true>, 512);
-    }
-    if (a.cols <= 256) return launch(quantize_kernel<T, 32, 8, false>, 32);
-    if (a.cols <= 2048) return launch(quantize_kernel<T, 128, 16, false>, 128);
-    return launch(quantize_kernel<T, 512, 16, false>, 512);
+    // (as few threads as hold the row in registers: several rows of a CTA wait for each other less)
+    const int vectors = a.cols / V;
+    if (vectors <= 128) return launch(quantize_kernel<T, 32, 4, false, HALF>, quantize_kernel<T, 32, 4, true, HALF>, 32);
+    if (vectors <= 512) return launch(quantize_kernel<T, 128, 4, false, HALF>, quantize_kernel<T, 128, 4, true, HALF>, 128);
+    if (vectors <= 1024) return launch(quantize_kernel<T, 256, 4, false, HALF>, quantize_kernel<T, 256, 4, true, HALF>, 256);
+    return launch(quantize_kernel<T, 512, 5, false, HALF>, quantize_kernel<T, 512, 5, true, HALF>, 512);
 }
-qcnn_status launch_quantize(const void *x, long long ldx, int rows, int cols, int8_t *codes, long long ldc,
-                            int padded, float *scale, int dtype, cudaStream_t st) {
+// codes: int8, rows ldc apart; half: fp16, rows of 16-byte multiples
+qcnn_status launch_quantize(const void *x, long long ldx, int rows, int cols, void *codes, long long ldc, bool half,
+                            float *scale, int dtype, cudaStream_t st) {
     const int V = dtype == QCNN_BF16 ? 8 : 4;
     const int wide = reinterpret_cast<uintptr_t>(codes) % V == 0 && (ldc % V == 0 || rows == 1);
-    const QuantizeArgs a{x, ldx, rows, cols, padded, codes, ldc, scale, wide};
-    return dtype == QCNN_BF16 ? launch_quantize_of<unsigned short>(a, st) : launch_quantize_of<float>(a, st);
+    const QuantizeArgs a{x, ldx, rows, cols, codes, ldc, scale, wide};
+    if (dtype == QCNN_BF16)
+        return half ? launch_quantize_of<unsigned short, true>(a, st) : launch_quantize_of<unsigned short, false>(a, st);
+    return half ? launch_quantize_of<float, true>(a, st) : launch_quantize_of<float, false>(a, st);
 }
 
 // ------------------------------------------------------------------ product
@@ -266,7 +310,7 @@ qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_
         (N && !scale) || reinterpret_cast<uintptr_t>(scale) % 4)
         return QCNN_ERR_INVALID_ARG;
     if (N == 0) return QCNN_OK;
-    return launch_quantize(x, ldx, N, C, codes, ldc, C, scale, dtype, static_cast<cudaStream_t>(stream));
+    return launch_quantize(x, ldx, N, C, codes, ldc, false, scale, dtype, static_cast<cudaStream_t>(stream));
 }
 
 qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned, size_t *bytes) {
@@ -299,7 +343,7 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
     f.ldx = ldx;
     f.xscale = xscale;
     if (!xscale) {
-        rc = launch_quantize(x, ldx, N, Cs, s.codes, pad16(Cs), (int)pad16(Cs), s.scale, dtype, st);
+        rc = launch_quantize(x, ldx, N, Cs, s.codes, pad16(Cs), false, s.scale, dtype, st);
         if (rc != QCNN_OK) return rc;
         f.x = s.codes;
         f.ldx = pad16(Cs);
