@@ -4,9 +4,12 @@
 //   y = keep ? x / (1 - p) : 0 (+ r);   keep: word i mod 4 of Philox-4x32-10(counter (i / 4, offset),
 //   key seed) >= p 2^32, for element i of the matrix
 //
-// One pass: x (and r) read once, y written once; 905 MB of 16384 x 9216 bf16 with a residual at least
-// 134 us at the 6.78 TB/s of a copy.  Ten rounds are 20 multiplications of 32 x 32 -> 64 bits and as
-// many three-way xors per four elements, which run while the loads are on their way.
+// One pass: x (and r) read once, y written once.  Ten rounds are 20 products of 32 x 32 -> 64 bits per
+// four elements, and these go at 32 lanes per clock and SM (measured), nothing else of their warps'
+// quarter of the SM being issued meanwhile: 32 slots of a lane per element, of which 132 us for the 151
+// million elements of 16384 x 9216.  Four bytes an element (bf16 without a residual) are bound by that
+// (3001 x 5003 17 us, of which its bytes take 9), six (with a residual) by both (906 MB in 143 us, 6.3
+// TB/s), eight (fp32) by the bytes (604 MB in 91 us, 6.7 TB/s).
 #include "train.cuh"
 
 #include <cmath>
@@ -15,7 +18,8 @@
 namespace qcnn {
 namespace {
 
-constexpr unsigned long long kManyVectors = 1u << 20;  // from here on four per thread
+constexpr int kDropoutThreads = 128;
+constexpr unsigned long long kManyVectors = 1u << 19;  // from here on four per thread
 
 struct DropoutArgs {
     const void *x, *r;
@@ -86,14 +90,16 @@ __device__ __forceinline__ uint4 drop_vec(const uint4 &x, const uint4 &r, bool r
     return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-// U vectors of 16 bytes per thread, all loads first.  FLAT: no gaps between rows, so that the matrix
-// is one row, whatever its width (its last elements, fewer than a vector, go one by one); else rows
-// of whole vectors.
-template <typename T, int U, bool FLAT>
-__global__ void __launch_bounds__(256) dropout_vec_kernel(DropoutArgs d) {
-    constexpr int V = 16 / (int)sizeof(T);
+// U vectors of 16 bytes per thread, all loads first.  FLAT: no gaps between rows, so that the matrix is
+// one row, whatever its width (its last elements, fewer than a vector, go one by one); else rows of
+// whole vectors.  LOW: counters below 2^32, so that two of an element's products are the same for all.
+// (16384 x 9216 of zeros with a residual in bf16: a grid that stays and loads its next vectors ahead 152
+// to 163 us, this way 132; CTAs of 256 threads 137; one vector 146; counters of 64 bits 146.)
+template <typename T, int U, bool FLAT, bool LOW>
+__global__ void __launch_bounds__(kDropoutThreads) dropout_vec_kernel(DropoutArgs d) {
+    constexpr int V = 16 / (int)sizeof(T), B = kDropoutThreads;
     using L = unsigned long long;
-    const L vectors = d.n / V, first = (L)blockIdx.x * (256 * U) + threadIdx.x;
+    const L vectors = d.n / V, first = (L)blockIdx.x * (B * U) + threadIdx.x;
     const L offset = d.offset + (d.offset_add ? *d.offset_add : 0);
     const bool res = d.r != nullptr;
     const T *const x = static_cast<const T *>(d.x), *const r = static_cast<const T *>(d.r);
@@ -111,16 +117,17 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(DropoutArgs d) {
     uint4 a[U], b[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const L v = first + u * 256;
+        const L v = first + u * B;
         if (v >= vectors) continue;
         a[u] = *reinterpret_cast<const uint4 *>(x + at(v, d.ldx));
         if (res) b[u] = *reinterpret_cast<const uint4 *>(r + at(v, d.ldr));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const L v = first + u * 256;
+        const L v = first + u * B, block = v * (V / 4);
         if (v >= vectors) continue;
-        *reinterpret_cast<uint4 *>(y + at(v, d.ldy)) = drop_vec<T>(a[u], b[u], res, d, v * (V / 4), offset);
+        *reinterpret_cast<uint4 *>(y + at(v, d.ldy)) =
+            drop_vec<T>(a[u], b[u], res, d, LOW ? (L)(unsigned)block : block, offset);
     }
     if constexpr (FLAT) {
         const int rest = (int)(d.n - vectors * V);
@@ -182,14 +189,16 @@ qcnn_status dropout(const void *x, long long ldx, int N, int C, double p, uint64
     const bool flat = N == 1 || (ldx == C && ldy == C && (!r || ldr == C));
     if ((flat || C % V == 0) && vec(x, ldx, flat) && vec(y, ldy, flat) && (!r || vec(r, ldr, flat))) {
         const unsigned long long vectors = d.n / V;
-        const int U = vectors >= kManyVectors ? 4 : 1;
-        const unsigned long long ctas = std::max(1ull, (vectors + 256 * U - 1) / (256 * U));
+        const int per = (vectors >= kManyVectors ? 4 : 1) * kDropoutThreads;
+        const unsigned long long ctas = std::max(1ull, (vectors + per - 1) / per);
         if (ctas > INT_MAX) return QCNN_ERR_UNSUPPORTED;
+        const bool low = vectors * (V / 4) < 1ull << 32, many = vectors >= kManyVectors;
         const auto launch = [&](auto *type) {
             using T = std::remove_pointer_t<decltype(type)>;
-            const auto k = U == 4 ? (flat ? dropout_vec_kernel<T, 4, true> : dropout_vec_kernel<T, 4, false>)
-                                  : (flat ? dropout_vec_kernel<T, 1, true> : dropout_vec_kernel<T, 1, false>);
-            return launch_pdl(k, dim3((unsigned)ctas), dim3(256), 0, st, d);
+            auto k = many ? dropout_vec_kernel<T, 4, true, true> : dropout_vec_kernel<T, 1, true, true>;
+            if (!flat) k = many ? dropout_vec_kernel<T, 4, false, true> : dropout_vec_kernel<T, 1, false, true>;
+            if (!low) k = flat ? dropout_vec_kernel<T, 4, true, false> : dropout_vec_kernel<T, 4, false, false>;
+            return launch_pdl(k, dim3((unsigned)ctas), dim3(kDropoutThreads), 0, st, d);
         };
         return V == 8 ? launch(static_cast<unsigned short *>(nullptr)) : launch(static_cast<float *>(nullptr));
     }
