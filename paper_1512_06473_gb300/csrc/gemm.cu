@@ -74,16 +74,7 @@ qcnn_status set_operand(const GemmOperand &o, int P, bool gen, int rows, int row
 // are contiguous.
 qcnn_status raw_map(const void *p, long long inner, long long outer, long long row_bytes, unsigned box_x,
                     unsigned box_y, bool swizzle, CUtensorMap *map) {
-    const EncodeTiled enc = encode_tiled();
-    if (!enc) return QCNN_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-    const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
-    const cuuint32_t box[2] = {box_x, box_y}, steps[2] = {1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(p), dims, strides, box, steps,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? QCNN_OK : cuda_status(cudaErrorInvalidValue);
+    return tensor_map(CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p, inner, outer, row_bytes, box_x, box_y, swizzle, map);
 }
 // Maps and way of an fp32 A (RawWay).
 qcnn_status set_raw(const GemmOperand &o, int rows, int k, GemmArgs *g) {
@@ -218,6 +209,20 @@ static GemmPlan plan_gemm_anew(int planes, int kind, int m, int n, int k, int ma
         }
     }
     return best;
+}
+
+qcnn_status tensor_map(CUtensorMapDataType type, const void *p, long long inner, long long outer, long long row_bytes,
+                       unsigned box_x, unsigned box_y, bool swizzle, CUtensorMap *map) {
+    const EncodeTiled enc = encode_tiled();
+    if (!enc) return QCNN_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+    const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {box_x, box_y}, steps[2] = {1, 1};
+    const CUresult r = enc(map, type, 2, const_cast<void *>(p), dims, strides, box, steps,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? QCNN_OK : cuda_status(cudaErrorInvalidValue);
 }
 
 GemmPlan plan_gemm(int planes, int kind, int m, int n, int k, int max_groups) {

@@ -97,6 +97,11 @@ bool gemm_together(const GemmPlan &a, int m_a, int n_a, int k_a, const GemmPlan 
 // terms is refused.
 qcnn_status launch_gemm(const GemmPlan &plan, const GemmProblem *p, int count, cudaStream_t st);
 
+// The map of a matrix of `outer` rows for copies of boxes, in the 128-byte swizzle or none; zeros
+// outside it.
+qcnn_status tensor_map(CUtensorMapDataType type, const void *p, long long inner, long long outer, long long row_bytes,
+                       unsigned box_x, unsigned box_y, bool swizzle, CUtensorMap *map);
+
 // Smallest multiple of 8 elements: rows of 16-byte multiples.
 inline long long pad8(long long v) { return (v + 7) / 8 * 8; }
 // Of a matrix with room for whole tiles.

@@ -3,6 +3,7 @@
 //
 //   scale = max(max |x| / 127, 2^-126), q = rint(x / scale);
 //   y = act(xscale[n] wscale[m] sum_k q[n][k] W[m][k] + bias[m]) + r
+#include "int8_gemm.cuh"
 #include "train.cuh"
 
 namespace qcnn {
@@ -225,14 +226,14 @@ template <int NB, bool VEC>
 __global__ void __launch_bounds__(256) few_rows_kernel(Int8Product f) {
     constexpr int OUT = 4;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c0 = (blockIdx.x * 8 + warp) * OUT, n0 = blockIdx.y * NB;
+    const int c0 = (blockIdx.x * 8 + warp) * OUT;
     grid_dep_sync();
     if (c0 >= f.Ct) return;
     const int8_t *w[OUT], *x[NB];
 #pragma unroll
     for (int i = 0; i < OUT; ++i) w[i] = f.W + (long long)min(c0 + i, f.Ct - 1) * f.ldw;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) x[n] = f.x + (long long)min(n0 + n, f.N - 1) * f.ldx;
+    for (int n = 0; n < NB; ++n) x[n] = f.x + (long long)min(n, f.N - 1) * f.ldx;
     int acc[OUT][NB] = {};
     const int whole = VEC ? f.Cs / 16 * 16 : 0;
     for (int k = lane * 16; k < whole; k += 512) {
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(256) few_rows_kernel(Int8Product f) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             const int sum = __reduce_add_sync(0xffffffffu, acc[i][n]);
-            const int m = c0 + i, r = n0 + n;
+            const int m = c0 + i, r = n;
             if (lane != (i * NB + n) % 32 || m >= f.Ct || r >= f.N) continue;
             const GemmEpi &e = f.e;
             float v = (float)sum * f.xscale[r] * f.wscale[m];
@@ -277,25 +278,82 @@ __global__ void __launch_bounds__(256) few_rows_kernel(Int8Product f) {
         }
 }
 
+// ------------------------------------------------------------------ copies
+// What the tensor-core product cannot read as it is: codes of x as fp16, and codes of W whose rows are
+// off 16 bytes.  A warp takes pieces of rows, a lane 16 neighbours at a time.
+struct CopyJob {
+    const int8_t *src = nullptr;
+    long long ld = 0, rows = 0;
+    int cols = 0, per_row = 0, vec = 0;
+    void *dst = nullptr;
+    long long pitch = 0;  // elements, a multiple of 16 bytes
+    int blocks = 0;       // CTAs of 256 threads; 0: nothing to do
+};
+constexpr int kCopyCols = 2048;
+template <bool HALF>
+__device__ __forceinline__ void copy_part(const CopyJob &j, int block) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long all = j.rows * j.per_row;
+    for (long long i = (long long)block * 8 + warp; i < all; i += (long long)j.blocks * 8) {
+        const long long r = i / j.per_row;
+        const int first = (int)(i - r * j.per_row) * kCopyCols, end = min(j.cols, first + kCopyCols);
+        const int8_t *s = j.src + r * j.ld;
+        for (int c = first + lane * 16; c < end; c += 512) {
+            unsigned w[4] = {};
+            if (j.vec && c + 16 <= j.cols) {
+                const uint4 q = *reinterpret_cast<const uint4 *>(s + c);
+                w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (c + k < j.cols) w[k / 4] |= (unsigned)(uint8_t)s[c + k] << k % 4 * 8;
+            }
+            if constexpr (!HALF) {
+                *reinterpret_cast<uint4 *>(static_cast<int8_t *>(j.dst) + r * j.pitch + c) =
+                    make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                unsigned h[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float2 v = make_float2((float)(int8_t)(w[k / 2] >> k % 2 * 16),
+                                                 (float)(int8_t)(w[k / 2] >> (k % 2 * 16 + 8)));
+                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h[k]) : "f"(v.y), "f"(v.x));
+                }
+                uint4 *d = reinterpret_cast<uint4 *>(static_cast<unsigned short *>(j.dst) + r * j.pitch + c);
+                d[0] = make_uint4(h[0], h[1], h[2], h[3]);
+                if (c + 8 < j.pitch) d[1] = make_uint4(h[4], h[5], h[6], h[7]);
+            }
+        }
+    }
+}
+__global__ void __launch_bounds__(256) copy_kernel(CopyJob x, CopyJob w) {
+    grid_dep_sync();
+    if ((int)blockIdx.x < x.blocks) copy_part<true>(x, blockIdx.x);
+    else copy_part<false>(w, blockIdx.x - x.blocks);
+}
+
 // ------------------------------------------------------------------- space
+long long pad16(long long v) { return (v + 15) / 16 * 16; }
+bool rows16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 16 == 0; }
+bool codes_ok(const void *p, long long ld, long long rows, long long cols) { return ld >= cols && (rows == 0 || p); }
+
+// Up to 8 rows: dp4a, x as codes.  More: the tensor cores, x in fp16, W's rows on 16 bytes.
 struct Space {
-    int8_t *codes = nullptr;
+    void *x = nullptr;
     float *scale = nullptr;
+    int8_t *w = nullptr;
     size_t bytes = 0;
 };
-long long pad16(long long v) { return (v + 15) / 16 * 16; }
-Space carve(int N, int Cs, bool x_codes, void *ws) {
+Space carve(int N, int Cs, int Ct, bool x_codes, bool w_copy, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     Space s;
-    if (!x_codes) {
-        s.codes = c.array<int8_t>((size_t)N * pad16(Cs));
-        s.scale = c.array<float>(N);
-    }
+    const bool few = N <= kFewRows;
+    if (!x_codes || !few) s.x = c.take(few ? (size_t)N * pad16(Cs) : (size_t)N * pad8(Cs) * 2);
+    if (!x_codes) s.scale = c.array<float>(N);
+    if (w_copy && !few) s.w = c.array<int8_t>((size_t)Ct * pad16(Cs));
     s.bytes = c.used;
     return s;
 }
-bool rows16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 16 == 0; }
-bool codes_ok(const void *p, long long ld, long long rows, long long cols) { return ld >= cols && (rows == 0 || p); }
 
 }  // namespace
 }  // namespace qcnn
@@ -315,8 +373,7 @@ qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_
 
 qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned, size_t *bytes) {
     if (!bytes || N < 0 || Cs <= 0 || Cs > kMaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
-    (void)aligned;
-    *bytes = N ? carve(N, Cs, x_codes, nullptr).bytes : 0;
+    *bytes = N ? carve(N, Cs, Ct, x_codes, !aligned, nullptr).bytes : 0;
     return QCNN_OK;
 }
 
@@ -333,40 +390,68 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
         reinterpret_cast<uintptr_t>(xscale) % 4)
         return QCNN_ERR_INVALID_ARG;
     if (N == 0) return QCNN_OK;
-    const Space s = carve(N, Cs, xscale != nullptr, workspace);
+    const bool w_copy = !rows16(W, ldw);
+    const Space s = carve(N, Cs, Ct, xscale != nullptr, w_copy, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
     if (rc != QCNN_OK) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     PdlScope pdl;
-    Int8Product f;
-    f.x = static_cast<const int8_t *>(x);
-    f.ldx = ldx;
-    f.xscale = xscale;
+    const bool few = N <= kFewRows;
+    const int8_t *codes = static_cast<const int8_t *>(x);
     if (!xscale) {
-        rc = launch_quantize(x, ldx, N, Cs, s.codes, pad16(Cs), false, s.scale, dtype, st);
+        rc = launch_quantize(x, ldx, N, Cs, s.x, few ? pad16(Cs) : pad8(Cs), !few, s.scale, dtype, st);
         if (rc != QCNN_OK) return rc;
-        f.x = s.codes;
-        f.ldx = pad16(Cs);
-        f.xscale = s.scale;
+        xscale = s.scale;
+        codes = static_cast<const int8_t *>(s.x);
+        ldx = pad16(Cs);
     }
-    f.W = W;
-    f.ldw = ldw;
-    f.wscale = wscale;
-    f.N = N;
-    f.Cs = Cs;
-    f.Ct = Ct;
+    GemmEpi e;
     const int type = dtype == QCNN_BF16 ? GEMM_T_BF16 : GEMM_T_F32;
-    f.e.bias = bias;
-    f.e.act = act;
-    f.e.add = residual;
-    f.e.lda = ldr;
-    f.e.add_type = type;
-    f.e.out = y;
-    f.e.ldo = ldy;
-    f.e.out_type = type;
-    const bool vec = rows16(f.x, f.ldx) && rows16(W, ldw);
-    const dim3 grid(cdiv(Ct, 32), cdiv(N, N > 4 ? 8 : N));
-    if (grid.y > 65535) return QCNN_ERR_UNSUPPORTED;
+    e.bias = bias;
+    e.act = act;
+    e.add = residual;
+    e.lda = ldr;
+    e.add_type = type;
+    e.out = y;
+    e.ldo = ldy;
+    e.out_type = type;
+    if (!few) {
+        const auto job = [&](const void *src, long long ld, long long rows, void *dst, long long pitch) {
+            CopyJob j;
+            j.src = static_cast<const int8_t *>(src);
+            j.ld = ld;
+            j.rows = rows;
+            j.cols = Cs;
+            j.per_row = cdiv(Cs, kCopyCols);
+            j.vec = rows16(src, ld);
+            j.dst = dst;
+            j.pitch = pitch;
+            j.blocks = (int)std::min<long long>((rows * j.per_row + 7) / 8, (long long)num_sms() * 8);
+            return j;
+        };
+        CopyJob jx, jw;
+        if (xscale != s.scale) jx = job(x, ldx, N, s.x, pad8(Cs));
+        if (w_copy) jw = job(W, ldw, Ct, s.w, pad16(Cs));
+        if (jx.blocks + jw.blocks &&
+            (rc = launch_pdl(copy_kernel, dim3(jx.blocks + jw.blocks), dim3(256), 0, st, jx, jw)) != QCNN_OK)
+            return rc;
+        Int8Problem p;
+        p.x = s.x;
+        p.ldx = pad8(Cs);
+        p.W = w_copy ? s.w : W;
+        p.ldw = w_copy ? pad16(Cs) : ldw;
+        p.w_late = w_copy;
+        p.xscale = xscale;
+        p.wscale = wscale;
+        p.m = Ct;
+        p.n = N;
+        p.k = Cs;
+        p.e = e;
+        return launch_int8(plan_int8(Ct, N, Cs), p, st);
+    }
+    const Int8Product f{codes, W, ldx, ldw, xscale, wscale, N, Cs, Ct, e};
+    const bool vec = rows16(codes, ldx) && !w_copy;
+    const dim3 grid(cdiv(Ct, 32));
     const auto launch = [&](auto k) { return launch_pdl(k, grid, dim3(256), 0, st, f); };
     if (N == 1) return launch(vec ? few_rows_kernel<1, true> : few_rows_kernel<1, false>);
     if (N == 2) return launch(vec ? few_rows_kernel<2, true> : few_rows_kernel<2, false>);

@@ -1,0 +1,28 @@
+// int8_gemm.cuh -- the product of codes on the tensor cores (int8_gemm.cu) for int8.cu: its plan and its
+// launch.
+#pragma once
+
+#include "gemm.cuh"
+
+namespace qcnn {
+
+// y[n][m] = epilogue of xscale[n] wscale[m] sum_k x[n][k] W[m][k].
+struct Int8Problem {
+    const void *x;       // fp16 [n][k], rows of 16-byte multiples, 16-byte aligned
+    long long ldx;
+    const int8_t *W;     // [m][k], 16-byte aligned rows
+    long long ldw;
+    bool w_late = false; // W comes from a kernel of this call
+    const float *xscale, *wscale;
+    int m, n, k;
+    GemmEpi e;  // bias, act, add (beta 1), out
+};
+struct Int8Plan {
+    int cg = 1, bn = 0;
+    int splits = 1, kb_per_split = 0;  // shares of a tile's terms, a CTA of a cluster each
+    double score = 0;                  // estimated SM clocks
+};
+Int8Plan plan_int8(int m, int n, int k);
+qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t st);
+
+}  // namespace qcnn
