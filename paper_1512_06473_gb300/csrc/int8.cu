@@ -52,7 +52,9 @@ struct QuantizeArgs {
     void *codes;    // int8, or (HALF) fp16 with zeros up to the next multiple of 8
     long long ldc;  // elements
     float *scale;
-    int wide;  // codes go several at a time
+    int wide;   // codes go several at a time
+    int *sums;  // HALF: null, or of the codes' magnitudes, [rows][segs]
+    int segs;
 };
 
 // G threads a row (a warp, several or the CTA), which keep up to H vectors of 16 bytes each between
@@ -62,7 +64,14 @@ struct QuantizeArgs {
 template <typename T, int G, int H, bool SHIFT, bool HALF>
 __global__ void __launch_bounds__(G > 256 ? G : 256) quantize_kernel(QuantizeArgs a) {
     constexpr int E = (int)sizeof(T), V = 16 / E, BLOCK = G > 256 ? G : 256, ROWS = BLOCK / G;
+    // segments of 1024 codes of a row
+    constexpr int SEGS = !HALF ? 1 : G == 512 ? (kMaxTerms + 1) / kInt8Segment : G * H * V / kInt8Segment + 1;
     __shared__ float red[BLOCK / 32];
+    [[maybe_unused]] __shared__ int seg[ROWS][SEGS];
+    if constexpr (HALF) {
+        for (int i = threadIdx.x; i < ROWS * SEGS; i += BLOCK) seg[i / SEGS][i % SEGS] = 0;
+        if (G == 32) __syncthreads();  // (else a barrier follows)
+    }
     grid_dep_sync();
     const int t = threadIdx.x % G, group = threadIdx.x / G;
     const long long row = (long long)blockIdx.x * ROWS + group;
@@ -139,13 +148,16 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) quantize_kernel(QuantizeArg
 #pragma unroll
         for (int i = 0; i < G / 32; ++i) top = max_nan(top, red[group * (G / 32) + i]);
     }
-    if (!is) return;
+    if constexpr (!HALF)
+        if (!is) return;
     const RowScale s = row_scale(top);
-    if (t == 0) a.scale[row] = s.scale;
+    if (is && t == 0) a.scale[row] = s.scale;
     const bool none = s.inverse == 0.f;
-    int8_t *const bytes = static_cast<int8_t *>(a.codes) + row * a.ldc;
-    unsigned short *const halves = static_cast<unsigned short *>(a.codes) + row * a.ldc;
+    [[maybe_unused]] int8_t *const bytes = static_cast<int8_t *>(a.codes) + row * a.ldc;
+    [[maybe_unused]] unsigned short *const halves = static_cast<unsigned short *>(a.codes) + row * a.ldc;
+    // the sum of the codes' magnitudes (HALF)
     auto put = [&](unsigned v, const Vec &from) {
+        float magnitude = 0.f;
         Vec r = from;
         if (none) r = Vec{};
         float2 c[V / 2];
@@ -153,6 +165,8 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) quantize_kernel(QuantizeArg
         for (int i = 0; i < V / 2; ++i) c[i] = rounded(value(r, 2 * i), value(r, 2 * i + 1), s.inverse);
         if constexpr (HALF) {
             unsigned short *const o = halves + (size_t)v * V;
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) magnitude += fabsf(c[i].x - kRound) + fabsf(c[i].y - kRound);
             if constexpr (V == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_half(c[0]), pack_half(c[1]));
             else *reinterpret_cast<uint4 *>(o) = make_uint4(pack_half(c[0]), pack_half(c[1]), pack_half(c[2]), pack_half(c[3]));
         } else {
@@ -168,18 +182,39 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) quantize_kernel(QuantizeArg
                 for (int i = 0; i < V; ++i) o[i] = (int8_t)(w[i / 4] >> i % 4 * 8);
             }
         }
+        return magnitude;
     };
+    // (a warp's vectors, 128 or 256 codes, lie in one segment; v0: the first of them)
+    [[maybe_unused]] auto count = [&](unsigned v0, float magnitude) {
+        const int sum = __reduce_add_sync(0xffffffffu, (int)magnitude);
+        if (threadIdx.x % 32 == 0 && sum) atomicAdd(&seg[group][v0 * V / kInt8Segment], sum);
+    };
+    const unsigned t0 = t & ~31;
 #pragma unroll
-    for (int h = 0; h < H; ++h)
-        if (t + h * G < vectors) put(t + h * G, kept[h]);
+    for (int h = 0; h < H; ++h) {
+        float magnitude = 0.f;
+        if (t + h * G < vectors) magnitude = put(t + h * G, kept[h]);
+        if (HALF && a.sums && t0 + h * G < vectors) count(t0 + h * G, magnitude);
+    }
     if constexpr (H >= 5)
 #pragma unroll 2
-        for (unsigned v = t + H * G; v < vectors; v += G) put(v, load(v));
+        for (unsigned v0 = t0 + H * G; v0 < vectors; v0 += G) {
+            const unsigned v = v0 + threadIdx.x % 32;
+            float magnitude = 0.f;
+            if (v < vectors) magnitude = put(v, load(v));
+            if (HALF && a.sums) count(v0, magnitude);
+        }
     const float2 c = rounded(none ? 0.f : value(last, 0), 0.f, s.inverse);
     if constexpr (HALF) {
         const unsigned pad = (8 - a.cols % 8) % 8;
         if (t < rest) halves[(size_t)vectors * V + t] = (unsigned short)pack_half(c);
-        if (t < pad) halves[a.cols + t] = 0;
+        if (is && t < pad) halves[a.cols + t] = 0;
+        if (a.sums) {
+            if (t < rest) atomicAdd(&seg[group][(vectors * V + t) / kInt8Segment], (int)fabsf(c.x - kRound));
+            __syncthreads();
+            if (is)
+                for (int i = t; i < a.segs; i += G) a.sums[row * a.segs + i] = seg[group][i];
+        }
     } else {
         if (t < rest) bytes[(size_t)vectors * V + t] = (int8_t)__float_as_uint(c.x);
     }
@@ -203,10 +238,10 @@ qcnn_status launch_quantize_of(const QuantizeArgs &a, cudaStream_t st) {
 }
 // codes: int8, rows ldc apart; half: fp16, rows of 16-byte multiples
 qcnn_status launch_quantize(const void *x, long long ldx, int rows, int cols, void *codes, long long ldc, bool half,
-                            float *scale, int dtype, cudaStream_t st) {
+                            float *scale, int *sums, int dtype, cudaStream_t st) {
     const int V = dtype == QCNN_BF16 ? 8 : 4;
     const int wide = reinterpret_cast<uintptr_t>(codes) % V == 0 && (ldc % V == 0 || rows == 1);
-    const QuantizeArgs a{x, ldx, rows, cols, codes, ldc, scale, wide};
+    const QuantizeArgs a{x, ldx, rows, cols, codes, ldc, scale, wide, sums, cdiv(cols, kInt8Segment)};
     if (dtype == QCNN_BF16)
         return half ? launch_quantize_of<unsigned short, true>(a, st) : launch_quantize_of<unsigned short, false>(a, st);
     return half ? launch_quantize_of<float, true>(a, st) : launch_quantize_of<float, false>(a, st);
@@ -287,9 +322,10 @@ struct CopyJob {
     int cols = 0, per_row = 0, vec = 0;
     void *dst = nullptr;
     long long pitch = 0;  // elements, a multiple of 16 bytes
+    int *sums = nullptr;  // HALF: null, or of the codes' magnitudes, a piece of a row each
     int blocks = 0;       // CTAs of 256 threads; 0: nothing to do
 };
-constexpr int kCopyCols = 2048;
+constexpr int kCopyCols = kInt8Segment;
 template <bool HALF>
 __device__ __forceinline__ void copy_part(const CopyJob &j, int block) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -298,6 +334,7 @@ __device__ __forceinline__ void copy_part(const CopyJob &j, int block) {
         const long long r = i / j.per_row;
         const int first = (int)(i - r * j.per_row) * kCopyCols, end = min(j.cols, first + kCopyCols);
         const int8_t *s = j.src + r * j.ld;
+        [[maybe_unused]] int magnitude = 0;
         for (int c = first + lane * 16; c < end; c += 512) {
             unsigned w[4] = {};
             if (j.vec && c + 16 <= j.cols) {
@@ -318,10 +355,17 @@ __device__ __forceinline__ void copy_part(const CopyJob &j, int block) {
                     const float2 v = make_float2((float)(int8_t)(w[k / 2] >> k % 2 * 16),
                                                  (float)(int8_t)(w[k / 2] >> (k % 2 * 16 + 8)));
                     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h[k]) : "f"(v.y), "f"(v.x));
+                    magnitude += (int)(fabsf(v.x) + fabsf(v.y));
                 }
                 uint4 *d = reinterpret_cast<uint4 *>(static_cast<unsigned short *>(j.dst) + r * j.pitch + c);
                 d[0] = make_uint4(h[0], h[1], h[2], h[3]);
                 if (c + 8 < j.pitch) d[1] = make_uint4(h[4], h[5], h[6], h[7]);
+            }
+        }
+        if constexpr (HALF) {
+            if (j.sums) {
+                magnitude = __reduce_add_sync(0xffffffffu, magnitude);
+                if (lane == 0) j.sums[i] = magnitude;
             }
         }
     }
@@ -341,6 +385,7 @@ bool codes_ok(const void *p, long long ld, long long rows, long long cols) { ret
 struct Space {
     void *x = nullptr;
     float *scale = nullptr;
+    int *sums = nullptr;
     int8_t *w = nullptr;
     size_t bytes = 0;
 };
@@ -350,6 +395,7 @@ Space carve(int N, int Cs, int Ct, bool x_codes, bool w_copy, void *ws) {
     const bool few = N <= kFewRows;
     if (!x_codes || !few) s.x = c.take(few ? (size_t)N * pad16(Cs) : (size_t)N * pad8(Cs) * 2);
     if (!x_codes) s.scale = c.array<float>(N);
+    if (!few && int8_sums(plan_int8(Ct, N, Cs), Cs)) s.sums = c.array<int>((size_t)N * cdiv(Cs, kInt8Segment));
     if (w_copy && !few) s.w = c.array<int8_t>((size_t)Ct * pad16(Cs));
     s.bytes = c.used;
     return s;
@@ -368,7 +414,7 @@ qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_
         (N && !scale) || reinterpret_cast<uintptr_t>(scale) % 4)
         return QCNN_ERR_INVALID_ARG;
     if (N == 0) return QCNN_OK;
-    return launch_quantize(x, ldx, N, C, codes, ldc, false, scale, dtype, static_cast<cudaStream_t>(stream));
+    return launch_quantize(x, ldx, N, C, codes, ldc, false, scale, nullptr, dtype, static_cast<cudaStream_t>(stream));
 }
 
 qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned, size_t *bytes) {
@@ -399,7 +445,7 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
     const bool few = N <= kFewRows;
     const int8_t *codes = static_cast<const int8_t *>(x);
     if (!xscale) {
-        rc = launch_quantize(x, ldx, N, Cs, s.x, few ? pad16(Cs) : pad8(Cs), !few, s.scale, dtype, st);
+        rc = launch_quantize(x, ldx, N, Cs, s.x, few ? pad16(Cs) : pad8(Cs), !few, s.scale, s.sums, dtype, st);
         if (rc != QCNN_OK) return rc;
         xscale = s.scale;
         codes = static_cast<const int8_t *>(s.x);
@@ -430,7 +476,10 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
             return j;
         };
         CopyJob jx, jw;
-        if (xscale != s.scale) jx = job(x, ldx, N, s.x, pad8(Cs));
+        if (xscale != s.scale) {
+            jx = job(x, ldx, N, s.x, pad8(Cs));
+            jx.sums = s.sums;
+        }
         if (w_copy) jw = job(W, ldw, Ct, s.w, pad16(Cs));
         if (jx.blocks + jw.blocks &&
             (rc = launch_pdl(copy_kernel, dim3(jx.blocks + jw.blocks), dim3(256), 0, st, jx, jw)) != QCNN_OK)
@@ -443,6 +492,8 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
         p.w_late = w_copy;
         p.xscale = xscale;
         p.wscale = wscale;
+        p.sums = s.sums;
+        p.segs = cdiv(Cs, kInt8Segment);
         p.m = Ct;
         p.n = N;
         p.k = Cs;

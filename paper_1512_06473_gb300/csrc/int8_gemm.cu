@@ -49,6 +49,8 @@ struct Int8Args {
     unsigned stage;  // bytes of a stage of x
     unsigned idesc;
     const float *xscale, *wscale;
+    const int *sums;  // WIDE: of the magnitudes of x's codes, [n][segs], each of 1024 terms; null: segs 1
+    int segs;
     GemmEpi e;
 };
 struct Int8Shared {
@@ -70,6 +72,25 @@ __device__ __forceinline__ Int8Tile int8_tile(const Int8Args &g, int u, int shar
     t.kb1 = min(g.kblocks, t.kb0 + g.kb_per_split);
     return t;
 }
+
+// The largest sum of magnitudes of a segment in the 256 rows of x from n0 on: loads, and their maximum.
+__device__ __forceinline__ void load_sums(const Int8Args &g, int n0, int seg, int (&v)[8]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int n = n0 + lane + 32 * i;
+        v[i] = n < g.n && seg < g.segs ? g.sums[(long long)n * g.segs + seg] : 0;
+    }
+}
+__device__ __forceinline__ int most_of(const int (&v)[8]) {
+    int t = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t = max(t, v[i]);
+    return __reduce_max_sync(0xffffffffu, t);
+}
+// Where a sum in the accumulators ends (exclusive): the last segment, from k0's on, with which it is sure
+// to stay exact, any code of W being at most 128.  used: the magnitudes in it so far.
+__device__ __forceinline__ bool ends_here(int used, int next) { return used + next > (1 << 24) / 128; }
 
 __device__ __forceinline__ bool wait_for(Int8Shared &s, uint64_t *bar, unsigned parity) {
     bool ok = mbar_wait_bounded(bar, parity, 64);
@@ -120,6 +141,30 @@ __device__ __forceinline__ void tmem_st32(unsigned taddr, const unsigned (&v)[32
         : "memory");
 }
 
+// An arrival on CTA 0 of the pair, of what this thread did to tensor memory.  (Its default order, of
+// this CTA alone: with .release.cluster, which waits for what the thread has under way, a block of 64
+// terms took 1,700 clocks instead of 600.)
+__device__ __forceinline__ void arrive_first(uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\t"
+        "mapa.shared::cluster.u32 a, %0, 0;\n\t"
+        "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}\n" ::"r"(smem_addr(bar))
+        : "memory");
+}
+// 64 columns of this warp's lanes; tmem_ld_wait before they are used.
+__device__ __forceinline__ void tmem_ld32_nowait(unsigned taddr, float (&a)[16], float (&b)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]), "=f"(a[4]), "=f"(a[5]), "=f"(a[6]), "=f"(a[7]), "=f"(a[8]),
+          "=f"(a[9]), "=f"(a[10]), "=f"(a[11]), "=f"(a[12]), "=f"(a[13]), "=f"(a[14]), "=f"(a[15]), "=f"(b[0]),
+          "=f"(b[1]), "=f"(b[2]), "=f"(b[3]), "=f"(b[4]), "=f"(b[5]), "=f"(b[6]), "=f"(b[7]), "=f"(b[8]), "=f"(b[9]),
+          "=f"(b[10]), "=f"(b[11]), "=f"(b[12]), "=f"(b[13]), "=f"(b[14]), "=f"(b[15])
+        : "r"(taddr)
+        : "memory");
+}
+
 // Four codes as fp16: a byte with its sign bit turned over is code + 128, below 0x64 in the high byte
 // 1024 more; 1152 taken off leaves the code, exactly.
 __device__ __forceinline__ void widen4(unsigned w, unsigned &lo, unsigned &hi) {
@@ -129,12 +174,80 @@ __device__ __forceinline__ void widen4(unsigned w, unsigned &lo, unsigned &hi) {
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(0x64806480u));
 }
 
+// ------------------------------------------------------------------ epilogue
+// 16 columns of a lane: sums v of row m (of m_end), columns n to n + left - 1, to the result.  xs: the
+// columns' scales.  A warp's lanes are neighbours in the result; two-byte elements go in pairs where
+// pairs are aligned (gemm_kernel.cuh).  The whole warp calls it.
+__device__ __forceinline__ void int8_finish(const GemmEpi &e, int m_end, int m, int n, int left, float alpha, float bias,
+                                            const float *xs, float (&v)[16]) {
+    const bool f32 = e.out_type == GEMM_T_F32, odd = m & 1, in = m < m_end;
+    const int count = in ? min(left, 16) : 0;
+    unsigned r[16];
+    if (e.add) {  // (on its way while the activation is computed)
+        if (f32) {
+            const float *p = static_cast<const float *>(e.add) + (long long)n * e.lda + m;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) r[j] = j < count ? __float_as_uint(p[j * e.lda]) : 0;
+        } else if (e.pair & 4) {
+            const unsigned short *p = static_cast<const unsigned short *>(e.add) + (long long)(n + odd) * e.lda + (m - odd);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                r[j] = 2 * j < count - odd ? *reinterpret_cast<const unsigned *>(p + 2 * j * e.lda) : 0;
+        } else {
+            const unsigned short *p = static_cast<const unsigned short *>(e.add) + (long long)n * e.lda + m;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) r[j] = j < count ? (unsigned)p[j * e.lda] << 16 : 0;
+        }
+    }
+    const float2 a2 = make_float2(alpha, alpha), b2 = make_float2(bias, bias);
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+        const float4 s = *reinterpret_cast<const float4 *>(xs + j);
+        float2 z = __ffma2_rn(a2, __fmul2_rn(make_float2(v[j], v[j + 1]), make_float2(s.x, s.y)), b2);
+        v[j] = z.x, v[j + 1] = z.y;
+        z = __ffma2_rn(a2, __fmul2_rn(make_float2(v[j + 2], v[j + 3]), make_float2(s.z, s.w)), b2);
+        v[j + 2] = z.x, v[j + 3] = z.y;
+    }
+    act16(v, e.act);
+    if (e.add) {
+        if (!f32 && e.pair & 4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned x = exchange(r[j], odd);
+                add2(v[2 * j], v[2 * j + 1], __uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) add2(v[j], v[j + 1], __uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+        }
+    }
+    if (f32) {
+        float *p = static_cast<float *>(e.out) + (long long)n * e.ldo + m;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < count) p[j * e.ldo] = v[j];
+    } else if (e.pair & 1) {
+        unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)(n + odd) * e.ldo + (m - odd);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const unsigned x = exchange(pack_bf16x2(v[2 * j], v[2 * j + 1]), odd);
+            if (2 * j < count - odd) *reinterpret_cast<unsigned *>(p + 2 * j * e.ldo) = x;
+        }
+    } else {
+        unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)n * e.ldo + m;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < count) p[j * e.ldo] = float_to_bf16(v[j]);
+    }
+}
+
 // ------------------------------------------------------------------- kernel
 // WIDE: tiles of 256 columns.
 template <int CG, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant__ Int8Args g) {
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ Int8Shared sh;
+    __shared__ __align__(16) float column_scales[8][16];
     unsigned char *const smem = smem_raw + (-smem_addr(smem_raw) & 1023u);  // (swizzle atoms)
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -175,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
     tc_fence_after_sync();
     const unsigned tmem = sh.tmem;
 
-    if (warp < 4) set_registers<56, false>();
+    if (warp < 4) set_registers<40, false>();
     if (warp == 0) {
         // ----------------------------------------------------------- TMA of x
         if (elect_one()) {
@@ -209,48 +322,76 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         __syncwarp();
     } else if (warp == 1) {
         // --------------------------------------------------------------- MMA
-        if (rank == 0 && elect_one()) {
+        if (rank == 0) {
+            const bool lead = elect_one();
+            if (WIDE && g.sums) grid_dep_sync();
             int slot = 0;
             unsigned par = 0;
-            unsigned sums = 0;  // of up to 1024 terms, so far
+            unsigned sums = 0;  // in the accumulators, so far
             bool ok = true;
             const uint64_t desc = 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61 |
                                   (uint64_t)((smem_addr(smem) >> 4) & 0x3FFFu);
             for (int u = first_unit; u < g.units && ok; u += step) {
                 const Int8Tile t = int8_tile(g, u, share);
-                for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += kSumBlocks, ++sums) {
+                bool first = true;  // of a sum
+                [[maybe_unused]] int used = 0, more[8];
+                if (WIDE && g.sums) {
+                    load_sums(g, t.nt * 256, 0, more);
+                    used = most_of(more);
+                }
+                for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += kSumBlocks) {
                     const int k1 = min(t.kb1, k0 + kSumBlocks);
+                    if (WIDE && g.sums) load_sums(g, t.nt * 256, k0 / kSumBlocks + 1, more);
                     const unsigned buf = WIDE ? 0 : sums & 1, round = WIDE ? sums : sums >> 1;
+                    bool end = true;
                     for (int kb = k0; kb < k1; ++kb) {
-                        if (!(ok = wait_for(sh, &sh.full[slot], par))) break;
+                        if (!(ok = warp_wait_for(sh, &sh.full[slot], par))) break;
                         tc_fence_after_sync();
+                        if (WIDE && kb + 1 == k1 && k1 < t.kb1 && g.sums) {
+                            const int next = most_of(more);
+                            end = ends_here(used, next);
+                            used = end ? next : used + next;
+                        }
+                        const bool last = end && kb + 1 == k1;
                         const unsigned a = tmem + 256 + slot * kWCols;
                         const uint64_t b = desc + (uint64_t)(slot * (g.stage >> 4));
 #pragma unroll
                         for (int h = 0; h < NH; ++h) {
-                            if (kb == k0) {
-                                if (!(ok = wait_for(sh, &sh.tempty[buf + h], (round & 1) ^ 1))) break;
+                            if (first) {
+                                if (!(ok = warp_wait_for(sh, &sh.tempty[buf + h], (round & 1) ^ 1))) break;
                                 tc_fence_after_sync();
                             }
                             const unsigned d = tmem + (buf + h) * 128;
+                            if (lead) {
 #pragma unroll
-                            for (int s = 0; s < 4; ++s)
-                                mma_tmem<CG>(d, a + s * 8, b + h * (rows_x * 8) + s * 2, g.idesc, kb > k0 || s > 0);
-                            if (kb + 1 == k1 && (h + 1 < NH || NH == 1)) commit<CG>(&sh.tfull[buf + h]);
+                                for (int s = 0; s < 4; ++s)
+                                    mma_tmem<CG>(d, a + s * 8, b + h * (rows_x * 8) + s * 2, g.idesc, !first || s > 0);
+                                if (last && h + 1 < NH) commit<CG>(&sh.tfull[buf + h]);
+                            }
                         }
                         if (!ok) break;
-                        commit<CG>(&sh.empty[slot]);
-                        if (NH == 2 && kb + 1 == k1) commit<CG>(&sh.tfull[1]);
+                        first = false;
+                        if (lead) {
+                            commit<CG>(&sh.empty[slot]);
+                            if (last) commit<CG>(&sh.tfull[buf + NH - 1]);
+                        }
+                        __syncwarp();
                         if (++slot == g.S) {
                             slot = 0;
                             par ^= 1;
                         }
                     }
+                    if (end) {
+                        first = true;
+                        ++sums;
+                    }
                 }
             }
             // nothing in flight when the tensor memory is freed
-            commit_here<CG>(&sh.done);
-            mbar_wait_bounded(&sh.done, 0, kPolls);
+            if (lead) {
+                commit_here<CG>(&sh.done);
+                mbar_wait_bounded(&sh.done, 0, kPolls);
+            }
         }
         __syncwarp();
     } else if (warp == 2) {
@@ -282,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         __syncwarp();
     } else if (warp >= 4 && warp < 12) {
         // ---------------------------------------------------- drain, epilogue
-        set_registers<184, true>();
+        set_registers<200, true>();
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const unsigned tl = tmem + ((unsigned)(quarter * 32) << 16);
         grid_dep_sync();
@@ -294,6 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         unsigned sums = 0;
         bool ok = true;
         float acc[CH][16];
+        float *const scales = column_scales[warp - 4];
         auto release = [&](unsigned buf) {
             tc_fence_before_sync();
             __syncwarp();
@@ -305,42 +447,63 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         for (int u = first_unit; u < g.units; u += step) {
             const Int8Tile t = int8_tile(g, u, share);
             const int m = (t.mt * CG + (int)rank) * 128 + quarter * 32 + lane, n0 = t.nt * g.bn;
-            for (int k0 = t.kb0; k0 < t.kb1; k0 += kSumBlocks, ++sums) {
+            [[maybe_unused]] int used = 0, more[8];
+            if (WIDE && g.sums) {
+                load_sums(g, n0, 0, more);
+                used = most_of(more);
+            }
+            // (the residual's lines, from memory to the L2)
+            if (WIDE && e.add) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = n0 + half * 128 + lane + 32 * i, m1 = m - lane;
+                    if (n < g.n && m1 < g.m)
+                        asm volatile("prefetch.global.L2 [%0];\n" ::"l"(
+                            static_cast<const char *>(e.add) +
+                            ((long long)n * e.lda + m1) * (e.add_type == GEMM_T_F32 ? 4 : 2)));
+                }
+            }
+            bool first = true;
+            for (int k0 = t.kb0; k0 < t.kb1; k0 += kSumBlocks) {
+                if (WIDE && k0 + kSumBlocks < t.kb1 && g.sums) {  // (as the MMAs' warp)
+                    load_sums(g, n0, k0 / kSumBlocks + 1, more);
+                    const int next = most_of(more);
+                    const bool end = ends_here(used, next);
+                    used = end ? next : used + next;
+                    if (!end) continue;
+                }
                 const unsigned buf = WIDE ? half : sums & 1;
                 if (!(ok = warp_wait_for(sh, &sh.tfull[buf], (WIDE ? sums : sums >> 1) & 1))) break;
+                ++sums;
                 tc_fence_after_sync();
+                const unsigned from = tl + buf * 128;
+                if (WIDE && first) {
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    if (c < chunks) {
-                        float v[16];
-                        tmem_ld16(tl + buf * 128 + (WIDE ? c : 2 * c + half) * 16, v);
-                        if (k0 == t.kb0) {
+                    for (int c = 0; c < CH; c += 2) tmem_ld32_nowait(from + c * 16, acc[c], acc[c + 1]);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) acc[c][i] = v[i];
-                        } else {
+                    for (int c = 0; c < CH; ++c)
 #pragma unroll
-                            for (int i = 0; i < 16; i += 2) add2(acc[c][i], acc[c][i + 1], v[i], v[i + 1]);
+                        for (int i = 0; i < 16; ++i) asm volatile("" : "+f"(acc[c][i]));  // (not used before)
+                } else {
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        if (c < chunks) {
+                            float v[16];
+                            tmem_ld16(from + (WIDE ? c : 2 * c + half) * 16, v);
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                if (first) acc[c][i] = v[i], acc[c][i + 1] = v[i + 1];
+                                else add2(acc[c][i], acc[c][i + 1], v[i], v[i + 1]);
+                            }
                         }
                     }
                 }
+                first = false;
                 release(buf);
             }
             if (!ok) break;
-            const bool rows_full = m - lane + 32 <= g.m;
             const float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
-            [[maybe_unused]] const unsigned stash = smem_addr(smem);  // (where the stages were)
-            Chunk16 add;
-            auto fetch = [&](int i) {
-                if (e.add && i < chunks) {
-                    const int n = n0 + chunk_at(i) * 16, left = g.n - n;
-                    if (left <= 0) return;
-                    if (rows_full && left >= 16)
-                        fetch16<false, true>(add, e.add, e.add_type, e.lda, e.pair & 4, g.m, m, n, left);
-                    else
-                        fetch16<false, false>(add, e.add, e.add_type, e.lda, e.pair & 4, g.m, m, n, left);
-                }
-            };
-            if (g.cl == 1) fetch(0);
             // (the sums move through the first chunk's registers: unrolled, the epilogue's instructions
             // would come eight times)
 #pragma unroll 1
@@ -354,20 +517,17 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
 #pragma unroll
                     for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 1][j];
                 if (g.cl > 1) {  // to the cluster
-                    const unsigned d = stash + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
+                    const unsigned d = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(d + j * 512), "f"(v[4 * j]),
                                      "f"(v[4 * j + 1]), "f"(v[4 * j + 2]), "f"(v[4 * j + 3])
                                      : "memory");
                 } else if (left > 0) {
-                    const float xs = lane < 16 && lane < left ? g.xscale[n + lane] : 0.f;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] *= __shfl_sync(0xffffffffu, xs, j);
-                    if (rows_full && left >= 16)
-                        finish_out<false, true>(e, g.m, m, n, left, alpha, bias, v, add, [&] { fetch(i + 1); });
-                    else
-                        finish_out<false, false>(e, g.m, m, n, left, alpha, bias, v, add, [&] { fetch(i + 1); });
+                    __syncwarp();  // (the chunk before has been read)
+                    if (lane < 16) scales[lane] = lane < left ? g.xscale[n + lane] : 0.f;
+                    __syncwarp();
+                    int8_finish(e, g.m, m, n, left, alpha, bias, scales, v);
                 }
             }
         }
@@ -379,20 +539,14 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 cluster_sync_all();
                 const Int8Tile t = int8_tile(g, first_unit, share);
                 const int m = t.mt * 128 + quarter * 32 + lane;
-                const bool rows_full = m - lane + 32 <= g.m;
                 const float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
 #pragma unroll 1
                 for (int c = share + half * g.cl; c < g.bn / 16; c += 2 * g.cl) {
                     const int n = t.nt * g.bn + c * 16, left = g.n - n;
                     if (left <= 0) break;
-                    Chunk16 add;
-                    if (e.add) {
-                        if (rows_full && left >= 16)
-                            fetch16<false, true>(add, e.add, e.add_type, e.lda, e.pair & 4, g.m, m, n, left);
-                        else
-                            fetch16<false, false>(add, e.add, e.add_type, e.lda, e.pair & 4, g.m, m, n, left);
-                    }
-                    const float xs = lane < 16 && lane < left ? g.xscale[n + lane] : 0.f;
+                    __syncwarp();
+                    if (lane < 16) scales[lane] = lane < left ? g.xscale[n + lane] : 0.f;
+                    __syncwarp();
                     const unsigned mine = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
                     float v[16];
 #pragma unroll
@@ -411,12 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
 #pragma unroll
                         for (int i = 0; i < 16; ++i) v[i] += r[i];
                     }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] *= __shfl_sync(0xffffffffu, xs, j);
-                    if (rows_full && left >= 16)
-                        finish_out<false, true>(e, g.m, m, n, left, alpha, bias, v, add, [] {});
-                    else
-                        finish_out<false, false>(e, g.m, m, n, left, alpha, bias, v, add, [] {});
+                    int8_finish(e, g.m, m, n, left, alpha, bias, scales, v);
                 }
                 __syncwarp();
                 cluster_sync_all();  // (no CTA leaves while another reads from it)
@@ -424,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         }
     } else if (warp >= 12) {
         // -------------------------------------------------------------- widen
-        set_registers<88, false>();
+        set_registers<72, false>();
         const int quarter = warp & 3;
         const unsigned a_dst = tmem + 256 + ((unsigned)(quarter * 32) << 16);
         const unsigned own = raw0 + (quarter * 32 + lane) * 128;  // (the pieces of a row permuted: 128-byte swizzle)
@@ -435,24 +584,18 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             const Int8Tile t = int8_tile(g, u, share);
             for (int kb = t.kb0; kb < t.kb1 && ok; kb += 2) {
                 if (!(ok = warp_wait_for(sh, &sh.raw_full[rslot], rpar))) break;
-                unsigned w[32];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n"
-                                 : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
-                                 : "r"(own + rslot * kRawBytes + ((i ^ (lane & 7)) << 4)));
-                __syncwarp();
-                if (lane == 0) arrive(&sh.raw_empty[rslot]);
-                if (++rslot == kRawStages) {
-                    rslot = 0;
-                    rpar ^= 1;
-                }
+                const unsigned from = own + rslot * kRawBytes;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     if (kb + s >= t.kb1) break;
-                    unsigned v[32];
+                    unsigned w[16], v[32];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) widen4(w[16 * s + i], v[2 * i], v[2 * i + 1]);
+                    for (int i = 0; i < 4; ++i)
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n"
+                                     : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
+                                     : "r"(from + (((4 * s + i) ^ (lane & 7)) << 4)));
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) widen4(w[i], v[2 * i], v[2 * i + 1]);
                     if (!(ok = warp_wait_for(sh, &sh.empty[slot], par ^ 1))) break;
                     tc_fence_after_sync();
                     tmem_st32(a_dst + slot * kWCols, v);
@@ -461,12 +604,17 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                     __syncwarp();
                     if (lane == 0) {
                         if constexpr (CG == 1) arrive(&sh.full[slot]);
-                        else arrive_leader(&sh.full[slot]);
+                        else arrive_first(&sh.full[slot]);
                     }
                     if (++slot == g.S) {
                         slot = 0;
                         par ^= 1;
                     }
+                }
+                if (lane == 0) arrive(&sh.raw_empty[rslot]);
+                if (++rslot == kRawStages) {
+                    rslot = 0;
+                    rpar ^= 1;
                 }
             }
         }
@@ -581,6 +729,8 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
     g.S = (int)std::min<size_t>(kWStages, (kSmem - 1024 - kRawStages * (size_t)kRawBytes) / g.stage);
     // fp32 sums of fp16, 128 (256) rows x the columns of an accumulator
     g.idesc = (1u << 4) | (uint32_t)((wide ? 128 : bn) >> 3) << 17 | (uint32_t)(128 * cg >> 4) << 24;
+    g.sums = wide && p.segs > 1 ? p.sums : nullptr;
+    g.segs = p.segs;
     g.xscale = p.xscale;
     g.wscale = p.wscale;
     g.e = p.e;

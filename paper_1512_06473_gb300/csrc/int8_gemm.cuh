@@ -14,6 +14,8 @@ struct Int8Problem {
     long long ldw;
     bool w_late = false; // W comes from a kernel of this call
     const float *xscale, *wscale;
+    const int *sums = nullptr;  // of the magnitudes of x's codes, [n][segs]: of 1024 terms each (int8_sums)
+    int segs = 0;
     int m, n, k;
     GemmEpi e;  // bias, act, add (beta 1), out
 };
@@ -23,6 +25,10 @@ struct Int8Plan {
     double score = 0;                  // estimated SM clocks
 };
 Int8Plan plan_int8(int m, int n, int k);
+// Terms of a segment whose sum is exact whatever the codes are, and whether a plan of k terms goes by the
+// sums of magnitudes.
+constexpr int kInt8Segment = 1024;
+inline bool int8_sums(const Int8Plan &p, int k) { return p.bn == 256 && k > kInt8Segment; }
 qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t st);
 
 }  // namespace qcnn
