@@ -10,7 +10,6 @@ namespace qcnn {
 namespace {
 
 constexpr float kInv127 = 1.f / 127.f;
-constexpr int kMaxTerms = 131071;  // whose sum of products fits 32 bits
 
 // --------------------------------------------------------------- quantizer
 // A row's largest magnitude, NaN if it holds one (max.NaN).  |x| / scale <= 127 (1 + 2^-21), so no code
@@ -65,7 +64,7 @@ template <typename T, int G, int H, bool SHIFT, bool HALF>
 __global__ void __launch_bounds__(G > 256 ? G : 256) quantize_kernel(QuantizeArgs a) {
     constexpr int E = (int)sizeof(T), V = 16 / E, BLOCK = G > 256 ? G : 256, ROWS = BLOCK / G;
     // segments of 1024 codes of a row
-    constexpr int SEGS = !HALF ? 1 : G == 512 ? (kMaxTerms + 1) / kInt8Segment : G * H * V / kInt8Segment + 1;
+    constexpr int SEGS = !HALF ? 1 : G == 512 ? (kInt8MaxTerms + 1) / kInt8Segment : G * H * V / kInt8Segment + 1;
     __shared__ float red[BLOCK / 32];
     [[maybe_unused]] __shared__ int seg[ROWS][SEGS];
     if constexpr (HALF) {
@@ -418,7 +417,7 @@ qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_
 }
 
 qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned, size_t *bytes) {
-    if (!bytes || N < 0 || Cs <= 0 || Cs > kMaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
+    if (!bytes || N < 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
     *bytes = N ? carve(N, Cs, Ct, x_codes, !aligned, nullptr).bytes : 0;
     return QCNN_OK;
 }
@@ -427,7 +426,7 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
                                     const int8_t *W, long long ldw, const float *wscale, int Ct, const float *bias,
                                     int act, const void *residual, long long ldr, void *y, long long ldy, int dtype,
                                     void *workspace, size_t workspace_bytes, void *stream) {
-    if (N < 0 || Cs <= 0 || Cs > kMaxTerms || Ct <= 0 || !dtype_ok(dtype) || act < QCNN_ACT_NONE ||
+    if (N < 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0 || !dtype_ok(dtype) || act < QCNN_ACT_NONE ||
         act > QCNN_ACT_SILU)
         return QCNN_ERR_INVALID_ARG;
     if (!(xscale ? codes_ok(x, ldx, N, Cs) : matrix_ok(x, ldx, N, Cs, dtype)) || !codes_ok(W, ldw, Ct, Cs) ||

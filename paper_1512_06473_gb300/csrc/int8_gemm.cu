@@ -5,8 +5,8 @@
 // GB300's tensor cores multiply fp16 at many times their rate of 8-bit integers, and fp16 holds
 // every code exactly: W is widened on its way, from bytes in shared memory to tensor memory, from where
 // the MMAs take it as their operand A; x comes widened (fp16, of the pass that quantizes it) as B.  So W
-// is read once, as bytes, and shared memory carries per 64 terms and 128 rows 8 KB of W in and out beside
-// x's tile in and out.
+// is read once, as bytes, and shared memory carries per 128 terms and 128 rows 16 KB of W in and out
+// beside x's tile in and out.
 //
 // Sums.  Products of codes are integers of at most 2^14, sums of up to 1024 of them at most 2^24: fp32
 // accumulators hold every one of them exactly.  After 1024 terms a sum is drained to fp32 registers and
@@ -33,19 +33,21 @@ namespace qcnn {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kWStages = 8;            // stages of W in TMEM at most
-constexpr int kWCols = 32;             // TMEM columns of one
-constexpr int kRawTerms = 128;         // terms of a copy of W: 128 rows x 128 bytes
-constexpr unsigned kRawBytes = 128 * kRawTerms;
-constexpr int kRawStages = 4;
-constexpr int kSumBlocks = 16;         // blocks of 64 terms whose sum is exact
+constexpr int kTerms = 128;            // of a block (with half of that, its waits took a fifth of the time)
+constexpr int kStages = 4;             // blocks of W in TMEM, at most
+constexpr int kWCols = 64;             // TMEM columns of one
+constexpr unsigned kRawBytes = 128 * kTerms;  // a copy of W: 128 rows
+constexpr int kRawStagesMax = 8;
+constexpr int kSumBlocks = kInt8Segment / kTerms;  // blocks whose sum is exact, whatever the codes
+constexpr int kSegWords = (kInt8MaxTerms / kInt8Segment + 32) / 32;
 constexpr size_t kSmem = 222 * 1024;   // dynamic, with 1 KB to align the stages
 constexpr size_t kSmemFloor = 120 * 1024;  // one CTA per SM: all tensor memory is taken
 
 struct Int8Args {
     CUtensorMap map_w, map_x;
     int m, n, kblocks, m_tiles, n_tiles, kb_per_split, group, units;
-    int bn, S, cl, w_late;
+    int bn, S, R, cl, w_late;
+    int keep;        // WIDE: a tile's residual, in shared memory behind the stages
     unsigned stage;  // bytes of a stage of x
     unsigned idesc;
     const float *xscale, *wscale;
@@ -54,7 +56,9 @@ struct Int8Args {
     GemmEpi e;
 };
 struct Int8Shared {
-    uint64_t full[kWStages], empty[kWStages], raw_full[kRawStages], raw_empty[kRawStages], tfull[2], tempty[2], done;
+    uint64_t full[kStages], empty[kStages], raw_full[kRawStagesMax], raw_empty[kRawStagesMax], tfull[2], tempty[2], done;
+    uint64_t plan_full[2], plan_empty[2];
+    unsigned ends[2][kSegWords];  // of two tiles: bit s: a sum ends with segment s
     unsigned tmem;
     int give_up;
 };
@@ -72,25 +76,6 @@ __device__ __forceinline__ Int8Tile int8_tile(const Int8Args &g, int u, int shar
     t.kb1 = min(g.kblocks, t.kb0 + g.kb_per_split);
     return t;
 }
-
-// The largest sum of magnitudes of a segment in the 256 rows of x from n0 on: loads, and their maximum.
-__device__ __forceinline__ void load_sums(const Int8Args &g, int n0, int seg, int (&v)[8]) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int n = n0 + lane + 32 * i;
-        v[i] = n < g.n && seg < g.segs ? g.sums[(long long)n * g.segs + seg] : 0;
-    }
-}
-__device__ __forceinline__ int most_of(const int (&v)[8]) {
-    int t = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t = max(t, v[i]);
-    return __reduce_max_sync(0xffffffffu, t);
-}
-// Where a sum in the accumulators ends (exclusive): the last segment, from k0's on, with which it is sure
-// to stay exact, any code of W being at most 128.  used: the magnitudes in it so far.
-__device__ __forceinline__ bool ends_here(int used, int next) { return used + next > (1 << 24) / 128; }
 
 __device__ __forceinline__ bool wait_for(Int8Shared &s, uint64_t *bar, unsigned parity) {
     bool ok = mbar_wait_bounded(bar, parity, 64);
@@ -175,31 +160,64 @@ __device__ __forceinline__ void widen4(unsigned w, unsigned &lo, unsigned &hi) {
 }
 
 // ------------------------------------------------------------------ epilogue
-// 16 columns of a lane: sums v of row m (of m_end), columns n to n + left - 1, to the result.  xs: the
-// columns' scales.  A warp's lanes are neighbours in the result; two-byte elements go in pairs where
-// pairs are aligned (gemm_kernel.cuh).  The whole warp calls it.
-__device__ __forceinline__ void int8_finish(const GemmEpi &e, int m_end, int m, int n, int left, float alpha, float bias,
-                                            const float *xs, float (&v)[16]) {
-    const bool f32 = e.out_type == GEMM_T_F32, odd = m & 1, in = m < m_end;
-    const int count = in ? min(left, 16) : 0;
-    unsigned r[16];
-    if (e.add) {  // (on its way while the activation is computed)
-        if (f32) {
-            const float *p = static_cast<const float *>(e.add) + (long long)n * e.lda + m;
+// gelu(z) = max(z, 0) - |z| / 2 erfc(|z| / sqrt 2), erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 +
+// p x): Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, to 1.5e-7, here of |z| / 2.
+// silu(z) = z / (1 + exp(-z)).  In pairs, exponentials and reciprocals by the fast units (2 and 1 ulp):
+// with erff the 256 x 256 tiles of 4096 terms took longer in the epilogue than in the products.
+__device__ __forceinline__ float fast_rcp(float x) {
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ void gelu2(float &a, float &b) {
+    const float2 z = make_float2(fabsf(a), fabsf(b));
+    const float2 d = __ffma2_rn(z, both(0.3275911f * 0.70710678118654752f), both(1.f));
+    const float2 t = make_float2(fast_rcp(d.x), fast_rcp(d.y));
+    const float2 x = __fmul2_rn(__fmul2_rn(z, z), both(-0.5f * kLog2e));
+    const float2 q = make_float2(ex2(x.x), ex2(x.y));
+    float2 p = __ffma2_rn(t, both(1.061405429f), both(-1.453152027f));
+    p = __ffma2_rn(p, t, both(1.421413741f));
+    p = __ffma2_rn(p, t, both(-0.284496736f));
+    p = __ffma2_rn(p, t, both(0.254829592f));
+    p = __fmul2_rn(__fmul2_rn(p, t), __fmul2_rn(q, __fmul2_rn(z, both(-0.5f))));
+    // (from 16 on nothing of p is left; -infinity leaves NaN, as infinity times zero does)
+    a = z.x < 16.f ? fmaxf(a, 0.f) + p.x : a < 0.f ? a * 0.f : a;
+    b = z.y < 16.f ? fmaxf(b, 0.f) + p.y : b < 0.f ? b * 0.f : b;
+}
+__device__ __forceinline__ void int8_act16(float (&v)[16], int act) {
+    if (act == QCNN_ACT_RELU) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) r[j] = j < count ? __float_as_uint(p[j * e.lda]) : 0;
-        } else if (e.pair & 4) {
-            const unsigned short *p = static_cast<const unsigned short *>(e.add) + (long long)(n + odd) * e.lda + (m - odd);
+        for (int i = 0; i < 16; ++i) v[i] = act_apply(v[i], QCNN_ACT_RELU);
+    } else if (act == QCNN_ACT_GELU) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                r[j] = 2 * j < count - odd ? *reinterpret_cast<const unsigned *>(p + 2 * j * e.lda) : 0;
-        } else {
-            const unsigned short *p = static_cast<const unsigned short *>(e.add) + (long long)n * e.lda + m;
+        for (int i = 0; i < 16; i += 2) gelu2(v[i], v[i + 1]);
+    } else if (act == QCNN_ACT_SILU) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) r[j] = j < count ? (unsigned)p[j * e.lda] << 16 : 0;
-        }
+        for (int i = 0; i < 16; ++i) v[i] *= fast_rcp(1.f + ex2(-kLog2e * v[i]));
     }
-    const float2 a2 = make_float2(alpha, alpha), b2 = make_float2(bias, bias);
+}
+
+// What the residual has at 16 columns of a lane from n on; count: of them that exist.
+__device__ __forceinline__ void fetch_values(const GemmEpi &e, int m, int n, int count, float (&r)[16]) {
+    if (e.out_type == GEMM_T_F32) {
+        const float *p = static_cast<const float *>(e.add) + (long long)n * e.lda + m;
+#pragma unroll
+        for (int j = 0; j < 16; ++j, p += e.lda) r[j] = j < count ? *p : 0.f;
+    } else {
+        const unsigned short *p = static_cast<const unsigned short *>(e.add) + (long long)n * e.lda + m;
+#pragma unroll
+        for (int j = 0; j < 16; ++j, p += e.lda) r[j] = j < count ? bf16_to_float(*p) : 0.f;
+    }
+}
+// 16 columns of a lane: sums v of row m, columns n to n + count - 1, to the result.  xs: the columns'
+// scales; kept: the residual's bf16 values in shared memory, a column's every 32, or null.  A warp's lanes
+// are neighbours in the result; two-byte elements go in pairs where pairs are aligned (gemm_kernel.cuh).
+// The whole warp calls it.
+__device__ __forceinline__ void int8_finish(const GemmEpi &e, int m, int n, int count, float alpha, float bias,
+                                            const float *xs, const unsigned short *kept, float (&v)[16]) {
+    const bool odd = m & 1;
+    const float2 a2 = both(alpha), b2 = both(bias);
 #pragma unroll
     for (int j = 0; j < 16; j += 4) {
         const float4 s = *reinterpret_cast<const float4 *>(xs + j);
@@ -208,36 +226,36 @@ __device__ __forceinline__ void int8_finish(const GemmEpi &e, int m_end, int m, 
         z = __ffma2_rn(a2, __fmul2_rn(make_float2(v[j + 2], v[j + 3]), make_float2(s.z, s.w)), b2);
         v[j + 2] = z.x, v[j + 3] = z.y;
     }
-    act16(v, e.act);
-    if (e.add) {
-        if (!f32 && e.pair & 4) {
+    if (kept) {
+        int8_act16(v, e.act);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned x = exchange(r[j], odd);
-                add2(v[2 * j], v[2 * j + 1], __uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
-            }
-        } else {
+        for (int j = 0; j < 16; j += 2) add2(v[j], v[j + 1], bf16_to_float(kept[j * 32]), bf16_to_float(kept[j * 32 + 32]));
+    } else if (e.add) {
+        float r[16];
+        fetch_values(e, m, n, count, r);
+        int8_act16(v, e.act);
 #pragma unroll
-            for (int j = 0; j < 16; j += 2) add2(v[j], v[j + 1], __uint_as_float(r[j]), __uint_as_float(r[j + 1]));
-        }
+        for (int j = 0; j < 16; j += 2) add2(v[j], v[j + 1], r[j], r[j + 1]);
+    } else {
+        int8_act16(v, e.act);
     }
-    if (f32) {
+    if (e.out_type == GEMM_T_F32) {
         float *p = static_cast<float *>(e.out) + (long long)n * e.ldo + m;
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (j < count) p[j * e.ldo] = v[j];
+        for (int j = 0; j < 16; ++j, p += e.ldo)
+            if (j < count) *p = v[j];
     } else if (e.pair & 1) {
         unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)(n + odd) * e.ldo + (m - odd);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 8; ++j, p += 2 * e.ldo) {
             const unsigned x = exchange(pack_bf16x2(v[2 * j], v[2 * j + 1]), odd);
-            if (2 * j < count - odd) *reinterpret_cast<unsigned *>(p + 2 * j * e.ldo) = x;
+            if (2 * j < count - odd) *reinterpret_cast<unsigned *>(p) = x;
         }
     } else {
         unsigned short *p = static_cast<unsigned short *>(e.out) + (long long)n * e.ldo + m;
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (j < count) p[j * e.ldo] = float_to_bf16(v[j]);
+        for (int j = 0; j < 16; ++j, p += e.ldo)
+            if (j < count) *p = float_to_bf16(v[j]);
     }
 }
 
@@ -247,7 +265,7 @@ template <int CG, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant__ Int8Args g) {
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ Int8Shared sh;
-    __shared__ __align__(16) float column_scales[8][16];
+    __shared__ __align__(16) float column_scales[8][32];
     unsigned char *const smem = smem_raw + (-smem_addr(smem_raw) & 1023u);  // (swizzle atoms)
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -268,13 +286,15 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             mbar_init(&sh.full[i], 1 + 4 * CG);
             mbar_init(&sh.empty[i], 1);
         }
-        for (int i = 0; i < kRawStages; ++i) {
+        for (int i = 0; i < g.R; ++i) {
             mbar_init(&sh.raw_full[i], 1);
             mbar_init(&sh.raw_empty[i], 4);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.tfull[i], 1);
             mbar_init(&sh.tempty[i], (WIDE ? 4 : 8) * CG);
+            mbar_init(&sh.plan_full[i], 1);
+            mbar_init(&sh.plan_empty[i], 8 + (rank == 0));  // (the epilogue's warps, the MMAs' thread)
         }
         mbar_init(&sh.done, 1);
         sh.give_up = 0;
@@ -288,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
     tc_fence_after_sync();
     const unsigned tmem = sh.tmem;
 
-    if (warp < 4) set_registers<40, false>();
+    if (warp < 4) set_registers<48, false>();
     if (warp == 0) {
         // ----------------------------------------------------------- TMA of x
         if (elect_one()) {
@@ -305,8 +325,8 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                     if (rank == 0) arrive_expect(full, g.stage * CG);
                     const unsigned d = smem_addr(smem) + slot * g.stage;
 #pragma unroll
-                    for (int h = 0; h < NH; ++h)
-                        tma_box<CG>(d + h * rows_x * 128, &g.map_x, kb * 64, n0 + h * 128, full);
+                    for (int i = 0; i < 2 * NH; ++i)
+                        tma_box<CG>(d + i * rows_x * 128, &g.map_x, kb * kTerms + (i & 1) * 64, n0 + (i >> 1) * 128, full);
                     ++issued;
                     if (++slot == g.S) {
                         slot = 0;
@@ -322,76 +342,57 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         __syncwarp();
     } else if (warp == 1) {
         // --------------------------------------------------------------- MMA
-        if (rank == 0) {
-            const bool lead = elect_one();
-            if (WIDE && g.sums) grid_dep_sync();
+        if (rank == 0 && elect_one()) {
             int slot = 0;
             unsigned par = 0;
-            unsigned sums = 0;  // in the accumulators, so far
+            unsigned sums = 0, tiles = 0;  // so far
             bool ok = true;
             const uint64_t desc = 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61 |
                                   (uint64_t)((smem_addr(smem) >> 4) & 0x3FFFu);
-            for (int u = first_unit; u < g.units && ok; u += step) {
+            for (int u = first_unit; u < g.units && ok; u += step, ++tiles) {
                 const Int8Tile t = int8_tile(g, u, share);
+                const bool planned = WIDE && g.sums;
+                if (planned && !(ok = wait_for(sh, &sh.plan_full[tiles & 1], tiles >> 1 & 1))) break;
                 bool first = true;  // of a sum
-                [[maybe_unused]] int used = 0, more[8];
-                if (WIDE && g.sums) {
-                    load_sums(g, t.nt * 256, 0, more);
-                    used = most_of(more);
-                }
-                for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += kSumBlocks) {
-                    const int k1 = min(t.kb1, k0 + kSumBlocks);
-                    if (WIDE && g.sums) load_sums(g, t.nt * 256, k0 / kSumBlocks + 1, more);
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    const int seg = (kb - t.kb0) / kSumBlocks;
+                    const bool last = kb + 1 == t.kb1 || ((kb + 1 - t.kb0) % kSumBlocks == 0 &&
+                                                          (!planned || sh.ends[tiles & 1][seg / 32] >> seg % 32 & 1));
                     const unsigned buf = WIDE ? 0 : sums & 1, round = WIDE ? sums : sums >> 1;
-                    bool end = true;
-                    for (int kb = k0; kb < k1; ++kb) {
-                        if (!(ok = warp_wait_for(sh, &sh.full[slot], par))) break;
-                        tc_fence_after_sync();
-                        if (WIDE && kb + 1 == k1 && k1 < t.kb1 && g.sums) {
-                            const int next = most_of(more);
-                            end = ends_here(used, next);
-                            used = end ? next : used + next;
-                        }
-                        const bool last = end && kb + 1 == k1;
-                        const unsigned a = tmem + 256 + slot * kWCols;
-                        const uint64_t b = desc + (uint64_t)(slot * (g.stage >> 4));
+                    if (!(ok = wait_for(sh, &sh.full[slot], par))) break;
+                    tc_fence_after_sync();
+                    const unsigned a = tmem + 256 + slot * kWCols;
+                    const uint64_t b = desc + (uint64_t)(slot * (g.stage >> 4));
 #pragma unroll
-                        for (int h = 0; h < NH; ++h) {
-                            if (first) {
-                                if (!(ok = warp_wait_for(sh, &sh.tempty[buf + h], (round & 1) ^ 1))) break;
-                                tc_fence_after_sync();
-                            }
-                            const unsigned d = tmem + (buf + h) * 128;
-                            if (lead) {
+                    for (int h = 0; h < NH; ++h) {
+                        if (first) {
+                            if (!(ok = wait_for(sh, &sh.tempty[buf + h], (round & 1) ^ 1))) break;
+                            tc_fence_after_sync();
+                        }
+                        const unsigned d = tmem + (buf + h) * 128;
 #pragma unroll
-                                for (int s = 0; s < 4; ++s)
-                                    mma_tmem<CG>(d, a + s * 8, b + h * (rows_x * 8) + s * 2, g.idesc, !first || s > 0);
-                                if (last && h + 1 < NH) commit<CG>(&sh.tfull[buf + h]);
-                            }
-                        }
-                        if (!ok) break;
-                        first = false;
-                        if (lead) {
-                            commit<CG>(&sh.empty[slot]);
-                            if (last) commit<CG>(&sh.tfull[buf + NH - 1]);
-                        }
-                        __syncwarp();
-                        if (++slot == g.S) {
-                            slot = 0;
-                            par ^= 1;
-                        }
+                        for (int s = 0; s < 8; ++s)
+                            mma_tmem<CG>(d, a + s * 8, b + (2 * h + s / 4) * (rows_x * 8) + s % 4 * 2, g.idesc,
+                                         !first || s > 0);
+                        if (last && h + 1 < NH) commit<CG>(&sh.tfull[buf + h]);
                     }
-                    if (end) {
-                        first = true;
+                    if (!ok) break;
+                    commit<CG>(&sh.empty[slot]);
+                    if (last) {
+                        commit<CG>(&sh.tfull[buf + NH - 1]);
                         ++sums;
                     }
+                    first = last;
+                    if (++slot == g.S) {
+                        slot = 0;
+                        par ^= 1;
+                    }
                 }
+                if (planned) arrive(&sh.plan_empty[tiles & 1]);
             }
             // nothing in flight when the tensor memory is freed
-            if (lead) {
-                commit_here<CG>(&sh.done);
-                mbar_wait_bounded(&sh.done, 0, kPolls);
-            }
+            commit_here<CG>(&sh.done);
+            mbar_wait_bounded(&sh.done, 0, kPolls);
         }
         __syncwarp();
     } else if (warp == 2) {
@@ -406,24 +407,61 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             for (int u = first_unit; u < g.units && ok; u += step) {
                 const Int8Tile t = int8_tile(g, u, share);
                 const int m0 = (t.mt * CG + (int)rank) * 128;
-                for (int kb = t.kb0; kb < t.kb1; kb += 2) {
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!(ok = wait_for(sh, &sh.raw_empty[slot], par ^ 1))) break;
                     arrive_expect(&sh.raw_full[slot], kRawBytes);
-                    tma_load_2d(raw0 + slot * kRawBytes, &g.map_w, kb * 64, m0, &sh.raw_full[slot]);
+                    tma_load_2d(raw0 + slot * kRawBytes, &g.map_w, kb * kTerms, m0, &sh.raw_full[slot]);
                     ++issued;
-                    if (++slot == kRawStages) {
+                    if (++slot == g.R) {
                         slot = 0;
                         par ^= 1;
                     }
                 }
             }
-            for (unsigned i = issued > (unsigned)kRawStages ? issued - kRawStages : 0; i < issued; ++i)
-                mbar_wait_bounded(&sh.raw_full[i % kRawStages], i / kRawStages & 1, kPolls);
+            for (unsigned i = issued > (unsigned)g.R ? issued - g.R : 0; i < issued; ++i)
+                mbar_wait_bounded(&sh.raw_full[i % g.R], i / g.R & 1, kPolls);
+        }
+        __syncwarp();
+    } else if (WIDE && warp == 3) {
+        // ------------------------------------------------ where sums are drained
+        // A sum goes on while it is sure to stay exact: any code of W is at most 128, so while 128 times
+        // the magnitudes of x's codes in it, of the tile's row that has most in a segment, stay within
+        // 2^24.
+        if (g.sums) {
+            grid_dep_sync();
+            unsigned tiles = 0;
+            for (int u = first_unit; u < g.units; u += step, ++tiles) {
+                const Int8Tile t = int8_tile(g, u, share);
+                if (!warp_wait_for(sh, &sh.plan_empty[tiles & 1], (tiles >> 1 & 1) ^ 1)) break;
+                int used = 0;
+                unsigned word = 0;
+                for (int seg = 0; seg < g.segs; ++seg) {
+                    int most = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int n = t.nt * 256 + lane + 32 * i;
+                        if (n < g.n) most = max(most, g.sums[(long long)n * g.segs + seg]);
+                    }
+                    most = __reduce_max_sync(0xffffffffu, most);
+                    if (used + most > (1 << 24) / 128) {  // (the one before is the last)
+                        if (seg % 32) word |= 1u << (seg - 1) % 32;
+                        else if (seg && lane == 0) sh.ends[tiles & 1][seg / 32 - 1] |= 1u << 31;
+                        used = 0;
+                    }
+                    used += most;
+                    if (seg % 32 == 31 || seg + 1 == g.segs) {
+                        if (lane == 0) sh.ends[tiles & 1][seg / 32] = word;
+                        word = 0;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) arrive(&sh.plan_full[tiles & 1]);
+            }
         }
         __syncwarp();
     } else if (warp >= 4 && warp < 12) {
         // ---------------------------------------------------- drain, epilogue
-        set_registers<200, true>();
+        set_registers<192, true>();
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const unsigned tl = tmem + ((unsigned)(quarter * 32) << 16);
         grid_dep_sync();
@@ -432,10 +470,13 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         // this warp's chunk i: WIDE: of its accumulator; else every other one
         const int chunks = WIDE ? 8 : (g.bn / 16 - half + 1) / 2;
         auto chunk_at = [&](int i) { return WIDE ? half * 8 + i : 2 * i + half; };
-        unsigned sums = 0;
+        unsigned sums = 0, tiles = 0;
         bool ok = true;
         float acc[CH][16];
         float *const scales = column_scales[warp - 4];
+        unsigned short *const kept =
+            WIDE && g.keep ? reinterpret_cast<unsigned short *>(smem + g.S * g.stage + g.R * kRawBytes) + (warp - 4) * 4096
+                           : nullptr;
         auto release = [&](unsigned buf) {
             tc_fence_before_sync();
             __syncwarp();
@@ -447,31 +488,30 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         for (int u = first_unit; u < g.units; u += step) {
             const Int8Tile t = int8_tile(g, u, share);
             const int m = (t.mt * CG + (int)rank) * 128 + quarter * 32 + lane, n0 = t.nt * g.bn;
-            [[maybe_unused]] int used = 0, more[8];
-            if (WIDE && g.sums) {
-                load_sums(g, n0, 0, more);
-                used = most_of(more);
-            }
-            // (the residual's lines, from memory to the L2)
-            if (WIDE && e.add) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = n0 + half * 128 + lane + 32 * i, m1 = m - lane;
-                    if (n < g.n && m1 < g.m)
-                        asm volatile("prefetch.global.L2 [%0];\n" ::"l"(
-                            static_cast<const char *>(e.add) +
-                            ((long long)n * e.lda + m1) * (e.add_type == GEMM_T_F32 ? 4 : 2)));
+            // the residual of this warp's 32 rows x 128 columns, on its way while the products run
+            // (loaded chunk by chunk in the epilogue it took 30 to 45 us of 4096 x 4096 -> 8192)
+            if (kept) {
+                __syncwarp();  // (the tile before has been read)
+                const unsigned d = smem_addr(kept);
+                const int m1 = m - lane + (lane & 3) * 8;  // (8 rows, of a column of four pieces)
+                const unsigned bytes = (unsigned)max(0, min(8, g.m - m1)) * 2;
+#pragma unroll 4
+                for (int c = lane >> 2; c < 128; c += 8) {
+                    const int n = n0 + half * 128 + c;
+                    const bool is = n < g.n && bytes > 0;
+                    const void *src = static_cast<const unsigned short *>(e.add) + (is ? (long long)n * e.lda + m1 : 0);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(d + c * 64 + (lane & 3) * 16),
+                                 "l"(src), "r"(is ? bytes : 0u)
+                                 : "memory");
                 }
+                cp_async_commit();
             }
+            const bool planned = WIDE && g.sums;
+            if (planned && !(ok = warp_wait_for(sh, &sh.plan_full[tiles & 1], tiles >> 1 & 1))) break;
             bool first = true;
             for (int k0 = t.kb0; k0 < t.kb1; k0 += kSumBlocks) {
-                if (WIDE && k0 + kSumBlocks < t.kb1 && g.sums) {  // (as the MMAs' warp)
-                    load_sums(g, n0, k0 / kSumBlocks + 1, more);
-                    const int next = most_of(more);
-                    const bool end = ends_here(used, next);
-                    used = end ? next : used + next;
-                    if (!end) continue;
-                }
+                const int seg = (k0 - t.kb0) / kSumBlocks;
+                if (planned && k0 + kSumBlocks < t.kb1 && !(sh.ends[tiles & 1][seg / 32] >> seg % 32 & 1)) continue;
                 const unsigned buf = WIDE ? half : sums & 1;
                 if (!(ok = warp_wait_for(sh, &sh.tfull[buf], (WIDE ? sums : sums >> 1) & 1))) break;
                 ++sums;
@@ -503,34 +543,49 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 release(buf);
             }
             if (!ok) break;
+            if (planned && lane == 0) arrive(&sh.plan_empty[tiles & 1]);
+            ++tiles;
+            if (kept) {
+                cp_async_wait<0>();
+                __syncwarp();
+            }
             const float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
-            // (the sums move through the first chunk's registers: unrolled, the epilogue's instructions
-            // would come eight times)
+            // (Two chunks at a time, whose residual is fetched together; the sums move through the first
+            // two's registers: unrolled, the epilogue's instructions would come eight times.)
 #pragma unroll 1
-            for (int i = 0; i < chunks; ++i) {
-                const int c = chunk_at(i), n = n0 + c * 16, left = g.n - n;
-                float v[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = acc[0][j];
-#pragma unroll
-                for (int k = 0; k + 1 < CH; ++k)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 1][j];
+            for (int i = 0; i < chunks; i += 2) {
+                const int c0 = chunk_at(i), c1 = chunk_at(i + 1);
                 if (g.cl > 1) {  // to the cluster
-                    const unsigned d = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(d + j * 512), "f"(v[4 * j]),
-                                     "f"(v[4 * j + 1]), "f"(v[4 * j + 2]), "f"(v[4 * j + 3])
-                                     : "memory");
-                } else if (left > 0) {
-                    __syncwarp();  // (the chunk before has been read)
-                    if (lane < 16) scales[lane] = lane < left ? g.xscale[n + lane] : 0.f;
+                    for (int k = 0; k < 2; ++k) {
+                        if (i + k >= chunks) break;
+                        const unsigned d = smem_addr(smem) + (unsigned)((k ? c1 : c0) * 4 + quarter) * 2048 + lane * 16;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(d + j * 512),
+                                         "f"(acc[k][4 * j]), "f"(acc[k][4 * j + 1]), "f"(acc[k][4 * j + 2]),
+                                         "f"(acc[k][4 * j + 3])
+                                         : "memory");
+                    }
+                } else {
+                    const int n1 = n0 + c0 * 16, n2 = n0 + c1 * 16;
+                    const int left1 = g.n - n1, left2 = i + 1 < chunks ? g.n - n2 : 0;
+                    const int count1 = m < g.m ? min(left1, 16) : 0, count2 = m < g.m ? min(left2, 16) : 0;
+                    __syncwarp();  // (the columns before have been read)
+                    const int left = lane < 16 ? left1 : left2, at = lane & 15;
+                    scales[lane] = at < left ? g.xscale[(lane < 16 ? n1 : n2) + at] : 0.f;
                     __syncwarp();
-                    int8_finish(e, g.m, m, n, left, alpha, bias, scales, v);
+                    const unsigned short *const r = kept ? kept + i * 512 + lane : nullptr;
+                    if (left1 > 0) int8_finish(e, m, n1, count1, alpha, bias, scales, r, acc[0]);
+                    if (left2 > 0) int8_finish(e, m, n2, count2, alpha, bias, scales + 16, r ? r + 512 : r, acc[1]);
                 }
+#pragma unroll
+                for (int k = 0; k + 2 < CH; ++k)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 2][j];
             }
         }
+        if (kept) cp_async_wait<0>();
         if constexpr (CG == 1) {
             if (g.cl > 1) {
                 // The sums of a tile's shares meet in shared memory, where each CTA has left its own: each
@@ -544,6 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 for (int c = share + half * g.cl; c < g.bn / 16; c += 2 * g.cl) {
                     const int n = t.nt * g.bn + c * 16, left = g.n - n;
                     if (left <= 0) break;
+                    const int count = m < g.m ? min(left, 16) : 0;
                     __syncwarp();
                     if (lane < 16) scales[lane] = lane < left ? g.xscale[n + lane] : 0.f;
                     __syncwarp();
@@ -555,17 +611,17 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                     for (int s = 0; s < g.cl; ++s) {
                         unsigned at;
                         asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(mine), "r"(s));
-                        float r[16];
+                        float o[16];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n"
-                                         : "=f"(r[4 * i]), "=f"(r[4 * i + 1]), "=f"(r[4 * i + 2]), "=f"(r[4 * i + 3])
+                                         : "=f"(o[4 * i]), "=f"(o[4 * i + 1]), "=f"(o[4 * i + 2]), "=f"(o[4 * i + 3])
                                          : "r"(at + i * 512)
                                          : "memory");
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] += r[i];
+                        for (int i = 0; i < 16; ++i) v[i] += o[i];
                     }
-                    int8_finish(e, g.m, m, n, left, alpha, bias, scales, v);
+                    int8_finish(e, m, n, count, alpha, bias, scales, nullptr, v);
                 }
                 __syncwarp();
                 cluster_sync_all();  // (no CTA leaves while another reads from it)
@@ -573,49 +629,56 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         }
     } else if (warp >= 12) {
         // -------------------------------------------------------------- widen
-        set_registers<72, false>();
+        set_registers<80, false>();
         const int quarter = warp & 3;
         const unsigned a_dst = tmem + 256 + ((unsigned)(quarter * 32) << 16);
         const unsigned own = raw0 + (quarter * 32 + lane) * 128;  // (the pieces of a row permuted: 128-byte swizzle)
         int slot = 0, rslot = 0;
         unsigned par = 0, rpar = 0;
         bool ok = true;
-        for (int u = first_unit; u < g.units && ok; u += step) {
+        int left = 0;  // blocks
+        for (int u = first_unit; u < g.units; u += step) {
             const Int8Tile t = int8_tile(g, u, share);
-            for (int kb = t.kb0; kb < t.kb1 && ok; kb += 2) {
-                if (!(ok = warp_wait_for(sh, &sh.raw_full[rslot], rpar))) break;
-                const unsigned from = own + rslot * kRawBytes;
+            left += t.kb1 - t.kb0;
+        }
+        unsigned w[32];
+        auto read = [&] {
+            if (!(ok = warp_wait_for(sh, &sh.raw_full[rslot], rpar))) return;
+            const unsigned from = own + rslot * kRawBytes;
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (kb + s >= t.kb1) break;
-                    unsigned w[16], v[32];
+            for (int i = 0; i < 8; ++i)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n"
+                             : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
+                             : "r"(from + ((i ^ (lane & 7)) << 4)));
+        };
+        if (left) read();
+        for (; left > 0 && ok; --left) {
+            if (!(ok = warp_wait_for(sh, &sh.empty[slot], par ^ 1))) break;
+            tc_fence_after_sync();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n"
-                                     : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
-                                     : "r"(from + (((4 * s + i) ^ (lane & 7)) << 4)));
+            for (int s = 0; s < 2; ++s) {
+                unsigned v[32];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) widen4(w[i], v[2 * i], v[2 * i + 1]);
-                    if (!(ok = warp_wait_for(sh, &sh.empty[slot], par ^ 1))) break;
-                    tc_fence_after_sync();
-                    tmem_st32(a_dst + slot * kWCols, v);
-                    asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 1) arrive(&sh.full[slot]);
-                        else arrive_first(&sh.full[slot]);
-                    }
-                    if (++slot == g.S) {
-                        slot = 0;
-                        par ^= 1;
-                    }
-                }
-                if (lane == 0) arrive(&sh.raw_empty[rslot]);
-                if (++rslot == kRawStages) {
-                    rslot = 0;
-                    rpar ^= 1;
-                }
+                for (int i = 0; i < 16; ++i) widen4(w[16 * s + i], v[2 * i], v[2 * i + 1]);
+                tmem_st32(a_dst + slot * kWCols + s * 32, v);
+            }
+            __syncwarp();  // (all have read)
+            if (lane == 0) arrive(&sh.raw_empty[rslot]);
+            if (++rslot == g.R) {
+                rslot = 0;
+                rpar ^= 1;
+            }
+            if (left > 1) read();  // (the next, while the stores are under way)
+            asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (CG == 1) arrive(&sh.full[slot]);
+                else arrive_first(&sh.full[slot]);
+            }
+            if (++slot == g.S) {
+                slot = 0;
+                par ^= 1;
             }
         }
     }
@@ -649,37 +712,36 @@ bool in_pairs(const void *p, int type, long long ld, int m) {
 
 Int8Plan plan_int8_anew(int m, int n, int k, int sms) {
     Int8Plan best;
-    const int kblocks = cdiv(k, 64);
+    const int kblocks = cdiv(k, kTerms);
     static const int tiles[5] = {16, 32, 64, 128, 256};
-    for (int cg = 1; cg <= 2; ++cg)
-        for (int bn : tiles) {
-            if (cg == 2 && bn != 256) continue;
-            if (bn > 16 && bn >= 2 * n) continue;
-            const int mt = cdiv(m, 128 * cg), nt = cdiv(n, bn);
-            const long long units = (long long)mt * nt;
-            // clocks of a block of 64 terms: MMAs; bytes of W at the memory's rate when all SMs read, with
-            // x's at TMA's; shared memory, in and out; the widening
-            const double mma = 4 * (bn / 2 + 10.0), w = 8192.0, x = bn / cg * 128.0;
-            const double per = std::max({mma, w / 23.0, (w + x) / 50.0, 2 * (w + x) / 128.0, 250.0});
-            const double tail = 4500.0 + bn * 16.0;
-            for (int cl = 1; cl <= 8; cl *= 2) {
-                if (cl > 1 && (cg > 1 || bn > 128 || 2 * cl > kblocks)) break;
-                const int kps = cdiv(cdiv(kblocks, cl), 2) * 2;
-                if (cdiv(kblocks, kps) != cl) continue;
-                const int slots = cl == 1 ? sms / cg
-                                          : std::max(1, cluster_capacity(reinterpret_cast<const void *>(int8_kernel<1, false>),
-                                                                         kThreads, cl, kSmem));
-                const double waves = (double)((units + slots - 1) / slots);
-                const double meet = cl > 1 ? 2500.0 + bn * 10.0 : 0.0, more = cl > 1 ? tail + meet : 1000.0;
-                const double score = waves * kps * per + tail + meet + (waves - 1) * more;
-                if (best.bn && score >= best.score) continue;
-                best.cg = cg;
-                best.bn = bn;
-                best.splits = cl;
-                best.kb_per_split = kps;
-                best.score = score;
-            }
+    for (int bn : tiles) {
+        const int cg = bn == 256 ? 2 : 1;
+        if (bn > 16 && bn >= 2 * n) continue;
+        const int mt = cdiv(m, 128 * cg), nt = cdiv(n, bn);
+        const long long units = (long long)mt * nt;
+        // clocks of a block of 128 terms: MMAs; bytes of W at the memory's rate when all SMs read, with
+        // x's at TMA's; shared memory, in and out; the widening
+        const double mma = 8 * (bn / 2 + 10.0), w = kRawBytes, x = bn / cg * 256.0;
+        const double per = std::max({mma, w / 23.0, (w + x) / 50.0, 2 * (w + x) / 128.0, 500.0});
+        const double tail = 4500.0 + bn * 16.0;
+        for (int cl = 1; cl <= 8; cl *= 2) {
+            if (cl > 1 && (cg > 1 || cl > kblocks)) break;
+            const int kps = cdiv(kblocks, cl);
+            if (cdiv(kblocks, kps) != cl) continue;
+            const int slots = cl == 1 ? sms / cg
+                                      : std::max(1, cluster_capacity(reinterpret_cast<const void *>(int8_kernel<1, false>),
+                                                                     kThreads, cl, kSmem));
+            const double waves = (double)((units + slots - 1) / slots);
+            const double meet = cl > 1 ? 2500.0 + bn * 10.0 : 0.0, more = cl > 1 ? tail + meet : 1000.0;
+            const double score = waves * kps * per + tail + meet + (waves - 1) * more;
+            if (best.bn && score >= best.score) continue;
+            best.cg = cg;
+            best.bn = bn;
+            best.splits = cl;
+            best.kb_per_split = kps;
+            best.score = score;
         }
+    }
     return best;
 }
 
@@ -705,13 +767,13 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
     Int8Args g = {};
     const int cg = plan.cg, bn = plan.bn, wide = bn == 256;
     const int box = (wide ? 128 : bn) / cg;  // rows of x at a time
-    qcnn_status rc = tensor_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, p.W, p.k, p.m, p.ldw, kRawTerms, 128, true, &g.map_w);
+    qcnn_status rc = tensor_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, p.W, p.k, p.m, p.ldw, kTerms, 128, true, &g.map_w);
     if (rc != QCNN_OK) return rc;
     rc = tensor_map(CU_TENSOR_MAP_DATA_TYPE_FLOAT16, p.x, p.k, p.n, p.ldx * 2, 64, box, true, &g.map_x);
     if (rc != QCNN_OK) return rc;
     g.m = p.m;
     g.n = p.n;
-    g.kblocks = cdiv(p.k, 64);
+    g.kblocks = cdiv(p.k, kTerms);
     g.m_tiles = cdiv(p.m, 128 * cg);
     g.n_tiles = cdiv(p.n, bn);
     g.kb_per_split = plan.splits > 1 ? plan.kb_per_split : g.kblocks;
@@ -725,8 +787,12 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
     g.bn = bn;
     g.cl = plan.splits;
     g.w_late = p.w_late;
-    g.stage = (unsigned)(bn / cg * 128);
-    g.S = (int)std::min<size_t>(kWStages, (kSmem - 1024 - kRawStages * (size_t)kRawBytes) / g.stage);
+    g.stage = (unsigned)(bn / cg * 2 * kTerms);
+    g.keep = wide && p.e.add && p.e.out_type == GEMM_T_BF16 && reinterpret_cast<uintptr_t>(p.e.add) % 16 == 0 &&
+             p.e.lda % 8 == 0;
+    const size_t keep = g.keep ? 128 * 256 * 2 : 0;
+    g.S = g.keep ? kStages - 1 : kStages;
+    g.R = (int)std::min<size_t>(kRawStagesMax, (kSmem - 1024 - keep - g.S * (size_t)g.stage) / kRawBytes);
     // fp32 sums of fp16, 128 (256) rows x the columns of an accumulator
     g.idesc = (1u << 4) | (uint32_t)((wide ? 128 : bn) >> 3) << 17 | (uint32_t)(128 * cg >> 4) << 24;
     g.sums = wide && p.segs > 1 ? p.sums : nullptr;
@@ -735,13 +801,11 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
     g.wscale = p.wscale;
     g.e = p.e;
     g.e.beta = 1.f;
-    g.e.pair = (in_pairs(p.e.out, p.e.out_type, p.e.ldo, p.m) ? 1 : 0) |
-               (in_pairs(p.e.add, p.e.add_type, p.e.lda, p.m) ? 4 : 0);
+    g.e.pair = in_pairs(p.e.out, p.e.out_type, p.e.ldo, p.m) ? 1 : 0;
     const size_t stash = g.cl > 1 ? (size_t)bn * 512 : 0;
-    const size_t smem = std::max({kSmemFloor, g.S * (size_t)g.stage + kRawStages * (size_t)kRawBytes + 1024, stash + 1024});
+    const size_t smem = std::max({kSmemFloor, g.S * (size_t)g.stage + g.R * (size_t)kRawBytes + keep + 1024, stash + 1024});
     const int ctas = g.cl > 1 ? g.units * g.cl : std::min(g.units, num_sms() / cg) * cg;
-    if (cg == 2) return launch_of<2, true>(g, ctas, smem, st);
-    return wide ? launch_of<1, true>(g, ctas, smem, st) : launch_of<1, false>(g, ctas, smem, st);
+    return wide ? launch_of<2, true>(g, ctas, smem, st) : launch_of<1, false>(g, ctas, smem, st);
 }
 
 }  // namespace qcnn
