@@ -47,7 +47,8 @@ struct Int8Args {
     CUtensorMap map_w, map_x;
     int m, n, kblocks, m_tiles, n_tiles, kb_per_split, group, units;
     int bn, S, R, cl, w_late;
-    int keep;        // WIDE: a tile's residual, in shared memory behind the stages
+    int staged;      // WIDE: results (and the residual) pass through shared memory behind the stages
+    CUtensorMap map_out, map_add;
     unsigned stage;  // bytes of a stage of x
     unsigned idesc;
     const float *xscale, *wscale;
@@ -58,6 +59,7 @@ struct Int8Args {
 struct Int8Shared {
     uint64_t full[kStages], empty[kStages], raw_full[kRawStagesMax], raw_empty[kRawStagesMax], tfull[2], tempty[2], done;
     uint64_t plan_full[2], plan_empty[2];
+    uint64_t residual[8];
     unsigned ends[2][kSegWords];  // of two tiles: bit s: a sum ends with segment s
     unsigned tmem;
     int give_up;
@@ -170,20 +172,25 @@ __device__ __forceinline__ float fast_rcp(float x) {
     return r;
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float above_zero(float a) {  // (NaN stays)
+    float r;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(a));
+    return r;
+}
 __device__ __forceinline__ void gelu2(float &a, float &b) {
-    const float2 z = make_float2(fabsf(a), fabsf(b));
-    const float2 d = __ffma2_rn(z, both(0.3275911f * 0.70710678118654752f), both(1.f));
-    const float2 t = make_float2(fast_rcp(d.x), fast_rcp(d.y));
-    const float2 x = __fmul2_rn(__fmul2_rn(z, z), both(-0.5f * kLog2e));
+    const float2 z = make_float2(a, b);
+    constexpr float kP = 0.3275911f * 0.70710678118654752f;
+    const float2 t = make_float2(fast_rcp(fmaf(fabsf(a), kP, 1.f)), fast_rcp(fmaf(fabsf(b), kP, 1.f)));
+    const float2 x = __fmul2_rn(__fmul2_rn(z, both(-0.5f * kLog2e)), z);
     const float2 q = make_float2(ex2(x.x), ex2(x.y));
-    float2 p = __ffma2_rn(t, both(1.061405429f), both(-1.453152027f));
-    p = __ffma2_rn(p, t, both(1.421413741f));
-    p = __ffma2_rn(p, t, both(-0.284496736f));
-    p = __ffma2_rn(p, t, both(0.254829592f));
-    p = __fmul2_rn(__fmul2_rn(p, t), __fmul2_rn(q, __fmul2_rn(z, both(-0.5f))));
-    // (from 16 on nothing of p is left; -infinity leaves NaN, as infinity times zero does)
-    a = z.x < 16.f ? fmaxf(a, 0.f) + p.x : a < 0.f ? a * 0.f : a;
-    b = z.y < 16.f ? fmaxf(b, 0.f) + p.y : b < 0.f ? b * 0.f : b;
+    // (the polynomial times -1/2)
+    float2 p = __ffma2_rn(t, both(-0.5f * 1.061405429f), both(0.5f * 1.453152027f));
+    p = __ffma2_rn(p, t, both(-0.5f * 1.421413741f));
+    p = __ffma2_rn(p, t, both(0.5f * 0.284496736f));
+    p = __ffma2_rn(p, t, both(-0.5f * 0.254829592f));
+    p = __fmul2_rn(__fmul2_rn(p, t), q);
+    a = fmaf(fabsf(a), p.x, above_zero(a));  // (an infinite z leaves NaN: q is 0)
+    b = fmaf(fabsf(b), p.y, above_zero(b));
 }
 __device__ __forceinline__ void int8_act16(float (&v)[16], int act) {
     if (act == QCNN_ACT_RELU) {
@@ -198,6 +205,56 @@ __device__ __forceinline__ void int8_act16(float (&v)[16], int act) {
     }
 }
 
+// v = alpha xs v + bias of 16 columns.
+__device__ __forceinline__ void scaled16(float (&v)[16], const float *xs, float alpha, float bias) {
+    const float2 a2 = both(alpha), b2 = both(bias);
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+        const float4 s = *reinterpret_cast<const float4 *>(xs + j);
+        float2 z = __ffma2_rn(a2, __fmul2_rn(make_float2(v[j], v[j + 1]), make_float2(s.x, s.y)), b2);
+        v[j] = z.x, v[j + 1] = z.y;
+        z = __ffma2_rn(a2, __fmul2_rn(make_float2(v[j + 2], v[j + 3]), make_float2(s.z, s.w)), b2);
+        v[j + 2] = z.x, v[j + 3] = z.y;
+    }
+}
+
+// WIDE, where TMA can write the result (and read the residual): a warp's 32 rows x 64 columns pass
+// through its part of shared memory, [column][row], the residual there before and the result after, each
+// element a lane's own.  Few instructions for an element are what counts: a tile's epilogue is run
+// through once, from an instruction cache that does not hold it (stores from registers, with their
+// addresses and edges, were 235 instructions per 16 columns, and as long as the products of 1024 terms).
+constexpr unsigned kStagedBytes = 8192;  // of a warp: 128 columns of bf16, 64 of fp32
+template <typename T>
+__device__ __forceinline__ void staged16(float (&v)[16], const float *xs, float alpha, float bias, int act, bool res,
+                                         T *at) {
+    scaled16(v, xs, alpha, bias);
+    int8_act16(v, act);
+    if (res) {
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            if constexpr (sizeof(T) == 4) add2(v[j], v[j + 1], at[j * 32], at[j * 32 + 32]);
+            else add2(v[j], v[j + 1], bf16_to_float(at[j * 32]), bf16_to_float(at[j * 32 + 32]));
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 16; j += 2) {
+        if constexpr (sizeof(T) == 4) {
+            at[j * 32] = v[j], at[j * 32 + 32] = v[j + 1];
+        } else {
+            const unsigned w = pack_bf16x2(v[j], v[j + 1]);
+            at[j * 32] = (unsigned short)w, at[j * 32 + 32] = (unsigned short)(w >> 16);
+        }
+    }
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, unsigned src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n" ::"l"(map),
+                 "r"(x), "r"(y), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
+}
+// Until this thread's stores have read their shared memory.
+__device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
+
 // What the residual has at 16 columns of a lane from n on; count: of them that exist.
 __device__ __forceinline__ void fetch_values(const GemmEpi &e, int m, int n, int count, float (&r)[16]) {
     if (e.out_type == GEMM_T_F32) {
@@ -211,26 +268,13 @@ __device__ __forceinline__ void fetch_values(const GemmEpi &e, int m, int n, int
     }
 }
 // 16 columns of a lane: sums v of row m, columns n to n + count - 1, to the result.  xs: the columns'
-// scales; kept: the residual's bf16 values in shared memory, a column's every 32, or null.  A warp's lanes
-// are neighbours in the result; two-byte elements go in pairs where pairs are aligned (gemm_kernel.cuh).
-// The whole warp calls it.
+// scales.  A warp's lanes are neighbours in the result; two-byte elements go in pairs where pairs are
+// aligned (gemm_kernel.cuh).  The whole warp calls it.
 __device__ __forceinline__ void int8_finish(const GemmEpi &e, int m, int n, int count, float alpha, float bias,
-                                            const float *xs, const unsigned short *kept, float (&v)[16]) {
+                                            const float *xs, float (&v)[16]) {
     const bool odd = m & 1;
-    const float2 a2 = both(alpha), b2 = both(bias);
-#pragma unroll
-    for (int j = 0; j < 16; j += 4) {
-        const float4 s = *reinterpret_cast<const float4 *>(xs + j);
-        float2 z = __ffma2_rn(a2, __fmul2_rn(make_float2(v[j], v[j + 1]), make_float2(s.x, s.y)), b2);
-        v[j] = z.x, v[j + 1] = z.y;
-        z = __ffma2_rn(a2, __fmul2_rn(make_float2(v[j + 2], v[j + 3]), make_float2(s.z, s.w)), b2);
-        v[j + 2] = z.x, v[j + 3] = z.y;
-    }
-    if (kept) {
-        int8_act16(v, e.act);
-#pragma unroll
-        for (int j = 0; j < 16; j += 2) add2(v[j], v[j + 1], bf16_to_float(kept[j * 32]), bf16_to_float(kept[j * 32 + 32]));
-    } else if (e.add) {
+    scaled16(v, xs, alpha, bias);
+    if (e.add) {
         float r[16];
         fetch_values(e, m, n, count, r);
         int8_act16(v, e.act);
@@ -265,7 +309,7 @@ template <int CG, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant__ Int8Args g) {
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ Int8Shared sh;
-    __shared__ __align__(16) float column_scales[8][32];
+    __shared__ __align__(16) float column_scales[8][128];
     unsigned char *const smem = smem_raw + (-smem_addr(smem_raw) & 1023u);  // (swizzle atoms)
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -296,6 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             mbar_init(&sh.plan_full[i], 1);
             mbar_init(&sh.plan_empty[i], 8 + (rank == 0));  // (the epilogue's warps, the MMAs' thread)
         }
+        for (int i = 0; i < 8; ++i) mbar_init(&sh.residual[i], 1);
         mbar_init(&sh.done, 1);
         sh.give_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -474,9 +519,21 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         bool ok = true;
         float acc[CH][16];
         float *const scales = column_scales[warp - 4];
-        unsigned short *const kept =
-            WIDE && g.keep ? reinterpret_cast<unsigned short *>(smem + g.S * g.stage + g.R * kRawBytes) + (warp - 4) * 4096
-                           : nullptr;
+        // (WIDE) this warp's part of the shared memory that results pass through
+        [[maybe_unused]] unsigned char *const mine = smem + g.S * g.stage + g.R * kRawBytes + (warp - 4) * kStagedBytes;
+        [[maybe_unused]] const bool f32 = e.out_type == GEMM_T_F32, lead = elect_one();
+        [[maybe_unused]] uint64_t *const there = &sh.residual[warp - 4];
+        [[maybe_unused]] unsigned loads = 0;  // of the residual, so far
+        // 64 columns of the residual (bf16: and the next 64), when what was stored from there has been read
+        [[maybe_unused]] auto load_residual = [&](int x, int y) {
+            if (lead) {
+                tma_stores_read();
+                arrive_expect(there, 8192);
+                tma_load_2d(smem_addr(mine), &g.map_add, x, y, there);
+                if (!f32) tma_load_2d(smem_addr(mine) + 4096, &g.map_add, x, y + 64, there);
+            }
+            ++loads;
+        };
         auto release = [&](unsigned buf) {
             tc_fence_before_sync();
             __syncwarp();
@@ -488,24 +545,18 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         for (int u = first_unit; u < g.units; u += step) {
             const Int8Tile t = int8_tile(g, u, share);
             const int m = (t.mt * CG + (int)rank) * 128 + quarter * 32 + lane, n0 = t.nt * g.bn;
-            // the residual of this warp's 32 rows x 128 columns, on its way while the products run
-            // (loaded chunk by chunk in the epilogue it took 30 to 45 us of 4096 x 4096 -> 8192)
-            if (kept) {
-                __syncwarp();  // (the tile before has been read)
-                const unsigned d = smem_addr(kept);
-                const int m1 = m - lane + (lane & 3) * 8;  // (8 rows, of a column of four pieces)
-                const unsigned bytes = (unsigned)max(0, min(8, g.m - m1)) * 2;
-#pragma unroll 4
-                for (int c = lane >> 2; c < 128; c += 8) {
-                    const int n = n0 + half * 128 + c;
-                    const bool is = n < g.n && bytes > 0;
-                    const void *src = static_cast<const unsigned short *>(e.add) + (is ? (long long)n * e.lda + m1 : 0);
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(d + c * 64 + (lane & 3) * 16),
-                                 "l"(src), "r"(is ? bytes : 0u)
-                                 : "memory");
-                }
-                cp_async_commit();
+            // the scales of its columns
+            __syncwarp();  // (the tile before has been read)
+#pragma unroll
+            for (int i = lane; i < 128; i += 32) {
+                const int n = n0 + (WIDE ? half * 128 : 0) + i;
+                scales[i] = n < g.n ? g.xscale[n] : 0.f;
             }
+            __syncwarp();
+            const float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
+            // the residual, on its way while the products run
+            const int mw = m - lane, nw = n0 + half * 128;
+            if (WIDE && g.staged && e.add) load_residual(mw, nw);
             const bool planned = WIDE && g.sums;
             if (planned && !(ok = warp_wait_for(sh, &sh.plan_full[tiles & 1], tiles >> 1 & 1))) break;
             bool first = true;
@@ -545,47 +596,73 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             if (!ok) break;
             if (planned && lane == 0) arrive(&sh.plan_empty[tiles & 1]);
             ++tiles;
-            if (kept) {
-                cp_async_wait<0>();
-                __syncwarp();
-            }
-            const float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
-            // (Two chunks at a time, whose residual is fetched together; the sums move through the first
-            // two's registers: unrolled, the epilogue's instructions would come eight times.)
+            // (Four chunks at a time; the sums move through their registers: all eight unrolled, the
+            // epilogue's instructions would come eight times, and each move counts too.)
+            if (WIDE && g.staged) {
+                const auto rounds = [&](auto *at) {  // of 64 columns
 #pragma unroll 1
-            for (int i = 0; i < chunks; i += 2) {
-                const int c0 = chunk_at(i), c1 = chunk_at(i + 1);
-                if (g.cl > 1) {  // to the cluster
+                    for (int i = 0; i < 2; ++i) {
+                        if (e.add && (i == 0 || f32)) {
+                            if (!(ok = warp_wait_for(sh, there, (loads - 1) & 1))) return;
+                        } else if (i == 0 || f32) {
+                            if (lead) tma_stores_read();
+                            __syncwarp();
+                        }
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        if (i + k >= chunks) break;
-                        const unsigned d = smem_addr(smem) + (unsigned)((k ? c1 : c0) * 4 + quarter) * 2048 + lane * 16;
+                        for (int k = 0; k < 4; ++k)
+                            staged16(acc[k], scales + (4 * i + k) * 16, alpha, bias, e.act, e.add, at + k * 512);
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lead && mw < g.m && nw + i * 64 < g.n)  // (else none of it is in the matrix)
+                            tma_store(&g.map_out, mw, nw + i * 64, smem_addr(mine) + (f32 ? 0 : i * 4096));
+                        if (i == 0) {
+                            if (!f32) at += 2048;
+                            else if (e.add) load_residual(mw, nw + 64);
+#pragma unroll
+                            for (int k = 0; k + 4 < CH; ++k)
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 4][j];
+                        }
+                    }
+                };
+                if (f32) rounds(reinterpret_cast<float *>(mine) + lane);
+                else rounds(reinterpret_cast<unsigned short *>(mine) + lane);
+                if (!ok) break;
+                continue;
+            }
+            const float *const xs = scales - (WIDE ? half * 128 : 0);
+#pragma unroll 1
+            for (int i = 0; i < chunks; i += 4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = chunk_at(i + k), n = n0 + c * 16, left = g.n - n;
+                    if (i + k >= chunks) break;
+                    if (g.cl > 1) {  // to the cluster
+                        const unsigned d = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
                             asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(d + j * 512),
                                          "f"(acc[k][4 * j]), "f"(acc[k][4 * j + 1]), "f"(acc[k][4 * j + 2]),
                                          "f"(acc[k][4 * j + 3])
                                          : "memory");
+                    } else if (left > 0) {
+                        int8_finish(e, m, n, m < g.m ? min(left, 16) : 0, alpha, bias, xs + c * 16, acc[k]);
                     }
-                } else {
-                    const int n1 = n0 + c0 * 16, n2 = n0 + c1 * 16;
-                    const int left1 = g.n - n1, left2 = i + 1 < chunks ? g.n - n2 : 0;
-                    const int count1 = m < g.m ? min(left1, 16) : 0, count2 = m < g.m ? min(left2, 16) : 0;
-                    __syncwarp();  // (the columns before have been read)
-                    const int left = lane < 16 ? left1 : left2, at = lane & 15;
-                    scales[lane] = at < left ? g.xscale[(lane < 16 ? n1 : n2) + at] : 0.f;
-                    __syncwarp();
-                    const unsigned short *const r = kept ? kept + i * 512 + lane : nullptr;
-                    if (left1 > 0) int8_finish(e, m, n1, count1, alpha, bias, scales, r, acc[0]);
-                    if (left2 > 0) int8_finish(e, m, n2, count2, alpha, bias, scales + 16, r ? r + 512 : r, acc[1]);
                 }
+                if (CH > 4 && i == 0)
 #pragma unroll
-                for (int k = 0; k + 2 < CH; ++k)
+                    for (int k = 0; k + 4 < CH; ++k)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 2][j];
+                        for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 4][j];
             }
         }
-        if (kept) cp_async_wait<0>();
+        if (WIDE && g.staged) {  // nothing of its own under way when the CTA leaves
+            if (lead) {
+                if (loads) mbar_wait_bounded(there, (loads - 1) & 1, kPolls);
+                tma_stores_read();
+            }
+            __syncwarp();
+        }
         if constexpr (CG == 1) {
             if (g.cl > 1) {
                 // The sums of a tile's shares meet in shared memory, where each CTA has left its own: each
@@ -600,9 +677,6 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                     const int n = t.nt * g.bn + c * 16, left = g.n - n;
                     if (left <= 0) break;
                     const int count = m < g.m ? min(left, 16) : 0;
-                    __syncwarp();
-                    if (lane < 16) scales[lane] = lane < left ? g.xscale[n + lane] : 0.f;
-                    __syncwarp();
                     const unsigned mine = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
                     float v[16];
 #pragma unroll
@@ -621,7 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
 #pragma unroll
                         for (int i = 0; i < 16; ++i) v[i] += o[i];
                     }
-                    int8_finish(e, m, n, count, alpha, bias, scales, nullptr, v);
+                    int8_finish(e, m, n, count, alpha, bias, scales + c * 16, v);
                 }
                 __syncwarp();
                 cluster_sync_all();  // (no CTA leaves while another reads from it)
@@ -788,11 +862,21 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
     g.cl = plan.splits;
     g.w_late = p.w_late;
     g.stage = (unsigned)(bn / cg * 2 * kTerms);
-    g.keep = wide && p.e.add && p.e.out_type == GEMM_T_BF16 && reinterpret_cast<uintptr_t>(p.e.add) % 16 == 0 &&
-             p.e.lda % 8 == 0;
-    const size_t keep = g.keep ? 128 * 256 * 2 : 0;
-    g.S = g.keep ? kStages - 1 : kStages;
-    g.R = (int)std::min<size_t>(kRawStagesMax, (kSmem - 1024 - keep - g.S * (size_t)g.stage) / kRawBytes);
+    const auto tma_can = [](const void *q, long long row_bytes) {
+        return reinterpret_cast<uintptr_t>(q) % 16 == 0 && row_bytes % 16 == 0;
+    };
+    const int size = p.e.out_type == GEMM_T_F32 ? 4 : 2;
+    g.staged = wide && tma_can(p.e.out, p.e.ldo * size) && (!p.e.add || tma_can(p.e.add, p.e.lda * size));
+    if (g.staged) {
+        const CUtensorMapDataType type = size == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+        rc = tensor_map(type, p.e.out, p.m, p.n, p.e.ldo * size, 32, 64, false, &g.map_out);
+        if (rc == QCNN_OK && p.e.add)
+            rc = tensor_map(type, p.e.add, p.m, p.n, p.e.lda * size, 32, 64, false, &g.map_add);
+        if (rc != QCNN_OK) return rc;
+    }
+    const size_t staged = g.staged ? 8 * (size_t)kStagedBytes : 0;
+    g.S = g.staged ? kStages - 1 : kStages;
+    g.R = (int)std::min<size_t>(kRawStagesMax, (kSmem - 1024 - staged - g.S * (size_t)g.stage) / kRawBytes);
     // fp32 sums of fp16, 128 (256) rows x the columns of an accumulator
     g.idesc = (1u << 4) | (uint32_t)((wide ? 128 : bn) >> 3) << 17 | (uint32_t)(128 * cg >> 4) << 24;
     g.sums = wide && p.segs > 1 ? p.sums : nullptr;
@@ -803,7 +887,7 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
     g.e.beta = 1.f;
     g.e.pair = in_pairs(p.e.out, p.e.out_type, p.e.ldo, p.m) ? 1 : 0;
     const size_t stash = g.cl > 1 ? (size_t)bn * 512 : 0;
-    const size_t smem = std::max({kSmemFloor, g.S * (size_t)g.stage + g.R * (size_t)kRawBytes + keep + 1024, stash + 1024});
+    const size_t smem = std::max({kSmemFloor, g.S * (size_t)g.stage + g.R * (size_t)kRawBytes + staged + 1024, stash + 1024});
     const int ctas = g.cl > 1 ? g.units * g.cl : std::min(g.units, num_sms() / cg) * cg;
     return wide ? launch_of<2, true>(g, ctas, smem, st) : launch_of<1, false>(g, ctas, smem, st);
 }
