@@ -786,8 +786,9 @@ qcnn_status qcnn_dropout_backward(const void *dy, long long lddy, int N, int C, 
  *   [N][Cs] codes with xscale [N].  bias [Ct] fp32 or NULL; residual [N][Ct] of dtype or NULL (may be
  *   y itself); y [N][Ct] of dtype.  Any code from -128 to 127 will do; Cs <= 131071.
  *   Sums of up to 1024 terms are exact, those of several such blocks are added in fp32 (exact while
- *   they stay below 2^24; of up to 8 rows all sums are exact); then two products, bias, activation and
- *   residual in fp32, and one rounding to dtype.
+ *   they stay below 2^24; of few rows, N <= 8 and N Cs <= 40960, they are exact integers rounded
+ *   once); then two products, bias, activation (exponentials and reciprocals of GELU and SiLU to a few
+ *   units of their last bit, GELU's erf to 1.5e-7) and residual in fp32, and one rounding to dtype.
  *   Workspace: from the query (x_codes: xscale is given); `aligned`: W, and x if it is codes, have
  *   16-byte aligned bases and row distances that are multiples of 16.
  */

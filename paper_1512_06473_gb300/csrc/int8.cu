@@ -246,70 +246,239 @@ qcnn_status launch_quantize(const void *x, long long ldx, int rows, int cols, vo
     return half ? launch_quantize_of<float, true>(a, st) : launch_quantize_of<float, false>(a, st);
 }
 
-// ------------------------------------------------------------------ product
+// ------------------------------------------------------------------ few rows
+// No tensor cores: W is streamed once through sums of four products (dp4a, exact).
 struct Int8Product {
-    const int8_t *x, *W;
+    const void *x;        // codes, or (fused kernel) fp32 or bf16
+    const int8_t *W;
     long long ldx, ldw;
-    const float *xscale, *wscale;
+    const float *xscale, *wscale;  // (xscale: of codes)
     int N, Cs, Ct;
     GemmEpi e;  // bias, act, add (beta 1), out; n = row, m = output
+    int kw;     // warps that share an output's terms
 };
 
-// A warp sums four outputs x NB rows, four products at a time (dp4a).
-template <int NB, bool VEC>
-__global__ void __launch_bounds__(256) few_rows_kernel(Int8Product f) {
-    constexpr int OUT = 4;
+constexpr int kOut = 4;  // outputs of a warp
+__device__ __forceinline__ void finish_one(const GemmEpi &e, int r, int m, float v) {
+    if (e.bias) v += e.bias[m];
+    v = act_apply(v, e.act);
+    if (e.add) v += load_as(e.add, e.add_type, (long long)r * e.lda + m);
+    if (e.out_type == GEMM_T_F32) static_cast<float *>(e.out)[(long long)r * e.ldo + m] = v;
+    else static_cast<unsigned short *>(e.out)[(long long)r * e.ldo + m] = float_to_bf16(v);
+}
+__device__ __forceinline__ int dot16(const uint4 &a, const uint4 &b, int c) {
+    c = __dp4a((int)a.x, (int)b.x, c);
+    c = __dp4a((int)a.y, (int)b.y, c);
+    c = __dp4a((int)a.z, (int)b.z, c);
+    return __dp4a((int)a.w, (int)b.w, c);
+}
+
+// One launch, no workspace: each CTA makes the codes of x for itself, in shared memory, while its first
+// weights are on their way.  A warp sums kOut outputs x NB rows, or kw warps do, each a part of the terms.
+// VEC: W's rows on 16 bytes.  T: float, bf16, or int8_t (codes).
+// CTAs per SM and their threads: with more rows one, whose threads share the work on x.  (8 x 9216 -> 4096 in
+// fp32 18.4 us, 22.9 with two of 256 threads; one row of 4096 -> 1000 4.0, 4.6 with one of 512.)
+constexpr int few_ctas(int NB) { return NB <= 2 ? 2 : 1; }
+constexpr int few_threads(int NB) { return 512 / few_ctas(NB); }
+template <typename T, int NB, bool VEC>
+__global__ void __launch_bounds__(few_threads(NB), few_ctas(NB)) few_rows_kernel(Int8Product f) {
+    constexpr int kWarps = few_threads(NB) / 32;
+    extern __shared__ __align__(16) int8_t codes[];  // [NB][pitch]
+    __shared__ unsigned top[NB];
+    __shared__ float scale[NB];
+    __shared__ int red[kWarps][kOut * NB];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c0 = (blockIdx.x * 8 + warp) * OUT;
+    const int pitch = (f.Cs + 15) / 16 * 16, kw = f.kw;
+    const int part = warp & (kw - 1), per = kWarps / kw, groups = (f.Ct + kOut - 1) / kOut;
+    const int whole = VEC ? f.Cs / 16 : 0;  // vectors of 16 codes
+    int group = blockIdx.x * per + warp / kw;
     grid_dep_sync();
-    if (c0 >= f.Ct) return;
-    const int8_t *w[OUT], *x[NB];
+    const int8_t *w[kOut];
+    auto rows_of = [&] {
 #pragma unroll
-    for (int i = 0; i < OUT; ++i) w[i] = f.W + (long long)min(c0 + i, f.Ct - 1) * f.ldw;
+        for (int i = 0; i < kOut; ++i) w[i] = f.W + (long long)min(group * kOut + i, f.Ct - 1) * f.ldw;
+    };
+    constexpr int D = NB == 1 ? 4 : 1;  // steps of W that are loaded before x's codes are made
+    uint4 first[D][kOut];
+    const int v0 = part * 32 + lane;
+    auto load_first = [&] {
+        rows_of();
 #pragma unroll
-    for (int n = 0; n < NB; ++n) x[n] = f.x + (long long)min(n, f.N - 1) * f.ldx;
-    int acc[OUT][NB] = {};
-    const int whole = VEC ? f.Cs / 16 * 16 : 0;
-    for (int k = lane * 16; k < whole; k += 512) {
-        uint4 v[OUT];
+        for (int d = 0; d < D; ++d)
+            if (VEC && v0 + d * kw * 32 < whole)
 #pragma unroll
-        for (int i = 0; i < OUT; ++i) v[i] = *reinterpret_cast<const uint4 *>(w[i] + k);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(x[n] + k);
-#pragma unroll
-            for (int i = 0; i < OUT; ++i) {
-                acc[i][n] = __dp4a((int)v[i].x, (int)u.x, acc[i][n]);
-                acc[i][n] = __dp4a((int)v[i].y, (int)u.y, acc[i][n]);
-                acc[i][n] = __dp4a((int)v[i].z, (int)u.z, acc[i][n]);
-                acc[i][n] = __dp4a((int)v[i].w, (int)u.w, acc[i][n]);
+                for (int i = 0; i < kOut; ++i) first[d][i] = reinterpret_cast<const uint4 *>(w[i])[v0 + d * kw * 32];
+    };
+    load_first();
+
+    // ---- the codes of x: 16 / NB warps a row
+    {
+        constexpr int WR = kWarps / NB;
+        const int n = warp / WR, at = (warp % WR) * 32 + lane;
+        int8_t *const out = codes + n * pitch;
+        if (n < f.N) {
+            const T *const x = static_cast<const T *>(f.x) + (long long)n * f.ldx;
+            if constexpr (sizeof(T) == 1) {
+                if (at == 0) scale[n] = f.xscale[n];
+                if (reinterpret_cast<uintptr_t>(x) % 16 == 0) {
+                    for (int v = at; v < f.Cs / 16; v += WR * 32)
+                        reinterpret_cast<uint4 *>(out)[v] = reinterpret_cast<const uint4 *>(x)[v];
+                    for (int c = f.Cs / 16 * 16 + at; c < f.Cs; c += WR * 32) out[c] = x[c];
+                } else {
+                    for (int c = at; c < f.Cs; c += WR * 32) out[c] = x[c];
+                }
             }
         }
-    }
-    for (int k = whole + lane; k < f.Cs; k += 32) {
-        int v[OUT];
+        if constexpr (sizeof(T) > 1) {
+            if (threadIdx.x < NB) top[threadIdx.x] = 0;
+            __syncthreads();
+            constexpr int V = 16 / (int)sizeof(T), H = 4;  // vectors of x kept by a lane
+            const T *const x = static_cast<const T *>(f.x) + (long long)(n < f.N ? n : 0) * f.ldx;
+            const int cols = n < f.N ? f.Cs : 0;
+            const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0;
+            const int vectors = wide ? cols / V : 0;
+            auto value = [](const uint4 &q, int i) {
+                const unsigned u[4] = {q.x, q.y, q.z, q.w};
+                if constexpr (V == 4) return __uint_as_float(u[i]);
+                else return __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+            };
+            auto single = [&](int c) {
+                if constexpr (V == 4) return x[c];
+                else return bf16_to_float(x[c]);
+            };
+            uint4 kept[H];
+            float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < OUT; ++i) v[i] = w[i][k];
+            for (int h = 0; h < H; ++h)
+                if (at + h * WR * 32 < vectors) kept[h] = reinterpret_cast<const uint4 *>(x)[at + h * WR * 32];
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+            for (int h = 0; h < H; ++h)
+                if (at + h * WR * 32 < vectors)
 #pragma unroll
-            for (int i = 0; i < OUT; ++i) acc[i][n] += v[i] * x[n][k];
-    }
+                    for (int i = 0; i < V; ++i) most = max_nan(most, fabsf(value(kept[h], i)));
+            for (int v = at + H * WR * 32; v < vectors; v += WR * 32) {
+                const uint4 q = reinterpret_cast<const uint4 *>(x)[v];
 #pragma unroll
-    for (int i = 0; i < OUT; ++i)
+                for (int i = 0; i < V; ++i) most = max_nan(most, fabsf(value(q, i)));
+            }
+            for (int c = vectors * V + at; c < cols; c += WR * 32) most = max_nan(most, fabsf(single(c)));
+            const unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint(most) & 0x7fffffffu);
+            if (lane == 0) atomicMax(&top[n], bits);
+            __syncthreads();
+            const RowScale s = row_scale(__uint_as_float(top[n]));
+            const bool none = s.inverse == 0.f;
+            if (n < f.N && at == 0) scale[n] = s.scale;
+            auto put = [&](int v, uint4 q) {
+                if (none) q = make_uint4(0, 0, 0, 0);
+                unsigned c[V / 4];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            const int sum = __reduce_add_sync(0xffffffffu, acc[i][n]);
-            const int m = c0 + i, r = n;
-            if (lane != (i * NB + n) % 32 || m >= f.Ct || r >= f.N) continue;
-            const GemmEpi &e = f.e;
-            float v = (float)sum * f.xscale[r] * f.wscale[m];
-            if (e.bias) v += e.bias[m];
-            v = act_apply(v, e.act);
-            if (e.add) v += load_as(e.add, e.add_type, (long long)r * e.lda + m);
-            if (e.out_type == GEMM_T_F32) static_cast<float *>(e.out)[(long long)r * e.ldo + m] = v;
-            else static_cast<unsigned short *>(e.out)[(long long)r * e.ldo + m] = float_to_bf16(v);
+                for (int i = 0; i < V / 4; ++i)
+                    c[i] = pack_codes(rounded(value(q, 4 * i), value(q, 4 * i + 1), s.inverse),
+                                      rounded(value(q, 4 * i + 2), value(q, 4 * i + 3), s.inverse));
+                if constexpr (V == 4) reinterpret_cast<unsigned *>(out)[v] = c[0];
+                else reinterpret_cast<uint2 *>(out)[v] = make_uint2(c[0], c[1]);
+            };
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+                if (at + h * WR * 32 < vectors) put(at + h * WR * 32, kept[h]);
+            for (int v = at + H * WR * 32; v < vectors; v += WR * 32) put(v, reinterpret_cast<const uint4 *>(x)[v]);
+            for (int c = vectors * V + at; c < cols; c += WR * 32)
+                out[c] = (int8_t)__float_as_uint(rounded(none ? 0.f : single(c), 0.f, s.inverse).x);
         }
+    }
+    __syncthreads();
+
+    // ---- the sums (all warps go through as many rounds: partial sums meet in shared memory)
+    const int rounds = (groups + (int)gridDim.x * per - 1) / ((int)gridDim.x * per);
+    for (int round = 0; round < rounds; ++round) {
+        int acc[kOut][NB] = {};
+        if (group < groups) {
+#pragma unroll
+            for (int d = 0; d < D; ++d)
+                if (VEC && v0 + d * kw * 32 < whole) {
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        const uint4 u = reinterpret_cast<const uint4 *>(codes + n * pitch)[v0 + d * kw * 32];
+#pragma unroll
+                        for (int i = 0; i < kOut; ++i) acc[i][n] = dot16(first[d][i], u, acc[i][n]);
+                    }
+                }
+#pragma unroll(NB == 1 ? 4 : NB <= 4 ? 2 : 1)
+            for (int v = v0 + D * kw * 32; v < whole; v += kw * 32) {
+                uint4 q[kOut];
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) q[i] = reinterpret_cast<const uint4 *>(w[i])[v];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    const uint4 u = reinterpret_cast<const uint4 *>(codes + n * pitch)[v];
+#pragma unroll
+                    for (int i = 0; i < kOut; ++i) acc[i][n] = dot16(q[i], u, acc[i][n]);
+                }
+            }
+            for (int k = whole * 16 + v0; k < f.Cs; k += kw * 32) {
+                int q[kOut];
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) q[i] = w[i][k];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    const int u = codes[n * pitch + k];
+#pragma unroll
+                    for (int i = 0; i < kOut; ++i) acc[i][n] += q[i] * u;
+                }
+            }
+        }
+        const int mine = group;
+        group += gridDim.x * per;
+        if (group < groups) load_first();
+#pragma unroll
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const int sum = __reduce_add_sync(0xffffffffu, acc[i][n]);
+                if (lane == i * NB + n) red[warp][lane] = sum;
+            }
+        if (kw > 1) __syncthreads();
+        else __syncwarp();
+        const int i = lane / NB, n = lane % NB, m = mine * kOut + i;
+        if (part == 0 && lane < kOut * NB && mine < groups && m < f.Ct && n < f.N) {
+            int sum = 0;
+            for (int p = 0; p < kw; ++p) sum += red[warp + p][lane];
+            finish_one(f.e, n, m, (float)sum * scale[n] * f.wscale[m]);
+        }
+        if (kw > 1 && round + 1 < rounds) __syncthreads();
+    }
+}
+
+int few_block(int N) { return N <= 2 ? N : N <= 4 ? 4 : 8; }  // rows of a kernel
+// Whether that is sooner done than a product on the tensor cores behind a launch that makes the codes:
+// every CTA making them for itself costs more with more of them.  us, few rows and tensor cores: 1 x 9216
+// -> 4096 10.5 and 11.4, 4 x 9216 -> 4096 13.2 and 16.0, 8 x 4096 -> 1000 7.2 and 9.9, -> 4096 10.4 and 11.5, ->
+// 8192 14.0 and 14.5; 8 x 9216 -> 4096 18.8 and 15.7, -> 9216 27 and 23.
+bool few_rows(int N, int Cs) { return N <= kFewRows && (long long)N * Cs <= 40960; }
+
+template <typename T, bool VEC>
+qcnn_status launch_few_of(Int8Product f, cudaStream_t st) {
+    const int NB = few_block(f.N), groups = cdiv(f.Ct, kOut), most = few_ctas(NB) * num_sms();
+    const int threads = few_threads(NB), warps = threads / 32;
+    // as many warps to an output as have terms, while the outputs alone do not take all warps
+    f.kw = 1;
+    while (f.kw < warps && groups * 2ll * f.kw <= most * warps && f.Cs > f.kw * 512) f.kw *= 2;
+    const dim3 grid(std::min(most, cdiv(groups, warps / f.kw)));
+    const size_t smem = (size_t)NB * ((f.Cs + 15) / 16 * 16);
+    const auto launch = [&](auto k) {
+        const qcnn_status rc = allow_smem(reinterpret_cast<const void *>(k));
+        return rc != QCNN_OK ? rc : launch_pdl(k, grid, dim3(threads), smem, st, f);
+    };
+    if (NB == 1) return launch(few_rows_kernel<T, 1, VEC>);
+    if (NB == 2) return launch(few_rows_kernel<T, 2, VEC>);
+    if (NB == 4) return launch(few_rows_kernel<T, 4, VEC>);
+    return launch(few_rows_kernel<T, 8, VEC>);
+}
+qcnn_status launch_few(const Int8Product &f, bool codes, int dtype, bool vec, cudaStream_t st) {
+    if (codes) return vec ? launch_few_of<int8_t, true>(f, st) : launch_few_of<int8_t, false>(f, st);
+    if (dtype == QCNN_BF16)
+        return vec ? launch_few_of<unsigned short, true>(f, st) : launch_few_of<unsigned short, false>(f, st);
+    return vec ? launch_few_of<float, true>(f, st) : launch_few_of<float, false>(f, st);
 }
 
 // ------------------------------------------------------------------ copies
@@ -380,7 +549,7 @@ long long pad16(long long v) { return (v + 15) / 16 * 16; }
 bool rows16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 16 == 0; }
 bool codes_ok(const void *p, long long ld, long long rows, long long cols) { return ld >= cols && (rows == 0 || p); }
 
-// Up to 8 rows: dp4a, x as codes.  More: the tensor cores, x in fp16, W's rows on 16 bytes.
+// (few rows: none) x in fp16, its scales and sums, W's rows on 16 bytes.
 struct Space {
     void *x = nullptr;
     float *scale = nullptr;
@@ -391,11 +560,11 @@ struct Space {
 Space carve(int N, int Cs, int Ct, bool x_codes, bool w_copy, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     Space s;
-    const bool few = N <= kFewRows;
-    if (!x_codes || !few) s.x = c.take(few ? (size_t)N * pad16(Cs) : (size_t)N * pad8(Cs) * 2);
+    if (few_rows(N, Cs)) return s;
+    s.x = c.take((size_t)N * pad8(Cs) * 2);
     if (!x_codes) s.scale = c.array<float>(N);
-    if (!few && int8_sums(plan_int8(Ct, N, Cs), Cs)) s.sums = c.array<int>((size_t)N * cdiv(Cs, kInt8Segment));
-    if (w_copy && !few) s.w = c.array<int8_t>((size_t)Ct * pad16(Cs));
+    if (int8_sums(plan_int8(Ct, N, Cs), Cs)) s.sums = c.array<int>((size_t)N * cdiv(Cs, kInt8Segment));
+    if (w_copy) s.w = c.array<int8_t>((size_t)Ct * pad16(Cs));
     s.bytes = c.used;
     return s;
 }
@@ -441,15 +610,6 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
     if (rc != QCNN_OK) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     PdlScope pdl;
-    const bool few = N <= kFewRows;
-    const int8_t *codes = static_cast<const int8_t *>(x);
-    if (!xscale) {
-        rc = launch_quantize(x, ldx, N, Cs, s.x, few ? pad16(Cs) : pad8(Cs), !few, s.scale, s.sums, dtype, st);
-        if (rc != QCNN_OK) return rc;
-        xscale = s.scale;
-        codes = static_cast<const int8_t *>(s.x);
-        ldx = pad16(Cs);
-    }
     GemmEpi e;
     const int type = dtype == QCNN_BF16 ? GEMM_T_BF16 : GEMM_T_F32;
     e.bias = bias;
@@ -460,53 +620,48 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
     e.out = y;
     e.ldo = ldy;
     e.out_type = type;
-    if (!few) {
-        const auto job = [&](const void *src, long long ld, long long rows, void *dst, long long pitch) {
-            CopyJob j;
-            j.src = static_cast<const int8_t *>(src);
-            j.ld = ld;
-            j.rows = rows;
-            j.cols = Cs;
-            j.per_row = cdiv(Cs, kCopyCols);
-            j.vec = rows16(src, ld);
-            j.dst = dst;
-            j.pitch = pitch;
-            j.blocks = (int)std::min<long long>((rows * j.per_row + 7) / 8, (long long)num_sms() * 8);
-            return j;
-        };
-        CopyJob jx, jw;
-        if (xscale != s.scale) {
-            jx = job(x, ldx, N, s.x, pad8(Cs));
-            jx.sums = s.sums;
-        }
-        if (w_copy) jw = job(W, ldw, Ct, s.w, pad16(Cs));
-        if (jx.blocks + jw.blocks &&
-            (rc = launch_pdl(copy_kernel, dim3(jx.blocks + jw.blocks), dim3(256), 0, st, jx, jw)) != QCNN_OK)
-            return rc;
-        Int8Problem p;
-        p.x = s.x;
-        p.ldx = pad8(Cs);
-        p.W = w_copy ? s.w : W;
-        p.ldw = w_copy ? pad16(Cs) : ldw;
-        p.w_late = w_copy;
-        p.xscale = xscale;
-        p.wscale = wscale;
-        p.sums = s.sums;
-        p.segs = cdiv(Cs, kInt8Segment);
-        p.m = Ct;
-        p.n = N;
-        p.k = Cs;
-        p.e = e;
-        return launch_int8(plan_int8(Ct, N, Cs), p, st);
+    if (few_rows(N, Cs))
+        return launch_few(Int8Product{x, W, ldx, ldw, xscale, wscale, N, Cs, Ct, e, 1}, xscale != nullptr, dtype, !w_copy, st);
+    CopyJob jx, jw;
+    const auto job = [&](const void *src, long long ld, long long rows, void *dst, long long pitch) {
+        CopyJob j;
+        j.src = static_cast<const int8_t *>(src);
+        j.ld = ld;
+        j.rows = rows;
+        j.cols = Cs;
+        j.per_row = cdiv(Cs, kCopyCols);
+        j.vec = rows16(src, ld);
+        j.dst = dst;
+        j.pitch = pitch;
+        j.blocks = (int)std::min<long long>((rows * j.per_row + 7) / 8, (long long)num_sms() * 8);
+        return j;
+    };
+    if (!xscale) {
+        rc = launch_quantize(x, ldx, N, Cs, s.x, pad8(Cs), true, s.scale, s.sums, dtype, st);
+        if (rc != QCNN_OK) return rc;
+    } else {
+        jx = job(x, ldx, N, s.x, pad8(Cs));
+        jx.sums = s.sums;
     }
-    const Int8Product f{codes, W, ldx, ldw, xscale, wscale, N, Cs, Ct, e};
-    const bool vec = rows16(codes, ldx) && !w_copy;
-    const dim3 grid(cdiv(Ct, 32));
-    const auto launch = [&](auto k) { return launch_pdl(k, grid, dim3(256), 0, st, f); };
-    if (N == 1) return launch(vec ? few_rows_kernel<1, true> : few_rows_kernel<1, false>);
-    if (N == 2) return launch(vec ? few_rows_kernel<2, true> : few_rows_kernel<2, false>);
-    if (N <= 4) return launch(vec ? few_rows_kernel<4, true> : few_rows_kernel<4, false>);
-    return launch(vec ? few_rows_kernel<8, true> : few_rows_kernel<8, false>);
+    if (w_copy) jw = job(W, ldw, Ct, s.w, pad16(Cs));
+    if (jx.blocks + jw.blocks &&
+        (rc = launch_pdl(copy_kernel, dim3(jx.blocks + jw.blocks), dim3(256), 0, st, jx, jw)) != QCNN_OK)
+        return rc;
+    Int8Problem p;
+    p.x = s.x;
+    p.ldx = pad8(Cs);
+    p.W = w_copy ? s.w : W;
+    p.ldw = w_copy ? pad16(Cs) : ldw;
+    p.w_late = w_copy;
+    p.xscale = xscale ? xscale : s.scale;
+    p.wscale = wscale;
+    p.sums = s.sums;
+    p.segs = cdiv(Cs, kInt8Segment);
+    p.m = Ct;
+    p.n = N;
+    p.k = Cs;
+    p.e = e;
+    return launch_int8(plan_int8(Ct, N, Cs), p, st);
 }
 
 }  // extern "C"
