@@ -785,10 +785,9 @@ qcnn_status qcnn_dropout_backward(const void *dy, long long lddy, int N, int C, 
  *   xscale NULL: x [N][Cs] of dtype, whose rows the call quantizes as qcnn_int8_quantize does; else x
  *   [N][Cs] codes with xscale [N].  bias [Ct] fp32 or NULL; residual [N][Ct] of dtype or NULL (may be
  *   y itself); y [N][Ct] of dtype.  Any code from -128 to 127 will do; Cs <= 131071.
- *   Sums of up to 1024 terms are exact, those of several such blocks are added in fp32 (exact while
- *   they stay below 2^24; of few rows, N <= 8 and N Cs <= 40960, they are exact integers rounded
- *   once); then two products, bias, activation (exponentials and reciprocals of GELU and SiLU to a few
- *   units of their last bit, GELU's erf to 1.5e-7) and residual in fp32, and one rounding to dtype.
+ *   The sums are exact integers, rounded to fp32 once; then two products, bias, activation and residual
+ *   in fp32, and one rounding to dtype.  (On the tensor cores GELU's erf is good to 1.5e-7, exponentials
+ *   and reciprocals to a few units of their last bit.)
  *   Workspace: from the query (x_codes: xscale is given); `aligned`: W, and x if it is codes, have
  *   16-byte aligned bases and row distances that are multiples of 16.
  */
@@ -796,6 +795,12 @@ qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_
                                float *scale, int dtype, void *stream);
 qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned,
                                            size_t *bytes);
+/* qcnn_int8_route_info -- how qcnn_int8_dense_forward goes about these sizes.  info receives: [0] 1 where
+ * rows are summed without the tensor cores (in one launch, without a workspace), else 0 and [1] rows
+ * of x per tile, [2] CTAs per tile (a pair's two each have 128 outputs), [3] CTAs of a cluster that share
+ * a tile's terms (1: none); all 0 where [0] is 1.  Errors are those of qcnn_int8_dense_workspace_size, and
+ * QCNN_ERR_INVALID_ARG for N = 0. */
+qcnn_status qcnn_int8_route_info(int N, int Cs, int Ct, int info[4]);
 qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *xscale, int N, int Cs,
                                     const int8_t *W, long long ldw, const float *wscale, int Ct,
                                     const float *bias, int act, const void *residual, long long ldr,

@@ -31,7 +31,8 @@ __all__ = ["lut_build", "fc_forward", "conv_forward", "conv_pack_codes", "maxpoo
            "ConvLayer", "FCLayer", "PoolLayer", "Net", "launch_count", "QcnnError", "load",
            "set_debug", "debug_checks", "device_check", "smem_load_rate",
            "dense_forward", "dense_backward", "xent_forward", "xent_grad", "xent_route",
-           "orthogonalize", "dropout_forward", "dropout_backward", "int8_quantize", "int8_dense_forward"]
+           "orthogonalize", "dropout_forward", "dropout_backward", "int8_quantize", "int8_dense_forward",
+           "int8_route"]
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -763,4 +764,4 @@ def load_model(blob_or_path, device="cuda", stream=None) -> LoadedNet:
 
 from .finetune import (dense_backward, dense_forward, dropout_backward, dropout_forward,  # noqa: E402
                        orthogonalize, xent_forward, xent_grad, xent_route)
-from .int8 import int8_dense_forward, int8_quantize  # noqa: E402
+from .int8 import int8_dense_forward, int8_quantize, int8_route  # noqa: E402

@@ -138,6 +138,7 @@ _SIGS = {
     "qcnn_int8_quantize": (c_int, [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_void_p, c_int,
                                    c_void_p]),
     "qcnn_int8_dense_workspace_size": (c_int, [c_int] * 5 + [ctypes.POINTER(c_size_t)]),
+    "qcnn_int8_route_info": (c_int, [c_int] * 3 + [ctypes.POINTER(c_int)]),
     "qcnn_int8_dense_forward": (c_int, [c_void_p, c_int64, c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p,
                                         c_int, c_void_p, c_int, c_void_p, c_int64, c_void_p, c_int64, c_int,
                                         c_void_p, c_size_t, c_void_p]),

@@ -288,6 +288,15 @@ __global__ void __launch_bounds__(few_threads(NB), few_ctas(NB)) few_rows_kernel
     __shared__ float scale[NB];
     __shared__ int red[kWarps][kOut * NB];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.y) {  // (more than eight rows: eight per CTA)
+        const long long n = (long long)blockIdx.y * NB;
+        f.x = static_cast<const T *>(f.x) + n * f.ldx;
+        if (f.xscale) f.xscale += n;
+        f.N -= (int)n;
+        const int size = f.e.out_type == GEMM_T_F32 ? 4 : 2;
+        f.e.out = static_cast<char *>(f.e.out) + n * f.e.ldo * size;
+        if (f.e.add) f.e.add = static_cast<const char *>(f.e.add) + n * f.e.lda * size;
+    }
     const int pitch = (f.Cs + 15) / 16 * 16, kw = f.kw;
     const int part = warp & (kw - 1), per = kWarps / kw, groups = (f.Ct + kOut - 1) / kOut;
     const int whole = VEC ? f.Cs / 16 : 0;  // vectors of 16 codes
@@ -449,21 +458,27 @@ __global__ void __launch_bounds__(few_threads(NB), few_ctas(NB)) few_rows_kernel
     }
 }
 
-int few_block(int N) { return N <= 2 ? N : N <= 4 ? 4 : 8; }  // rows of a kernel
+int few_block(int N) { return N <= 2 ? N : N <= 4 ? 4 : 8; }  // rows of a kernel, of a CTA
 // Whether that is sooner done than a product on the tensor cores behind a launch that makes the codes:
-// every CTA making them for itself costs more with more of them.  us, few rows and tensor cores: 1 x 9216
-// -> 4096 10.5 and 11.4, 4 x 9216 -> 4096 13.2 and 16.0, 8 x 4096 -> 1000 7.2 and 9.9, -> 4096 10.4 and 11.5, ->
-// 8192 14.0 and 14.5; 8 x 9216 -> 4096 18.8 and 15.7, -> 9216 27 and 23.
-bool few_rows(int N, int Cs) { return N <= kFewRows && (long long)N * Cs <= 40960; }
+// every CTA making them for itself costs more with more of them, and sums of four products, and the
+// joining of each output's, more with more of those.  us, few rows and tensor cores: 1 x 9216 -> 4096 10.5
+// and 11.4, 4 x 9216 -> 4096 13.2 and 16.0, 8 x 4096 -> 1000 7.2 and 9.9, -> 4096 10.4 and 11.5, -> 8192 14.0 and
+// 14.5; 8 x 9216 -> 4096 18.8 and 15.7, -> 9216 27 and 23.  More rows: 64 x 1024 -> 1024 5.1 and 7.2, 30 x 2000
+// -> 2000 7.9 and 9.6, 100 x 1000 -> 1000 7.6 and 8.0; 9 x 4096 -> 4096 12.5 and 11.0, 57 x 78 -> 6139 12.8 and 6.1.
+bool few_rows(int N, int Cs, int Ct) {
+    if ((long long)std::min(N, kFewRows) * Cs > 40960) return false;
+    return N <= kFewRows || ((long long)N * Ct <= 1 << 17 && (double)N * Cs * Ct <= 1.2e8);
+}
 
 template <typename T, bool VEC>
 qcnn_status launch_few_of(Int8Product f, cudaStream_t st) {
-    const int NB = few_block(f.N), groups = cdiv(f.Ct, kOut), most = few_ctas(NB) * num_sms();
+    const int NB = few_block(f.N), groups = cdiv(f.Ct, kOut), blocks = cdiv(f.N, NB);
+    const int most = std::max(1, few_ctas(NB) * num_sms() / blocks);
     const int threads = few_threads(NB), warps = threads / 32;
     // as many warps to an output as have terms, while the outputs alone do not take all warps
     f.kw = 1;
     while (f.kw < warps && groups * 2ll * f.kw <= most * warps && f.Cs > f.kw * 512) f.kw *= 2;
-    const dim3 grid(std::min(most, cdiv(groups, warps / f.kw)));
+    const dim3 grid(std::min(most, cdiv(groups, warps / f.kw)), blocks);
     const size_t smem = (size_t)NB * ((f.Cs + 15) / 16 * 16);
     const auto launch = [&](auto k) {
         const qcnn_status rc = allow_smem(reinterpret_cast<const void *>(k));
@@ -560,7 +575,7 @@ struct Space {
 Space carve(int N, int Cs, int Ct, bool x_codes, bool w_copy, void *ws) {
     Carver c{static_cast<uint8_t *>(ws)};
     Space s;
-    if (few_rows(N, Cs)) return s;
+    if (few_rows(N, Cs, Ct)) return s;
     s.x = c.take((size_t)N * pad8(Cs) * 2);
     if (!x_codes) s.scale = c.array<float>(N);
     if (int8_sums(plan_int8(Ct, N, Cs), Cs)) s.sums = c.array<int>((size_t)N * cdiv(Cs, kInt8Segment));
@@ -588,6 +603,17 @@ qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_
 qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned, size_t *bytes) {
     if (!bytes || N < 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
     *bytes = N ? carve(N, Cs, Ct, x_codes, !aligned, nullptr).bytes : 0;
+    return QCNN_OK;
+}
+
+qcnn_status qcnn_int8_route_info(int N, int Cs, int Ct, int info[4]) {
+    if (!info || N <= 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
+    const bool few = few_rows(N, Cs, Ct);
+    const Int8Plan p = few ? Int8Plan{0, 0, 0} : plan_int8(Ct, N, Cs);
+    info[0] = few;
+    info[1] = p.bn;
+    info[2] = p.cg;
+    info[3] = p.splits;
     return QCNN_OK;
 }
 
@@ -620,7 +646,7 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
     e.out = y;
     e.ldo = ldy;
     e.out_type = type;
-    if (few_rows(N, Cs))
+    if (few_rows(N, Cs, Ct))
         return launch_few(Int8Product{x, W, ldx, ldw, xscale, wscale, N, Cs, Ct, e, 1}, xscale != nullptr, dtype, !w_copy, st);
     CopyJob jx, jw;
     const auto job = [&](const void *src, long long ld, long long rows, void *dst, long long pitch) {

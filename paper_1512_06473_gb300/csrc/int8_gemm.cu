@@ -9,8 +9,9 @@
 // beside x's tile in and out.
 //
 // Sums.  Products of codes are integers of at most 2^14, sums of up to 1024 of them at most 2^24: fp32
-// accumulators hold every one of them exactly.  After 1024 terms a sum is drained to fp32 registers and
-// added there.
+// accumulators hold every one of them exactly.  Before a sum could leave that range it is drained to
+// registers, and the sums that a result has more than one of are added there as integers: exact, and
+// rounded to fp32 once.
 //
 // Tile.  As gemm_kernel.cuh's: 128 (a pair of CTAs: 256) rows of m, TMEM lanes, x bn columns of n.  256
 // columns are two accumulators of 128 that the MMAs of a block of 64 terms fill one after the other, so
@@ -559,7 +560,14 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             if (WIDE && g.staged && e.add) load_residual(mw, nw);
             const bool planned = WIDE && g.sums;
             if (planned && !(ok = warp_wait_for(sh, &sh.plan_full[tiles & 1], tiles >> 1 & 1))) break;
-            bool first = true;
+            bool first = true, whole = false;  // whole: acc holds integers
+            auto to_whole = [&] {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c][i] = __int_as_float((int)acc[c][i]);
+                whole = true;
+            };
             for (int k0 = t.kb0; k0 < t.kb1; k0 += kSumBlocks) {
                 const int seg = (k0 - t.kb0) / kSumBlocks;
                 if (planned && k0 + kSumBlocks < t.kb1 && !(sh.ends[tiles & 1][seg / 32] >> seg % 32 & 1)) continue;
@@ -568,6 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 ++sums;
                 tc_fence_after_sync();
                 const unsigned from = tl + buf * 128;
+                if (!first && !whole) to_whole();  // (from the second on they are added as integers)
                 if (WIDE && first) {
 #pragma unroll
                     for (int c = 0; c < CH; c += 2) tmem_ld32_nowait(from + c * 16, acc[c], acc[c + 1]);
@@ -583,10 +592,8 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                             float v[16];
                             tmem_ld16(from + (WIDE ? c : 2 * c + half) * 16, v);
 #pragma unroll
-                            for (int i = 0; i < 16; i += 2) {
-                                if (first) acc[c][i] = v[i], acc[c][i + 1] = v[i + 1];
-                                else add2(acc[c][i], acc[c][i + 1], v[i], v[i + 1]);
-                            }
+                            for (int i = 0; i < 16; ++i)
+                                acc[c][i] = first ? v[i] : __int_as_float(__float_as_int(acc[c][i]) + (int)v[i]);
                         }
                     }
                 }
@@ -596,6 +603,14 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             if (!ok) break;
             if (planned && lane == 0) arrive(&sh.plan_empty[tiles & 1]);
             ++tiles;
+            if (g.cl > 1) {
+                if (!whole) to_whole();  // (the shares' sums meet as integers)
+            } else if (whole) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c][i] = (float)__float_as_int(acc[c][i]);
+            }
             // (Four chunks at a time; the sums move through their registers: all eight unrolled, the
             // epilogue's instructions would come eight times, and each move counts too.)
             if (WIDE && g.staged) {
@@ -666,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         if constexpr (CG == 1) {
             if (g.cl > 1) {
                 // The sums of a tile's shares meet in shared memory, where each CTA has left its own: each
-                // adds up a part of the columns, in the order of the shares, and does their epilogue.
+                // adds up a part of the columns and does their epilogue.
                 __syncwarp();
                 cluster_sync_all();
                 const Int8Tile t = int8_tile(g, first_unit, share);
@@ -678,23 +693,24 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                     if (left <= 0) break;
                     const int count = m < g.m ? min(left, 16) : 0;
                     const unsigned mine = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
-                    float v[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+                    int sum[16] = {};
 #pragma unroll 4
                     for (int s = 0; s < g.cl; ++s) {
                         unsigned at;
                         asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(mine), "r"(s));
-                        float o[16];
+                        int o[16];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n"
-                                         : "=f"(o[4 * i]), "=f"(o[4 * i + 1]), "=f"(o[4 * i + 2]), "=f"(o[4 * i + 3])
+                            asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];\n"
+                                         : "=r"(o[4 * i]), "=r"(o[4 * i + 1]), "=r"(o[4 * i + 2]), "=r"(o[4 * i + 3])
                                          : "r"(at + i * 512)
                                          : "memory");
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] += o[i];
+                        for (int i = 0; i < 16; ++i) sum[i] += o[i];
                     }
+                    float v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = (float)sum[i];
                     int8_finish(e, m, n, count, alpha, bias, scales + c * 16, v);
                 }
                 __syncwarp();
@@ -865,8 +881,10 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
     const auto tma_can = [](const void *q, long long row_bytes) {
         return reinterpret_cast<uintptr_t>(q) % 16 == 0 && row_bytes % 16 == 0;
     };
-    const int size = p.e.out_type == GEMM_T_F32 ? 4 : 2;
-    g.staged = wide && tma_can(p.e.out, p.e.ldo * size) && (!p.e.add || tma_can(p.e.add, p.e.lda * size));
+    const long long size = p.e.out_type == GEMM_T_F32 ? 4 : 2;
+    // (a store writes the 16 bytes that a row of the result ends in as a whole)
+    g.staged = wide && p.m * size % 16 == 0 && tma_can(p.e.out, p.e.ldo * size) &&
+               (!p.e.add || tma_can(p.e.add, p.e.lda * size));
     if (g.staged) {
         const CUtensorMapDataType type = size == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
         rc = tensor_map(type, p.e.out, p.m, p.n, p.e.ldo * size, 32, 64, false, &g.map_out);

@@ -7,11 +7,12 @@ workspaces are as in the fine-tuning calls (finetune.py).
 """
 from __future__ import annotations
 
+import ctypes
 from typing import Optional
 
 import torch
 
-from . import _lib, _scratch, _stream, _workspace, finetune
+from . import _lib, _made_on, _scratch, _stream, _workspace, finetune
 from ._lib import load
 from .finetune import _DTYPES, _F32, _act, _first, _matrix, _new, _vector
 
@@ -27,9 +28,11 @@ def int8_quantize(x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=No
     N, C = x.shape
     if out is None:
         ldo = (C + 15) & ~15
-        out = _new(x, (N, ldo), _I8, stream)
-        if ldo != C:
-            out = out[:, :C]
+        if ldo == C:
+            out = _new(x, (N, C), _I8, stream)
+        else:  # (rows on 16 bytes in one step: a slice of whole rows takes 5 us more)
+            out = _made_on(stream, x.device,
+                           lambda: torch.empty_strided((N, C), (ldo, 1), dtype=_I8, device=x.device))
     else:
         ldo = _matrix(out, "out", _I8, dev, N, C)
     scale = _new(x, (N,), _F32, stream)
@@ -38,6 +41,17 @@ def int8_quantize(x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=No
     if st:
         _lib.check(st, "qcnn_int8_quantize")
     return out, scale
+
+
+def int8_route(N: int, Cs: int, Ct: int):
+    """How int8_dense_forward goes about these sizes (qcnn_int8_route_info): a dict with "few" (rows
+    summed without the tensor cores), "rows" of x and "ctas" per tile, and "shares" of its terms
+    (all 0 where few)."""
+    info = (ctypes.c_int * 4)()
+    _lib.check(load().qcnn_int8_route_info(N, Cs, Ct, info), "qcnn_int8_route_info")
+    d = dict(zip(("few", "rows", "ctas", "shares"), list(info)))
+    d["few"] = bool(d["few"])
+    return d
 
 
 def int8_dense_forward(x: torch.Tensor, weight: torch.Tensor, wscale: torch.Tensor,

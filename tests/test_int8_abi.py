@@ -80,11 +80,12 @@ def test_dense_refuses(bad):
 
 
 def test_dense_wants_its_workspace():
-    need = _size(16, 64, 32, 0, 1)
+    large = dict(N=300, Cs=2000, Ct=1000, ldx=2000, ldw=2000, ldy=1000)
+    need = _size(300, 2000, 1000, 0, 1)
     assert need > 0
-    assert _dense(wsb=need - 1) == _lib.ERR_WORKSPACE
-    assert _dense(work=None, wsb=need) == _lib.ERR_WORKSPACE
-    assert _dense(work=P + 128, wsb=need) == _lib.ERR_WORKSPACE
+    assert _dense(**large, wsb=need - 1) == _lib.ERR_WORKSPACE
+    assert _dense(**large, work=None, wsb=need) == _lib.ERR_WORKSPACE
+    assert _dense(**large, work=P + 128, wsb=need) == _lib.ERR_WORKSPACE
 
 
 def test_nothing_to_do_is_done():
@@ -99,6 +100,8 @@ def test_workspaces():
     assert lib.qcnn_int8_dense_workspace_size(1, 1, 1, 0, 0, None) == _lib.ERR_INVALID_ARG
     for bad in ((-1, 1, 1), (1, 0, 1), (1, 1, 0), (1, 131072, 1)):
         assert lib.qcnn_int8_dense_workspace_size(*bad, 0, 0, ctypes.byref(nb)) == _lib.ERR_INVALID_ARG
+    # few rows need none
+    assert _size(8, 4096, 1000, 0, 0) == 0 and _size(64, 512, 1000, 1, 0) == 0
     for N in (1, 4, 8, 9, 16, 100, 3001):
         for Cs, Ct in ((4096, 4096), (4096, 1000), (70, 30), (2047, 3001), (131071, 5)):
             for codes in (0, 1):
