@@ -3,10 +3,11 @@ are quantized, the FC layers behind them are still dense and are fine-tuned on t
 quantized layers' outputs, then quantized too.
 
 A small network on synthetic images, labelled by a fixed random teacher.  Each step runs
-the quantized conv stack, two dense layers, softmax cross entropy with its gradient, the
-backward pass, and updates the weights along their orthogonalised momentum.
+the quantized conv stack, two dense layers with dropout between them, softmax cross entropy
+with its gradient, the backward pass, and updates the weights along their orthogonalised
+momentum.  The trained layers are then quantized in both ways: with codebooks, and to 8-bit integers.
 
-    python examples/finetune_fc.py [--steps 60] [--dtype fp32|bf16]
+    python examples/finetune_fc.py [--steps 60] [--dtype fp32|bf16] [--dropout 0.0]
 """
 import argparse
 import os
@@ -45,7 +46,7 @@ class Update:
         self.weight.add_(o, alpha=-self.lr * max(1.0, m / n) ** 0.5)
 
 
-def main(steps=60, dtype="fp32", seed=0, show=True):
+def main(steps=60, dtype="fp32", seed=0, show=True, dropout=0.0):
     dt = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
     g = torch.Generator(device="cuda").manual_seed(seed)
     net = conv_stack(g)
@@ -63,7 +64,11 @@ def main(steps=60, dtype="fp32", seed=0, show=True):
     for step in range(steps):
         x = net.forward(images).flatten(1).to(dt)
         h, z = q.dense_forward(x, w1, b1, act="relu", pre=True)
+        if dropout:  # (what is dropped follows from seed and step: nothing is kept for the way back)
+            h = q.dropout_forward(h, dropout, seed, step, out=h)
         loss, _, dh, dw2, db2 = q.xent_grad(h, w2, labels, b2)
+        if dropout:
+            dh = q.dropout_backward(dh, dropout, seed, step, out=dh)
         _, dw1, db1 = q.dense_backward(dh, x, w1, z, "relu", need_dx=False)
         u1.step(dw1)
         u2.step(dw2)
@@ -86,11 +91,14 @@ def main(steps=60, dtype="fp32", seed=0, show=True):
     keep = labels >= 0
     dense_h = q.dense_forward(features.to(dt), w1, b1, act="relu")
     dense_logits = q.dense_forward(dense_h, w2, b2).float()
-    right = [float((v.argmax(1)[keep] == labels[keep]).float().mean()) for v in (dense_logits, logits)]
+    (c1, s1), (c2, s2) = q.int8_quantize(w1), q.int8_quantize(w2)
+    int8_h = q.int8_dense_forward(features.to(dt), c1, s1, b1, act="relu")
+    int8_logits = q.int8_dense_forward(int8_h, c2, s2, b2).float()
+    right = [float((v.argmax(1)[keep] == labels[keep]).float().mean()) for v in (dense_logits, logits, int8_logits)]
     losses = [float(v) for v in history]
     if show:
         print(f"loss {losses[0]:.4f} -> {losses[-1]:.4f}; right on the training images: dense "
-              f"{right[0]:.1%}, quantized {right[1]:.1%}")
+              f"{right[0]:.1%}, quantized {right[1]:.1%}, in 8 bits {right[2]:.1%}")
     return losses, right
 
 
@@ -98,5 +106,6 @@ if __name__ == "__main__":
     p = argparse.ArgumentParser()
     p.add_argument("--steps", type=int, default=60)
     p.add_argument("--dtype", choices=["fp32", "bf16"], default="fp32")
+    p.add_argument("--dropout", type=float, default=0.0)
     a = p.parse_args()
-    main(a.steps, a.dtype)
+    main(a.steps, a.dtype, dropout=a.dropout)

@@ -139,7 +139,7 @@ __device__ __forceinline__ void arrive_first(uint64_t *bar) {
         "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}\n" ::"r"(smem_addr(bar))
         : "memory");
 }
-// 64 columns of this warp's lanes; tmem_ld_wait before they are used.
+// 32 columns of this warp's lanes, there after tcgen05.wait::ld.
 __device__ __forceinline__ void tmem_ld32_nowait(unsigned taddr, float (&a)[16], float (&b)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
