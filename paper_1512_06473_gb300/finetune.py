@@ -16,7 +16,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from . import _device, _empty, _lib, _scratch, _stream, _workspace
+from . import _device, _empty, _lib, _raw_stream, _scratch, _stream, _workspace
 from ._lib import load
 
 _DTYPES = {torch.float32: _lib.F32, torch.bfloat16: _lib.BF16}
@@ -66,10 +66,16 @@ def _matrix(t, name, dtype, dev, rows=None, cols=None):
 
 
 def _vector(t, name, dtype, dev, n):
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or t.get_device() != dev or \
-            t.shape != (n,) or (n > 1 and t.stride(0) != 1):
-        _refuse(t, name, dtype, dev, (n,))
-    return t.data_ptr()
+    # (attributes by themselves: a comparison of shapes makes a tuple, 0.2 us)
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.get_device() == dev and t.dim() == 1 and \
+            t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(t, name, dtype, dev, (n,))
+
+
+def _here(stream, dev):
+    """_stream's handle, dev being the current device."""
+    return _raw_stream(dev) if stream is None else _stream(stream)
 
 
 def _aligned(code, x, ldx, w, ldw):
@@ -272,18 +278,19 @@ def _dropout(name, x, x_name, p, seed, offset, residual, out, stream):
     elif not 0 <= offset < 1 << 64:
         raise ValueError(f"offset must be a number of 64 bits, got {offset}")
     ldr = 0 if residual is None else _matrix(residual, "residual", dt, dev, N, C)
-    if out is None:
-        out, ldo = _new(x, (N, C), dt, stream), C
-    else:
+    if out is not None:
         ldo = _matrix(out, "out", dt, dev, N, C)
+    else:
+        ldo = C
+        out = torch.empty_like(x) if stream is None and ldx == C and x.is_contiguous() else _new(x, (N, C), dt, stream)
     lib = load()
     if name == "qcnn_dropout_forward":
         st = lib.qcnn_dropout_forward(x.data_ptr(), ldx, N, C, p, seed, offset, add,
                                       None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldo,
-                                      code, _stream(stream))
+                                      code, _here(stream, dev))
     else:
         st = lib.qcnn_dropout_backward(x.data_ptr(), ldx, N, C, p, seed, offset, add, out.data_ptr(), ldo, code,
-                                       _stream(stream))
+                                       _here(stream, dev))
     if st:
         _lib.check(st, name)
     return out

@@ -12,9 +12,9 @@ from typing import Optional
 
 import torch
 
-from . import _lib, _made_on, _scratch, _stream, _workspace, finetune
+from . import _lib, _made_on, _scratch, _workspace, finetune
 from ._lib import load
-from .finetune import _DTYPES, _F32, _act, _first, _matrix, _new, _vector
+from .finetune import _DTYPES, _F32, _act, _first, _here, _matrix, _new, _vector
 
 _I8 = torch.int8
 
@@ -37,7 +37,7 @@ def int8_quantize(x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=No
         ldo = _matrix(out, "out", _I8, dev, N, C)
     scale = _new(x, (N,), _F32, stream)
     st = load().qcnn_int8_quantize(x.data_ptr(), ldx, N, C, out.data_ptr(), ldo, scale.data_ptr(), code,
-                                   _stream(stream))
+                                   _here(stream, dev))
     if st:
         _lib.check(st, "qcnn_int8_quantize")
     return out, scale
@@ -99,7 +99,7 @@ def int8_dense_forward(x: torch.Tensor, weight: torch.Tensor, wscale: torch.Tens
         out = _new(x, (N, Ct), dt, stream)
     st = lib.qcnn_int8_dense_forward(x.data_ptr(), ldx, xs, N, Cs, weight.data_ptr(), ldw, wsc, Ct, b, a,
                                      None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy,
-                                     code, ws.data_ptr() if nb else None, wsb, _stream(stream))
+                                     code, ws.data_ptr() if nb else None, wsb, _here(stream, dev))
     if st:
         _lib.check(st, "qcnn_int8_dense_forward")
     return out
