@@ -13,10 +13,11 @@
 // registers, and the sums that a result has more than one of are added there as integers: exact, and
 // rounded to fp32 once.
 //
-// Tile.  As gemm_kernel.cuh's: 128 (a pair of CTAs: 256) rows of m, TMEM lanes, x bn columns of n.  256
-// columns are two accumulators of 128 that the MMAs of a block of 64 terms fill one after the other, so
-// that draining the first overlaps the MMAs of the second; fewer columns take two accumulators in turn.
-// TMEM: 256 columns of accumulators, eight stages of W, 64 terms in 32 columns each.
+// Tile.  As gemm_kernel.cuh's: 128 (a pair of CTAs: 256) rows of m, TMEM lanes, x bn columns of n.  160 to
+// 256 columns (of a pair, in steps of 32, so that the last round of tiles is a full one: 1000 x 2000 ->
+// 3000 in tiles of 192 20.0 us, of 256 22.5; 1500 x 9216 -> 4096 94 and 108) are two accumulators, of 64 to 128 columns, that the MMAs of a block
+// of 128 terms fill one after the other, so that draining the first overlaps the MMAs of the second; up to
+// 128 columns take two accumulators in turn.  TMEM: 256 columns of accumulators, four stages of W, 128 terms in 64 columns each.
 //
 // Roles (16 warps): 0 TMA of x, 1 MMA, 2 TMEM and TMA of W, 4-11 drain and epilogue (two warps per TMEM
 // lane quarter), 12-15 widen: a warp has its 32 rows of W, a lane a row, 128 terms at a time.
@@ -40,7 +41,7 @@ constexpr int kWCols = 64;             // TMEM columns of one
 constexpr unsigned kRawBytes = 128 * kTerms;  // a copy of W: 128 rows
 constexpr int kRawStagesMax = 8;
 constexpr int kSumBlocks = kInt8Segment / kTerms;  // blocks whose sum is exact, whatever the codes
-constexpr int kSegWords = (kInt8MaxTerms / kInt8Segment + 32) / 32;
+constexpr int kSegs = kInt8MaxTerms / kInt8Segment + 1;  // segments at most
 constexpr size_t kSmem = 222 * 1024;   // dynamic, with 1 KB to align the stages
 constexpr size_t kSmemFloor = 120 * 1024;  // one CTA per SM: all tensor memory is taken
 
@@ -48,10 +49,12 @@ struct Int8Args {
     CUtensorMap map_w, map_x;
     int m, n, kblocks, m_tiles, n_tiles, kb_per_split, group, units;
     int bn, S, R, cl, w_late;
+    int wide[2];     // WIDE: columns of a tile's two accumulators
+    uint32_t idesc[2];
+    CUtensorMap map_x2;  // WIDE: x for the second
     int staged;      // WIDE: results (and the residual) pass through shared memory behind the stages
     CUtensorMap map_out, map_add;
     unsigned stage;  // bytes of a stage of x
-    unsigned idesc;
     const float *xscale, *wscale;
     const int *sums;  // WIDE: of the magnitudes of x's codes, [n][segs], each of 1024 terms; null: segs 1
     int segs;
@@ -61,7 +64,9 @@ struct Int8Shared {
     uint64_t full[kStages], empty[kStages], raw_full[kRawStagesMax], raw_empty[kRawStagesMax], tfull[2], tempty[2], done;
     uint64_t plan_full[2], plan_empty[2];
     uint64_t residual[8];
-    unsigned ends[2][kSegWords];  // of two tiles: bit s: a sum ends with segment s
+    // Of two tiles: whether a sum ends with segment s.  (A byte each: as bits of words, ends[s / 32] >> s % 32,
+    // the compiled address of the word was off its four bytes from s = 8 on, and the kernel faulted.)
+    uint8_t ends[2][kSegs];
     unsigned tmem;
     int give_up;
 };
@@ -219,8 +224,8 @@ __device__ __forceinline__ void scaled16(float (&v)[16], const float *xs, float 
     }
 }
 
-// WIDE, where TMA can write the result (and read the residual): a warp's 32 rows x 64 columns pass
-// through its part of shared memory, [column][row], the residual there before and the result after, each
+// WIDE, where TMA can write the result (and read the residual): a warp's 32 rows of m pass through its
+// part of shared memory, [column][row], by chunks of 16 columns, the residual there before and the result after, each
 // element a lane's own.  Few instructions for an element are what counts: a tile's epilogue is run
 // through once, from an instruction cache that does not hold it (stores from registers, with their
 // addresses and edges, were 235 instructions per 16 columns, and as long as the products of 1024 terms).
@@ -251,7 +256,6 @@ __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, 
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n" ::"l"(map),
                  "r"(x), "r"(y), "r"(src)
                  : "memory");
-    asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
 }
 // Until this thread's stores have read their shared memory.
 __device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
@@ -305,7 +309,7 @@ __device__ __forceinline__ void int8_finish(const GemmEpi &e, int m, int n, int 
 }
 
 // ------------------------------------------------------------------- kernel
-// WIDE: tiles of 256 columns.
+// WIDE: tiles of 160 to 256 columns, by pairs of CTAs.
 template <int CG, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant__ Int8Args g) {
     extern __shared__ __align__(128) unsigned char smem_raw[];
@@ -323,8 +327,9 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
     }
     const int first_unit = (int)blockIdx.x / (CG * g.cl), step = (int)gridDim.x / (CG * g.cl);
     constexpr int NH = WIDE ? 2 : 1;                 // accumulators of a tile
-    const int cols = WIDE ? 128 : g.bn;              // columns of one
-    const int rows_x = cols / CG;                    // rows of x per accumulator, here
+    // (columns that a tile has before accumulator h, and rows of x here that the first one's MMAs read)
+    [[maybe_unused]] const int wide0 = WIDE ? g.wide[0] : g.bn;
+    const int rows_x = wide0 / CG;
     const unsigned raw0 = smem_addr(smem) + g.S * g.stage;
     if (tid == 0) {
         for (int i = 0; i < g.S; ++i) {
@@ -365,14 +370,19 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             for (int u = first_unit; u < g.units && ok; u += step) {
                 const Int8Tile t = int8_tile(g, u, share);
                 const int n0 = t.nt * g.bn + (int)rank * rows_x;
+                [[maybe_unused]] const int n1 = t.nt * g.bn + wide0 + (int)rank * (g.wide[1] / CG);
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!(ok = wait_for(sh, &sh.empty[slot], par ^ 1))) break;
                     uint64_t *const full = &sh.full[slot];
                     if (rank == 0) arrive_expect(full, g.stage * CG);
                     const unsigned d = smem_addr(smem) + slot * g.stage;
 #pragma unroll
-                    for (int i = 0; i < 2 * NH; ++i)
-                        tma_box<CG>(d + i * rows_x * 128, &g.map_x, kb * kTerms + (i & 1) * 64, n0 + (i >> 1) * 128, full);
+                    for (int i = 0; i < 2; ++i) {
+                        tma_box<CG>(d + i * rows_x * 128, &g.map_x, kb * kTerms + i * 64, n0, full);
+                        if constexpr (WIDE)
+                            tma_box<CG>(d + (2 * rows_x + i * (g.wide[1] / CG)) * 128, &g.map_x2, kb * kTerms + i * 64, n1,
+                                        full);
+                    }
                     ++issued;
                     if (++slot == g.S) {
                         slot = 0;
@@ -403,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     const int seg = (kb - t.kb0) / kSumBlocks;
                     const bool last = kb + 1 == t.kb1 || ((kb + 1 - t.kb0) % kSumBlocks == 0 &&
-                                                          (!planned || sh.ends[tiles & 1][seg / 32] >> seg % 32 & 1));
+                                                          (!planned || sh.ends[tiles & 1][seg]));
                     const unsigned buf = WIDE ? 0 : sums & 1, round = WIDE ? sums : sums >> 1;
                     if (!(ok = wait_for(sh, &sh.full[slot], par))) break;
                     tc_fence_after_sync();
@@ -416,10 +426,11 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                             tc_fence_after_sync();
                         }
                         const unsigned d = tmem + (buf + h) * 128;
+                        const uint64_t bh = b + h * (2 * rows_x * 8);
+                        const unsigned half_terms = (h ? g.wide[1] / CG : rows_x) * 8;
 #pragma unroll
                         for (int s = 0; s < 8; ++s)
-                            mma_tmem<CG>(d, a + s * 8, b + (2 * h + s / 4) * (rows_x * 8) + s % 4 * 2, g.idesc,
-                                         !first || s > 0);
+                            mma_tmem<CG>(d, a + s * 8, bh + s / 4 * half_terms + s % 4 * 2, g.idesc[h], !first || s > 0);
                         if (last && h + 1 < NH) commit<CG>(&sh.tfull[buf + h]);
                     }
                     if (!ok) break;
@@ -480,25 +491,17 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 const Int8Tile t = int8_tile(g, u, share);
                 if (!warp_wait_for(sh, &sh.plan_empty[tiles & 1], (tiles >> 1 & 1) ^ 1)) break;
                 int used = 0;
-                unsigned word = 0;
                 for (int seg = 0; seg < g.segs; ++seg) {
                     int most = 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int n = t.nt * 256 + lane + 32 * i;
-                        if (n < g.n) most = max(most, g.sums[(long long)n * g.segs + seg]);
+                        const int c = lane + 32 * i, n = t.nt * g.bn + c;
+                        if (c < g.bn && n < g.n) most = max(most, g.sums[(long long)n * g.segs + seg]);
                     }
                     most = __reduce_max_sync(0xffffffffu, most);
-                    if (used + most > (1 << 24) / 128) {  // (the one before is the last)
-                        if (seg % 32) word |= 1u << (seg - 1) % 32;
-                        else if (seg && lane == 0) sh.ends[tiles & 1][seg / 32 - 1] |= 1u << 31;
-                        used = 0;
-                    }
-                    used += most;
-                    if (seg % 32 == 31 || seg + 1 == g.segs) {
-                        if (lane == 0) sh.ends[tiles & 1][seg / 32] = word;
-                        word = 0;
-                    }
+                    const bool full = used + most > (1 << 24) / 128;  // (the one before is the last)
+                    if (seg && lane == 0) sh.ends[tiles & 1][seg - 1] = full;
+                    used = full ? most : used + most;
                 }
                 __syncwarp();
                 if (lane == 0) arrive(&sh.plan_full[tiles & 1]);
@@ -514,8 +517,9 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         const GemmEpi &e = g.e;
         constexpr int CH = WIDE ? 8 : 4;  // chunks of 16 columns of a warp at most
         // this warp's chunk i: WIDE: of its accumulator; else every other one
-        const int chunks = WIDE ? 8 : (g.bn / 16 - half + 1) / 2;
-        auto chunk_at = [&](int i) { return WIDE ? half * 8 + i : 2 * i + half; };
+        const int chunks = WIDE ? g.wide[half] / 16 : (g.bn / 16 - half + 1) / 2;
+        [[maybe_unused]] const int before = half ? wide0 : 0;  // (WIDE) columns of the tile before this warp's
+        auto chunk_at = [&](int i) { return WIDE ? before / 16 + i : 2 * i + half; };
         unsigned sums = 0, tiles = 0;
         bool ok = true;
         float acc[CH][16];
@@ -525,13 +529,14 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         [[maybe_unused]] const bool f32 = e.out_type == GEMM_T_F32, lead = elect_one();
         [[maybe_unused]] uint64_t *const there = &sh.residual[warp - 4];
         [[maybe_unused]] unsigned loads = 0;  // of the residual, so far
-        // 64 columns of the residual (bf16: and the next 64), when what was stored from there has been read
-        [[maybe_unused]] auto load_residual = [&](int x, int y) {
+        // the residual of chunks c0 to c1 - 1, when what was stored from there has been read
+        [[maybe_unused]] auto load_residual = [&](int x, int y, int c0, int c1) {
             if (lead) {
+                const unsigned bytes = f32 ? 2048 : 1024;
                 tma_stores_read();
-                arrive_expect(there, 8192);
-                tma_load_2d(smem_addr(mine), &g.map_add, x, y, there);
-                if (!f32) tma_load_2d(smem_addr(mine) + 4096, &g.map_add, x, y + 64, there);
+                arrive_expect(there, (c1 - c0) * bytes);
+                for (int c = c0; c < c1; ++c)
+                    tma_load_2d(smem_addr(mine) + (c - c0) * bytes, &g.map_add, x, y + c * 16, there);
             }
             ++loads;
         };
@@ -550,14 +555,14 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             __syncwarp();  // (the tile before has been read)
 #pragma unroll
             for (int i = lane; i < 128; i += 32) {
-                const int n = n0 + (WIDE ? half * 128 : 0) + i;
+                const int n = n0 + (WIDE ? before : 0) + i;
                 scales[i] = n < g.n ? g.xscale[n] : 0.f;
             }
             __syncwarp();
             const float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
             // the residual, on its way while the products run
-            const int mw = m - lane, nw = n0 + half * 128;
-            if (WIDE && g.staged && e.add) load_residual(mw, nw);
+            const int mw = m - lane, nw = n0 + before;
+            if (WIDE && g.staged && e.add) load_residual(mw, nw, 0, f32 ? 4 : chunks);
             const bool planned = WIDE && g.sums;
             if (planned && !(ok = warp_wait_for(sh, &sh.plan_full[tiles & 1], tiles >> 1 & 1))) break;
             bool first = true, whole = false;  // whole: acc holds integers
@@ -570,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             };
             for (int k0 = t.kb0; k0 < t.kb1; k0 += kSumBlocks) {
                 const int seg = (k0 - t.kb0) / kSumBlocks;
-                if (planned && k0 + kSumBlocks < t.kb1 && !(sh.ends[tiles & 1][seg / 32] >> seg % 32 & 1)) continue;
+                if (planned && k0 + kSumBlocks < t.kb1 && !(sh.ends[tiles & 1][seg])) continue;
                 const unsigned buf = WIDE ? half : sums & 1;
                 if (!(ok = warp_wait_for(sh, &sh.tfull[buf], (WIDE ? sums : sums >> 1) & 1))) break;
                 ++sums;
@@ -614,7 +619,8 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             // (Four chunks at a time; the sums move through their registers: all eight unrolled, the
             // epilogue's instructions would come eight times, and each move counts too.)
             if (WIDE && g.staged) {
-                const auto rounds = [&](auto *at) {  // of 64 columns
+                const auto rounds = [&](auto *at) {  // of four chunks
+                    constexpr unsigned kBytes = sizeof(*at) * 512;  // of one
 #pragma unroll 1
                     for (int i = 0; i < 2; ++i) {
                         if (e.add && (i == 0 || f32)) {
@@ -625,14 +631,17 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                         }
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            staged16(acc[k], scales + (4 * i + k) * 16, alpha, bias, e.act, e.add, at + k * 512);
+                            if (4 * i + k < chunks)
+                                staged16(acc[k], scales + (4 * i + k) * 16, alpha, bias, e.act, e.add, at + k * 512);
                         fence_async_smem();
                         __syncwarp();
-                        if (lead && mw < g.m && nw + i * 64 < g.n)  // (else none of it is in the matrix)
-                            tma_store(&g.map_out, mw, nw + i * 64, smem_addr(mine) + (f32 ? 0 : i * 4096));
+                        if (lead && mw < g.m)
+                            for (int c = 4 * i; c < min(4 * i + 4, chunks) && nw + c * 16 < g.n; ++c)
+                                tma_store(&g.map_out, mw, nw + c * 16, smem_addr(mine) + (f32 ? c & 3 : c) * kBytes);
+                        if (lead) asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
                         if (i == 0) {
                             if (!f32) at += 2048;
-                            else if (e.add) load_residual(mw, nw + 64);
+                            else if (e.add) load_residual(mw, nw, 4, chunks);
 #pragma unroll
                             for (int k = 0; k + 4 < CH; ++k)
 #pragma unroll
@@ -645,7 +654,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 if (!ok) break;
                 continue;
             }
-            const float *const xs = scales - (WIDE ? half * 128 : 0);
+            const float *const xs = scales - (WIDE ? before : 0);
 #pragma unroll 1
             for (int i = 0; i < chunks; i += 4) {
 #pragma unroll
@@ -803,16 +812,18 @@ bool in_pairs(const void *p, int type, long long ld, int m) {
 Int8Plan plan_int8_anew(int m, int n, int k, int sms) {
     Int8Plan best;
     const int kblocks = cdiv(k, kTerms);
-    static const int tiles[5] = {16, 32, 64, 128, 256};
+    static const int tiles[8] = {16, 32, 64, 128, 160, 192, 224, 256};
     for (int bn : tiles) {
-        const int cg = bn == 256 ? 2 : 1;
+        const int cg = bn > 128 ? 2 : 1;
         if (bn > 16 && bn >= 2 * n) continue;
         const int mt = cdiv(m, 128 * cg), nt = cdiv(n, bn);
         const long long units = (long long)mt * nt;
-        // clocks of a block of 128 terms: MMAs; bytes of W at the memory's rate when all SMs read, with
-        // x's at TMA's; shared memory, in and out; the widening
+        // Clocks of a block of 128 terms: MMAs; bytes of W at the memory's rate when all SMs read, with
+        // x's at TMA's; shared memory, in and out; the widening.  (Pairs as measured: 1,200 with 160
+        // columns, 1,350 with 224, 1,390 with 256; of a CTA with 128 950 to 1,200.)
         const double mma = 8 * (bn / 2 + 10.0), w = kRawBytes, x = bn / cg * 256.0;
-        const double per = std::max({mma, w / 23.0, (w + x) / 50.0, 2 * (w + x) / 128.0, 500.0});
+        const double per = cg == 2 ? 1000.0 + 1.5 * bn
+                                   : std::max({mma, w / 23.0, (w + x) / 50.0, 2.4 * (w + x) / 128.0, 500.0});
         const double tail = 4500.0 + bn * 16.0;
         for (int cl = 1; cl <= 8; cl *= 2) {
             if (cl > 1 && (cg > 1 || cl > kblocks)) break;
@@ -855,12 +866,19 @@ Int8Plan plan_int8(int m, int n, int k) {
 
 qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t st) {
     Int8Args g = {};
-    const int cg = plan.cg, bn = plan.bn, wide = bn == 256;
-    const int box = (wide ? 128 : bn) / cg;  // rows of x at a time
+    const int cg = plan.cg, bn = plan.bn;
+    const bool wide = bn > 128;
+    // (of a pair's MMAs an accumulator has a multiple of 32 columns)
+    const int wide0 = bn > 192 ? 128 : 96, cols = wide ? wide0 : bn;
+    if (wide ? bn % 32 || bn < 160 || bn > 256 : bn % 16) return QCNN_ERR_UNSUPPORTED;
     qcnn_status rc = tensor_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, p.W, p.k, p.m, p.ldw, kTerms, 128, true, &g.map_w);
     if (rc != QCNN_OK) return rc;
-    rc = tensor_map(CU_TENSOR_MAP_DATA_TYPE_FLOAT16, p.x, p.k, p.n, p.ldx * 2, 64, box, true, &g.map_x);
+    rc = tensor_map(CU_TENSOR_MAP_DATA_TYPE_FLOAT16, p.x, p.k, p.n, p.ldx * 2, 64, cols / cg, true, &g.map_x);
+    if (rc == QCNN_OK && wide)
+        rc = tensor_map(CU_TENSOR_MAP_DATA_TYPE_FLOAT16, p.x, p.k, p.n, p.ldx * 2, 64, (bn - wide0) / cg, true, &g.map_x2);
     if (rc != QCNN_OK) return rc;
+    g.wide[0] = wide0;
+    g.wide[1] = bn - wide0;
     g.m = p.m;
     g.n = p.n;
     g.kblocks = cdiv(p.k, kTerms);
@@ -887,16 +905,17 @@ qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t
                (!p.e.add || tma_can(p.e.add, p.e.lda * size));
     if (g.staged) {
         const CUtensorMapDataType type = size == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-        rc = tensor_map(type, p.e.out, p.m, p.n, p.e.ldo * size, 32, 64, false, &g.map_out);
+        rc = tensor_map(type, p.e.out, p.m, p.n, p.e.ldo * size, 32, 16, false, &g.map_out);
         if (rc == QCNN_OK && p.e.add)
-            rc = tensor_map(type, p.e.add, p.m, p.n, p.e.lda * size, 32, 64, false, &g.map_add);
+            rc = tensor_map(type, p.e.add, p.m, p.n, p.e.lda * size, 32, 16, false, &g.map_add);
         if (rc != QCNN_OK) return rc;
     }
     const size_t staged = g.staged ? 8 * (size_t)kStagedBytes : 0;
     g.S = g.staged ? kStages - 1 : kStages;
     g.R = (int)std::min<size_t>(kRawStagesMax, (kSmem - 1024 - staged - g.S * (size_t)g.stage) / kRawBytes);
     // fp32 sums of fp16, 128 (256) rows x the columns of an accumulator
-    g.idesc = (1u << 4) | (uint32_t)((wide ? 128 : bn) >> 3) << 17 | (uint32_t)(128 * cg >> 4) << 24;
+    for (int h = 0; h < 2; ++h)
+        g.idesc[h] = (1u << 4) | (uint32_t)((h ? bn - wide0 : cols) >> 3) << 17 | (uint32_t)(128 * cg >> 4) << 24;
     g.sums = wide && p.segs > 1 ? p.sums : nullptr;
     g.segs = p.segs;
     g.xscale = p.xscale;

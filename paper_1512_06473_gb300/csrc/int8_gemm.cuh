@@ -29,7 +29,7 @@ Int8Plan plan_int8(int m, int n, int k);
 // sums of magnitudes.
 constexpr int kInt8Segment = 1024;
 constexpr int kInt8MaxTerms = 131071;  // whose sum of products fits 32 bits
-inline bool int8_sums(const Int8Plan &p, int k) { return p.bn == 256 && k > kInt8Segment; }
+inline bool int8_sums(const Int8Plan &p, int k) { return p.bn > 128 && k > kInt8Segment; }
 qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t st);
 
 }  // namespace qcnn

@@ -17,7 +17,8 @@ I8 = torch.int8
 TILES = [  # N, Cs, Ct
     (16, 9216, 4096), (8, 5121, 100), (257, 64, 513), (33, 9216, 130), (128, 1024, 1029), (700, 1024, 640),
     (129, 1000, 1024), (1025, 1100, 700), (200, 9216, 1000), (300, 2048, 1000), (300, 5000, 2001), (601, 4097, 3001),
-    (2000, 200, 1500), (2049, 1025, 1537), (1999, 3000, 1535)]
+    (2000, 200, 1500), (2049, 1025, 1537), (1999, 3000, 1535), (3001, 2047, 5003), (1000, 1000, 4000), (1999, 9216, 2001),
+    (3000, 12000, 1000)]
 
 
 def _case(seed, N, Cs, Ct, codes, dtype, low=-127, high=127):
@@ -34,9 +35,9 @@ def _case(seed, N, Cs, Ct, codes, dtype, low=-127, high=127):
 def test_every_route_is_among_them():
     routes = [q.int8_route(*t) for t in TILES]
     assert not any(r["few"] for r in routes)
-    assert {r["rows"] for r in routes} == {16, 32, 64, 128, 256}
+    assert {r["rows"] for r in routes} == {16, 32, 64, 128, 160, 192, 224, 256}
     assert {r["shares"] for r in routes} == {1, 2, 4, 8}
-    assert all((r["ctas"] == 2) == (r["rows"] == 256) for r in routes)
+    assert all((r["ctas"] == 2) == (r["rows"] > 128) for r in routes)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -105,7 +106,7 @@ def test_weights_and_codes_of_any_alignment(shape, pitch, off, codes):
 
 
 @pytest.mark.parametrize("shape", [(300, 1024, 1000), (300, 5000, 2001), (601, 9216, 3001), (1999, 3000, 1535),
-                                   (1500, 9216, 1301)])
+                                   (1500, 9216, 1301), (2300, 9216, 2100), (600, 131071, 2001), (2304, 131071, 2048)])
 def test_sums_are_exact(shape):
     """Sums below 2^24 in magnitude come out exactly, whatever is summed on the way."""
     N, Cs, Ct = shape
