@@ -183,6 +183,8 @@ __device__ __forceinline__ float above_zero(float a) {  // (NaN stays)
     asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(a));
     return r;
 }
+// |a|, but of +inf the largest finite value: times erfc's 0 that is 0, and gelu(inf) = inf.
+__device__ __forceinline__ float magnitude(float a) { return fmaxf(fminf(a, 3.402823466e38f), -a); }
 __device__ __forceinline__ void gelu2(float &a, float &b) {
     const float2 z = make_float2(a, b);
     constexpr float kP = 0.3275911f * 0.70710678118654752f;
@@ -195,8 +197,8 @@ __device__ __forceinline__ void gelu2(float &a, float &b) {
     p = __ffma2_rn(p, t, both(0.5f * 0.284496736f));
     p = __ffma2_rn(p, t, both(-0.5f * 0.254829592f));
     p = __fmul2_rn(__fmul2_rn(p, t), q);
-    a = fmaf(fabsf(a), p.x, above_zero(a));  // (an infinite z leaves NaN: q is 0)
-    b = fmaf(fabsf(b), p.y, above_zero(b));
+    a = fmaf(magnitude(a), p.x, above_zero(a));
+    b = fmaf(magnitude(b), p.y, above_zero(b));
 }
 __device__ __forceinline__ void int8_act16(float (&v)[16], int act) {
     if (act == QCNN_ACT_RELU) {

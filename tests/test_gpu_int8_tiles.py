@@ -125,8 +125,8 @@ def test_sums_are_exact(shape):
     # every product the largest there is, of both signs by blocks of 1024
     x = torch.full((N, Cs), -128, device="cuda", dtype=I8)
     w = torch.full((Ct, Cs), -128, device="cuda", dtype=I8)
-    w[:, 1024:2048] = 127
-    w[:, 3072:4096] = 127
+    for block in (1, 3):
+        w[:, 1024 * block:1024 * block + 1024] = 127
     w[:, 4096:] = 1
     y = q.int8_dense_forward(x, w, one(Ct), xscale=one(N))
     assert torch.equal(y.double(), x.double() @ w.double().T)
@@ -161,6 +161,28 @@ def test_non_finite_rows(shape, dtype):
         assert bool(finite[rest][:, keep].all())
         if act == "none":
             assert not bool(finite[:, 5].any())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(3, 70, 90), (300, 2048, 1000), (2000, 1500, 1500), (2000, 300, 1501)])
+def test_infinite_sums_keep_what_the_activations_make_of_them(shape, dtype):
+    """Biases of infinities, and sums at fp32's end: z Phi(z) and z / (1 + exp(-z)) on every route."""
+    N, Cs, Ct = shape
+    g, x, _, w, ws, (c, s) = _case(10, N, Cs, Ct, False, dtype)
+    b = torch.zeros(Ct, device="cuda")
+    b[:4] = torch.tensor([float("inf"), float("-inf"), 3.3e38, -3.3e38], device="cuda")
+    for act in ("none", "relu", "gelu", "silu"):
+        y = q.int8_dense_forward(x, w, ws, b, act=act)
+        assert bool((y[:, 0] == float("inf")).all())
+        if act == "relu":
+            assert bool((y[:, 1] == 0).all())
+        elif act != "none":
+            assert bool(torch.isnan(y[:, 1]).all())  # (-inf times 0, as in the formulas)
+        top = 3.3e38 if dtype == F32 else float(torch.tensor(3.3e38).to(BF16))
+        assert bool(((y[:, 2].double() / top - 1).abs() <= 2.0 ** -7).all())
+        if act != "none":
+            assert bool((y[:, 3] == 0).all())
+        assert bool(torch.isfinite(y[:, 4:]).all())
 
 
 @pytest.mark.parametrize("N,Cs,Ct", [(8, 5120, 500), (9, 5120, 400), (64, 1024, 1831), (128, 900, 1024), (1000, 100, 131),
