@@ -8,7 +8,7 @@
 // four elements, and these go at 32 lanes per clock and SM (measured), nothing else of their warps'
 // quarter of the SM being issued meanwhile: 32 slots of a lane per element, of which 132 us for the 151
 // million elements of 16384 x 9216.  Four bytes an element (bf16 without a residual) are bound by that
-// (3001 x 5003 17 us, of which its bytes take 9), six (with a residual) by both (906 MB in 143 us, 6.3
+// (3001 x 5003 17 us, of which its bytes take 9), six (with a residual) by both (906 MB in 139 us, 6.5
 // TB/s), eight (fp32) by the bytes (604 MB in 91 us, 6.7 TB/s).
 #include "train.cuh"
 

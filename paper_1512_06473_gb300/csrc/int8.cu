@@ -57,7 +57,8 @@ struct QuantizeArgs {
 };
 
 // G threads a row (a warp, several or the CTA), which keep up to H vectors of 16 bytes each between
-// the two steps; what a row has beyond that is read again.  SHIFT: rows begin off the 16 bytes, and a
+// the two steps; what a row has beyond that is read again.  Bound by the bytes (4096 x 9216 in fp32 28.8
+// us, 6.6 TB/s).  SHIFT: rows begin off the 16 bytes, and a
 // vector is taken out of the two aligned ones that it lies in (1000 x 4097 in bf16 8.6 us element by
 // element).
 template <typename T, int G, int H, bool SHIFT, bool HALF>

@@ -13,11 +13,17 @@
 // registers, and the sums that a result has more than one of are added there as integers: exact, and
 // rounded to fp32 once.
 //
-// Tile.  As gemm_kernel.cuh's: 128 (a pair of CTAs: 256) rows of m, TMEM lanes, x bn columns of n.  160 to
-// 256 columns (of a pair, in steps of 32, so that the last round of tiles is a full one: 1000 x 2000 ->
-// 3000 in tiles of 192 20.0 us, of 256 22.5; 1500 x 9216 -> 4096 94 and 108) are two accumulators, of 64 to 128 columns, that the MMAs of a block
-// of 128 terms fill one after the other, so that draining the first overlaps the MMAs of the second; up to
-// 128 columns take two accumulators in turn.  TMEM: 256 columns of accumulators, four stages of W, 128 terms in 64 columns each.
+// Tile.  As gemm_kernel.cuh's: 128 (a pair of CTAs: 256) rows of m, TMEM lanes, x bn columns of n.  160
+// to 256 columns (of a pair, in steps of 32, so that the last round of tiles is a full one: 1000 x 2000 ->
+// 3000 in tiles of 192 20.0 us, of 256 22.5; 1500 x 9216 -> 4096 94 and 108) are two accumulators, of 64 to
+// 128 columns, that the MMAs of a block of 128 terms fill one after the other, so that draining the first
+// overlaps the MMAs of the second; up to 128 columns take two accumulators in turn.  TMEM: 256 columns of
+// accumulators, four stages of W, 128 terms in 64 columns each.
+//
+// Bounds.  Large: the MMAs (4096 x 4096 -> 8192 with GELU and a residual in bf16 147 us, 1.87 PFLOP/s, the
+// tensor pipe active for 73%).  Ragged: last rounds and stores of odd rows (3001 x 2047 -> 5003 in fp32 44
+// us).  One tile of rows: what a CTA loads for a block of 128 terms, x's tile twice as much as W's (128 x
+// 9216 -> 4096 16 us, tensor pipe 16%).
 //
 // Roles (16 warps): 0 TMA of x, 1 MMA, 2 TMEM and TMA of W, 4-11 drain and epilogue (two warps per TMEM
 // lane quarter), 12-15 widen: a warp has its 32 rows of W, a lane a row, 128 terms at a time.
@@ -64,8 +70,7 @@ struct Int8Shared {
     uint64_t full[kStages], empty[kStages], raw_full[kRawStagesMax], raw_empty[kRawStagesMax], tfull[2], tempty[2], done;
     uint64_t plan_full[2], plan_empty[2];
     uint64_t residual[8];
-    // Of two tiles: whether a sum ends with segment s.  (A byte each: as bits of words, ends[s / 32] >> s % 32,
-    // the compiled address of the word was off its four bytes from s = 8 on, and the kernel faulted.)
+    // Of two tiles: whether a sum ends with segment s, a byte each.
     uint8_t ends[2][kSegs];
     unsigned tmem;
     int give_up;
