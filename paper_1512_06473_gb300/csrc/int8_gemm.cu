@@ -25,8 +25,9 @@
 // us).  One tile of rows: what a CTA loads for a block of 128 terms, x's tile twice as much as W's (128 x
 // 9216 -> 4096 16 us, tensor pipe 16%).
 //
-// Roles (16 warps): 0 TMA of x, 1 MMA, 2 TMEM and TMA of W, 4-11 drain and epilogue (two warps per TMEM
-// lane quarter), 12-15 widen: a warp has its 32 rows of W, a lane a row, 128 terms at a time.
+// Roles (20 warps, WIDE 16): 0 TMA of x, 1 MMA, 2 TMEM and TMA of W, 3 (WIDE) where sums are drained, 4-11
+// drain and epilogue (two warps per TMEM lane quarter), from 12 on widen: a warp has its 32 rows of W, a lane
+// a row, 128 terms at a time.
 #define QCNN_UNIT_RECORDS
 #include "int8_gemm.cuh"
 
@@ -40,7 +41,10 @@
 namespace qcnn {
 namespace {
 
-constexpr int kThreads = 512;
+// WIDE: one group of four warps widens (the drain's registers leave no room for another); else two, a block
+// each in turn (16 x 9216 -> 9216 22.0 us, 24.5 with one, 257 x 2047 -> 2001 13.8 and 15.3, 64 x 9216 -> 4096
+// 18.0 and 18.9; 128 columns, bound by shared memory, the same).
+constexpr int int8_threads(bool wide) { return wide ? 512 : 640; }
 constexpr int kTerms = 128;            // of a block (with half of that, its waits took a fifth of the time)
 constexpr int kStages = 4;             // blocks of W in TMEM, at most
 constexpr int kWCols = 64;             // TMEM columns of one
@@ -318,7 +322,7 @@ __device__ __forceinline__ void int8_finish(const GemmEpi &e, int m, int n, int 
 // ------------------------------------------------------------------- kernel
 // WIDE: tiles of 160 to 256 columns, by pairs of CTAs.
 template <int CG, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant__ Int8Args g) {
+__global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __grid_constant__ Int8Args g) {
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ Int8Shared sh;
     __shared__ __align__(16) float column_scales[8][128];
@@ -366,6 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
     tc_fence_after_sync();
     const unsigned tmem = sh.tmem;
 
+    // (640 threads: 48, 2 x 144 and 2 x 72 are 480, 5 x 96; 512: 48, 2 x 192 and 80 are 512, 4 x 128)
     if (warp < 4) set_registers<48, false>();
     if (warp == 0) {
         // ----------------------------------------------------------- TMA of x
@@ -517,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         __syncwarp();
     } else if (warp >= 4 && warp < 12) {
         // ---------------------------------------------------- drain, epilogue
-        set_registers<192, true>();
+        set_registers<WIDE ? 192 : 144, true>();
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const unsigned tl = tmem + ((unsigned)(quarter * 32) << 16);
         grid_dep_sync();
@@ -735,14 +740,19 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
         }
     } else if (warp >= 12) {
         // -------------------------------------------------------------- widen
-        set_registers<80, false>();
-        const int quarter = warp & 3;
+        set_registers<WIDE ? 80 : 72, false>();
+        // (a group: every second block; WIDE: all)
+        constexpr int GROUPS = WIDE ? 1 : 2;
+        const int quarter = warp & 3, group = (warp - 12) >> 2;
         const unsigned a_dst = tmem + 256 + ((unsigned)(quarter * 32) << 16);
         const unsigned own = raw0 + (quarter * 32 + lane) * 128;  // (the pieces of a row permuted: 128-byte swizzle)
-        int slot = 0, rslot = 0;
+        int slot = group, rslot = group;
         unsigned par = 0, rpar = 0;
+        auto next = [](int &at, unsigned &parity, int stages) {
+            if ((at += GROUPS) >= stages) at -= stages, parity ^= 1;
+        };
         bool ok = true;
-        int left = 0;  // blocks
+        int left = -group;  // blocks from this group's on
         for (int u = first_unit; u < g.units; u += step) {
             const Int8Tile t = int8_tile(g, u, share);
             left += t.kb1 - t.kb0;
@@ -757,8 +767,8 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                              : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
                              : "r"(from + ((i ^ (lane & 7)) << 4)));
         };
-        if (left) read();
-        for (; left > 0 && ok; --left) {
+        if (left > 0) read();
+        for (; left > 0 && ok; left -= GROUPS) {
             if (!(ok = warp_wait_for(sh, &sh.empty[slot], par ^ 1))) break;
             tc_fence_after_sync();
 #pragma unroll
@@ -770,11 +780,8 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
             }
             __syncwarp();  // (all have read)
             if (lane == 0) arrive(&sh.raw_empty[rslot]);
-            if (++rslot == g.R) {
-                rslot = 0;
-                rpar ^= 1;
-            }
-            if (left > 1) read();  // (the next, while the stores are under way)
+            next(rslot, rpar, g.R);
+            if (left > GROUPS) read();  // (the next, while the stores are under way)
             asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
             tc_fence_before_sync();
             __syncwarp();
@@ -782,10 +789,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_kernel(const __grid_constant
                 if constexpr (CG == 1) arrive(&sh.full[slot]);
                 else arrive_first(&sh.full[slot]);
             }
-            if (++slot == g.S) {
-                slot = 0;
-                par ^= 1;
-            }
+            next(slot, par, g.S);
         }
     }
     if constexpr (CG == 1) {
@@ -808,7 +812,7 @@ qcnn_status launch_of(const Int8Args &g, int ctas, size_t smem, cudaStream_t st)
     const qcnn_status rc = allow_smem(reinterpret_cast<const void *>(k));
     if (rc != QCNN_OK) return rc;
     const int cluster = CG * g.cl;
-    return launch_k(k, dim3(ctas), dim3(kThreads), smem, st, dim3(cluster > 1 ? cluster : 0, 1, 1), g);
+    return launch_k(k, dim3(ctas), dim3(int8_threads(WIDE)), smem, st, dim3(cluster > 1 ? cluster : 0, 1, 1), g);
 }
 
 // Whether a matrix of two-byte elements can go in pairs of neighbours along m.
@@ -838,7 +842,7 @@ Int8Plan plan_int8_anew(int m, int n, int k, int sms) {
             if (cdiv(kblocks, kps) != cl) continue;
             const int slots = cl == 1 ? sms / cg
                                       : std::max(1, cluster_capacity(reinterpret_cast<const void *>(int8_kernel<1, false>),
-                                                                     kThreads, cl, kSmem));
+                                                                     int8_threads(false), cl, kSmem));
             const double waves = (double)((units + slots - 1) / slots);
             const double meet = cl > 1 ? 2500.0 + bn * 10.0 : 0.0, more = cl > 1 ? tail + meet : 1000.0;
             const double score = waves * kps * per + tail + meet + (waves - 1) * more;
