@@ -22,8 +22,8 @@
 //
 // Bounds.  Large: the MMAs (4096 x 4096 -> 8192 with GELU and a residual in bf16 147 us, 1.87 PFLOP/s, the
 // tensor pipe active for 73%).  Ragged: last rounds and stores of odd rows (3001 x 2047 -> 5003 in fp32 44
-// us).  One tile of rows: what a CTA loads for a block of 128 terms, x's tile twice as much as W's (128 x
-// 9216 -> 4096 16 us, tensor pipe 16%).
+// us).  Tiles of 128 columns of one CTA: what passes through its shared memory for a block of 128 terms, 48 KB in
+// and out, 768 of its 1,000 clocks (128 x 9216 -> 4096 16 us, tensor pipe 16%); narrower ones: the widening.
 //
 // Roles (20 warps, WIDE 16): 0 TMA of x, 1 MMA, 2 TMEM and TMA of W, 3 (WIDE) where sums are drained, 4-11
 // drain and epilogue (two warps per TMEM lane quarter), from 12 on widen: a warp has its 32 rows of W, a lane
@@ -41,9 +41,10 @@
 namespace qcnn {
 namespace {
 
-// WIDE: one group of four warps widens (the drain's registers leave no room for another); else two, a block
-// each in turn (16 x 9216 -> 9216 22.0 us, 24.5 with one, 257 x 2047 -> 2001 13.8 and 15.3, 64 x 9216 -> 4096
-// 18.0 and 18.9; 128 columns, bound by shared memory, the same).
+// WIDE: one group of four warps widens (the drain's registers leave no room for another).  Else two, in turn a
+// block each, up to 64 columns (16 x 9216 -> 9216 22.0 us, 24.5 with one, 257 x 2047 -> 2001 13.6 and 15.1, 64 x
+// 9216 -> 4096 17.9 and 19.0); of 128 columns, bound by shared memory, one (128 x 9216 -> 4096 20.6, 21.1 with
+// two).
 constexpr int int8_threads(bool wide) { return wide ? 512 : 640; }
 constexpr int kTerms = 128;            // of a block (with half of that, its waits took a fifth of the time)
 constexpr int kStages = 4;             // blocks of W in TMEM, at most
@@ -741,19 +742,18 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
     } else if (warp >= 12) {
         // -------------------------------------------------------------- widen
         set_registers<WIDE ? 80 : 72, false>();
-        // (a group: every second block; WIDE: all)
-        constexpr int GROUPS = WIDE ? 1 : 2;
+        const int groups = WIDE || g.bn > 64 ? 1 : 2;  // each has every second block
         const int quarter = warp & 3, group = (warp - 12) >> 2;
         const unsigned a_dst = tmem + 256 + ((unsigned)(quarter * 32) << 16);
         const unsigned own = raw0 + (quarter * 32 + lane) * 128;  // (the pieces of a row permuted: 128-byte swizzle)
         int slot = group, rslot = group;
         unsigned par = 0, rpar = 0;
-        auto next = [](int &at, unsigned &parity, int stages) {
-            if ((at += GROUPS) >= stages) at -= stages, parity ^= 1;
+        auto next = [groups](int &at, unsigned &parity, int stages) {
+            if ((at += groups) >= stages) at -= stages, parity ^= 1;
         };
         bool ok = true;
-        int left = -group;  // blocks from this group's on
-        for (int u = first_unit; u < g.units; u += step) {
+        int left = -group;  // blocks from this group's first on
+        for (int u = first_unit; u < g.units && group < groups; u += step) {
             const Int8Tile t = int8_tile(g, u, share);
             left += t.kb1 - t.kb0;
         }
@@ -768,7 +768,7 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
                              : "r"(from + ((i ^ (lane & 7)) << 4)));
         };
         if (left > 0) read();
-        for (; left > 0 && ok; left -= GROUPS) {
+        for (; left > 0 && ok; left -= groups) {
             if (!(ok = warp_wait_for(sh, &sh.empty[slot], par ^ 1))) break;
             tc_fence_after_sync();
 #pragma unroll
@@ -781,7 +781,7 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
             __syncwarp();  // (all have read)
             if (lane == 0) arrive(&sh.raw_empty[rslot]);
             next(rslot, rpar, g.R);
-            if (left > GROUPS) read();  // (the next, while the stores are under way)
+            if (left > groups) read();  // (the next, while the stores are under way)
             asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
             tc_fence_before_sync();
             __syncwarp();
