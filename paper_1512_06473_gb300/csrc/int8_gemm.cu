@@ -181,7 +181,8 @@ __device__ __forceinline__ void widen4(unsigned w, unsigned &lo, unsigned &hi) {
 // gelu(z) = max(z, 0) - |z| / 2 erfc(|z| / sqrt 2), erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 +
 // p x): Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, to 1.5e-7, here of |z| / 2.
 // silu(z) = z / (1 + exp(-z)).  In pairs, exponentials and reciprocals by the fast units (2 and 1 ulp):
-// with erff the 256 x 256 tiles of 4096 terms took longer in the epilogue than in the products.
+// with erff the 256 x 256 tiles of 4096 terms took longer in the epilogue than in the products.  For
+// bf16 results, whose rounding is up to 2^-8 of them.
 __device__ __forceinline__ float fast_rcp(float x) {
     float r;
     asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -210,10 +211,71 @@ __device__ __forceinline__ void gelu2(float &a, float &b) {
     a = fmaf(magnitude(a), p.x, above_zero(a));
     b = fmaf(magnitude(b), p.y, above_zero(b));
 }
-__device__ __forceinline__ void int8_act16(float (&v)[16], int act) {
+// The same for fp32 results, to their last bits.
+// gelu: below 1.5 z (1/2 + z R(z^2)), R a polynomial near (Phi(z) - 1/2) / z (to 2.7e-9 of it); beyond as above
+// with a sixth term and coefficients for that range alone (to 6e-7 of erfc, 4e-8 of what it is taken from).
+// Both fitted for the least largest error (Lawson's weights).  In fp32 2.9e-8 of the norm of normal z where
+// erff has 4.8e-8.
+__device__ __forceinline__ void gelu2_exact(float &a, float &b) {
+    const float2 z = make_float2(a, b), u = __fmul2_rn(z, z);
+    float2 r = __ffma2_rn(u, both(4.11555712e-07f), both(-8.71830202e-06f));
+    r = __ffma2_rn(r, u, both(0.000114356385f));
+    r = __ffma2_rn(r, u, both(-0.00118648848f));
+    r = __ffma2_rn(r, u, both(0.0099732413f));
+    r = __ffma2_rn(r, u, both(-0.066490335f));
+    r = __ffma2_rn(r, u, both(0.398942279f));
+    const float2 near = __ffma2_rn(z, __fmul2_rn(z, r), __fmul2_rn(z, both(0.5f)));
+    constexpr float kP = 0.3275911f * 0.70710678118654752f;
+    const float2 t = make_float2(fast_rcp(fmaf(fabsf(a), kP, 1.f)), fast_rcp(fmaf(fabsf(b), kP, 1.f)));
+    const float2 x = __fmul2_rn(__fmul2_rn(z, both(-0.5f * kLog2e)), z);
+    const float2 q = make_float2(ex2(x.x), ex2(x.y));
+    // (times -1/2)
+    float2 p = __ffma2_rn(t, both(-0.5f * 0.324728743f), both(0.5f * 0.128127106f));
+    p = __ffma2_rn(p, t, both(-0.5f * 0.295275164f));
+    p = __ffma2_rn(p, t, both(-0.5f * 0.132917903f));
+    p = __ffma2_rn(p, t, both(-0.5f * 0.191366617f));
+    p = __ffma2_rn(p, t, both(-0.5f * 0.184408403f));
+    p = __fmul2_rn(__fmul2_rn(p, t), q);
+    a = fabsf(a) < 1.5f ? near.x : fmaf(magnitude(a), p.x, above_zero(a));
+    b = fabsf(b) < 1.5f ? near.y : fmaf(magnitude(b), p.y, above_zero(b));
+}
+// silu: z log2 e in two parts, the second (what rounding the first took off, and log2 e's own rest) as 1 + d ln 2
+// behind the exponential.  z is held to where that is finite: beyond, exp(-z) is 0 or infinite all the same.
+__device__ __forceinline__ void silu2_exact(float &a, float &b) {
+    const float2 z = make_float2(fminf(fmaxf(a, -200.f), 200.f), fminf(fmaxf(b, -200.f), 200.f));
+    const float2 t = __fmul2_rn(z, both(-kLog2e));
+    float2 d = __ffma2_rn(z, both(kLog2e), t);
+    d = __ffma2_rn(z, both((float)(1.4426950408889634074 - kLog2e)), d);
+    float2 q = __fmul2_rn(make_float2(ex2(t.x), ex2(t.y)), __ffma2_rn(d, both(-0.69314718f), both(1.f)));
+    q = __fadd2_rn(q, both(1.f));
+    a *= fast_rcp(q.x);
+    b *= fast_rcp(q.y);
+}
+// exact: of fp32 results
+__device__ __forceinline__ void int8_act16(float (&v)[16], int act, bool exact) {
     if (act == QCNN_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = act_apply(v[i], QCNN_ACT_RELU);
+    } else if (exact) {
+        if (act == QCNN_ACT_GELU) {
+            // (four at a time, the others moving up: its instructions come four times and not sixteen, and its
+            // constants, in pairs, leave the drain its registers)
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+                float t[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t[j] = v[j];
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) gelu2_exact(t[j], t[j + 1]);
+#pragma unroll
+                for (int j = 0; j < 12; ++j) v[j] = v[j + 4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[12 + j] = t[j];
+            }
+        } else if (act == QCNN_ACT_SILU) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) silu2_exact(v[i], v[i + 1]);
+        }
     } else if (act == QCNN_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < 16; i += 2) gelu2(v[i], v[i + 1]);
@@ -246,7 +308,7 @@ template <typename T>
 __device__ __forceinline__ void staged16(float (&v)[16], const float *xs, float alpha, float bias, int act, bool res,
                                          T *at) {
     scaled16(v, xs, alpha, bias);
-    int8_act16(v, act);
+    int8_act16(v, act, sizeof(T) == 4);
     if (res) {
 #pragma unroll
         for (int j = 0; j < 16; j += 2) {
@@ -294,11 +356,11 @@ __device__ __forceinline__ void int8_finish(const GemmEpi &e, int m, int n, int 
     if (e.add) {
         float r[16];
         fetch_values(e, m, n, count, r);
-        int8_act16(v, e.act);
+        int8_act16(v, e.act, e.out_type == GEMM_T_F32);
 #pragma unroll
         for (int j = 0; j < 16; j += 2) add2(v[j], v[j + 1], r[j], r[j + 1]);
     } else {
-        int8_act16(v, e.act);
+        int8_act16(v, e.act, e.out_type == GEMM_T_F32);
     }
     if (e.out_type == GEMM_T_F32) {
         float *p = static_cast<float *>(e.out) + (long long)n * e.ldo + m;
@@ -668,29 +730,38 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
                 continue;
             }
             const float *const xs = scales - (WIDE ? before : 0);
-#pragma unroll 1
-            for (int i = 0; i < chunks; i += 4) {
+            const auto chunk = [&](int c, float (&v)[16]) {
+                const int n = n0 + c * 16, left = g.n - n;
+                if (g.cl > 1) {  // to the cluster
+                    const unsigned d = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int c = chunk_at(i + k), n = n0 + c * 16, left = g.n - n;
-                    if (i + k >= chunks) break;
-                    if (g.cl > 1) {  // to the cluster
-                        const unsigned d = smem_addr(smem) + (unsigned)(c * 4 + quarter) * 2048 + lane * 16;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(d + j * 512),
-                                         "f"(acc[k][4 * j]), "f"(acc[k][4 * j + 1]), "f"(acc[k][4 * j + 2]),
-                                         "f"(acc[k][4 * j + 3])
-                                         : "memory");
-                    } else if (left > 0) {
-                        int8_finish(e, m, n, m < g.m ? min(left, 16) : 0, alpha, bias, xs + c * 16, acc[k]);
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(d + j * 512), "f"(v[4 * j]),
+                                     "f"(v[4 * j + 1]), "f"(v[4 * j + 2]), "f"(v[4 * j + 3])
+                                     : "memory");
+                } else if (left > 0) {
+                    int8_finish(e, m, n, m < g.m ? min(left, 16) : 0, alpha, bias, xs + c * 16, v);
                 }
-                if (CH > 4 && i == 0)
+            };
+            if constexpr (WIDE) {
+                // (one copy of the instructions: 3001 x 2047 -> 5003 in bf16 with GELU 67.9 us, with four 80.8)
+#pragma unroll 1
+                for (int i = 0; i < chunks; ++i) {
+                    chunk(chunk_at(i), acc[0]);
 #pragma unroll
-                    for (int k = 0; k + 4 < CH; ++k)
+                    for (int k = 0; k < 3; ++k)
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 4][j];
+                        for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 1][j];
+                    if (i == 3)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) acc[k][j] = acc[k + 4][j];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < chunks) chunk(chunk_at(i), acc[i]);
             }
         }
         if (WIDE && g.staged) {  // nothing of its own under way when the CTA leaves
