@@ -453,7 +453,9 @@ __global__ void __launch_bounds__(few_threads(NB), few_ctas(NB)) few_rows_kernel
         if (part == 0 && lane < kOut * NB && mine < groups && m < f.Ct && n < f.N) {
             int sum = 0;
             for (int p = 0; p < kw; ++p) sum += red[warp + p][lane];
-            finish_one(f.e, n, m, (float)sum * scale[n] * f.wscale[m]);
+            const float xs = scale[n], ws = f.wscale[m];
+            const bool swap = !(fabsf(xs) < kLargeScale);  // (as scaled16_large has it)
+            finish_one(f.e, n, m, (float)sum * (swap ? ws : xs) * (swap ? xs : ws));
         }
         if (kw > 1 && round + 1 < rounds) __syncthreads();
     }

@@ -29,6 +29,8 @@ Int8Plan plan_int8(int m, int n, int k);
 // sums of magnitudes.
 constexpr int kInt8Segment = 1024;
 constexpr int kInt8MaxTerms = 131071;  // whose sum of products fits 32 bits
+// A row's scale from which on a sum takes the output's first: a sum below 2^31 times less stays finite.
+constexpr float kLargeScale = 0x1p96f;
 inline bool int8_sums(const Int8Plan &p, int k) { return p.bn > 128 && k > kInt8Segment; }
 qcnn_status launch_int8(const Int8Plan &plan, const Int8Problem &p, cudaStream_t st);
 
