@@ -144,14 +144,15 @@ __device__ __forceinline__ void tmem_st32(unsigned taddr, const unsigned (&v)[32
         : "memory");
 }
 
-// An arrival on CTA 0 of the pair, of what this thread did to tensor memory.  (Its default order, of
-// this CTA alone: with .release.cluster, which waits for what the thread has under way, a block of 64
-// terms took 1,700 clocks instead of 600.)
+// An arrival on CTA 0 of the pair, of what this thread did to tensor memory: tcgen05.wait::st has completed
+// its stores and the fence before it orders them with the arrival, so that the arrival itself orders nothing
+// and is relaxed, at the scope of both CTAs.  (With .release.cluster, which waits for all that the thread has
+// under way, a block of 64 terms took 1,700 clocks instead of 600.)
 __device__ __forceinline__ void arrive_first(uint64_t *bar) {
     asm volatile(
         "{\n\t.reg .b32 a;\n\t"
         "mapa.shared::cluster.u32 a, %0, 0;\n\t"
-        "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}\n" ::"r"(smem_addr(bar))
+        "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [a];\n\t}\n" ::"r"(smem_addr(bar))
         : "memory");
 }
 // 32 columns of this warp's lanes, there after tcgen05.wait::ld.
