@@ -100,6 +100,7 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_vec_kernel(DropoutArg
     constexpr int V = 16 / (int)sizeof(T), B = kDropoutThreads;
     using L = unsigned long long;
     const L vectors = d.n / V, first = (L)blockIdx.x * (B * U) + threadIdx.x;
+    grid_dep_sync();
     const L offset = d.offset + (d.offset_add ? *d.offset_add : 0);
     const bool res = d.r != nullptr;
     const T *const x = static_cast<const T *>(d.x), *const r = static_cast<const T *>(d.r);
@@ -147,6 +148,7 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_vec_kernel(DropoutArg
 template <typename T>
 __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs d) {
     const unsigned long long block = (unsigned long long)blockIdx.x * 256 + threadIdx.x, i0 = block * 4;
+    grid_dep_sync();
     if (i0 >= d.n) return;
     unsigned w[4];
     philox(block, d.offset + (d.offset_add ? *d.offset_add : 0), d.k0, d.k1, w);

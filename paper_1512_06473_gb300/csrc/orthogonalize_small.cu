@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_small_kernel(const Args a) 
     __shared__ double2 norms[kThreads / 32 + 8];
     cg::cluster_group cluster = cg::this_cluster();
     cluster.barrier_arrive();  // (this CTA runs: its shared memory may be written to)
+    grid_dep_sync();
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int p4 = a.p4, pp = p4 * p4;
