@@ -784,7 +784,8 @@ qcnn_status qcnn_dropout_backward(const void *dy, long long lddy, int N, int C, 
  *   W [Ct][Cs] codes with wscale [Ct], as qcnn_int8_quantize gives them for the dense weights.
  *   xscale NULL: x [N][Cs] of dtype, whose rows the call quantizes as qcnn_int8_quantize does; else x
  *   [N][Cs] codes with xscale [N].  bias [Ct] fp32 or NULL; residual [N][Ct] of dtype or NULL (may be
- *   y itself); y [N][Ct] of dtype.  Any code from -128 to 127 will do; Cs <= 131071.
+ *   y itself); y [N][Ct] of dtype.  Any code from -128 to 127 will do; Cs <= 131071, N
+ *   and Ct <= 2^31 - 257 (QCNN_ERR_UNSUPPORTED).
  *   The sums are exact integers, rounded to fp32 once; then two products, bias, activation and residual
  *   in fp32, and one rounding to dtype.  (GELU is within 2^-22 |z| and SiLU within 10 2^-24 of itself before
  *   that; of bf16 results on the tensor cores, whose rounding is coarser, GELU within 2^-20 |z|.)

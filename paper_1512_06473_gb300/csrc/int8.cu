@@ -566,6 +566,11 @@ __global__ void __launch_bounds__(256) copy_kernel(CopyJob x, CopyJob w) {
 long long pad16(long long v) { return (v + 15) / 16 * 16; }
 bool rows16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 16 == 0; }
 bool codes_ok(const void *p, long long ld, long long rows, long long cols) { return ld >= cols && (rows == 0 || p); }
+// Tiles of up to 256 rows or outputs count from 0 in ints, past the last of them too.
+qcnn_status dense_sizes(int N, int Cs, int Ct) {
+    if (N < 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
+    return std::max(N, Ct) > INT_MAX - 256 ? QCNN_ERR_UNSUPPORTED : QCNN_OK;
+}
 
 // (few rows: none) x in fp16, its scales and sums, W's rows on 16 bytes.
 struct Space {
@@ -604,13 +609,15 @@ qcnn_status qcnn_int8_quantize(const void *x, long long ldx, int N, int C, int8_
 }
 
 qcnn_status qcnn_int8_dense_workspace_size(int N, int Cs, int Ct, int x_codes, int aligned, size_t *bytes) {
-    if (!bytes || N < 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
+    const qcnn_status sizes = bytes ? dense_sizes(N, Cs, Ct) : QCNN_ERR_INVALID_ARG;
+    if (sizes != QCNN_OK) return sizes;
     *bytes = N ? carve(N, Cs, Ct, x_codes, !aligned, nullptr).bytes : 0;
     return QCNN_OK;
 }
 
 qcnn_status qcnn_int8_route_info(int N, int Cs, int Ct, int info[4]) {
-    if (!info || N <= 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0) return QCNN_ERR_INVALID_ARG;
+    const qcnn_status sizes = info && N ? dense_sizes(N, Cs, Ct) : QCNN_ERR_INVALID_ARG;
+    if (sizes != QCNN_OK) return sizes;
     const bool few = few_rows(N, Cs, Ct);
     const Int8Plan p = few ? Int8Plan{0, 0, 0} : plan_int8(Ct, N, Cs);
     info[0] = few;
@@ -624,15 +631,15 @@ qcnn_status qcnn_int8_dense_forward(const void *x, long long ldx, const float *x
                                     const int8_t *W, long long ldw, const float *wscale, int Ct, const float *bias,
                                     int act, const void *residual, long long ldr, void *y, long long ldy, int dtype,
                                     void *workspace, size_t workspace_bytes, void *stream) {
-    if (N < 0 || Cs <= 0 || Cs > kInt8MaxTerms || Ct <= 0 || !dtype_ok(dtype) || act < QCNN_ACT_NONE ||
-        act > QCNN_ACT_SILU)
+    const qcnn_status sizes = dense_sizes(N, Cs, Ct);
+    if (sizes == QCNN_ERR_INVALID_ARG || !dtype_ok(dtype) || act < QCNN_ACT_NONE || act > QCNN_ACT_SILU)
         return QCNN_ERR_INVALID_ARG;
     if (!(xscale ? codes_ok(x, ldx, N, Cs) : matrix_ok(x, ldx, N, Cs, dtype)) || !codes_ok(W, ldw, Ct, Cs) ||
         !wscale || !matrix_ok(y, ldy, N, Ct, dtype) || (residual && !matrix_ok(residual, ldr, N, Ct, dtype)) ||
         reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(wscale) % 4 ||
         reinterpret_cast<uintptr_t>(xscale) % 4)
         return QCNN_ERR_INVALID_ARG;
-    if (N == 0) return QCNN_OK;
+    if (sizes != QCNN_OK || N == 0) return sizes;
     const bool w_copy = !rows16(W, ldw);
     const Space s = carve(N, Cs, Ct, xscale != nullptr, w_copy, workspace);
     qcnn_status rc = workspace_ok(workspace, workspace_bytes, s.bytes);
