@@ -299,9 +299,10 @@ __device__ __forceinline__ void scaled16(float (&v)[16], const float *xs, float 
         v[j + 2] = z.x, v[j + 3] = z.y;
     }
 }
-// The same where a scale may be larger: such columns take alpha first.  (In its own place, before the
-// epilogue, which then has scales of one: as a branch of scaled16, whose instructions come many times, 3001 x
-// 2047 -> 5003 took 58.6 us instead of 56.8 without a large scale.)
+// The same where a scale may be larger: such columns take alpha first.  (In a place of its own, before the
+// epilogue, which then has scales of one, or behind a branch around the whole of int8_finish: as a branch of
+// scaled16, whose instructions come many times, 3001 x 2047 -> 5003 took 58.6 us instead of 56.8 without a
+// large scale.)
 __device__ __forceinline__ void scaled16_large(float (&v)[16], const float *xs, float alpha, float bias) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -359,12 +360,14 @@ __device__ __forceinline__ void fetch_values(const GemmEpi &e, int m, int n, int
     }
 }
 // 16 columns of a lane: sums v of row m, columns n to n + count - 1, to the result.  xs: the columns'
-// scales.  A warp's lanes are neighbours in the result; two-byte elements go in pairs where pairs are
-// aligned (gemm_kernel.cuh).  The whole warp calls it.
+// scales; LARGE: some from kLargeScale on.  A warp's lanes are neighbours in the result; two-byte elements go
+// in pairs where pairs are aligned (gemm_kernel.cuh).  The whole warp calls it.
+template <bool LARGE = false>
 __device__ __forceinline__ void int8_finish(const GemmEpi &e, int m, int n, int count, float alpha, float bias,
                                             const float *xs, float (&v)[16]) {
     const bool odd = m & 1;
-    scaled16(v, xs, alpha, bias);
+    if constexpr (LARGE) scaled16_large(v, xs, alpha, bias);
+    else scaled16(v, xs, alpha, bias);
     if (e.add) {
         float r[16];
         fetch_values(e, m, n, count, r);
@@ -400,7 +403,7 @@ template <int CG, bool WIDE>
 __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __grid_constant__ Int8Args g) {
     extern __shared__ __align__(128) unsigned char smem_raw[];
     __shared__ Int8Shared sh;
-    __shared__ __align__(16) float column_scales[8][128], ones[16];
+    __shared__ __align__(16) float column_scales[8][128];
     unsigned char *const smem = smem_raw + (-smem_addr(smem_raw) & 1023u);  // (swizzle atoms)
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -724,8 +727,9 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
                 alpha = 1.f, bias = 0.f;
                 __syncwarp();
             }
-            // (Four chunks at a time; the sums move through their registers: all eight unrolled, the
-            // epilogue's instructions would come eight times, and each move counts too.)
+            // (Four chunks at a time, two by two; the sums move through their registers: all eight unrolled, the
+            // epilogue's instructions would come eight times, and each move counts too.  4096 x 1024 -> 8192 in fp32
+            // with GELU 90.7 us, with four copies 93.8, with one 95.8.)
             if (WIDE && g.staged) {
                 const auto rounds = [&](auto *at) {  // of four chunks
                     constexpr unsigned kBytes = sizeof(*at) * 512;  // of one
@@ -737,10 +741,18 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
                             if (lead) tma_stores_read();
                             __syncwarp();
                         }
+#pragma unroll 1
+                        for (int k = 0; k < 4; k += 2) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (4 * i + k < chunks)
-                                staged16(acc[k], scales + (4 * i + k) * 16, alpha, bias, e.act, e.add, at + k * 512);
+                            for (int q = 0; q < 2; ++q)
+                                if (4 * i + k + q < chunks)
+                                    staged16(acc[q], scales + (4 * i + k + q) * 16, alpha, bias, e.act, e.add,
+                                             at + (k + q) * 512);
+#pragma unroll
+                            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) acc[q][j] = acc[q + 2][j];
+                        }
                         fence_async_smem();
                         __syncwarp();
                         if (lead && mw < g.m)
@@ -793,8 +805,10 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < chunks) chunk(chunk_at(i), acc[i]);
+                for (int i = 0; i < 4; ++i) {
+                    if (i >= chunks) break;
+                    chunk(chunk_at(i), acc[i]);
+                }
             }
         }
         if (WIDE && g.staged) {  // nothing of its own under way when the CTA leaves
@@ -812,13 +826,7 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
                 cluster_sync_all();
                 const Int8Tile t = int8_tile(g, first_unit, share);
                 const int m = t.mt * 128 + quarter * 32 + lane;
-                float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
-                const float w = alpha, b = bias;
-                if (large) {
-                    if (lane < 16) ones[lane] = 1.f;
-                    alpha = 1.f, bias = 0.f;
-                    __syncwarp();
-                }
+                const float alpha = m < g.m ? g.wscale[m] : 0.f, bias = e.bias && m < g.m ? e.bias[m] : 0.f;
 #pragma unroll 1
                 for (int c = share + half * g.cl; c < g.bn / 16; c += 2 * g.cl) {
                     const int n = t.nt * g.bn + c * 16, left = g.n - n;
@@ -843,12 +851,8 @@ __global__ void __launch_bounds__(int8_threads(WIDE), 1) int8_kernel(const __gri
                     float v[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = (float)sum[i];
-                    const float *xs = scales + c * 16;
-                    if (large) {
-                        scaled16_large(v, xs, w, b);
-                        xs = ones;
-                    }
-                    int8_finish(e, m, n, count, alpha, bias, xs, v);
+                    if (large) int8_finish<true>(e, m, n, count, alpha, bias, scales + c * 16, v);
+                    else int8_finish(e, m, n, count, alpha, bias, scales + c * 16, v);
                 }
                 __syncwarp();
                 cluster_sync_all();  // (no CTA leaves while another reads from it)
