@@ -19,7 +19,10 @@ namespace qcnn {
 namespace {
 
 constexpr int kDropoutThreads = 128;
-constexpr unsigned long long kManyVectors = 1u << 19;  // from here on four per thread
+// From here on four per thread.  us, one and four: fp32 2^19 vectors 5.2 and 5.4, 2^20 9.5 and 8.2, 2^21 18.6 and
+// 13.9; bf16 2^19 6.2 and 6.6 (with a residual 6.5 and 8.0), 2^20 10.6 and 11.0 (10.9 and 12.1), 2^21 19.2 and
+// 19.0 (20.0 and 20.7), 2^23 69 and 62 (70 and 66).
+constexpr unsigned long long kManyVectors = 1u << 19;
 
 struct DropoutArgs {
     const void *x, *r;

@@ -1,7 +1,7 @@
 // int8.cu -- qcnn_int8_quantize and qcnn_int8_dense_forward: rows in 8-bit integers with a scale each,
 // and a dense layer of such weights.
 //
-//   scale = max(max |x| / 127, 2^-126), q = rint(x / scale);
+//   scale = max(max |x| (1 / 127), 2^-126), q = rint(x (1 / scale)), each step rounded to fp32;
 //   y = act(xscale[n] wscale[m] sum_k q[n][k] W[m][k] + bias[m]) + r
 #include "int8_gemm.cuh"
 #include "train.cuh"
@@ -26,7 +26,7 @@ __device__ __forceinline__ RowScale row_scale(float top) {
     const float t = __fmul_rn(top, kInv127), s = t < 1.17549435e-38f ? 1.17549435e-38f : t;
     return {s, s <= 3.402823466e38f ? __frcp_rn(s) : 0.f};
 }
-// x / scale to the nearest integers, ties to even: in the low bits of floats around 1.5 2^23.
+// x (1 / scale) to the nearest integers, ties to even: in the low bits of floats around 1.5 2^23.
 // (Products one by one: a packed product and a packed sum, in intrinsics or with .rn in PTX, became one
 // operation that rounds once, and ties of bf16 rows went the other way.)
 constexpr float kRound = 12582912.f;
@@ -464,10 +464,14 @@ __global__ void __launch_bounds__(few_threads(NB), few_ctas(NB)) few_rows_kernel
 int few_block(int N) { return N <= 2 ? N : N <= 4 ? 4 : 8; }  // rows of a kernel, of a CTA
 // Whether that is sooner done than a product on the tensor cores behind a launch that makes the codes:
 // every CTA making them for itself costs more with more of them, and sums of four products, and the
-// joining of each output's, more with more of those.  us, few rows and tensor cores: 1 x 9216 -> 4096 10.5
-// and 11.4, 4 x 9216 -> 4096 13.2 and 16.0, 8 x 4096 -> 1000 7.2 and 9.9, -> 4096 10.4 and 11.5, -> 8192 14.0 and
-// 14.5; 8 x 9216 -> 4096 18.8 and 15.7, -> 9216 27 and 23.  More rows: 64 x 1024 -> 1024 5.1 and 7.2, 30 x 2000
-// -> 2000 7.9 and 9.6, 100 x 1000 -> 1000 7.6 and 8.0; 9 x 4096 -> 4096 12.5 and 11.0, 57 x 78 -> 6139 12.8 and 6.1.
+// joining of each output's, more with more of those.  us from memory, few rows and tensor cores: 1 x 9216 -> 4096
+// 10.9 and 15.3, 4 x 9216 -> 4096 13.4 and 15.5, 8 x 4096 -> 1000 7.3 and 10.4, -> 4096 10.5 and 11.7, -> 8192
+// 14.2 and 14.5; 8 x 9216 -> 4096 17.9 and 15.5, -> 9216 27.4 and 21.8.  More rows: 64 x 1024 -> 1024 5.0 and 8.3,
+// 16 x 2000 -> 2000 8.5 and 9.6, 30 x 2000 -> 2000 10.1 and 9.8, 100 x 1000 -> 1000 7.9 and 9.0; 9 x 4096 -> 4096
+// 12.5 and 11.9, 57 x 78 -> 6139 12.4 and 6.5.  x as codes: 8 x 4096 -> 4096 9.0 and 11.8, 30 x 2000 -> 2000 8.0 and
+// 9.8, 8 x 9216 -> 4096 14.6 and 15.5.  It goes by sizes alone, so that where it holds no workspace is asked for:
+// with W off 16 bytes one row is sooner here (9216 -> 4096 28.8 and 38.1, 4096 -> 1000 6.7 and 14.0), four rows and
+// more are not (4 x 9216 -> 4096 49 and 37, 8 x 4096 -> 4096 36.6 and 22.0, 64 x 1024 -> 1024 11.9 and 10.6).
 bool few_rows(int N, int Cs, int Ct) {
     if ((long long)std::min(N, kFewRows) * Cs > 40960) return false;
     return N <= kFewRows || ((long long)N * Ct <= 1 << 17 && (double)N * Cs * Ct <= 1.2e8);

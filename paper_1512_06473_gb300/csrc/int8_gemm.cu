@@ -2,8 +2,9 @@
 //
 //   y[n][m] = act(xscale[n] (wscale[m] sum_k x[n][k] W[m][k]) + bias[m]) + r
 //
-// GB300's tensor cores multiply fp16 at many times their rate of 8-bit integers, and fp16 holds
-// every code exactly: W is widened on its way, from bytes in shared memory to tensor memory, from where
+// GB300's tcgen05 multiplies no 8-bit integers (kind::i8 does not assemble for sm_103a), and those of mma.sync go
+// at 158 TOP/s (m16n8k32 from registers, measured) where fp16 by tcgen05 has 1,880 TFLOP/s; and fp16 holds every
+// code exactly: W is widened on its way, from bytes in shared memory to tensor memory, from where
 // the MMAs take it as their operand A; x comes widened (fp16, of the pass that quantizes it) as B.  So W
 // is read once, as bytes, and shared memory carries per 128 terms and 128 rows 16 KB of W in and out
 // beside x's tile in and out.
@@ -18,10 +19,10 @@
 // 3000 in tiles of 192 20.0 us, of 256 22.5; 1500 x 9216 -> 4096 94 and 108) are two accumulators, of 64 to
 // 128 columns, that the MMAs of a block of 128 terms fill one after the other, so that draining the first
 // overlaps the MMAs of the second; up to 128 columns take two accumulators in turn.  TMEM: 256 columns of
-// accumulators, four stages of W, 128 terms in 64 columns each.
+// accumulators, four stages of W (three where results are staged), 128 terms in 64 columns each.
 //
-// Bounds.  Large: the MMAs (4096 x 4096 -> 8192 with GELU and a residual in bf16 147 us, 1.87 PFLOP/s, the
-// tensor pipe active for 73%).  Ragged: last rounds and stores of odd rows (3001 x 2047 -> 5003 in fp32 44
+// Bounds.  Large: the MMAs (4096 x 4096 -> 8192 with GELU and a residual in bf16 145 us, 1.9 PFLOP/s, the
+// tensor pipe active for 75%).  Ragged: last rounds and stores of odd rows (3001 x 2047 -> 5003 in fp32 42
 // us).  Tiles of 128 columns of one CTA: what passes through its shared memory for a block of 128 terms, 48 KB in
 // and out, 768 of its 1,000 clocks (128 x 9216 -> 4096 16 us, tensor pipe 16%); narrower ones: the widening.
 //
@@ -75,7 +76,8 @@ struct Int8Shared {
     uint64_t full[kStages], empty[kStages], raw_full[kRawStagesMax], raw_empty[kRawStagesMax], tfull[2], tempty[2], done;
     uint64_t plan_full[2], plan_empty[2];
     uint64_t residual[8];
-    // Of two tiles: whether a sum ends with segment s, a byte each.
+    // Of two tiles: whether a sum ends with segment s.  A byte each: kept as bits of 32-bit words, whose indices
+    // were in range, the kernel faulted from segment 8 on; why was not found.
     uint8_t ends[2][kSegs];
     unsigned tmem;
     int give_up;
@@ -313,9 +315,8 @@ __device__ __forceinline__ void scaled16_large(float (&v)[16], const float *xs, 
 
 // WIDE, where TMA can write the result (and read the residual): a warp's 32 rows of m pass through its
 // part of shared memory, [column][row], by chunks of 16 columns, the residual there before and the result after, each
-// element a lane's own.  Few instructions for an element are what counts: a tile's epilogue is run
-// through once, from an instruction cache that does not hold it (stores from registers, with their
-// addresses and edges, were 235 instructions per 16 columns, and as long as the products of 1024 terms).
+// element a lane's own.  Few instructions for an element, and few copies of them, are what counts: a tile's
+// epilogue is run through once, and is slower the longer its code is (see the copies' times in the kernel).
 constexpr unsigned kStagedBytes = 8192;  // of a warp: 128 columns of bf16, 64 of fp32
 template <typename T>
 __device__ __forceinline__ void staged16(float (&v)[16], const float *xs, float alpha, float bias, int act, bool res,

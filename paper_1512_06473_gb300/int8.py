@@ -21,8 +21,8 @@ _I8 = torch.int8
 
 def int8_quantize(x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None):
     """(codes [N, C] int8, scale [N] float32) of the rows of x [N, C]: scale = the row's largest
-    magnitude / 127, codes the whole numbers nearest to x / scale (qcnn_int8_quantize).  Of dense
-    weights [Ct, Cs] they are what int8_dense_forward takes."""
+    magnitude times 1/127, codes the whole numbers nearest to x times 1/scale, each step rounded to
+    fp32 (qcnn_int8_quantize).  Of dense weights [Ct, Cs] they are what int8_dense_forward takes."""
     code, dev = _first(x, "x")
     ldx = _matrix(x, "x", x.dtype, dev)
     N, C = x.shape
